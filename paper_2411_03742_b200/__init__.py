@@ -7,9 +7,12 @@ library raises.
 from . import workloads  # noqa: F401
 
 
+_LAZY = {"AdaCons": "binding", "AdaConsError": "binding", "load_library": "binding", "Orthogonalizer": "orth"}
+
+
 def __getattr__(name):
-    if name in ("AdaCons", "AdaConsError", "load_library", "binding"):
+    if name in _LAZY or name in _LAZY.values():
         import importlib
-        mod = importlib.import_module(".binding", __name__)
-        return mod if name == "binding" else getattr(mod, name)
+        mod = importlib.import_module("." + _LAZY.get(name, name), __name__)
+        return getattr(mod, name) if name in _LAZY else mod
     raise AttributeError(name)

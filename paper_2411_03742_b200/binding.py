@@ -75,6 +75,12 @@ def load_library() -> ctypes.CDLL:
         "adacons_get_profile": [vp, P(dbl), P(i64), vp],
         "adacons_stats_noalloc": [vp, i32, i64, i32, vp, vp],
         "adacons_version": [],
+        # include/adacons_ops.h
+        "adacons_orth_create": [P(vp), i32, i64, i32, P(i64), P(i64), P(i64), i32, i32, P(dbl), dbl],
+        "adacons_orth_apply": [vp, vp, vp, vp],
+        "adacons_orth_get_status": [vp, P(ctypes.c_uint32), vp],
+        "adacons_orth_get_info": [vp, i32, P(i64)],
+        "adacons_orth_destroy": [vp],
     }
     for name, args in protos.items():
         fn = getattr(lib, name)

@@ -15,9 +15,15 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG_DIR, "libadacons_b200.so")
-SOURCES = ["adacons.cu"]
-DEPS = ["adacons.cu", "adacons_kernels.cuh", "adacons_common.cuh", "adacons_pass1.cuh", "adacons_coeff.cuh",
-        "adacons_pass2.cuh", "adacons_fused.cuh", "adacons_gram.cuh", "adacons_shift.cuh"]
+OBJ_DIR = os.path.join(PKG_DIR, "_build")
+_COMMON = ["csrc/adacons_common.cuh", "include/adacons.h"]
+_OPS = _COMMON + ["csrc/adacons_tc.cuh", "csrc/adacons_host.cuh", "include/adacons_ops.h"]
+# translation units and what each includes
+SOURCES = {
+    "adacons.cu": _COMMON + ["csrc/" + f for f in ("adacons_kernels.cuh", "adacons_pass1.cuh", "adacons_coeff.cuh", "adacons_pass2.cuh",
+                                                   "adacons_fused.cuh", "adacons_gram.cuh", "adacons_shift.cuh")],
+    "adacons_orth.cu": _OPS + ["csrc/adacons_orth.cuh"],
+}
 
 
 def _nvcc() -> str:
@@ -27,31 +33,42 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found (set NVCC or put it on PATH)")
 
 
+def _dep_path(name: str) -> str:
+    return os.path.join(PKG_DIR if name.startswith("csrc/") else ROOT, name)
+
+
+def _newest(source: str) -> float:
+    return max(os.path.getmtime(p) for p in [os.path.join(CSRC, source), os.path.abspath(__file__)] + [_dep_path(n) for n in SOURCES[source]])
+
+
+def _object(source: str) -> str:
+    return os.path.join(OBJ_DIR, source[:-len(".cu")] + ".o")
+
+
 def is_stale() -> bool:
-    if not os.path.exists(LIB_PATH):
-        return True
-    t = os.path.getmtime(LIB_PATH)
-    deps = [os.path.join(CSRC, f) for f in DEPS] + [os.path.join(INCLUDE, "adacons.h"), os.path.abspath(__file__)]
-    return any(os.path.getmtime(p) > t for p in deps)
+    return not os.path.exists(LIB_PATH) or any(_newest(s) > os.path.getmtime(LIB_PATH) for s in SOURCES)
+
+
+def _run(cmds, verbose: bool) -> None:
+    """Run the commands side by side; raise with the output of the first that fails."""
+    procs = [(c, subprocess.Popen(c, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)) for c in cmds]
+    done = [(c, p, p.communicate()[0]) for c, p in procs]
+    for cmd, p, text in done:
+        if p.returncode != 0:
+            raise RuntimeError("nvcc failed:\n" + " ".join(cmd) + "\n" + text)
+        if verbose:
+            sys.stderr.write(text)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not is_stale():
         return LIB_PATH
-    cmd = [
-        _nvcc(), "-shared", "-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-lineinfo",
-        "-gencode", "arch=compute_100a,code=sm_100a",
-        "-I", INCLUDE, "-I", CSRC,
-        "-o", LIB_PATH,
-    ] + [os.path.join(CSRC, s) for s in SOURCES]
-    if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed:\n" + " ".join(cmd) + "\n" + res.stdout + res.stderr)
-    if verbose:
-        sys.stderr.write(res.stderr)
+    os.makedirs(OBJ_DIR, exist_ok=True)
+    arch = ["-gencode", "arch=compute_100a,code=sm_100a"]
+    todo = [s for s in SOURCES if force or not os.path.exists(_object(s)) or _newest(s) > os.path.getmtime(_object(s))]
+    _run([[_nvcc()] + (["-Xptxas", "-v"] if verbose else []) + ["-c", "-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-lineinfo"] + arch +
+          ["-I", INCLUDE, "-I", CSRC, "-o", _object(s), os.path.join(CSRC, s)] for s in todo], verbose)
+    _run([[_nvcc(), "-shared", "-Xcompiler", "-fPIC"] + arch + ["-o", LIB_PATH] + [_object(s) for s in SOURCES]], verbose)
     return LIB_PATH
 
 
