@@ -27,7 +27,7 @@ extern "C" {
  *   dtype    ADACONS_F32 or ADACONS_BF16: storage of the update and of the result.  bf16: products of
  *            fp16 operands with the iterate held in 22 bits; the result is within about one bf16
  *            rounding.  fp32: operands as pairs of fp16 values, about 1e-6 of the result's norm.
- *   rows, cols, offsets  host arrays; matrices must not overlap and must lie inside [0, d); sides up to 2^24.
+ *   rows, cols, offsets  host arrays; matrices must not overlap and must lie inside [0, d); sides up to 2^18.
  *            Elements outside the matrices (biases, gains) are neither read nor written.
  *   scaling  0: none; 1: each matrix's result times sqrt(max(1, rows / cols)).
  *   coeffs   host array of 3 * steps values a, b, c (one triple per step), 1 <= steps <= 64.  Iterates
@@ -36,7 +36,7 @@ extern "C" {
  *            that matrix only.
  * adacons_orth_create allocates about 8 bytes per element of the matrices and 4 (bf16) or 8 (fp32) per
  * element of their short sides squared.
- * Errors: EINVAL, ELIMIT (a side beyond 2^24), ENOMEM, ECUDA, EARCH.
+ * Errors: EINVAL, ELIMIT (a side beyond 2^18), ENOMEM, ECUDA, EARCH.
  */
 typedef struct adacons_orth adacons_orth;
 
@@ -45,7 +45,7 @@ int adacons_orth_create(adacons_orth **out, int dtype, int64_t d, int num_matric
                         const double *coeffs, double eps);
 
 /* One pass over the vector.  update and out may be the same buffer; any element alignment is served
- * (8 / 16 bytes for bf16 / fp32 let the result be written in vectors).  A context holds the iterates:
+ * (16-byte aligned buffers, offsets and rows that are multiples of 8 elements let the result be written in vectors).  A context holds the iterates:
  * calls on one context must be ordered (one stream, or events).  Errors: EINVAL, ECUDA. */
 int adacons_orth_apply(adacons_orth *ctx, const void *update, void *out, void *cuda_stream);
 

@@ -22,18 +22,21 @@ struct adacons_orth {
   size_t bytes = 0;
   const OrthMat* mats = nullptr;
   const CUtensorMap* maps = nullptr;
-  const OrthTile *sym_tiles = nullptr, *full_tiles = nullptr, *load_tiles = nullptr;
+  const OrthTile* load_tiles = nullptr;
+  const OrthTile* tiles[3] = {};      // by OrthKind
+  int num_tiles[3] = {}, cg[3] = {};
   const OrthChunk* chunks = nullptr;
   double* partial = nullptr;
   uint32_t* flags = nullptr;
-  int num_sym = 0, num_full = 0, num_load = 0, num_chunks = 0;
-  int sym_tn = 256, full_tn = 256;
+  int num_load = 0, num_chunks = 0;
   int64_t launches = 0;
 };
 
 namespace {
 
-constexpr int64_t kMaxSide = 1 << 24;
+// A side is the K of a product; the tensor cores' rounding toward zero makes a sum over it low by up to
+// 4e-8 per 16 elements, 6.5e-4 at this limit: below the rounding of the fp16 operands.
+constexpr int64_t kMaxSide = 1 << 18;
 
 struct Arena {                        // offsets first, pointers once the allocation exists
   size_t used = 0;
@@ -44,39 +47,57 @@ struct Arena {                        // offsets first, pointers once the alloca
   }
 };
 
-// Tile width of a product: the wide tile halves the operand traffic per product, the narrow one gives
-// small problems enough tiles to occupy the device.
-int pick_tn(const std::vector<OrthMat>& mats, bool full, int sms) {
-  int64_t tiles = 0;
-  for (const OrthMat& m : mats) {
-    const int64_t ti = (m.r + kOrthTM - 1) / kOrthTM;
-    tiles += full ? ti * ((m.l + 255) / 256) : (ti * ((m.r + 255) / 256) + 1) / 2;
+// The tiles of one product for a tiling with CG blocks per tile, longest first, as the persistent
+// blocks (or pairs) take them in turn, and the modelled time of the busiest one in cycles.  The model:
+// a stage's products take 64 (128) cycles per 16 K elements and fp16 pass, a lone block about 1.3 times that (its operand
+// traffic from L2 per product is twice a pair's), an epilogue overlaps with the next tile's products.
+double plan_tiles(const std::vector<OrthMat>& mats, int kind, bool split, int cg, int sms, std::vector<OrthTile>* tiles) {
+  const int tm = 128 * cg, tn = split ? 128 : 128 * cg;
+  tiles->clear();
+  std::vector<int> order(mats.size());
+  for (size_t k = 0; k < mats.size(); ++k) order[k] = static_cast<int>(k);
+  auto depth = [&](int k) { return kind == kOrthGram ? mats[k].l : mats[k].r; };
+  std::sort(order.begin(), order.end(), [&](int x, int y) { return depth(x) != depth(y) ? depth(x) > depth(y) : x < y; });
+  const int workers = sms / cg;
+  std::vector<double> busy(workers, 0.0);
+  for (int k : order) {
+    const int cols = kind == kOrthApply ? mats[k].l : mats[k].r;
+    const double stages = (depth(k) + kOrthTK - 1) / kOrthTK;
+    const double products = stages * 4 * (tn / 2) * (split ? 3 : 1) * (cg == 1 ? 1.3 : 1.0);
+    const double cost = std::max(products, 16.0 * tn) + 500.0;
+    for (int64_t j = 0; j * tn < cols; ++j)
+      for (int64_t i = 0; i * tm < mats[k].r; ++i) {
+        if (kind != kOrthApply && i * tm + tm - 1 < j * tn) continue;
+        busy[tiles->size() % workers] += cost;
+        tiles->push_back({k, static_cast<int>(i), static_cast<int>(j), 0});
+      }
   }
-  return tiles >= 2 * sms ? 256 : 128;
+  return *std::max_element(busy.begin(), busy.end()) + 16.0 * tn;
 }
 
-template <int KIND, bool SPLIT, int TN>
+template <int KIND, bool SPLIT, int CG>
 bool launch_product(const adacons_orth* c, const OrthParams& p, cudaStream_t st) {
-  const size_t smem = OrthSmem<TN>::kBytes + 1024;
-  static_assert(OrthSmem<TN>::kBytes + 1024 <= 227 * 1024, "shared memory of a block");
-  auto* kernel = &orth_product_kernel<KIND, SPLIT, TN>;
-  return launch(kernel, dim3(std::min(p.num_tiles, c->dev.sms)), dim3(kOrthThreads), smem, st, true, p);
+  static_assert(OrthTiling<SPLIT, CG>::kBytes <= 227 * 1024, "shared memory of a block");
+  const int blocks = std::min(p.num_tiles, c->dev.sms / CG) * CG;
+  return launch(&orth_product_kernel<KIND, SPLIT, CG>, dim3(blocks), dim3(kOrthThreads), OrthTiling<SPLIT, CG>::kBytes, st, true, CG, p);
 }
 
 template <int KIND>
-bool launch_kind(const adacons_orth* c, const OrthParams& p, int tn, cudaStream_t st) {
-  if (c->dtype == ADACONS_F32) return tn == 256 ? launch_product<KIND, true, 256>(c, p, st) : launch_product<KIND, true, 128>(c, p, st);
-  return tn == 256 ? launch_product<KIND, false, 256>(c, p, st) : launch_product<KIND, false, 128>(c, p, st);
+bool launch_kind(const adacons_orth* c, OrthParams p, cudaStream_t st) {
+  p.tiles = c->tiles[KIND];
+  p.num_tiles = c->num_tiles[KIND];
+  if (c->dtype == ADACONS_F32) return c->cg[KIND] == 2 ? launch_product<KIND, true, 2>(c, p, st) : launch_product<KIND, true, 1>(c, p, st);
+  return c->cg[KIND] == 2 ? launch_product<KIND, false, 2>(c, p, st) : launch_product<KIND, false, 1>(c, p, st);
 }
 
-template <int KIND, bool SPLIT, int TN>
+template <int KIND, bool SPLIT, int CG>
 bool raise_smem() {
-  if (cudaFuncSetAttribute(orth_product_kernel<KIND, SPLIT, TN>, cudaFuncAttributeMaxDynamicSharedMemorySize, OrthSmem<TN>::kBytes + 1024) == cudaSuccess) return true;
+  if (cudaFuncSetAttribute(orth_product_kernel<KIND, SPLIT, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, OrthTiling<SPLIT, CG>::kBytes) == cudaSuccess) return true;
   cudaGetLastError();
   return false;
 }
 template <int KIND>
-bool raise_smem_kind() { return raise_smem<KIND, false, 256>() && raise_smem<KIND, false, 128>() && raise_smem<KIND, true, 256>() && raise_smem<KIND, true, 128>(); }
+bool raise_smem_kind() { return raise_smem<KIND, false, 1>() && raise_smem<KIND, false, 2>() && raise_smem<KIND, true, 1>() && raise_smem<KIND, true, 2>(); }
 
 int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* rows, const int64_t* cols, const int64_t* offsets, int scaling,
            int steps, const double* coeffs, double eps) {
@@ -109,7 +130,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
 
   std::vector<OrthMat> mats(num);
   std::vector<OrthChunk> chunks;
-  std::vector<OrthTile> load, sym, full;
+  std::vector<OrthTile> load, lists[3];
   for (int k = 0; k < num; ++k) {
     OrthMat& m = mats[k];
     std::memset(&m, 0, sizeof(m));
@@ -119,7 +140,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
     m.ldx = (m.l + 7) / 8 * 8;
     m.lds = (m.r + 7) / 8 * 8;
     m.offset = offsets[k];
-    m.vec_out = m.l % 4 == 0 && offsets[k] % 4 == 0;
+    m.vec_out = m.l % 8 == 0 && offsets[k] % 8 == 0;
     m.scale = scaling ? static_cast<float>(std::sqrt(std::max(1.0, static_cast<double>(rows[k]) / static_cast<double>(cols[k])))) : 1.f;
     m.norm_first = static_cast<int>(chunks.size());
     m.norm_count = static_cast<int>((rows[k] * cols[k] + kOrthNormChunk - 1) / kOrthNormChunk);
@@ -127,37 +148,23 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
     for (int i = 0; i < (m.r + kOrthLoadTile - 1) / kOrthLoadTile; ++i)
       for (int j = 0; j < (m.l + kOrthLoadTile - 1) / kOrthLoadTile; ++j) load.push_back({k, i, j, 0});
   }
-  c->sym_tn = pick_tn(mats, false, dev.sms);
-  c->full_tn = pick_tn(mats, true, dev.sms);
-  // longest products first: a tile's cost goes with r (Poly, Apply) and l (Gram)
-  std::vector<int> order(num);
-  for (int k = 0; k < num; ++k) order[k] = k;
-  std::sort(order.begin(), order.end(), [&](int x, int y) {
-    return mats[x].l != mats[y].l ? mats[x].l > mats[y].l : mats[x].r != mats[y].r ? mats[x].r > mats[y].r : x < y;
-  });
-  for (int k : order) {
-    const OrthMat& m = mats[k];
-    for (int j = 0; j * c->sym_tn < m.r; ++j)
-      for (int i = 0; i * kOrthTM < m.r; ++i)
-        if (i * kOrthTM + kOrthTM - 1 >= j * c->sym_tn) sym.push_back({k, i, j, 0});
+  for (int kind = 0; kind < 3; ++kind) {
+    std::vector<OrthTile> one, two;
+    const double t1 = plan_tiles(mats, kind, split, 1, dev.sms, &one), t2 = plan_tiles(mats, kind, split, 2, dev.sms, &two);
+    c->cg[kind] = t2 < t1 ? 2 : 1;
+    lists[kind] = t2 < t1 ? two : one;
+    c->num_tiles[kind] = static_cast<int>(lists[kind].size());
   }
-  std::sort(order.begin(), order.end(), [&](int x, int y) {
-    return mats[x].r != mats[y].r ? mats[x].r > mats[y].r : x < y;
-  });
-  for (int k : order)
-    for (int j = 0; static_cast<int64_t>(j) * c->full_tn < mats[k].l; ++j)
-      for (int i = 0; i * kOrthTM < mats[k].r; ++i) full.push_back({k, i, j, 0});
   c->num_chunks = static_cast<int>(chunks.size());
   c->num_load = static_cast<int>(load.size());
-  c->num_sym = static_cast<int>(sym.size());
-  c->num_full = static_cast<int>(full.size());
 
   Arena a;
   const size_t at_mats = a.take(num * sizeof(OrthMat)), at_maps = a.take(static_cast<size_t>(num) * kMapCount * sizeof(CUtensorMap));
-  const size_t at_sym = a.take(sym.size() * sizeof(OrthTile)), at_full = a.take(full.size() * sizeof(OrthTile));
+  size_t at_tiles[3];
+  for (int kind = 0; kind < 3; ++kind) at_tiles[kind] = a.take(lists[kind].size() * sizeof(OrthTile));
   const size_t at_load = a.take(load.size() * sizeof(OrthTile)), at_chunks = a.take(chunks.size() * sizeof(OrthChunk));
   const size_t at_partial = a.take(chunks.size() * sizeof(double)), at_flags = a.take(sizeof(uint32_t));
-  const size_t lists = a.used;
+  const size_t head = a.used;
   std::vector<size_t> at(static_cast<size_t>(num) * kMapCount, 0);
   for (int k = 0; k < num; ++k)
     for (int q = 0; q < kMapCount; ++q) {
@@ -167,7 +174,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
     }
   c->bytes = a.used;
   if (cudaMalloc(&c->memory, c->bytes) != cudaSuccess) { cudaGetLastError(); delete c; return ADACONS_ENOMEM; }
-  std::vector<unsigned char> host(lists, 0);
+  std::vector<unsigned char> host(head, 0);
   std::vector<CUtensorMap> maps(static_cast<size_t>(num) * kMapCount);
   for (int k = 0; k < num; ++k) {
     OrthMat& m = mats[k];
@@ -189,13 +196,15 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   }
   std::memcpy(host.data() + at_mats, mats.data(), num * sizeof(OrthMat));
   std::memcpy(host.data() + at_maps, maps.data(), maps.size() * sizeof(CUtensorMap));
-  std::memcpy(host.data() + at_sym, sym.data(), sym.size() * sizeof(OrthTile));
-  std::memcpy(host.data() + at_full, full.data(), full.size() * sizeof(OrthTile));
+  for (int kind = 0; kind < 3; ++kind) {
+    std::memcpy(host.data() + at_tiles[kind], lists[kind].data(), lists[kind].size() * sizeof(OrthTile));
+    c->tiles[kind] = reinterpret_cast<const OrthTile*>(c->memory + at_tiles[kind]);
+  }
   std::memcpy(host.data() + at_load, load.data(), load.size() * sizeof(OrthTile));
   std::memcpy(host.data() + at_chunks, chunks.data(), chunks.size() * sizeof(OrthChunk));
   // the padding of the iterates is read by the epilogues (never by a product): zero it once
-  if (cudaMemset(c->memory + lists, 0, c->bytes - lists) != cudaSuccess ||
-      cudaMemcpy(c->memory, host.data(), lists, cudaMemcpyHostToDevice) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
+  if (cudaMemset(c->memory + head, 0, c->bytes - head) != cudaSuccess ||
+      cudaMemcpy(c->memory, host.data(), head, cudaMemcpyHostToDevice) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
     cudaGetLastError();
     cudaFree(c->memory);
     delete c;
@@ -203,8 +212,6 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   }
   c->mats = reinterpret_cast<const OrthMat*>(c->memory + at_mats);
   c->maps = reinterpret_cast<const CUtensorMap*>(c->memory + at_maps);
-  c->sym_tiles = reinterpret_cast<const OrthTile*>(c->memory + at_sym);
-  c->full_tiles = reinterpret_cast<const OrthTile*>(c->memory + at_full);
   c->load_tiles = reinterpret_cast<const OrthTile*>(c->memory + at_load);
   c->chunks = reinterpret_cast<const OrthChunk*>(c->memory + at_chunks);
   c->partial = reinterpret_cast<double*>(c->memory + at_partial);
@@ -239,19 +246,18 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   bool ok;
   if (c->dtype == ADACONS_F32) {
-    ok = launch(&orth_norm_kernel<0>, dim3(c->num_chunks), dim3(256), 0, st, false, update, c->mats, c->chunks, c->partial) &&
-         launch(&orth_load_kernel<0>, dim3(c->num_load), dim3(256), 0, st, true, update, c->mats, c->load_tiles, static_cast<const double*>(c->partial), c->eps);
+    ok = launch(&orth_norm_kernel<0>, dim3(c->num_chunks), dim3(256), 0, st, false, 1, update, c->mats, c->chunks, c->partial) &&
+         launch(&orth_load_kernel<0>, dim3(c->num_load), dim3(256), 0, st, true, 1, update, c->mats, c->load_tiles, static_cast<const double*>(c->partial), c->eps);
   } else {
-    ok = launch(&orth_norm_kernel<1>, dim3(c->num_chunks), dim3(256), 0, st, false, update, c->mats, c->chunks, c->partial) &&
-         launch(&orth_load_kernel<1>, dim3(c->num_load), dim3(256), 0, st, true, update, c->mats, c->load_tiles, static_cast<const double*>(c->partial), c->eps);
+    ok = launch(&orth_norm_kernel<1>, dim3(c->num_chunks), dim3(256), 0, st, false, 1, update, c->mats, c->chunks, c->partial) &&
+         launch(&orth_load_kernel<1>, dim3(c->num_load), dim3(256), 0, st, true, 1, update, c->mats, c->load_tiles, static_cast<const double*>(c->partial), c->eps);
   }
   OrthParams p = {};
   p.mats = c->mats;
   p.maps = c->maps;
   p.flags = c->flags;
   p.out = out;
-  p.out_bf16 = c->dtype == ADACONS_BF16;
-  p.out_aligned = reinterpret_cast<uintptr_t>(out) % (4 * elem) == 0;
+  p.out_aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0;
   for (int s = 0; ok && s < c->steps; ++s) {
     const double* k = &c->coeffs[3 * s];
     p.src = s & 1;
@@ -260,12 +266,7 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
     p.c = static_cast<float>(k[2]);
     p.t = s >= 3 ? static_cast<float>(-0.75 * (k[1] + k[2])) : 0.f;
     p.last = s == c->steps - 1;
-    p.tiles = c->sym_tiles;
-    p.num_tiles = c->num_sym;
-    ok = launch_kind<kOrthGram>(c, p, c->sym_tn, st) && launch_kind<kOrthPoly>(c, p, c->sym_tn, st);
-    p.tiles = c->full_tiles;
-    p.num_tiles = c->num_full;
-    ok = ok && launch_kind<kOrthApply>(c, p, c->full_tn, st);
+    ok = launch_kind<kOrthGram>(c, p, st) && launch_kind<kOrthPoly>(c, p, st) && launch_kind<kOrthApply>(c, p, st);
   }
   c->launches = 2 + 3 * c->steps;
   return ok ? ADACONS_OK : ADACONS_ECUDA;

@@ -19,7 +19,10 @@ namespace adacons {
 // pair hi + lo of fp16 values of 2^11 X (22 bits, range 2^-25 .. 2^16 after the power-of-two scale),
 // S and B as 2^13 S and 2^11 B.  In a bf16 context the products take the hi parts only, and the term
 // a X takes the pair; in an fp32 context S and B are pairs too and each product is the sum
-// lo hi + hi lo + hi hi, smallest terms first, in one fp32 accumulator.
+// (lo hi + hi lo) + hi hi.  The tensor cores round a running sum toward zero, low by up to 4e-8 of it
+// per chained product: harmless beside an 11-bit operand, but 4e-5 of an fp32 result after five steps
+// on sides of 1024.  There the hi hi terms are chained over 256 K elements at most and the chunks'
+// sums added by the epilogue, round to nearest (the small terms, 2^-11 of the sum, in one accumulator).
 // Why not bf16 operands: rounding the iterates to 8 bits costs 1e-2 of the result's norm on a
 // Gaussian matrix and 1e-1 on one with a few strong directions (the small singular values grow
 // 3.4-fold per step and the rounding noise of the strong ones grows with them); 11 bits with the
@@ -29,10 +32,10 @@ namespace adacons {
 // place of a, an identity in exact arithmetic; it brings the error from 1.7e-3 to 1.1e-3 on Gaussian
 // matrices (on a matrix of rank 8 plus noise 5e-4 instead of 1.5e-4, still a third of the rounding).
 // ----------------------------------------------------------------------------------------------
-constexpr int kOrthTM = 128;             // rows of an output tile
 constexpr int kOrthTK = 64;              // K elements per stage: one 128-byte swizzled row
+constexpr int kOrthChunk = 4;            // fp32 contexts: stages (256 K elements) per hi hi accumulator
 constexpr float kOrthXScale = 2048.f, kOrthSScale = 8192.f, kOrthBScale = 2048.f;
-constexpr int kOrthThreads = 192;        // warps 0-3 epilogue, 4 TMA, 5 MMA
+constexpr int kOrthThreads = 352;        // warps 0-7 epilogue, 8 operand copies, 9 products, 10 epilogue copies
 constexpr int kOrthNormChunk = 16384;    // elements per block of the norm kernel
 constexpr int kOrthLoadTile = 64;
 
@@ -43,7 +46,7 @@ struct OrthMat {
   int r, l;                // X is r x l, r <= l
   int transposed;          // the matrix in the vector has l rows of r elements
   int ldx, lds;            // row pitch of X and of S, B (elements)
-  int vec_out;             // output rows start on 8- (bf16) or 16-byte (fp32) boundaries relative to the vector's start
+  int vec_out;             // rows of the result are whole groups of 8 elements, aligned relative to the vector's start
   int norm_first, norm_count;
   float scale;
   long long offset;        // of the matrix in the vector
@@ -62,7 +65,7 @@ struct OrthParams {
   int src;                       // buffer of X that is read
   float a, b, c, t;              // t: what is added to B's diagonal
   void* out;                     // last step: the flat result
-  int last, out_bf16, out_aligned;
+  int last, out_aligned;
   uint32_t* flags;
 };
 
@@ -152,272 +155,475 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, const Or
 
 // ----------------------------------------------------------------------------------------------
 // The three products of a step, all matrices of the vector in one persistent launch.
-// Output tiles of 128 x TN; one warp copies operand stages (128 + TN rows of 64 K elements) by TMA,
-// one thread issues the tcgen05 products into one of two TMEM accumulators, four warps drain the
-// other.  S and S S are symmetric: only tiles that reach the lower triangle are computed, and each
-// writes its mirror image where no tile does.
 //   Gram   S = X X^T        both operands K-major, straight from X's rows
 //   Poly   B = b S + c S S + t I
 //   Apply  X' = (a - t) X + B X    the right operand is X again, MN-major: no transposed copy exists
-// The epilogue turns each 32 x 32 block of the accumulator in shared memory so that global reads and
-// writes run along rows; mirror images and transposed results are written from the accumulator's own
-// orientation, where the lanes of a warp are neighbours.
+// S and S S are symmetric: only tiles that reach the lower triangle are computed, and each writes its
+// mirror image where no tile does.
+//
+// Tiles.  CG = 2: a pair of blocks (two SMs) shares a tile of 256 x TN; each holds 128 rows of the left
+// operand, half of the right one and 128 rows of the result, so that an operand byte from L2 feeds
+// twice the products of a single block's tile.  CG = 1: 128 x 128, for problems with too few tiles to occupy the device.
+// In each block one warp copies operand stages by TMA, one thread (of the even block) issues the
+// tcgen05 products into one of two TMEM accumulators, and eight warps drain the other.
+//
+// The epilogue works on strips of 128 rows x 64 columns in shared memory: a further warp brings what is
+// added (X, S) by TMA two or three strips ahead, the eight warps put the result in its place, and the
+// strip leaves by TMA, which also clips the matrix's edges.  With plain loads and stores of 8 bytes a
+// lane instead, the epilogue of a 256 x 256 tile took 25,000 cycles where its products take 8,000 (K = 1024).
+// Mirror images and transposed results are written from the accumulator's own orientation, where
+// the lanes of a warp are neighbours in memory.
 // ----------------------------------------------------------------------------------------------
-template <int TN> struct OrthSmem {
-  static constexpr uint32_t kA = kOrthTM * kOrthTK * 2, kB = TN * kOrthTK * 2, kStage = kA + kB;
-  static constexpr int kStages = TN == 256 ? 4 : 6;
-  static constexpr uint32_t kTurn = kStages * kStage;                // 4 warps x 32 x 32 fp32
-  static constexpr uint32_t kBars = kTurn + 4 * 4096;
-  static constexpr uint32_t kBytes = kBars + 256;
+constexpr uint32_t kOrthStripPart = 128 * 128;   // 128 rows x 64 fp16 values: two boxes of 64 swizzled rows
+template <bool SPLIT, int CG> struct OrthTiling {
+  static constexpr int kTM = 128 * CG, kTN = SPLIT ? 128 : 128 * CG;
+  static constexpr int kParts = SPLIT ? 2 : 1;
+  static constexpr int kBRows = kTN / CG;                            // of the right operand, in each block
+  static constexpr uint32_t kA = 128 * kOrthTK * 2, kB = kBRows * kOrthTK * 2;
+  static constexpr uint32_t kStage = kParts * (kA + kB);             // A hi (lo), B hi (lo)
+  static constexpr int kRing = SPLIT ? 2 : 3;                        // strips
+  static constexpr int kStages = (224 * 1024 - kRing * 2 * kOrthStripPart) / kStage;
+  static constexpr uint32_t kStrips = kStages * kStage;
+  static constexpr uint32_t kBars = kStrips + kRing * 2 * kOrthStripPart;
+  static constexpr uint32_t kBytes = kBars + 256 + 1024;             // + alignment of the base
+  static constexpr int kBlocks = kTN / 64;                           // strips of a tile
+  static constexpr uint32_t kTmemCols = SPLIT ? 512 : 2 * kTN;       // big[2] (small[2])
 };
 
-template <int KIND, bool SPLIT, int TN>
-__device__ __forceinline__ void orth_epilogue_tile(const OrthParams& p, const OrthTile t, uint32_t tmem, float* turn, uint64_t* drained) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const OrthMat& m = p.mats[t.mat];
-  const int r = m.r, ncols = KIND == kOrthApply ? m.l : m.r, ld = KIND == kOrthApply ? m.ldx : m.lds;
-  const int row0 = t.i * kOrthTM + warp * 32;
-  const int q = lane & 7, sub = lane >> 3;
-  const __half* add_hi = KIND == kOrthApply ? m.x[p.src][0] : m.s[0];
-  const __half* add_lo = KIND == kOrthApply ? m.x[p.src][1] : m.s[1];
-  __half* dst_hi = KIND == kOrthGram ? m.s[0] : KIND == kOrthPoly ? m.b[0] : m.x[p.src ^ 1][0];
-  __half* dst_lo = KIND == kOrthGram ? m.s[1] : KIND == kOrthPoly ? m.b[1] : m.x[p.src ^ 1][1];
+// What of a tile exists: strips with columns inside the matrix, none for a block without rows.
+template <int KIND, bool SPLIT, int CG>
+__device__ __forceinline__ int orth_live_strips(const OrthMat& m, const OrthTile& t, int rank) {
+  using T = OrthTiling<SPLIT, CG>;
+  if (t.i * T::kTM + rank * 128 >= m.r) return 0;
+  const int left = ((KIND == kOrthApply ? m.l : m.r) - t.j * T::kTN + 63) / 64;
+  return left < T::kBlocks ? left : T::kBlocks;
+}
+
+__device__ __forceinline__ void orth_unpack8(const uint4& v, float (&f)[8]) {
+  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&u[k]));
+    f[2 * k] = p.x;
+    f[2 * k + 1] = p.y;
+  }
+}
+__device__ __forceinline__ uint32_t orth_pack2(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// One 32 x 32 block of the product: row0 + lane is this thread's row, acc its 32 columns from col0 on.
+// hi / lo: the block's place in the strip, `half` selecting its 64 bytes of each 128-byte row.
+template <int KIND, bool SPLIT, int CG>
+__device__ __forceinline__ void orth_finish_block(const OrthParams& p, const OrthMat& m, int row0, int col0, const uint32_t (&acc)[32],
+                                                  unsigned char* hi, unsigned char* lo, int half) {
+  using T = OrthTiling<SPLIT, CG>;
+  const int lane = threadIdx.x & 31;
+  const int r = m.r, ncols = KIND == kOrthApply ? m.l : m.r, row = row0 + lane;
   const bool last = KIND == kOrthApply && p.last;
-  constexpr bool kAddLo = KIND == kOrthApply || SPLIT;      // X is always a pair, S only in an fp32 context
-  constexpr bool kStoreLo = KIND == kOrthApply || SPLIT;
-#pragma unroll 1
-  for (int ch = 0; ch < TN / 32; ++ch) {
-    const int col0 = t.j * TN + ch * 32;
-    const bool live = col0 < ncols && row0 < r;
-    uint2 ah[8], al[8];
-    if (KIND != kOrthGram && live) {
+  constexpr bool kPair = KIND == kOrthApply || SPLIT;      // X is always a pair, S and B only in an fp32 context
+  // where no tile above the diagonal is computed, its image comes from here
+  const bool mirror = KIND != kOrthApply && !((col0 / T::kTM) * T::kTM + T::kTM - 1 >= (row0 / T::kTN) * T::kTN);
+  const bool turned = last && m.transposed;
+  __half* dst_hi = KIND == kOrthGram ? m.s[0] : m.b[0];
+  __half* dst_lo = KIND == kOrthGram ? m.s[1] : m.b[1];
+  unsigned char* hrow = hi + lane * 128;
+  unsigned char* lrow = lo + lane * 128;
 #pragma unroll
-      for (int it = 0; it < 8; ++it) {
-        const int row = row0 + it * 4 + sub, col = col0 + q * 4;
-        ah[it] = al[it] = make_uint2(0u, 0u);
-        if (row < r && col < ld) {
-          const long long at = static_cast<long long>(row) * ld + col;
-          ah[it] = *reinterpret_cast<const uint2*>(add_hi + at);
-          if (kAddLo) al[it] = *reinterpret_cast<const uint2*>(add_lo + at);
-        }
+  for (int g = 0; g < 4; ++g) {
+    const int at = ((4 * half + g) ^ (lane & 7)) * 16;
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(acc[8 * g + e]);
+    if constexpr (KIND == kOrthGram) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= kOrthSScale / (kOrthXScale * kOrthXScale);
+    } else {
+      float x[8];
+      orth_unpack8(*reinterpret_cast<const uint4*>(hrow + at), x);
+      if (kPair) {
+        float y[8];
+        orth_unpack8(*reinterpret_cast<const uint4*>(lrow + at), y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += y[e];
+      }
+      const float by_x = KIND == kOrthPoly ? p.b * (kOrthBScale / kOrthSScale) : p.a - p.t;
+      const float by_v = KIND == kOrthPoly ? p.c * (kOrthBScale / (kOrthSScale * kOrthSScale)) : 1.f / kOrthBScale;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = by_x * x[e] + by_v * v[e];
+      if (KIND == kOrthPoly && row0 == col0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (8 * g + e == lane) v[e] += p.t * kOrthBScale;
       }
     }
-    uint32_t acc[32];
-    tmem_ld32(tmem + ch * 32 + (static_cast<uint32_t>(warp * 32) << 16), acc);
-    tmem_wait_ld();
-    if (ch == TN / 32 - 1) {                     // the accumulator is free for the tile after next
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_one(drained);
-    }
-    if (!live) continue;
+    if (!last) {
+      uint32_t h[4], l[4];
 #pragma unroll
-    for (int g = 0; g < 8; ++g)
-      *reinterpret_cast<uint4*>(turn + lane * 32 + ((g ^ (lane & 7)) * 4)) = make_uint4(acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]);
-    __syncwarp();
-    // a tile above the diagonal that is not computed gets its mirror image from here
-    const bool mirror = KIND != kOrthApply && !((col0 / kOrthTM) * kOrthTM + kOrthTM - 1 >= (row0 / TN) * TN);
-    const bool keep = mirror || (last && m.transposed);
-#pragma unroll
-    for (int it = 0; it < 8; ++it) {
-      const int lrow = it * 4 + sub, row = row0 + lrow, col = col0 + q * 4;
-      float* cell = turn + lrow * 32 + ((q ^ (lrow & 7)) * 4);
-      const float4 v4 = *reinterpret_cast<const float4*>(cell);
-      float v[4] = {v4.x, v4.y, v4.z, v4.w};
-      float add[4] = {0.f, 0.f, 0.f, 0.f};
-      if (KIND != kOrthGram) {
-        const float2 h0 = __half22float2(*reinterpret_cast<const __half2*>(&ah[it].x)), h1 = __half22float2(*reinterpret_cast<const __half2*>(&ah[it].y));
-        add[0] = h0.x; add[1] = h0.y; add[2] = h1.x; add[3] = h1.y;
-        if (kAddLo) {
-          const float2 l0 = __half22float2(*reinterpret_cast<const __half2*>(&al[it].x)), l1 = __half22float2(*reinterpret_cast<const __half2*>(&al[it].y));
-          add[0] += l0.x; add[1] += l0.y; add[2] += l1.x; add[3] += l1.y;
+      for (int k = 0; k < 4; ++k) {
+        h[k] = orth_pack2(v[2 * k], v[2 * k + 1]);
+        if (kPair) {
+          const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&h[k]));
+          l[k] = orth_pack2(v[2 * k] - b.x, v[2 * k + 1] - b.y);
         }
       }
+      *reinterpret_cast<uint4*>(hrow + at) = make_uint4(h[0], h[1], h[2], h[3]);
+      if (kPair) *reinterpret_cast<uint4*>(lrow + at) = make_uint4(l[0], l[1], l[2], l[3]);
+      if (mirror) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (KIND == kOrthGram) v[e] *= kOrthSScale / (kOrthXScale * kOrthXScale);
-        if (KIND == kOrthPoly) {
-          v[e] = (p.c * (kOrthBScale / (kOrthSScale * kOrthSScale))) * v[e] + (p.b * (kOrthBScale / kOrthSScale)) * add[e];
-          if (row == col + e) v[e] += p.t * kOrthBScale;
-        }
-        if (KIND == kOrthApply) v[e] = (p.a - p.t) * add[e] + v[e] * (1.f / kOrthBScale);
-        if (last) v[e] *= m.scale / kOrthXScale;
-      }
-      if (keep) *reinterpret_cast<float4*>(cell) = make_float4(v[0], v[1], v[2], v[3]);
-      if (row >= r || col >= ncols) continue;
-      if (!last) {
-        const long long at = static_cast<long long>(row) * ld + col;
-        __half h[4], l[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) orth_split(v[e], h[e], l[e]);
-        *reinterpret_cast<uint2*>(dst_hi + at) = *reinterpret_cast<const uint2*>(h);
-        if (kStoreLo) *reinterpret_cast<uint2*>(dst_lo + at) = *reinterpret_cast<const uint2*>(l);
-      } else if (!m.transposed) {
-        const long long at = m.offset + static_cast<long long>(row) * m.l + col;
-        if (m.vec_out && p.out_aligned && col + 3 < ncols) {
-          if (p.out_bf16) *reinterpret_cast<uint2*>(static_cast<unsigned short*>(p.out) + at) = make_uint2(pack_bf16x2_rn(v[0], v[1]), pack_bf16x2_rn(v[2], v[3]));
-          else *reinterpret_cast<float4*>(static_cast<float*>(p.out) + at) = make_float4(v[0], v[1], v[2], v[3]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (col + e < ncols) {
-              if (p.out_bf16) static_cast<unsigned short*>(p.out)[at + e] = static_cast<unsigned short>(pack_bf16x2_rn(v[e], 0.f) & 0xffffu);
-              else static_cast<float*>(p.out)[at + e] = v[e];
-            }
-        }
-      }
-    }
-    if (keep) {
-      __syncwarp();
-      const int row = row0 + lane;
-#pragma unroll
-      for (int g = 0; g < 8; ++g) {
-        const float4 v4 = *reinterpret_cast<const float4*>(turn + lane * 32 + ((g ^ (lane & 7)) * 4));
-        const float v[4] = {v4.x, v4.y, v4.z, v4.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int col = col0 + 4 * g + e;
-          if (row >= r || col >= ncols) continue;
-          if (KIND != kOrthApply) {
-            const long long at = static_cast<long long>(col) * ld + row;
-            __half h, l;
-            orth_split(v[e], h, l);
-            dst_hi[at] = h;
-            if (kStoreLo) dst_lo[at] = l;
-          } else {
-            const long long at = m.offset + static_cast<long long>(col) * m.r + row;
-            if (p.out_bf16) static_cast<unsigned short*>(p.out)[at] = static_cast<unsigned short>(pack_bf16x2_rn(v[e], 0.f) & 0xffffu);
-            else static_cast<float*>(p.out)[at] = v[e];
+        for (int e = 0; e < 8; ++e) {
+          const int col = col0 + 8 * g + e;
+          if (row < r && col < ncols) {
+            const long long to = static_cast<long long>(col) * m.lds + row;
+            reinterpret_cast<unsigned short*>(dst_hi)[to] = static_cast<unsigned short>(h[e / 2] >> (16 * (e & 1)));
+            if (kPair) reinterpret_cast<unsigned short*>(dst_lo)[to] = static_cast<unsigned short>(l[e / 2] >> (16 * (e & 1)));
           }
         }
       }
+      continue;
     }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= m.scale / kOrthXScale;
+    if (turned) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int col = col0 + 8 * g + e;
+        if (row < r && col < ncols) {
+          const long long to = m.offset + static_cast<long long>(col) * r + row;
+          if (SPLIT) static_cast<float*>(p.out)[to] = v[e];
+          else static_cast<unsigned short*>(p.out)[to] = static_cast<unsigned short>(pack_bf16x2_rn(v[e], 0.f) & 0xffffu);
+        }
+      }
+    } else if (SPLIT) {                            // the strip's two parts hold the upper and the lower halves of the fp32 words
+      uint32_t u[4], d[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t x0 = __float_as_uint(v[2 * k]), x1 = __float_as_uint(v[2 * k + 1]);
+        u[k] = __byte_perm(x0, x1, 0x7632);
+        d[k] = __byte_perm(x0, x1, 0x5410);
+      }
+      *reinterpret_cast<uint4*>(hrow + at) = make_uint4(u[0], u[1], u[2], u[3]);
+      *reinterpret_cast<uint4*>(lrow + at) = make_uint4(d[0], d[1], d[2], d[3]);
+    } else {
+      *reinterpret_cast<uint4*>(hrow + at) =
+          make_uint4(pack_bf16x2_rn(v[0], v[1]), pack_bf16x2_rn(v[2], v[3]), pack_bf16x2_rn(v[4], v[5]), pack_bf16x2_rn(v[6], v[7]));
+    }
+  }
+  if (last && !turned) {                           // to the vector, along rows
     __syncwarp();
+    const bool vec = m.vec_out && p.out_aligned;
+    if (vec) {                                     // 8 columns a lane, 8 rows at a time
+      const int q = lane & 3;
+#pragma unroll
+      for (int it = 0; it < 4; ++it) {
+        const int lr = it * 8 + (lane >> 2), col = col0 + 8 * q;
+        const int at = lr * 128 + ((4 * half + q) ^ (lr & 7)) * 16;
+        if (row0 + lr >= r || col >= ncols) continue;
+        const long long to = m.offset + static_cast<long long>(row0 + lr) * m.l + col;
+        const uint4 u = *reinterpret_cast<const uint4*>(hi + at);
+        if (SPLIT) {
+          const uint4 d = *reinterpret_cast<const uint4*>(lo + at);
+          uint4* dst = reinterpret_cast<uint4*>(static_cast<float*>(p.out) + to);
+          dst[0] = make_uint4(__byte_perm(d.x, u.x, 0x5410), __byte_perm(d.x, u.x, 0x7632), __byte_perm(d.y, u.y, 0x5410), __byte_perm(d.y, u.y, 0x7632));
+          dst[1] = make_uint4(__byte_perm(d.z, u.z, 0x5410), __byte_perm(d.z, u.z, 0x7632), __byte_perm(d.w, u.w, 0x5410), __byte_perm(d.w, u.w, 0x7632));
+        } else {
+          *reinterpret_cast<uint4*>(static_cast<unsigned short*>(p.out) + to) = u;
+        }
+      }
+    } else {                                       // one column a lane
+      const int col = col0 + lane;
+      for (int lr = 0; lr < 32 && row0 + lr < r; ++lr) {
+        const int at = lr * 128 + ((4 * half + (lane >> 3)) ^ (lr & 7)) * 16 + (lane & 7) * 2;
+        if (col >= ncols) continue;
+        const long long to = m.offset + static_cast<long long>(row0 + lr) * m.l + col;
+        const uint32_t u = *reinterpret_cast<const unsigned short*>(hi + at);
+        if (SPLIT) static_cast<uint32_t*>(p.out)[to] = u << 16 | *reinterpret_cast<const unsigned short*>(lo + at);
+        else static_cast<unsigned short*>(p.out)[to] = static_cast<unsigned short>(u);
+      }
+    }
   }
 }
 
-template <int KIND, bool SPLIT, int TN>
+template <int KIND, bool SPLIT, int CG>
 __global__ void __launch_bounds__(kOrthThreads, 1) orth_product_kernel(const OrthParams p) {
   extern __shared__ unsigned char smem_dyn[];
-  using L = OrthSmem<TN>;
+  using T = OrthTiling<SPLIT, CG>;
   unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
-  float* turn = reinterpret_cast<float*>(smem + L::kTurn);
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + L::kBars);
-  uint64_t* empty = full + L::kStages;
-  uint64_t* acc_full = empty + L::kStages;       // [2]
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + T::kBars);
+  uint64_t* empty = full + T::kStages;
+  uint64_t* acc_full = empty + T::kStages;       // [2]
   uint64_t* acc_free = acc_full + 2;             // [2]
-  uint64_t* drain = acc_free + 2;
+  uint64_t* strip_full = acc_free + 2;           // [kRing] what is added has arrived (or, with nothing to add, the place is free)
+  uint64_t* strip_done = strip_full + T::kRing;  // [kRing] the eight warps have put the result there
+  uint64_t* drain = strip_done + T::kRing;
   __shared__ uint32_t s_tmem;
-  __shared__ int s_issued;
+  __shared__ int s_issued, s_strips;
   __shared__ volatile int s_abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = CG == 2 ? static_cast<int>(cluster_rank()) : 0;
+  const int first = blockIdx.x / CG, stride = gridDim.x / CG;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < L::kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_free[s], 4); }
+    for (int s = 0; s < T::kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_free[s], 8 * CG); }
+    for (int s = 0; s < T::kRing; ++s) { mbar_init(&strip_full[s], 1); mbar_init(&strip_done[s], 8); }
     mbar_init(drain, 1);
     s_abort = 0;
     s_issued = 0;
+    s_strips = 0;
     mbar_init_fence();
     fence_proxy_async_smem();
   }
-  if (warp == 5) tmem_alloc(&s_tmem, 2 * TN);
+  if (warp == 9) tmem_alloc<CG>(&s_tmem, T::kTmemCols);
   tc_fence_before();
   __syncthreads();
+  if (CG == 2) cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
   pdl_launch_dependents();
   pdl_wait();
 
-  constexpr int kPasses = SPLIT ? 3 : 1;         // lo hi, hi lo, hi hi
-  if (warp == 4) {
+  if (warp == 8) {
     if (lane == 0) {
       int stage = 0, issued = 0;
       uint32_t parity = 1;                       // the stages start out empty
       bool ok = true;
-      for (int k = blockIdx.x; ok && k < p.num_tiles; k += gridDim.x) {
+      for (int k = first; ok && k < p.num_tiles; k += stride) {
         const OrthTile t = p.tiles[k];
         const CUtensorMap* maps = p.maps + static_cast<long long>(t.mat) * kMapCount;
         const int K = KIND == kOrthGram ? p.mats[t.mat].l : p.mats[t.mat].r;
-        const int a_map = KIND == kOrthGram ? kMapX0 + 2 * p.src : KIND == kOrthPoly ? kMapS : kMapB;
-        const int b_map = KIND == kOrthPoly ? kMapS : kMapX0 + 2 * p.src;
-        for (int pass = 0; ok && pass < kPasses; ++pass) {
-          const CUtensorMap* ma = maps + a_map + (SPLIT && pass == 0 ? 1 : 0);
-          const CUtensorMap* mb = maps + b_map + (SPLIT && pass == 1 ? 1 : 0);
-          for (int k0 = 0; k0 < K; k0 += kOrthTK) {
-            if (s_abort || !mbar_wait_bounded(&empty[stage], parity)) { s_abort = 1; ok = false; break; }
-            unsigned char* sa = smem + stage * L::kStage;
-            unsigned char* sb = sa + L::kA;
-            mbar_expect_tx(&full[stage], L::kStage);
+        const CUtensorMap* ma = maps + (KIND == kOrthGram ? kMapX0 + 2 * p.src : KIND == kOrthPoly ? kMapS : kMapB);
+        const CUtensorMap* mb = maps + (KIND == kOrthPoly ? kMapS : kMapX0 + 2 * p.src);
+        const int arow = t.i * T::kTM + rank * 128, brow = t.j * T::kTN + rank * T::kBRows;
+        for (int k0 = 0; k0 < K; k0 += kOrthTK) {
+          if (s_abort || !mbar_wait_bounded(&empty[stage], parity)) { s_abort = 1; ok = false; break; }
+          unsigned char* at = smem + stage * T::kStage;
+          if (rank == 0) mbar_expect_tx(&full[stage], CG * T::kStage);      // the pair's bytes all count on the even block's barrier
+          auto load = [&](unsigned char* dst, const CUtensorMap* map, int x, int y) {
+            if (CG == 2) tma_load_2d_pair(dst, map, &full[stage], x, y);
+            else tma_load_2d(dst, map, &full[stage], x, y);
+          };
 #pragma unroll
-            for (int h = 0; h < kOrthTM / 64; ++h) tma_load_2d(sa + h * 8192, ma, &full[stage], k0, t.i * kOrthTM + h * 64);
+          for (int part = 0; part < T::kParts; ++part) {
 #pragma unroll
-            for (int h = 0; h < TN / 64; ++h) {
-              if (KIND == kOrthApply) tma_load_2d(sb + h * 8192, mb, &full[stage], t.j * TN + h * 64, k0);
-              else tma_load_2d(sb + h * 8192, mb, &full[stage], k0, t.j * TN + h * 64);
+            for (int h = 0; h < 2; ++h) load(at + part * T::kA + h * 8192, ma + part, k0, arow + h * 64);
+#pragma unroll
+            for (int h = 0; h < T::kBRows / 64; ++h) {
+              unsigned char* dst = at + T::kParts * T::kA + part * T::kB + h * 8192;
+              if (KIND == kOrthApply) load(dst, mb + part, brow + h * 64, k0);
+              else load(dst, mb + part, k0, brow + h * 64);
             }
-            ++issued;
-            if (++stage == L::kStages) { stage = 0; parity ^= 1u; }
           }
+          ++issued;
+          if (++stage == T::kStages) { stage = 0; parity ^= 1u; }
         }
       }
       s_issued = issued;
     }
-  } else if (warp == 5) {
-    if (lane == 0) {
-      constexpr uint32_t idesc = mma_idesc(kOrthTM, TN, false, false, KIND == kOrthApply);
-      int stage = 0, buf = 0;
+  } else if (warp == 9) {
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc = mma_idesc(T::kTM, T::kTN, false, false, KIND == kOrthApply);
+      int stage = 0, buf = 0, small = 0;
       uint32_t parity = 0, acc_parity = 1;
       bool ok = true;
-      for (int k = blockIdx.x; ok && k < p.num_tiles; k += gridDim.x) {
-        const OrthTile t = p.tiles[k];
-        const int K = KIND == kOrthGram ? p.mats[t.mat].l : p.mats[t.mat].r;
-        const int steps = kPasses * ((K + kOrthTK - 1) / kOrthTK);
-        if (s_abort || !mbar_wait_bounded(&acc_free[buf], acc_parity)) { s_abort = 1; break; }
-        tc_fence_after();
-        const uint32_t d = tmem + buf * TN;
+      for (int k = first; ok && k < p.num_tiles; k += stride) {
+        const int mat = p.tiles[k].mat;
+        const int K = KIND == kOrthGram ? p.mats[mat].l : p.mats[mat].r;
+        const int steps = (K + kOrthTK - 1) / kOrthTK;
         for (int s = 0; s < steps; ++s) {
+          const int in_acc = SPLIT ? s % kOrthChunk : s;
+          if (in_acc == 0) {
+            if (s_abort || !mbar_wait_bounded(&acc_free[buf], acc_parity)) { s_abort = 1; ok = false; break; }
+            tc_fence_after();
+          }
           if (s_abort || !mbar_wait_bounded(&full[stage], parity)) { s_abort = 1; ok = false; break; }
           tc_fence_after();
-          const uint32_t sa = smem_addr(smem + stage * L::kStage), sb = sa + L::kA;
+          const uint32_t big = tmem + buf * T::kTN, low = tmem + (2 + small) * T::kTN;
+          const uint32_t sa = smem_addr(smem + stage * T::kStage), sb = sa + T::kParts * T::kA;
+          auto b_desc = [&](uint32_t base, int kk) { return KIND == kOrthApply ? desc_mnmajor(base + kk * 2048, 8192) : desc_kmajor(base + kk * 32); };
 #pragma unroll
-          for (int kk = 0; kk < kOrthTK / 16; ++kk)
-            mma_ss(d, desc_kmajor(sa + kk * 32), KIND == kOrthApply ? desc_mnmajor(sb + kk * 2048, 8192) : desc_kmajor(sb + kk * 32), idesc,
-                   (s | kk) != 0);
-          mma_commit(&empty[stage]);
-          if (++stage == L::kStages) { stage = 0; parity ^= 1u; }
+          for (int kk = 0; kk < kOrthTK / 16; ++kk) {
+            if (SPLIT) {
+              mma_ss<CG>(low, desc_kmajor(sa + T::kA + kk * 32), b_desc(sb, kk), idesc, (s | kk) != 0);
+              mma_ss<CG>(low, desc_kmajor(sa + kk * 32), b_desc(sb + T::kB, kk), idesc, 1);
+            }
+            mma_ss<CG>(big, desc_kmajor(sa + kk * 32), b_desc(sb, kk), idesc, (in_acc | kk) != 0);
+          }
+          mma_commit<CG>(&empty[stage]);
+          if (++stage == T::kStages) { stage = 0; parity ^= 1u; }
+          if (s == steps - 1 || (SPLIT && in_acc == kOrthChunk - 1)) {
+            mma_commit<CG>(&acc_full[buf]);
+            buf ^= 1;
+            if (buf == 0) acc_parity ^= 1u;
+          }
         }
-        if (ok) mma_commit(&acc_full[buf]);
-        buf ^= 1;
-        if (buf == 0) acc_parity ^= 1u;
+        small ^= 1;
       }
-      if (s_abort) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
+      if (s_abort) { mma_commit<CG>(drain); mbar_wait_bounded(drain, 0); }
+    }
+  } else if (warp == 10) {
+    if (lane == 0) {
+      // strips in the order of the tiles: `ask` runs kRing ahead of `give`
+      struct Walk { int k, strip, live; OrthTile t; };
+      auto open = [&](Walk& w) {                           // to the next tile that has strips here
+        for (; w.k < p.num_tiles; w.k += stride) {
+          w.t = p.tiles[w.k];
+          w.live = orth_live_strips<KIND, SPLIT, CG>(p.mats[w.t.mat], w.t, rank);
+          w.strip = 0;
+          if (w.live > 0) return;
+        }
+      };
+      auto next = [&](Walk& w) { if (++w.strip == w.live) { w.k += stride; open(w); } };
+      const bool last = KIND == kOrthApply && p.last;
+      constexpr int kAddParts = KIND == kOrthGram ? 0 : KIND == kOrthApply || SPLIT ? 2 : 1;
+      constexpr int kOutParts = KIND == kOrthApply || SPLIT ? 2 : 1;
+      int loads = 0;
+      auto fetch = [&](Walk& w) {
+        const int b = loads % T::kRing;
+        unsigned char* at = smem + T::kStrips + b * 2 * kOrthStripPart;
+        if constexpr (kAddParts == 0) {
+          mbar_arrive_one(&strip_full[b]);
+        } else {
+          const CUtensorMap* map = p.maps + static_cast<long long>(w.t.mat) * kMapCount + (KIND == kOrthPoly ? kMapS : kMapX0 + 2 * p.src);
+          const int row = w.t.i * T::kTM + rank * 128, col = w.t.j * T::kTN + w.strip * 64;
+          mbar_expect_tx(&strip_full[b], kAddParts * kOrthStripPart);
+#pragma unroll
+          for (int part = 0; part < kAddParts; ++part)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) tma_load_2d(at + part * kOrthStripPart + h * 8192, map + part, &strip_full[b], col, row + h * 64);
+        }
+        ++loads;
+        next(w);
+      };
+      Walk ask = {first, 0, 0, {}}, give = {first, 0, 0, {}};
+      open(ask);
+      open(give);
+      for (int s = 0; s < T::kRing && ask.k < p.num_tiles; ++s) fetch(ask);
+      int b = 0;
+      uint32_t parity = 0;
+      while (give.k < p.num_tiles) {
+        if (s_abort || !mbar_wait_bounded(&strip_done[b], parity)) { s_abort = 1; break; }
+        if (!last) {
+          const CUtensorMap* map = p.maps + static_cast<long long>(give.t.mat) * kMapCount + (KIND == kOrthGram ? kMapS : KIND == kOrthPoly ? kMapB : kMapX0 + 2 * (p.src ^ 1));
+          const unsigned char* at = smem + T::kStrips + b * 2 * kOrthStripPart;
+          const int row = give.t.i * T::kTM + rank * 128, col = give.t.j * T::kTN + give.strip * 64;
+#pragma unroll
+          for (int part = 0; part < kOutParts; ++part)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (row + h * 64 < p.mats[give.t.mat].r) tma_store_2d(map + part, at + part * kOrthStripPart + h * 8192, col, row + h * 64);
+          bulk_commit();
+          bulk_wait_read<0>();
+        }
+        if (ask.k < p.num_tiles) fetch(ask);               // into the place that has just been read
+        next(give);
+        if (++b == T::kRing) { b = 0; parity ^= 1u; }
+      }
+      bulk_wait<0>();
+      s_strips = kAddParts ? loads : 0;
     }
   } else {
-    int buf = 0;
-    uint32_t parity = 0;
-    for (int k = blockIdx.x; k < p.num_tiles; k += gridDim.x) {
-      const bool got = !s_abort && mbar_wait_bounded(&acc_full[buf], parity);
-      if (!__all_sync(0xffffffffu, got)) { s_abort = 1; break; }
-      tc_fence_after();
-      orth_epilogue_tile<KIND, SPLIT, TN>(p, p.tiles[k], tmem + buf * TN, turn + warp * 1024, &acc_free[buf]);
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const int half = warp >> 2;                            // this warp's 32 columns of each strip
+    int buf = 0, small = 0, place = 0;
+    uint32_t parity = 0, strip_parity = 0;
+    auto wait_for = [&](uint64_t* bar, uint32_t phase) {
+      const bool got = !s_abort && mbar_wait_bounded(bar, phase);
+      if (!__all_sync(0xffffffffu, got)) { s_abort = 1; return false; }
+      return true;
+    };
+    auto release = [&]() {                                 // this warp has read all it needs of the accumulator
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) { if (CG == 2) mbar_arrive_leader(&acc_free[buf]); else mbar_arrive_one(&acc_free[buf]); }
       buf ^= 1;
       if (buf == 0) parity ^= 1u;
+    };
+    auto finish = [&](const OrthMat& m, const OrthTile& t, int strip, const uint32_t (&acc)[32]) {
+      if (!wait_for(&strip_full[place], strip_parity)) return false;
+      unsigned char* at = smem + T::kStrips + place * 2 * kOrthStripPart + (warp & 3) * 32 * 128;
+      orth_finish_block<KIND, SPLIT, CG>(p, m, t.i * T::kTM + rank * 128 + (warp & 3) * 32, t.j * T::kTN + strip * 64 + half * 32, acc, at, at + kOrthStripPart, half);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_one(&strip_done[place]);
+      if (++place == T::kRing) { place = 0; strip_parity ^= 1u; }
+      return true;
+    };
+    bool ok = true;
+    for (int k = first; ok && k < p.num_tiles; k += stride) {
+      const OrthTile t = p.tiles[k];
+      const OrthMat& m = p.mats[t.mat];
+      const int live = orth_live_strips<KIND, SPLIT, CG>(m, t, rank);
+      if (!SPLIT) {
+        if (!wait_for(&acc_full[buf], parity)) break;
+        tc_fence_after();
+        const uint32_t base = tmem + buf * T::kTN + half * 32 + lanes;
+        if (live == 0) release();
+        for (int s = 0; ok && s < live; ++s) {
+          uint32_t acc[32];
+          tmem_ld32(base + s * 64, acc);
+          tmem_wait_ld();
+          if (s == live - 1) release();
+          ok = finish(m, t, s, acc);
+        }
+      } else {
+        const int K = KIND == kOrthGram ? m.l : m.r;
+        const int chunks = ((K + kOrthTK - 1) / kOrthTK + kOrthChunk - 1) / kOrthChunk;
+        float sum[T::kBlocks][32];
+        for (int q = 0; q < chunks; ++q) {
+          if (!wait_for(&acc_full[buf], parity)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t base = tmem + buf * T::kTN + half * 32 + lanes;
+#pragma unroll
+          for (int s = 0; s < T::kBlocks; ++s) {
+            uint32_t acc[32];
+            tmem_ld32(base + s * 64, acc);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) sum[s][e] = q == 0 ? __uint_as_float(acc[e]) : __fadd_rn(sum[s][e], __uint_as_float(acc[e]));
+          }
+          if (q == chunks - 1) {                           // the last chunk's commit covers the small terms too
+#pragma unroll
+            for (int s = 0; s < T::kBlocks; ++s) {
+              uint32_t acc[32];
+              tmem_ld32(tmem + (2 + small) * T::kTN + half * 32 + lanes + s * 64, acc);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) sum[s][e] = __fadd_rn(sum[s][e], __uint_as_float(acc[e]));
+            }
+          }
+          release();
+        }
+        small ^= 1;
+#pragma unroll
+        for (int s = 0; s < T::kBlocks; ++s) {
+          if (!ok || s >= live) continue;
+          uint32_t acc[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) acc[e] = __float_as_uint(sum[s][e]);
+          ok = finish(m, t, s, acc);
+        }
+      }
     }
   }
+  __syncwarp();
   tc_fence_before();
   __syncthreads();
+  if (CG == 2) cluster_sync_all();               // the pair's copies and arrivals are all in, unless a wait expired
   if (s_abort && threadIdx.x == 0) {             // no copy may land after the block has gone
-    for (int s = 0; s < L::kStages && s < s_issued; ++s) {
-      const int uses = (s_issued - 1 - s) / L::kStages;          // the stage's last copy is its use number `uses`
+    for (int s = 0; rank == 0 && s < T::kStages && s < s_issued; ++s) {
+      const int uses = (s_issued - 1 - s) / T::kStages;          // the stage's last copy is its use number `uses`
       mbar_wait_bounded(&full[s], uses & 1);
     }
+    for (int s = 0; s < T::kRing && s < s_strips; ++s) mbar_wait_bounded(&strip_full[s], ((s_strips - 1 - s) / T::kRing) & 1);
     atomicOr(p.flags, kFlagTimeout);
   }
   __syncthreads();
-  if (warp == 5) {
+  if (CG == 2) cluster_sync_all();
+  if (warp == 9) {
     tc_fence_after();
-    tmem_dealloc(tmem, 2 * TN);
+    tmem_dealloc<CG>(tmem, T::kTmemCols);
   }
 }
 
