@@ -62,6 +62,56 @@ int adacons_orth_get_info(adacons_orth *ctx, int key, int64_t *value);
 /* The caller makes sure that no work of the context is still running.  NULL is accepted. */
 int adacons_orth_destroy(adacons_orth *ctx);
 
+/* ------------------------------------------------------------------------------------------------
+ * Attention and its gradient.
+ *
+ * Per query head:  S = scale Q K^T, -inf where a query does not see a key;  lse = log sum exp S;
+ *     O = exp(S - lse) V
+ * Key j is visible to query i when j < kv_lens[batch] and, with `causal`, j <= i + kv_len - q_len (the
+ * last query sees the last key).  A query that sees no key has O = 0, lse = -inf, and takes no part in any
+ * gradient.  Keys from kv_lens[batch] on may hold anything, Inf and NaN included; their gradients are 0.
+ * Query heads h kv_heads / q_heads share a key head; its gradients are the sums over them.
+ */
+enum { ADACONS_F16 = 2 }; /* attention takes ADACONS_BF16 and ADACONS_F16 */
+
+/* A tensor of 16-bit elements (batch, token, head, element): strides in elements, the last one is 1.
+ * Any order of the first three dimensions is served (slices of a packed projection, head-major or
+ * token-major).  data must be 16-byte aligned, and the strides positive multiples of 8; those of
+ * dimensions of size 1 are not looked at. */
+typedef struct adacons_attn_tensor {
+  void *data;
+  int64_t batch_stride, seq_stride, head_stride;
+} adacons_attn_tensor;
+
+typedef struct adacons_attn_shape {
+  int dtype;              /* ADACONS_BF16 or ADACONS_F16 */
+  int batch;              /* 0 .. 65535 */
+  int q_heads, kv_heads;  /* q_heads a multiple of kv_heads */
+  int q_len, kv_len;      /* tokens, 0 .. 2^30 */
+  int head_dim;           /* a multiple of 8 up to 128 */
+  int causal;             /* 0 or 1 */
+  float scale;            /* > 0; usually head_dim^-1/2 */
+  const int32_t *kv_lens; /* device pointer, `batch` values (clamped to 0 .. kv_len), or NULL: all keys */
+} adacons_attn_shape;
+
+/* out: as q; lse: (batch, q_heads, q_len) fp32, contiguous.  out must not overlap the inputs.
+ * Errors: EINVAL, EALIGN, ELIMIT (head_dim > 128, sizes beyond the above), ECUDA, EARCH. */
+int adacons_attn_forward(const adacons_attn_shape *shape, const adacons_attn_tensor *q, const adacons_attn_tensor *k,
+                         const adacons_attn_tensor *v, const adacons_attn_tensor *out, float *lse, void *cuda_stream);
+
+/* dq, dk, dv from dout, with the probabilities recomputed from lse.  dq, dk and dv are written, not added to,
+ * and must not overlap the inputs.  workspace: device memory of adacons_attn_workspace_bytes, 16-byte
+ * aligned, free for other use after the call's work.  Errors: as the forward pass. */
+int adacons_attn_workspace_bytes(const adacons_attn_shape *shape, int64_t *bytes);
+int adacons_attn_backward(const adacons_attn_shape *shape, const adacons_attn_tensor *dout, const adacons_attn_tensor *q,
+                          const adacons_attn_tensor *k, const adacons_attn_tensor *v, const adacons_attn_tensor *out,
+                          const float *lse, const adacons_attn_tensor *dq, const adacons_attn_tensor *dk,
+                          const adacons_attn_tensor *dv, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/* ADACONS_FLAG_TIMEOUT if a bounded wait expired in an attention kernel of the current device since the last
+ * call (results since are invalid); clears it.  Synchronises `cuda_stream`. */
+int adacons_attn_get_status(uint32_t *flags, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,7 +7,8 @@ library raises.
 from . import workloads  # noqa: F401
 
 
-_LAZY = {"AdaCons": "binding", "AdaConsError": "binding", "load_library": "binding", "Orthogonalizer": "orth"}
+_LAZY = {"AdaCons": "binding", "AdaConsError": "binding", "load_library": "binding", "Orthogonalizer": "orth",
+         "attention_forward": "attention", "attention_backward": "attention"}
 
 
 def __getattr__(name):

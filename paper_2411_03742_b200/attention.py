@@ -1,0 +1,163 @@
+"""Attention and its gradient through the library's kernels.
+
+`attention_forward` and `attention_backward` marshal arguments only; `attention` is the two of them as
+one differentiable torch operation.  Tensors are (batch, token, head, element) in bf16 or fp16, with any
+strides whose last one is 1 and whose others are multiples of 8: slices of a packed projection, or
+head-major memory seen through a transpose, are taken as they are.  There is no fallback.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+
+from .binding import BF16, _check, _stream_handle, load_library
+
+F16 = 2
+
+
+class _Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("seq_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class _Shape(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("batch", ctypes.c_int), ("q_heads", ctypes.c_int), ("kv_heads", ctypes.c_int), ("q_len", ctypes.c_int),
+                ("kv_len", ctypes.c_int), ("head_dim", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float), ("kv_lens", ctypes.c_void_p)]
+
+
+def _arg(t):
+    st = t.stride()
+    return ctypes.byref(_Tensor(t.data_ptr(), st[0], st[1], st[2]))
+
+
+_checked = set()        # layouts that have passed check_attention
+
+
+def check_attention(q, k, v, kv_lens=None, like_q=(), like_k=(), rows=(), want_cuda: bool = True) -> None:
+    """Raise ValueError unless q, k, v (and what is shaped like them) are 4-D tensors of one 16-bit type on one
+    device whose sizes fit together; rows: (batch, q_heads, q_len) fp32 tensors; kv_lens: int32 (batch,)."""
+    import torch
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k and v must have four dimensions: batch, token, head, element")
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"attention takes bfloat16 and float16, got {q.dtype}")
+    B, Sq, Hq, D = q.shape
+    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} do not fit q {tuple(q.shape)}")
+    if k.shape[2] == 0 or Hq == 0 or Hq % k.shape[2] != 0:
+        raise ValueError(f"{Hq} query heads cannot share {k.shape[2]} key heads")
+    if D % 8 != 0 or not 8 <= D <= 128:
+        raise ValueError(f"head sizes are multiples of 8 up to 128, got {D}")
+    for name, t, shape in [("k", k, k.shape), ("v", v, k.shape)] + [(n, t, q.shape) for n, t in like_q] + [(n, t, k.shape) for n, t in like_k]:
+        if t.dtype != q.dtype or t.shape != shape:
+            raise ValueError(f"{name} must be {q.dtype} of shape {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    for name, t in [("q", q), ("k", k), ("v", v)] + list(like_q) + list(like_k):
+        if t.device != q.device or (want_cuda and not t.is_cuda):
+            raise ValueError(f"{name} must be a CUDA tensor on q's device")
+        if t.stride(3) != 1 or any(t.shape[i] > 1 and (t.stride(i) % 8 != 0 or t.stride(i) <= 0) for i in range(3)):
+            raise ValueError(f"{name}: the last stride must be 1 and the others positive multiples of 8, got {t.stride()}")
+    for name, t in rows:
+        if t.dtype != torch.float32 or tuple(t.shape) != (B, Hq, Sq) or not t.is_contiguous() or t.device != q.device:
+            raise ValueError(f"{name} must be a contiguous float32 tensor of shape {(B, Hq, Sq)} on q's device")
+    if kv_lens is not None and (kv_lens.dtype != torch.int32 or tuple(kv_lens.shape) != (B,) or kv_lens.device != q.device or (B > 1 and kv_lens.stride(0) != 1)):
+        raise ValueError(f"kv_lens must be a contiguous int32 tensor of shape {(B,)} on q's device")
+
+
+def _layout(t):
+    return None if t is None else (t.dtype, t.shape, t.stride(), t.device)
+
+
+def _shape(q, k, scale, causal, kv_lens):
+    import torch
+    B, Sq, Hq, D = q.shape
+    return _Shape(BF16 if q.dtype == torch.bfloat16 else F16, B, Hq, k.shape[2], Sq, k.shape[1], D, int(bool(causal)),
+                  1.0 / math.sqrt(D) if scale is None else float(scale), None if kv_lens is None else kv_lens.data_ptr())
+
+
+def attention_forward(q, k, v, *, scale=None, causal: bool = False, kv_lens=None, out=None, lse=None, stream=None):
+    """(out, lse): out = softmax(scale q k^T + mask) v, shaped like q, and the rows' log-sum-exp, (batch,
+    q_heads, q_len) fp32.  scale defaults to head_dim^-1/2; kv_lens (int32) hides each batch's keys from there on."""
+    import torch
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+    sig = (_layout(q), _layout(k), _layout(v), _layout(out), _layout(lse), _layout(kv_lens))
+    if sig not in _checked:
+        check_attention(q, k, v, kv_lens, like_q=[("out", out)], rows=[("lse", lse)])
+        _checked.add(sig)
+    shape = _shape(q, k, scale, causal, kv_lens)
+    _check(load_library().adacons_attn_forward(ctypes.byref(shape), _arg(q), _arg(k), _arg(v), _arg(out), lse.data_ptr(), _stream_handle(stream)),
+           "adacons_attn_forward")
+    return out, lse
+
+
+def workspace_bytes(q, k) -> int:
+    """Bytes of device memory that attention_backward works in."""
+    n = ctypes.c_int64()
+    _check(load_library().adacons_attn_workspace_bytes(ctypes.byref(_shape(q, k, None, False, None)), ctypes.byref(n)), "adacons_attn_workspace_bytes")
+    return n.value
+
+
+def attention_backward(dout, q, k, v, out, lse, *, scale=None, causal: bool = False, kv_lens=None, dq=None, dk=None, dv=None, workspace=None,
+                       stream=None):
+    """(dq, dk, dv) of attention_forward with the same scale, causal and kv_lens, from its out and lse and the
+    gradient dout.  workspace: a uint8 tensor of workspace_bytes(q, k), made here if not given (a call on a
+    stream other than the current one should bring its own)."""
+    import torch
+    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
+    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
+    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
+    if workspace is None:
+        B, Sq, Hq, _ = q.shape
+        workspace = torch.empty(8 * B * Hq * ((Sq + 127) // 128 * 128), dtype=torch.uint8, device=q.device)
+    sig = (_layout(q), _layout(k), _layout(v), _layout(out), _layout(lse), _layout(kv_lens), _layout(dout), _layout(dq), _layout(dk), _layout(dv))
+    if sig not in _checked:
+        check_attention(q, k, v, kv_lens, like_q=[("dout", dout), ("out", out), ("dq", dq)], like_k=[("dk", dk), ("dv", dv)], rows=[("lse", lse)])
+        _checked.add(sig)
+    if workspace.device != q.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous on q's device")
+    shape = _shape(q, k, scale, causal, kv_lens)
+    _check(load_library().adacons_attn_backward(ctypes.byref(shape), _arg(dout), _arg(q), _arg(k), _arg(v), _arg(out), lse.data_ptr(), _arg(dq), _arg(dk),
+                                                _arg(dv), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_handle(stream)),
+           "adacons_attn_backward")
+    return dq, dk, dv
+
+
+def status(stream=None) -> int:
+    """The ADACONS_FLAG_TIMEOUT bit of the current device's attention calls since the last look (0: all waits ended)."""
+    v = ctypes.c_uint32()
+    _check(load_library().adacons_attn_get_status(ctypes.byref(v), _stream_handle(stream)), "adacons_attn_get_status")
+    return v.value
+
+
+def attention(q, k, v, *, scale=None, causal: bool = False, kv_lens=None):
+    """attention_forward's out as a differentiable function of q, k and v."""
+    return _function().apply(q, k, v, scale, causal, kv_lens)
+
+
+_FUNCTION = None
+
+
+def _function():
+    global _FUNCTION
+    if _FUNCTION is None:
+        import torch
+
+        class Attention(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, q, k, v, scale, causal, kv_lens):
+                out, lse = attention_forward(q, k, v, scale=scale, causal=causal, kv_lens=kv_lens)
+                ctx.save_for_backward(q, k, v, out, lse, *([] if kv_lens is None else [kv_lens]))
+                ctx.how = (scale, causal)
+                return out
+
+            @staticmethod
+            def backward(ctx, dout):
+                q, k, v, out, lse, *lens = ctx.saved_tensors
+                if dout.stride(3) != 1 or any(n > 1 and (s % 8 != 0 or s <= 0) for n, s in zip(dout.shape[:3], dout.stride())):
+                    dout = dout.contiguous()        # a broadcast gradient, of a sum for instance
+                dq, dk, dv = attention_backward(dout, q, k, v, out, lse, scale=ctx.how[0], causal=ctx.how[1], kv_lens=lens[0] if lens else None)
+                return dq, dk, dv, None, None, None
+
+        _FUNCTION = Attention
+    return _FUNCTION

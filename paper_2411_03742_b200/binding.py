@@ -81,6 +81,10 @@ def load_library() -> ctypes.CDLL:
         "adacons_orth_get_status": [vp, P(ctypes.c_uint32), vp],
         "adacons_orth_get_info": [vp, i32, P(i64)],
         "adacons_orth_destroy": [vp],
+        "adacons_attn_forward": [vp] * 7,
+        "adacons_attn_workspace_bytes": [vp, P(i64)],
+        "adacons_attn_backward": [vp] * 11 + [i64, vp],
+        "adacons_attn_get_status": [P(ctypes.c_uint32), vp],
     }
     for name, args in protos.items():
         fn = getattr(lib, name)

@@ -23,6 +23,7 @@ SOURCES = {
     "adacons.cu": _COMMON + ["csrc/" + f for f in ("adacons_kernels.cuh", "adacons_pass1.cuh", "adacons_coeff.cuh", "adacons_pass2.cuh",
                                                    "adacons_fused.cuh", "adacons_gram.cuh", "adacons_shift.cuh")],
     "adacons_orth.cu": _OPS + ["csrc/adacons_orth.cuh"],
+    "adacons_attn.cu": _OPS + ["csrc/adacons_attn.cuh"],
 }
 
 

@@ -1,0 +1,230 @@
+// Host side of attention and its gradient (include/adacons_ops.h): checks, tensor maps and launches.
+#include "adacons_ops.h"
+
+#include <cmath>
+#include <mutex>
+
+#include "adacons_attn.cuh"
+#include "adacons_host.cuh"
+
+using namespace adacons;
+
+static __device__ uint32_t g_attn_flags;
+
+namespace {
+
+constexpr int kMaxDevices = 64;
+
+struct AttnDevice {
+  bool ready = false;
+  DeviceInfo info;
+  uint32_t* flags = nullptr;
+};
+
+template <typename K>
+bool raise(K kernel, uint32_t bytes) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)) == cudaSuccess) return true;
+  cudaGetLastError();
+  return false;
+}
+template <int D, bool BF16>
+bool raise_all() {
+  static_assert(AttnFwdSmem<D>::kBytes <= 227 * 1024 && AttnDkvSmem<D>::kBytes <= 227 * 1024 && AttnDqSmem<D>::kBytes <= 227 * 1024, "shared memory of a block");
+  return raise(attn_forward_kernel<D, BF16>, AttnFwdSmem<D>::kBytes) && raise(attn_dkv_kernel<D, BF16>, AttnDkvSmem<D>::kBytes) &&
+         raise(attn_dq_kernel<D, BF16>, AttnDqSmem<D>::kBytes);
+}
+
+// The first call on a device sets the kernels' shared-memory limits; later ones only look the entry up.
+int attn_device(AttnDevice** out) {
+  static std::mutex mutex;
+  static AttnDevice devices[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return ADACONS_ECUDA; }
+  if (dev < 0 || dev >= kMaxDevices) return ADACONS_ELIMIT;
+  std::lock_guard<std::mutex> lock(mutex);
+  AttnDevice& d = devices[dev];
+  if (!d.ready) {
+    const int rc = query_device(&d.info);
+    if (rc != ADACONS_OK) return rc;
+    void* flags = nullptr;
+    if (!raise_all<64, true>() || !raise_all<64, false>() || !raise_all<128, true>() || !raise_all<128, false>() ||
+        cudaGetSymbolAddress(&flags, g_attn_flags) != cudaSuccess) {
+      cudaGetLastError();
+      return ADACONS_ECUDA;
+    }
+    d.flags = static_cast<uint32_t*>(flags);
+    d.ready = true;
+  }
+  *out = &d;
+  return ADACONS_OK;
+}
+
+int check_shape(const adacons_attn_shape* s) {
+  if (s == nullptr) return ADACONS_EINVAL;
+  if (s->dtype != ADACONS_BF16 && s->dtype != ADACONS_F16) return ADACONS_EINVAL;
+  if (s->batch < 0 || s->q_heads < 1 || s->kv_heads < 1 || s->q_heads % s->kv_heads != 0 || s->q_len < 0 || s->kv_len < 0) return ADACONS_EINVAL;
+  if (s->head_dim < 8 || s->head_dim % 8 != 0) return ADACONS_EINVAL;
+  if (!(s->scale > 0.f) || !std::isfinite(s->scale) || (s->causal != 0 && s->causal != 1)) return ADACONS_EINVAL;
+  if (s->head_dim > 128 || s->batch > 65535 || s->q_heads > 65535 || s->q_len > (1 << 30) || s->kv_len > (1 << 30)) return ADACONS_ELIMIT;
+  return ADACONS_OK;
+}
+
+// Strides of dimensions of size one are never used, whatever the caller has there.
+int check_tensor(const adacons_attn_tensor* t, int batch, int len, int heads) {
+  if (t == nullptr) return ADACONS_EINVAL;
+  if (batch == 0 || len == 0) return ADACONS_OK;
+  if (t->data == nullptr) return ADACONS_EINVAL;
+  const int64_t strides[3] = {t->batch_stride, t->seq_stride, t->head_stride};
+  const int sizes[3] = {batch, len, heads};
+  if (reinterpret_cast<uintptr_t>(t->data) % 16 != 0) return ADACONS_EALIGN;
+  for (int k = 0; k < 3; ++k) {
+    if (sizes[k] == 1) continue;
+    if (strides[k] <= 0 || strides[k] >= (1ll << 38)) return ADACONS_EINVAL;
+    if (strides[k] % 8 != 0) return ADACONS_EALIGN;
+  }
+  return ADACONS_OK;
+}
+
+bool make_map(const AttnDevice& d, CUtensorMap* map, const adacons_attn_shape* s, const adacons_attn_tensor* t, int len, int heads, const void* spare) {
+  // a tensor without tokens is never read, but its map has to exist
+  const void* base = len > 0 ? t->data : spare;
+  const cuuint64_t dims[4] = {static_cast<cuuint64_t>(s->head_dim), static_cast<cuuint64_t>(len > 0 ? len : 1), static_cast<cuuint64_t>(heads),
+                              static_cast<cuuint64_t>(s->batch)};
+  const cuuint64_t one = static_cast<cuuint64_t>(s->head_dim) * 2;
+  const cuuint64_t strides[3] = {len > 1 ? static_cast<cuuint64_t>(t->seq_stride) * 2 : one, heads > 1 && len > 0 ? static_cast<cuuint64_t>(t->head_stride) * 2 : one,
+                                 s->batch > 1 && len > 0 ? static_cast<cuuint64_t>(t->batch_stride) * 2 : one};
+  const cuuint32_t box[4] = {64, kAttnTile, 1, 1};
+  return encode_map(d.info, map, s->dtype == ADACONS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides, box);
+}
+
+AttnOut as_out(const adacons_attn_tensor* t) { return {t->data, t->batch_stride, t->seq_stride, t->head_stride}; }
+
+AttnParams base_params(const AttnDevice& d, const adacons_attn_shape* s) {
+  AttnParams p = {};
+  p.B = s->batch;
+  p.Hq = s->q_heads;
+  p.Hkv = s->kv_heads;
+  p.Sq = s->q_len;
+  p.Sk = s->kv_len;
+  p.D = s->head_dim;
+  p.causal = s->causal;
+  p.sq_pad = (s->q_len + kAttnTile - 1) / kAttnTile * kAttnTile;
+  p.scale = s->scale;
+  p.scale_log2 = s->scale * kLog2e;
+  p.kv_lens = s->kv_lens;
+  p.flags = d.flags;
+  return p;
+}
+
+template <int D, bool BF16>
+bool run_forward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const AttnParams& p, cudaStream_t st) {
+  return launch(&attn_forward_kernel<D, BF16>, dim3((p.Sq + 2 * kAttnTile - 1) / (2 * kAttnTile), p.Hq, p.B), dim3(kAttnThreads), AttnFwdSmem<D>::kBytes, st,
+                false, 1, mq, mk, mv, p);
+}
+
+template <int D, bool BF16>
+bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo, AttnParams p, const adacons_attn_tensor* dout,
+                  const adacons_attn_tensor* out, const float* lse, AttnOut dq, AttnOut dk, AttnOut dv, float* lse2, float* delta, cudaStream_t st) {
+  const long long rows = static_cast<long long>(p.B) * p.Hq * p.sq_pad;
+  p.lse2 = lse2;
+  p.delta = delta;
+  const AttnRows a = {dout->data, dout->batch_stride, dout->seq_stride, dout->head_stride}, b = {out->data, out->batch_stride, out->seq_stride, out->head_stride};
+  if (rows > 0 && !launch(&attn_delta_kernel<BF16>, dim3(static_cast<unsigned>((rows + 7) / 8)), dim3(256), 0, st, false, 1, a, b, lse, p.Hq, p.Sq, p.sq_pad, p.D, rows, lse2, delta))
+    return false;
+  AttnParams pkv = p, pq = p;
+  pkv.out0 = dk;
+  pkv.out1 = dv;
+  pq.out0 = dq;
+  if (p.Sk > 0 && !launch(&attn_dkv_kernel<D, BF16>, dim3((p.Sk + kAttnTile - 1) / kAttnTile, p.Hkv, p.B), dim3(kAttnThreads), AttnDkvSmem<D>::kBytes, st, true, 1, mq, mk, mv, mdo, pkv))
+    return false;
+  return p.Sq == 0 || launch(&attn_dq_kernel<D, BF16>, dim3(p.sq_pad / kAttnTile, p.Hq, p.B), dim3(kAttnThreads), AttnDqSmem<D>::kBytes, st, true, 1, mq, mk, mv, mdo, pq);
+}
+
+int64_t workspace_bytes(const adacons_attn_shape* s) {
+  const int64_t pad = (static_cast<int64_t>(s->q_len) + kAttnTile - 1) / kAttnTile * kAttnTile;
+  return 2 * sizeof(float) * pad * s->q_heads * s->batch;
+}
+
+}  // namespace
+
+extern "C" {
+
+int adacons_attn_forward(const adacons_attn_shape* s, const adacons_attn_tensor* q, const adacons_attn_tensor* k, const adacons_attn_tensor* v,
+                         const adacons_attn_tensor* out, float* lse, void* cuda_stream) {
+  int rc = check_shape(s);
+  if (rc != ADACONS_OK) return rc;
+  if ((rc = check_tensor(q, s->batch, s->q_len, s->q_heads)) != ADACONS_OK || (rc = check_tensor(out, s->batch, s->q_len, s->q_heads)) != ADACONS_OK ||
+      (rc = check_tensor(k, s->batch, s->kv_len, s->kv_heads)) != ADACONS_OK || (rc = check_tensor(v, s->batch, s->kv_len, s->kv_heads)) != ADACONS_OK)
+    return rc;
+  if (s->batch == 0 || s->q_len == 0) return ADACONS_OK;
+  if (lse == nullptr || reinterpret_cast<uintptr_t>(lse) % 4 != 0) return ADACONS_EINVAL;
+  AttnDevice* d = nullptr;
+  if ((rc = attn_device(&d)) != ADACONS_OK) return rc;
+  CUtensorMap mq, mk, mv;
+  if (!make_map(*d, &mq, s, q, s->q_len, s->q_heads, q->data) || !make_map(*d, &mk, s, k, s->kv_len, s->kv_heads, q->data) ||
+      !make_map(*d, &mv, s, v, s->kv_len, s->kv_heads, q->data))
+    return ADACONS_ECUDA;
+  AttnParams p = base_params(*d, s);
+  p.out0 = as_out(out);
+  p.lse = lse;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  bool ok;
+  if (s->head_dim <= 64) ok = s->dtype == ADACONS_BF16 ? run_forward<64, true>(mq, mk, mv, p, st) : run_forward<64, false>(mq, mk, mv, p, st);
+  else ok = s->dtype == ADACONS_BF16 ? run_forward<128, true>(mq, mk, mv, p, st) : run_forward<128, false>(mq, mk, mv, p, st);
+  return ok ? ADACONS_OK : ADACONS_ECUDA;
+}
+
+int adacons_attn_workspace_bytes(const adacons_attn_shape* s, int64_t* bytes) {
+  if (bytes == nullptr) return ADACONS_EINVAL;
+  const int rc = check_shape(s);
+  if (rc == ADACONS_OK) *bytes = workspace_bytes(s);
+  return rc;
+}
+
+int adacons_attn_backward(const adacons_attn_shape* s, const adacons_attn_tensor* dout, const adacons_attn_tensor* q, const adacons_attn_tensor* k,
+                          const adacons_attn_tensor* v, const adacons_attn_tensor* out, const float* lse, const adacons_attn_tensor* dq,
+                          const adacons_attn_tensor* dk, const adacons_attn_tensor* dv, void* workspace, int64_t bytes, void* cuda_stream) {
+  int rc = check_shape(s);
+  if (rc != ADACONS_OK) return rc;
+  const adacons_attn_tensor* by_q[] = {dout, q, out, dq};
+  const adacons_attn_tensor* by_k[] = {k, v, dk, dv};
+  for (const adacons_attn_tensor* t : by_q)
+    if ((rc = check_tensor(t, s->batch, s->q_len, s->q_heads)) != ADACONS_OK) return rc;
+  for (const adacons_attn_tensor* t : by_k)
+    if ((rc = check_tensor(t, s->batch, s->kv_len, s->kv_heads)) != ADACONS_OK) return rc;
+  if (s->batch == 0 || (s->q_len == 0 && s->kv_len == 0)) return ADACONS_OK;
+  if (s->q_len > 0 && (lse == nullptr || reinterpret_cast<uintptr_t>(lse) % 4 != 0 || workspace == nullptr || bytes < workspace_bytes(s))) return ADACONS_EINVAL;
+  if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return ADACONS_EALIGN;
+  AttnDevice* d = nullptr;
+  if ((rc = attn_device(&d)) != ADACONS_OK) return rc;
+  const void* spare = s->q_len > 0 ? q->data : k->data;
+  CUtensorMap mq, mk, mv, mdo;
+  if (!make_map(*d, &mq, s, q, s->q_len, s->q_heads, spare) || !make_map(*d, &mk, s, k, s->kv_len, s->kv_heads, spare) ||
+      !make_map(*d, &mv, s, v, s->kv_len, s->kv_heads, spare) || !make_map(*d, &mdo, s, dout, s->q_len, s->q_heads, spare))
+    return ADACONS_ECUDA;
+  const AttnParams p = base_params(*d, s);
+  float* lse2 = static_cast<float*>(workspace);
+  float* delta = lse2 + static_cast<int64_t>(p.B) * p.Hq * p.sq_pad;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  auto go = [&](auto run) { return run(mq, mk, mv, mdo, p, dout, out, lse, as_out(dq), as_out(dk), as_out(dv), lse2, delta, st); };
+  bool ok;
+  if (s->head_dim <= 64) ok = s->dtype == ADACONS_BF16 ? go(run_backward<64, true>) : go(run_backward<64, false>);
+  else ok = s->dtype == ADACONS_BF16 ? go(run_backward<128, true>) : go(run_backward<128, false>);
+  return ok ? ADACONS_OK : ADACONS_ECUDA;
+}
+
+int adacons_attn_get_status(uint32_t* flags, void* cuda_stream) {
+  if (flags == nullptr) return ADACONS_EINVAL;
+  AttnDevice* d = nullptr;
+  const int rc = attn_device(&d);
+  if (rc != ADACONS_OK) return rc;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (cudaMemcpyAsync(flags, d->flags, sizeof(uint32_t), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+      cudaMemsetAsync(d->flags, 0, sizeof(uint32_t), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
+    cudaGetLastError();
+    return ADACONS_ECUDA;
+  }
+  return ADACONS_OK;
+}
+
+}  // extern "C"

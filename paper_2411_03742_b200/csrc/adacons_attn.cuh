@@ -1,0 +1,855 @@
+// Attention and its gradient on the tensor cores: kernels (sm_100a).
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "adacons_tc.cuh"
+
+namespace adacons {
+
+// ----------------------------------------------------------------------------------------------
+// For one query head:  S = scale Q K^T with -inf where a query does not see a key,
+//     lse_i = log sum_j exp S_ij     P = exp(S - lse)     O = P V
+// and from dO, with Delta_i = sum_d dO_id O_id:
+//     dV = P^T dO     dP = dO V^T     dS = P o (dP - Delta)     dQ = scale dS K     dK = scale dS^T Q
+// Key j is visible to query i when j < kv_len and, with a causal mask, j <= i + Sk - Sq.  A query
+// that sees no key has O = 0, lse = -inf and no part in any gradient.
+//
+// Operand tiles are 128 rows (queries or keys) of 64 or 128 head elements, fetched by TMA from 4-D
+// tensors (element, token, head, batch): whatever lies past the last token or the head's last element
+// arrives as zero, so that odd lengths and head sizes need no other code.  A tile is one or two blocks
+// of 128 swizzled 128-byte rows; read along its rows it is the K-major operand of a product over head
+// elements, read across them the MN-major operand of a product over tokens, from the same bytes.
+// Keys from kv_len on may hold anything, Inf and NaN included: their rows are zeroed in shared
+// memory before any product over keys (0 x NaN would spread to every query).
+// S, the statistics, the accumulators and dS up to its rounding are fp32; P and dS are rounded to the
+// inputs' 16-bit type as operands of the second products, an error of the size of the results' own rounding.
+// ----------------------------------------------------------------------------------------------
+constexpr int kAttnTile = 128;
+constexpr int kAttnThreads = 320;                // warps 0-7 elementwise, 8 copies, 9 products
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct AttnOut { void* p; long long batch, seq, head; };     // element strides
+
+struct AttnParams {
+  int B, Hq, Hkv, Sq, Sk, D;
+  int causal;
+  int sq_pad;                    // rows of the padded statistics
+  float scale, scale_log2;       // scale, scale * log2(e)
+  const int* kv_lens;            // [B] or null
+  float* lse;                    // forward: [B][Hq][Sq]
+  const float* lse2;             // backward: lse log2(e), +inf where a row has no key or does not exist: [B][Hq][sq_pad]
+  const float* delta;            // likewise, 0 there
+  AttnOut out0, out1;            // forward: O; backward: dQ, or dK and dV
+  uint32_t* flags;
+};
+
+template <int D> struct AttnTile {
+  static constexpr uint32_t kBlock = kAttnTile * 128;         // 128 rows x 64 elements
+  static constexpr uint32_t kBytes = kBlock * (D / 64);
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack16(float lo, float hi) {
+  if (BF16) return pack_bf16x2_rn(lo, hi);
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <bool BF16>
+__device__ __forceinline__ float2 unpack16(uint32_t u) {
+  if (BF16) return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+  return __half22float2(*reinterpret_cast<const __half2*>(&u));
+}
+
+template <int D>
+__device__ __forceinline__ void attn_load_tile(unsigned char* dst, const CUtensorMap* map, uint64_t* bar, int row, int head, int batch) {
+#pragma unroll
+  for (int h = 0; h < D / 64; ++h) tma_load_4d(dst + h * AttnTile<D>::kBlock, map, bar, h * 64, row, head, batch);
+}
+// rows [first, 128) of a tile become zero; called by one warp, before the tile is an operand
+template <int D>
+__device__ __forceinline__ void attn_zero_rows(unsigned char* tile, int first) {
+  const int lane = threadIdx.x & 31;
+  for (int k = lane; k < (kAttnTile - first) * 8; k += 32)
+#pragma unroll
+    for (int h = 0; h < D / 64; ++h) *reinterpret_cast<uint4*>(tile + h * AttnTile<D>::kBlock + first * 128 + k * 16) = make_uint4(0u, 0u, 0u, 0u);
+  fence_proxy_async_smem();
+  __syncwarp();
+}
+
+// 128 x 128 product over head elements: rows of `a` with rows of `b`
+template <int D, bool BF16>
+__device__ __forceinline__ void attn_mma_rows(uint32_t d, uint32_t a, uint32_t b) {
+  constexpr uint32_t idesc = mma_idesc(kAttnTile, kAttnTile, BF16, false, false);
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) {
+    const uint32_t off = (k / 4) * AttnTile<D>::kBlock + (k % 4) * 32;
+    mma_ss(d, desc_kmajor(a + off), desc_kmajor(b + off), idesc, k != 0);
+  }
+}
+// 128 x D product over tokens: 16-bit values in tensor memory with the tokens of `b`.  The 128 columns of
+// values lie in two halves of 32 words, `step` apart.
+template <int D, bool BF16>
+__device__ __forceinline__ void attn_mma_tokens(uint32_t d, uint32_t a, uint32_t step, uint32_t b, bool accumulate) {
+  constexpr uint32_t idesc = mma_idesc(kAttnTile, D, BF16, false, true);
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    mma_ts(d, a + (k / 4) * step + (k % 4) * 8, desc_mnmajor(b + k * 2048, AttnTile<D>::kBlock), idesc, (accumulate || k != 0) ? 1u : 0u);
+}
+
+// Row `row` of an accumulator (this thread's lane), columns [0, D), times `mul`, to global memory.
+template <int D, bool BF16>
+__device__ __forceinline__ void attn_store_row(const AttnParams& p, const AttnOut& o, uint32_t tmem, int batch, int head, int row, bool live, float mul) {
+  unsigned short* dst = static_cast<unsigned short*>(o.p) + batch * o.batch + static_cast<long long>(row) * o.seq + head * o.head;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) {
+    uint32_t v[32];
+    __syncwarp();
+    tmem_ld32(tmem + c * 32, v);
+    tmem_wait_ld();
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      if (!live || c * 32 + g * 8 >= p.D) continue;       // the head size is a multiple of eight
+      uint32_t w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = pack16<BF16>(__uint_as_float(v[8 * g + 2 * k]) * mul, __uint_as_float(v[8 * g + 2 * k + 1]) * mul);
+      *reinterpret_cast<uint4*>(dst + c * 32 + g * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+__device__ __forceinline__ void attn_zero_row(const AttnParams& p, const AttnOut& o, int batch, int head, int row) {
+  unsigned short* dst = static_cast<unsigned short*>(o.p) + batch * o.batch + static_cast<long long>(row) * o.seq + head * o.head;
+  for (int k = 0; k < p.D; k += 8) *reinterpret_cast<uint4*>(dst + k) = make_uint4(0u, 0u, 0u, 0u);
+}
+
+__device__ __forceinline__ int attn_kv_len(const AttnParams& p, int batch) {
+  if (p.kv_lens == nullptr) return p.Sk;
+  const int n = p.kv_lens[batch];
+  return n < 0 ? 0 : n > p.Sk ? p.Sk : n;
+}
+
+// ----------------------------------------------------------------------------------------------
+// Forward.  A block owns two tiles of 128 queries and walks over the key tiles, the softmax of one
+// query tile running while the tensor cores work for the other.  Tensor memory: S of both tiles (128
+// columns each, later the rounded P in its place) and both accumulators.  A thread holds one query's
+// whole row of scores, so that maximum and sum need no exchange.  The running maximum is only raised
+// when a row's scores exceed it by more than 2^8 in the exponential (the quotient O / sum does not
+// depend on it, and fp32 and bf16 have the range): the accumulator is then rescaled in place, which
+// after the first few key tiles hardly happens.
+// ----------------------------------------------------------------------------------------------
+template <int D> struct AttnFwdSmem {
+  static constexpr uint32_t kT = AttnTile<D>::kBytes;
+  static constexpr int kSlots = D == 128 ? 5 : 8;              // ring of K and V tiles in turn
+  static constexpr uint32_t kKV = 2 * kT, kBars = kKV + kSlots * kT, kBytes = kBars + 256 + 1024;
+};
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const AttnParams p) {
+  extern __shared__ unsigned char smem_dyn[];
+  using L = AttnFwdSmem<D>;
+  unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
+  uint64_t* q_full = reinterpret_cast<uint64_t*>(smem + L::kBars);
+  uint64_t* kv_full = q_full + 1;                // [kSlots]
+  uint64_t* kv_free = kv_full + L::kSlots;       // [kSlots]
+  uint64_t* s_full = kv_free + L::kSlots;        // [2]
+  uint64_t* p_full = s_full + 2;                 // [2]
+  uint64_t* o_full = p_full + 2;                 // [2]
+  uint64_t* drain = o_full + 2;
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int head = blockIdx.y, batch = blockIdx.z;
+  const int blk = gridDim.x - 1 - blockIdx.x;    // with a causal mask the last queries have the most keys: first
+  const int q0 = blk * 2 * kAttnTile;
+
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 1);
+    for (int s = 0; s < L::kSlots; ++s) { mbar_init(&kv_full[s], 1); mbar_init(&kv_free[s], 1); }
+    for (int t = 0; t < 2; ++t) { mbar_init(&s_full[t], 1); mbar_init(&p_full[t], 4); mbar_init(&o_full[t], 1); }
+    mbar_init(drain, 1);
+    s_abort = 0;
+    mbar_init_fence();
+    fence_proxy_async_smem();
+  }
+  if (warp == 9) tmem_alloc(&s_tmem, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  const int kv_len = attn_kv_len(p, batch);
+  const int off = p.Sk - p.Sq;
+  const int q_last = min(q0 + 2 * kAttnTile, p.Sq) - 1;
+  const int seen = p.causal ? min(kv_len, max(0, q_last + off + 1)) : kv_len;     // keys that any query of the block sees
+  const int tiles = (seen + kAttnTile - 1) / kAttnTile;
+
+  if (tiles > 0 && warp == 8) {
+    if (lane == 0) {
+      mbar_expect_tx(q_full, 2 * L::kT);
+      for (int t = 0; t < 2; ++t) attn_load_tile<D>(smem + t * L::kT, &mq, q_full, q0 + t * kAttnTile, head, batch);
+      const int kv_head = head / (p.Hq / p.Hkv);
+      int slot = 0, issued = 0;
+      uint32_t parity = 1;
+      for (int n = 0; n < 2 * tiles; ++n) {      // K_0 V_0 K_1 V_1 ..
+        if (s_abort || !mbar_wait_bounded(&kv_free[slot], parity)) { s_abort = 1; break; }
+        mbar_expect_tx(&kv_full[slot], L::kT);
+        attn_load_tile<D>(smem + L::kKV + slot * L::kT, n & 1 ? &mv : &mk, &kv_full[slot], (n >> 1) * kAttnTile, kv_head, batch);
+        ++issued;
+        if (++slot == L::kSlots) { slot = 0; parity ^= 1u; }
+      }
+      if (s_abort) {                             // no copy may land after the block has gone
+        mbar_wait_bounded(q_full, 0);
+        for (int s = 0; s < L::kSlots && s < issued; ++s) mbar_wait_bounded(&kv_full[s], ((issued - 1 - s) / L::kSlots) & 1);
+      }
+    }
+  } else if (tiles > 0 && warp == 9) {
+    int slot = 0;
+    uint32_t parity = 0;
+    bool ok = mbar_wait_bounded(q_full, 0);
+    // waits for a slot; V tiles that reach past kv_len get their rows zeroed
+    auto take = [&](int valid) -> uint32_t {
+      ok = ok && !s_abort && mbar_wait_bounded(&kv_full[slot], parity);
+      ok = __all_sync(0xffffffffu, ok);
+      if (ok && valid < kAttnTile) attn_zero_rows<D>(smem + L::kKV + slot * L::kT, valid);
+      const uint32_t at = smem_addr(smem + L::kKV + slot * L::kT);
+      return at;
+    };
+    auto wait_p = [&](int t, int j) {
+      ok = ok && !s_abort && mbar_wait_bounded(&p_full[t], j & 1);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+    };
+    auto advance = [&]() { if (++slot == L::kSlots) { slot = 0; parity ^= 1u; } };
+    const uint32_t sq = smem_addr(smem);
+    uint32_t k_at = take(kAttnTile);
+    if (ok && lane == 0) {
+      tc_fence_after();
+      for (int t = 0; t < 2; ++t) {
+        attn_mma_rows<D, BF16>(tmem + t * 128, sq + t * L::kT, k_at);
+        mma_commit(&s_full[t]);
+      }
+      mma_commit(&kv_free[slot]);
+    }
+    __syncwarp();
+    advance();
+    for (int j = 0; ok && j < tiles; ++j) {
+      const int v_slot = slot;
+      const uint32_t v_at = take(min(kv_len - j * kAttnTile, kAttnTile));
+      advance();
+      int k_slot = slot;
+      if (ok && j + 1 < tiles) { k_slot = slot; k_at = take(kAttnTile); advance(); }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if (ok) wait_p(t, j);
+        if (ok && lane == 0) {
+          attn_mma_tokens<D, BF16>(tmem + 256 + t * 128, tmem + t * 128, 32, v_at, j != 0);
+          if (j + 1 < tiles) {
+            attn_mma_rows<D, BF16>(tmem + t * 128, sq + t * L::kT, k_at);
+            mma_commit(&s_full[t]);
+          } else {
+            mma_commit(&o_full[t]);
+          }
+          if (t == 1) {
+            mma_commit(&kv_free[v_slot]);
+            if (j + 1 < tiles) mma_commit(&kv_free[k_slot]);
+          }
+        }
+        __syncwarp();
+      }
+    }
+    if (!ok) {
+      s_abort = 1;
+      if (lane == 0) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
+    }
+  } else if (warp < 8) {
+    const int t = warp >> 2;
+    const int row = q0 + t * kAttnTile + (warp & 3) * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_at = tmem + t * 128 + lanes, o_at = tmem + 256 + t * 128 + lanes;
+    const int limit = p.causal ? min(kv_len, row + off + 1) : kv_len;        // this query's keys: [0, limit)
+    const int warp_limit = p.causal ? min(kv_len, row - lane + off + 1) : kv_len;   // all of the warp's queries see these
+    float top = -INFINITY, sum = 0.f;            // running maximum of scale_log2 S and the sum under it
+    bool ok = true;
+    for (int j = 0; ok && j < tiles; ++j) {
+      ok = !s_abort && mbar_wait_bounded(&s_full[t], j & 1);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t s[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32(s_at + c * 32, s[c]);
+      tmem_wait_ld();
+      const int k0 = j * kAttnTile;
+      if (k0 + kAttnTile > warp_limit) {         // warp-uniform: some score of the tile is masked
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (k0 + c * 32 + e >= limit) s[c][e] = 0xff800000u;
+      }
+      float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int e = 0; e < 32; ++e) m[e & 3] = fmaxf(m[e & 3], __uint_as_float(s[c][e]));
+      const float tile_top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * p.scale_log2;
+      const bool raise = tile_top > top + 8.f;   // also the first time a row sees a key
+      if (__any_sync(0xffffffffu, raise)) {
+        const float next = raise ? tile_top : top;
+        const float factor = raise ? exp2_fast(top - next) : 1.f;
+        sum *= factor;
+        top = next;
+        if (j > 0) {
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            tmem_ld32(o_at + c * 32, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
+            tmem_st32(o_at + c * 32, o);
+          }
+        }
+      }
+      const float base = top == -INFINITY ? 0.f : top;
+      float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {              // 64 keys at a time: 32 words of P
+        uint32_t w[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const float p0 = exp2_fast(fmaf(__uint_as_float(s[2 * c + e / 16][(2 * e) & 31]), p.scale_log2, -base));
+          const float p1 = exp2_fast(fmaf(__uint_as_float(s[2 * c + e / 16][(2 * e + 1) & 31]), p.scale_log2, -base));
+          part[(2 * e) & 3] += p0;
+          part[(2 * e + 1) & 3] += p1;
+          w[e] = pack16<BF16>(p0, p1);
+        }
+        tmem_st32(s_at + c * 32, w);
+      }
+      sum += (part[0] + part[1]) + (part[2] + part[3]);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_one(&p_full[t]);
+    }
+    const bool live = row < p.Sq;
+    if (ok && tiles > 0) {
+      ok = !s_abort && mbar_wait_bounded(&o_full[t], 0);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      if (ok) attn_store_row<D, BF16>(p, p.out0, o_at, batch, head, row, live, sum == 0.f ? 0.f : 1.f / sum);
+    } else if (tiles == 0 && live) {
+      attn_zero_row(p, p.out0, batch, head, row);
+    }
+    if (ok && live) p.lse[(static_cast<long long>(batch) * p.Hq + head) * p.Sq + row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    if (!ok) s_abort = 1;
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (s_abort && threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// ----------------------------------------------------------------------------------------------
+// Before the gradient: Delta_i = sum_d dO_id O_id and the log-sum-exp in base 2, padded to whole tiles
+// so that the gradient kernels copy them 128 at a time.  One warp per query and head.
+// ----------------------------------------------------------------------------------------------
+struct AttnRows { const void* p; long long batch, seq, head; };
+
+template <bool BF16>
+__global__ void __launch_bounds__(256) attn_delta_kernel(const AttnRows dout, const AttnRows out, const float* lse, int Hq, int Sq, int sq_pad, int D,
+                                                         long long rows, float* lse2, float* delta) {
+  const long long n = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  pdl_launch_dependents();
+  if (n >= rows) return;
+  const long long bh = n / sq_pad;
+  const int row = static_cast<int>(n - bh * sq_pad), head = static_cast<int>(bh % Hq);
+  const long long batch = bh / Hq;
+  float sum = 0.f, l = -INFINITY;
+  if (row < Sq) {
+    const unsigned short* a = static_cast<const unsigned short*>(dout.p) + batch * dout.batch + row * dout.seq + head * dout.head;
+    const unsigned short* b = static_cast<const unsigned short*>(out.p) + batch * out.batch + row * out.seq + head * out.head;
+    if (4 * lane < D) {                          // D <= 128, a multiple of eight
+      const uint2 x = *reinterpret_cast<const uint2*>(a + 4 * lane), y = *reinterpret_cast<const uint2*>(b + 4 * lane);
+      const float2 x0 = unpack16<BF16>(x.x), x1 = unpack16<BF16>(x.y), y0 = unpack16<BF16>(y.x), y1 = unpack16<BF16>(y.y);
+      sum = (x0.x * y0.x + x0.y * y0.y) + (x1.x * y1.x + x1.y * y1.y);
+    }
+    l = lse[bh * Sq + row];
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (lane == 0) {
+    const bool none = l == -INFINITY;
+    lse2[n] = none ? INFINITY : l * kLog2e;
+    delta[n] = none ? 0.f : sum;
+  }
+}
+
+// ----------------------------------------------------------------------------------------------
+// dK and dV.  A block owns 128 keys of one key head and walks over the query tiles of all query heads
+// that share it: the shared head's gradient is a sum in tensor memory, in a fixed order, without atomics.
+// Tensor memory (512 columns at D = 128): S^T, dP^T, dV, dK.  P^T and dS^T, rounded, take the places of S^T
+// and dP^T and are the left operands of dV += P^T dO and dK += dS^T Q straight from there.
+// The products are issued so that each elementwise phase has two products beside it:
+//     P(i) from S(i)       | dK(i-1), dP(i)
+//     dS(i) from P, dP(i)  | dV(i), S(i+1)
+// Two warps share a block of 32 keys, 64 queries each.
+// ----------------------------------------------------------------------------------------------
+template <int D> struct AttnDkvSmem {
+  static constexpr uint32_t kT = AttnTile<D>::kBytes;
+  static constexpr int kStages = D == 128 ? 2 : 4;
+  static constexpr uint32_t kRing = 2 * kT, kStage = 2 * kT;                    // K, V | (Q, dO) per stage
+  static constexpr uint32_t kStats = kRing + kStages * kStage;                  // lse2, delta: 2 x 512 bytes per stage
+  static constexpr uint32_t kBars = kStats + kStages * 1024, kBytes = kBars + 256 + 1024;
+};
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(smem_addr(dst)), "l"(src), "r"(bytes), "r"(smem_addr(bar)) : "memory");
+}
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
+                const __grid_constant__ CUtensorMap mdo, const AttnParams p) {
+  extern __shared__ unsigned char smem_dyn[];
+  using L = AttnDkvSmem<D>;
+  unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
+  uint64_t* kv_full = reinterpret_cast<uint64_t*>(smem + L::kBars);
+  uint64_t* full = kv_full + 1;                  // [kStages]
+  uint64_t* free_ = full + L::kStages;           // [kStages]
+  uint64_t* s_full = free_ + L::kStages;
+  uint64_t* p_full = s_full + 1;
+  uint64_t* dp_full = p_full + 1;
+  uint64_t* ds_full = dp_full + 1;
+  uint64_t* done = ds_full + 1;
+  uint64_t* drain = done + 1;
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int kv_head = blockIdx.y, batch = blockIdx.z;
+  const int k0 = blockIdx.x * kAttnTile;         // with a causal mask the first keys have the most queries: first
+  const int group = p.Hq / p.Hkv;
+
+  if (threadIdx.x == 0) {
+    mbar_init(kv_full, 1);
+    for (int s = 0; s < L::kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&free_[s], 1); }
+    mbar_init(s_full, 1);
+    mbar_init(p_full, 8);
+    mbar_init(dp_full, 1);
+    mbar_init(ds_full, 8);
+    mbar_init(done, 1);
+    mbar_init(drain, 1);
+    s_abort = 0;
+    mbar_init_fence();
+    fence_proxy_async_smem();
+  }
+  if (warp == 9) tmem_alloc(&s_tmem, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  const uint32_t t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 384;
+  const int kv_len = attn_kv_len(p, batch);
+  const int off = p.Sk - p.Sq;
+  const int q_tiles = (p.Sq + kAttnTile - 1) / kAttnTile;
+  // the first query that sees any of these keys: i >= k0 - off
+  const int first = p.causal ? min(q_tiles, max(0, k0 - off) / kAttnTile) : 0;
+  const int per_head = k0 < kv_len ? q_tiles - first : 0;
+  const int items = group * per_head;
+  pdl_wait();                                    // the statistics
+
+  if (items > 0 && warp == 8) {
+    if (lane == 0) {
+      mbar_expect_tx(kv_full, 2 * L::kT);
+      attn_load_tile<D>(smem, &mk, kv_full, k0, kv_head, batch);
+      attn_load_tile<D>(smem + L::kT, &mv, kv_full, k0, kv_head, batch);
+      int stage = 0, issued = 0;
+      uint32_t parity = 1;
+      for (int n = 0; n < items; ++n) {
+        const int head = kv_head * group + n / per_head, q0 = (first + n % per_head) * kAttnTile;
+        if (s_abort || !mbar_wait_bounded(&free_[stage], parity)) { s_abort = 1; break; }
+        unsigned char* at = smem + L::kRing + stage * L::kStage;
+        unsigned char* stats = smem + L::kStats + stage * 1024;
+        const long long base = (static_cast<long long>(batch) * p.Hq + head) * p.sq_pad + q0;
+        mbar_expect_tx(&full[stage], L::kStage + 1024);
+        attn_load_tile<D>(at, &mq, &full[stage], q0, head, batch);
+        attn_load_tile<D>(at + L::kT, &mdo, &full[stage], q0, head, batch);
+        bulk_load(stats, p.lse2 + base, 512, &full[stage]);
+        bulk_load(stats + 512, p.delta + base, 512, &full[stage]);
+        ++issued;
+        if (++stage == L::kStages) { stage = 0; parity ^= 1u; }
+      }
+      if (s_abort) {
+        mbar_wait_bounded(kv_full, 0);
+        for (int s = 0; s < L::kStages && s < issued; ++s) mbar_wait_bounded(&full[s], ((issued - 1 - s) / L::kStages) & 1);
+      }
+    }
+  } else if (items > 0 && warp == 9) {
+    bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(kv_full, 0));
+    if (ok && k0 + kAttnTile > kv_len) {
+      attn_zero_rows<D>(smem, kv_len - k0);
+      attn_zero_rows<D>(smem + L::kT, kv_len - k0);
+    }
+    if (lane == 0) {
+      const uint32_t sk = smem_addr(smem), sv = sk + L::kT;
+      auto q_at = [&](int n) { return smem_addr(smem + L::kRing + (n % L::kStages) * L::kStage); };
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        ok = ok && !s_abort && mbar_wait_bounded(bar, parity);
+        tc_fence_after();
+        return ok;
+      };
+      if (wait(&full[0], 0)) {
+        attn_mma_rows<D, BF16>(t_s, sk, q_at(0));
+        mma_commit(s_full);
+        attn_mma_rows<D, BF16>(t_dp, sv, q_at(0) + L::kT);
+        mma_commit(dp_full);
+      }
+      for (int n = 0; ok && n < items; ++n) {
+        const int next = n + 1;
+        if (!wait(p_full, n & 1)) break;
+        attn_mma_tokens<D, BF16>(t_dv, t_s, 64, q_at(n) + L::kT, n != 0);
+        if (next < items) {
+          if (!wait(&full[next % L::kStages], (next / L::kStages) & 1)) break;
+          attn_mma_rows<D, BF16>(t_s, sk, q_at(next));
+          mma_commit(s_full);
+        }
+        if (!wait(ds_full, n & 1)) break;
+        attn_mma_tokens<D, BF16>(t_dk, t_dp, 64, q_at(n), n != 0);
+        mma_commit(&free_[n % L::kStages]);
+        if (next < items) {
+          attn_mma_rows<D, BF16>(t_dp, sv, q_at(next) + L::kT);
+          mma_commit(dp_full);
+        } else {
+          mma_commit(done);
+        }
+      }
+      if (!ok) {
+        s_abort = 1;
+        mma_commit(drain);
+        mbar_wait_bounded(drain, 0);
+      }
+    }
+  } else if (warp < 8) {
+    const int half = warp >> 2;                  // this warp's 64 queries of each tile
+    const int key = k0 + (warp & 3) * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_at = t_s + lanes + half * 64, dp_at = t_dp + lanes + half * 64;
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = !s_abort && mbar_wait_bounded(bar, parity);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      return ok;
+    };
+    for (int n = 0; n < items; ++n) {
+      const int stage = n % L::kStages, q0 = (first + n % per_head) * kAttnTile + half * 64;
+      const float4* lse2 = reinterpret_cast<const float4*>(smem + L::kStats + stage * 1024) + half * 16;
+      const float4* delta = reinterpret_cast<const float4*>(smem + L::kStats + stage * 1024 + 512) + half * 16;
+      // key j is seen by query i when j < kv_len and j - off <= i
+      const int from = key >= kv_len ? 0x7fffffff : p.causal ? key - off - q0 : 0;       // first column of this row that is not masked
+      const int warp_from = k0 + (warp & 3) * 32 + 31 >= kv_len ? 0x7fffffff : p.causal ? key - lane + 31 - off - q0 : 0;
+      if (!wait(&full[stage], (n / L::kStages) & 1)) break;          // the statistics are this thread's to read
+      if (!wait(s_full, n & 1)) break;
+      float pr[64];
+      {
+        uint32_t s[2][32];
+        tmem_ld32(s_at, s[0]);
+        tmem_ld32(s_at + 32, s[1]);
+        tmem_wait_ld();
+#pragma unroll
+        for (int g = 0; g < 16; ++g) {
+          const float4 l = lse2[g];
+          const float lv[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) pr[4 * g + e] = exp2_fast(fmaf(__uint_as_float(s[g / 8][(4 * g + e) & 31]), p.scale_log2, -lv[e]));
+        }
+      }
+      if (warp_from > 0) {
+#pragma unroll
+        for (int e = 0; e < 64; ++e) pr[e] = e >= from ? pr[e] : 0.f;
+      }
+      {
+        uint32_t w[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) w[e] = pack16<BF16>(pr[2 * e], pr[2 * e + 1]);
+        tmem_st32(s_at, w);
+        tmem_wait_st();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_one(p_full);
+      if (!wait(dp_full, n & 1)) break;
+      {
+        uint32_t d[2][32];
+        tmem_ld32(dp_at, d[0]);
+        tmem_ld32(dp_at + 32, d[1]);
+        tmem_wait_ld();
+        uint32_t w[32];
+#pragma unroll
+        for (int g = 0; g < 16; ++g) {
+          const float4 l = delta[g];
+          const float lv[4] = {l.x, l.y, l.z, l.w};
+          float ds[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ds[e] = pr[4 * g + e] * (__uint_as_float(d[g / 8][(4 * g + e) & 31]) - lv[e]);
+          w[2 * g] = pack16<BF16>(ds[0], ds[1]);
+          w[2 * g + 1] = pack16<BF16>(ds[2], ds[3]);
+        }
+        tmem_st32(dp_at, w);
+        tmem_wait_st();
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_one(ds_full);
+    }
+    const bool live = key < p.Sk;
+    if (items > 0) {
+      if (ok) wait(done, 0);
+      if (ok) {
+        if (half == 0) attn_store_row<D, BF16>(p, p.out1, t_dv + lanes, batch, kv_head, key, live, 1.f);
+        else attn_store_row<D, BF16>(p, p.out0, t_dk + lanes, batch, kv_head, key, live, p.scale);
+      } else {
+        s_abort = 1;
+      }
+    } else if (live) {
+      attn_zero_row(p, half == 0 ? p.out1 : p.out0, batch, kv_head, key);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (s_abort && threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// ----------------------------------------------------------------------------------------------
+// dQ.  A block owns 128 queries of one head and walks over the key tiles, recomputing S and dP: with
+// seven products in all instead of five, but no sum across blocks (adding dQ from the key blocks would
+// need fp32 atomics, whose order changes the result, or a pass over fp32 partial sums).
+// Tensor memory: S twice, dP, dQ.  S(j+1) and dP(j+1) run beside the elementwise phase of tile j, and
+// dQ += dS(j) K(j), with dS in the place of S(j), beside that of tile j+1.
+// ----------------------------------------------------------------------------------------------
+template <int D> struct AttnDqSmem {
+  static constexpr uint32_t kT = AttnTile<D>::kBytes;
+  static constexpr int kKs = D == 128 ? 3 : 5, kVs = D == 128 ? 2 : 4;
+  static constexpr uint32_t kK = 2 * kT, kV = kK + kKs * kT, kBars = kV + kVs * kT, kBytes = kBars + 256 + 1024;
+};
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
+               const __grid_constant__ CUtensorMap mdo, const AttnParams p) {
+  extern __shared__ unsigned char smem_dyn[];
+  using L = AttnDqSmem<D>;
+  unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
+  uint64_t* q_full = reinterpret_cast<uint64_t*>(smem + L::kBars);
+  uint64_t* k_full = q_full + 1;                 // [kKs]
+  uint64_t* k_free = k_full + L::kKs;            // [kKs]
+  uint64_t* v_full = k_free + L::kKs;            // [kVs]
+  uint64_t* v_free = v_full + L::kVs;            // [kVs]
+  uint64_t* s_full = v_free + L::kVs;            // [2]
+  uint64_t* dp_full = s_full + 2;
+  uint64_t* dp_read = dp_full + 1;
+  uint64_t* ds_full = dp_read + 1;
+  uint64_t* done = ds_full + 1;
+  uint64_t* drain = done + 1;
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_abort;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int head = blockIdx.y, batch = blockIdx.z;
+  const int q0 = (gridDim.x - 1 - blockIdx.x) * kAttnTile;
+
+  if (threadIdx.x == 0) {
+    mbar_init(q_full, 1);
+    for (int s = 0; s < L::kKs; ++s) { mbar_init(&k_full[s], 1); mbar_init(&k_free[s], 1); }
+    for (int s = 0; s < L::kVs; ++s) { mbar_init(&v_full[s], 1); mbar_init(&v_free[s], 1); }
+    mbar_init(&s_full[0], 1);
+    mbar_init(&s_full[1], 1);
+    mbar_init(dp_full, 1);
+    mbar_init(dp_read, 8);
+    mbar_init(ds_full, 8);
+    mbar_init(done, 1);
+    mbar_init(drain, 1);
+    s_abort = 0;
+    mbar_init_fence();
+    fence_proxy_async_smem();
+  }
+  if (warp == 9) tmem_alloc(&s_tmem, 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  const uint32_t t_dp = tmem + 256, t_dq = tmem + 384;
+  const int kv_len = attn_kv_len(p, batch);
+  const int off = p.Sk - p.Sq;
+  const int q_last = min(q0 + kAttnTile, p.Sq) - 1;
+  const int seen = p.causal ? min(kv_len, max(0, q_last + off + 1)) : kv_len;
+  const int tiles = (seen + kAttnTile - 1) / kAttnTile;
+  pdl_wait();
+
+  if (tiles > 0 && warp == 8) {
+    if (lane == 0) {
+      mbar_expect_tx(q_full, 2 * L::kT);
+      attn_load_tile<D>(smem, &mq, q_full, q0, head, batch);
+      attn_load_tile<D>(smem + L::kT, &mdo, q_full, q0, head, batch);
+      const int kv_head = head / (p.Hq / p.Hkv);
+      int issued = 0;
+      for (int j = 0; j < tiles; ++j) {
+        const int ks = j % L::kKs, vs = j % L::kVs;
+        if (s_abort || !mbar_wait_bounded(&k_free[ks], ((j / L::kKs) & 1) ^ 1)) { s_abort = 1; break; }
+        mbar_expect_tx(&k_full[ks], L::kT);
+        attn_load_tile<D>(smem + L::kK + ks * L::kT, &mk, &k_full[ks], j * kAttnTile, kv_head, batch);
+        issued = 2 * j + 1;
+        if (s_abort || !mbar_wait_bounded(&v_free[vs], ((j / L::kVs) & 1) ^ 1)) { s_abort = 1; break; }
+        mbar_expect_tx(&v_full[vs], L::kT);
+        attn_load_tile<D>(smem + L::kV + vs * L::kT, &mv, &v_full[vs], j * kAttnTile, kv_head, batch);
+        issued = 2 * j + 2;
+      }
+      if (s_abort) {
+        mbar_wait_bounded(q_full, 0);
+        const int nk = (issued + 1) / 2, nv = issued / 2;
+        for (int s = 0; s < L::kKs && s < nk; ++s) mbar_wait_bounded(&k_full[s], ((nk - 1 - s) / L::kKs) & 1);
+        for (int s = 0; s < L::kVs && s < nv; ++s) mbar_wait_bounded(&v_full[s], ((nv - 1 - s) / L::kVs) & 1);
+      }
+    }
+  } else if (tiles > 0 && warp == 9) {
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = ok && !s_abort && mbar_wait_bounded(bar, parity);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      return ok;
+    };
+    const uint32_t sq = smem_addr(smem), sdo = sq + L::kT;
+    auto scores = [&](int j) {                   // S(j)
+      const int ks = j % L::kKs;
+      if (!wait(&k_full[ks], (j / L::kKs) & 1)) return;
+      unsigned char* at = smem + L::kK + ks * L::kT;
+      if ((j + 1) * kAttnTile > kv_len) attn_zero_rows<D>(at, kv_len - j * kAttnTile);
+      if (lane == 0) {
+        attn_mma_rows<D, BF16>(tmem + (j & 1) * 128, sq, smem_addr(at));
+        mma_commit(&s_full[j & 1]);
+      }
+      __syncwarp();
+    };
+    auto dprobs = [&](int j) {                   // dP(j)
+      const int vs = j % L::kVs;
+      if (!wait(&v_full[vs], (j / L::kVs) & 1)) return;
+      unsigned char* at = smem + L::kV + vs * L::kT;
+      if ((j + 1) * kAttnTile > kv_len) attn_zero_rows<D>(at, kv_len - j * kAttnTile);
+      if (lane == 0) {
+        attn_mma_rows<D, BF16>(t_dp, sdo, smem_addr(at));
+        mma_commit(dp_full);
+        mma_commit(&v_free[vs]);
+      }
+      __syncwarp();
+    };
+    if (wait(q_full, 0)) {
+      scores(0);
+      if (ok) dprobs(0);
+    }
+    for (int j = 0; ok && j < tiles; ++j) {
+      if (j + 1 < tiles) {
+        scores(j + 1);
+        if (!ok || !wait(dp_read, j & 1)) break;
+        dprobs(j + 1);
+        if (!ok) break;
+      }
+      if (!wait(ds_full, j & 1)) break;
+      if (lane == 0) {
+        attn_mma_tokens<D, BF16>(t_dq, tmem + (j & 1) * 128, 64, smem_addr(smem + L::kK + (j % L::kKs) * L::kT), j != 0);
+        mma_commit(&k_free[j % L::kKs]);
+        if (j == tiles - 1) mma_commit(done);
+      }
+      __syncwarp();
+    }
+    if (!ok) {
+      s_abort = 1;
+      if (lane == 0) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
+    }
+  } else if (warp < 8) {
+    const int half = warp >> 2;                  // this warp's 64 keys of each tile
+    const int row = q0 + (warp & 3) * 32 + lane;
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const long long stat = (static_cast<long long>(batch) * p.Hq + head) * p.sq_pad + row;      // rows are padded: always there
+    const float lse2 = p.lse2[stat], delta = p.delta[stat];
+    const int limit = p.causal ? min(kv_len, row + off + 1) : kv_len;
+    const int warp_limit = p.causal ? min(kv_len, row - lane + off + 1) : kv_len;
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = !s_abort && mbar_wait_bounded(bar, parity);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      return ok;
+    };
+    for (int j = 0; j < tiles; ++j) {
+      const uint32_t s_at = tmem + (j & 1) * 128 + lanes + half * 64, dp_at = t_dp + lanes + half * 64;
+      const int k0 = j * kAttnTile + half * 64;
+      if (!wait(&s_full[j & 1], (j >> 1) & 1)) break;
+      float pr[64];
+      {
+        uint32_t s[2][32];
+        tmem_ld32(s_at, s[0]);
+        tmem_ld32(s_at + 32, s[1]);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 64; ++e) pr[e] = exp2_fast(fmaf(__uint_as_float(s[e / 32][e & 31]), p.scale_log2, -lse2));
+      }
+      if (k0 + 64 > warp_limit) {
+#pragma unroll
+        for (int e = 0; e < 64; ++e) pr[e] = k0 + e < limit ? pr[e] : 0.f;
+      }
+      if (!wait(dp_full, j & 1)) break;
+      uint32_t w[32];
+      {
+        uint32_t d[2][32];
+        tmem_ld32(dp_at, d[0]);
+        tmem_ld32(dp_at + 32, d[1]);
+        tmem_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_one(dp_read);
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+          w[e] = pack16<BF16>(pr[2 * e] * (__uint_as_float(d[e / 16][(2 * e) & 31]) - delta), pr[2 * e + 1] * (__uint_as_float(d[e / 16][(2 * e + 1) & 31]) - delta));
+      }
+      tmem_st32(s_at, w);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_one(ds_full);
+    }
+    const bool live = row < p.Sq;
+    if (tiles > 0) {
+      if (ok) wait(done, 0);
+      if (ok && half == 0) attn_store_row<D, BF16>(p, p.out0, t_dq + lanes, batch, head, row, live, p.scale);
+      if (!ok) s_abort = 1;
+    } else if (live && half == 0) {
+      attn_zero_row(p, p.out0, batch, head, row);
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (s_abort && threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
+  if (warp == 9) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+}  // namespace adacons
