@@ -112,6 +112,39 @@ int adacons_attn_backward(const adacons_attn_shape *shape, const adacons_attn_te
  * call (results since are invalid); clears it.  Synchronises `cuda_stream`. */
 int adacons_attn_get_status(uint32_t *flags, void *cuda_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Rotary positions.
+ *
+ * Pair i of a head at position t is turned by the angle t f_i and multiplied by `gain`:
+ *     (a, b) -> gain (a cos - b sin, a sin + b cos)
+ * with (a, b) = elements (i, i + rot/2) of the head or, interleaved, (2i, 2i+1).  Elements from `rot` on
+ * pass through unchanged.  The gradient of the turn is the turn by the negative angle with the same gain:
+ * inverse = 1.
+ *   rot          even, 2 .. 4096: the rotated elements of a head.
+ *   frequencies  host array of rot/2 angles per position, in radians; any scaling for long contexts is in
+ *                them.  The angle is formed and reduced in fp64: positions up to 2^31 keep their precision.
+ * Errors: EINVAL, ELIMIT, ENOMEM, ECUDA, EARCH.
+ */
+typedef struct adacons_rope adacons_rope;
+int adacons_rope_create(adacons_rope **out, int rot, const double *frequencies, double gain, int interleaved);
+
+typedef struct adacons_rope_shape {
+  int dtype;                 /* ADACONS_F32 or ADACONS_BF16 */
+  int batch, len, heads;     /* heads * head_dim up to 2^26 */
+  int head_dim;              /* >= rot */
+} adacons_rope_shape;
+
+/* x, y: (batch, token, head, element) with the element stride 1; x_strides, y_strides: host arrays of the
+ * other three strides in elements, any values.  y may be x with the same strides, otherwise they must not overlap.
+ * positions: device pointer to batch * len values in that order (contiguous), or NULL: token s of every
+ * sequence is at position first + s.  16-byte aligned data whose strides and rot, head_dim are multiples of
+ * 16 bytes (rot of 32) are moved in vectors, anything else element by element.  Errors: EINVAL, ELIMIT, ECUDA. */
+int adacons_rope_apply(adacons_rope *ctx, const adacons_rope_shape *shape, const void *x, const int64_t *x_strides, void *y,
+                       const int64_t *y_strides, const int32_t *positions, int64_t first, int inverse, void *cuda_stream);
+
+/* NULL is accepted. */
+int adacons_rope_destroy(adacons_rope *ctx);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,7 +8,7 @@ from . import workloads  # noqa: F401
 
 
 _LAZY = {"AdaCons": "binding", "AdaConsError": "binding", "load_library": "binding", "Orthogonalizer": "orth",
-         "attention_forward": "attention", "attention_backward": "attention"}
+         "attention_forward": "attention", "attention_backward": "attention", "Rope": "rope"}
 
 
 def __getattr__(name):

@@ -85,6 +85,9 @@ def load_library() -> ctypes.CDLL:
         "adacons_attn_workspace_bytes": [vp, P(i64)],
         "adacons_attn_backward": [vp] * 11 + [i64, vp],
         "adacons_attn_get_status": [P(ctypes.c_uint32), vp],
+        "adacons_rope_create": [P(vp), i32, P(dbl), dbl, i32],
+        "adacons_rope_apply": [vp, vp, vp, P(i64), vp, P(i64), vp, i64, i32, vp],
+        "adacons_rope_destroy": [vp],
     }
     for name, args in protos.items():
         fn = getattr(lib, name)

@@ -24,6 +24,7 @@ SOURCES = {
                                                    "adacons_fused.cuh", "adacons_gram.cuh", "adacons_shift.cuh")],
     "adacons_orth.cu": _OPS + ["csrc/adacons_orth.cuh"],
     "adacons_attn.cu": _OPS + ["csrc/adacons_attn.cuh"],
+    "adacons_rope.cu": _OPS + ["csrc/adacons_rope.cuh"],
 }
 
 
