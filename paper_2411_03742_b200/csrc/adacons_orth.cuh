@@ -21,7 +21,7 @@ namespace adacons {
 // a X takes the pair; in an fp32 context S and B are pairs too and each product is the sum
 // (lo hi + hi lo) + hi hi.  The tensor cores round a running sum toward zero, low by up to 4e-8 of it
 // per chained product: harmless beside an 11-bit operand, but 4e-5 of an fp32 result after five steps
-// on sides of 1024.  There the hi hi terms are chained over 256 K elements at most and the chunks'
+// on sides of 1024.  There the hi hi terms are chained over 128 K elements at most and the chunks'
 // sums added by the epilogue, round to nearest (the small terms, 2^-11 of the sum, in one accumulator).
 // Why not bf16 operands: rounding the iterates to 8 bits costs 1e-2 of the result's norm on a
 // Gaussian matrix and 1e-1 on one with a few strong directions (the small singular values grow
@@ -33,7 +33,7 @@ namespace adacons {
 // matrices (on a matrix of rank 8 plus noise 5e-4 instead of 1.5e-4, still a third of the rounding).
 // ----------------------------------------------------------------------------------------------
 constexpr int kOrthTK = 64;              // K elements per stage: one 128-byte swizzled row
-constexpr int kOrthChunk = 4;            // fp32 contexts: stages (256 K elements) per hi hi accumulator
+constexpr int kOrthChunk = 2;            // fp32 contexts: stages (128 K elements) per hi hi accumulator
 constexpr float kOrthXScale = 2048.f, kOrthSScale = 8192.f, kOrthBScale = 2048.f;
 constexpr int kOrthThreads = 352;        // warps 0-7 epilogue, 8 operand copies, 9 products, 10 epilogue copies
 constexpr int kOrthNormChunk = 16384;    // elements per block of the norm kernel

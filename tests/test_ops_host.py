@@ -1,0 +1,174 @@
+"""CPU-only checks of the training operators' boundary: the library exports what include/adacons_ops.h
+declares, the binding has a prototype for each, bad arguments are refused with a code before any device
+is touched, and the rotary angles of every scaling are what their formulas say."""
+import ctypes
+import math
+import os
+import re
+
+import pytest
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+EINVAL, EALIGN, ELIMIT = 1, 2, 7
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2411_03742_b200 import binding, build
+    build.build()
+    return binding.load_library()
+
+
+def declared():
+    text = open(os.path.join(ROOT, "include", "adacons_ops.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    return sorted(set(re.findall(r"\b(adacons_(?:orth|attn|rope)_[a-z_0-9]+)\s*\(", text)))
+
+
+def test_every_declared_function_is_exported_and_has_a_prototype(lib):
+    names = declared()
+    assert len(names) == 12, names
+    for name in names:
+        assert getattr(lib, name).argtypes is not None, name
+
+
+def test_header_compiles_as_c99(tmp_path):
+    import shutil
+    import subprocess
+    src = tmp_path / "use.c"
+    src.write_text('#include "adacons_ops.h"\nint main(void) { adacons_attn_shape s; (void)s; return ADACONS_F16 == 2 ? 0 : 1; }\n')
+    cc = shutil.which("gcc") or shutil.which("cc")
+    assert cc
+    subprocess.run([cc, "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), "-c", str(src), "-o", str(tmp_path / "use.o")], check=True)
+
+
+def _orth(lib, dtype=1, d=100, rows=(5,), cols=(7,), offsets=(0,), scaling=0, steps=1, coeffs=(1.0, 0.0, 0.0), eps=0.0, num=None):
+    n = len(rows)
+    i64 = ctypes.c_int64 * n
+    ctx = ctypes.c_void_p()
+    return lib.adacons_orth_create(ctypes.byref(ctx), dtype, d, n if num is None else num, i64(*rows), i64(*cols), i64(*offsets), scaling, steps,
+                                   (ctypes.c_double * len(coeffs))(*coeffs), eps)
+
+
+@pytest.mark.parametrize("bad, code", [
+    (dict(dtype=2), EINVAL), (dict(d=0), EINVAL), (dict(num=0), EINVAL), (dict(rows=(0,)), EINVAL), (dict(cols=(-1,)), EINVAL),
+    (dict(offsets=(-1,)), EINVAL), (dict(offsets=(66,)), EINVAL), (dict(rows=(50,)), EINVAL),
+    (dict(rows=(5, 5), cols=(7, 7), offsets=(0, 34)), EINVAL), (dict(scaling=2), EINVAL), (dict(steps=0), EINVAL), (dict(steps=65), EINVAL),
+    (dict(coeffs=(1.0, math.nan, 0.0)), EINVAL), (dict(eps=-1.0), EINVAL), (dict(eps=math.inf), EINVAL),
+    (dict(d=1 << 40, rows=((1 << 18) + 1,), cols=(1,)), ELIMIT),
+])
+def test_orth_refusals(lib, bad, code):
+    assert _orth(lib, **bad) == code
+
+
+def test_orth_null_pointers(lib):
+    assert lib.adacons_orth_create(None, 1, 1, 1, None, None, None, 0, 1, None, 0.0) == EINVAL
+    assert lib.adacons_orth_apply(None, None, None, None) == EINVAL
+    assert lib.adacons_orth_destroy(None) == 0
+
+
+def _attn(lib, data=1 << 20, strides=(64, 64, 64), **change):
+    from paper_2411_03742_b200.attention import _Shape, _Tensor
+    fields = dict(dtype=1, batch=2, q_heads=4, kv_heads=2, q_len=3, kv_len=5, head_dim=64, causal=0, scale=0.125, kv_lens=None)
+    fields.update(change)
+    s, t = _Shape(**fields), _Tensor(data, *strides)
+    r = ctypes.byref
+    n = ctypes.c_int64()
+    return (lib.adacons_attn_forward(r(s), r(t), r(t), r(t), r(t), None, None),
+            lib.adacons_attn_backward(r(s), r(t), r(t), r(t), r(t), r(t), None, r(t), r(t), r(t), None, 0, None),
+            lib.adacons_attn_workspace_bytes(r(s), r(n)))
+
+
+@pytest.mark.parametrize("bad, code", [
+    (dict(dtype=0), EINVAL), (dict(dtype=3), EINVAL), (dict(batch=-1), EINVAL), (dict(q_heads=0), EINVAL), (dict(q_heads=3), EINVAL), (dict(kv_heads=0), EINVAL),
+    (dict(q_len=-1), EINVAL), (dict(kv_len=-1), EINVAL), (dict(head_dim=60), EINVAL), (dict(head_dim=0), EINVAL), (dict(scale=0.0), EINVAL),
+    (dict(scale=math.nan), EINVAL), (dict(scale=-1.0), EINVAL), (dict(causal=2), EINVAL), (dict(head_dim=136), ELIMIT), (dict(batch=65536), ELIMIT),
+])
+def test_attention_refuses_bad_shapes(lib, bad, code):
+    assert _attn(lib, **bad) == (code, code, code)
+
+
+@pytest.mark.parametrize("bad, code", [
+    (dict(data=None), EINVAL), (dict(data=(1 << 20) + 8), EALIGN), (dict(strides=(64, 4, 64)), EALIGN), (dict(strides=(0, 64, 64)), EINVAL),
+    (dict(strides=(-64, 64, 64)), EINVAL), (dict(), EINVAL),          # the last: no lse, no workspace
+])
+def test_attention_refuses_bad_tensors(lib, bad, code):
+    assert _attn(lib, **bad)[:2] == (code, code)
+
+
+def test_attention_without_work_succeeds_without_a_device(lib):
+    assert _attn(lib, batch=0, data=None) == (0, 0, 0)
+    assert _attn(lib, q_len=0, kv_len=0, data=None) == (0, 0, 0)
+
+
+def test_rope_refusals(lib):
+    ctx = ctypes.c_void_p()
+    f = (ctypes.c_double * 2)(1.0, 0.5)
+    assert lib.adacons_rope_create(None, 4, f, 1.0, 0) == EINVAL
+    assert lib.adacons_rope_create(ctypes.byref(ctx), 3, f, 1.0, 0) == EINVAL
+    assert lib.adacons_rope_create(ctypes.byref(ctx), 0, f, 1.0, 0) == EINVAL
+    assert lib.adacons_rope_create(ctypes.byref(ctx), 4, f, math.inf, 0) == EINVAL
+    assert lib.adacons_rope_create(ctypes.byref(ctx), 4, f, 1.0, 2) == EINVAL
+    assert lib.adacons_rope_create(ctypes.byref(ctx), 4, (ctypes.c_double * 2)(1.0, math.nan), 1.0, 0) == EINVAL
+    assert lib.adacons_rope_create(ctypes.byref(ctx), 8192, f, 1.0, 0) == ELIMIT
+    assert lib.adacons_rope_apply(None, None, None, None, None, None, None, 0, 0, None) == EINVAL
+    assert lib.adacons_rope_destroy(None) == 0
+
+
+def test_binding_checks():
+    from paper_2411_03742_b200 import attention, orth, rope
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(*s, dtype=dt)  # noqa: E731
+    q, k = z(2, 5, 4, 16), z(2, 7, 2, 16)
+    ok = dict(want_cuda=False)
+    attention.check_attention(q, k, k, **ok)
+    packed = z(2, 5, 8, 16)
+    attention.check_attention(packed[:, :, :4], packed[:, :, 4:6], packed[:, :, 6:], **ok)
+    for bad in [(q[0], k, k), (q.float(), k, k), (q, k, z(2, 8, 2, 16)), (q, z(2, 7, 3, 16), z(2, 7, 3, 16)), (z(2, 5, 4, 12), z(2, 7, 2, 12), z(2, 7, 2, 12)),
+                (z(2, 5, 4, 136), z(2, 7, 2, 136), z(2, 7, 2, 136)), (q, z(1, 7, 2, 16), z(1, 7, 2, 16)), (q, k, k.half()), (z(2, 5, 4, 32)[..., ::2], k, k),
+                (z(2, 5, 4, 20)[..., :16], k, k), (z(2, 1, 4, 16).expand(2, 5, 4, 16), k, k)]:
+        with pytest.raises(ValueError):
+            attention.check_attention(*bad, **ok)
+    with pytest.raises(ValueError):
+        attention.check_attention(q, k, k, torch.zeros(2, dtype=torch.int64), **ok)
+    with pytest.raises(ValueError):
+        attention.check_attention(q, k, k, torch.zeros(3, dtype=torch.int32), **ok)
+    with pytest.raises(ValueError):
+        attention.check_attention(q, k, k, rows=[("lse", torch.zeros(2, 5, 4))], **ok)
+    with pytest.raises(ValueError):
+        attention.check_attention(q, k, k)                                    # not on a device
+    orth.check_vectors(10, "bf16", z(10), z(10), want_cuda=False)
+    for bad in [(z(9), z(10)), (z(10), z(10, dt=torch.float32)), (z(20)[::2], z(10)), (z(2, 5), z(10))]:
+        with pytest.raises(ValueError):
+            orth.check_vectors(10, "bf16", *bad, want_cuda=False)
+    x = z(2, 5, 4, 16)
+    rope.check_rope(16, x, None, x, want_cuda=False)
+    for bad in [(20, x, None, x), (16, x[0], None, x[0]), (16, x.half(), None, x.half()), (16, x, None, z(2, 5, 4, 18)), (16, x, torch.zeros(2, 5), x),
+                (16, x, None, z(2, 1, 4, 16).expand(2, 5, 4, 16)), (16, z(2, 5, 4, 32)[..., ::2], None, x)]:
+        with pytest.raises(ValueError):
+            rope.check_rope(*bad, want_cuda=False)
+
+
+def test_rotary_frequencies():
+    from paper_2411_03742_b200.rope import frequencies
+    f, g = frequencies(8, 100.0)
+    assert g == 1.0 and f == pytest.approx([1.0, 100 ** -0.25, 0.1, 100 ** -0.75], rel=1e-14)
+    lin, g = frequencies(8, 100.0, ("linear", 4.0))
+    assert g == 1.0 and lin == pytest.approx([x / 4 for x in f], rel=1e-14)
+    ntk, g = frequencies(64, 10000.0, ("ntk", 8.0))
+    plain, _ = frequencies(64, 10000.0)
+    assert g == 1.0 and ntk[0] == 1.0 and ntk[-1] == pytest.approx(plain[-1] / 8.0, rel=1e-12)   # the definition: the slowest pair, eight times slower
+    yarn, g = frequencies(64, 10000.0, ("yarn", 16.0, 4096))
+    assert g == pytest.approx(0.1 * math.log(16.0) + 1.0, rel=1e-15)
+    turns = [4096 * x / (2 * math.pi) for x in plain]
+    for t, x, y in zip(turns, plain, yarn):
+        if t > 40:
+            assert y == pytest.approx(x, rel=1e-14)
+        elif t < 0.8:
+            assert y == pytest.approx(x / 16, rel=1e-14)
+        else:
+            assert x / 16 * (1 - 1e-12) <= y <= x * (1 + 1e-12)
+    assert frequencies(8, 100.0, ("linear", 1.0))[0] == f
+    for bad in [dict(dim=3), dict(dim=0), dict(dim=8, base=0.0), dict(dim=8, scaling=("linear", 0.5)), dict(dim=8, scaling=("what", 2.0)), dict(dim=2, scaling=("ntk", 2.0))]:
+        with pytest.raises(ValueError):
+            frequencies(**bad)
