@@ -9,8 +9,11 @@ from __future__ import annotations
 
 import ctypes
 import math
+import threading
 
-from .binding import BF16, _check, _stream_handle, load_library
+import torch
+
+from .binding import BF16, _check, _raw_stream, _stream_handle, load_library
 
 F16 = 2
 
@@ -24,18 +27,37 @@ class _Shape(ctypes.Structure):
                 ("kv_len", ctypes.c_int), ("head_dim", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float), ("kv_lens", ctypes.c_void_p)]
 
 
-def _arg(t):
-    st = t.stride()
-    return ctypes.byref(_Tensor(t.data_ptr(), st[0], st[1], st[2]))
+class _Plans(threading.local):
+    """Per thread: the argument blocks of layouts that have passed the checks.  Only the data pointers change between
+    calls, and nothing of a call is kept but its layout."""
+
+    def __init__(self):
+        self.known = {}
 
 
-_checked = set()        # layouts that have passed check_attention
+_plans = _Plans()
+
+
+class _Plan:
+    """Shape and tensor blocks of one layout, and references to them for the call."""
+
+    def __init__(self, shape, tensors):
+        self.shape, self.shape_ref = shape, ctypes.byref(shape)
+        self.blocks = [_Tensor(None, *t.stride()[:3]) for t in tensors]
+        self.refs = [ctypes.byref(b) for b in self.blocks]
+        self.workspace = 0
+
+
+def _remember(sig, plan):
+    if len(_plans.known) >= 1024:        # a program with ever new lengths
+        _plans.known.clear()
+    _plans.known[sig] = plan
+    return plan
 
 
 def check_attention(q, k, v, kv_lens=None, like_q=(), like_k=(), rows=(), want_cuda: bool = True) -> None:
     """Raise ValueError unless q, k, v (and what is shaped like them) are 4-D tensors of one 16-bit type on one
     device whose sizes fit together; rows: (batch, q_heads, q_len) fp32 tensors; kv_lens: int32 (batch,)."""
-    import torch
     if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
         raise ValueError("q, k and v must have four dimensions: batch, token, head, element")
     if q.dtype not in (torch.bfloat16, torch.float16):
@@ -63,11 +85,10 @@ def check_attention(q, k, v, kv_lens=None, like_q=(), like_k=(), rows=(), want_c
 
 
 def _layout(t):
-    return None if t is None else (t.dtype, t.shape, t.stride(), t.device)
+    return None if t is None else (t.dtype, t.shape, t.stride(), t.get_device())
 
 
 def _shape(q, k, scale, causal, kv_lens):
-    import torch
     B, Sq, Hq, D = q.shape
     return _Shape(BF16 if q.dtype == torch.bfloat16 else F16, B, Hq, k.shape[2], Sq, k.shape[1], D, int(bool(causal)),
                   1.0 / math.sqrt(D) if scale is None else float(scale), None if kv_lens is None else kv_lens.data_ptr())
@@ -76,18 +97,21 @@ def _shape(q, k, scale, causal, kv_lens):
 def attention_forward(q, k, v, *, scale=None, causal: bool = False, kv_lens=None, out=None, lse=None, stream=None):
     """(out, lse): out = softmax(scale q k^T + mask) v, shaped like q, and the rows' log-sum-exp, (batch,
     q_heads, q_len) fp32.  scale defaults to head_dim^-1/2; kv_lens (int32) hides each batch's keys from there on."""
-    import torch
+    sig = (_layout(q), _layout(k), _layout(v), _layout(kv_lens), scale, causal, _layout(out), _layout(lse))
+    plan = _plans.known.get(sig)
+    if plan is None:
+        check_attention(q, k, v, kv_lens, like_q=[] if out is None else [("out", out)], rows=[] if lse is None else [("lse", lse)])
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None:
-        lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
-    sig = (_layout(q), _layout(k), _layout(v), _layout(out), _layout(lse), _layout(kv_lens))
-    if sig not in _checked:
-        check_attention(q, k, v, kv_lens, like_q=[("out", out)], rows=[("lse", lse)])
-        _checked.add(sig)
-    shape = _shape(q, k, scale, causal, kv_lens)
-    _check(load_library().adacons_attn_forward(ctypes.byref(shape), _arg(q), _arg(k), _arg(v), _arg(out), lse.data_ptr(), _stream_handle(stream)),
-           "adacons_attn_forward")
+        lse = q.new_empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32)
+    if plan is None:
+        plan = _remember(sig, _Plan(_shape(q, k, scale, causal, kv_lens), (q, k, v, out)))
+    if kv_lens is not None:
+        plan.shape.kv_lens = kv_lens.data_ptr()
+    for block, t in zip(plan.blocks, (q, k, v, out)):
+        block.data = t.data_ptr()
+    _check(load_library().adacons_attn_forward(plan.shape_ref, *plan.refs, lse.data_ptr(), _raw_stream(stream, sig[0][3])), "adacons_attn_forward")
     return out, lse
 
 
@@ -103,23 +127,29 @@ def attention_backward(dout, q, k, v, out, lse, *, scale=None, causal: bool = Fa
     """(dq, dk, dv) of attention_forward with the same scale, causal and kv_lens, from its out and lse and the
     gradient dout.  workspace: a uint8 tensor of workspace_bytes(q, k), made here if not given (a call on a
     stream other than the current one should bring its own)."""
-    import torch
-    dq = torch.empty(q.shape, dtype=q.dtype, device=q.device) if dq is None else dq
-    dk = torch.empty(k.shape, dtype=k.dtype, device=k.device) if dk is None else dk
-    dv = torch.empty(v.shape, dtype=v.dtype, device=v.device) if dv is None else dv
+    sig = (_layout(q), _layout(k), _layout(v), _layout(kv_lens), scale, causal, _layout(out), _layout(lse), _layout(dout), _layout(dq), _layout(dk), _layout(dv))
+    plan = _plans.known.get(sig)
+    if plan is None:
+        check_attention(q, k, v, kv_lens, like_q=[(n, t) for n, t in (("dout", dout), ("out", out), ("dq", dq)) if t is not None],
+                        like_k=[(n, t) for n, t in (("dk", dk), ("dv", dv)) if t is not None], rows=[("lse", lse)])
+    dq = torch.empty_like(q, memory_format=torch.contiguous_format) if dq is None else dq
+    dk = torch.empty_like(k, memory_format=torch.contiguous_format) if dk is None else dk
+    dv = torch.empty_like(v, memory_format=torch.contiguous_format) if dv is None else dv
+    if plan is None:
+        plan = _Plan(_shape(q, k, scale, causal, kv_lens), (dout, q, k, v, out, dq, dk, dv))
+        plan.workspace = workspace_bytes(q, k)
+        _remember(sig, plan)
     if workspace is None:
-        B, Sq, Hq, _ = q.shape
-        workspace = torch.empty(8 * B * Hq * ((Sq + 127) // 128 * 128), dtype=torch.uint8, device=q.device)
-    sig = (_layout(q), _layout(k), _layout(v), _layout(out), _layout(lse), _layout(kv_lens), _layout(dout), _layout(dq), _layout(dk), _layout(dv))
-    if sig not in _checked:
-        check_attention(q, k, v, kv_lens, like_q=[("dout", dout), ("out", out), ("dq", dq)], like_k=[("dk", dk), ("dv", dv)], rows=[("lse", lse)])
-        _checked.add(sig)
-    if workspace.device != q.device or not workspace.is_contiguous():
+        workspace = lse.new_empty(plan.workspace // 4)
+    elif workspace.get_device() != sig[0][3] or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous on q's device")
-    shape = _shape(q, k, scale, causal, kv_lens)
-    _check(load_library().adacons_attn_backward(ctypes.byref(shape), _arg(dout), _arg(q), _arg(k), _arg(v), _arg(out), lse.data_ptr(), _arg(dq), _arg(dk),
-                                                _arg(dv), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_handle(stream)),
-           "adacons_attn_backward")
+    if kv_lens is not None:
+        plan.shape.kv_lens = kv_lens.data_ptr()
+    for block, t in zip(plan.blocks, (dout, q, k, v, out, dq, dk, dv)):
+        block.data = t.data_ptr()
+    r = plan.refs
+    _check(load_library().adacons_attn_backward(plan.shape_ref, r[0], r[1], r[2], r[3], r[4], lse.data_ptr(), r[5], r[6], r[7], workspace.data_ptr(),
+                                                workspace.numel() * workspace.element_size(), _raw_stream(stream, sig[0][3])), "adacons_attn_backward")
     return dq, dk, dv
 
 
@@ -132,32 +162,21 @@ def status(stream=None) -> int:
 
 def attention(q, k, v, *, scale=None, causal: bool = False, kv_lens=None):
     """attention_forward's out as a differentiable function of q, k and v."""
-    return _function().apply(q, k, v, scale, causal, kv_lens)
+    return _Attention.apply(q, k, v, scale, causal, kv_lens)
 
 
-_FUNCTION = None
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, scale, causal, kv_lens):
+        out, lse = attention_forward(q, k, v, scale=scale, causal=causal, kv_lens=kv_lens)
+        ctx.save_for_backward(q, k, v, out, lse, *([] if kv_lens is None else [kv_lens]))
+        ctx.how = (scale, causal)
+        return out
 
-
-def _function():
-    global _FUNCTION
-    if _FUNCTION is None:
-        import torch
-
-        class Attention(torch.autograd.Function):
-            @staticmethod
-            def forward(ctx, q, k, v, scale, causal, kv_lens):
-                out, lse = attention_forward(q, k, v, scale=scale, causal=causal, kv_lens=kv_lens)
-                ctx.save_for_backward(q, k, v, out, lse, *([] if kv_lens is None else [kv_lens]))
-                ctx.how = (scale, causal)
-                return out
-
-            @staticmethod
-            def backward(ctx, dout):
-                q, k, v, out, lse, *lens = ctx.saved_tensors
-                if dout.stride(3) != 1 or any(n > 1 and (s % 8 != 0 or s <= 0) for n, s in zip(dout.shape[:3], dout.stride())):
-                    dout = dout.contiguous()        # a broadcast gradient, of a sum for instance
-                dq, dk, dv = attention_backward(dout, q, k, v, out, lse, scale=ctx.how[0], causal=ctx.how[1], kv_lens=lens[0] if lens else None)
-                return dq, dk, dv, None, None, None
-
-        _FUNCTION = Attention
-    return _FUNCTION
+    @staticmethod
+    def backward(ctx, dout):
+        q, k, v, out, lse, *lens = ctx.saved_tensors
+        if dout.stride(3) != 1 or any(n > 1 and (s % 8 != 0 or s <= 0) for n, s in zip(dout.shape[:3], dout.stride())):
+            dout = dout.contiguous()        # a broadcast gradient, of a sum for instance
+        dq, dk, dv = attention_backward(dout, q, k, v, out, lse, scale=ctx.how[0], causal=ctx.how[1], kv_lens=lens[0] if lens else None)
+        return dq, dk, dv, None, None, None

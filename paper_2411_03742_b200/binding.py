@@ -115,6 +115,17 @@ def _stream_handle(stream) -> int:
     return int(stream.cuda_stream)
 
 
+def _raw_stream(stream, device_index: int) -> int:
+    """_stream_handle without building a Stream object: small calls are bound by the host."""
+    if stream is not None:
+        return int(stream.cuda_stream)
+    import torch
+    try:
+        return torch._C._cuda_getCurrentRawStream(device_index)
+    except AttributeError:
+        return int(torch.cuda.current_stream(device_index).cuda_stream)
+
+
 def stats_noalloc(grads, pq_out, stream=None) -> None:
     """p_i = <g_i, gbar> and q_i = ||g_i||^2 of an N x d CUDA tensor into `pq_out` (CUDA tensor of
     2N float64), through the entry point that allocates no device memory (N <= NOALLOC_MAX_N).

@@ -29,9 +29,8 @@ bool raise(K kernel, uint32_t bytes) {
 }
 template <int D, bool BF16>
 bool raise_all() {
-  static_assert(AttnFwdSmem<D>::kBytes <= 227 * 1024 && AttnDkvSmem<D>::kBytes <= 227 * 1024 && AttnDqSmem<D>::kBytes <= 227 * 1024, "shared memory of a block");
-  return raise(attn_forward_kernel<D, BF16>, AttnFwdSmem<D>::kBytes) && raise(attn_dkv_kernel<D, BF16>, AttnDkvSmem<D>::kBytes) &&
-         raise(attn_dq_kernel<D, BF16>, AttnDqSmem<D>::kBytes);
+  static_assert(AttnFwdSmem<D>::kBytes <= 227 * 1024 && attn_backward_smem<D>() <= 227 * 1024, "shared memory of a block");
+  return raise(attn_forward_kernel<D, BF16>, AttnFwdSmem<D>::kBytes) && raise(attn_backward_kernel<D, BF16>, attn_backward_smem<D>());
 }
 
 // The first call on a device sets the kernels' shared-memory limits; later ones only look the entry up.
@@ -131,13 +130,13 @@ bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMa
   const AttnRows a = {dout->data, dout->batch_stride, dout->seq_stride, dout->head_stride}, b = {out->data, out->batch_stride, out->seq_stride, out->head_stride};
   if (rows > 0 && !launch(&attn_delta_kernel<BF16>, dim3(static_cast<unsigned>((rows + 7) / 8)), dim3(256), 0, st, false, 1, a, b, lse, p.Hq, p.Sq, p.sq_pad, p.D, rows, lse2, delta))
     return false;
-  AttnParams pkv = p, pq = p;
-  pkv.out0 = dk;
-  pkv.out1 = dv;
-  pq.out0 = dq;
-  if (p.Sk > 0 && !launch(&attn_dkv_kernel<D, BF16>, dim3((p.Sk + kAttnTile - 1) / kAttnTile, p.Hkv, p.B), dim3(kAttnThreads), AttnDkvSmem<D>::kBytes, st, true, 1, mq, mk, mv, mdo, pkv))
-    return false;
-  return p.Sq == 0 || launch(&attn_dq_kernel<D, BF16>, dim3(p.sq_pad / kAttnTile, p.Hq, p.B), dim3(kAttnThreads), AttnDqSmem<D>::kBytes, st, true, 1, mq, mk, mv, mdo, pq);
+  p.out = dq;
+  p.dk = dk;
+  p.dv = dv;
+  const int64_t q_tiles = p.sq_pad / kAttnTile, k_tiles = (static_cast<int64_t>(p.Sk) + kAttnTile - 1) / kAttnTile;
+  const int64_t key_blocks = k_tiles * p.Hkv * p.B, blocks = key_blocks + q_tiles * p.Hq * p.B;
+  return blocks <= 0x7fffffff && launch(&attn_backward_kernel<D, BF16>, dim3(static_cast<unsigned>(blocks)), dim3(kAttnThreads), attn_backward_smem<D>(), st, true, 1,
+                                        mq, mk, mv, mdo, p, static_cast<int>(key_blocks), static_cast<int>(q_tiles));
 }
 
 int64_t workspace_bytes(const adacons_attn_shape* s) {
@@ -165,7 +164,7 @@ int adacons_attn_forward(const adacons_attn_shape* s, const adacons_attn_tensor*
       !make_map(*d, &mv, s, v, s->kv_len, s->kv_heads, q->data))
     return ADACONS_ECUDA;
   AttnParams p = base_params(*d, s);
-  p.out0 = as_out(out);
+  p.out = as_out(out);
   p.lse = lse;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   bool ok;

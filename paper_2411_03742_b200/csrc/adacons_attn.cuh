@@ -40,7 +40,7 @@ struct AttnParams {
   float* lse;                    // forward: [B][Hq][Sq]
   const float* lse2;             // backward: lse log2(e), +inf where a row has no key or does not exist: [B][Hq][sq_pad]
   const float* delta;            // likewise, 0 there
-  AttnOut out0, out1;            // forward: O; backward: dQ, or dK and dV
+  AttnOut out, dk, dv;           // forward: O; backward: dQ, dK, dV
   uint32_t* flags;
 };
 
@@ -342,9 +342,9 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       ok = !s_abort && mbar_wait_bounded(&o_full[t], 0);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
-      if (ok) attn_store_row<D, BF16>(p, p.out0, o_at, batch, head, row, live, sum == 0.f ? 0.f : 1.f / sum);
+      if (ok) attn_store_row<D, BF16>(p, p.out, o_at, batch, head, row, live, sum == 0.f ? 0.f : 1.f / sum);
     } else if (tiles == 0 && live) {
-      attn_zero_row(p, p.out0, batch, head, row);
+      attn_zero_row(p, p.out, batch, head, row);
     }
     if (ok && live) p.lse[(static_cast<long long>(batch) * p.Hq + head) * p.Sq + row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     if (!ok) s_abort = 1;
@@ -419,12 +419,9 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 }
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kAttnThreads, 1)
-attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
-                const __grid_constant__ CUtensorMap mdo, const AttnParams p) {
-  extern __shared__ unsigned char smem_dyn[];
+__device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo,
+                                               const AttnParams& p, const int tile, const int kv_head, const int batch) {
   using L = AttnDkvSmem<D>;
-  unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
   uint64_t* kv_full = reinterpret_cast<uint64_t*>(smem + L::kBars);
   uint64_t* full = kv_full + 1;                  // [kStages]
   uint64_t* free_ = full + L::kStages;           // [kStages]
@@ -437,8 +434,7 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int kv_head = blockIdx.y, batch = blockIdx.z;
-  const int k0 = blockIdx.x * kAttnTile;         // with a causal mask the first keys have the most queries: first
+  const int k0 = tile * kAttnTile;
   const int group = p.Hq / p.Hkv;
 
   if (threadIdx.x == 0) {
@@ -617,13 +613,13 @@ attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ 
     if (items > 0) {
       if (ok) wait(done, 0);
       if (ok) {
-        if (half == 0) attn_store_row<D, BF16>(p, p.out1, t_dv + lanes, batch, kv_head, key, live, 1.f);
-        else attn_store_row<D, BF16>(p, p.out0, t_dk + lanes, batch, kv_head, key, live, p.scale);
+        if (half == 0) attn_store_row<D, BF16>(p, p.dv, t_dv + lanes, batch, kv_head, key, live, 1.f);
+        else attn_store_row<D, BF16>(p, p.dk, t_dk + lanes, batch, kv_head, key, live, p.scale);
       } else {
         s_abort = 1;
       }
     } else if (live) {
-      attn_zero_row(p, half == 0 ? p.out1 : p.out0, batch, kv_head, key);
+      attn_zero_row(p, half == 0 ? p.dv : p.dk, batch, kv_head, key);
     }
   }
   __syncwarp();
@@ -650,12 +646,9 @@ template <int D> struct AttnDqSmem {
 };
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kAttnThreads, 1)
-attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
-               const __grid_constant__ CUtensorMap mdo, const AttnParams p) {
-  extern __shared__ unsigned char smem_dyn[];
+__device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo,
+                                              const AttnParams& p, const int tile, const int head, const int batch) {
   using L = AttnDqSmem<D>;
-  unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
   uint64_t* q_full = reinterpret_cast<uint64_t*>(smem + L::kBars);
   uint64_t* k_full = q_full + 1;                 // [kKs]
   uint64_t* k_free = k_full + L::kKs;            // [kKs]
@@ -664,14 +657,15 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
   uint64_t* s_full = v_free + L::kVs;            // [2]
   uint64_t* dp_full = s_full + 2;
   uint64_t* dp_read = dp_full + 1;
+  // two, by the parity of the tile: S and dP of the next tile do not wait for dS of this one, so the
+  // warps could complete a second phase of a single barrier before its first has been looked at
   uint64_t* ds_full = dp_read + 1;
-  uint64_t* done = ds_full + 1;
+  uint64_t* done = ds_full + 2;
   uint64_t* drain = done + 1;
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int head = blockIdx.y, batch = blockIdx.z;
-  const int q0 = (gridDim.x - 1 - blockIdx.x) * kAttnTile;
+  const int q0 = tile * kAttnTile;
 
   if (threadIdx.x == 0) {
     mbar_init(q_full, 1);
@@ -681,7 +675,8 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
     mbar_init(&s_full[1], 1);
     mbar_init(dp_full, 1);
     mbar_init(dp_read, 8);
-    mbar_init(ds_full, 8);
+    mbar_init(&ds_full[0], 8);
+    mbar_init(&ds_full[1], 8);
     mbar_init(done, 1);
     mbar_init(drain, 1);
     s_abort = 0;
@@ -769,7 +764,7 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
         dprobs(j + 1);
         if (!ok) break;
       }
-      if (!wait(ds_full, j & 1)) break;
+      if (!wait(&ds_full[j & 1], (j >> 1) & 1)) break;
       if (lane == 0) {
         attn_mma_tokens<D, BF16>(t_dq, tmem + (j & 1) * 128, 64, smem_addr(smem + L::kK + (j % L::kKs) * L::kT), j != 0);
         mma_commit(&k_free[j % L::kKs]);
@@ -831,15 +826,15 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_one(ds_full);
+      if (lane == 0) mbar_arrive_one(&ds_full[j & 1]);
     }
     const bool live = row < p.Sq;
     if (tiles > 0) {
       if (ok) wait(done, 0);
-      if (ok && half == 0) attn_store_row<D, BF16>(p, p.out0, t_dq + lanes, batch, head, row, live, p.scale);
+      if (ok && half == 0) attn_store_row<D, BF16>(p, p.out, t_dq + lanes, batch, head, row, live, p.scale);
       if (!ok) s_abort = 1;
     } else if (live && half == 0) {
-      attn_zero_row(p, p.out0, batch, head, row);
+      attn_zero_row(p, p.out, batch, head, row);
     }
   }
   __syncwarp();
@@ -849,6 +844,30 @@ attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ C
   if (warp == 9) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
+  }
+}
+
+// Both in one launch: the key blocks first (four products a tile and, with shared heads, several query
+// heads), the query blocks fill the device as those run out.  With a causal mask the first keys have the
+// most queries and the last queries the most keys: long blocks first in either part, all heads of one tile together.
+template <int D> constexpr uint32_t attn_backward_smem() { return AttnDkvSmem<D>::kBytes > AttnDqSmem<D>::kBytes ? AttnDkvSmem<D>::kBytes : AttnDqSmem<D>::kBytes; }
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kAttnThreads, 1)
+attn_backward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
+                     const __grid_constant__ CUtensorMap mdo, const AttnParams p, const int key_blocks, const int q_tiles) {
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
+  int n = blockIdx.x;
+  if (n < key_blocks) {
+    const int heads = p.Hkv * p.B, tile = n / heads;
+    n -= tile * heads;
+    attn_dkv_block<D, BF16>(smem, mq, mk, mv, mdo, p, tile, n % p.Hkv, n / p.Hkv);
+  } else {
+    n -= key_blocks;
+    const int heads = p.Hq * p.B, tile = n / heads;
+    n -= tile * heads;
+    attn_dq_block<D, BF16>(smem, mq, mk, mv, mdo, p, q_tiles - 1 - tile, n % p.Hq, n / p.Hq);
   }
 }
 

@@ -9,7 +9,9 @@ from __future__ import annotations
 
 import ctypes
 
-from .binding import BF16, F32, _check, _stream_handle, load_library
+import torch
+
+from .binding import BF16, F32, _check, _raw_stream, _stream_handle, load_library
 
 # enum adacons_orth_info
 INFO_BYTES, INFO_LAUNCHES = 0, 1
@@ -75,11 +77,12 @@ class Orthogonalizer:
     def apply(self, update, out, stream=None) -> None:
         """out[matrix] = orthogonalised update[matrix] for every matrix; the rest of `out` stays as it is.
         Flat CUDA tensors of d elements; `out` may be `update`."""
-        sig = (update.dtype, update.shape, update.stride(), update.device, out.dtype, out.shape, out.stride(), out.device)
+        device = update.get_device()
+        sig = (update.dtype, update.shape, update.stride(), device, out.dtype, out.shape, out.stride(), out.get_device())
         if sig != self._checked:
             check_vectors(self.d, self.dtype, update, out)
             self._checked = sig
-        _check(self._lib.adacons_orth_apply(self._ctx, update.data_ptr(), out.data_ptr(), _stream_handle(stream)), "adacons_orth_apply")
+        _check(self._lib.adacons_orth_apply(self._ctx, update.data_ptr(), out.data_ptr(), _raw_stream(stream, device)), "adacons_orth_apply")
 
     def status(self, stream=None) -> int:
         """The ADACONS_FLAG_TIMEOUT bit since the last call (0: all waits ended)."""
@@ -95,7 +98,6 @@ class Orthogonalizer:
 
 def check_vectors(d: int, dtype: str, update, out, want_cuda: bool = True) -> None:
     """Raise ValueError unless both are contiguous vectors of d elements of `dtype` on one (CUDA) device."""
-    import torch
     tdt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
     for name, t in (("update", update), ("out", out)):
         if t.dtype != tdt:

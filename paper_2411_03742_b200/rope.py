@@ -8,7 +8,9 @@ from __future__ import annotations
 import ctypes
 import math
 
-from .binding import BF16, F32, _check, _stream_handle, load_library
+import torch
+
+from .binding import BF16, F32, _check, _raw_stream, load_library
 
 
 def frequencies(dim: int, base: float = 10000.0, scaling=None):
@@ -89,30 +91,31 @@ class Rope:
         """x turned, (batch, token, head, element) in float32 or bfloat16 with unit stride along the elements;
         positions: int32 (batch, token), or None: token s is at position first + s.  out: a new tensor
         unless given; x itself is allowed.  inverse: the gradient's turn, by the negative angles."""
-        import torch
-        if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        sig = (x.dtype, x.shape, x.stride(), x.device, out.dtype, out.shape, out.stride(), out.device,
-               None if positions is None else (positions.dtype, positions.shape, positions.stride(), positions.device))
+        device = x.get_device()
+        sig = (x.dtype, x.shape, x.stride(), device, None if out is None else (out.dtype, out.shape, out.stride(), out.get_device(), out.data_ptr() == x.data_ptr()),
+               None if positions is None else (positions.dtype, positions.shape, positions.stride(), positions.get_device()))
         args = self._checked.get(sig)
+        if out is None:
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
         if args is None:
             check_rope(self.dim, x, positions, out)
             B, S, H, D = x.shape
             i64 = ctypes.c_int64 * 3
+            if len(self._checked) >= 1024:       # a program with ever new lengths
+                self._checked.clear()
             args = self._checked[sig] = (_Shape(F32 if x.dtype == torch.float32 else BF16, B, S, H, D), i64(*x.stride()[:3]), i64(*out.stride()[:3]))
         _check(self._lib.adacons_rope_apply(self._ctx, ctypes.byref(args[0]), x.data_ptr(), args[1], out.data_ptr(), args[2],
-                                            None if positions is None else positions.data_ptr(), int(first), int(bool(inverse)), _stream_handle(stream)),
+                                            None if positions is None else positions.data_ptr(), int(first), int(bool(inverse)), _raw_stream(stream, device)),
                "adacons_rope_apply")
         return out
 
     def __call__(self, x, positions=None, first: int = 0):
         """apply as a differentiable function of x."""
-        return _function().apply(x, self, positions, first)
+        return _Turn.apply(x, self, positions, first)
 
 
 def check_rope(dim: int, x, positions, out, want_cuda: bool = True) -> None:
     """Raise ValueError unless x and out are alike, four-dimensional, of a type the kernel has, and positions fit."""
-    import torch
     if x.dim() != 4:
         raise ValueError("x must have four dimensions: batch, token, head, element")
     if x.dtype not in (torch.float32, torch.bfloat16):
@@ -134,26 +137,15 @@ def check_rope(dim: int, x, positions, out, want_cuda: bool = True) -> None:
         raise ValueError(f"positions must be a contiguous int32 tensor of shape {tuple(x.shape[:2])} on x's device")
 
 
-_FUNCTION = None
+class _Turn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, rope, positions, first):
+        ctx.rope, ctx.first = rope, first
+        ctx.save_for_backward(*([] if positions is None else [positions]))
+        return rope.apply(x, positions, first=first)
 
-
-def _function():
-    global _FUNCTION
-    if _FUNCTION is None:
-        import torch
-
-        class Turn(torch.autograd.Function):
-            @staticmethod
-            def forward(ctx, x, rope, positions, first):
-                ctx.rope, ctx.first = rope, first
-                ctx.save_for_backward(*([] if positions is None else [positions]))
-                return rope.apply(x, positions, first=first)
-
-            @staticmethod
-            def backward(ctx, dy):
-                pos = ctx.saved_tensors[0] if ctx.saved_tensors else None
-                dy = dy if dy.stride(3) == 1 else dy.contiguous()
-                return ctx.rope.apply(dy, pos, inverse=True, first=ctx.first), None, None, None
-
-        _FUNCTION = Turn
-    return _FUNCTION
+    @staticmethod
+    def backward(ctx, dy):
+        pos = ctx.saved_tensors[0] if ctx.saved_tensors else None
+        dy = dy if dy.stride(3) == 1 else dy.contiguous()
+        return ctx.rope.apply(dy, pos, inverse=True, first=ctx.first), None, None, None
