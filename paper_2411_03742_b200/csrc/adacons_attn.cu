@@ -118,7 +118,7 @@ AttnParams base_params(const AttnDevice& d, const adacons_attn_shape* s) {
 template <int D, bool BF16>
 bool run_forward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const AttnParams& p, cudaStream_t st) {
   return launch(&attn_forward_kernel<D, BF16>, dim3((p.Sq + 2 * kAttnTile - 1) / (2 * kAttnTile), p.Hq, p.B), dim3(kAttnThreads), AttnFwdSmem<D>::kBytes, st,
-                false, 1, mq, mk, mv, p);
+                kLaunchPlain, 1, mq, mk, mv, p);
 }
 
 template <int D, bool BF16>
@@ -128,14 +128,14 @@ bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMa
   p.lse2 = lse2;
   p.delta = delta;
   const AttnRows a = {dout->data, dout->batch_stride, dout->seq_stride, dout->head_stride}, b = {out->data, out->batch_stride, out->seq_stride, out->head_stride};
-  if (rows > 0 && !launch(&attn_delta_kernel<BF16>, dim3(static_cast<unsigned>((rows + 7) / 8)), dim3(256), 0, st, false, 1, a, b, lse, p.Hq, p.Sq, p.sq_pad, p.D, rows, lse2, delta))
+  if (rows > 0 && !launch(&attn_delta_kernel<BF16>, dim3(static_cast<unsigned>((rows + 7) / 8)), dim3(256), 0, st, kLaunchPlain, 1, a, b, lse, p.Hq, p.Sq, p.sq_pad, p.D, rows, lse2, delta))
     return false;
   p.out = dq;
   p.dk = dk;
   p.dv = dv;
   const int64_t q_tiles = p.sq_pad / kAttnTile, k_tiles = (static_cast<int64_t>(p.Sk) + kAttnTile - 1) / kAttnTile;
   const int64_t key_blocks = k_tiles * p.Hkv * p.B, blocks = key_blocks + q_tiles * p.Hq * p.B;
-  return blocks <= 0x7fffffff && launch(&attn_backward_kernel<D, BF16>, dim3(static_cast<unsigned>(blocks)), dim3(kAttnThreads), attn_backward_smem<D>(), st, true, 1,
+  return blocks <= 0x7fffffff && launch(&attn_backward_kernel<D, BF16>, dim3(static_cast<unsigned>(blocks)), dim3(kAttnThreads), attn_backward_smem<D>(), st, kLaunchOverlap, 1,
                                         mq, mk, mv, mdo, p, static_cast<int>(key_blocks), static_cast<int>(q_tiles));
 }
 

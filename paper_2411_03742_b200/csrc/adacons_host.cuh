@@ -44,18 +44,22 @@ inline bool encode_map(const DeviceInfo& info, CUtensorMap* map, CUtensorMapData
                      CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// `overlap`: programmatic stream serialisation; `cluster`: blocks per cluster.
+enum LaunchKind { kLaunchPlain = 0, kLaunchOverlap = 1, kLaunchCooperative = 2 };   // overlap: programmatic stream serialisation
 template <typename... Params, typename... Args>
-inline bool launch(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, bool overlap, int cluster, Args... args) {
+inline bool launch(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, LaunchKind kind, int cluster, Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = block;
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
-  if (overlap) {
+  if (kind == kLaunchOverlap) {
     attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (kind == kLaunchCooperative) {
+    attr[cfg.numAttrs].id = cudaLaunchAttributeCooperative;
+    attr[cfg.numAttrs++].val.cooperative = 1;
   }
   if (cluster > 1) {
     attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;

@@ -4,7 +4,9 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <memory>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "adacons_host.cuh"
@@ -17,17 +19,13 @@ struct adacons_orth {
   int dtype = 0, steps = 0;
   int64_t d = 0;
   double eps = 0;
-  std::vector<double> coeffs;         // [steps][a, b, c]
   unsigned char* memory = nullptr;    // one allocation: descriptors, lists, partial sums, iterates
   size_t bytes = 0;
-  const OrthMat* mats = nullptr;
-  const CUtensorMap* maps = nullptr;
   const OrthTile* load_tiles = nullptr;
-  const OrthTile* tiles[3] = {};      // by OrthKind
-  int num_tiles[3] = {}, cg[3] = {};
   const OrthChunk* chunks = nullptr;
   double* partial = nullptr;
-  uint32_t* flags = nullptr;
+  OrthParams params = {};             // all but the result's address
+  int cg = 1, blocks = 0;
   int num_load = 0, num_chunks = 0;
   int64_t launches = 0;
 };
@@ -47,57 +45,102 @@ struct Arena {                        // offsets first, pointers once the alloca
   }
 };
 
-// The tiles of one product for a tiling with CG blocks per tile, longest first, as the persistent
-// blocks (or pairs) take them in turn, and the modelled time of the busiest one in cycles.  The model:
-// a stage's products take 64 (128) cycles per 16 K elements and fp16 pass, a lone block about 1.3 times that (its operand
-// traffic from L2 per product is twice a pair's), an epilogue overlaps with the next tile's products.
-double plan_tiles(const std::vector<OrthMat>& mats, int kind, bool split, int cg, int sms, std::vector<OrthTile>* tiles) {
+// Who computes which tile of a step's three products, for a tiling with CG blocks per tile.
+struct OrthPlan {
+  int cg = 1, workers = 1;
+  std::vector<OrthTile> tiles[3];
+  std::vector<int> begin[3];
+  std::vector<int> parts[3];          // [matrix]
+  double cycles = 0;                  // modelled time of a step
+};
+
+// Matrices in one order for all workers, the deepest products first; each tile goes to the worker with the
+// least to do so far.  The model: a stage (64 K elements) takes 830 cycles of a pair and 650 of a lone block
+// (measured; the lone block's tile is a quarter), three times the products in an fp32 context 1200; an
+// epilogue overlaps with the next tile; a step cannot be shorter than the longest matrix's three products
+// with about 6000 cycles from the last stage of one to the first of the next.
+OrthPlan plan_step(const std::vector<OrthMat>& mats, bool split, int cg, int workers) {
+  OrthPlan plan;
   const int tm = 128 * cg, tn = split ? 128 : 128 * cg;
-  tiles->clear();
-  std::vector<int> order(mats.size());
-  for (size_t k = 0; k < mats.size(); ++k) order[k] = static_cast<int>(k);
-  auto depth = [&](int k) { return kind == kOrthGram ? mats[k].l : mats[k].r; };
-  std::sort(order.begin(), order.end(), [&](int x, int y) { return depth(x) != depth(y) ? depth(x) > depth(y) : x < y; });
-  const int workers = sms / cg;
-  std::vector<double> busy(workers, 0.0);
-  for (int k : order) {
-    const int cols = kind == kOrthApply ? mats[k].l : mats[k].r;
-    const double stages = (depth(k) + kOrthTK - 1) / kOrthTK;
-    const double products = stages * 4 * (tn / 2) * (split ? 3 : 1) * (cg == 1 ? 1.3 : 1.0);
-    const double cost = std::max(products, 16.0 * tn) + 500.0;
-    for (int64_t j = 0; j * tn < cols; ++j)
-      for (int64_t i = 0; i * tm < mats[k].r; ++i) {
-        if (kind != kOrthApply && i * tm + tm - 1 < j * tn) continue;
-        busy[tiles->size() % workers] += cost;
-        tiles->push_back({k, static_cast<int>(i), static_cast<int>(j), 0});
-      }
+  const double stage = split ? 1200.0 : cg == 2 ? 830.0 : 650.0;
+  const int num = static_cast<int>(mats.size());
+  std::vector<int> order(num);
+  for (int k = 0; k < num; ++k) order[k] = k;
+  auto size = [&](int k) { return static_cast<double>(mats[k].r) * mats[k].r * mats[k].l; };
+  std::sort(order.begin(), order.end(), [&](int x, int y) { return size(x) != size(y) ? size(x) > size(y) : x < y; });
+  auto depth = [&](int kind, int k) { return kind == kOrthGram ? mats[k].l : mats[k].r; };
+  int64_t most = 0;
+  for (int kind = 0; kind < 3; ++kind) {
+    int64_t count = 0;
+    for (const OrthMat& m : mats) count += static_cast<int64_t>((m.r + tm - 1) / tm) * (((kind == kOrthApply ? m.l : m.r) + tn - 1) / tn);
+    most = std::max(most, count);
   }
-  return *std::max_element(busy.begin(), busy.end()) + 16.0 * tn;
+  plan.cg = cg;
+  plan.workers = static_cast<int>(std::min<int64_t>(workers, most));
+  std::vector<double> chain(num, 0.0);
+  std::vector<std::pair<double, int>> heap;          // (-load, -worker): the least loaded, then the first, on top
+  for (int w = 0; w < plan.workers; ++w) heap.emplace_back(0.0, -w);
+  std::make_heap(heap.begin(), heap.end());
+  for (int kind = 0; kind < 3; ++kind) {
+    std::vector<std::vector<OrthTile>> mine(plan.workers);
+    plan.parts[kind].assign(num, 0);
+    for (int k : order) {
+      const int cols = kind == kOrthApply ? mats[k].l : mats[k].r;
+      const double cost = std::max(stage * ((depth(kind, k) + kOrthTK - 1) / kOrthTK), 16.0 * tn) + 1500.0;
+      int64_t count = 0;
+      for (int64_t j = 0; j * tn < cols; ++j)
+        for (int64_t i = 0; i * tm < mats[k].r; ++i) {
+          if (kind != kOrthApply && i * tm + tm - 1 < j * tn) continue;
+          std::pop_heap(heap.begin(), heap.end());
+          mine[-heap.back().second].push_back({k, static_cast<int>(i), static_cast<int>(j), depth(kind, k)});
+          heap.back().first -= cost;
+          std::push_heap(heap.begin(), heap.end());
+          for (int rank = 0; rank < cg; ++rank) plan.parts[kind][k] += i * tm + rank * 128 < mats[k].r;
+          ++count;
+        }
+      chain[k] += cost * ((count + plan.workers - 1) / plan.workers) + 6000.0;
+    }
+    plan.begin[kind].push_back(0);
+    for (const auto& list : mine) {
+      plan.tiles[kind].insert(plan.tiles[kind].end(), list.begin(), list.end());
+      plan.begin[kind].push_back(static_cast<int>(plan.tiles[kind].size()));
+    }
+  }
+  for (const auto& h : heap) plan.cycles = std::max(plan.cycles, -h.first);
+  for (double c : chain) plan.cycles = std::max(plan.cycles, c);
+  return plan;
 }
 
-template <int KIND, bool SPLIT, int CG>
-bool launch_product(const adacons_orth* c, const OrthParams& p, cudaStream_t st) {
-  static_assert(OrthTiling<SPLIT, CG>::kBytes <= 227 * 1024, "shared memory of a block");
-  const int blocks = std::min(p.num_tiles, c->dev.sms / CG) * CG;
-  return launch(&orth_product_kernel<KIND, SPLIT, CG>, dim3(blocks), dim3(kOrthThreads), OrthTiling<SPLIT, CG>::kBytes, st, true, CG, p);
+template <bool SPLIT, int CG>
+int prepare_kernel(int sms, int* workers) {
+  using T = OrthTiling<SPLIT, CG>;
+  static_assert(T::kBytes <= 227 * 1024, "shared memory of a block");
+  auto* kernel = &orth_steps_kernel<SPLIT, CG>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kBytes) != cudaSuccess) { cudaGetLastError(); return ADACONS_ECUDA; }
+  if (CG == 1) {
+    *workers = sms;                   // one block an SM fits: its shared memory is checked above
+    return ADACONS_OK;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(sms / CG * CG);
+  cfg.blockDim = dim3(kOrthThreads);
+  cfg.dynamicSmemBytes = T::kBytes;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = CG;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int pairs = 0;
+  if (cudaOccupancyMaxActiveClusters(&pairs, kernel, &cfg) != cudaSuccess) { cudaGetLastError(); return ADACONS_ECUDA; }
+  *workers = std::min(pairs, sms / CG);
+  return *workers > 0 ? ADACONS_OK : ADACONS_ECUDA;
 }
 
-template <int KIND>
-bool launch_kind(const adacons_orth* c, OrthParams p, cudaStream_t st) {
-  p.tiles = c->tiles[KIND];
-  p.num_tiles = c->num_tiles[KIND];
-  if (c->dtype == ADACONS_F32) return c->cg[KIND] == 2 ? launch_product<KIND, true, 2>(c, p, st) : launch_product<KIND, true, 1>(c, p, st);
-  return c->cg[KIND] == 2 ? launch_product<KIND, false, 2>(c, p, st) : launch_product<KIND, false, 1>(c, p, st);
+template <bool SPLIT, int CG>
+bool launch_steps(const adacons_orth* c, const OrthParams& p, cudaStream_t st) {
+  return launch(&orth_steps_kernel<SPLIT, CG>, dim3(c->blocks), dim3(kOrthThreads), OrthTiling<SPLIT, CG>::kBytes, st, kLaunchCooperative, CG, p);
 }
-
-template <int KIND, bool SPLIT, int CG>
-bool raise_smem() {
-  if (cudaFuncSetAttribute(orth_product_kernel<KIND, SPLIT, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, OrthTiling<SPLIT, CG>::kBytes) == cudaSuccess) return true;
-  cudaGetLastError();
-  return false;
-}
-template <int KIND>
-bool raise_smem_kind() { return raise_smem<KIND, false, 1>() && raise_smem<KIND, false, 2>() && raise_smem<KIND, true, 1>() && raise_smem<KIND, true, 2>(); }
 
 int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* rows, const int64_t* cols, const int64_t* offsets, int scaling,
            int steps, const double* coeffs, double eps) {
@@ -117,20 +160,23 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   DeviceInfo dev;
   int rc = query_device(&dev);
   if (rc != ADACONS_OK) return rc;
-  if (!raise_smem_kind<kOrthGram>() || !raise_smem_kind<kOrthPoly>() || !raise_smem_kind<kOrthApply>()) return ADACONS_ECUDA;
+  const bool split = dtype == ADACONS_F32;
+  int singles = 0, pairs = 0;
+  rc = split ? prepare_kernel<true, 1>(dev.sms, &singles) : prepare_kernel<false, 1>(dev.sms, &singles);
+  if (rc == ADACONS_OK) rc = split ? prepare_kernel<true, 2>(dev.sms, &pairs) : prepare_kernel<false, 2>(dev.sms, &pairs);
+  if (rc != ADACONS_OK) return rc;
 
-  adacons_orth* c = new adacons_orth();
+  std::unique_ptr<adacons_orth> holder(new adacons_orth());      // released at the end: nothing leaks if a list runs out of memory
+  adacons_orth* c = holder.get();
   c->dev = dev;
   c->dtype = dtype;
   c->d = d;
   c->steps = steps;
   c->eps = eps;
-  c->coeffs.assign(coeffs, coeffs + 3 * steps);
-  const bool split = dtype == ADACONS_F32;
 
   std::vector<OrthMat> mats(num);
   std::vector<OrthChunk> chunks;
-  std::vector<OrthTile> load, lists[3];
+  std::vector<OrthTile> load;
   for (int k = 0; k < num; ++k) {
     OrthMat& m = mats[k];
     std::memset(&m, 0, sizeof(m));
@@ -148,20 +194,31 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
     for (int i = 0; i < (m.r + kOrthLoadTile - 1) / kOrthLoadTile; ++i)
       for (int j = 0; j < (m.l + kOrthLoadTile - 1) / kOrthLoadTile; ++j) load.push_back({k, i, j, 0});
   }
-  for (int kind = 0; kind < 3; ++kind) {
-    std::vector<OrthTile> one, two;
-    const double t1 = plan_tiles(mats, kind, split, 1, dev.sms, &one), t2 = plan_tiles(mats, kind, split, 2, dev.sms, &two);
-    c->cg[kind] = t2 < t1 ? 2 : 1;
-    lists[kind] = t2 < t1 ? two : one;
-    c->num_tiles[kind] = static_cast<int>(lists[kind].size());
+  OrthPlan plan = plan_step(mats, split, 1, singles);
+  {
+    OrthPlan two = plan_step(mats, split, 2, pairs);
+    if (two.cycles < plan.cycles) plan = std::move(two);
+  }
+  c->cg = plan.cg;
+  c->blocks = plan.workers * plan.cg;
+  for (int k = 0; k < num; ++k)
+    for (int kind = 0; kind < 3; ++kind) mats[k].parts[kind] = plan.parts[kind][k];
+  std::vector<OrthStep> step_coeffs(steps);
+  for (int s = 0; s < steps; ++s) {
+    const double* q = coeffs + 3 * s;
+    step_coeffs[s] = {static_cast<float>(q[0]), static_cast<float>(q[1]), static_cast<float>(q[2]), s >= 3 ? static_cast<float>(-0.75 * (q[1] + q[2])) : 0.f};
   }
   c->num_chunks = static_cast<int>(chunks.size());
   c->num_load = static_cast<int>(load.size());
 
   Arena a;
   const size_t at_mats = a.take(num * sizeof(OrthMat)), at_maps = a.take(static_cast<size_t>(num) * kMapCount * sizeof(CUtensorMap));
-  size_t at_tiles[3];
-  for (int kind = 0; kind < 3; ++kind) at_tiles[kind] = a.take(lists[kind].size() * sizeof(OrthTile));
+  size_t at_tiles[3], at_begin[3];
+  for (int kind = 0; kind < 3; ++kind) {
+    at_tiles[kind] = a.take(plan.tiles[kind].size() * sizeof(OrthTile));
+    at_begin[kind] = a.take(plan.begin[kind].size() * sizeof(int));
+  }
+  const size_t at_coeffs = a.take(step_coeffs.size() * sizeof(OrthStep)), at_done = a.take(num * sizeof(unsigned));
   const size_t at_load = a.take(load.size() * sizeof(OrthTile)), at_chunks = a.take(chunks.size() * sizeof(OrthChunk));
   const size_t at_partial = a.take(chunks.size() * sizeof(double)), at_flags = a.take(sizeof(uint32_t));
   const size_t head = a.used;
@@ -173,9 +230,9 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
       at[k * kMapCount + q] = a.take(static_cast<size_t>(mats[k].r) * (is_x ? mats[k].ldx : mats[k].lds) * sizeof(__half));
     }
   c->bytes = a.used;
-  if (cudaMalloc(&c->memory, c->bytes) != cudaSuccess) { cudaGetLastError(); delete c; return ADACONS_ENOMEM; }
   std::vector<unsigned char> host(head, 0);
   std::vector<CUtensorMap> maps(static_cast<size_t>(num) * kMapCount);
+  if (cudaMalloc(&c->memory, c->bytes) != cudaSuccess) { cudaGetLastError(); return ADACONS_ENOMEM; }
   for (int k = 0; k < num; ++k) {
     OrthMat& m = mats[k];
     __half** fields[kMapCount] = {&m.x[0][0], &m.x[0][1], &m.x[1][0], &m.x[1][1], &m.s[0], &m.s[1], &m.b[0], &m.b[1]};
@@ -189,17 +246,20 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
       const cuuint32_t box[2] = {64, 64};
       if (!encode_map(dev, &maps[k * kMapCount + q], CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, c->memory + where, dims, strides, box)) {
         cudaFree(c->memory);
-        delete c;
         return ADACONS_ECUDA;
       }
     }
   }
   std::memcpy(host.data() + at_mats, mats.data(), num * sizeof(OrthMat));
   std::memcpy(host.data() + at_maps, maps.data(), maps.size() * sizeof(CUtensorMap));
+  OrthParams& p = c->params;
   for (int kind = 0; kind < 3; ++kind) {
-    std::memcpy(host.data() + at_tiles[kind], lists[kind].data(), lists[kind].size() * sizeof(OrthTile));
-    c->tiles[kind] = reinterpret_cast<const OrthTile*>(c->memory + at_tiles[kind]);
+    std::memcpy(host.data() + at_tiles[kind], plan.tiles[kind].data(), plan.tiles[kind].size() * sizeof(OrthTile));
+    std::memcpy(host.data() + at_begin[kind], plan.begin[kind].data(), plan.begin[kind].size() * sizeof(int));
+    p.tiles[kind] = reinterpret_cast<const OrthTile*>(c->memory + at_tiles[kind]);
+    p.begin[kind] = reinterpret_cast<const int*>(c->memory + at_begin[kind]);
   }
+  std::memcpy(host.data() + at_coeffs, step_coeffs.data(), step_coeffs.size() * sizeof(OrthStep));
   std::memcpy(host.data() + at_load, load.data(), load.size() * sizeof(OrthTile));
   std::memcpy(host.data() + at_chunks, chunks.data(), chunks.size() * sizeof(OrthChunk));
   // the padding of the iterates is read by the epilogues (never by a product): zero it once
@@ -207,16 +267,18 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
       cudaMemcpy(c->memory, host.data(), head, cudaMemcpyHostToDevice) != cudaSuccess || cudaDeviceSynchronize() != cudaSuccess) {
     cudaGetLastError();
     cudaFree(c->memory);
-    delete c;
     return ADACONS_ECUDA;
   }
-  c->mats = reinterpret_cast<const OrthMat*>(c->memory + at_mats);
-  c->maps = reinterpret_cast<const CUtensorMap*>(c->memory + at_maps);
+  p.mats = reinterpret_cast<const OrthMat*>(c->memory + at_mats);
+  p.maps = reinterpret_cast<const CUtensorMap*>(c->memory + at_maps);
+  p.coeffs = reinterpret_cast<const OrthStep*>(c->memory + at_coeffs);
+  p.done = reinterpret_cast<unsigned*>(c->memory + at_done);
+  p.flags = reinterpret_cast<uint32_t*>(c->memory + at_flags);
+  p.steps = steps;
   c->load_tiles = reinterpret_cast<const OrthTile*>(c->memory + at_load);
   c->chunks = reinterpret_cast<const OrthChunk*>(c->memory + at_chunks);
   c->partial = reinterpret_cast<double*>(c->memory + at_partial);
-  c->flags = reinterpret_cast<uint32_t*>(c->memory + at_flags);
-  *out = c;
+  *out = holder.release();
   return ADACONS_OK;
 }
 
@@ -244,39 +306,29 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
   const size_t elem = c->dtype == ADACONS_F32 ? 4 : 2;
   if (reinterpret_cast<uintptr_t>(update) % elem != 0 || reinterpret_cast<uintptr_t>(out) % elem != 0) return ADACONS_EINVAL;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  bool ok;
-  if (c->dtype == ADACONS_F32) {
-    ok = launch(&orth_norm_kernel<0>, dim3(c->num_chunks), dim3(256), 0, st, false, 1, update, c->mats, c->chunks, c->partial) &&
-         launch(&orth_load_kernel<0>, dim3(c->num_load), dim3(256), 0, st, true, 1, update, c->mats, c->load_tiles, static_cast<const double*>(c->partial), c->eps);
-  } else {
-    ok = launch(&orth_norm_kernel<1>, dim3(c->num_chunks), dim3(256), 0, st, false, 1, update, c->mats, c->chunks, c->partial) &&
-         launch(&orth_load_kernel<1>, dim3(c->num_load), dim3(256), 0, st, true, 1, update, c->mats, c->load_tiles, static_cast<const double*>(c->partial), c->eps);
-  }
-  OrthParams p = {};
-  p.mats = c->mats;
-  p.maps = c->maps;
-  p.flags = c->flags;
+  OrthParams p = c->params;
   p.out = out;
   p.out_aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0;
-  for (int s = 0; ok && s < c->steps; ++s) {
-    const double* k = &c->coeffs[3 * s];
-    p.src = s & 1;
-    p.a = static_cast<float>(k[0]);
-    p.b = static_cast<float>(k[1]);
-    p.c = static_cast<float>(k[2]);
-    p.t = s >= 3 ? static_cast<float>(-0.75 * (k[1] + k[2])) : 0.f;
-    p.last = s == c->steps - 1;
-    ok = launch_kind<kOrthGram>(c, p, st) && launch_kind<kOrthPoly>(c, p, st) && launch_kind<kOrthApply>(c, p, st);
+  const double* partial = c->partial;
+  bool ok;
+  if (c->dtype == ADACONS_F32) {
+    ok = launch(&orth_norm_kernel<0>, dim3(c->num_chunks), dim3(256), 0, st, kLaunchPlain, 1, update, p.mats, c->chunks, c->partial) &&
+         launch(&orth_load_kernel<0>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, p.mats, c->load_tiles, partial, c->eps, p.done) &&
+         (c->cg == 2 ? launch_steps<true, 2>(c, p, st) : launch_steps<true, 1>(c, p, st));
+  } else {
+    ok = launch(&orth_norm_kernel<1>, dim3(c->num_chunks), dim3(256), 0, st, kLaunchPlain, 1, update, p.mats, c->chunks, c->partial) &&
+         launch(&orth_load_kernel<1>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, p.mats, c->load_tiles, partial, c->eps, p.done) &&
+         (c->cg == 2 ? launch_steps<false, 2>(c, p, st) : launch_steps<false, 1>(c, p, st));
   }
-  c->launches = 2 + 3 * c->steps;
+  c->launches = 3;
   return ok ? ADACONS_OK : ADACONS_ECUDA;
 }
 
 int adacons_orth_get_status(adacons_orth* c, uint32_t* flags, void* cuda_stream) {
   if (c == nullptr || flags == nullptr) return ADACONS_EINVAL;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (cudaMemcpyAsync(flags, c->flags, sizeof(uint32_t), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
-      cudaMemsetAsync(c->flags, 0, sizeof(uint32_t), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
+  if (cudaMemcpyAsync(flags, c->params.flags, sizeof(uint32_t), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+      cudaMemsetAsync(c->params.flags, 0, sizeof(uint32_t), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
     cudaGetLastError();
     return ADACONS_ECUDA;
   }

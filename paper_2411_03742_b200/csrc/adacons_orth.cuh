@@ -48,24 +48,27 @@ struct OrthMat {
   int ldx, lds;            // row pitch of X and of S, B (elements)
   int vec_out;             // rows of the result are whole groups of 8 elements, aligned relative to the vector's start
   int norm_first, norm_count;
+  int parts[3];            // tiles that the blocks store, by kind
   float scale;
   long long offset;        // of the matrix in the vector
   __half* x[2][2];         // [buffer][hi, lo]
   __half* s[2];
   __half* b[2];
 };
-struct OrthTile { int mat, i, j, pad; };
+struct OrthTile { int mat, i, j, depth; };     // depth: K elements of the product
+struct OrthStep { float a, b, c, t; };         // t: what is added to B's diagonal
 struct OrthChunk { int mat; int first; };      // norm kernel: chunk number within the matrix
 
 struct OrthParams {
   const OrthMat* mats;
   const CUtensorMap* maps;       // [matrix][kMapCount]
-  const OrthTile* tiles;
-  int num_tiles;
-  int src;                       // buffer of X that is read
-  float a, b, c, t;              // t: what is added to B's diagonal
-  void* out;                     // last step: the flat result
-  int last, out_aligned;
+  const OrthTile* tiles[3];      // by kind, each worker's after the other's
+  const int* begin[3];           // [workers + 1]
+  const OrthStep* coeffs;        // [steps]
+  unsigned* done;                // [matrix] blocks' tiles stored so far
+  int steps;
+  void* out;                     // the flat result
+  int out_aligned;
   uint32_t* flags;
 };
 
@@ -110,7 +113,7 @@ __device__ __forceinline__ void orth_split(float v, __half& hi, __half& lo) {
 
 // X_0 = G / (|G|_F + eps) as pairs, transposed where the matrix is taller than wide.
 template <int DT>
-__global__ void __launch_bounds__(256) orth_load_kernel(const void* in, const OrthMat* mats, const OrthTile* tiles, const double* partial, double eps) {
+__global__ void __launch_bounds__(256) orth_load_kernel(const void* in, const OrthMat* mats, const OrthTile* tiles, const double* partial, double eps, unsigned* done) {
   __shared__ float s_tile[kOrthLoadTile][kOrthLoadTile + 1];
   __shared__ double s_sum[8];
   pdl_launch_dependents();
@@ -118,6 +121,7 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, const Or
   const OrthTile t = tiles[blockIdx.x];
   const OrthMat& m = mats[t.mat];
   const int tid = threadIdx.x;
+  if (tid == 0 && t.i == 0 && t.j == 0) done[t.mat] = 0u;
   double sum = 0.0;
   for (int k = tid; k < m.norm_count; k += 256) sum += partial[m.norm_first + k];
 #pragma unroll
@@ -154,7 +158,15 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, const Or
 }
 
 // ----------------------------------------------------------------------------------------------
-// The three products of a step, all matrices of the vector in one persistent launch.
+// All steps of all matrices in one persistent launch, one block per SM.
+//
+// Every block (or pair) has its share of the tiles of each product, dealt out by their cost, and goes through
+// the steps with it.  A matrix's next product starts when all tiles of its last one are stored, which a
+// counter per matrix says; the matrices are in the same order everywhere, so that while one is completed
+// elsewhere the others keep the block busy.  One launch per product instead (three a step) left the device
+// idle at every boundary: 7 to 10 us for the smallest matrix, and half of the time of one encoder layer.
+// The blocks wait for one another, so the launch is cooperative; each wait is bounded.
+//
 //   Gram   S = X X^T        both operands K-major, straight from X's rows
 //   Poly   B = b S + c S S + t I
 //   Apply  X' = (a - t) X + B X    the right operand is X again, MN-major: no transposed copy exists
@@ -191,11 +203,11 @@ template <bool SPLIT, int CG> struct OrthTiling {
 };
 
 // What of a tile exists: strips with columns inside the matrix, none for a block without rows.
-template <int KIND, bool SPLIT, int CG>
-__device__ __forceinline__ int orth_live_strips(const OrthMat& m, const OrthTile& t, int rank) {
+template <bool SPLIT, int CG>
+__device__ __forceinline__ int orth_live_strips(int kind, const OrthMat& m, const OrthTile& t, int rank) {
   using T = OrthTiling<SPLIT, CG>;
   if (t.i * T::kTM + rank * 128 >= m.r) return 0;
-  const int left = ((KIND == kOrthApply ? m.l : m.r) - t.j * T::kTN + 63) / 64;
+  const int left = ((kind == kOrthApply ? m.l : m.r) - t.j * T::kTN + 63) / 64;
   return left < T::kBlocks ? left : T::kBlocks;
 }
 
@@ -216,12 +228,12 @@ __device__ __forceinline__ uint32_t orth_pack2(float a, float b) {
 // One 32 x 32 block of the product: row0 + lane is this thread's row, acc its 32 columns from col0 on.
 // hi / lo: the block's place in the strip, `half` selecting its 64 bytes of each 128-byte row.
 template <int KIND, bool SPLIT, int CG>
-__device__ __forceinline__ void orth_finish_block(const OrthParams& p, const OrthMat& m, int row0, int col0, const uint32_t (&acc)[32],
+__device__ __forceinline__ void orth_finish_block(const OrthParams& p, const OrthStep& step, bool last_step, const OrthMat& m, int row0, int col0, const uint32_t (&acc)[32],
                                                   unsigned char* hi, unsigned char* lo, int half) {
   using T = OrthTiling<SPLIT, CG>;
   const int lane = threadIdx.x & 31;
   const int r = m.r, ncols = KIND == kOrthApply ? m.l : m.r, row = row0 + lane;
-  const bool last = KIND == kOrthApply && p.last;
+  const bool last = KIND == kOrthApply && last_step;
   constexpr bool kPair = KIND == kOrthApply || SPLIT;      // X is always a pair, S and B only in an fp32 context
   // where no tile above the diagonal is computed, its image comes from here
   const bool mirror = KIND != kOrthApply && !((col0 / T::kTM) * T::kTM + T::kTM - 1 >= (row0 / T::kTN) * T::kTN);
@@ -248,14 +260,14 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] += y[e];
       }
-      const float by_x = KIND == kOrthPoly ? p.b * (kOrthBScale / kOrthSScale) : p.a - p.t;
-      const float by_v = KIND == kOrthPoly ? p.c * (kOrthBScale / (kOrthSScale * kOrthSScale)) : 1.f / kOrthBScale;
+      const float by_x = KIND == kOrthPoly ? step.b * (kOrthBScale / kOrthSScale) : step.a - step.t;
+      const float by_v = KIND == kOrthPoly ? step.c * (kOrthBScale / (kOrthSScale * kOrthSScale)) : 1.f / kOrthBScale;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = by_x * x[e] + by_v * v[e];
       if (KIND == kOrthPoly && row0 == col0) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (8 * g + e == lane) v[e] += p.t * kOrthBScale;
+          if (8 * g + e == lane) v[e] += step.t * kOrthBScale;
       }
     }
     if (!last) {
@@ -345,8 +357,57 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
   }
 }
 
-template <int KIND, bool SPLIT, int CG>
-__global__ void __launch_bounds__(kOrthThreads, 1) orth_product_kernel(const OrthParams p) {
+// The products of one block in the order in which all of its warps go through them.
+struct OrthWalk {
+  const OrthParams& p;
+  const int worker;
+  int step, kind, k, end;
+  OrthTile t;
+  __device__ __forceinline__ OrthWalk(const OrthParams& params, int w) : p(params), worker(w), step(0), kind(-1), k(0), end(0) { next(); }
+  __device__ __forceinline__ bool more() const { return step < p.steps; }
+  __device__ __forceinline__ void next() {
+    ++k;
+    while (k >= end) {
+      if (++kind == 3) { kind = 0; ++step; }
+      if (step == p.steps) return;
+      const int* begin = kind == 0 ? p.begin[0] : kind == 1 ? p.begin[1] : p.begin[2];
+      k = begin[worker];
+      end = begin[worker + 1];
+    }
+    t = (kind == 0 ? p.tiles[0] : kind == 1 ? p.tiles[1] : p.tiles[2])[k];
+  }
+  // stored tiles of the matrix that this product needs: all of its earlier products
+  __device__ __forceinline__ unsigned needs() const {
+    const OrthMat& m = p.mats[t.mat];
+    const unsigned g = m.parts[0], q = m.parts[1], a = m.parts[2];
+    return step * (g + q + a) + (kind > 0 ? g : 0u) + (kind > 1 ? q : 0u);
+  }
+};
+
+__device__ __forceinline__ unsigned orth_load_acquire(const unsigned* p) {
+  unsigned v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+// Whether what a product reads is there; the copies that follow are ordered behind the look.
+__device__ __forceinline__ bool orth_ready(const OrthWalk& w) {
+  if (orth_load_acquire(w.p.done + w.t.mat) < w.needs()) return false;
+  asm volatile("fence.proxy.async.global;" ::: "memory");
+  return true;
+}
+__device__ __forceinline__ bool orth_wait_ready(const OrthWalk& w, volatile int* s_abort) {
+  if (orth_ready(w)) return true;
+  const unsigned long long t0 = global_timer_ns();
+  while (!*s_abort) {
+    if (orth_ready(w)) return true;
+    __nanosleep(40);
+    if (global_timer_ns() - t0 > kWaitLimitNs) return false;
+  }
+  return false;
+}
+
+template <bool SPLIT, int CG>
+__global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthParams p) {
   extern __shared__ unsigned char smem_dyn[];
   using T = OrthTiling<SPLIT, CG>;
   unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
@@ -362,7 +423,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_product_kernel(const Ort
   __shared__ volatile int s_abort;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = CG == 2 ? static_cast<int>(cluster_rank()) : 0;
-  const int first = blockIdx.x / CG, stride = gridDim.x / CG;
+  const int worker = blockIdx.x / CG;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < T::kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
@@ -381,22 +442,21 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_product_kernel(const Ort
   if (CG == 2) cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
-  pdl_launch_dependents();
-  pdl_wait();
 
   if (warp == 8) {
     if (lane == 0) {
       int stage = 0, issued = 0;
       uint32_t parity = 1;                       // the stages start out empty
       bool ok = true;
-      for (int k = first; ok && k < p.num_tiles; k += stride) {
-        const OrthTile t = p.tiles[k];
-        const CUtensorMap* maps = p.maps + static_cast<long long>(t.mat) * kMapCount;
-        const int K = KIND == kOrthGram ? p.mats[t.mat].l : p.mats[t.mat].r;
-        const CUtensorMap* ma = maps + (KIND == kOrthGram ? kMapX0 + 2 * p.src : KIND == kOrthPoly ? kMapS : kMapB);
-        const CUtensorMap* mb = maps + (KIND == kOrthPoly ? kMapS : kMapX0 + 2 * p.src);
-        const int arow = t.i * T::kTM + rank * 128, brow = t.j * T::kTN + rank * T::kBRows;
-        for (int k0 = 0; k0 < K; k0 += kOrthTK) {
+      for (OrthWalk w(p, worker); ok && w.more(); w.next()) {
+        const CUtensorMap* maps = p.maps + static_cast<long long>(w.t.mat) * kMapCount;
+        const CUtensorMap* x_map = maps + kMapX0 + 2 * (w.step & 1);
+        const CUtensorMap* ma = w.kind == kOrthGram ? x_map : w.kind == kOrthPoly ? maps + kMapS : maps + kMapB;
+        const CUtensorMap* mb = w.kind == kOrthPoly ? maps + kMapS : x_map;
+        const bool across = w.kind == kOrthApply;                           // the right operand's K runs along its rows
+        const int arow = w.t.i * T::kTM + rank * 128, brow = w.t.j * T::kTN + rank * T::kBRows;
+        if (!orth_wait_ready(w, &s_abort)) { s_abort = 1; break; }
+        for (int k0 = 0; k0 < w.t.depth; k0 += kOrthTK) {
           if (s_abort || !mbar_wait_bounded(&empty[stage], parity)) { s_abort = 1; ok = false; break; }
           unsigned char* at = smem + stage * T::kStage;
           if (rank == 0) mbar_expect_tx(&full[stage], CG * T::kStage);      // the pair's bytes all count on the even block's barrier
@@ -409,11 +469,8 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_product_kernel(const Ort
 #pragma unroll
             for (int h = 0; h < 2; ++h) load(at + part * T::kA + h * 8192, ma + part, k0, arow + h * 64);
 #pragma unroll
-            for (int h = 0; h < T::kBRows / 64; ++h) {
-              unsigned char* dst = at + T::kParts * T::kA + part * T::kB + h * 8192;
-              if (KIND == kOrthApply) load(dst, mb + part, brow + h * 64, k0);
-              else load(dst, mb + part, k0, brow + h * 64);
-            }
+            for (int h = 0; h < T::kBRows / 64; ++h)
+              load(at + T::kParts * T::kA + part * T::kB + h * 8192, mb + part, across ? brow + h * 64 : k0, across ? k0 : brow + h * 64);
           }
           ++issued;
           if (++stage == T::kStages) { stage = 0; parity ^= 1u; }
@@ -423,14 +480,15 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_product_kernel(const Ort
     }
   } else if (warp == 9) {
     if (lane == 0 && rank == 0) {
-      constexpr uint32_t idesc = mma_idesc(T::kTM, T::kTN, false, false, KIND == kOrthApply);
       int stage = 0, buf = 0, small = 0;
       uint32_t parity = 0, acc_parity = 1;
       bool ok = true;
-      for (int k = first; ok && k < p.num_tiles; k += stride) {
-        const int mat = p.tiles[k].mat;
-        const int K = KIND == kOrthGram ? p.mats[mat].l : p.mats[mat].r;
-        const int steps = (K + kOrthTK - 1) / kOrthTK;
+      for (OrthWalk w(p, worker); ok && w.more(); w.next()) {
+        const bool across = w.kind == kOrthApply;
+        const uint32_t idesc = across ? mma_idesc(T::kTM, T::kTN, false, false, true) : mma_idesc(T::kTM, T::kTN, false, false, false);
+        const uint64_t b_base = across ? desc_mnmajor(0, 8192) : desc_kmajor(0);
+        const uint32_t b_step = across ? 2048 / 16 : 32 / 16;              // descriptors count 16-byte units
+        const int steps = (w.t.depth + kOrthTK - 1) / kOrthTK;
         for (int s = 0; s < steps; ++s) {
           const int in_acc = SPLIT ? s % kOrthChunk : s;
           if (in_acc == 0) {
@@ -441,14 +499,14 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_product_kernel(const Ort
           tc_fence_after();
           const uint32_t big = tmem + buf * T::kTN, low = tmem + (2 + small) * T::kTN;
           const uint32_t sa = smem_addr(smem + stage * T::kStage), sb = sa + T::kParts * T::kA;
-          auto b_desc = [&](uint32_t base, int kk) { return KIND == kOrthApply ? desc_mnmajor(base + kk * 2048, 8192) : desc_kmajor(base + kk * 32); };
 #pragma unroll
           for (int kk = 0; kk < kOrthTK / 16; ++kk) {
+            const uint64_t b_hi = b_base + (sb >> 4) + kk * b_step;
             if (SPLIT) {
-              mma_ss<CG>(low, desc_kmajor(sa + T::kA + kk * 32), b_desc(sb, kk), idesc, (s | kk) != 0);
-              mma_ss<CG>(low, desc_kmajor(sa + kk * 32), b_desc(sb + T::kB, kk), idesc, 1);
+              mma_ss<CG>(low, desc_kmajor(sa + T::kA + kk * 32), b_hi, idesc, (s | kk) != 0);
+              mma_ss<CG>(low, desc_kmajor(sa + kk * 32), b_base + ((sb + T::kB) >> 4) + kk * b_step, idesc, 1);
             }
-            mma_ss<CG>(big, desc_kmajor(sa + kk * 32), b_desc(sb, kk), idesc, (in_acc | kk) != 0);
+            mma_ss<CG>(big, desc_kmajor(sa + kk * 32), b_hi, idesc, (in_acc | kk) != 0);
           }
           mma_commit<CG>(&empty[stage]);
           if (++stage == T::kStages) { stage = 0; parity ^= 1u; }
@@ -464,64 +522,77 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_product_kernel(const Ort
     }
   } else if (warp == 10) {
     if (lane == 0) {
-      // strips in the order of the tiles: `ask` runs kRing ahead of `give`
-      struct Walk { int k, strip, live; OrthTile t; };
-      auto open = [&](Walk& w) {                           // to the next tile that has strips here
-        for (; w.k < p.num_tiles; w.k += stride) {
-          w.t = p.tiles[w.k];
-          w.live = orth_live_strips<KIND, SPLIT, CG>(p.mats[w.t.mat], w.t, rank);
-          w.strip = 0;
-          if (w.live > 0) return;
+      // `ask` brings strips, at most kRing of them ahead of `give`, which sends them off
+      struct Strips {
+        OrthWalk w;
+        int strip, live;
+        __device__ __forceinline__ Strips(const OrthParams& p, int worker, int rank) : w(p, worker) { open(rank); }
+        __device__ __forceinline__ void open(int rank) {                   // the next tile that has strips here
+          for (; w.more(); w.next()) {
+            live = orth_live_strips<SPLIT, CG>(w.kind, w.p.mats[w.t.mat], w.t, rank);
+            strip = 0;
+            if (live > 0) return;
+          }
         }
+        __device__ __forceinline__ void next(int rank) { if (++strip == live) { w.next(); open(rank); } }
       };
-      auto next = [&](Walk& w) { if (++w.strip == w.live) { w.k += stride; open(w); } };
-      const bool last = KIND == kOrthApply && p.last;
-      constexpr int kAddParts = KIND == kOrthGram ? 0 : KIND == kOrthApply || SPLIT ? 2 : 1;
-      constexpr int kOutParts = KIND == kOrthApply || SPLIT ? 2 : 1;
-      int loads = 0;
-      auto fetch = [&](Walk& w) {
-        const int b = loads % T::kRing;
-        unsigned char* at = smem + T::kStrips + b * 2 * kOrthStripPart;
-        if constexpr (kAddParts == 0) {
-          mbar_arrive_one(&strip_full[b]);
-        } else {
-          const CUtensorMap* map = p.maps + static_cast<long long>(w.t.mat) * kMapCount + (KIND == kOrthPoly ? kMapS : kMapX0 + 2 * p.src);
-          const int row = w.t.i * T::kTM + rank * 128, col = w.t.j * T::kTN + w.strip * 64;
-          mbar_expect_tx(&strip_full[b], kAddParts * kOrthStripPart);
-#pragma unroll
-          for (int part = 0; part < kAddParts; ++part)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) tma_load_2d(at + part * kOrthStripPart + h * 8192, map + part, &strip_full[b], col, row + h * 64);
-        }
-        ++loads;
-        next(w);
-      };
-      Walk ask = {first, 0, 0, {}}, give = {first, 0, 0, {}};
-      open(ask);
-      open(give);
-      for (int s = 0; s < T::kRing && ask.k < p.num_tiles; ++s) fetch(ask);
-      int b = 0;
+      Strips ask(p, worker, rank), give(p, worker, rank);
+      int loads = 0, stored = 0, b = 0;
       uint32_t parity = 0;
-      while (give.k < p.num_tiles) {
-        if (s_abort || !mbar_wait_bounded(&strip_done[b], parity)) { s_abort = 1; break; }
-        if (!last) {
-          const CUtensorMap* map = p.maps + static_cast<long long>(give.t.mat) * kMapCount + (KIND == kOrthGram ? kMapS : KIND == kOrthPoly ? kMapB : kMapX0 + 2 * (p.src ^ 1));
-          const unsigned char* at = smem + T::kStrips + b * 2 * kOrthStripPart;
-          const int row = give.t.i * T::kTM + rank * 128, col = give.t.j * T::kTN + give.strip * 64;
+      while (give.w.more() && !s_abort) {
+        const int ahead = loads - stored;
+        if (ask.w.more() && ahead < T::kRing) {
+          const int to = loads % T::kRing;
+          unsigned char* at = smem + T::kStrips + to * 2 * kOrthStripPart;
+          if (ask.w.kind == kOrthGram) {
+            mbar_arrive_one(&strip_full[to]);
+            ++loads;
+            ask.next(rank);
+            continue;
+          }
+          // nothing of this block may stay unsent while it waits for what others compute from it
+          const bool there = ahead > 0 ? orth_ready(ask.w) : orth_wait_ready(ask.w, &s_abort);
+          if (there) {
+            const int parts = ask.w.kind == kOrthApply || SPLIT ? 2 : 1;   // X is always a pair, S only in an fp32 context
+            const CUtensorMap* map = p.maps + static_cast<long long>(ask.w.t.mat) * kMapCount + (ask.w.kind == kOrthPoly ? kMapS : kMapX0 + 2 * (ask.w.step & 1));
+            const int row = ask.w.t.i * T::kTM + rank * 128, col = ask.w.t.j * T::kTN + ask.strip * 64;
+            mbar_expect_tx(&strip_full[to], parts * kOrthStripPart);
+            for (int part = 0; part < parts; ++part)
 #pragma unroll
-          for (int part = 0; part < kOutParts; ++part)
+              for (int h = 0; h < 2; ++h) tma_load_2d(at + part * kOrthStripPart + h * 8192, map + part, &strip_full[to], col, row + h * 64);
+            ++loads;
+            ask.next(rank);
+            continue;
+          }
+          if (ahead == 0) { s_abort = 1; break; }
+        }
+        if (!mbar_wait_bounded(&strip_done[b], parity)) { s_abort = 1; break; }
+        const bool last = give.w.kind == kOrthApply && give.w.step == p.steps - 1;     // written to the result by the warps themselves
+        if (!last) {
+          const int parts = give.w.kind == kOrthApply || SPLIT ? 2 : 1;
+          const CUtensorMap* map = p.maps + static_cast<long long>(give.w.t.mat) * kMapCount +
+                                   (give.w.kind == kOrthGram ? kMapS : give.w.kind == kOrthPoly ? kMapB : kMapX0 + 2 * ((give.w.step & 1) ^ 1));
+          const unsigned char* at = smem + T::kStrips + b * 2 * kOrthStripPart;
+          const int row = give.w.t.i * T::kTM + rank * 128, col = give.w.t.j * T::kTN + give.strip * 64;
+          for (int part = 0; part < parts; ++part)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              if (row + h * 64 < p.mats[give.t.mat].r) tma_store_2d(map + part, at + part * kOrthStripPart + h * 8192, col, row + h * 64);
+              if (row + h * 64 < p.mats[give.w.t.mat].r) tma_store_2d(map + part, at + part * kOrthStripPart + h * 8192, col, row + h * 64);
           bulk_commit();
-          bulk_wait_read<0>();
+          if (give.strip == give.live - 1) {               // the tile is complete: say so once its bytes are
+            bulk_wait<0>();
+            asm volatile("fence.proxy.async.global;" ::: "memory");
+            asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.done + give.w.t.mat) : "memory");
+          } else {
+            bulk_wait_read<0>();
+          }
         }
-        if (ask.k < p.num_tiles) fetch(ask);               // into the place that has just been read
-        next(give);
+        ++stored;
+        give.next(rank);
         if (++b == T::kRing) { b = 0; parity ^= 1u; }
       }
       bulk_wait<0>();
-      s_strips = kAddParts ? loads : 0;
+      s_strips = loads;
     }
   } else {
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -540,10 +611,14 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_product_kernel(const Ort
       buf ^= 1;
       if (buf == 0) parity ^= 1u;
     };
-    auto finish = [&](const OrthMat& m, const OrthTile& t, int strip, const uint32_t (&acc)[32]) {
+    auto finish = [&](const OrthWalk& w, const OrthStep& step, const OrthMat& m, int strip, const uint32_t (&acc)[32]) {
       if (!wait_for(&strip_full[place], strip_parity)) return false;
       unsigned char* at = smem + T::kStrips + place * 2 * kOrthStripPart + (warp & 3) * 32 * 128;
-      orth_finish_block<KIND, SPLIT, CG>(p, m, t.i * T::kTM + rank * 128 + (warp & 3) * 32, t.j * T::kTN + strip * 64 + half * 32, acc, at, at + kOrthStripPart, half);
+      const int row0 = w.t.i * T::kTM + rank * 128 + (warp & 3) * 32, col0 = w.t.j * T::kTN + strip * 64 + half * 32;
+      const bool last = w.step == p.steps - 1;
+      if (w.kind == kOrthGram) orth_finish_block<kOrthGram, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
+      else if (w.kind == kOrthPoly) orth_finish_block<kOrthPoly, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
+      else orth_finish_block<kOrthApply, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive_one(&strip_done[place]);
@@ -551,25 +626,25 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_product_kernel(const Ort
       return true;
     };
     bool ok = true;
-    for (int k = first; ok && k < p.num_tiles; k += stride) {
-      const OrthTile t = p.tiles[k];
-      const OrthMat& m = p.mats[t.mat];
-      const int live = orth_live_strips<KIND, SPLIT, CG>(m, t, rank);
+    for (OrthWalk w(p, worker); ok && w.more(); w.next()) {
+      const OrthMat& m = p.mats[w.t.mat];
+      const OrthStep step = p.coeffs[w.step];
+      const int live = orth_live_strips<SPLIT, CG>(w.kind, m, w.t, rank);
       if (!SPLIT) {
         if (!wait_for(&acc_full[buf], parity)) break;
         tc_fence_after();
         const uint32_t base = tmem + buf * T::kTN + half * 32 + lanes;
         if (live == 0) release();
+#pragma unroll 1
         for (int s = 0; ok && s < live; ++s) {
           uint32_t acc[32];
           tmem_ld32(base + s * 64, acc);
           tmem_wait_ld();
           if (s == live - 1) release();
-          ok = finish(m, t, s, acc);
+          ok = finish(w, step, m, s, acc);
         }
       } else {
-        const int K = KIND == kOrthGram ? m.l : m.r;
-        const int chunks = ((K + kOrthTK - 1) / kOrthTK + kOrthChunk - 1) / kOrthChunk;
+        const int chunks = ((w.t.depth + kOrthTK - 1) / kOrthTK + kOrthChunk - 1) / kOrthChunk;
         float sum[T::kBlocks][32];
         for (int q = 0; q < chunks; ++q) {
           if (!wait_for(&acc_full[buf], parity)) { ok = false; break; }
@@ -602,7 +677,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_product_kernel(const Ort
           uint32_t acc[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) acc[e] = __float_as_uint(sum[s][e]);
-          ok = finish(m, t, s, acc);
+          ok = finish(w, step, m, s, acc);
         }
       }
     }

@@ -22,8 +22,8 @@ namespace {
 
 template <int DT, bool IL>
 bool launch_rope(const RopeParams& p, bool vec, unsigned blocks, cudaStream_t st) {
-  return vec ? launch(&rope_kernel<DT, IL, true>, dim3(blocks), dim3(kRopeThreads), 0, st, false, 1, p)
-             : launch(&rope_kernel<DT, IL, false>, dim3(blocks), dim3(kRopeThreads), 0, st, false, 1, p);
+  return vec ? launch(&rope_kernel<DT, IL, true>, dim3(blocks), dim3(kRopeThreads), 0, st, kLaunchPlain, 1, p)
+             : launch(&rope_kernel<DT, IL, false>, dim3(blocks), dim3(kRopeThreads), 0, st, kLaunchPlain, 1, p);
 }
 
 }  // namespace
