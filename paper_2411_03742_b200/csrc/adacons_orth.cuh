@@ -479,7 +479,11 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
       s_issued = issued;
     }
   } else if (warp == 9) {
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
+      // The whole warp goes through the loop, so that addresses and descriptors are uniform values; one
+      // lane issues.  With the loop itself inside one lane's branch, a product of 64 cycles took 150 to issue.
+      const bool issuer = elect_one();
+      const uint32_t base = smem_addr(smem) >> 4;                          // descriptors count 16-byte units
       int stage = 0, buf = 0, small = 0;
       uint32_t parity = 0, acc_parity = 1;
       bool ok = true;
@@ -487,38 +491,45 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
         const bool across = w.kind == kOrthApply;
         const uint32_t idesc = across ? mma_idesc(T::kTM, T::kTN, false, false, true) : mma_idesc(T::kTM, T::kTN, false, false, false);
         const uint64_t b_base = across ? desc_mnmajor(0, 8192) : desc_kmajor(0);
-        const uint32_t b_step = across ? 2048 / 16 : 32 / 16;              // descriptors count 16-byte units
+        const uint32_t b_step = across ? 2048 / 16 : 32 / 16;
         const int steps = (w.t.depth + kOrthTK - 1) / kOrthTK;
+        int in_acc = 0;
         for (int s = 0; s < steps; ++s) {
-          const int in_acc = SPLIT ? s % kOrthChunk : s;
           if (in_acc == 0) {
-            if (s_abort || !mbar_wait_bounded(&acc_free[buf], acc_parity)) { s_abort = 1; ok = false; break; }
-            tc_fence_after();
+            if (s_abort || !mbar_wait_bounded(&acc_free[buf], acc_parity)) ok = false;
           }
-          if (s_abort || !mbar_wait_bounded(&full[stage], parity)) { s_abort = 1; ok = false; break; }
+          ok = ok && !s_abort && mbar_wait_bounded(&full[stage], parity);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) { s_abort = 1; break; }
           tc_fence_after();
           const uint32_t big = tmem + buf * T::kTN, low = tmem + (2 + small) * T::kTN;
-          const uint32_t sa = smem_addr(smem + stage * T::kStage), sb = sa + T::kParts * T::kA;
+          const uint64_t a_hi = desc_kmajor(0) + (base + stage * (T::kStage >> 4)), a_lo = a_hi + (T::kA >> 4);
+          const uint64_t b_hi = b_base + (base + stage * (T::kStage >> 4) + ((T::kParts * T::kA) >> 4)), b_lo = b_hi + (T::kB >> 4);
+          if (issuer) {
 #pragma unroll
-          for (int kk = 0; kk < kOrthTK / 16; ++kk) {
-            const uint64_t b_hi = b_base + (sb >> 4) + kk * b_step;
-            if (SPLIT) {
-              mma_ss<CG>(low, desc_kmajor(sa + T::kA + kk * 32), b_hi, idesc, (s | kk) != 0);
-              mma_ss<CG>(low, desc_kmajor(sa + kk * 32), b_base + ((sb + T::kB) >> 4) + kk * b_step, idesc, 1);
+            for (int kk = 0; kk < kOrthTK / 16; ++kk) {
+              if (SPLIT) {
+                mma_ss<CG>(low, a_lo + kk * 2, b_hi + kk * b_step, idesc, kk != 0 ? 1u : s != 0);
+                mma_ss<CG>(low, a_hi + kk * 2, b_lo + kk * b_step, idesc, 1u);
+              }
+              mma_ss<CG>(big, a_hi + kk * 2, b_hi + kk * b_step, idesc, kk != 0 ? 1u : in_acc != 0);
             }
-            mma_ss<CG>(big, desc_kmajor(sa + kk * 32), b_hi, idesc, (in_acc | kk) != 0);
+            mma_commit<CG>(&empty[stage]);
           }
-          mma_commit<CG>(&empty[stage]);
+          __syncwarp();
           if (++stage == T::kStages) { stage = 0; parity ^= 1u; }
-          if (s == steps - 1 || (SPLIT && in_acc == kOrthChunk - 1)) {
-            mma_commit<CG>(&acc_full[buf]);
+          ++in_acc;
+          if (s == steps - 1 || (SPLIT && in_acc == kOrthChunk)) {
+            if (issuer) mma_commit<CG>(&acc_full[buf]);
+            in_acc = 0;
             buf ^= 1;
             if (buf == 0) acc_parity ^= 1u;
           }
         }
         small ^= 1;
       }
-      if (s_abort) { mma_commit<CG>(drain); mbar_wait_bounded(drain, 0); }
+      if (s_abort && issuer) { mma_commit<CG>(drain); mbar_wait_bounded(drain, 0); }
+      __syncwarp();
     }
   } else if (warp == 10) {
     if (lane == 0) {
