@@ -82,24 +82,29 @@ __device__ __forceinline__ void attn_zero_rows(unsigned char* tile, int first) {
   __syncwarp();
 }
 
+// The products are issued by one lane, but their descriptors are made by the whole warp, so that they are
+// uniform values (made inside the lane's branch they cost more time than the products themselves).
+template <int D> struct AttnDesc {
+  static __device__ __forceinline__ uint64_t rows(uint32_t addr) { return desc_kmajor(0) + (addr >> 4); }                                  // product over head elements
+  static __device__ __forceinline__ uint64_t tokens(uint32_t addr) { return desc_mnmajor(0, AttnTile<D>::kBlock) + (addr >> 4); }          // product over tokens
+};
 // 128 x 128 product over head elements: rows of `a` with rows of `b`
 template <int D, bool BF16>
-__device__ __forceinline__ void attn_mma_rows(uint32_t d, uint32_t a, uint32_t b) {
+__device__ __forceinline__ void attn_mma_rows(uint32_t d, uint64_t a, uint64_t b) {
   constexpr uint32_t idesc = mma_idesc(kAttnTile, kAttnTile, BF16, false, false);
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) {
-    const uint32_t off = (k / 4) * AttnTile<D>::kBlock + (k % 4) * 32;
-    mma_ss(d, desc_kmajor(a + off), desc_kmajor(b + off), idesc, k != 0);
+    const uint32_t off = ((k / 4) * AttnTile<D>::kBlock + (k % 4) * 32) >> 4;
+    mma_ss(d, a + off, b + off, idesc, k != 0);
   }
 }
 // 128 x D product over tokens: 16-bit values in tensor memory with the tokens of `b`.  The 128 columns of
 // values lie in two halves of 32 words, `step` apart.
 template <int D, bool BF16>
-__device__ __forceinline__ void attn_mma_tokens(uint32_t d, uint32_t a, uint32_t step, uint32_t b, bool accumulate) {
+__device__ __forceinline__ void attn_mma_tokens(uint32_t d, uint32_t a, uint32_t step, uint64_t b, bool accumulate) {
   constexpr uint32_t idesc = mma_idesc(kAttnTile, D, BF16, false, true);
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
-    mma_ts(d, a + (k / 4) * step + (k % 4) * 8, desc_mnmajor(b + k * 2048, AttnTile<D>::kBlock), idesc, (accumulate || k != 0) ? 1u : 0u);
+  for (int k = 0; k < 8; ++k) mma_ts(d, a + (k / 4) * step + (k % 4) * 8, b + k * (2048 >> 4), idesc, k != 0 ? 1u : accumulate);
 }
 
 // Row `row` of an accumulator (this thread's lane), columns [0, D), times `mul`, to global memory.
@@ -208,6 +213,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       }
     }
   } else if (tiles > 0 && warp == 9) {
+    const bool issuer = elect_one();
     int slot = 0;
     uint32_t parity = 0;
     bool ok = mbar_wait_bounded(q_full, 0);
@@ -216,8 +222,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       ok = ok && !s_abort && mbar_wait_bounded(&kv_full[slot], parity);
       ok = __all_sync(0xffffffffu, ok);
       if (ok && valid < kAttnTile) attn_zero_rows<D>(smem + L::kKV + slot * L::kT, valid);
-      const uint32_t at = smem_addr(smem + L::kKV + slot * L::kT);
-      return at;
+      return smem_addr(smem) + L::kKV + slot * L::kT;
     };
     auto wait_p = [&](int t, int j) {
       ok = ok && !s_abort && mbar_wait_bounded(&p_full[t], j & 1);
@@ -225,12 +230,13 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       tc_fence_after();
     };
     auto advance = [&]() { if (++slot == L::kSlots) { slot = 0; parity ^= 1u; } };
-    const uint32_t sq = smem_addr(smem);
-    uint32_t k_at = take(kAttnTile);
-    if (ok && lane == 0) {
-      tc_fence_after();
+    const uint64_t q_desc = AttnDesc<D>::rows(smem_addr(smem));
+    uint64_t k_desc = AttnDesc<D>::rows(take(kAttnTile));
+    tc_fence_after();
+    if (ok && issuer) {
+#pragma unroll
       for (int t = 0; t < 2; ++t) {
-        attn_mma_rows<D, BF16>(tmem + t * 128, sq + t * L::kT, k_at);
+        attn_mma_rows<D, BF16>(tmem + t * 128, q_desc + t * (L::kT >> 4), k_desc);
         mma_commit(&s_full[t]);
       }
       mma_commit(&kv_free[slot]);
@@ -239,24 +245,25 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     advance();
     for (int j = 0; ok && j < tiles; ++j) {
       const int v_slot = slot;
-      const uint32_t v_at = take(min(kv_len - j * kAttnTile, kAttnTile));
+      const uint64_t v_desc = AttnDesc<D>::tokens(take(min(kv_len - j * kAttnTile, kAttnTile)));
       advance();
-      int k_slot = slot;
-      if (ok && j + 1 < tiles) { k_slot = slot; k_at = take(kAttnTile); advance(); }
+      const int k_slot = slot;
+      const bool more = j + 1 < tiles;
+      if (ok && more) { k_desc = AttnDesc<D>::rows(take(kAttnTile)); advance(); }
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         if (ok) wait_p(t, j);
-        if (ok && lane == 0) {
-          attn_mma_tokens<D, BF16>(tmem + 256 + t * 128, tmem + t * 128, 32, v_at, j != 0);
-          if (j + 1 < tiles) {
-            attn_mma_rows<D, BF16>(tmem + t * 128, sq + t * L::kT, k_at);
+        if (ok && issuer) {
+          attn_mma_tokens<D, BF16>(tmem + 256 + t * 128, tmem + t * 128, 32, v_desc, j != 0);
+          if (more) {
+            attn_mma_rows<D, BF16>(tmem + t * 128, q_desc + t * (L::kT >> 4), k_desc);
             mma_commit(&s_full[t]);
           } else {
             mma_commit(&o_full[t]);
           }
           if (t == 1) {
             mma_commit(&kv_free[v_slot]);
-            if (j + 1 < tiles) mma_commit(&kv_free[k_slot]);
+            if (more) mma_commit(&kv_free[k_slot]);
           }
         }
         __syncwarp();
@@ -264,7 +271,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     }
     if (!ok) {
       s_abort = 1;
-      if (lane == 0) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
+      if (issuer) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
     }
   } else if (warp < 8) {
     const int t = warp >> 2;
@@ -497,44 +504,60 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       attn_zero_rows<D>(smem, kv_len - k0);
       attn_zero_rows<D>(smem + L::kT, kv_len - k0);
     }
-    if (lane == 0) {
-      const uint32_t sk = smem_addr(smem), sv = sk + L::kT;
-      auto q_at = [&](int n) { return smem_addr(smem + L::kRing + (n % L::kStages) * L::kStage); };
-      auto wait = [&](uint64_t* bar, uint32_t parity) {
-        ok = ok && !s_abort && mbar_wait_bounded(bar, parity);
-        tc_fence_after();
-        return ok;
-      };
-      if (wait(&full[0], 0)) {
-        attn_mma_rows<D, BF16>(t_s, sk, q_at(0));
+    const bool issuer = elect_one();
+    const uint64_t k_desc = AttnDesc<D>::rows(smem_addr(smem)), v_desc = k_desc + (L::kT >> 4);
+    const uint32_t ring = smem_addr(smem) + L::kRing;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = ok && !s_abort && mbar_wait_bounded(bar, parity);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      return ok;
+    };
+    if (wait(&full[0], 0)) {
+      const uint64_t q_desc = AttnDesc<D>::rows(ring);
+      if (issuer) {
+        attn_mma_rows<D, BF16>(t_s, k_desc, q_desc);
         mma_commit(s_full);
-        attn_mma_rows<D, BF16>(t_dp, sv, q_at(0) + L::kT);
+        attn_mma_rows<D, BF16>(t_dp, v_desc, q_desc + (L::kT >> 4));
         mma_commit(dp_full);
       }
-      for (int n = 0; ok && n < items; ++n) {
-        const int next = n + 1;
-        if (!wait(p_full, n & 1)) break;
-        attn_mma_tokens<D, BF16>(t_dv, t_s, 64, q_at(n) + L::kT, n != 0);
-        if (next < items) {
-          if (!wait(&full[next % L::kStages], (next / L::kStages) & 1)) break;
-          attn_mma_rows<D, BF16>(t_s, sk, q_at(next));
+      __syncwarp();
+    }
+    int stage = 0;
+    uint32_t next_parity = 0;              // of the next item's stage
+    for (int n = 0; ok && n < items; ++n) {
+      const bool more = n + 1 < items;
+      const int next_stage = stage + 1 == L::kStages ? 0 : stage + 1;
+      if (next_stage == 0) next_parity ^= 1u;
+      const uint64_t by_tokens = AttnDesc<D>::tokens(ring + stage * L::kStage), next_rows = AttnDesc<D>::rows(ring + next_stage * L::kStage);
+      if (!wait(p_full, n & 1)) break;
+      if (issuer) attn_mma_tokens<D, BF16>(t_dv, t_s, 64, by_tokens + (L::kT >> 4), n != 0);
+      __syncwarp();
+      if (more) {
+        if (!wait(&full[next_stage], next_parity)) break;
+        if (issuer) {
+          attn_mma_rows<D, BF16>(t_s, k_desc, next_rows);
           mma_commit(s_full);
         }
-        if (!wait(ds_full, n & 1)) break;
-        attn_mma_tokens<D, BF16>(t_dk, t_dp, 64, q_at(n), n != 0);
-        mma_commit(&free_[n % L::kStages]);
-        if (next < items) {
-          attn_mma_rows<D, BF16>(t_dp, sv, q_at(next) + L::kT);
+        __syncwarp();
+      }
+      if (!wait(ds_full, n & 1)) break;
+      if (issuer) {
+        attn_mma_tokens<D, BF16>(t_dk, t_dp, 64, by_tokens, n != 0);
+        mma_commit(&free_[stage]);
+        if (more) {
+          attn_mma_rows<D, BF16>(t_dp, v_desc, next_rows + (L::kT >> 4));
           mma_commit(dp_full);
         } else {
           mma_commit(done);
         }
       }
-      if (!ok) {
-        s_abort = 1;
-        mma_commit(drain);
-        mbar_wait_bounded(drain, 0);
-      }
+      __syncwarp();
+      stage = next_stage;
+    }
+    if (!ok) {
+      s_abort = 1;
+      if (issuer) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
     }
   } else if (warp < 8) {
     const int half = warp >> 2;                  // this warp's 64 queries of each tile
@@ -729,14 +752,16 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       tc_fence_after();
       return ok;
     };
-    const uint32_t sq = smem_addr(smem), sdo = sq + L::kT;
+    const bool issuer = elect_one();
+    const uint64_t q_desc = AttnDesc<D>::rows(smem_addr(smem)), do_desc = q_desc + (L::kT >> 4);
     auto scores = [&](int j) {                   // S(j)
       const int ks = j % L::kKs;
       if (!wait(&k_full[ks], (j / L::kKs) & 1)) return;
       unsigned char* at = smem + L::kK + ks * L::kT;
       if ((j + 1) * kAttnTile > kv_len) attn_zero_rows<D>(at, kv_len - j * kAttnTile);
-      if (lane == 0) {
-        attn_mma_rows<D, BF16>(tmem + (j & 1) * 128, sq, smem_addr(at));
+      const uint64_t k_desc = AttnDesc<D>::rows(smem_addr(at));
+      if (issuer) {
+        attn_mma_rows<D, BF16>(tmem + (j & 1) * 128, q_desc, k_desc);
         mma_commit(&s_full[j & 1]);
       }
       __syncwarp();
@@ -746,8 +771,9 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       if (!wait(&v_full[vs], (j / L::kVs) & 1)) return;
       unsigned char* at = smem + L::kV + vs * L::kT;
       if ((j + 1) * kAttnTile > kv_len) attn_zero_rows<D>(at, kv_len - j * kAttnTile);
-      if (lane == 0) {
-        attn_mma_rows<D, BF16>(t_dp, sdo, smem_addr(at));
+      const uint64_t v_desc = AttnDesc<D>::rows(smem_addr(at));
+      if (issuer) {
+        attn_mma_rows<D, BF16>(t_dp, do_desc, v_desc);
         mma_commit(dp_full);
         mma_commit(&v_free[vs]);
       }
@@ -765,8 +791,9 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
         if (!ok) break;
       }
       if (!wait(&ds_full[j & 1], (j >> 1) & 1)) break;
-      if (lane == 0) {
-        attn_mma_tokens<D, BF16>(t_dq, tmem + (j & 1) * 128, 64, smem_addr(smem + L::kK + (j % L::kKs) * L::kT), j != 0);
+      const uint64_t k_desc = AttnDesc<D>::tokens(smem_addr(smem) + L::kK + (j % L::kKs) * L::kT);
+      if (issuer) {
+        attn_mma_tokens<D, BF16>(t_dq, tmem + (j & 1) * 128, 64, k_desc, j != 0);
         mma_commit(&k_free[j % L::kKs]);
         if (j == tiles - 1) mma_commit(done);
       }
@@ -774,7 +801,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
     }
     if (!ok) {
       s_abort = 1;
-      if (lane == 0) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
+      if (issuer) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
     }
   } else if (warp < 8) {
     const int half = warp >> 2;                  // this warp's 64 keys of each tile
