@@ -26,7 +26,8 @@ namespace adacons {
 // inputs' 16-bit type as operands of the second products, an error of the size of the results' own rounding.
 // ----------------------------------------------------------------------------------------------
 constexpr int kAttnTile = 128;
-constexpr int kAttnThreads = 320;                // warps 0-7 elementwise, 8 copies, 9 products
+constexpr int kAttnThreads = 576;                // warps 0-15 elementwise, 16 copies, 17 products
+constexpr int kAttnCopyWarp = 16, kAttnMmaWarp = 17;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttnOut { void* p; long long batch, seq, head; };     // element strides
@@ -98,28 +99,28 @@ __device__ __forceinline__ void attn_mma_rows(uint32_t d, uint64_t a, uint64_t b
     mma_ss(d, a + off, b + off, idesc, k != 0);
   }
 }
-// 128 x D product over tokens: 16-bit values in tensor memory with the tokens of `b`.  The 128 columns of
-// values lie in two halves of 32 words, `step` apart.
+// 128 x D product over tokens: 16-bit values in tensor memory with the tokens of `b`.  Whoever had columns
+// 32 g .. 32 g + 31 of the fp32 scores puts their 16 words of 16-bit values in the first half of that place.
 template <int D, bool BF16>
-__device__ __forceinline__ void attn_mma_tokens(uint32_t d, uint32_t a, uint32_t step, uint64_t b, bool accumulate) {
+__device__ __forceinline__ void attn_mma_tokens(uint32_t d, uint32_t a, uint64_t b, bool accumulate) {
   constexpr uint32_t idesc = mma_idesc(kAttnTile, D, BF16, false, true);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) mma_ts(d, a + (k / 4) * step + (k % 4) * 8, b + k * (2048 >> 4), idesc, k != 0 ? 1u : accumulate);
+  for (int k = 0; k < 8; ++k) mma_ts(d, a + (k / 2) * 32 + (k % 2) * 8, b + k * (2048 >> 4), idesc, k != 0 ? 1u : accumulate);
 }
 
-// Row `row` of an accumulator (this thread's lane), columns [0, D), times `mul`, to global memory.
-template <int D, bool BF16>
-__device__ __forceinline__ void attn_store_row(const AttnParams& p, const AttnOut& o, uint32_t tmem, int batch, int head, int row, bool live, float mul) {
-  unsigned short* dst = static_cast<unsigned short*>(o.p) + batch * o.batch + static_cast<long long>(row) * o.seq + head * o.head;
+// Columns [first, first + 32 BLOCKS) of row `row` of an accumulator (this thread's lane), times `mul`, to global memory.
+template <int BLOCKS, bool BF16>
+__device__ __forceinline__ void attn_store_row(const AttnParams& p, const AttnOut& o, uint32_t tmem, int first, int batch, int head, int row, bool live, float mul) {
+  unsigned short* dst = static_cast<unsigned short*>(o.p) + batch * o.batch + static_cast<long long>(row) * o.seq + head * o.head + first;
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c) {
+  for (int c = 0; c < BLOCKS; ++c) {
     uint32_t v[32];
     __syncwarp();
-    tmem_ld32(tmem + c * 32, v);
+    tmem_ld32(tmem + first + c * 32, v);
     tmem_wait_ld();
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      if (!live || c * 32 + g * 8 >= p.D) continue;       // the head size is a multiple of eight
+      if (!live || first + c * 32 + g * 8 >= p.D) continue;       // the head size is a multiple of eight
       uint32_t w[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = pack16<BF16>(__uint_as_float(v[8 * g + 2 * k]) * mul, __uint_as_float(v[8 * g + 2 * k + 1]) * mul);
@@ -141,8 +142,9 @@ __device__ __forceinline__ int attn_kv_len(const AttnParams& p, int batch) {
 // ----------------------------------------------------------------------------------------------
 // Forward.  A block owns two tiles of 128 queries and walks over the key tiles, the softmax of one
 // query tile running while the tensor cores work for the other.  Tensor memory: S of both tiles (128
-// columns each, later the rounded P in its place) and both accumulators.  A thread holds one query's
-// whole row of scores, so that maximum and sum need no exchange.  The running maximum is only raised
+// columns each, later the rounded P in its place) and both accumulators.  Two threads share one query's
+// row of scores and exchange their maxima (one thread a row needs none, but with two warps per scheduler
+// every instruction's latency shows: 5200 cycles per pair of tiles, of which 2200 are products).  The running maximum is only raised
 // when a row's scores exceed it by more than 2^8 in the exponential (the quotient O / sum does not
 // depend on it, and fp32 and bf16 have the range): the accumulator is then rescaled in place, which
 // after the first few key tiles hardly happens.
@@ -150,7 +152,9 @@ __device__ __forceinline__ int attn_kv_len(const AttnParams& p, int batch) {
 template <int D> struct AttnFwdSmem {
   static constexpr uint32_t kT = AttnTile<D>::kBytes;
   static constexpr int kSlots = D == 128 ? 5 : 8;              // ring of K and V tiles in turn
-  static constexpr uint32_t kKV = 2 * kT, kBars = kKV + kSlots * kT, kBytes = kBars + 256 + 1024;
+  // In front of the tiles, which fill the rest of the block's 227 KB at D = 128: barriers, 2 words, the rows'
+  // exchange.  Dynamic shared memory starts on a 1024-byte boundary where a kernel has no static one.
+  static constexpr uint32_t kRow = 512, kTiles = 3072, kKV = 2 * kT, kBytes = kTiles + kKV + kSlots * kT;
 };
 
 template <int D, bool BF16>
@@ -158,16 +162,23 @@ __global__ void __launch_bounds__(kAttnThreads, 1)
 attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const AttnParams p) {
   extern __shared__ unsigned char smem_dyn[];
   using L = AttnFwdSmem<D>;
-  unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
-  uint64_t* q_full = reinterpret_cast<uint64_t*>(smem + L::kBars);
+  if ((smem_addr(smem_dyn) & 1023u) != 0) {      // the layout's premise; the whole block agrees
+    if (threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
+    return;
+  }
+  unsigned char* smem = smem_dyn + L::kTiles;
+  uint64_t* q_full = reinterpret_cast<uint64_t*>(smem_dyn);
   uint64_t* kv_full = q_full + 1;                // [kSlots]
   uint64_t* kv_free = kv_full + L::kSlots;       // [kSlots]
   uint64_t* s_full = kv_free + L::kSlots;        // [2]
   uint64_t* p_full = s_full + 2;                 // [2]
   uint64_t* o_full = p_full + 2;                 // [2]
-  uint64_t* drain = o_full + 2;
-  __shared__ uint32_t s_tmem;
-  __shared__ volatile int s_abort;
+  uint64_t* pair = o_full + 2;                   // [8] the two warps of a query tile's 32 rows
+  uint64_t* drain = pair + 8;
+  static_assert((1 + 2 * L::kSlots + 6 + 8 + 1) * 8 + 8 <= L::kRow && L::kRow + 2 * 2 * kAttnTile * 4 <= L::kTiles, "what lies in front of the tiles");
+  uint32_t& s_tmem = *reinterpret_cast<uint32_t*>(drain + 1);
+  volatile int& s_abort = *reinterpret_cast<volatile int*>(&s_tmem + 1);
+  float* s_row = reinterpret_cast<float*>(smem_dyn + L::kRow);       // [half][row]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int head = blockIdx.y, batch = blockIdx.z;
   const int blk = gridDim.x - 1 - blockIdx.x;    // with a causal mask the last queries have the most keys: first
@@ -176,13 +187,14 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
   if (threadIdx.x == 0) {
     mbar_init(q_full, 1);
     for (int s = 0; s < L::kSlots; ++s) { mbar_init(&kv_full[s], 1); mbar_init(&kv_free[s], 1); }
-    for (int t = 0; t < 2; ++t) { mbar_init(&s_full[t], 1); mbar_init(&p_full[t], 4); mbar_init(&o_full[t], 1); }
+    for (int t = 0; t < 2; ++t) { mbar_init(&s_full[t], 1); mbar_init(&p_full[t], 8); mbar_init(&o_full[t], 1); }
+    for (int t = 0; t < 8; ++t) mbar_init(&pair[t], 2);
     mbar_init(drain, 1);
     s_abort = 0;
     mbar_init_fence();
     fence_proxy_async_smem();
   }
-  if (warp == 9) tmem_alloc(&s_tmem, 512);
+  if (warp == kAttnMmaWarp) tmem_alloc(&s_tmem, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -193,7 +205,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
   const int seen = p.causal ? min(kv_len, max(0, q_last + off + 1)) : kv_len;     // keys that any query of the block sees
   const int tiles = (seen + kAttnTile - 1) / kAttnTile;
 
-  if (tiles > 0 && warp == 8) {
+  if (tiles > 0 && warp == kAttnCopyWarp) {
     if (lane == 0) {
       mbar_expect_tx(q_full, 2 * L::kT);
       for (int t = 0; t < 2; ++t) attn_load_tile<D>(smem + t * L::kT, &mq, q_full, q0 + t * kAttnTile, head, batch);
@@ -212,7 +224,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
         for (int s = 0; s < L::kSlots && s < issued; ++s) mbar_wait_bounded(&kv_full[s], ((issued - 1 - s) / L::kSlots) & 1);
       }
     }
-  } else if (tiles > 0 && warp == 9) {
+  } else if (tiles > 0 && warp == kAttnMmaWarp) {
     const bool issuer = elect_one();
     int slot = 0;
     uint32_t parity = 0;
@@ -254,7 +266,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       for (int t = 0; t < 2; ++t) {
         if (ok) wait_p(t, j);
         if (ok && issuer) {
-          attn_mma_tokens<D, BF16>(tmem + 256 + t * 128, tmem + t * 128, 32, v_desc, j != 0);
+          attn_mma_tokens<D, BF16>(tmem + 256 + t * 128, tmem + t * 128, v_desc, j != 0);
           if (more) {
             attn_mma_rows<D, BF16>(tmem + t * 128, q_desc + t * (L::kT >> 4), k_desc);
             mma_commit(&s_full[t]);
@@ -273,72 +285,94 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       s_abort = 1;
       if (issuer) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
     }
-  } else if (warp < 8) {
-    const int t = warp >> 2;
-    const int row = q0 + t * kAttnTile + (warp & 3) * 32 + lane;
+  } else if (warp < 16) {
+    const int t = warp >> 3, half = (warp >> 2) & 1;             // this warp's query tile and its 64 keys of each key tile
+    const int lrow = t * kAttnTile + (warp & 3) * 32 + lane, row = q0 + lrow;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_at = tmem + t * 128 + lanes, o_at = tmem + 256 + t * 128 + lanes;
+    const uint32_t s_at = tmem + t * 128 + half * 64 + lanes, o_at = tmem + 256 + t * 128 + lanes;
     const int limit = p.causal ? min(kv_len, row + off + 1) : kv_len;        // this query's keys: [0, limit)
     const int warp_limit = p.causal ? min(kv_len, row - lane + off + 1) : kv_len;   // all of the warp's queries see these
-    float top = -INFINITY, sum = 0.f;            // running maximum of scale_log2 S and the sum under it
+    uint64_t* both = &pair[t * 4 + (warp & 3)];
+    uint32_t turn = 0;
     bool ok = true;
+    // The other half's value for this row.  The next exchange comes after the products that both warps' P go
+    // into, so a place is never written before it has been read.
+    auto exchange = [&](float mine) {
+      s_row[half * 2 * kAttnTile + lrow] = mine;
+      __syncwarp();
+      if (lane == 0) mbar_arrive_one(both);
+      ok = ok && !s_abort && mbar_wait_bounded(both, turn);
+      ok = __all_sync(0xffffffffu, ok);
+      turn ^= 1u;
+      return s_row[(half ^ 1) * 2 * kAttnTile + lrow];
+    };
+    float top = -INFINITY, sum = 0.f;            // running maximum of scale_log2 S, this half's sum under it
+    const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
     for (int j = 0; ok && j < tiles; ++j) {
       ok = !s_abort && mbar_wait_bounded(&s_full[t], j & 1);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      uint32_t s[4][32];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32(s_at + c * 32, s[c]);
-      tmem_wait_ld();
-      const int k0 = j * kAttnTile;
-      if (k0 + kAttnTile > warp_limit) {         // warp-uniform: some score of the tile is masked
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
+      const int k0 = j * kAttnTile + half * 64;
+      const bool masked = k0 + 64 > warp_limit;              // warp-uniform: some score is masked
+      // 32 scores at a time, read again for the exponentials: 64 registers more would spill at this block size
+      uint32_t s[32];
+      auto fetch = [&](int c) {
+        tmem_ld32(s_at + c * 32, s);
+        tmem_wait_ld();
+        if (masked) {
 #pragma unroll
           for (int e = 0; e < 32; ++e)
-            if (k0 + c * 32 + e >= limit) s[c][e] = 0xff800000u;
-      }
+            if (k0 + c * 32 + e >= limit) s[e] = 0xff800000u;
+        }
+      };
       float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+      for (int c = 0; c < 2; ++c) {
+        fetch(c);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) m[e & 3] = fmaxf(m[e & 3], __uint_as_float(s[c][e]));
-      const float tile_top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * p.scale_log2;
+        for (int e = 0; e < 32; ++e) m[e & 3] = fmaxf(m[e & 3], __uint_as_float(s[e]));
+      }
+      float tile_top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+      tile_top = fmaxf(tile_top, exchange(tile_top)) * p.scale_log2;
+      if (!ok) break;
       const bool raise = tile_top > top + 8.f;   // also the first time a row sees a key
       if (__any_sync(0xffffffffu, raise)) {
         const float next = raise ? tile_top : top;
         const float factor = raise ? exp2_fast(top - next) : 1.f;
         sum *= factor;
         top = next;
-        if (j > 0) {
+        if (j > 0) {                             // half of the accumulator's columns
 #pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
+          for (int c = 0; c < D / 64; ++c) {
             uint32_t o[32];
-            tmem_ld32(o_at + c * 32, o);
+            tmem_ld32(o_at + half * (D / 2) + c * 32, o);
             tmem_wait_ld();
 #pragma unroll
             for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-            tmem_st32(o_at + c * 32, o);
+            tmem_st32(o_at + half * (D / 2) + c * 32, o);
           }
         }
       }
-      const float base = top == -INFINITY ? 0.f : top;
-      float part[4] = {0.f, 0.f, 0.f, 0.f};
+      const float base = top == -INFINITY ? 0.f : -top;
+      const float2 base2 = make_float2(base, base);
+      float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {              // 64 keys at a time: 32 words of P
-        uint32_t w[32];
+      for (int c = 0; c < 2; ++c) {
+        uint32_t w[16];
+        fetch(c);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const float p0 = exp2_fast(fmaf(__uint_as_float(s[2 * c + e / 16][(2 * e) & 31]), p.scale_log2, -base));
-          const float p1 = exp2_fast(fmaf(__uint_as_float(s[2 * c + e / 16][(2 * e + 1) & 31]), p.scale_log2, -base));
-          part[(2 * e) & 3] += p0;
-          part[(2 * e + 1) & 3] += p1;
-          w[e] = pack16<BF16>(p0, p1);
+        for (int e = 0; e < 16; ++e) {
+          float2 x = fma2(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), scale2, base2);
+          x.x = exp2_fast(x.x);
+          x.y = exp2_fast(x.y);
+          part[e & 1] = add2(part[e & 1], x);
+          w[e] = pack16<BF16>(x.x, x.y);
         }
-        tmem_st32(s_at + c * 32, w);
+        tmem_st16(s_at + c * 32, w);
       }
-      sum += (part[0] + part[1]) + (part[2] + part[3]);
+      part[0] = add2(part[0], part[1]);
+      sum += part[0].x + part[0].y;
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
@@ -349,18 +383,19 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       ok = !s_abort && mbar_wait_bounded(&o_full[t], 0);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
-      if (ok) attn_store_row<D, BF16>(p, p.out, o_at, batch, head, row, live, sum == 0.f ? 0.f : 1.f / sum);
-    } else if (tiles == 0 && live) {
+      sum += exchange(sum);
+      if (ok) attn_store_row<D / 64, BF16>(p, p.out, o_at, half * (D / 2), batch, head, row, live, sum == 0.f ? 0.f : 1.f / sum);
+    } else if (tiles == 0 && live && half == 0) {
       attn_zero_row(p, p.out, batch, head, row);
     }
-    if (ok && live) p.lse[(static_cast<long long>(batch) * p.Hq + head) * p.Sq + row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    if (ok && live && half == 0) p.lse[(static_cast<long long>(batch) * p.Hq + head) * p.Sq + row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     if (!ok) s_abort = 1;
   }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (s_abort && threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
-  if (warp == 9) {
+  if (warp == kAttnMmaWarp) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -410,7 +445,7 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnRows dout, co
 // The products are issued so that each elementwise phase has two products beside it:
 //     P(i) from S(i)       | dK(i-1), dP(i)
 //     dS(i) from P, dP(i)  | dV(i), S(i+1)
-// Two warps share a block of 32 keys, 64 queries each.
+// Four warps share a block of 32 keys, 32 queries each.
 // ----------------------------------------------------------------------------------------------
 template <int D> struct AttnDkvSmem {
   static constexpr uint32_t kT = AttnTile<D>::kBytes;
@@ -448,16 +483,16 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
     mbar_init(kv_full, 1);
     for (int s = 0; s < L::kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&free_[s], 1); }
     mbar_init(s_full, 1);
-    mbar_init(p_full, 8);
+    mbar_init(p_full, 16);
     mbar_init(dp_full, 1);
-    mbar_init(ds_full, 8);
+    mbar_init(ds_full, 16);
     mbar_init(done, 1);
     mbar_init(drain, 1);
     s_abort = 0;
     mbar_init_fence();
     fence_proxy_async_smem();
   }
-  if (warp == 9) tmem_alloc(&s_tmem, 512);
+  if (warp == kAttnMmaWarp) tmem_alloc(&s_tmem, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -472,7 +507,7 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
   const int items = group * per_head;
   pdl_wait();                                    // the statistics
 
-  if (items > 0 && warp == 8) {
+  if (items > 0 && warp == kAttnCopyWarp) {
     if (lane == 0) {
       mbar_expect_tx(kv_full, 2 * L::kT);
       attn_load_tile<D>(smem, &mk, kv_full, k0, kv_head, batch);
@@ -498,7 +533,7 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
         for (int s = 0; s < L::kStages && s < issued; ++s) mbar_wait_bounded(&full[s], ((issued - 1 - s) / L::kStages) & 1);
       }
     }
-  } else if (items > 0 && warp == 9) {
+  } else if (items > 0 && warp == kAttnMmaWarp) {
     bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(kv_full, 0));
     if (ok && k0 + kAttnTile > kv_len) {
       attn_zero_rows<D>(smem, kv_len - k0);
@@ -531,7 +566,7 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       if (next_stage == 0) next_parity ^= 1u;
       const uint64_t by_tokens = AttnDesc<D>::tokens(ring + stage * L::kStage), next_rows = AttnDesc<D>::rows(ring + next_stage * L::kStage);
       if (!wait(p_full, n & 1)) break;
-      if (issuer) attn_mma_tokens<D, BF16>(t_dv, t_s, 64, by_tokens + (L::kT >> 4), n != 0);
+      if (issuer) attn_mma_tokens<D, BF16>(t_dv, t_s, by_tokens + (L::kT >> 4), n != 0);
       __syncwarp();
       if (more) {
         if (!wait(&full[next_stage], next_parity)) break;
@@ -543,7 +578,7 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       }
       if (!wait(ds_full, n & 1)) break;
       if (issuer) {
-        attn_mma_tokens<D, BF16>(t_dk, t_dp, 64, by_tokens, n != 0);
+        attn_mma_tokens<D, BF16>(t_dk, t_dp, by_tokens, n != 0);
         mma_commit(&free_[stage]);
         if (more) {
           attn_mma_rows<D, BF16>(t_dp, v_desc, next_rows + (L::kT >> 4));
@@ -559,11 +594,12 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       s_abort = 1;
       if (issuer) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
     }
-  } else if (warp < 8) {
-    const int half = warp >> 2;                  // this warp's 64 queries of each tile
+  } else if (warp < 16) {
+    const int part = warp >> 2;                  // this warp's 32 queries of each tile
     const int key = k0 + (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_at = t_s + lanes + half * 64, dp_at = t_dp + lanes + half * 64;
+    const uint32_t s_at = t_s + lanes + part * 32, dp_at = t_dp + lanes + part * 32;
+    const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       ok = !s_abort && mbar_wait_bounded(bar, parity);
@@ -571,85 +607,84 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       tc_fence_after();
       return ok;
     };
+    int stage = 0, in_head = 0;
+    uint32_t stage_parity = 0;
     for (int n = 0; n < items; ++n) {
-      const int stage = n % L::kStages, q0 = (first + n % per_head) * kAttnTile + half * 64;
-      const float4* lse2 = reinterpret_cast<const float4*>(smem + L::kStats + stage * 1024) + half * 16;
-      const float4* delta = reinterpret_cast<const float4*>(smem + L::kStats + stage * 1024 + 512) + half * 16;
+      const int q0 = (first + in_head) * kAttnTile + part * 32;
+      if (++in_head == per_head) in_head = 0;
+      const float4* lse2 = reinterpret_cast<const float4*>(smem + L::kStats + stage * 1024) + part * 8;
+      const float4* delta = reinterpret_cast<const float4*>(smem + L::kStats + stage * 1024 + 512) + part * 8;
       // key j is seen by query i when j < kv_len and j - off <= i
       const int from = key >= kv_len ? 0x7fffffff : p.causal ? key - off - q0 : 0;       // first column of this row that is not masked
       const int warp_from = k0 + (warp & 3) * 32 + 31 >= kv_len ? 0x7fffffff : p.causal ? key - lane + 31 - off - q0 : 0;
-      if (!wait(&full[stage], (n / L::kStages) & 1)) break;          // the statistics are this thread's to read
+      if (!wait(&full[stage], stage_parity)) break;                  // the statistics are this thread's to read
+      if (++stage == L::kStages) { stage = 0; stage_parity ^= 1u; }
       if (!wait(s_full, n & 1)) break;
-      float pr[64];
+      float pr[32];
       {
-        uint32_t s[2][32];
-        tmem_ld32(s_at, s[0]);
-        tmem_ld32(s_at + 32, s[1]);
+        uint32_t s[32];
+        tmem_ld32(s_at, s);
         tmem_wait_ld();
 #pragma unroll
-        for (int g = 0; g < 16; ++g) {
+        for (int g = 0; g < 8; ++g) {
           const float4 l = lse2[g];
-          const float lv[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) pr[4 * g + e] = exp2_fast(fmaf(__uint_as_float(s[g / 8][(4 * g + e) & 31]), p.scale_log2, -lv[e]));
+          const float2 a = fma2(make_float2(__uint_as_float(s[4 * g]), __uint_as_float(s[4 * g + 1])), scale2, make_float2(-l.x, -l.y));
+          const float2 b = fma2(make_float2(__uint_as_float(s[4 * g + 2]), __uint_as_float(s[4 * g + 3])), scale2, make_float2(-l.z, -l.w));
+          pr[4 * g] = exp2_fast(a.x);
+          pr[4 * g + 1] = exp2_fast(a.y);
+          pr[4 * g + 2] = exp2_fast(b.x);
+          pr[4 * g + 3] = exp2_fast(b.y);
         }
       }
       if (warp_from > 0) {
 #pragma unroll
-        for (int e = 0; e < 64; ++e) pr[e] = e >= from ? pr[e] : 0.f;
+        for (int e = 0; e < 32; ++e) pr[e] = e >= from ? pr[e] : 0.f;
       }
-      {
-        uint32_t w[32];
+      uint32_t w[16];
 #pragma unroll
-        for (int e = 0; e < 32; ++e) w[e] = pack16<BF16>(pr[2 * e], pr[2 * e + 1]);
-        tmem_st32(s_at, w);
-        tmem_wait_st();
-      }
+      for (int e = 0; e < 16; ++e) w[e] = pack16<BF16>(pr[2 * e], pr[2 * e + 1]);
+      tmem_st16(s_at, w);
+      tmem_wait_st();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_one(p_full);
       if (!wait(dp_full, n & 1)) break;
       {
-        uint32_t d[2][32];
-        tmem_ld32(dp_at, d[0]);
-        tmem_ld32(dp_at + 32, d[1]);
+        uint32_t d[32];
+        tmem_ld32(dp_at, d);
         tmem_wait_ld();
-        uint32_t w[32];
 #pragma unroll
-        for (int g = 0; g < 16; ++g) {
+        for (int g = 0; g < 8; ++g) {
           const float4 l = delta[g];
-          const float lv[4] = {l.x, l.y, l.z, l.w};
-          float ds[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) ds[e] = pr[4 * g + e] * (__uint_as_float(d[g / 8][(4 * g + e) & 31]) - lv[e]);
-          w[2 * g] = pack16<BF16>(ds[0], ds[1]);
-          w[2 * g + 1] = pack16<BF16>(ds[2], ds[3]);
+          float2 a = add2(make_float2(__uint_as_float(d[4 * g]), __uint_as_float(d[4 * g + 1])), make_float2(-l.x, -l.y));
+          float2 b = add2(make_float2(__uint_as_float(d[4 * g + 2]), __uint_as_float(d[4 * g + 3])), make_float2(-l.z, -l.w));
+          a = mul2(a, make_float2(pr[4 * g], pr[4 * g + 1]));
+          b = mul2(b, make_float2(pr[4 * g + 2], pr[4 * g + 3]));
+          w[2 * g] = pack16<BF16>(a.x, a.y);
+          w[2 * g + 1] = pack16<BF16>(b.x, b.y);
         }
-        tmem_st32(dp_at, w);
-        tmem_wait_st();
       }
+      tmem_st16(dp_at, w);
+      tmem_wait_st();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_one(ds_full);
     }
     const bool live = key < p.Sk;
+    const AttnOut& mine = part < 2 ? p.dv : p.dk;
     if (items > 0) {
       if (ok) wait(done, 0);
-      if (ok) {
-        if (half == 0) attn_store_row<D, BF16>(p, p.dv, t_dv + lanes, batch, kv_head, key, live, 1.f);
-        else attn_store_row<D, BF16>(p, p.dk, t_dk + lanes, batch, kv_head, key, live, p.scale);
-      } else {
-        s_abort = 1;
-      }
-    } else if (live) {
-      attn_zero_row(p, half == 0 ? p.dv : p.dk, batch, kv_head, key);
+      if (ok) attn_store_row<D / 64, BF16>(p, mine, (part < 2 ? t_dv : t_dk) + lanes, (part & 1) * (D / 2), batch, kv_head, key, live, part < 2 ? 1.f : p.scale);
+      else s_abort = 1;
+    } else if (live && (part & 1) == 0) {
+      attn_zero_row(p, mine, batch, kv_head, key);
     }
   }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (s_abort && threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
-  if (warp == 9) {
+  if (warp == kAttnMmaWarp) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
@@ -697,16 +732,16 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
     mbar_init(&s_full[0], 1);
     mbar_init(&s_full[1], 1);
     mbar_init(dp_full, 1);
-    mbar_init(dp_read, 8);
-    mbar_init(&ds_full[0], 8);
-    mbar_init(&ds_full[1], 8);
+    mbar_init(dp_read, 16);
+    mbar_init(&ds_full[0], 16);
+    mbar_init(&ds_full[1], 16);
     mbar_init(done, 1);
     mbar_init(drain, 1);
     s_abort = 0;
     mbar_init_fence();
     fence_proxy_async_smem();
   }
-  if (warp == 9) tmem_alloc(&s_tmem, 512);
+  if (warp == kAttnMmaWarp) tmem_alloc(&s_tmem, 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -719,7 +754,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
   const int tiles = (seen + kAttnTile - 1) / kAttnTile;
   pdl_wait();
 
-  if (tiles > 0 && warp == 8) {
+  if (tiles > 0 && warp == kAttnCopyWarp) {
     if (lane == 0) {
       mbar_expect_tx(q_full, 2 * L::kT);
       attn_load_tile<D>(smem, &mq, q_full, q0, head, batch);
@@ -744,7 +779,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
         for (int s = 0; s < L::kVs && s < nv; ++s) mbar_wait_bounded(&v_full[s], ((nv - 1 - s) / L::kVs) & 1);
       }
     }
-  } else if (tiles > 0 && warp == 9) {
+  } else if (tiles > 0 && warp == kAttnMmaWarp) {
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       ok = ok && !s_abort && mbar_wait_bounded(bar, parity);
@@ -793,7 +828,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       if (!wait(&ds_full[j & 1], (j >> 1) & 1)) break;
       const uint64_t k_desc = AttnDesc<D>::tokens(smem_addr(smem) + L::kK + (j % L::kKs) * L::kT);
       if (issuer) {
-        attn_mma_tokens<D, BF16>(t_dq, tmem + (j & 1) * 128, 64, k_desc, j != 0);
+        attn_mma_tokens<D, BF16>(t_dq, tmem + (j & 1) * 128, k_desc, j != 0);
         mma_commit(&k_free[j % L::kKs]);
         if (j == tiles - 1) mma_commit(done);
       }
@@ -803,12 +838,13 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       s_abort = 1;
       if (issuer) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
     }
-  } else if (warp < 8) {
-    const int half = warp >> 2;                  // this warp's 64 keys of each tile
+  } else if (warp < 16) {
+    const int part = warp >> 2;                  // this warp's 32 keys of each tile
     const int row = q0 + (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const long long stat = (static_cast<long long>(batch) * p.Hq + head) * p.sq_pad + row;      // rows are padded: always there
     const float lse2 = p.lse2[stat], delta = p.delta[stat];
+    const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), lse22 = make_float2(-lse2, -lse2), delta2 = make_float2(-delta, -delta);
     const int limit = p.causal ? min(kv_len, row + off + 1) : kv_len;
     const int warp_limit = p.causal ? min(kv_len, row - lane + off + 1) : kv_len;
     bool ok = true;
@@ -819,37 +855,41 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       return ok;
     };
     for (int j = 0; j < tiles; ++j) {
-      const uint32_t s_at = tmem + (j & 1) * 128 + lanes + half * 64, dp_at = t_dp + lanes + half * 64;
-      const int k0 = j * kAttnTile + half * 64;
+      const uint32_t s_at = tmem + (j & 1) * 128 + lanes + part * 32, dp_at = t_dp + lanes + part * 32;
+      const int k0 = j * kAttnTile + part * 32;
       if (!wait(&s_full[j & 1], (j >> 1) & 1)) break;
-      float pr[64];
+      float pr[32];
       {
-        uint32_t s[2][32];
-        tmem_ld32(s_at, s[0]);
-        tmem_ld32(s_at + 32, s[1]);
+        uint32_t s[32];
+        tmem_ld32(s_at, s);
         tmem_wait_ld();
 #pragma unroll
-        for (int e = 0; e < 64; ++e) pr[e] = exp2_fast(fmaf(__uint_as_float(s[e / 32][e & 31]), p.scale_log2, -lse2));
+        for (int e = 0; e < 32; e += 2) {
+          const float2 a = fma2(make_float2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale2, lse22);
+          pr[e] = exp2_fast(a.x);
+          pr[e + 1] = exp2_fast(a.y);
+        }
       }
-      if (k0 + 64 > warp_limit) {
+      if (k0 + 32 > warp_limit) {
 #pragma unroll
-        for (int e = 0; e < 64; ++e) pr[e] = k0 + e < limit ? pr[e] : 0.f;
+        for (int e = 0; e < 32; ++e) pr[e] = k0 + e < limit ? pr[e] : 0.f;
       }
       if (!wait(dp_full, j & 1)) break;
-      uint32_t w[32];
+      uint32_t w[16];
       {
-        uint32_t d[2][32];
-        tmem_ld32(dp_at, d[0]);
-        tmem_ld32(dp_at + 32, d[1]);
+        uint32_t d[32];
+        tmem_ld32(dp_at, d);
         tmem_wait_ld();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_one(dp_read);
 #pragma unroll
-        for (int e = 0; e < 32; ++e)
-          w[e] = pack16<BF16>(pr[2 * e] * (__uint_as_float(d[e / 16][(2 * e) & 31]) - delta), pr[2 * e + 1] * (__uint_as_float(d[e / 16][(2 * e + 1) & 31]) - delta));
+        for (int e = 0; e < 16; ++e) {
+          const float2 a = mul2(add2(make_float2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1])), delta2), make_float2(pr[2 * e], pr[2 * e + 1]));
+          w[e] = pack16<BF16>(a.x, a.y);
+        }
       }
-      tmem_st32(s_at, w);
+      tmem_st16(s_at, w);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
@@ -858,9 +898,9 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
     const bool live = row < p.Sq;
     if (tiles > 0) {
       if (ok) wait(done, 0);
-      if (ok && half == 0) attn_store_row<D, BF16>(p, p.out, t_dq + lanes, batch, head, row, live, p.scale);
+      if (ok && part < 2) attn_store_row<D / 64, BF16>(p, p.out, t_dq + lanes, part * (D / 2), batch, head, row, live, p.scale);
       if (!ok) s_abort = 1;
-    } else if (live && half == 0) {
+    } else if (live && part == 0) {
       attn_zero_row(p, p.out, batch, head, row);
     }
   }
@@ -868,7 +908,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
   tc_fence_before();
   __syncthreads();
   if (s_abort && threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
-  if (warp == 9) {
+  if (warp == kAttnMmaWarp) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
