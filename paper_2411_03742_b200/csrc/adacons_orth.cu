@@ -21,7 +21,7 @@ struct adacons_orth {
   double eps = 0;
   unsigned char* memory = nullptr;    // one allocation: descriptors, lists, partial sums, iterates
   size_t bytes = 0;
-  const OrthTile* load_tiles = nullptr;
+  const OrthSpot* load_tiles = nullptr;
   const OrthChunk* chunks = nullptr;
   double* partial = nullptr;
   OrthParams params = {};             // all but the result's address
@@ -50,7 +50,6 @@ struct OrthPlan {
   int cg = 1, workers = 1;
   std::vector<OrthTile> tiles[3];
   std::vector<int> begin[3];
-  std::vector<int> parts[3];          // [matrix]
   double cycles = 0;                  // modelled time of a step
 };
 
@@ -78,34 +77,39 @@ OrthPlan plan_step(const std::vector<OrthMat>& mats, bool split, int cg, int wor
   plan.cg = cg;
   plan.workers = static_cast<int>(std::min<int64_t>(workers, most));
   std::vector<double> chain(num, 0.0);
+  std::vector<unsigned> stored(num, 0u), stored_after(num, 0u);
   std::vector<std::pair<double, int>> heap;          // (-load, -worker): the least loaded, then the first, on top
   for (int w = 0; w < plan.workers; ++w) heap.emplace_back(0.0, -w);
   std::make_heap(heap.begin(), heap.end());
   for (int kind = 0; kind < 3; ++kind) {
     std::vector<std::vector<OrthTile>> mine(plan.workers);
-    plan.parts[kind].assign(num, 0);
     for (int k : order) {
       const int cols = kind == kOrthApply ? mats[k].l : mats[k].r;
       const double cost = std::max(stage * ((depth(kind, k) + kOrthTK - 1) / kOrthTK), 16.0 * tn) + 1500.0;
       int64_t count = 0;
+      unsigned blocks = 0;                           // that store a tile of this product
       for (int64_t j = 0; j * tn < cols; ++j)
         for (int64_t i = 0; i * tm < mats[k].r; ++i) {
           if (kind != kOrthApply && i * tm + tm - 1 < j * tn) continue;
           std::pop_heap(heap.begin(), heap.end());
-          mine[-heap.back().second].push_back({k, static_cast<int>(i), static_cast<int>(j), depth(kind, k)});
+          mine[-heap.back().second].push_back({k, static_cast<int>(i), static_cast<int>(j), depth(kind, k), mats[k].r, cols, 0u, stored[k]});
           heap.back().first -= cost;
           std::push_heap(heap.begin(), heap.end());
-          for (int rank = 0; rank < cg; ++rank) plan.parts[kind][k] += i * tm + rank * 128 < mats[k].r;
+          for (int rank = 0; rank < cg; ++rank) blocks += i * tm + rank * 128 < mats[k].r;
           ++count;
         }
       chain[k] += cost * ((count + plan.workers - 1) / plan.workers) + 6000.0;
+      stored_after[k] = stored[k] + blocks;
     }
+    stored = stored_after;
     plan.begin[kind].push_back(0);
     for (const auto& list : mine) {
       plan.tiles[kind].insert(plan.tiles[kind].end(), list.begin(), list.end());
       plan.begin[kind].push_back(static_cast<int>(plan.tiles[kind].size()));
     }
   }
+  for (auto& list : plan.tiles)
+    for (OrthTile& t : list) t.per_step = stored[t.mat];
   for (const auto& h : heap) plan.cycles = std::max(plan.cycles, -h.first);
   for (double c : chain) plan.cycles = std::max(plan.cycles, c);
   return plan;
@@ -176,7 +180,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
 
   std::vector<OrthMat> mats(num);
   std::vector<OrthChunk> chunks;
-  std::vector<OrthTile> load;
+  std::vector<OrthSpot> load;
   for (int k = 0; k < num; ++k) {
     OrthMat& m = mats[k];
     std::memset(&m, 0, sizeof(m));
@@ -187,12 +191,13 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
     m.lds = (m.r + 7) / 8 * 8;
     m.offset = offsets[k];
     m.vec_out = m.l % 8 == 0 && offsets[k] % 8 == 0;
+    m.vec_in = offsets[k] % 8 == 0 && rows[k] * cols[k] % 8 == 0;
     m.scale = scaling ? static_cast<float>(std::sqrt(std::max(1.0, static_cast<double>(rows[k]) / static_cast<double>(cols[k])))) : 1.f;
     m.norm_first = static_cast<int>(chunks.size());
     m.norm_count = static_cast<int>((rows[k] * cols[k] + kOrthNormChunk - 1) / kOrthNormChunk);
     for (int q = 0; q < m.norm_count; ++q) chunks.push_back({k, q});
     for (int i = 0; i < (m.r + kOrthLoadTile - 1) / kOrthLoadTile; ++i)
-      for (int j = 0; j < (m.l + kOrthLoadTile - 1) / kOrthLoadTile; ++j) load.push_back({k, i, j, 0});
+      for (int j = 0; j < (m.l + kOrthLoadCols - 1) / kOrthLoadCols; ++j) load.push_back({k, i, j});
   }
   OrthPlan plan = plan_step(mats, split, 1, singles);
   {
@@ -201,8 +206,6 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   }
   c->cg = plan.cg;
   c->blocks = plan.workers * plan.cg;
-  for (int k = 0; k < num; ++k)
-    for (int kind = 0; kind < 3; ++kind) mats[k].parts[kind] = plan.parts[kind][k];
   std::vector<OrthStep> step_coeffs(steps);
   for (int s = 0; s < steps; ++s) {
     const double* q = coeffs + 3 * s;
@@ -219,7 +222,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
     at_begin[kind] = a.take(plan.begin[kind].size() * sizeof(int));
   }
   const size_t at_coeffs = a.take(step_coeffs.size() * sizeof(OrthStep)), at_done = a.take(num * sizeof(unsigned));
-  const size_t at_load = a.take(load.size() * sizeof(OrthTile)), at_chunks = a.take(chunks.size() * sizeof(OrthChunk));
+  const size_t at_load = a.take(load.size() * sizeof(OrthSpot)), at_chunks = a.take(chunks.size() * sizeof(OrthChunk));
   const size_t at_partial = a.take(chunks.size() * sizeof(double)), at_flags = a.take(sizeof(uint32_t));
   const size_t head = a.used;
   std::vector<size_t> at(static_cast<size_t>(num) * kMapCount, 0);
@@ -260,7 +263,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
     p.begin[kind] = reinterpret_cast<const int*>(c->memory + at_begin[kind]);
   }
   std::memcpy(host.data() + at_coeffs, step_coeffs.data(), step_coeffs.size() * sizeof(OrthStep));
-  std::memcpy(host.data() + at_load, load.data(), load.size() * sizeof(OrthTile));
+  std::memcpy(host.data() + at_load, load.data(), load.size() * sizeof(OrthSpot));
   std::memcpy(host.data() + at_chunks, chunks.data(), chunks.size() * sizeof(OrthChunk));
   // the padding of the iterates is read by the epilogues (never by a product): zero it once
   if (cudaMemset(c->memory + head, 0, c->bytes - head) != cudaSuccess ||
@@ -275,7 +278,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   p.done = reinterpret_cast<unsigned*>(c->memory + at_done);
   p.flags = reinterpret_cast<uint32_t*>(c->memory + at_flags);
   p.steps = steps;
-  c->load_tiles = reinterpret_cast<const OrthTile*>(c->memory + at_load);
+  c->load_tiles = reinterpret_cast<const OrthSpot*>(c->memory + at_load);
   c->chunks = reinterpret_cast<const OrthChunk*>(c->memory + at_chunks);
   c->partial = reinterpret_cast<double*>(c->memory + at_partial);
   *out = holder.release();
@@ -310,14 +313,15 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
   p.out = out;
   p.out_aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0;
   const double* partial = c->partial;
+  const int aligned = reinterpret_cast<uintptr_t>(update) % 16 == 0;
   bool ok;
   if (c->dtype == ADACONS_F32) {
-    ok = launch(&orth_norm_kernel<0>, dim3(c->num_chunks), dim3(256), 0, st, kLaunchPlain, 1, update, p.mats, c->chunks, c->partial) &&
-         launch(&orth_load_kernel<0>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, p.mats, c->load_tiles, partial, c->eps, p.done) &&
+    ok = launch(&orth_norm_kernel<0>, dim3(c->num_chunks), dim3(256), 0, st, kLaunchPlain, 1, update, aligned, p.mats, c->chunks, c->partial) &&
+         launch(&orth_load_kernel<0>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, aligned, p.mats, c->load_tiles, partial, c->eps, p.done) &&
          (c->cg == 2 ? launch_steps<true, 2>(c, p, st) : launch_steps<true, 1>(c, p, st));
   } else {
-    ok = launch(&orth_norm_kernel<1>, dim3(c->num_chunks), dim3(256), 0, st, kLaunchPlain, 1, update, p.mats, c->chunks, c->partial) &&
-         launch(&orth_load_kernel<1>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, p.mats, c->load_tiles, partial, c->eps, p.done) &&
+    ok = launch(&orth_norm_kernel<1>, dim3(c->num_chunks), dim3(256), 0, st, kLaunchPlain, 1, update, aligned, p.mats, c->chunks, c->partial) &&
+         launch(&orth_load_kernel<1>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, aligned, p.mats, c->load_tiles, partial, c->eps, p.done) &&
          (c->cg == 2 ? launch_steps<false, 2>(c, p, st) : launch_steps<false, 1>(c, p, st));
   }
   c->launches = 3;

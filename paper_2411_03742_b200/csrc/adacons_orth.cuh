@@ -37,7 +37,7 @@ constexpr int kOrthChunk = 2;            // fp32 contexts: stages (128 K element
 constexpr float kOrthXScale = 2048.f, kOrthSScale = 8192.f, kOrthBScale = 2048.f;
 constexpr int kOrthThreads = 352;        // warps 0-7 epilogue, 8 operand copies, 9 products, 10 epilogue copies
 constexpr int kOrthNormChunk = 16384;    // elements per block of the norm kernel
-constexpr int kOrthLoadTile = 64;
+constexpr int kOrthLoadTile = 64, kOrthLoadCols = 256;
 
 enum OrthKind { kOrthGram = 0, kOrthPoly = 1, kOrthApply = 2 };
 enum OrthMap { kMapX0 = 0, kMapX1 = 2, kMapS = 4, kMapB = 6, kMapCount = 8 };   // + 1: the lo part
@@ -47,15 +47,22 @@ struct OrthMat {
   int transposed;          // the matrix in the vector has l rows of r elements
   int ldx, lds;            // row pitch of X and of S, B (elements)
   int vec_out;             // rows of the result are whole groups of 8 elements, aligned relative to the vector's start
+  int vec_in;              // the matrix starts on, and is a multiple of, 8 elements
   int norm_first, norm_count;
-  int parts[3];            // tiles that the blocks store, by kind
   float scale;
   long long offset;        // of the matrix in the vector
   __half* x[2][2];         // [buffer][hi, lo]
   __half* s[2];
   __half* b[2];
 };
-struct OrthTile { int mat, i, j, depth; };     // depth: K elements of the product
+struct OrthSpot { int mat, i, j; };           // load kernel: a tile of a matrix
+// One tile of one product, with all that the copying and issuing warps need to know of its matrix.
+struct __align__(16) OrthTile {
+  int mat, i, j, depth;    // depth: K elements of the product
+  int rows, cols;          // of the product: r x l or r x r
+  unsigned per_step;       // tiles that the blocks store for this matrix in a step
+  unsigned before;         // of them, those that come before this product
+};
 struct OrthStep { float a, b, c, t; };         // t: what is added to B's diagonal
 struct OrthChunk { int mat; int first; };      // norm kernel: chunk number within the matrix
 
@@ -81,19 +88,48 @@ __device__ __forceinline__ float orth_in(const void* p, long long i) {
   return DT == 0 ? static_cast<const float*>(p)[i] : __uint_as_float(static_cast<uint32_t>(static_cast<const unsigned short*>(p)[i]) << 16);
 }
 
+// eight consecutive elements from a 16-byte boundary (fp32: 32 bytes of it)
 template <int DT>
-__global__ void __launch_bounds__(256) orth_norm_kernel(const void* in, const OrthMat* mats, const OrthChunk* chunks, double* partial) {
+__device__ __forceinline__ void orth_in8(const void* p, long long i, float (&v)[8]) {
+  if (DT == 0) {
+    const uint4 a = ld_stream_v4(static_cast<const float*>(p) + i), b = ld_stream_v4(static_cast<const float*>(p) + i + 4);
+    v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
+    v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
+  } else {
+    const uint4 a = ld_stream_v4(static_cast<const unsigned short*>(p) + i);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 f = unpack_pair<1>(a, k);
+      v[2 * k] = f.x;
+      v[2 * k + 1] = f.y;
+    }
+  }
+}
+
+template <int DT>
+__global__ void __launch_bounds__(256) orth_norm_kernel(const void* in, int aligned, const OrthMat* mats, const OrthChunk* chunks, double* partial) {
   __shared__ double s_sum[8];
   const OrthChunk ch = chunks[blockIdx.x];
-  const long long size = static_cast<long long>(mats[ch.mat].r) * mats[ch.mat].l;
+  const OrthMat& m = mats[ch.mat];
+  const long long size = static_cast<long long>(m.r) * m.l;
   const long long begin = static_cast<long long>(ch.first) * kOrthNormChunk;
   const long long end = begin + kOrthNormChunk < size ? begin + kOrthNormChunk : size;
-  const long long base = mats[ch.mat].offset;
+  const long long base = m.offset;
   double sum = 0.0;
+  if (aligned && m.vec_in) {                       // the matrix is whole groups of eight
+#pragma unroll 4
+    for (long long i = begin + 8 * threadIdx.x; i < end; i += 8 * 256) {
+      float v[8];
+      orth_in8<DT>(in, base + i, v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fma(static_cast<double>(v[e]), static_cast<double>(v[e]), sum);
+    }
+  } else {
 #pragma unroll 8
-  for (long long i = begin + threadIdx.x; i < end; i += 256) {
-    const double v = orth_in<DT>(in, base + i);
-    sum = fma(v, v, sum);
+    for (long long i = begin + threadIdx.x; i < end; i += 256) {
+      const double v = orth_in<DT>(in, base + i);
+      sum = fma(v, v, sum);
+    }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -111,14 +147,15 @@ __device__ __forceinline__ void orth_split(float v, __half& hi, __half& lo) {
   lo = __float2half_rn(v - __half2float(hi));
 }
 
-// X_0 = G / (|G|_F + eps) as pairs, transposed where the matrix is taller than wide.
+// X_0 = G / (|G|_F + eps) as pairs, transposed where the matrix is taller than wide.  A block makes 64 rows x
+// 256 columns of X, 64 x 64 at a time.
 template <int DT>
-__global__ void __launch_bounds__(256) orth_load_kernel(const void* in, const OrthMat* mats, const OrthTile* tiles, const double* partial, double eps, unsigned* done) {
+__global__ void __launch_bounds__(256) orth_load_kernel(const void* in, int aligned, const OrthMat* mats, const OrthSpot* tiles, const double* partial, double eps, unsigned* done) {
   __shared__ float s_tile[kOrthLoadTile][kOrthLoadTile + 1];
   __shared__ double s_sum[8];
   pdl_launch_dependents();
   pdl_wait();
-  const OrthTile t = tiles[blockIdx.x];
+  const OrthSpot t = tiles[blockIdx.x];
   const OrthMat& m = mats[t.mat];
   const int tid = threadIdx.x;
   if (tid == 0 && t.i == 0 && t.j == 0) done[t.mat] = 0u;
@@ -131,29 +168,65 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, const Or
   sum = 0.0;
   for (int w = 0; w < 8; ++w) sum += s_sum[w];
   const float mul = static_cast<float>(static_cast<double>(kOrthXScale) / (sqrt(sum) + eps));
-  // one tile of the matrix as it lies in the vector: `rows` x `cols`, row-major
-  const int rows = m.transposed ? m.l : m.r, cols = m.transposed ? m.r : m.l;
-  const int r0 = (m.transposed ? t.j : t.i) * kOrthLoadTile, c0 = (m.transposed ? t.i : t.j) * kOrthLoadTile;
-  const int tx = tid & 63, ty = tid >> 6;
+  const int rows = m.transposed ? m.l : m.r, cols = m.transposed ? m.r : m.l;      // as it lies in the vector, row-major
+  const bool vec = aligned && m.vec_in && cols % 8 == 0;
+  const int r = m.r, ldx = m.ldx, transposed = m.transposed;
+  const long long offset = m.offset;
+  __half *hi = m.x[0][0], *lo = m.x[0][1];
+  const int row_base = t.i * kOrthLoadTile;
+  if (vec && !transposed) {                        // straight through: 8 columns a thread, 8 threads a row of 64, 32 rows at a time
 #pragma unroll 4
-  for (int y = ty; y < kOrthLoadTile; y += 4) {
-    const int row = r0 + y, col = c0 + tx;
-    s_tile[y][tx] = row < rows && col < cols ? orth_in<DT>(in, m.offset + static_cast<long long>(row) * cols + col) * mul : 0.f;
+    for (int n = 0; n < 8; ++n) {
+      const int row = row_base + (n & 1) * 32 + (tid >> 3), col = t.j * kOrthLoadCols + (n >> 1) * kOrthLoadTile + (tid & 7) * 8;
+      if (row >= r || col >= cols) continue;
+      float v[8];
+      orth_in8<DT>(in, offset + static_cast<long long>(row) * cols + col, v);
+      __half h[8], l[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) orth_split(v[e] * mul, h[e], l[e]);
+      const long long at = static_cast<long long>(row) * ldx + col;
+      *reinterpret_cast<uint4*>(hi + at) = *reinterpret_cast<const uint4*>(h);
+      *reinterpret_cast<uint4*>(lo + at) = *reinterpret_cast<const uint4*>(l);
+    }
+    return;
   }
-  __syncthreads();
-  const int pair = tid & 31;
+  for (int n = 0; n < kOrthLoadCols / kOrthLoadTile; ++n) {
+    const int col_base = t.j * kOrthLoadCols + n * kOrthLoadTile;
+    if (col_base >= ldx) return;
+    const int r0 = transposed ? col_base : row_base, c0 = transposed ? row_base : col_base;
+    if (vec) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int y = q * 32 + (tid >> 3), x = (tid & 7) * 8;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (r0 + y < rows && c0 + x < cols) orth_in8<DT>(in, offset + static_cast<long long>(r0 + y) * cols + c0 + x, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s_tile[y][x + e] = v[e] * mul;
+      }
+    } else {
+      const int tx = tid & 63, ty = tid >> 6;
+#pragma unroll 8
+      for (int y = ty; y < kOrthLoadTile; y += 4) {
+        const int row = r0 + y, col = c0 + tx;
+        s_tile[y][tx] = row < rows && col < cols ? orth_in<DT>(in, offset + static_cast<long long>(row) * cols + col) * mul : 0.f;
+      }
+    }
+    __syncthreads();
+    const int pair = tid & 31;
 #pragma unroll 4
-  for (int y = tid >> 5; y < kOrthLoadTile; y += 8) {
-    const int row = t.i * kOrthLoadTile + y, col = t.j * kOrthLoadTile + 2 * pair;
-    if (row >= m.r || col >= m.ldx) continue;           // the pitch is even: a pair never straddles it
-    const float v0 = m.transposed ? s_tile[2 * pair][y] : s_tile[y][2 * pair];
-    const float v1 = m.transposed ? s_tile[2 * pair + 1][y] : s_tile[y][2 * pair + 1];
-    __half h0, l0, h1, l1;
-    orth_split(v0, h0, l0);
-    orth_split(v1, h1, l1);
-    const long long at = static_cast<long long>(row) * m.ldx + col;
-    *reinterpret_cast<__half2*>(m.x[0][0] + at) = __halves2half2(h0, h1);
-    *reinterpret_cast<__half2*>(m.x[0][1] + at) = __halves2half2(l0, l1);
+    for (int y = tid >> 5; y < kOrthLoadTile; y += 8) {
+      const int row = row_base + y, col = col_base + 2 * pair;
+      if (row >= r || col >= ldx) continue;             // the pitch is even: a pair never straddles it
+      const float v0 = transposed ? s_tile[2 * pair][y] : s_tile[y][2 * pair];
+      const float v1 = transposed ? s_tile[2 * pair + 1][y] : s_tile[y][2 * pair + 1];
+      __half h0, l0, h1, l1;
+      orth_split(v0, h0, l0);
+      orth_split(v1, h1, l1);
+      const long long at = static_cast<long long>(row) * ldx + col;
+      *reinterpret_cast<__half2*>(hi + at) = __halves2half2(h0, h1);
+      *reinterpret_cast<__half2*>(lo + at) = __halves2half2(l0, l1);
+    }
+    __syncthreads();
   }
 }
 
@@ -204,10 +277,10 @@ template <bool SPLIT, int CG> struct OrthTiling {
 
 // What of a tile exists: strips with columns inside the matrix, none for a block without rows.
 template <bool SPLIT, int CG>
-__device__ __forceinline__ int orth_live_strips(int kind, const OrthMat& m, const OrthTile& t, int rank) {
+__device__ __forceinline__ int orth_live_strips(const OrthTile& t, int rank) {
   using T = OrthTiling<SPLIT, CG>;
-  if (t.i * T::kTM + rank * 128 >= m.r) return 0;
-  const int left = ((kind == kOrthApply ? m.l : m.r) - t.j * T::kTN + 63) / 64;
+  if (t.i * T::kTM + rank * 128 >= t.rows) return 0;
+  const int left = (t.cols - t.j * T::kTN + 63) / 64;
   return left < T::kBlocks ? left : T::kBlocks;
 }
 
@@ -225,10 +298,12 @@ __device__ __forceinline__ uint32_t orth_pack2(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// One 32 x 32 block of the product: row0 + lane is this thread's row, acc its 32 columns from col0 on.
-// hi / lo: the block's place in the strip, `half` selecting its 64 bytes of each 128-byte row.
+// One 32 x 32 block of the product: row0 + lane is this thread's row; its 32 columns from col0 on are read from
+// tensor memory at `acc`.  hi / lo: the block's place in the strip, `half` selecting its 64 bytes of each 128-byte row.
+// A loop of 16 columns and not unrolled code for 32: every product of a small matrix runs this once, and
+// fetching the longer code took 3000 to 6000 cycles of it.  (With 8 columns a turn large matrices lose a tenth to the waits.)
 template <int KIND, bool SPLIT, int CG>
-__device__ __forceinline__ void orth_finish_block(const OrthParams& p, const OrthStep& step, bool last_step, const OrthMat& m, int row0, int col0, const uint32_t (&acc)[32],
+__device__ __forceinline__ void orth_finish_block(const OrthParams& p, const OrthStep& step, bool last_step, const OrthMat& m, int row0, int col0, uint32_t acc,
                                                   unsigned char* hi, unsigned char* lo, int half) {
   using T = OrthTiling<SPLIT, CG>;
   const int lane = threadIdx.x & 31;
@@ -238,36 +313,42 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
   // where no tile above the diagonal is computed, its image comes from here
   const bool mirror = KIND != kOrthApply && !((col0 / T::kTM) * T::kTM + T::kTM - 1 >= (row0 / T::kTN) * T::kTN);
   const bool turned = last && m.transposed;
-  __half* dst_hi = KIND == kOrthGram ? m.s[0] : m.b[0];
-  __half* dst_lo = KIND == kOrthGram ? m.s[1] : m.b[1];
+  unsigned short* dst_hi = reinterpret_cast<unsigned short*>(KIND == kOrthGram ? m.s[0] : m.b[0]);
+  unsigned short* dst_lo = reinterpret_cast<unsigned short*>(KIND == kOrthGram ? m.s[1] : m.b[1]);
   unsigned char* hrow = hi + lane * 128;
   unsigned char* lrow = lo + lane * 128;
+  const float by_x = KIND == kOrthPoly ? step.b * (kOrthBScale / kOrthSScale) : step.a - step.t;
+  const float by_v = KIND == kOrthGram ? kOrthSScale / (kOrthXScale * kOrthXScale) : KIND == kOrthPoly ? step.c * (kOrthBScale / (kOrthSScale * kOrthSScale)) : 1.f / kOrthBScale;
+  const int diagonal = KIND == kOrthPoly ? row - col0 : -1;      // the column, from col0, of this row's diagonal element
+#pragma unroll 1
+  for (int turn = 0; turn < 2; ++turn) {
+   uint32_t a[16];
+   tmem_ld16(acc + turn * 16, a);
+   tmem_wait_ld();
 #pragma unroll
-  for (int g = 0; g < 4; ++g) {
+   for (int sub = 0; sub < 2; ++sub) {
+    const int g = 2 * turn + sub;
     const int at = ((4 * half + g) ^ (lane & 7)) * 16;
     float v[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(acc[8 * g + e]);
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(a[8 * sub + e]);
     if constexpr (KIND == kOrthGram) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= kOrthSScale / (kOrthXScale * kOrthXScale);
+      for (int e = 0; e < 8; ++e) v[e] *= by_v;
     } else {
       float x[8];
       orth_unpack8(*reinterpret_cast<const uint4*>(hrow + at), x);
-      if (kPair) {
+      if constexpr (kPair) {
         float y[8];
         orth_unpack8(*reinterpret_cast<const uint4*>(lrow + at), y);
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] += y[e];
       }
-      const float by_x = KIND == kOrthPoly ? step.b * (kOrthBScale / kOrthSScale) : step.a - step.t;
-      const float by_v = KIND == kOrthPoly ? step.c * (kOrthBScale / (kOrthSScale * kOrthSScale)) : 1.f / kOrthBScale;
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = by_x * x[e] + by_v * v[e];
-      if (KIND == kOrthPoly && row0 == col0) {
+      if (KIND == kOrthPoly) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (8 * g + e == lane) v[e] += step.t * kOrthBScale;
+        for (int e = 0; e < 8; ++e) v[e] += 8 * g + e == diagonal ? step.t * kOrthBScale : 0.f;
       }
     }
     if (!last) {
@@ -282,14 +363,15 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
       }
       *reinterpret_cast<uint4*>(hrow + at) = make_uint4(h[0], h[1], h[2], h[3]);
       if (kPair) *reinterpret_cast<uint4*>(lrow + at) = make_uint4(l[0], l[1], l[2], l[3]);
-      if (mirror) {
+      if (mirror && row < r) {
+        const int col = col0 + 8 * g;
+        unsigned short* to_hi = dst_hi + static_cast<long long>(col) * m.lds + row;
+        unsigned short* to_lo = dst_lo + static_cast<long long>(col) * m.lds + row;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int col = col0 + 8 * g + e;
-          if (row < r && col < ncols) {
-            const long long to = static_cast<long long>(col) * m.lds + row;
-            reinterpret_cast<unsigned short*>(dst_hi)[to] = static_cast<unsigned short>(h[e / 2] >> (16 * (e & 1)));
-            if (kPair) reinterpret_cast<unsigned short*>(dst_lo)[to] = static_cast<unsigned short>(l[e / 2] >> (16 * (e & 1)));
+          if (col + e < ncols) {
+            to_hi[static_cast<long long>(e) * m.lds] = static_cast<unsigned short>(h[e / 2] >> (16 * (e & 1)));
+            if (kPair) to_lo[static_cast<long long>(e) * m.lds] = static_cast<unsigned short>(l[e / 2] >> (16 * (e & 1)));
           }
         }
       }
@@ -298,13 +380,13 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] *= m.scale / kOrthXScale;
     if (turned) {
+      const int col = col0 + 8 * g;
+      const long long to = m.offset + static_cast<long long>(col) * r + row;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int col = col0 + 8 * g + e;
-        if (row < r && col < ncols) {
-          const long long to = m.offset + static_cast<long long>(col) * r + row;
-          if (SPLIT) static_cast<float*>(p.out)[to] = v[e];
-          else static_cast<unsigned short*>(p.out)[to] = static_cast<unsigned short>(pack_bf16x2_rn(v[e], 0.f) & 0xffffu);
+        if (row < r && col + e < ncols) {
+          if (SPLIT) static_cast<float*>(p.out)[to + static_cast<long long>(e) * r] = v[e];
+          else static_cast<unsigned short*>(p.out)[to + static_cast<long long>(e) * r] = static_cast<unsigned short>(pack_bf16x2_rn(v[e], 0.f) & 0xffffu);
         }
       }
     } else if (SPLIT) {                            // the strip's two parts hold the upper and the lower halves of the fp32 words
@@ -321,6 +403,7 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
       *reinterpret_cast<uint4*>(hrow + at) =
           make_uint4(pack_bf16x2_rn(v[0], v[1]), pack_bf16x2_rn(v[2], v[3]), pack_bf16x2_rn(v[4], v[5]), pack_bf16x2_rn(v[6], v[7]));
     }
+   }
   }
   if (last && !turned) {                           // to the vector, along rows
     __syncwarp();
@@ -357,31 +440,43 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
   }
 }
 
-// The products of one block in the order in which all of its warps go through them.
+// The products of one block in the order in which all of its warps go through them.  The next tile's record
+// is on its way while a tile is worked on.
 struct OrthWalk {
   const OrthParams& p;
   const int worker;
-  int step, kind, k, end;
-  OrthTile t;
-  __device__ __forceinline__ OrthWalk(const OrthParams& params, int w) : p(params), worker(w), step(0), kind(-1), k(0), end(0) { next(); }
+  int begin[3], end[3];                          // this worker's tiles by kind
+  int step, kind, k;
+  int next_step, next_kind, next_k;
+  OrthTile t, next_t;
+  __device__ __forceinline__ OrthWalk(const OrthParams& params, int w) : p(params), worker(w) {
+#pragma unroll
+    for (int q = 0; q < 3; ++q) { begin[q] = p.begin[q][worker]; end[q] = p.begin[q][worker + 1]; }
+    next_step = 0;
+    next_kind = 0;
+    next_k = begin[0] - 1;
+    look_ahead();
+    next();
+  }
   __device__ __forceinline__ bool more() const { return step < p.steps; }
-  __device__ __forceinline__ void next() {
-    ++k;
-    while (k >= end) {
-      if (++kind == 3) { kind = 0; ++step; }
-      if (step == p.steps) return;
-      const int* begin = kind == 0 ? p.begin[0] : kind == 1 ? p.begin[1] : p.begin[2];
-      k = begin[worker];
-      end = begin[worker + 1];
+  __device__ __forceinline__ void look_ahead() {
+    ++next_k;
+    while (next_k >= (next_kind == 0 ? end[0] : next_kind == 1 ? end[1] : end[2])) {
+      if (++next_kind == 3) { next_kind = 0; ++next_step; }
+      if (next_step >= p.steps) return;
+      next_k = next_kind == 0 ? begin[0] : next_kind == 1 ? begin[1] : begin[2];
     }
-    t = (kind == 0 ? p.tiles[0] : kind == 1 ? p.tiles[1] : p.tiles[2])[k];
+    next_t = (next_kind == 0 ? p.tiles[0] : next_kind == 1 ? p.tiles[1] : p.tiles[2])[next_k];
+  }
+  __device__ __forceinline__ void next() {
+    step = next_step;
+    kind = next_kind;
+    k = next_k;
+    t = next_t;
+    if (step < p.steps) look_ahead();
   }
   // stored tiles of the matrix that this product needs: all of its earlier products
-  __device__ __forceinline__ unsigned needs() const {
-    const OrthMat& m = p.mats[t.mat];
-    const unsigned g = m.parts[0], q = m.parts[1], a = m.parts[2];
-    return step * (g + q + a) + (kind > 0 ? g : 0u) + (kind > 1 ? q : 0u);
-  }
+  __device__ __forceinline__ unsigned needs() const { return step * t.per_step + t.before; }
 };
 
 __device__ __forceinline__ unsigned orth_load_acquire(const unsigned* p) {
@@ -540,7 +635,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
         __device__ __forceinline__ Strips(const OrthParams& p, int worker, int rank) : w(p, worker) { open(rank); }
         __device__ __forceinline__ void open(int rank) {                   // the next tile that has strips here
           for (; w.more(); w.next()) {
-            live = orth_live_strips<SPLIT, CG>(w.kind, w.p.mats[w.t.mat], w.t, rank);
+            live = orth_live_strips<SPLIT, CG>(w.t, rank);
             strip = 0;
             if (live > 0) return;
           }
@@ -588,7 +683,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
           for (int part = 0; part < parts; ++part)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-              if (row + h * 64 < p.mats[give.w.t.mat].r) tma_store_2d(map + part, at + part * kOrthStripPart + h * 8192, col, row + h * 64);
+              if (row + h * 64 < give.w.t.rows) tma_store_2d(map + part, at + part * kOrthStripPart + h * 8192, col, row + h * 64);
           bulk_commit();
           if (give.strip == give.live - 1) {               // the tile is complete: say so once its bytes are
             bulk_wait<0>();
@@ -622,7 +717,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
       buf ^= 1;
       if (buf == 0) parity ^= 1u;
     };
-    auto finish = [&](const OrthWalk& w, const OrthStep& step, const OrthMat& m, int strip, const uint32_t (&acc)[32]) {
+    auto finish = [&](const OrthWalk& w, const OrthStep& step, const OrthMat& m, int strip, uint32_t acc) {
       if (!wait_for(&strip_full[place], strip_parity)) return false;
       unsigned char* at = smem + T::kStrips + place * 2 * kOrthStripPart + (warp & 3) * 32 * 128;
       const int row0 = w.t.i * T::kTM + rank * 128 + (warp & 3) * 32, col0 = w.t.j * T::kTN + strip * 64 + half * 32;
@@ -640,20 +735,14 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
     for (OrthWalk w(p, worker); ok && w.more(); w.next()) {
       const OrthMat& m = p.mats[w.t.mat];
       const OrthStep step = p.coeffs[w.step];
-      const int live = orth_live_strips<SPLIT, CG>(w.kind, m, w.t, rank);
+      const int live = orth_live_strips<SPLIT, CG>(w.t, rank);
       if (!SPLIT) {
         if (!wait_for(&acc_full[buf], parity)) break;
         tc_fence_after();
         const uint32_t base = tmem + buf * T::kTN + half * 32 + lanes;
-        if (live == 0) release();
 #pragma unroll 1
-        for (int s = 0; ok && s < live; ++s) {
-          uint32_t acc[32];
-          tmem_ld32(base + s * 64, acc);
-          tmem_wait_ld();
-          if (s == live - 1) release();
-          ok = finish(w, step, m, s, acc);
-        }
+        for (int s = 0; ok && s < live; ++s) ok = finish(w, step, m, s, base + s * 64);
+        release();
       } else {
         const int chunks = ((w.t.depth + kOrthTK - 1) / kOrthTK + kOrthChunk - 1) / kOrthChunk;
         float sum[T::kBlocks][32];
@@ -679,17 +768,27 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
               for (int e = 0; e < 32; ++e) sum[s][e] = __fadd_rn(sum[s][e], __uint_as_float(acc[e]));
             }
           }
-          release();
+          if (q < chunks - 1) release();
         }
-        small ^= 1;
+        if (!ok) break;
+        // The small terms' accumulator is written again by the tile after next, which waits for a chunk of the next tile
+        // to be drained here if that has two or more: then this chunk need not be held any longer.
+        const bool early = w.next_step >= p.steps || w.next_t.depth > kOrthChunk * kOrthTK;
+        if (early) release();
+        // the sums go back to where the small terms were, so that one loop serves either kind of context
 #pragma unroll
         for (int s = 0; s < T::kBlocks; ++s) {
-          if (!ok || s >= live) continue;
           uint32_t acc[32];
 #pragma unroll
           for (int e = 0; e < 32; ++e) acc[e] = __float_as_uint(sum[s][e]);
-          ok = finish(w, step, m, s, acc);
+          tmem_st32(tmem + (2 + small) * T::kTN + half * 32 + lanes + s * 64, acc);
         }
+        tmem_wait_st();
+        const uint32_t base = tmem + (2 + small) * T::kTN + half * 32 + lanes;
+#pragma unroll 1
+        for (int s = 0; ok && s < live; ++s) ok = finish(w, step, m, s, base + s * 64);
+        if (!early) release();
+        small ^= 1;
       }
     }
   }
