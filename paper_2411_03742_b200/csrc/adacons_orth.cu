@@ -4,6 +4,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <functional>
 #include <memory>
 #include <new>
 #include <utility>
@@ -26,7 +27,7 @@ struct adacons_orth {
   double* partial = nullptr;
   OrthParams params = {};             // all but the result's address
   int cg = 1, blocks = 0;
-  int num_load = 0, num_chunks = 0;
+  int num_load = 0, num_chunks = 0, num_mats = 0;
   int64_t launches = 0;
 };
 
@@ -45,74 +46,121 @@ struct Arena {                        // offsets first, pointers once the alloca
   }
 };
 
-// Who computes which tile of a step's three products, for a tiling with CG blocks per tile.
+// Who computes which tile when: one list of tiles per worker (a block, or a pair of them).
 struct OrthPlan {
-  int cg = 1, workers = 1;
-  std::vector<OrthTile> tiles[3];
-  std::vector<int> begin[3];
-  double cycles = 0;                  // modelled time of a step
+  int cg = 1, workers = 1, mirrored = 1;
+  std::vector<std::vector<OrthTile>> lists;
+  double cycles = 0;                  // modelled time
 };
 
-// Matrices in one order for all workers, the deepest products first; each tile goes to the worker with the
-// least to do so far.  The model: a stage (64 K elements) takes 830 cycles of a pair and 650 of a lone block
-// (measured; the lone block's tile is a quarter), three times the products in an fp32 context 1200; an
-// epilogue overlaps with the next tile; a step cannot be shorter than the longest matrix's three products
-// with about 6000 cycles from the last stage of one to the first of the next.
-OrthPlan plan_step(const std::vector<OrthMat>& mats, bool split, int cg, int workers) {
+// The simulation's costs, in cycles, measured on the kernel.  A stage (64 K elements): what a block's operands take to
+// arrive, about 60 bytes a cycle, 40 when all blocks load at once, or its products.  From the last product of a tile to where
+// others may read it: the strips' arithmetic (a pair's tile has four of them), the store, the fence, the counter, the look.
+// An fp32 context's mirror image is written from registers.
+struct OrthCosts {
+  double stage, strip, mirror, tail;
+  OrthCosts(bool split, int cg) : stage(split ? 1300 : cg == 2 ? 800 : 600), strip(split ? 1500 : 1300), mirror(split ? 6000 : 600), tail(6500) {}
+};
+
+OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int cg, bool mirrored, int workers) {
   OrthPlan plan;
-  const int tm = 128 * cg, tn = split ? 128 : 128 * cg;
-  const double stage = split ? 1200.0 : cg == 2 ? 830.0 : 650.0;
-  const int num = static_cast<int>(mats.size());
-  std::vector<int> order(num);
-  for (int k = 0; k < num; ++k) order[k] = k;
-  auto size = [&](int k) { return static_cast<double>(mats[k].r) * mats[k].r * mats[k].l; };
-  std::sort(order.begin(), order.end(), [&](int x, int y) { return size(x) != size(y) ? size(x) > size(y) : x < y; });
-  auto depth = [&](int kind, int k) { return kind == kOrthGram ? mats[k].l : mats[k].r; };
-  int64_t most = 0;
-  for (int kind = 0; kind < 3; ++kind) {
-    int64_t count = 0;
-    for (const OrthMat& m : mats) count += static_cast<int64_t>((m.r + tm - 1) / tm) * (((kind == kOrthApply ? m.l : m.r) + tn - 1) / tn);
-    most = std::max(most, count);
-  }
   plan.cg = cg;
-  plan.workers = static_cast<int>(std::min<int64_t>(workers, most));
-  std::vector<double> chain(num, 0.0);
-  std::vector<unsigned> stored(num, 0u), stored_after(num, 0u);
-  std::vector<std::pair<double, int>> heap;          // (-load, -worker): the least loaded, then the first, on top
-  for (int w = 0; w < plan.workers; ++w) heap.emplace_back(0.0, -w);
-  std::make_heap(heap.begin(), heap.end());
-  for (int kind = 0; kind < 3; ++kind) {
-    std::vector<std::vector<OrthTile>> mine(plan.workers);
-    for (int k : order) {
-      const int cols = kind == kOrthApply ? mats[k].l : mats[k].r;
-      const double cost = std::max(stage * ((depth(kind, k) + kOrthTK - 1) / kOrthTK), 16.0 * tn) + 1500.0;
-      int64_t count = 0;
-      unsigned blocks = 0;                           // that store a tile of this product
+  plan.mirrored = mirrored;
+  const OrthCosts cost(split, cg);
+  const int tm = 128 * cg, tn = 128 * cg, num = static_cast<int>(mats.size());
+  struct Spot { int i, j; };
+  struct Product { std::vector<Spot> spots; unsigned stored = 0, before = 0; int depth = 0; double busy = 0, after = 0, way = 0; };   // after: last stage to readable; way: both
+  std::vector<Product> products(static_cast<size_t>(num) * 3);
+  size_t most = 1;
+  for (int k = 0; k < num; ++k) {
+    unsigned before = 0;
+    for (int kind = 0; kind < 3; ++kind) {
+      Product& pr = products[3 * k + kind];
+      const int rows = mats[k].r, cols = kind == kOrthApply ? mats[k].l : mats[k].r;
+      pr.depth = kind == kOrthGram ? mats[k].l : mats[k].r;
       for (int64_t j = 0; j * tn < cols; ++j)
-        for (int64_t i = 0; i * tm < mats[k].r; ++i) {
-          if (kind != kOrthApply && i * tm + tm - 1 < j * tn) continue;
-          std::pop_heap(heap.begin(), heap.end());
-          mine[-heap.back().second].push_back({k, static_cast<int>(i), static_cast<int>(j), depth(kind, k), mats[k].r, cols, 0u, stored[k]});
-          heap.back().first -= cost;
-          std::push_heap(heap.begin(), heap.end());
-          for (int rank = 0; rank < cg; ++rank) blocks += i * tm + rank * 128 < mats[k].r;
-          ++count;
+        for (int64_t i = 0; i * tm < rows; ++i) {
+          if (kind != kOrthApply && mirrored && i < j) continue;
+          pr.spots.push_back({static_cast<int>(i), static_cast<int>(j)});
+          for (int rank = 0; rank < cg; ++rank) pr.stored += i * tm + rank * 128 < rows;
         }
-      chain[k] += cost * ((count + plan.workers - 1) / plan.workers) + 6000.0;
-      stored_after[k] = stored[k] + blocks;
-    }
-    stored = stored_after;
-    plan.begin[kind].push_back(0);
-    for (const auto& list : mine) {
-      plan.tiles[kind].insert(plan.tiles[kind].end(), list.begin(), list.end());
-      plan.begin[kind].push_back(static_cast<int>(plan.tiles[kind].size()));
+      pr.before = before;
+      before += pr.stored;
+      const int live = std::min((cols + 63) / 64, tn / 64);
+      pr.busy = std::max((pr.depth + kOrthTK - 1) / kOrthTK * cost.stage, tn / 64 * cost.strip);
+      pr.after = cost.tail + live * cost.strip + (kind != kOrthApply && mirrored && rows > tm ? cost.mirror : 0.0);
+      pr.way = pr.busy + pr.after;
+      most = std::max(most, pr.spots.size() * static_cast<size_t>(num));
     }
   }
-  for (auto& list : plan.tiles)
-    for (OrthTile& t : list) t.per_step = stored[t.mat];
-  for (const auto& h : heap) plan.cycles = std::max(plan.cycles, -h.first);
-  for (double c : chain) plan.cycles = std::max(plan.cycles, c);
+  plan.workers = static_cast<int>(std::min<size_t>(workers, most));
+  plan.lists.resize(plan.workers);
+  std::vector<double> step_way(num, 0.0);
+  for (int k = 0; k < num; ++k)
+    for (int kind = 0; kind < 3; ++kind) step_way[k] += products[3 * k + kind].way;
+
+  struct Open { double at, way; int mat, step, kind; size_t next; double end; };       // a product that may start at `at`
+  auto sooner = [](const Open& x, const Open& y) { return x.at != y.at ? x.at > y.at : x.mat > y.mat; };
+  auto shorter = [](const Open& x, const Open& y) { return x.way != y.way ? x.way < y.way : x.mat > y.mat; };
+  std::vector<Open> future, ready;     // heaps: the soonest, the one with the longest way to go
+  for (int k = 0; k < num; ++k) future.push_back({0.0, step_way[k] * steps, k, 0, 0, 0, 0.0});
+  std::make_heap(future.begin(), future.end(), sooner);
+  typedef std::pair<double, int> Free;                                                 // when, who
+  std::vector<Free> idle;
+  for (int w = 0; w < plan.workers; ++w) idle.emplace_back(0.0, w);
+  std::make_heap(idle.begin(), idle.end(), std::greater<Free>());
+  while (!future.empty() || !ready.empty()) {
+    std::pop_heap(idle.begin(), idle.end(), std::greater<Free>());
+    Free& who = idle.back();
+    if (ready.empty()) who.first = std::max(who.first, future.front().at);
+    while (!future.empty() && future.front().at <= who.first) {
+      std::pop_heap(future.begin(), future.end(), sooner);
+      ready.push_back(future.back());
+      std::push_heap(ready.begin(), ready.end(), shorter);
+      future.pop_back();
+    }
+    Open& open = ready.front();
+    const Product& pr = products[3 * open.mat + open.kind];
+    const Spot spot = pr.spots[open.next++];
+    const OrthMat& m = mats[open.mat];
+    const unsigned per_step = products[3 * open.mat + 2].before + products[3 * open.mat + 2].stored;
+    plan.lists[who.second].push_back({open.mat, spot.i, spot.j, pr.depth, m.r, open.kind == kOrthApply ? m.l : m.r, open.step * per_step + pr.before,
+                                      open.step * 4 + open.kind});
+    who.first += pr.busy;
+    open.end = std::max(open.end, who.first + pr.after);
+    std::push_heap(idle.begin(), idle.end(), std::greater<Free>());
+    if (open.next == pr.spots.size()) {
+      Open then = open;
+      std::pop_heap(ready.begin(), ready.end(), shorter);
+      ready.pop_back();
+      plan.cycles = std::max(plan.cycles, then.end);
+      then.at = then.end;
+      then.way -= pr.way;
+      then.next = 0;
+      if (++then.kind == 3) { then.kind = 0; ++then.step; }
+      if (then.step < steps) {
+        future.push_back(then);
+        std::push_heap(future.begin(), future.end(), sooner);
+      }
+    }
+  }
   return plan;
+}
+
+// The plan with the shortest simulated time: pairs or lone blocks, symmetric products mirrored or, where blocks
+// would idle, computed in full.  For vectors of many tiles only the first choice is tried.
+OrthPlan choose_plan(const std::vector<OrthMat>& mats, bool split, int steps, int singles, int pairs) {
+  double tiles = 0;
+  for (const OrthMat& m : mats) tiles += 3.0 * ((m.r + 255) / 256) * ((m.l + 255) / 256);
+  const bool many = tiles * steps > 40000;
+  OrthPlan best = simulate(mats, split, steps, split ? 1 : 2, true, split ? singles : pairs);
+  for (int cg = split ? 1 : 2; !many && cg >= 1; --cg)
+    for (int mirrored = 1; mirrored >= 0; --mirrored) {
+      if (cg == best.cg && mirrored) continue;
+      OrthPlan plan = simulate(mats, split, steps, cg, mirrored != 0, cg == 2 ? pairs : singles);
+      if (plan.cycles < best.cycles) best = std::move(plan);
+    }
+  return best;
 }
 
 template <bool SPLIT, int CG>
@@ -167,7 +215,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   const bool split = dtype == ADACONS_F32;
   int singles = 0, pairs = 0;
   rc = split ? prepare_kernel<true, 1>(dev.sms, &singles) : prepare_kernel<false, 1>(dev.sms, &singles);
-  if (rc == ADACONS_OK) rc = split ? prepare_kernel<true, 2>(dev.sms, &pairs) : prepare_kernel<false, 2>(dev.sms, &pairs);
+  if (rc == ADACONS_OK && !split) rc = prepare_kernel<false, 2>(dev.sms, &pairs);
   if (rc != ADACONS_OK) return rc;
 
   std::unique_ptr<adacons_orth> holder(new adacons_orth());      // released at the end: nothing leaks if a list runs out of memory
@@ -199,13 +247,16 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
     for (int i = 0; i < (m.r + kOrthLoadTile - 1) / kOrthLoadTile; ++i)
       for (int j = 0; j < (m.l + kOrthLoadCols - 1) / kOrthLoadCols; ++j) load.push_back({k, i, j});
   }
-  OrthPlan plan = plan_step(mats, split, 1, singles);
-  {
-    OrthPlan two = plan_step(mats, split, 2, pairs);
-    if (two.cycles < plan.cycles) plan = std::move(two);
-  }
+  const OrthPlan plan = choose_plan(mats, split, steps, singles, pairs);
   c->cg = plan.cg;
   c->blocks = plan.workers * plan.cg;
+  std::vector<OrthTile> tiles;
+  std::vector<int> begin(1, 0);
+  for (const auto& list : plan.lists) {
+    tiles.insert(tiles.end(), list.begin(), list.end());
+    begin.push_back(static_cast<int>(tiles.size()));
+  }
+  c->num_mats = num;
   std::vector<OrthStep> step_coeffs(steps);
   for (int s = 0; s < steps; ++s) {
     const double* q = coeffs + 3 * s;
@@ -216,11 +267,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
 
   Arena a;
   const size_t at_mats = a.take(num * sizeof(OrthMat)), at_maps = a.take(static_cast<size_t>(num) * kMapCount * sizeof(CUtensorMap));
-  size_t at_tiles[3], at_begin[3];
-  for (int kind = 0; kind < 3; ++kind) {
-    at_tiles[kind] = a.take(plan.tiles[kind].size() * sizeof(OrthTile));
-    at_begin[kind] = a.take(plan.begin[kind].size() * sizeof(int));
-  }
+  const size_t at_tiles = a.take(tiles.size() * sizeof(OrthTile)), at_begin = a.take(begin.size() * sizeof(int));
   const size_t at_coeffs = a.take(step_coeffs.size() * sizeof(OrthStep)), at_done = a.take(num * sizeof(unsigned));
   const size_t at_load = a.take(load.size() * sizeof(OrthSpot)), at_chunks = a.take(chunks.size() * sizeof(OrthChunk));
   const size_t at_partial = a.take(chunks.size() * sizeof(double)), at_flags = a.take(sizeof(uint32_t));
@@ -256,12 +303,11 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   std::memcpy(host.data() + at_mats, mats.data(), num * sizeof(OrthMat));
   std::memcpy(host.data() + at_maps, maps.data(), maps.size() * sizeof(CUtensorMap));
   OrthParams& p = c->params;
-  for (int kind = 0; kind < 3; ++kind) {
-    std::memcpy(host.data() + at_tiles[kind], plan.tiles[kind].data(), plan.tiles[kind].size() * sizeof(OrthTile));
-    std::memcpy(host.data() + at_begin[kind], plan.begin[kind].data(), plan.begin[kind].size() * sizeof(int));
-    p.tiles[kind] = reinterpret_cast<const OrthTile*>(c->memory + at_tiles[kind]);
-    p.begin[kind] = reinterpret_cast<const int*>(c->memory + at_begin[kind]);
-  }
+  std::memcpy(host.data() + at_tiles, tiles.data(), tiles.size() * sizeof(OrthTile));
+  std::memcpy(host.data() + at_begin, begin.data(), begin.size() * sizeof(int));
+  p.tiles = reinterpret_cast<const OrthTile*>(c->memory + at_tiles);
+  p.begin = reinterpret_cast<const int*>(c->memory + at_begin);
+  p.mirrored = plan.mirrored;
   std::memcpy(host.data() + at_coeffs, step_coeffs.data(), step_coeffs.size() * sizeof(OrthStep));
   std::memcpy(host.data() + at_load, load.data(), load.size() * sizeof(OrthSpot));
   std::memcpy(host.data() + at_chunks, chunks.data(), chunks.size() * sizeof(OrthChunk));
@@ -317,11 +363,11 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
   bool ok;
   if (c->dtype == ADACONS_F32) {
     ok = launch(&orth_norm_kernel<0>, dim3(c->num_chunks), dim3(256), 0, st, kLaunchPlain, 1, update, aligned, p.mats, c->chunks, c->partial) &&
-         launch(&orth_load_kernel<0>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, aligned, p.mats, c->load_tiles, partial, c->eps, p.done) &&
-         (c->cg == 2 ? launch_steps<true, 2>(c, p, st) : launch_steps<true, 1>(c, p, st));
+         launch(&orth_load_kernel<0>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, aligned, p.mats, c->load_tiles, partial, c->eps, p.done, c->num_mats) &&
+         launch_steps<true, 1>(c, p, st);
   } else {
     ok = launch(&orth_norm_kernel<1>, dim3(c->num_chunks), dim3(256), 0, st, kLaunchPlain, 1, update, aligned, p.mats, c->chunks, c->partial) &&
-         launch(&orth_load_kernel<1>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, aligned, p.mats, c->load_tiles, partial, c->eps, p.done) &&
+         launch(&orth_load_kernel<1>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, aligned, p.mats, c->load_tiles, partial, c->eps, p.done, c->num_mats) &&
          (c->cg == 2 ? launch_steps<false, 2>(c, p, st) : launch_steps<false, 1>(c, p, st));
   }
   c->launches = 3;

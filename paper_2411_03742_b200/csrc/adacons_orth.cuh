@@ -56,12 +56,12 @@ struct OrthMat {
   __half* b[2];
 };
 struct OrthSpot { int mat, i, j; };           // load kernel: a tile of a matrix
-// One tile of one product, with all that the copying and issuing warps need to know of its matrix.
+// One tile of one product, with all that the warps other than the epilogue's need to know of its matrix.
 struct __align__(16) OrthTile {
-  int mat, i, j, depth;    // depth: K elements of the product
+  int mat, i, j, depth;    // depth: K elements
   int rows, cols;          // of the product: r x l or r x r
-  unsigned per_step;       // tiles that the blocks store for this matrix in a step
-  unsigned before;         // of them, those that come before this product
+  unsigned needs;          // tiles of the matrix that the blocks must have stored before
+  int step_kind;           // step * 4 + OrthKind
 };
 struct OrthStep { float a, b, c, t; };         // t: what is added to B's diagonal
 struct OrthChunk { int mat; int first; };      // norm kernel: chunk number within the matrix
@@ -69,10 +69,11 @@ struct OrthChunk { int mat; int first; };      // norm kernel: chunk number with
 struct OrthParams {
   const OrthMat* mats;
   const CUtensorMap* maps;       // [matrix][kMapCount]
-  const OrthTile* tiles[3];      // by kind, each worker's after the other's
-  const int* begin[3];           // [workers + 1]
+  const OrthTile* tiles;         // each worker's after the other's
+  const int* begin;              // [workers + 1]
   const OrthStep* coeffs;        // [steps]
   unsigned* done;                // [matrix] blocks' tiles stored so far
+  int mirrored;                  // symmetric products are computed on and below the diagonal only
   int steps;
   void* out;                     // the flat result
   int out_aligned;
@@ -150,7 +151,7 @@ __device__ __forceinline__ void orth_split(float v, __half& hi, __half& lo) {
 // X_0 = G / (|G|_F + eps) as pairs, transposed where the matrix is taller than wide.  A block makes 64 rows x
 // 256 columns of X, 64 x 64 at a time.
 template <int DT>
-__global__ void __launch_bounds__(256) orth_load_kernel(const void* in, int aligned, const OrthMat* mats, const OrthSpot* tiles, const double* partial, double eps, unsigned* done) {
+__global__ void __launch_bounds__(256) orth_load_kernel(const void* in, int aligned, const OrthMat* mats, const OrthSpot* tiles, const double* partial, double eps, unsigned* done, int counters) {
   __shared__ float s_tile[kOrthLoadTile][kOrthLoadTile + 1];
   __shared__ double s_sum[8];
   pdl_launch_dependents();
@@ -158,7 +159,8 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, int alig
   const OrthSpot t = tiles[blockIdx.x];
   const OrthMat& m = mats[t.mat];
   const int tid = threadIdx.x;
-  if (tid == 0 && t.i == 0 && t.j == 0) done[t.mat] = 0u;
+  if (blockIdx.x == 0)
+    for (int k = tid; k < counters; k += 256) done[k] = 0u;
   double sum = 0.0;
   for (int k = tid; k < m.norm_count; k += 256) sum += partial[m.norm_first + k];
 #pragma unroll
@@ -233,22 +235,24 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, int alig
 // ----------------------------------------------------------------------------------------------
 // All steps of all matrices in one persistent launch, one block per SM.
 //
-// Every block (or pair) has its share of the tiles of each product, dealt out by their cost, and goes through
-// the steps with it.  A matrix's next product starts when all tiles of its last one are stored, which a
-// counter per matrix says; the matrices are in the same order everywhere, so that while one is completed
-// elsewhere the others keep the block busy.  One launch per product instead (three a step) left the device
-// idle at every boundary: 7 to 10 us for the smallest matrix, and half of the time of one encoder layer.
+// Every block (or pair) goes through its own list of tiles, which the host has laid out by simulating the
+// steps with measured costs: whoever is free takes the tile whose matrix has the longest way to go.  A
+// matrix's next product starts when all tiles of its last one are stored, which a counter per matrix says;
+// while one is completed elsewhere the others keep the block busy.  A tile never waits for one that comes
+// later in the simulated time, so the lists cannot lock.  One launch per product instead (three a step) left the
+// device idle at every boundary, half of the time of one encoder layer.
 // The blocks wait for one another, so the launch is cooperative; each wait is bounded.
 //
 //   Gram   S = X X^T        both operands K-major, straight from X's rows
 //   Poly   B = b S + c S S + t I
 //   Apply  X' = (a - t) X + B X    the right operand is X again, MN-major: no transposed copy exists
-// S and S S are symmetric: only tiles that reach the lower triangle are computed, and each writes its
-// mirror image where no tile does.
+// S and S S are symmetric: where there is work for all, only tiles that reach the lower triangle are computed,
+// and each writes its mirror image where no tile does.
 //
 // Tiles.  CG = 2: a pair of blocks (two SMs) shares a tile of 256 x TN; each holds 128 rows of the left
 // operand, half of the right one and 128 rows of the result, so that an operand byte from L2 feeds
-// twice the products of a single block's tile.  CG = 1: 128 x 128, for problems with too few tiles to occupy the device.
+// twice the products of a single block's tile.  CG = 1: 128 x 128, for problems with too few tiles to occupy the device, and
+// for fp32 contexts, whose three products a stage need no more of the operands than arrives (pairs were no faster there).
 // In each block one warp copies operand stages by TMA, one thread (of the even block) issues the
 // tcgen05 products into one of two TMEM accumulators, and eight warps drain the other.
 //
@@ -256,12 +260,14 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, int alig
 // added (X, S) by TMA two or three strips ahead, the eight warps put the result in its place, and the
 // strip leaves by TMA, which also clips the matrix's edges.  With plain loads and stores of 8 bytes a
 // lane instead, the epilogue of a 256 x 256 tile took 25,000 cycles where its products take 8,000 (K = 1024).
-// Mirror images and transposed results are written from the accumulator's own orientation, where
-// the lanes of a warp are neighbours in memory.
+// Mirror images go the same way, turned in the half of the strip that single values leave free (from an fp32
+// context's pairs, and for transposed results, straight to global memory from the accumulator's own orientation,
+// where the lanes of a warp are neighbours).  Written to global memory two bytes a lane, they cost a phase 13,000 cycles.
 // ----------------------------------------------------------------------------------------------
 constexpr uint32_t kOrthStripPart = 128 * 128;   // 128 rows x 64 fp16 values: two boxes of 64 swizzled rows
 template <bool SPLIT, int CG> struct OrthTiling {
-  static constexpr int kTM = 128 * CG, kTN = SPLIT ? 128 : 128 * CG;
+  static_assert(!SPLIT || CG == 1, "fp32 contexts use lone blocks");
+  static constexpr int kTM = 128 * CG, kTN = 128 * CG;
   static constexpr int kParts = SPLIT ? 2 : 1;
   static constexpr int kBRows = kTN / CG;                            // of the right operand, in each block
   static constexpr uint32_t kA = 128 * kOrthTK * 2, kB = kBRows * kOrthTK * 2;
@@ -298,23 +304,44 @@ __device__ __forceinline__ uint32_t orth_pack2(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// What the epilogue needs of a matrix, fetched once per tile and before its products are there: read where it
+// is used, it comes from global memory again at every strip, 700 of the 1000 cycles of one.
+struct OrthView {
+  int r, cols, lds, l, transposed, vec;
+  float scale;
+  long long offset;
+  unsigned short *hi, *lo;                         // where mirror images go
+  __device__ __forceinline__ OrthView(const OrthParams& p, const OrthTile& t) {
+    const OrthMat& m = p.mats[t.mat];
+    const int kind = t.step_kind & 3;
+    r = t.rows;
+    cols = t.cols;
+    l = m.l;
+    lds = m.lds;
+    transposed = m.transposed;
+    vec = m.vec_out && p.out_aligned;
+    scale = m.scale / kOrthXScale;
+    offset = m.offset;
+    hi = reinterpret_cast<unsigned short*>(kind == kOrthGram ? m.s[0] : m.b[0]);
+    lo = reinterpret_cast<unsigned short*>(kind == kOrthGram ? m.s[1] : m.b[1]);
+  }
+};
+
 // One 32 x 32 block of the product: row0 + lane is this thread's row; its 32 columns from col0 on are read from
 // tensor memory at `acc`.  hi / lo: the block's place in the strip, `half` selecting its 64 bytes of each 128-byte row.
 // A loop of 16 columns and not unrolled code for 32: every product of a small matrix runs this once, and
 // fetching the longer code took 3000 to 6000 cycles of it.  (With 8 columns a turn large matrices lose a tenth to the waits.)
 template <int KIND, bool SPLIT, int CG>
-__device__ __forceinline__ void orth_finish_block(const OrthParams& p, const OrthStep& step, bool last_step, const OrthMat& m, int row0, int col0, uint32_t acc,
+__device__ __forceinline__ void orth_finish_block(const OrthParams& p, const OrthStep& step, bool last_step, const OrthView& m, int row0, int col0, uint32_t acc,
                                                   unsigned char* hi, unsigned char* lo, int half) {
   using T = OrthTiling<SPLIT, CG>;
   const int lane = threadIdx.x & 31;
-  const int r = m.r, ncols = KIND == kOrthApply ? m.l : m.r, row = row0 + lane;
+  const int r = m.r, ncols = m.cols, row = row0 + lane;
   const bool last = KIND == kOrthApply && last_step;
   constexpr bool kPair = KIND == kOrthApply || SPLIT;      // X is always a pair, S and B only in an fp32 context
   // where no tile above the diagonal is computed, its image comes from here
-  const bool mirror = KIND != kOrthApply && !((col0 / T::kTM) * T::kTM + T::kTM - 1 >= (row0 / T::kTN) * T::kTN);
+  const bool mirror = KIND != kOrthApply && p.mirrored && row0 / T::kTM > col0 / T::kTN;
   const bool turned = last && m.transposed;
-  unsigned short* dst_hi = reinterpret_cast<unsigned short*>(KIND == kOrthGram ? m.s[0] : m.b[0]);
-  unsigned short* dst_lo = reinterpret_cast<unsigned short*>(KIND == kOrthGram ? m.s[1] : m.b[1]);
   unsigned char* hrow = hi + lane * 128;
   unsigned char* lrow = lo + lane * 128;
   const float by_x = KIND == kOrthPoly ? step.b * (kOrthBScale / kOrthSScale) : step.a - step.t;
@@ -363,10 +390,17 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
       }
       *reinterpret_cast<uint4*>(hrow + at) = make_uint4(h[0], h[1], h[2], h[3]);
       if (kPair) *reinterpret_cast<uint4*>(lrow + at) = make_uint4(l[0], l[1], l[2], l[3]);
-      if (mirror && row < r) {
+      if (!SPLIT && mirror) {                        // turned into the strip's free part: 64 rows, the strip's columns, of two boxes
+        const int r64 = row & 63;
+        unsigned char* turned_at = lo - static_cast<int>(row & 32) * 128 + (half * 32 + 8 * g) * 128 + (r64 & 7) * 2;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          *reinterpret_cast<unsigned short*>(turned_at + e * 128 + (((r64 >> 3) ^ e) * 16)) = static_cast<unsigned short>(h[e / 2] >> (16 * (e & 1)));
+      }
+      if (SPLIT && mirror && row < r) {
         const int col = col0 + 8 * g;
-        unsigned short* to_hi = dst_hi + static_cast<long long>(col) * m.lds + row;
-        unsigned short* to_lo = dst_lo + static_cast<long long>(col) * m.lds + row;
+        unsigned short* to_hi = m.hi + static_cast<long long>(col) * m.lds + row;
+        unsigned short* to_lo = m.lo + static_cast<long long>(col) * m.lds + row;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           if (col + e < ncols) {
@@ -378,7 +412,7 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
       continue;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= m.scale / kOrthXScale;
+    for (int e = 0; e < 8; ++e) v[e] *= m.scale;
     if (turned) {
       const int col = col0 + 8 * g;
       const long long to = m.offset + static_cast<long long>(col) * r + row;
@@ -407,8 +441,7 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
   }
   if (last && !turned) {                           // to the vector, along rows
     __syncwarp();
-    const bool vec = m.vec_out && p.out_aligned;
-    if (vec) {                                     // 8 columns a lane, 8 rows at a time
+    if (m.vec) {                                     // 8 columns a lane, 8 rows at a time
       const int q = lane & 3;
 #pragma unroll
       for (int it = 0; it < 4; ++it) {
@@ -440,43 +473,24 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
   }
 }
 
-// The products of one block in the order in which all of its warps go through them.  The next tile's record
+// The tiles of one block in the order in which all of its warps go through them.  The next tile's record
 // is on its way while a tile is worked on.
 struct OrthWalk {
   const OrthParams& p;
-  const int worker;
-  int begin[3], end[3];                          // this worker's tiles by kind
-  int step, kind, k;
-  int next_step, next_kind, next_k;
+  int k, end;
   OrthTile t, next_t;
-  __device__ __forceinline__ OrthWalk(const OrthParams& params, int w) : p(params), worker(w) {
-#pragma unroll
-    for (int q = 0; q < 3; ++q) { begin[q] = p.begin[q][worker]; end[q] = p.begin[q][worker + 1]; }
-    next_step = 0;
-    next_kind = 0;
-    next_k = begin[0] - 1;
-    look_ahead();
-    next();
+  __device__ __forceinline__ OrthWalk(const OrthParams& params, int worker) : p(params), k(p.begin[worker]), end(p.begin[worker + 1]) {
+    if (k < end) t = p.tiles[k];
+    if (k + 1 < end) next_t = p.tiles[k + 1];
   }
-  __device__ __forceinline__ bool more() const { return step < p.steps; }
-  __device__ __forceinline__ void look_ahead() {
-    ++next_k;
-    while (next_k >= (next_kind == 0 ? end[0] : next_kind == 1 ? end[1] : end[2])) {
-      if (++next_kind == 3) { next_kind = 0; ++next_step; }
-      if (next_step >= p.steps) return;
-      next_k = next_kind == 0 ? begin[0] : next_kind == 1 ? begin[1] : begin[2];
-    }
-    next_t = (next_kind == 0 ? p.tiles[0] : next_kind == 1 ? p.tiles[1] : p.tiles[2])[next_k];
-  }
+  __device__ __forceinline__ bool more() const { return k < end; }
   __device__ __forceinline__ void next() {
-    step = next_step;
-    kind = next_kind;
-    k = next_k;
+    ++k;
     t = next_t;
-    if (step < p.steps) look_ahead();
+    if (k + 1 < end) next_t = p.tiles[k + 1];
   }
-  // stored tiles of the matrix that this product needs: all of its earlier products
-  __device__ __forceinline__ unsigned needs() const { return step * t.per_step + t.before; }
+  __device__ __forceinline__ int kind() const { return t.step_kind & 3; }
+  __device__ __forceinline__ int step() const { return t.step_kind >> 2; }
 };
 
 __device__ __forceinline__ unsigned orth_load_acquire(const unsigned* p) {
@@ -486,7 +500,7 @@ __device__ __forceinline__ unsigned orth_load_acquire(const unsigned* p) {
 }
 // Whether what a product reads is there; the copies that follow are ordered behind the look.
 __device__ __forceinline__ bool orth_ready(const OrthWalk& w) {
-  if (orth_load_acquire(w.p.done + w.t.mat) < w.needs()) return false;
+  if (orth_load_acquire(w.p.done + w.t.mat) < w.t.needs) return false;
   asm volatile("fence.proxy.async.global;" ::: "memory");
   return true;
 }
@@ -545,10 +559,10 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
       bool ok = true;
       for (OrthWalk w(p, worker); ok && w.more(); w.next()) {
         const CUtensorMap* maps = p.maps + static_cast<long long>(w.t.mat) * kMapCount;
-        const CUtensorMap* x_map = maps + kMapX0 + 2 * (w.step & 1);
-        const CUtensorMap* ma = w.kind == kOrthGram ? x_map : w.kind == kOrthPoly ? maps + kMapS : maps + kMapB;
-        const CUtensorMap* mb = w.kind == kOrthPoly ? maps + kMapS : x_map;
-        const bool across = w.kind == kOrthApply;                           // the right operand's K runs along its rows
+        const CUtensorMap* x_map = maps + kMapX0 + 2 * (w.step() & 1);
+        const CUtensorMap* ma = w.kind() == kOrthGram ? x_map : w.kind() == kOrthPoly ? maps + kMapS : maps + kMapB;
+        const CUtensorMap* mb = w.kind() == kOrthPoly ? maps + kMapS : x_map;
+        const bool across = w.kind() == kOrthApply;                           // the right operand's K runs along its rows
         const int arow = w.t.i * T::kTM + rank * 128, brow = w.t.j * T::kTN + rank * T::kBRows;
         if (!orth_wait_ready(w, &s_abort)) { s_abort = 1; break; }
         for (int k0 = 0; k0 < w.t.depth; k0 += kOrthTK) {
@@ -583,7 +597,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
       uint32_t parity = 0, acc_parity = 1;
       bool ok = true;
       for (OrthWalk w(p, worker); ok && w.more(); w.next()) {
-        const bool across = w.kind == kOrthApply;
+        const bool across = w.kind() == kOrthApply;
         const uint32_t idesc = across ? mma_idesc(T::kTM, T::kTN, false, false, true) : mma_idesc(T::kTM, T::kTN, false, false, false);
         const uint64_t b_base = across ? desc_mnmajor(0, 8192) : desc_kmajor(0);
         const uint32_t b_step = across ? 2048 / 16 : 32 / 16;
@@ -650,7 +664,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
         if (ask.w.more() && ahead < T::kRing) {
           const int to = loads % T::kRing;
           unsigned char* at = smem + T::kStrips + to * 2 * kOrthStripPart;
-          if (ask.w.kind == kOrthGram) {
+          if (ask.w.kind() == kOrthGram) {
             mbar_arrive_one(&strip_full[to]);
             ++loads;
             ask.next(rank);
@@ -659,8 +673,8 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
           // nothing of this block may stay unsent while it waits for what others compute from it
           const bool there = ahead > 0 ? orth_ready(ask.w) : orth_wait_ready(ask.w, &s_abort);
           if (there) {
-            const int parts = ask.w.kind == kOrthApply || SPLIT ? 2 : 1;   // X is always a pair, S only in an fp32 context
-            const CUtensorMap* map = p.maps + static_cast<long long>(ask.w.t.mat) * kMapCount + (ask.w.kind == kOrthPoly ? kMapS : kMapX0 + 2 * (ask.w.step & 1));
+            const int parts = ask.w.kind() == kOrthApply || SPLIT ? 2 : 1;   // X is always a pair, S only in an fp32 context
+            const CUtensorMap* map = p.maps + static_cast<long long>(ask.w.t.mat) * kMapCount + (ask.w.kind() == kOrthPoly ? kMapS : kMapX0 + 2 * (ask.w.step() & 1));
             const int row = ask.w.t.i * T::kTM + rank * 128, col = ask.w.t.j * T::kTN + ask.strip * 64;
             mbar_expect_tx(&strip_full[to], parts * kOrthStripPart);
             for (int part = 0; part < parts; ++part)
@@ -673,17 +687,22 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
           if (ahead == 0) { s_abort = 1; break; }
         }
         if (!mbar_wait_bounded(&strip_done[b], parity)) { s_abort = 1; break; }
-        const bool last = give.w.kind == kOrthApply && give.w.step == p.steps - 1;     // written to the result by the warps themselves
+        const bool last = give.w.kind() == kOrthApply && give.w.step() == p.steps - 1;     // written to the result by the warps themselves
         if (!last) {
-          const int parts = give.w.kind == kOrthApply || SPLIT ? 2 : 1;
+          const int parts = give.w.kind() == kOrthApply || SPLIT ? 2 : 1;
           const CUtensorMap* map = p.maps + static_cast<long long>(give.w.t.mat) * kMapCount +
-                                   (give.w.kind == kOrthGram ? kMapS : give.w.kind == kOrthPoly ? kMapB : kMapX0 + 2 * ((give.w.step & 1) ^ 1));
+                                   (give.w.kind() == kOrthGram ? kMapS : give.w.kind() == kOrthPoly ? kMapB : kMapX0 + 2 * ((give.w.step() & 1) ^ 1));
           const unsigned char* at = smem + T::kStrips + b * 2 * kOrthStripPart;
           const int row = give.w.t.i * T::kTM + rank * 128, col = give.w.t.j * T::kTN + give.strip * 64;
           for (int part = 0; part < parts; ++part)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
               if (row + h * 64 < give.w.t.rows) tma_store_2d(map + part, at + part * kOrthStripPart + h * 8192, col, row + h * 64);
+          if (!SPLIT && p.mirrored && give.w.kind() != kOrthApply && give.w.t.i > give.w.t.j) {      // the mirror image
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (row + h * 64 < give.w.t.rows) tma_store_2d(map, at + kOrthStripPart + h * 8192, row + h * 64, col);
+          }
           bulk_commit();
           if (give.strip == give.live - 1) {               // the tile is complete: say so once its bytes are
             bulk_wait<0>();
@@ -717,13 +736,13 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
       buf ^= 1;
       if (buf == 0) parity ^= 1u;
     };
-    auto finish = [&](const OrthWalk& w, const OrthStep& step, const OrthMat& m, int strip, uint32_t acc) {
+    auto finish = [&](const OrthWalk& w, const OrthStep& step, const OrthView& m, int strip, uint32_t acc) {
       if (!wait_for(&strip_full[place], strip_parity)) return false;
       unsigned char* at = smem + T::kStrips + place * 2 * kOrthStripPart + (warp & 3) * 32 * 128;
       const int row0 = w.t.i * T::kTM + rank * 128 + (warp & 3) * 32, col0 = w.t.j * T::kTN + strip * 64 + half * 32;
-      const bool last = w.step == p.steps - 1;
-      if (w.kind == kOrthGram) orth_finish_block<kOrthGram, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
-      else if (w.kind == kOrthPoly) orth_finish_block<kOrthPoly, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
+      const bool last = w.step() == p.steps - 1;
+      if (w.kind() == kOrthGram) orth_finish_block<kOrthGram, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
+      else if (w.kind() == kOrthPoly) orth_finish_block<kOrthPoly, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
       else orth_finish_block<kOrthApply, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
       fence_proxy_async_smem();
       __syncwarp();
@@ -731,17 +750,22 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
       if (++place == T::kRing) { place = 0; strip_parity ^= 1u; }
       return true;
     };
+    auto finish_tile = [&](const OrthWalk& w, const OrthStep& step, const OrthView& m, int live, uint32_t base) {
+#pragma unroll 1
+      for (int s = 0; s < live; ++s)
+        if (!finish(w, step, m, s, base + s * 64)) return false;
+      return true;
+    };
     bool ok = true;
     for (OrthWalk w(p, worker); ok && w.more(); w.next()) {
-      const OrthMat& m = p.mats[w.t.mat];
-      const OrthStep step = p.coeffs[w.step];
+      const OrthView m(p, w.t);
+      const OrthStep step = p.coeffs[w.step()];
       const int live = orth_live_strips<SPLIT, CG>(w.t, rank);
       if (!SPLIT) {
         if (!wait_for(&acc_full[buf], parity)) break;
         tc_fence_after();
         const uint32_t base = tmem + buf * T::kTN + half * 32 + lanes;
-#pragma unroll 1
-        for (int s = 0; ok && s < live; ++s) ok = finish(w, step, m, s, base + s * 64);
+        ok = finish_tile(w, step, m, live, base);
         release();
       } else {
         const int chunks = ((w.t.depth + kOrthTK - 1) / kOrthTK + kOrthChunk - 1) / kOrthChunk;
@@ -773,7 +797,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
         if (!ok) break;
         // The small terms' accumulator is written again by the tile after next, which waits for a chunk of the next tile
         // to be drained here if that has two or more: then this chunk need not be held any longer.
-        const bool early = w.next_step >= p.steps || w.next_t.depth > kOrthChunk * kOrthTK;
+        const bool early = w.k + 1 >= w.end || w.next_t.depth > kOrthChunk * kOrthTK;
         if (early) release();
         // the sums go back to where the small terms were, so that one loop serves either kind of context
 #pragma unroll
@@ -785,8 +809,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
         }
         tmem_wait_st();
         const uint32_t base = tmem + (2 + small) * T::kTN + half * 32 + lanes;
-#pragma unroll 1
-        for (int s = 0; ok && s < live; ++s) ok = finish(w, step, m, s, base + s * 64);
+        ok = finish_tile(w, step, m, live, base);
         if (!early) release();
         small ^= 1;
       }
