@@ -27,6 +27,7 @@ struct adacons_orth {
   double* partial = nullptr;
   OrthParams params = {};             // all but the result's address
   int cg = 1, blocks = 0;
+  bool small = false;                 // all matrices fit the one-block kernel
   int num_load = 0, num_chunks = 0, num_mats = 0;
   int64_t launches = 0;
 };
@@ -189,6 +190,14 @@ int prepare_kernel(int sms, int* workers) {
   return *workers > 0 ? ADACONS_OK : ADACONS_ECUDA;
 }
 
+template <bool SPLIT>
+int prepare_small() {
+  static_assert(kSmallBytes <= 227 * 1024, "shared memory of a block");
+  if (cudaFuncSetAttribute(orth_small_kernel<SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmallBytes) == cudaSuccess) return ADACONS_OK;
+  cudaGetLastError();
+  return ADACONS_ECUDA;
+}
+
 template <bool SPLIT, int CG>
 bool launch_steps(const adacons_orth* c, const OrthParams& p, cudaStream_t st) {
   return launch(&orth_steps_kernel<SPLIT, CG>, dim3(c->blocks), dim3(kOrthThreads), OrthTiling<SPLIT, CG>::kBytes, st, kLaunchCooperative, CG, p);
@@ -216,6 +225,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   int singles = 0, pairs = 0;
   rc = split ? prepare_kernel<true, 1>(dev.sms, &singles) : prepare_kernel<false, 1>(dev.sms, &singles);
   if (rc == ADACONS_OK && !split) rc = prepare_kernel<false, 2>(dev.sms, &pairs);
+  if (rc == ADACONS_OK) rc = split ? prepare_small<true>() : prepare_small<false>();
   if (rc != ADACONS_OK) return rc;
 
   std::unique_ptr<adacons_orth> holder(new adacons_orth());      // released at the end: nothing leaks if a list runs out of memory
@@ -247,7 +257,11 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
     for (int i = 0; i < (m.r + kOrthLoadTile - 1) / kOrthLoadTile; ++i)
       for (int j = 0; j < (m.l + kOrthLoadCols - 1) / kOrthLoadCols; ++j) load.push_back({k, i, j});
   }
-  const OrthPlan plan = choose_plan(mats, split, steps, singles, pairs);
+  // The one-block kernel only where every matrix fits it: beside larger ones the small ones cost the general kernel
+  // next to nothing (their chain is the shorter), and a second launch would come on top.
+  c->small = true;
+  for (const OrthMat& m : mats) c->small = c->small && m.r <= kOrthSmallR && m.l <= kOrthSmallL;
+  const OrthPlan plan = c->small ? OrthPlan() : choose_plan(mats, split, steps, singles, pairs);
   c->cg = plan.cg;
   c->blocks = plan.workers * plan.cg;
   std::vector<OrthTile> tiles;
@@ -273,7 +287,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   const size_t at_partial = a.take(chunks.size() * sizeof(double)), at_flags = a.take(sizeof(uint32_t));
   const size_t head = a.used;
   std::vector<size_t> at(static_cast<size_t>(num) * kMapCount, 0);
-  for (int k = 0; k < num; ++k)
+  for (int k = 0; k < num && !c->small; ++k)
     for (int q = 0; q < kMapCount; ++q) {
       const bool is_x = q < kMapS;
       if (!is_x && (q & 1) && !split) continue;                  // S and B are pairs only in an fp32 context
@@ -360,8 +374,12 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
   p.out_aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0;
   const double* partial = c->partial;
   const int aligned = reinterpret_cast<uintptr_t>(update) % 16 == 0;
+  c->launches = c->small ? 1 : 3;
   bool ok;
-  if (c->dtype == ADACONS_F32) {
+  if (c->small) {
+    if (c->dtype == ADACONS_F32) ok = launch(&orth_small_kernel<true>, dim3(c->num_mats), dim3(kOrthSmallThreads), kSmallBytes, st, kLaunchPlain, 1, p, update, c->eps);
+    else ok = launch(&orth_small_kernel<false>, dim3(c->num_mats), dim3(kOrthSmallThreads), kSmallBytes, st, kLaunchPlain, 1, p, update, c->eps);
+  } else if (c->dtype == ADACONS_F32) {
     ok = launch(&orth_norm_kernel<0>, dim3(c->num_chunks), dim3(256), 0, st, kLaunchPlain, 1, update, aligned, p.mats, c->chunks, c->partial) &&
          launch(&orth_load_kernel<0>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, aligned, p.mats, c->load_tiles, partial, c->eps, p.done, c->num_mats) &&
          launch_steps<true, 1>(c, p, st);
@@ -370,7 +388,6 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
          launch(&orth_load_kernel<1>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, aligned, p.mats, c->load_tiles, partial, c->eps, p.done, c->num_mats) &&
          (c->cg == 2 ? launch_steps<false, 2>(c, p, st) : launch_steps<false, 1>(c, p, st));
   }
-  c->launches = 3;
   return ok ? ADACONS_OK : ADACONS_ECUDA;
 }
 

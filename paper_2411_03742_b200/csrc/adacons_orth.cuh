@@ -290,19 +290,56 @@ __device__ __forceinline__ int orth_live_strips(const OrthTile& t, int rank) {
   return left < T::kBlocks ? left : T::kBlocks;
 }
 
-__device__ __forceinline__ void orth_unpack8(const uint4& v, float (&f)[8]) {
-  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+// Eight elements: v <- by_v v + by_x (hi + lo), two at a time.
+__device__ __forceinline__ void orth_scale8(float2 (&v)[4], float by_v) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = mul2(v[k], make_float2(by_v, by_v));
+}
+__device__ __forceinline__ void orth_add8(float2 (&v)[4], float by_x, const unsigned char* at) {
+  const uint4 x = *reinterpret_cast<const uint4*>(at);
+  const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = fma2(make_float2(by_x, by_x), __half22float2(*reinterpret_cast<const __half2*>(&u[k])), v[k]);
+}
+__device__ __forceinline__ void orth_diagonal8(float2 (&v)[4], int at, float t) {        // element `at` of the eight, if it is one
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const float2 p = __half22float2(*reinterpret_cast<const __half2*>(&u[k]));
-    f[2 * k] = p.x;
-    f[2 * k + 1] = p.y;
+    v[k].x += at == 2 * k ? t : 0.f;
+    v[k].y += at == 2 * k + 1 ? t : 0.f;
   }
 }
-__device__ __forceinline__ uint32_t orth_pack2(float a, float b) {
-  const __half2 h = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&h);
+// hi and (in h and l) the rest, each rounded to fp16
+template <bool PAIR>
+__device__ __forceinline__ void orth_round8(const float2 (&v)[4], uint4& h, uint4& l) {
+  uint32_t a[4], b[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const __half2 q = __float22half2_rn(v[k]);
+    a[k] = *reinterpret_cast<const uint32_t*>(&q);
+    if (PAIR) {
+      const float2 f = __half22float2(q);
+      const __half2 rest = __float22half2_rn(add2(v[k], make_float2(-f.x, -f.y)));
+      b[k] = *reinterpret_cast<const uint32_t*>(&rest);
+    }
+  }
+  h = make_uint4(a[0], a[1], a[2], a[3]);
+  if (PAIR) l = make_uint4(b[0], b[1], b[2], b[3]);
 }
+// fp32 words as their upper and lower halves, in the two parts of a place
+__device__ __forceinline__ void orth_halves8(const float2 (&v)[4], uint4& upper, uint4& lower) {
+  uint32_t u[4], d[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    u[k] = __byte_perm(__float_as_uint(v[k].x), __float_as_uint(v[k].y), 0x7632);
+    d[k] = __byte_perm(__float_as_uint(v[k].x), __float_as_uint(v[k].y), 0x5410);
+  }
+  upper = make_uint4(u[0], u[1], u[2], u[3]);
+  lower = make_uint4(d[0], d[1], d[2], d[3]);
+}
+__device__ __forceinline__ uint4 orth_bf16x8(const float2 (&v)[4]) {
+  return make_uint4(pack_bf16x2_rn(v[0].x, v[0].y), pack_bf16x2_rn(v[1].x, v[1].y), pack_bf16x2_rn(v[2].x, v[2].y), pack_bf16x2_rn(v[3].x, v[3].y));
+}
+__device__ __forceinline__ uint32_t orth_word(const uint4& v, int k) { return k == 0 ? v.x : k == 1 ? v.y : k == 2 ? v.z : v.w; }
 
 // What the epilogue needs of a matrix, fetched once per tile and before its products are there: read where it
 // is used, it comes from global memory again at every strip, 700 of the 1000 cycles of one.
@@ -346,7 +383,6 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
   unsigned char* lrow = lo + lane * 128;
   const float by_x = KIND == kOrthPoly ? step.b * (kOrthBScale / kOrthSScale) : step.a - step.t;
   const float by_v = KIND == kOrthGram ? kOrthSScale / (kOrthXScale * kOrthXScale) : KIND == kOrthPoly ? step.c * (kOrthBScale / (kOrthSScale * kOrthSScale)) : 1.f / kOrthBScale;
-  const int diagonal = KIND == kOrthPoly ? row - col0 : -1;      // the column, from col0, of this row's diagonal element
 #pragma unroll 1
   for (int turn = 0; turn < 2; ++turn) {
    uint32_t a[16];
@@ -356,46 +392,26 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
    for (int sub = 0; sub < 2; ++sub) {
     const int g = 2 * turn + sub;
     const int at = ((4 * half + g) ^ (lane & 7)) * 16;
-    float v[8];
+    float2 v[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(a[8 * sub + e]);
-    if constexpr (KIND == kOrthGram) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= by_v;
-    } else {
-      float x[8];
-      orth_unpack8(*reinterpret_cast<const uint4*>(hrow + at), x);
-      if constexpr (kPair) {
-        float y[8];
-        orth_unpack8(*reinterpret_cast<const uint4*>(lrow + at), y);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += y[e];
-      }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = by_x * x[e] + by_v * v[e];
-      if (KIND == kOrthPoly) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += 8 * g + e == diagonal ? step.t * kOrthBScale : 0.f;
-      }
+    for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(a[8 * sub + 2 * k]), __uint_as_float(a[8 * sub + 2 * k + 1]));
+    orth_scale8(v, by_v);
+    if constexpr (KIND != kOrthGram) {
+      orth_add8(v, by_x, hrow + at);
+      if (kPair) orth_add8(v, by_x, lrow + at);
+      if (KIND == kOrthPoly && row0 == col0) orth_diagonal8(v, lane - 8 * g, step.t * kOrthBScale);
     }
     if (!last) {
-      uint32_t h[4], l[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        h[k] = orth_pack2(v[2 * k], v[2 * k + 1]);
-        if (kPair) {
-          const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&h[k]));
-          l[k] = orth_pack2(v[2 * k] - b.x, v[2 * k + 1] - b.y);
-        }
-      }
-      *reinterpret_cast<uint4*>(hrow + at) = make_uint4(h[0], h[1], h[2], h[3]);
-      if (kPair) *reinterpret_cast<uint4*>(lrow + at) = make_uint4(l[0], l[1], l[2], l[3]);
+      uint4 h, l;
+      orth_round8<kPair>(v, h, l);
+      *reinterpret_cast<uint4*>(hrow + at) = h;
+      if (kPair) *reinterpret_cast<uint4*>(lrow + at) = l;
       if (!SPLIT && mirror) {                        // turned into the strip's free part: 64 rows, the strip's columns, of two boxes
         const int r64 = row & 63;
         unsigned char* turned_at = lo - static_cast<int>(row & 32) * 128 + (half * 32 + 8 * g) * 128 + (r64 & 7) * 2;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          *reinterpret_cast<unsigned short*>(turned_at + e * 128 + (((r64 >> 3) ^ e) * 16)) = static_cast<unsigned short>(h[e / 2] >> (16 * (e & 1)));
+          *reinterpret_cast<unsigned short*>(turned_at + e * 128 + (((r64 >> 3) ^ e) * 16)) = static_cast<unsigned short>(orth_word(h, e / 2) >> (16 * (e & 1)));
       }
       if (SPLIT && mirror && row < r) {
         const int col = col0 + 8 * g;
@@ -404,38 +420,32 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           if (col + e < ncols) {
-            to_hi[static_cast<long long>(e) * m.lds] = static_cast<unsigned short>(h[e / 2] >> (16 * (e & 1)));
-            if (kPair) to_lo[static_cast<long long>(e) * m.lds] = static_cast<unsigned short>(l[e / 2] >> (16 * (e & 1)));
+            to_hi[static_cast<long long>(e) * m.lds] = static_cast<unsigned short>(orth_word(h, e / 2) >> (16 * (e & 1)));
+            to_lo[static_cast<long long>(e) * m.lds] = static_cast<unsigned short>(orth_word(l, e / 2) >> (16 * (e & 1)));
           }
         }
       }
       continue;
     }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= m.scale;
+    orth_scale8(v, m.scale);
     if (turned) {
       const int col = col0 + 8 * g;
       const long long to = m.offset + static_cast<long long>(col) * r + row;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
+        const float f = e & 1 ? v[e / 2].y : v[e / 2].x;
         if (row < r && col + e < ncols) {
-          if (SPLIT) static_cast<float*>(p.out)[to + static_cast<long long>(e) * r] = v[e];
-          else static_cast<unsigned short*>(p.out)[to + static_cast<long long>(e) * r] = static_cast<unsigned short>(pack_bf16x2_rn(v[e], 0.f) & 0xffffu);
+          if (SPLIT) static_cast<float*>(p.out)[to + static_cast<long long>(e) * r] = f;
+          else static_cast<unsigned short*>(p.out)[to + static_cast<long long>(e) * r] = static_cast<unsigned short>(pack_bf16x2_rn(f, 0.f) & 0xffffu);
         }
       }
     } else if (SPLIT) {                            // the strip's two parts hold the upper and the lower halves of the fp32 words
-      uint32_t u[4], d[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t x0 = __float_as_uint(v[2 * k]), x1 = __float_as_uint(v[2 * k + 1]);
-        u[k] = __byte_perm(x0, x1, 0x7632);
-        d[k] = __byte_perm(x0, x1, 0x5410);
-      }
-      *reinterpret_cast<uint4*>(hrow + at) = make_uint4(u[0], u[1], u[2], u[3]);
-      *reinterpret_cast<uint4*>(lrow + at) = make_uint4(d[0], d[1], d[2], d[3]);
+      uint4 u, d;
+      orth_halves8(v, u, d);
+      *reinterpret_cast<uint4*>(hrow + at) = u;
+      *reinterpret_cast<uint4*>(lrow + at) = d;
     } else {
-      *reinterpret_cast<uint4*>(hrow + at) =
-          make_uint4(pack_bf16x2_rn(v[0], v[1]), pack_bf16x2_rn(v[2], v[3]), pack_bf16x2_rn(v[4], v[5]), pack_bf16x2_rn(v[6], v[7]));
+      *reinterpret_cast<uint4*>(hrow + at) = orth_bf16x8(v);
     }
    }
   }
@@ -833,6 +843,218 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
     tc_fence_after();
     tmem_dealloc<CG>(tmem, T::kTmemCols);
   }
+}
+
+// ----------------------------------------------------------------------------------------------
+// Vectors of small matrices only (short side up to 128, long side up to 256): one block takes a matrix through
+// everything, norm to result, with X, S and B in shared memory and the accumulators in tensor memory; nothing but the
+// matrix itself crosses global memory.  What bounds it is the chain of a step's three products and epilogues,
+// 4 to 6 us a step; through the general kernel the same chain is 15 to 20 us, most of it stores, fences and
+// looks at counters (96 x 200 fp32: 115 us there).
+//
+// X is held as up to four blocks of 128 rows x 64 columns (swizzled 128-byte rows, as TMA would leave them):
+// K-major operand of the Gram product, MN-major right operand of the Apply product.  S and B share a place: B
+// replaces S element by element once the product that reads S is complete.
+// ----------------------------------------------------------------------------------------------
+constexpr int kOrthSmallR = 128, kOrthSmallL = 256;
+constexpr int kOrthSmallThreads = 544;           // warps 0-15 elementwise, 16 products
+constexpr uint32_t kSmallBlock = 128 * 128, kSmallXLo = 4 * kSmallBlock, kSmallS = 8 * kSmallBlock, kSmallSLo = 10 * kSmallBlock, kSmallBytes = 12 * kSmallBlock + 1024;
+
+template <bool SPLIT>
+__global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const OrthParams p, const void* in, double eps) {
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
+  __shared__ uint64_t s_done;
+  __shared__ uint32_t s_tmem;
+  __shared__ double s_sum[16];
+  __shared__ volatile int s_abort;
+  constexpr int DT = SPLIT ? 0 : 1;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const OrthMat m = p.mats[blockIdx.x];
+  if (tid == 0) { mbar_init(&s_done, 1); s_abort = 0; mbar_init_fence(); }
+  if (warp == 16) tmem_alloc(&s_tmem, 512);
+  // X_0, transposed where the matrix is taller than wide; everything outside it stays zero
+  for (int k = tid; k < static_cast<int>(12 * kSmallBlock / 16); k += kOrthSmallThreads) reinterpret_cast<uint4*>(smem)[k] = make_uint4(0u, 0u, 0u, 0u);
+  const int size = m.r * m.l;
+  double sum = 0.0;
+  const int width = m.transposed ? m.r : m.l;     // of a row in the vector
+  const int step_y = kOrthSmallThreads / width, step_x = kOrthSmallThreads - step_y * width;
+  // element (y, x) of the matrix in X's blocks
+  auto place_of = [&](int y, int x) {
+    const int row = m.transposed ? x : y, col = m.transposed ? y : x;
+    return (col >> 6) * kSmallBlock + row * 128 + ((((col >> 3) & 7) ^ (row & 7)) << 4) + (col & 7) * 2;
+  };
+  __syncthreads();                                 // the zeros
+  // As it comes first: bf16 where the hi parts will be, fp32 as upper and lower halves.
+  for (int k0 = tid, y = tid / width, x = tid - y * width; k0 < size;) {       // eight loads on their way at a time
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = k0 + e * kOrthSmallThreads < size ? orth_in<DT>(in, m.offset + k0 + e * kOrthSmallThreads) : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      sum = fma(static_cast<double>(v[e]), static_cast<double>(v[e]), sum);
+      if (k0 < size) {
+        const uint32_t at = place_of(y, x), bits = __float_as_uint(v[e]);
+        *reinterpret_cast<unsigned short*>(smem + at) = static_cast<unsigned short>(bits >> 16);
+        if (SPLIT) *reinterpret_cast<unsigned short*>(smem + kSmallXLo + at) = static_cast<unsigned short>(bits);
+      }
+      k0 += kOrthSmallThreads;
+      y += step_y;
+      x += step_x;
+      if (x >= width) { x -= width; ++y; }
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (warp < 16 && lane == 0) s_sum[warp] = sum;
+  __shared__ double s_last;
+  if (warp == 16 && lane == 0) s_last = sum;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  sum = s_last;
+  for (int w = 0; w < 16; ++w) sum += s_sum[w];
+  const float mul = static_cast<float>(static_cast<double>(kOrthXScale) / (sqrt(sum) + eps));
+  for (int k = tid; k < 8 * ((m.l + 63) / 64) * m.r; k += kOrthSmallThreads) {       // then pairs of 2^11 X_0, eight elements at a time
+    const int group = k / m.r;
+    unsigned char* at = smem + (group >> 3) * kSmallBlock + (k - group * m.r) * 128 + (group & 7) * 16;
+    const uint4 u = *reinterpret_cast<const uint4*>(at), d = *reinterpret_cast<const uint4*>(at + kSmallXLo);
+    float2 v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t a = orth_word(u, q), b = SPLIT ? orth_word(d, q) : 0u;
+      v[q] = make_float2(__uint_as_float(__byte_perm(b, a, 0x5410)), __uint_as_float(__byte_perm(b, a, 0x7632)));
+    }
+    orth_scale8(v, mul);
+    uint4 h, l;
+    orth_round8<true>(v, h, l);
+    *reinterpret_cast<uint4*>(at) = h;
+    *reinterpret_cast<uint4*>(at + kSmallXLo) = l;
+  }
+  fence_proxy_async_smem();
+  __syncthreads();
+
+  bool issuer = false;
+  if (warp == 16) issuer = elect_one();
+  const int row = (warp & 3) * 32 + lane, part = warp >> 2;
+  const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+  const uint32_t base = smem_addr(smem);
+  const int r16 = (m.r + 15) / 16, l16 = (m.l + 15) / 16;
+  uint32_t parity = 0;
+  // Tensor memory: Gram and Poly 128 columns of sums over K below 128, 128 beyond, 128 of small terms; Apply 256 and 256.
+  for (int s = 0; s < p.steps; ++s) {
+    const OrthStep step = p.coeffs[s];
+    const bool last = s == p.steps - 1;
+    for (int kind = 0; kind < 3; ++kind) {
+      if (warp == 16) {
+        const uint64_t x_rows = desc_kmajor(0) + (base >> 4), x_cols = desc_mnmajor(0, kSmallBlock) + (base >> 4), s_rows = desc_kmajor(0) + ((base + kSmallS) >> 4);
+        const uint64_t a0 = kind == kOrthGram ? x_rows : s_rows, b0 = kind == kOrthPoly ? s_rows : kind == kOrthGram ? x_rows : x_cols;
+        const uint32_t a_lo = (kind == kOrthGram ? kSmallXLo : kSmallSLo - kSmallS) >> 4, b_lo = (kind == kOrthPoly ? kSmallSLo - kSmallS : kSmallXLo) >> 4;
+        const uint32_t idesc = kind == kOrthApply ? mma_idesc(128, 0, false, false, true) | (static_cast<uint32_t>(l16 * 16) >> 3 << 17) : mma_idesc(128, 128, false, false, false);
+        const uint32_t low = tmem + 256;
+        const int steps_k = kind == kOrthGram ? l16 : r16;
+        // the whole warp loops, so that the descriptors are uniform values; one lane issues
+        for (int k0 = 0; k0 < steps_k; k0 += 4) {
+          const uint32_t block = (k0 >> 2) * (kSmallBlock >> 4);
+          const uint64_t a = a0 + block, b = b0 + (kind == kOrthApply ? static_cast<uint32_t>(k0) * (2048 >> 4) : block);
+          const uint32_t b_step = kind == kOrthApply ? 2048 >> 4 : 32 >> 4, big = tmem + (k0 >= 8 ? 128 : 0), more = k0 != 0, more_big = k0 != 0 && k0 != 8;
+          if (issuer) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              if (k0 + kk >= steps_k) continue;
+              if (SPLIT) {
+                mma_ss(low, a + a_lo + kk * 2, b + kk * b_step, idesc, kk != 0 ? 1u : more);
+                mma_ss(low, a + kk * 2, b + b_lo + kk * b_step, idesc, 1u);
+              }
+              mma_ss(big, a + kk * 2, b + kk * b_step, idesc, kk != 0 ? 1u : more_big);
+            }
+          }
+          __syncwarp();
+        }
+        if (issuer) mma_commit(&s_done);
+        __syncwarp();
+      }
+      if (!mbar_wait_bounded(&s_done, parity)) s_abort = 1;
+      parity ^= 1u;
+      tc_fence_after();
+      if (warp < 16 && (warp & 3) * 32 < m.r) {    // rows beyond the matrix are zero and stay so
+        const bool beyond = kind == kOrthGram && l16 > 8;
+        const int col0 = part * (kind == kOrthApply ? 64 : 32), cols = kind == kOrthApply ? m.l : m.r;
+        unsigned char* place = smem + (kind == kOrthApply ? 0u : kSmallS) + (col0 >> 6) * kSmallBlock + row * 128;
+        const uint32_t place_lo = kind == kOrthApply ? kSmallXLo : kSmallSLo - kSmallS;
+        const float by_x = kind == kOrthPoly ? step.b * (kOrthBScale / kOrthSScale) : step.a - step.t;
+        const float by_v = kind == kOrthGram ? kOrthSScale / (kOrthXScale * kOrthXScale)
+                                             : kind == kOrthPoly ? step.c * (kOrthBScale / (kOrthSScale * kOrthSScale)) : 1.f / kOrthBScale;
+        const int turns = kind == kOrthApply ? 4 : 2;
+#pragma unroll 1
+        for (int turn = 0; turn < turns; ++turn) {
+          const int col = col0 + turn * 16;
+          if (col >= cols) break;                  // warp-uniform; what lies beyond is zero and stays so
+          float2 v[8];
+          {
+            uint32_t a[16];
+            auto take = [&](uint32_t from, bool add) {
+              tmem_ld16(from, a);
+              tmem_wait_ld();
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                const float2 f = make_float2(__uint_as_float(a[2 * k]), __uint_as_float(a[2 * k + 1]));
+                v[k] = add ? add2(v[k], f) : f;
+              }
+            };
+            take(tmem + lanes + col, false);
+            if (beyond) take(tmem + 128 + lanes + col, true);
+            if (SPLIT) take(tmem + 256 + lanes + col, true);
+          }
+#pragma unroll
+          for (int sub = 0; sub < 2; ++sub) {
+            unsigned char* at = place + (((((col & 63) >> 3) + sub) ^ (row & 7)) << 4);
+            float2 w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = v[4 * sub + k];
+            orth_scale8(w, by_v);
+            if (kind != kOrthGram) {
+              orth_add8(w, by_x, at);
+              if (SPLIT || kind == kOrthApply) orth_add8(w, by_x, at + place_lo);
+              if (kind == kOrthPoly && part == (warp & 3)) orth_diagonal8(w, row - col - 8 * sub, step.t * kOrthBScale);
+            }
+            uint4 h, l;
+            if (kind == kOrthApply && last) {      // the result in X's place: bf16, or the upper and lower halves of fp32 words
+              orth_scale8(w, m.scale / kOrthXScale);
+              if (SPLIT) orth_halves8(w, h, l);
+              else h = orth_bf16x8(w);
+            } else {
+              orth_round8<true>(w, h, l);
+            }
+            *reinterpret_cast<uint4*>(at) = h;
+            if (SPLIT || (kind == kOrthApply && !last)) *reinterpret_cast<uint4*>(at + place_lo) = l;
+          }
+        }
+        fence_proxy_async_smem();
+        tc_fence_before();
+      }
+      __syncthreads();
+      tc_fence_after();
+      if (s_abort) break;                          // set before the barrier: the whole block agrees
+    }
+    if (s_abort) break;
+  }
+  if (!s_abort) {                                  // to the vector, as it lies there
+#pragma unroll 4
+    for (int k = tid, y = tid / width, x = tid - y * width; k < size; k += kOrthSmallThreads) {
+      const uint32_t at = place_of(y, x);
+      const uint32_t u = *reinterpret_cast<const unsigned short*>(smem + at);
+      if (SPLIT) static_cast<uint32_t*>(p.out)[m.offset + k] = u << 16 | *reinterpret_cast<const unsigned short*>(smem + kSmallXLo + at);
+      else static_cast<unsigned short*>(p.out)[m.offset + k] = static_cast<unsigned short>(u);
+      y += step_y;
+      x += step_x;
+      if (x >= width) { x -= width; ++y; }
+    }
+  }
+  if (s_abort && tid == 0) atomicOr(p.flags, kFlagTimeout);
+  __syncthreads();
+  if (warp == 16) tmem_dealloc(tmem, 512);
 }
 
 }  // namespace adacons
