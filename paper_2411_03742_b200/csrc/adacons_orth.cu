@@ -377,8 +377,8 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
   c->launches = c->small ? 1 : 3;
   bool ok;
   if (c->small) {
-    if (c->dtype == ADACONS_F32) ok = launch(&orth_small_kernel<true>, dim3(c->num_mats), dim3(kOrthSmallThreads), kSmallBytes, st, kLaunchPlain, 1, p, update, c->eps);
-    else ok = launch(&orth_small_kernel<false>, dim3(c->num_mats), dim3(kOrthSmallThreads), kSmallBytes, st, kLaunchPlain, 1, p, update, c->eps);
+    if (c->dtype == ADACONS_F32) ok = launch(&orth_small_kernel<true>, dim3(c->num_mats), dim3(kOrthSmallThreads), kSmallBytes, st, kLaunchPlain, 1, p, update, aligned, c->eps);
+    else ok = launch(&orth_small_kernel<false>, dim3(c->num_mats), dim3(kOrthSmallThreads), kSmallBytes, st, kLaunchPlain, 1, p, update, aligned, c->eps);
   } else if (c->dtype == ADACONS_F32) {
     ok = launch(&orth_norm_kernel<0>, dim3(c->num_chunks), dim3(256), 0, st, kLaunchPlain, 1, update, aligned, p.mats, c->chunks, c->partial) &&
          launch(&orth_load_kernel<0>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, aligned, p.mats, c->load_tiles, partial, c->eps, p.done, c->num_mats) &&

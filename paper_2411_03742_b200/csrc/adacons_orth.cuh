@@ -861,7 +861,7 @@ constexpr int kOrthSmallThreads = 544;           // warps 0-15 elementwise, 16 p
 constexpr uint32_t kSmallBlock = 128 * 128, kSmallXLo = 4 * kSmallBlock, kSmallS = 8 * kSmallBlock, kSmallSLo = 10 * kSmallBlock, kSmallBytes = 12 * kSmallBlock + 1024;
 
 template <bool SPLIT>
-__global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const OrthParams p, const void* in, double eps) {
+__global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const OrthParams p, const void* in, int aligned, double eps) {
   extern __shared__ unsigned char smem_dyn[];
   unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
   __shared__ uint64_t s_done;
@@ -885,23 +885,44 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
     return (col >> 6) * kSmallBlock + row * 128 + ((((col >> 3) & 7) ^ (row & 7)) << 4) + (col & 7) * 2;
   };
   __syncthreads();                                 // the zeros
-  // As it comes first: bf16 where the hi parts will be, fp32 as upper and lower halves.
-  for (int k0 = tid, y = tid / width, x = tid - y * width; k0 < size;) {       // eight loads on their way at a time
-    float v[8];
+  // Rows of whole groups of eight: all of a thread's elements in flight at once, kept until the norm is known.
+  constexpr int kHeld = kOrthSmallR * kOrthSmallL / 8 / kOrthSmallThreads + 1;
+  const bool vec = aligned && m.vec_in && width % 8 == 0;
+  float held[kHeld][8];
+  if (vec) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = k0 + e * kOrthSmallThreads < size ? orth_in<DT>(in, m.offset + k0 + e * kOrthSmallThreads) : 0.f;
+    for (int q = 0; q < kHeld; ++q) {
+      const int k = tid + q * kOrthSmallThreads;
+      if (8 * k < size) {
+        orth_in8<DT>(in, m.offset + 8 * k, held[q]);
+      } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      sum = fma(static_cast<double>(v[e]), static_cast<double>(v[e]), sum);
-      if (k0 < size) {
-        const uint32_t at = place_of(y, x), bits = __float_as_uint(v[e]);
-        *reinterpret_cast<unsigned short*>(smem + at) = static_cast<unsigned short>(bits >> 16);
-        if (SPLIT) *reinterpret_cast<unsigned short*>(smem + kSmallXLo + at) = static_cast<unsigned short>(bits);
+        for (int e = 0; e < 8; ++e) held[q][e] = 0.f;
       }
-      k0 += kOrthSmallThreads;
-      y += step_y;
-      x += step_x;
-      if (x >= width) { x -= width; ++y; }
+    }
+#pragma unroll
+    for (int q = 0; q < kHeld; ++q)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fma(static_cast<double>(held[q][e]), static_cast<double>(held[q][e]), sum);
+  } else {
+    // As it comes first: bf16 where the hi parts will be, fp32 as upper and lower halves.
+    for (int k0 = tid, y = tid / width, x = tid - y * width; k0 < size;) {       // eight loads on their way at a time
+      float v[8];
+  #pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = k0 + e * kOrthSmallThreads < size ? orth_in<DT>(in, m.offset + k0 + e * kOrthSmallThreads) : 0.f;
+  #pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        sum = fma(static_cast<double>(v[e]), static_cast<double>(v[e]), sum);
+        if (k0 < size) {
+          const uint32_t at = place_of(y, x), bits = __float_as_uint(v[e]);
+          *reinterpret_cast<unsigned short*>(smem + at) = static_cast<unsigned short>(bits >> 16);
+          if (SPLIT) *reinterpret_cast<unsigned short*>(smem + kSmallXLo + at) = static_cast<unsigned short>(bits);
+        }
+        k0 += kOrthSmallThreads;
+        y += step_y;
+        x += step_x;
+        if (x >= width) { x -= width; ++y; }
+      }
     }
   }
 #pragma unroll
@@ -916,21 +937,48 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
   sum = s_last;
   for (int w = 0; w < 16; ++w) sum += s_sum[w];
   const float mul = static_cast<float>(static_cast<double>(kOrthXScale) / (sqrt(sum) + eps));
-  for (int k = tid; k < 8 * ((m.l + 63) / 64) * m.r; k += kOrthSmallThreads) {       // then pairs of 2^11 X_0, eight elements at a time
-    const int group = k / m.r;
-    unsigned char* at = smem + (group >> 3) * kSmallBlock + (k - group * m.r) * 128 + (group & 7) * 16;
-    const uint4 u = *reinterpret_cast<const uint4*>(at), d = *reinterpret_cast<const uint4*>(at + kSmallXLo);
-    float2 v[4];
+  if (vec) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint32_t a = orth_word(u, q), b = SPLIT ? orth_word(d, q) : 0u;
-      v[q] = make_float2(__uint_as_float(__byte_perm(b, a, 0x5410)), __uint_as_float(__byte_perm(b, a, 0x7632)));
+    for (int q = 0; q < kHeld; ++q) {
+      const int k = 8 * (tid + q * kOrthSmallThreads);
+      if (k >= size) continue;
+      const int y = k / width, x = k - y * width;
+      float2 v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = make_float2(held[q][2 * e], held[q][2 * e + 1]);
+      orth_scale8(v, mul);
+      uint4 h, l;
+      orth_round8<true>(v, h, l);
+      if (!m.transposed) {
+        const uint32_t at = place_of(y, x);
+        *reinterpret_cast<uint4*>(smem + at) = h;
+        *reinterpret_cast<uint4*>(smem + kSmallXLo + at) = l;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t at = place_of(y, x + e);
+          *reinterpret_cast<unsigned short*>(smem + at) = static_cast<unsigned short>(orth_word(h, e / 2) >> (16 * (e & 1)));
+          *reinterpret_cast<unsigned short*>(smem + kSmallXLo + at) = static_cast<unsigned short>(orth_word(l, e / 2) >> (16 * (e & 1)));
+        }
+      }
     }
-    orth_scale8(v, mul);
-    uint4 h, l;
-    orth_round8<true>(v, h, l);
-    *reinterpret_cast<uint4*>(at) = h;
-    *reinterpret_cast<uint4*>(at + kSmallXLo) = l;
+  } else {
+    for (int k = tid; k < 8 * ((m.l + 63) / 64) * m.r; k += kOrthSmallThreads) {       // then pairs of 2^11 X_0, eight elements at a time
+      const int group = k / m.r;
+      unsigned char* at = smem + (group >> 3) * kSmallBlock + (k - group * m.r) * 128 + (group & 7) * 16;
+      const uint4 u = *reinterpret_cast<const uint4*>(at), d = *reinterpret_cast<const uint4*>(at + kSmallXLo);
+      float2 v[4];
+  #pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t a = orth_word(u, q), b = SPLIT ? orth_word(d, q) : 0u;
+        v[q] = make_float2(__uint_as_float(__byte_perm(b, a, 0x5410)), __uint_as_float(__byte_perm(b, a, 0x7632)));
+      }
+      orth_scale8(v, mul);
+      uint4 h, l;
+      orth_round8<true>(v, h, l);
+      *reinterpret_cast<uint4*>(at) = h;
+      *reinterpret_cast<uint4*>(at + kSmallXLo) = l;
+    }
   }
   fence_proxy_async_smem();
   __syncthreads();
@@ -993,19 +1041,17 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
           if (col >= cols) break;                  // warp-uniform; what lies beyond is zero and stays so
           float2 v[8];
           {
-            uint32_t a[16];
-            auto take = [&](uint32_t from, bool add) {
-              tmem_ld16(from, a);
-              tmem_wait_ld();
+            uint32_t a[16], b[16], c[16];          // all loads, then one wait
+            tmem_ld16(tmem + lanes + col, a);
+            if (beyond) tmem_ld16(tmem + 128 + lanes + col, b);
+            if (SPLIT) tmem_ld16(tmem + 256 + lanes + col, c);
+            tmem_wait_ld();
 #pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const float2 f = make_float2(__uint_as_float(a[2 * k]), __uint_as_float(a[2 * k + 1]));
-                v[k] = add ? add2(v[k], f) : f;
-              }
-            };
-            take(tmem + lanes + col, false);
-            if (beyond) take(tmem + 128 + lanes + col, true);
-            if (SPLIT) take(tmem + 256 + lanes + col, true);
+            for (int k = 0; k < 8; ++k) {
+              v[k] = make_float2(__uint_as_float(a[2 * k]), __uint_as_float(a[2 * k + 1]));
+              if (beyond) v[k] = add2(v[k], make_float2(__uint_as_float(b[2 * k]), __uint_as_float(b[2 * k + 1])));
+              if (SPLIT) v[k] = add2(v[k], make_float2(__uint_as_float(c[2 * k]), __uint_as_float(c[2 * k + 1])));
+            }
           }
 #pragma unroll
           for (int sub = 0; sub < 2; ++sub) {
