@@ -21,7 +21,7 @@ namespace adacons {
 // a X takes the pair; in an fp32 context S and B are pairs too and each product is the sum
 // (lo hi + hi lo) + hi hi.  The tensor cores round a running sum toward zero, low by up to 4e-8 of it
 // per chained product: harmless beside an 11-bit operand, but 4e-5 of an fp32 result after five steps
-// on sides of 1024.  There the hi hi terms are chained over 128 K elements at most and the chunks'
+// on sides of 1024.  There the hi hi terms are chained over 64 K elements at most and the chunks'
 // sums added by the epilogue, round to nearest (the small terms, 2^-11 of the sum, in one accumulator).
 // Why not bf16 operands: rounding the iterates to 8 bits costs 1e-2 of the result's norm on a
 // Gaussian matrix and 1e-1 on one with a few strong directions (the small singular values grow
@@ -33,7 +33,7 @@ namespace adacons {
 // matrices (on a matrix of rank 8 plus noise 5e-4 instead of 1.5e-4, still a third of the rounding).
 // ----------------------------------------------------------------------------------------------
 constexpr int kOrthTK = 64;              // K elements per stage: one 128-byte swizzled row
-constexpr int kOrthChunk = 2;            // fp32 contexts: stages (128 K elements) per hi hi accumulator
+constexpr int kOrthChunk = 1;            // fp32 contexts: stages (64 K elements) per hi hi accumulator
 constexpr float kOrthXScale = 2048.f, kOrthSScale = 8192.f, kOrthBScale = 2048.f;
 constexpr int kOrthThreads = 352;        // warps 0-7 epilogue, 8 operand copies, 9 products, 10 epilogue copies
 constexpr int kOrthNormChunk = 16384;    // elements per block of the norm kernel
@@ -779,31 +779,28 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
         release();
       } else {
         const int chunks = ((w.t.depth + kOrthTK - 1) / kOrthTK + kOrthChunk - 1) / kOrthChunk;
-        float sum[T::kBlocks][32];
-        for (int q = 0; q < chunks; ++q) {
-          if (!wait_for(&acc_full[buf], parity)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t base = tmem + buf * T::kTN + half * 32 + lanes;
+        float2 sum[T::kBlocks][16];
+#pragma unroll
+        for (int s = 0; s < T::kBlocks; ++s)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sum[s][e] = make_float2(0.f, 0.f);
+        auto drain_into_sum = [&](uint32_t from) {
 #pragma unroll
           for (int s = 0; s < T::kBlocks; ++s) {
             uint32_t acc[32];
-            tmem_ld32(base + s * 64, acc);
+            tmem_ld32(from + s * 64, acc);
             tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 32; ++e) sum[s][e] = q == 0 ? __uint_as_float(acc[e]) : __fadd_rn(sum[s][e], __uint_as_float(acc[e]));
+            for (int e = 0; e < 16; ++e) sum[s][e] = add2(sum[s][e], make_float2(__uint_as_float(acc[2 * e]), __uint_as_float(acc[2 * e + 1])));
           }
-          if (q == chunks - 1) {                           // the last chunk's commit covers the small terms too
-#pragma unroll
-            for (int s = 0; s < T::kBlocks; ++s) {
-              uint32_t acc[32];
-              tmem_ld32(tmem + (2 + small) * T::kTN + half * 32 + lanes + s * 64, acc);
-              tmem_wait_ld();
-#pragma unroll
-              for (int e = 0; e < 32; ++e) sum[s][e] = __fadd_rn(sum[s][e], __uint_as_float(acc[e]));
-            }
-          }
+        };
+        for (int q = 0; q < chunks; ++q) {
+          if (!wait_for(&acc_full[buf], parity)) { ok = false; break; }
+          tc_fence_after();
+          drain_into_sum(tmem + buf * T::kTN + half * 32 + lanes);
           if (q < chunks - 1) release();
         }
+        if (ok) drain_into_sum(tmem + (2 + small) * T::kTN + half * 32 + lanes);       // the last chunk's commit covers the small terms too
         if (!ok) break;
         // The small terms' accumulator is written again by the tile after next, which waits for a chunk of the next tile
         // to be drained here if that has two or more: then this chunk need not be held any longer.
@@ -814,7 +811,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
         for (int s = 0; s < T::kBlocks; ++s) {
           uint32_t acc[32];
 #pragma unroll
-          for (int e = 0; e < 32; ++e) acc[e] = __float_as_uint(sum[s][e]);
+          for (int e = 0; e < 32; ++e) acc[e] = __float_as_uint(e & 1 ? sum[s][e / 2].y : sum[s][e / 2].x);
           tmem_st32(tmem + (2 + small) * T::kTN + half * 32 + lanes + s * 64, acc);
         }
         tmem_wait_st();
@@ -990,7 +987,7 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
   const uint32_t base = smem_addr(smem);
   const int r16 = (m.r + 15) / 16, l16 = (m.l + 15) / 16;
   uint32_t parity = 0;
-  // Tensor memory: Gram and Poly 128 columns of sums over K below 128, 128 beyond, 128 of small terms; Apply 256 and 256.
+  // Tensor memory: one accumulator of 128 columns (Apply: 256) for each 64 of K.
   for (int s = 0; s < p.steps; ++s) {
     const OrthStep step = p.coeffs[s];
     const bool last = s == p.steps - 1;
@@ -1000,26 +997,29 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
         const uint64_t a0 = kind == kOrthGram ? x_rows : s_rows, b0 = kind == kOrthPoly ? s_rows : kind == kOrthGram ? x_rows : x_cols;
         const uint32_t a_lo = (kind == kOrthGram ? kSmallXLo : kSmallSLo - kSmallS) >> 4, b_lo = (kind == kOrthPoly ? kSmallSLo - kSmallS : kSmallXLo) >> 4;
         const uint32_t idesc = kind == kOrthApply ? mma_idesc(128, 0, false, false, true) | (static_cast<uint32_t>(l16 * 16) >> 3 << 17) : mma_idesc(128, 128, false, false, false);
-        const uint32_t low = tmem + 256;
         const int steps_k = kind == kOrthGram ? l16 : r16;
-        // the whole warp loops, so that the descriptors are uniform values; one lane issues
-        for (int k0 = 0; k0 < steps_k; k0 += 4) {
-          const uint32_t block = (k0 >> 2) * (kSmallBlock >> 4);
-          const uint64_t a = a0 + block, b = b0 + (kind == kOrthApply ? static_cast<uint32_t>(k0) * (2048 >> 4) : block);
-          const uint32_t b_step = kind == kOrthApply ? 2048 >> 4 : 32 >> 4, big = tmem + (k0 >= 8 ? 128 : 0), more = k0 != 0, more_big = k0 != 0 && k0 != 8;
-          if (issuer) {
+        const uint32_t b_step = kind == kOrthApply ? 2048 >> 4 : 32 >> 4, wide = kind == kOrthApply ? 256 : 128;
+        // The small terms first, then the hi hi ones: on top of them, and from K = 64 (Apply: 64) on in accumulators of
+        // their own, chained four products at most.  The whole warp loops, so that the descriptors are uniform values; one lane issues.
+        for (int pass = SPLIT ? 0 : 1; pass < 2; ++pass)
+          for (int k0 = 0; k0 < steps_k; k0 += 4) {
+            const uint32_t block = (k0 >> 2) * (kSmallBlock >> 4);
+            const uint64_t a = a0 + block, b = b0 + (kind == kOrthApply ? static_cast<uint32_t>(k0) * (2048 >> 4) : block);
+            const uint32_t d = tmem + (pass == 0 ? 0u : static_cast<uint32_t>(k0 >> 2) * wide), more = pass == 0 ? k0 != 0 : SPLIT && k0 == 0;
+            if (issuer) {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-              if (k0 + kk >= steps_k) continue;
-              if (SPLIT) {
-                mma_ss(low, a + a_lo + kk * 2, b + kk * b_step, idesc, kk != 0 ? 1u : more);
-                mma_ss(low, a + kk * 2, b + b_lo + kk * b_step, idesc, 1u);
+              for (int kk = 0; kk < 4; ++kk) {
+                if (k0 + kk >= steps_k) continue;
+                if (pass == 0) {
+                  mma_ss(d, a + a_lo + kk * 2, b + kk * b_step, idesc, kk != 0 ? 1u : more);
+                  mma_ss(d, a + kk * 2, b + b_lo + kk * b_step, idesc, 1u);
+                } else {
+                  mma_ss(d, a + kk * 2, b + kk * b_step, idesc, kk != 0 ? 1u : more);
+                }
               }
-              mma_ss(big, a + kk * 2, b + kk * b_step, idesc, kk != 0 ? 1u : more_big);
             }
+            __syncwarp();
           }
-          __syncwarp();
-        }
         if (issuer) mma_commit(&s_done);
         __syncwarp();
       }
@@ -1027,7 +1027,8 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
       parity ^= 1u;
       tc_fence_after();
       if (warp < 16 && (warp & 3) * 32 < m.r) {    // rows beyond the matrix are zero and stay so
-        const bool beyond = kind == kOrthGram && l16 > 8;
+        const int chains = ((kind == kOrthGram ? l16 : r16) + 3) / 4;
+        const uint32_t wide = kind == kOrthApply ? 256 : 128;
         const int col0 = part * (kind == kOrthApply ? 64 : 32), cols = kind == kOrthApply ? m.l : m.r;
         unsigned char* place = smem + (kind == kOrthApply ? 0u : kSmallS) + (col0 >> 6) * kSmallBlock + row * 128;
         const uint32_t place_lo = kind == kOrthApply ? kSmallXLo : kSmallSLo - kSmallS;
@@ -1041,16 +1042,24 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
           if (col >= cols) break;                  // warp-uniform; what lies beyond is zero and stays so
           float2 v[8];
           {
-            uint32_t a[16], b[16], c[16];          // all loads, then one wait
+            uint32_t a[16], b[16];
             tmem_ld16(tmem + lanes + col, a);
-            if (beyond) tmem_ld16(tmem + 128 + lanes + col, b);
-            if (SPLIT) tmem_ld16(tmem + 256 + lanes + col, c);
+            if (chains > 1) tmem_ld16(tmem + wide + lanes + col, b);
             tmem_wait_ld();
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               v[k] = make_float2(__uint_as_float(a[2 * k]), __uint_as_float(a[2 * k + 1]));
-              if (beyond) v[k] = add2(v[k], make_float2(__uint_as_float(b[2 * k]), __uint_as_float(b[2 * k + 1])));
-              if (SPLIT) v[k] = add2(v[k], make_float2(__uint_as_float(c[2 * k]), __uint_as_float(c[2 * k + 1])));
+              if (chains > 1) v[k] = add2(v[k], make_float2(__uint_as_float(b[2 * k]), __uint_as_float(b[2 * k + 1])));
+            }
+            if (chains > 2) {                      // the Gram product of more than 128 columns
+              tmem_ld16(tmem + 2 * wide + lanes + col, a);
+              if (chains > 3) tmem_ld16(tmem + 3 * wide + lanes + col, b);
+              tmem_wait_ld();
+#pragma unroll
+              for (int k = 0; k < 8; ++k) {
+                v[k] = add2(v[k], make_float2(__uint_as_float(a[2 * k]), __uint_as_float(a[2 * k + 1])));
+                if (chains > 3) v[k] = add2(v[k], make_float2(__uint_as_float(b[2 * k]), __uint_as_float(b[2 * k + 1])));
+              }
             }
           }
 #pragma unroll
