@@ -29,7 +29,7 @@ bool raise(K kernel, uint32_t bytes) {
 }
 template <int D, bool BF16>
 bool raise_all() {
-  static_assert(AttnFwdSmem<D>::kBytes <= 227 * 1024 && attn_backward_smem<D>() <= 227 * 1024, "shared memory of a block");
+  static_assert(AttnFwdSmem<D>::kBytes <= 112 * 1024 && attn_backward_smem<D>() <= 227 * 1024, "shared memory of a block");
   return raise(attn_forward_kernel<D, BF16>, AttnFwdSmem<D>::kBytes) && raise(attn_backward_kernel<D, BF16>, attn_backward_smem<D>());
 }
 
@@ -117,8 +117,8 @@ AttnParams base_params(const AttnDevice& d, const adacons_attn_shape* s) {
 
 template <int D, bool BF16>
 bool run_forward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const AttnParams& p, cudaStream_t st) {
-  return launch(&attn_forward_kernel<D, BF16>, dim3((p.Sq + 2 * kAttnTile - 1) / (2 * kAttnTile), p.Hq, p.B), dim3(kAttnThreads), AttnFwdSmem<D>::kBytes, st,
-                kLaunchPlain, 1, mq, mk, mv, p);
+  return launch(&attn_forward_kernel<D, BF16>, dim3((p.Sq + kAttnTile - 1) / kAttnTile, p.Hq, p.B), dim3(kFwdThreads), AttnFwdSmem<D>::kBytes, st, kLaunchPlain, 1,
+                mq, mk, mv, p);
 }
 
 template <int D, bool BF16>

@@ -55,6 +55,11 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
   if (BF16) return pack_bf16x2_rn(lo, hi);
@@ -101,11 +106,17 @@ __device__ __forceinline__ void attn_mma_rows(uint32_t d, uint64_t a, uint64_t b
 }
 // 128 x D product over tokens: 16-bit values in tensor memory with the tokens of `b`.  Whoever had columns
 // 32 g .. 32 g + 31 of the fp32 scores puts their 16 words of 16-bit values in the first half of that place.
+// 32 tokens: k and k + 1 of the eight groups of 16.
 template <int D, bool BF16>
-__device__ __forceinline__ void attn_mma_tokens(uint32_t d, uint32_t a, uint64_t b, bool accumulate) {
+__device__ __forceinline__ void attn_mma_some_tokens(uint32_t d, uint32_t a, uint64_t b, int k, bool accumulate) {
   constexpr uint32_t idesc = mma_idesc(kAttnTile, D, BF16, false, true);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) mma_ts(d, a + (k / 2) * 32 + (k % 2) * 8, b + k * (2048 >> 4), idesc, k != 0 ? 1u : accumulate);
+  for (int e = 0; e < 2; ++e) mma_ts(d, a + (k / 2) * 32 + e * 8, b + (k + e) * (2048 >> 4), idesc, e != 0 ? 1u : accumulate);
+}
+template <int D, bool BF16>
+__device__ __forceinline__ void attn_mma_tokens(uint32_t d, uint32_t a, uint64_t b, bool accumulate) {
+#pragma unroll
+  for (int k = 0; k < 8; k += 2) attn_mma_some_tokens<D, BF16>(d, a, b, k, accumulate || k != 0);
 }
 
 // Columns [first, first + 32 BLOCKS) of row `row` of an accumulator (this thread's lane), times `mul`, to global memory.
@@ -140,75 +151,72 @@ __device__ __forceinline__ int attn_kv_len(const AttnParams& p, int batch) {
 }
 
 // ----------------------------------------------------------------------------------------------
-// Forward.  A block owns two tiles of 128 queries and walks over the key tiles, the softmax of one
-// query tile running while the tensor cores work for the other.  Tensor memory: S of both tiles (128
-// columns each, later the rounded P in its place) and both accumulators.  Two threads share one query's
-// row of scores and exchange their maxima (one thread a row needs none, but with two warps per scheduler
-// every instruction's latency shows: 5200 cycles per pair of tiles, of which 2200 are products).  The running maximum is only raised
-// when a row's scores exceed it by more than 2^8 in the exponential (the quotient O / sum does not
-// depend on it, and fp32 and bf16 have the range): the accumulator is then rescaled in place, which
-// after the first few key tiles hardly happens.
+// Forward.  A block owns 128 queries of one head and walks over the key tiles: S = Q K^T, softmax, O += P V,
+// one after the other; two blocks share an SM, and one's softmax runs while the tensor cores work for the other.
+// (One block with two query tiles in turn reads K and V half as often, but is no faster at 8192 tokens, 562 us
+// against 573, and slower where blocks are few or short: 2048 causal tokens of 8 heads 42 us against 35.)
+// Tensor memory: S (128 columns, later the rounded P in its place) and the accumulator.
+// Two threads share one query's row of scores and exchange their maxima (one thread a row needs none, but with two
+// warps per scheduler every instruction's latency shows).  The running maximum is only raised when a row's scores exceed
+// it by more than 2^8 in the exponential (the quotient O / sum does not depend on it, and fp32 and bf16 have the
+// range): the accumulator is then rescaled in place, which after the first few key tiles hardly happens.
 // ----------------------------------------------------------------------------------------------
+constexpr int kFwdThreads = 320;                 // warps 0-7 softmax, 8 copies, 9 products
 template <int D> struct AttnFwdSmem {
   static constexpr uint32_t kT = AttnTile<D>::kBytes;
-  static constexpr int kSlots = D == 128 ? 5 : 8;              // ring of K and V tiles in turn
-  // In front of the tiles, which fill the rest of the block's 227 KB at D = 128: barriers, 2 words, the rows'
-  // exchange.  Dynamic shared memory starts on a 1024-byte boundary where a kernel has no static one.
-  static constexpr uint32_t kRow = 512, kTiles = 3072, kKV = 2 * kT, kBytes = kTiles + kKV + kSlots * kT;
+  static constexpr int kSlots = D == 128 ? 2 : 5;              // ring of K and V tiles in turn
+  static constexpr uint32_t kKV = kT, kBars = kKV + kSlots * kT, kBytes = kBars + 256 + 1024;
 };
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kAttnThreads, 1)
+__global__ void __launch_bounds__(kFwdThreads, 2)
 attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const AttnParams p) {
   extern __shared__ unsigned char smem_dyn[];
   using L = AttnFwdSmem<D>;
-  if ((smem_addr(smem_dyn) & 1023u) != 0) {      // the layout's premise; the whole block agrees
-    if (threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
-    return;
-  }
-  unsigned char* smem = smem_dyn + L::kTiles;
-  uint64_t* q_full = reinterpret_cast<uint64_t*>(smem_dyn);
+  unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
+  uint64_t* q_full = reinterpret_cast<uint64_t*>(smem + L::kBars);
   uint64_t* kv_full = q_full + 1;                // [kSlots]
   uint64_t* kv_free = kv_full + L::kSlots;       // [kSlots]
-  uint64_t* s_full = kv_free + L::kSlots;        // [2]
-  uint64_t* p_full = s_full + 2;                 // [2]
-  uint64_t* o_full = p_full + 2;                 // [2]
-  uint64_t* pair = o_full + 2;                   // [8] the two warps of a query tile's 32 rows
-  uint64_t* drain = pair + 8;
-  static_assert((1 + 2 * L::kSlots + 6 + 8 + 1) * 8 + 8 <= L::kRow && L::kRow + 2 * 2 * kAttnTile * 4 <= L::kTiles, "what lies in front of the tiles");
-  uint32_t& s_tmem = *reinterpret_cast<uint32_t*>(drain + 1);
-  volatile int& s_abort = *reinterpret_cast<volatile int*>(&s_tmem + 1);
-  float* s_row = reinterpret_cast<float*>(smem_dyn + L::kRow);       // [half][row]
+  uint64_t* s_full = kv_free + L::kSlots;
+  uint64_t* p_full = s_full + 1;                 // [2] the even and the odd 32 keys of either half
+  uint64_t* o_full = p_full + 2;
+  uint64_t* pair = o_full + 1;                   // [4] the two warps of 32 rows
+  uint64_t* drain = pair + 4;
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_abort;
+  __shared__ float s_row[2][kAttnTile];          // [half][row]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int head = blockIdx.y, batch = blockIdx.z;
-  const int blk = gridDim.x - 1 - blockIdx.x;    // with a causal mask the last queries have the most keys: first
-  const int q0 = blk * 2 * kAttnTile;
+  const int q0 = (gridDim.x - 1 - blockIdx.x) * kAttnTile;     // with a causal mask the last queries have the most keys: first
 
   if (threadIdx.x == 0) {
     mbar_init(q_full, 1);
     for (int s = 0; s < L::kSlots; ++s) { mbar_init(&kv_full[s], 1); mbar_init(&kv_free[s], 1); }
-    for (int t = 0; t < 2; ++t) { mbar_init(&s_full[t], 1); mbar_init(&p_full[t], 8); mbar_init(&o_full[t], 1); }
-    for (int t = 0; t < 8; ++t) mbar_init(&pair[t], 2);
+    mbar_init(s_full, 1);
+    mbar_init(&p_full[0], 8);
+    mbar_init(&p_full[1], 8);
+    mbar_init(o_full, 1);
+    for (int t = 0; t < 4; ++t) mbar_init(&pair[t], 2);
     mbar_init(drain, 1);
     s_abort = 0;
     mbar_init_fence();
     fence_proxy_async_smem();
   }
-  if (warp == kAttnMmaWarp) tmem_alloc(&s_tmem, 512);
+  if (warp == 9) tmem_alloc(&s_tmem, 256);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = s_tmem;
+  const uint32_t t_s = s_tmem, t_o = t_s + 128;
   const int kv_len = attn_kv_len(p, batch);
   const int off = p.Sk - p.Sq;
-  const int q_last = min(q0 + 2 * kAttnTile, p.Sq) - 1;
+  const int q_last = min(q0 + kAttnTile, p.Sq) - 1;
   const int seen = p.causal ? min(kv_len, max(0, q_last + off + 1)) : kv_len;     // keys that any query of the block sees
   const int tiles = (seen + kAttnTile - 1) / kAttnTile;
 
-  if (tiles > 0 && warp == kAttnCopyWarp) {
+  if (tiles > 0 && warp == 8) {
     if (lane == 0) {
-      mbar_expect_tx(q_full, 2 * L::kT);
-      for (int t = 0; t < 2; ++t) attn_load_tile<D>(smem + t * L::kT, &mq, q_full, q0 + t * kAttnTile, head, batch);
+      mbar_expect_tx(q_full, L::kT);
+      attn_load_tile<D>(smem, &mq, q_full, q0, head, batch);
       const int kv_head = head / (p.Hq / p.Hkv);
       int slot = 0, issued = 0;
       uint32_t parity = 1;
@@ -224,7 +232,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
         for (int s = 0; s < L::kSlots && s < issued; ++s) mbar_wait_bounded(&kv_full[s], ((issued - 1 - s) / L::kSlots) & 1);
       }
     }
-  } else if (tiles > 0 && warp == kAttnMmaWarp) {
+  } else if (tiles > 0 && warp == 9) {
     const bool issuer = elect_one();
     int slot = 0;
     uint32_t parity = 0;
@@ -236,80 +244,69 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       if (ok && valid < kAttnTile) attn_zero_rows<D>(smem + L::kKV + slot * L::kT, valid);
       return smem_addr(smem) + L::kKV + slot * L::kT;
     };
-    auto wait_p = [&](int t, int j) {
-      ok = ok && !s_abort && mbar_wait_bounded(&p_full[t], j & 1);
-      ok = __all_sync(0xffffffffu, ok);
-      tc_fence_after();
-    };
     auto advance = [&]() { if (++slot == L::kSlots) { slot = 0; parity ^= 1u; } };
     const uint64_t q_desc = AttnDesc<D>::rows(smem_addr(smem));
-    uint64_t k_desc = AttnDesc<D>::rows(take(kAttnTile));
-    tc_fence_after();
-    if (ok && issuer) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        attn_mma_rows<D, BF16>(tmem + t * 128, q_desc + t * (L::kT >> 4), k_desc);
-        mma_commit(&s_full[t]);
+    for (int j = 0; j < tiles; ++j) {
+      // S(j) takes the place of P(j - 1), which the product before it has read
+      const uint64_t k_desc = AttnDesc<D>::rows(take(kAttnTile));
+      tc_fence_after();
+      if (ok && issuer) {
+        attn_mma_rows<D, BF16>(t_s, q_desc, k_desc);
+        mma_commit(s_full);
+        mma_commit(&kv_free[slot]);
       }
-      mma_commit(&kv_free[slot]);
-    }
-    __syncwarp();
-    advance();
-    for (int j = 0; ok && j < tiles; ++j) {
-      const int v_slot = slot;
-      const uint64_t v_desc = AttnDesc<D>::tokens(take(min(kv_len - j * kAttnTile, kAttnTile)));
+      __syncwarp();
       advance();
-      const int k_slot = slot;
-      const bool more = j + 1 < tiles;
-      if (ok && more) { k_desc = AttnDesc<D>::rows(take(kAttnTile)); advance(); }
+      const uint64_t v_desc = AttnDesc<D>::tokens(take(min(kv_len - j * kAttnTile, kAttnTile)));
+      // the product over the even 32 keys of either half runs beside the exponentials of the odd ones
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (ok) wait_p(t, j);
+      for (int c = 0; c < 2; ++c) {
+        ok = ok && !s_abort && mbar_wait_bounded(&p_full[c], j & 1);
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after();
         if (ok && issuer) {
-          attn_mma_tokens<D, BF16>(tmem + 256 + t * 128, tmem + t * 128, v_desc, j != 0);
-          if (more) {
-            attn_mma_rows<D, BF16>(tmem + t * 128, q_desc + t * (L::kT >> 4), k_desc);
-            mma_commit(&s_full[t]);
-          } else {
-            mma_commit(&o_full[t]);
-          }
-          if (t == 1) {
-            mma_commit(&kv_free[v_slot]);
-            if (more) mma_commit(&kv_free[k_slot]);
-          }
+          attn_mma_some_tokens<D, BF16>(t_o, t_s, v_desc, 2 * c, j != 0 || c != 0);
+          attn_mma_some_tokens<D, BF16>(t_o, t_s, v_desc, 4 + 2 * c, true);
         }
         __syncwarp();
       }
+      if (!ok) break;
+      if (issuer) {
+        mma_commit(&kv_free[slot]);
+        if (j == tiles - 1) mma_commit(o_full);
+      }
+      __syncwarp();
+      advance();
     }
     if (!ok) {
       s_abort = 1;
       if (issuer) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
     }
-  } else if (warp < 16) {
-    const int t = warp >> 3, half = (warp >> 2) & 1;             // this warp's query tile and its 64 keys of each key tile
-    const int lrow = t * kAttnTile + (warp & 3) * 32 + lane, row = q0 + lrow;
+  } else if (warp < 8) {
+    const int half = warp >> 2;                  // this warp's 64 keys of each tile
+    const int lrow = (warp & 3) * 32 + lane, row = q0 + lrow;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const uint32_t s_at = tmem + t * 128 + half * 64 + lanes, o_at = tmem + 256 + t * 128 + lanes;
+    const uint32_t s_at = t_s + half * 64 + lanes, o_at = t_o + lanes;
     const int limit = p.causal ? min(kv_len, row + off + 1) : kv_len;        // this query's keys: [0, limit)
     const int warp_limit = p.causal ? min(kv_len, row - lane + off + 1) : kv_len;   // all of the warp's queries see these
-    uint64_t* both = &pair[t * 4 + (warp & 3)];
+    uint64_t* both = &pair[warp & 3];
     uint32_t turn = 0;
     bool ok = true;
     // The other half's value for this row.  The next exchange comes after the products that both warps' P go
     // into, so a place is never written before it has been read.
     auto exchange = [&](float mine) {
-      s_row[half * 2 * kAttnTile + lrow] = mine;
+      s_row[half][lrow] = mine;
       __syncwarp();
       if (lane == 0) mbar_arrive_one(both);
       ok = ok && !s_abort && mbar_wait_bounded(both, turn);
       ok = __all_sync(0xffffffffu, ok);
       turn ^= 1u;
-      return s_row[(half ^ 1) * 2 * kAttnTile + lrow];
+      return s_row[half ^ 1][lrow];
     };
     float top = -INFINITY, sum = 0.f;            // running maximum of scale_log2 S, this half's sum under it
     const float2 scale2 = make_float2(p.scale_log2, p.scale_log2);
     for (int j = 0; ok && j < tiles; ++j) {
-      ok = !s_abort && mbar_wait_bounded(&s_full[t], j & 1);
+      ok = !s_abort && mbar_wait_bounded(s_full, j & 1);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
@@ -326,14 +323,14 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
             if (k0 + c * 32 + e >= limit) s[e] = 0xff800000u;
         }
       };
-      float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      float m[2] = {-INFINITY, -INFINITY};
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         fetch(c);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) m[e & 3] = fmaxf(m[e & 3], __uint_as_float(s[e]));
+        for (int e = 0; e < 32; e += 2) m[(e >> 1) & 1] = max3(m[(e >> 1) & 1], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
       }
-      float tile_top = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3]));
+      float tile_top = fmaxf(m[0], m[1]);
       tile_top = fmaxf(tile_top, exchange(tile_top)) * p.scale_log2;
       if (!ok) break;
       const bool raise = tile_top > top + 8.f;   // also the first time a row sees a key
@@ -370,17 +367,17 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
           w[e] = pack16<BF16>(x.x, x.y);
         }
         tmem_st16(s_at + c * 32, w);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_one(&p_full[c]);
       }
       part[0] = add2(part[0], part[1]);
       sum += part[0].x + part[0].y;
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_one(&p_full[t]);
     }
     const bool live = row < p.Sq;
     if (ok && tiles > 0) {
-      ok = !s_abort && mbar_wait_bounded(&o_full[t], 0);
+      ok = !s_abort && mbar_wait_bounded(o_full, 0);
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
       sum += exchange(sum);
@@ -395,9 +392,9 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
   tc_fence_before();
   __syncthreads();
   if (s_abort && threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
-  if (warp == kAttnMmaWarp) {
+  if (warp == 9) {
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(t_s, 256);
   }
 }
 
