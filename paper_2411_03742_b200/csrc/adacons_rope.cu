@@ -20,6 +20,15 @@ struct adacons_rope {
 
 namespace {
 
+RopeDivisor divisor(int64_t d) {
+  RopeDivisor r;
+  r.d = static_cast<int>(d);
+  r.s = 0;
+  while ((1ll << r.s) < d) ++r.s;
+  r.m = static_cast<unsigned>(((1ull << (31 + r.s)) + static_cast<unsigned long long>(d) - 1) / static_cast<unsigned long long>(d));
+  return r;
+}
+
 template <int DT, bool IL>
 bool launch_rope(const RopeParams& p, bool vec, unsigned blocks, cudaStream_t st) {
   return vec ? launch(&rope_kernel<DT, IL, true>, dim3(blocks), dim3(kRopeThreads), 0, st, kLaunchPlain, 1, p)
@@ -99,7 +108,12 @@ int adacons_rope_apply(adacons_rope* c, const adacons_rope_shape* s, const void*
   int64_t tpb = std::max<int64_t>(1, (4 * kRopeThreads + per_token - 1) / std::max<int64_t>(1, per_token));
   tpb = std::min<int64_t>(tpb, std::max<int64_t>(1, p.tokens / (4 * c->sms)));
   tpb = std::min<int64_t>(tpb, std::max(1, kRopeMaxTable / (p.rot / 2)));
+  tpb = std::min<int64_t>(tpb, kRopeMaxTokens);
   p.tokens_per_block = static_cast<int>(tpb);
+  // as the kernel counts them
+  const int64_t rest = x == y ? 0 : (p.dim - p.rot) / (vec ? n : 1), per_head = p.rot / 2 / (vec ? n : 1) + (vec ? (rest + 1) / 2 : rest);
+  p.per_head = divisor(per_head);
+  p.per_token = divisor(per_head * p.heads);
   const int64_t blocks = (p.tokens + tpb - 1) / tpb;
   if (blocks > 0x7fffffff) return ADACONS_ELIMIT;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

@@ -18,6 +18,14 @@ namespace adacons {
 // ----------------------------------------------------------------------------------------------
 constexpr int kRopeThreads = 256;
 constexpr int kRopeMaxTable = 2048;            // (cos, sin) pairs in a block's table
+constexpr int kRopeMaxTokens = 64;             // of a block
+
+// n / d for 0 <= n < 2^31 by a multiplication: m = ceil(2^(31 + s) / d) with s = ceil(log2 d)
+struct RopeDivisor {
+  unsigned m;
+  int s, d;
+  __device__ __forceinline__ int divide(int n) const { return static_cast<int>((static_cast<unsigned long long>(static_cast<unsigned>(n)) * m) >> (31 + s)); }
+};
 
 struct RopeParams {
   const void* x;
@@ -31,6 +39,7 @@ struct RopeParams {
   float gain;
   int inverse;
   int tokens_per_block;
+  RopeDivisor per_token, per_head;       // work items
 };
 
 template <int DT> struct RopeVec;
@@ -57,11 +66,12 @@ template <int DT> __device__ __forceinline__ void rope_put(void* p, long long i,
   else static_cast<unsigned short*>(p)[i] = static_cast<unsigned short>(pack_bf16x2_rn(v, 0.f) & 0xffffu);
 }
 
-// Work items of one (token, head).  VEC: rotated pairs in groups of kN (two 16-byte vectors), then the rest in
-// groups of one vector; otherwise one pair, then one element, at a time.
+// Work items of one (token, head).  VEC: rotated pairs in groups of kN (two 16-byte vectors), then the rest two
+// vectors at a time; otherwise one pair, then one element.
 template <int DT, bool INTERLEAVED, bool VEC>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) {
   __shared__ float2 table[kRopeMaxTable];
+  __shared__ long long s_x[kRopeMaxTokens], s_y[kRopeMaxTokens];       // where the tokens start, in elements
   using V = RopeVec<DT>;
   constexpr int N = VEC ? V::kN : 1;
   const int pairs = p.rot / 2;
@@ -77,55 +87,68 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p) 
     sincospif(static_cast<float>(2.0 * turn), &s, &c);
     table[k] = make_float2(c * p.gain, (p.inverse ? -s : s) * p.gain);
   }
+  if (threadIdx.x < count) {
+    const long long t = t0 + threadIdx.x, b = t / p.seq, sq = t - b * p.seq;
+    s_x[threadIdx.x] = b * p.xb + sq * p.xs;
+    s_y[threadIdx.x] = b * p.yb + sq * p.ys;
+  }
   __syncthreads();
-  const int turned = pairs / N, still = (p.dim - p.rot) / N, per_head = turned + still, per_token = per_head * p.heads;
+  // in place, what is not turned is where it belongs
+  const int rest = p.x == p.y ? 0 : (p.dim - p.rot) / N, turned = pairs / N, per_head = turned + (VEC ? (rest + 1) / 2 : rest), per_token = per_head * p.heads;
   const int work = count * per_token;
-#pragma unroll 2
+  constexpr int kElem = DT == 0 ? 4 : 2;
+#pragma unroll 4
   for (int k = threadIdx.x; k < work; k += kRopeThreads) {
-    const int tok = k / per_token, in_token = k - tok * per_token;
-    const int head = in_token / per_head, item = in_token - head * per_head;
-    const long long t = t0 + tok, b = t / p.seq, s = t - b * p.seq;
-    const long long xi = b * p.xb + s * p.xs + head * p.xh, yi = b * p.yb + s * p.ys + head * p.yh;
-    const int elem = DT == 0 ? 4 : 2;
-    const char* x = static_cast<const char*>(p.x) + xi * elem;
-    char* y = static_cast<char*>(p.y) + yi * elem;
-    if (item >= turned) {
-      const int e = p.rot + (item - turned) * N;
-      if (VEC) *reinterpret_cast<uint4*>(y + e * elem) = ld_nc_v4(x + e * elem);
-      else rope_put<DT>(y, e, rope_get<DT>(x, e));
-      continue;
-    }
+    const int tok = p.per_token.divide(k), in_token = k - tok * per_token;
+    const int head = p.per_head.divide(in_token), item = in_token - head * per_head;
+    const char* x = static_cast<const char*>(p.x) + (s_x[tok] + head * p.xh) * kElem;
+    char* y = static_cast<char*>(p.y) + (s_y[tok] + head * p.yh) * kElem;
     const float2* cs = table + tok * pairs + item * N;
+    const bool turn = item < turned;
     if (!VEC) {
+      if (!turn) {
+        const int e = p.rot + item - turned;
+        rope_put<DT>(y, e, rope_get<DT>(x, e));
+        continue;
+      }
       const int ia = INTERLEAVED ? 2 * item : item, ib = INTERLEAVED ? 2 * item + 1 : item + pairs;
       const float a = rope_get<DT>(x, ia), q = rope_get<DT>(x, ib);
       rope_put<DT>(y, ia, a * cs[0].x - q * cs[0].y);
       rope_put<DT>(y, ib, a * cs[0].y + q * cs[0].x);
       continue;
     }
-    const int ea = INTERLEAVED ? 2 * item * N : item * N, eb = INTERLEAVED ? ea + N : ea + pairs;
-    float u[V::kN], w[V::kN], ou[V::kN], ow[V::kN];
-    V::unpack(*reinterpret_cast<const uint4*>(x + ea * elem), u);
-    V::unpack(*reinterpret_cast<const uint4*>(x + eb * elem), w);
-    if (INTERLEAVED) {
+    // two vectors either way, so that turned and untouched items of a warp load and store together
+    const int ea = turn ? (INTERLEAVED ? 2 * item * N : item * N) : p.rot + 2 * (item - turned) * N;
+    const int eb = turn && !INTERLEAVED ? ea + pairs : ea + N;
+    const bool two = turn || 2 * (item - turned) + 1 < rest;
+    uint4 va = *reinterpret_cast<const uint4*>(x + ea * kElem), vb = make_uint4(0u, 0u, 0u, 0u);
+    if (two) vb = *reinterpret_cast<const uint4*>(x + eb * kElem);
+    if (turn) {
+      float u[V::kN], w[V::kN], ou[V::kN], ow[V::kN];
+      V::unpack(va, u);
+      V::unpack(vb, w);
+      if (INTERLEAVED) {
 #pragma unroll
-      for (int e = 0; e < V::kN; e += 2) {
-        const float2 c0 = cs[e / 2], c1 = cs[V::kN / 2 + e / 2];
-        ou[e] = u[e] * c0.x - u[e + 1] * c0.y;
-        ou[e + 1] = u[e] * c0.y + u[e + 1] * c0.x;
-        ow[e] = w[e] * c1.x - w[e + 1] * c1.y;
-        ow[e + 1] = w[e] * c1.y + w[e + 1] * c1.x;
-      }
-    } else {
+        for (int e = 0; e < V::kN; e += 2) {
+          const float2 c0 = cs[e / 2], c1 = cs[V::kN / 2 + e / 2];
+          ou[e] = u[e] * c0.x - u[e + 1] * c0.y;
+          ou[e + 1] = u[e] * c0.y + u[e + 1] * c0.x;
+          ow[e] = w[e] * c1.x - w[e + 1] * c1.y;
+          ow[e + 1] = w[e] * c1.y + w[e + 1] * c1.x;
+        }
+      } else {
 #pragma unroll
-      for (int e = 0; e < V::kN; ++e) {
-        const float2 c0 = cs[e];
-        ou[e] = u[e] * c0.x - w[e] * c0.y;
-        ow[e] = u[e] * c0.y + w[e] * c0.x;
+        for (int e = 0; e < V::kN; ++e) {
+          const float2 c0 = cs[e];
+          ou[e] = u[e] * c0.x - w[e] * c0.y;
+          ow[e] = u[e] * c0.y + w[e] * c0.x;
+        }
       }
+      va = V::pack(ou);
+      vb = V::pack(ow);
     }
-    *reinterpret_cast<uint4*>(y + ea * elem) = V::pack(ou);
-    *reinterpret_cast<uint4*>(y + eb * elem) = V::pack(ow);
+    *reinterpret_cast<uint4*>(y + ea * kElem) = va;
+    if (two) *reinterpret_cast<uint4*>(y + eb * kElem) = vb;
   }
 }
 
