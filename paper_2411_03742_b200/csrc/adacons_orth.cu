@@ -127,7 +127,7 @@ OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int c
     const unsigned per_step = products[3 * open.mat + 2].before + products[3 * open.mat + 2].stored;
     plan.lists[who.second].push_back({open.mat, spot.i, spot.j, pr.depth, m.r, open.kind == kOrthApply ? m.l : m.r, open.step * per_step + pr.before,
                                       open.step * 4 + open.kind});
-    who.first += pr.busy;
+    who.first = std::max(who.first, open.at) + pr.busy;      // idle since before the product could start
     open.end = std::max(open.end, who.first + pr.after);
     std::push_heap(idle.begin(), idle.end(), std::greater<Free>());
     if (open.next == pr.spots.size()) {
