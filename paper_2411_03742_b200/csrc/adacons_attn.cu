@@ -29,7 +29,7 @@ bool raise(K kernel, uint32_t bytes) {
 }
 template <int D, bool BF16>
 bool raise_all() {
-  static_assert(AttnFwdSmem<D>::kBytes <= 112 * 1024 && attn_backward_smem<D>() <= 227 * 1024, "shared memory of a block");
+  static_assert(AttnFwdSmem<D>::kBytes <= 112 * 1024 && attn_backward_smem<D>() <= (AttnBwd<D>::kBlocks == 2 ? 112 : 227) * 1024, "shared memory of a block");
   return raise(attn_forward_kernel<D, BF16>, AttnFwdSmem<D>::kBytes) && raise(attn_backward_kernel<D, BF16>, attn_backward_smem<D>());
 }
 
@@ -84,7 +84,7 @@ int check_tensor(const adacons_attn_tensor* t, int batch, int len, int heads) {
   return ADACONS_OK;
 }
 
-bool make_map(const AttnDevice& d, CUtensorMap* map, const adacons_attn_shape* s, const adacons_attn_tensor* t, int len, int heads, const void* spare) {
+bool make_map(const AttnDevice& d, CUtensorMap* map, const adacons_attn_shape* s, const adacons_attn_tensor* t, int len, int heads, const void* spare, int rows) {
   // a tensor without tokens is never read, but its map has to exist
   const void* base = len > 0 ? t->data : spare;
   const cuuint64_t dims[4] = {static_cast<cuuint64_t>(s->head_dim), static_cast<cuuint64_t>(len > 0 ? len : 1), static_cast<cuuint64_t>(heads),
@@ -92,7 +92,7 @@ bool make_map(const AttnDevice& d, CUtensorMap* map, const adacons_attn_shape* s
   const cuuint64_t one = static_cast<cuuint64_t>(s->head_dim) * 2;
   const cuuint64_t strides[3] = {len > 1 ? static_cast<cuuint64_t>(t->seq_stride) * 2 : one, heads > 1 && len > 0 ? static_cast<cuuint64_t>(t->head_stride) * 2 : one,
                                  s->batch > 1 && len > 0 ? static_cast<cuuint64_t>(t->batch_stride) * 2 : one};
-  const cuuint32_t box[4] = {64, kAttnTile, 1, 1};
+  const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(rows), 1, 1};
   return encode_map(d.info, map, s->dtype == ADACONS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides, box);
 }
 
@@ -135,7 +135,7 @@ bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMa
   p.dv = dv;
   const int64_t q_tiles = p.sq_pad / kAttnTile, k_tiles = (static_cast<int64_t>(p.Sk) + kAttnTile - 1) / kAttnTile;
   const int64_t key_blocks = k_tiles * p.Hkv * p.B, blocks = key_blocks + q_tiles * p.Hq * p.B;
-  return blocks <= 0x7fffffff && launch(&attn_backward_kernel<D, BF16>, dim3(static_cast<unsigned>(blocks)), dim3(kAttnThreads), attn_backward_smem<D>(), st, kLaunchOverlap, 1,
+  return blocks <= 0x7fffffff && launch(&attn_backward_kernel<D, BF16>, dim3(static_cast<unsigned>(blocks)), dim3(AttnBwd<D>::kThreads), attn_backward_smem<D>(), st, kLaunchOverlap, 1,
                                         mq, mk, mv, mdo, p, static_cast<int>(key_blocks), static_cast<int>(q_tiles));
 }
 
@@ -160,8 +160,8 @@ int adacons_attn_forward(const adacons_attn_shape* s, const adacons_attn_tensor*
   AttnDevice* d = nullptr;
   if ((rc = attn_device(&d)) != ADACONS_OK) return rc;
   CUtensorMap mq, mk, mv;
-  if (!make_map(*d, &mq, s, q, s->q_len, s->q_heads, q->data) || !make_map(*d, &mk, s, k, s->kv_len, s->kv_heads, q->data) ||
-      !make_map(*d, &mv, s, v, s->kv_len, s->kv_heads, q->data))
+  if (!make_map(*d, &mq, s, q, s->q_len, s->q_heads, q->data, kAttnTile) || !make_map(*d, &mk, s, k, s->kv_len, s->kv_heads, q->data, kAttnTile) ||
+      !make_map(*d, &mv, s, v, s->kv_len, s->kv_heads, q->data, kAttnTile))
     return ADACONS_ECUDA;
   AttnParams p = base_params(*d, s);
   p.out = as_out(out);
@@ -197,9 +197,10 @@ int adacons_attn_backward(const adacons_attn_shape* s, const adacons_attn_tensor
   AttnDevice* d = nullptr;
   if ((rc = attn_device(&d)) != ADACONS_OK) return rc;
   const void* spare = s->q_len > 0 ? q->data : k->data;
+  const int rows = s->head_dim <= 64 ? AttnBwd<64>::kTok : AttnBwd<128>::kTok;
   CUtensorMap mq, mk, mv, mdo;
-  if (!make_map(*d, &mq, s, q, s->q_len, s->q_heads, spare) || !make_map(*d, &mk, s, k, s->kv_len, s->kv_heads, spare) ||
-      !make_map(*d, &mv, s, v, s->kv_len, s->kv_heads, spare) || !make_map(*d, &mdo, s, dout, s->q_len, s->q_heads, spare))
+  if (!make_map(*d, &mq, s, q, s->q_len, s->q_heads, spare, rows) || !make_map(*d, &mk, s, k, s->kv_len, s->kv_heads, spare, rows) ||
+      !make_map(*d, &mv, s, v, s->kv_len, s->kv_heads, spare, rows) || !make_map(*d, &mdo, s, dout, s->q_len, s->q_heads, spare, rows))
     return ADACONS_ECUDA;
   const AttnParams p = base_params(*d, s);
   float* lse2 = static_cast<float*>(workspace);

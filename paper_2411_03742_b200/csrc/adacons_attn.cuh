@@ -26,8 +26,6 @@ namespace adacons {
 // inputs' 16-bit type as operands of the second products, an error of the size of the results' own rounding.
 // ----------------------------------------------------------------------------------------------
 constexpr int kAttnTile = 128;
-constexpr int kAttnThreads = 576;                // warps 0-15 elementwise, 16 copies, 17 products
-constexpr int kAttnCopyWarp = 16, kAttnMmaWarp = 17;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttnOut { void* p; long long batch, seq, head; };     // element strides
@@ -77,11 +75,11 @@ __device__ __forceinline__ void attn_load_tile(unsigned char* dst, const CUtenso
 #pragma unroll
   for (int h = 0; h < D / 64; ++h) tma_load_4d(dst + h * AttnTile<D>::kBlock, map, bar, h * 64, row, head, batch);
 }
-// rows [first, 128) of a tile become zero; called by one warp, before the tile is an operand
-template <int D>
+// rows [first, ROWS) of a tile become zero; called by one warp, before the tile is an operand
+template <int D, int ROWS>
 __device__ __forceinline__ void attn_zero_rows(unsigned char* tile, int first) {
   const int lane = threadIdx.x & 31;
-  for (int k = lane; k < (kAttnTile - first) * 8; k += 32)
+  for (int k = lane; k < (ROWS - first) * 8; k += 32)
 #pragma unroll
     for (int h = 0; h < D / 64; ++h) *reinterpret_cast<uint4*>(tile + h * AttnTile<D>::kBlock + first * 128 + k * 16) = make_uint4(0u, 0u, 0u, 0u);
   fence_proxy_async_smem();
@@ -94,10 +92,10 @@ template <int D> struct AttnDesc {
   static __device__ __forceinline__ uint64_t rows(uint32_t addr) { return desc_kmajor(0) + (addr >> 4); }                                  // product over head elements
   static __device__ __forceinline__ uint64_t tokens(uint32_t addr) { return desc_mnmajor(0, AttnTile<D>::kBlock) + (addr >> 4); }          // product over tokens
 };
-// 128 x 128 product over head elements: rows of `a` with rows of `b`
-template <int D, bool BF16>
+// 128 x N product over head elements: rows of `a` with rows of `b`
+template <int D, bool BF16, int N>
 __device__ __forceinline__ void attn_mma_rows(uint32_t d, uint64_t a, uint64_t b) {
-  constexpr uint32_t idesc = mma_idesc(kAttnTile, kAttnTile, BF16, false, false);
+  constexpr uint32_t idesc = mma_idesc(kAttnTile, N, BF16, false, false);
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) {
     const uint32_t off = ((k / 4) * AttnTile<D>::kBlock + (k % 4) * 32) >> 4;
@@ -106,17 +104,17 @@ __device__ __forceinline__ void attn_mma_rows(uint32_t d, uint64_t a, uint64_t b
 }
 // 128 x D product over tokens: 16-bit values in tensor memory with the tokens of `b`.  Whoever had columns
 // 32 g .. 32 g + 31 of the fp32 scores puts their 16 words of 16-bit values in the first half of that place.
-// 32 tokens: k and k + 1 of the eight groups of 16.
+// 32 tokens: k and k + 1 of the groups of 16.
 template <int D, bool BF16>
 __device__ __forceinline__ void attn_mma_some_tokens(uint32_t d, uint32_t a, uint64_t b, int k, bool accumulate) {
   constexpr uint32_t idesc = mma_idesc(kAttnTile, D, BF16, false, true);
 #pragma unroll
   for (int e = 0; e < 2; ++e) mma_ts(d, a + (k / 2) * 32 + e * 8, b + (k + e) * (2048 >> 4), idesc, e != 0 ? 1u : accumulate);
 }
-template <int D, bool BF16>
+template <int D, bool BF16, int TOKENS>
 __device__ __forceinline__ void attn_mma_tokens(uint32_t d, uint32_t a, uint64_t b, bool accumulate) {
 #pragma unroll
-  for (int k = 0; k < 8; k += 2) attn_mma_some_tokens<D, BF16>(d, a, b, k, accumulate || k != 0);
+  for (int k = 0; k < TOKENS / 16; k += 2) attn_mma_some_tokens<D, BF16>(d, a, b, k, accumulate || k != 0);
 }
 
 // Columns [first, first + 32 BLOCKS) of row `row` of an accumulator (this thread's lane), times `mul`, to global memory.
@@ -241,7 +239,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     auto take = [&](int valid) -> uint32_t {
       ok = ok && !s_abort && mbar_wait_bounded(&kv_full[slot], parity);
       ok = __all_sync(0xffffffffu, ok);
-      if (ok && valid < kAttnTile) attn_zero_rows<D>(smem + L::kKV + slot * L::kT, valid);
+      if (ok && valid < kAttnTile) attn_zero_rows<D, kAttnTile>(smem + L::kKV + slot * L::kT, valid);
       return smem_addr(smem) + L::kKV + slot * L::kT;
     };
     auto advance = [&]() { if (++slot == L::kSlots) { slot = 0; parity ^= 1u; } };
@@ -251,7 +249,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       const uint64_t k_desc = AttnDesc<D>::rows(take(kAttnTile));
       tc_fence_after();
       if (ok && issuer) {
-        attn_mma_rows<D, BF16>(t_s, q_desc, k_desc);
+        attn_mma_rows<D, BF16, kAttnTile>(t_s, q_desc, k_desc);
         mma_commit(s_full);
         mma_commit(&kv_free[slot]);
       }
@@ -444,12 +442,28 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnRows dout, co
 //     dS(i) from P, dP(i)  | dV(i), S(i+1)
 // Four warps share a block of 32 keys, 32 queries each.
 // ----------------------------------------------------------------------------------------------
+// The streamed tiles (queries here, keys below) are 128 tokens at D = 128.  At D = 64 they are 64: tensor memory
+// then holds two blocks an SM (256 columns each), which overlap where a block is short or waits for its own chain;
+// with 128 tokens and one block the encoder shape (512 tokens, 64 elements) took 72 us.
+template <int D> struct AttnBwd {
+  static constexpr int kTok = D == 128 ? 128 : 64;               // tokens of a streamed tile
+  static constexpr int kParts = kTok / 32, kElem = 4 * kParts;   // elementwise warps: 32 rows x 32 columns each
+  static constexpr int kCopyWarp = kElem, kMmaWarp = kElem + 1, kThreads = kElem * 32 + 64, kBlocks = D == 128 ? 1 : 2;
+  static constexpr uint32_t kTmem = 2 * kTok + 2 * D;
+  static constexpr uint32_t kRes = AttnTile<D>::kBytes, kStr = kRes * kTok / 128;      // bytes of a resident, a streamed tile
+  // the box of the tensor maps is one streamed tile's rows
+  static __device__ __forceinline__ void load_resident(unsigned char* dst, const CUtensorMap* map, uint64_t* bar, int row, int head, int batch) {
+#pragma unroll
+    for (int h = 0; h < 128 / kTok; ++h) attn_load_tile<D>(dst + h * kStr, map, bar, row + h * kTok, head, batch);
+  }
+};
 template <int D> struct AttnDkvSmem {
-  static constexpr uint32_t kT = AttnTile<D>::kBytes;
+  using G = AttnBwd<D>;
   static constexpr int kStages = D == 128 ? 2 : 4;
-  static constexpr uint32_t kRing = 2 * kT, kStage = 2 * kT;                    // K, V | (Q, dO) per stage
-  static constexpr uint32_t kStats = kRing + kStages * kStage;                  // lse2, delta: 2 x 512 bytes per stage
-  static constexpr uint32_t kBars = kStats + kStages * 1024, kBytes = kBars + 256 + 1024;
+  static constexpr uint32_t kRing = 2 * G::kRes, kStage = 2 * G::kStr;          // K, V | (Q, dO) per stage
+  static constexpr uint32_t kStat = G::kTok * 4;                                // lse2, delta: bytes per stage of each
+  static constexpr uint32_t kStats = kRing + kStages * kStage;
+  static constexpr uint32_t kBars = kStats + kStages * 2 * kStat, kBytes = kBars + 256 + 1024;
 };
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
@@ -461,6 +475,7 @@ template <int D, bool BF16>
 __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo,
                                                const AttnParams& p, const int tile, const int kv_head, const int batch) {
   using L = AttnDkvSmem<D>;
+  using G = AttnBwd<D>;
   uint64_t* kv_full = reinterpret_cast<uint64_t*>(smem + L::kBars);
   uint64_t* full = kv_full + 1;                  // [kStages]
   uint64_t* free_ = full + L::kStages;           // [kStages]
@@ -480,48 +495,48 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
     mbar_init(kv_full, 1);
     for (int s = 0; s < L::kStages; ++s) { mbar_init(&full[s], 1); mbar_init(&free_[s], 1); }
     mbar_init(s_full, 1);
-    mbar_init(p_full, 16);
+    mbar_init(p_full, G::kElem);
     mbar_init(dp_full, 1);
-    mbar_init(ds_full, 16);
+    mbar_init(ds_full, G::kElem);
     mbar_init(done, 1);
     mbar_init(drain, 1);
     s_abort = 0;
     mbar_init_fence();
     fence_proxy_async_smem();
   }
-  if (warp == kAttnMmaWarp) tmem_alloc(&s_tmem, 512);
+  if (warp == G::kMmaWarp) tmem_alloc(&s_tmem, G::kTmem);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
-  const uint32_t t_s = tmem, t_dp = tmem + 128, t_dv = tmem + 256, t_dk = tmem + 384;
+  const uint32_t t_s = tmem, t_dp = tmem + G::kTok, t_dv = tmem + 2 * G::kTok, t_dk = t_dv + D;
   const int kv_len = attn_kv_len(p, batch);
   const int off = p.Sk - p.Sq;
-  const int q_tiles = (p.Sq + kAttnTile - 1) / kAttnTile;
+  const int q_tiles = (p.Sq + G::kTok - 1) / G::kTok;
   // the first query that sees any of these keys: i >= k0 - off
-  const int first = p.causal ? min(q_tiles, max(0, k0 - off) / kAttnTile) : 0;
+  const int first = p.causal ? min(q_tiles, max(0, k0 - off) / G::kTok) : 0;
   const int per_head = k0 < kv_len ? q_tiles - first : 0;
   const int items = group * per_head;
   pdl_wait();                                    // the statistics
 
-  if (items > 0 && warp == kAttnCopyWarp) {
+  if (items > 0 && warp == G::kCopyWarp) {
     if (lane == 0) {
-      mbar_expect_tx(kv_full, 2 * L::kT);
-      attn_load_tile<D>(smem, &mk, kv_full, k0, kv_head, batch);
-      attn_load_tile<D>(smem + L::kT, &mv, kv_full, k0, kv_head, batch);
+      mbar_expect_tx(kv_full, 2 * G::kRes);
+      G::load_resident(smem, &mk, kv_full, k0, kv_head, batch);
+      G::load_resident(smem + G::kRes, &mv, kv_full, k0, kv_head, batch);
       int stage = 0, issued = 0;
       uint32_t parity = 1;
       for (int n = 0; n < items; ++n) {
-        const int head = kv_head * group + n / per_head, q0 = (first + n % per_head) * kAttnTile;
+        const int head = kv_head * group + n / per_head, q0 = (first + n % per_head) * G::kTok;
         if (s_abort || !mbar_wait_bounded(&free_[stage], parity)) { s_abort = 1; break; }
         unsigned char* at = smem + L::kRing + stage * L::kStage;
-        unsigned char* stats = smem + L::kStats + stage * 1024;
+        unsigned char* stats = smem + L::kStats + stage * 2 * L::kStat;
         const long long base = (static_cast<long long>(batch) * p.Hq + head) * p.sq_pad + q0;
-        mbar_expect_tx(&full[stage], L::kStage + 1024);
+        mbar_expect_tx(&full[stage], L::kStage + 2 * L::kStat);
         attn_load_tile<D>(at, &mq, &full[stage], q0, head, batch);
-        attn_load_tile<D>(at + L::kT, &mdo, &full[stage], q0, head, batch);
-        bulk_load(stats, p.lse2 + base, 512, &full[stage]);
-        bulk_load(stats + 512, p.delta + base, 512, &full[stage]);
+        attn_load_tile<D>(at + G::kStr, &mdo, &full[stage], q0, head, batch);
+        bulk_load(stats, p.lse2 + base, L::kStat, &full[stage]);
+        bulk_load(stats + L::kStat, p.delta + base, L::kStat, &full[stage]);
         ++issued;
         if (++stage == L::kStages) { stage = 0; parity ^= 1u; }
       }
@@ -530,14 +545,14 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
         for (int s = 0; s < L::kStages && s < issued; ++s) mbar_wait_bounded(&full[s], ((issued - 1 - s) / L::kStages) & 1);
       }
     }
-  } else if (items > 0 && warp == kAttnMmaWarp) {
+  } else if (items > 0 && warp == G::kMmaWarp) {
     bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(kv_full, 0));
     if (ok && k0 + kAttnTile > kv_len) {
-      attn_zero_rows<D>(smem, kv_len - k0);
-      attn_zero_rows<D>(smem + L::kT, kv_len - k0);
+      attn_zero_rows<D, kAttnTile>(smem, kv_len - k0);
+      attn_zero_rows<D, kAttnTile>(smem + G::kRes, kv_len - k0);
     }
     const bool issuer = elect_one();
-    const uint64_t k_desc = AttnDesc<D>::rows(smem_addr(smem)), v_desc = k_desc + (L::kT >> 4);
+    const uint64_t k_desc = AttnDesc<D>::rows(smem_addr(smem)), v_desc = k_desc + (G::kRes >> 4);
     const uint32_t ring = smem_addr(smem) + L::kRing;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       ok = ok && !s_abort && mbar_wait_bounded(bar, parity);
@@ -548,9 +563,9 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
     if (wait(&full[0], 0)) {
       const uint64_t q_desc = AttnDesc<D>::rows(ring);
       if (issuer) {
-        attn_mma_rows<D, BF16>(t_s, k_desc, q_desc);
+        attn_mma_rows<D, BF16, G::kTok>(t_s, k_desc, q_desc);
         mma_commit(s_full);
-        attn_mma_rows<D, BF16>(t_dp, v_desc, q_desc + (L::kT >> 4));
+        attn_mma_rows<D, BF16, G::kTok>(t_dp, v_desc, q_desc + (G::kStr >> 4));
         mma_commit(dp_full);
       }
       __syncwarp();
@@ -563,22 +578,22 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       if (next_stage == 0) next_parity ^= 1u;
       const uint64_t by_tokens = AttnDesc<D>::tokens(ring + stage * L::kStage), next_rows = AttnDesc<D>::rows(ring + next_stage * L::kStage);
       if (!wait(p_full, n & 1)) break;
-      if (issuer) attn_mma_tokens<D, BF16>(t_dv, t_s, by_tokens + (L::kT >> 4), n != 0);
+      if (issuer) attn_mma_tokens<D, BF16, G::kTok>(t_dv, t_s, by_tokens + (G::kStr >> 4), n != 0);
       __syncwarp();
       if (more) {
         if (!wait(&full[next_stage], next_parity)) break;
         if (issuer) {
-          attn_mma_rows<D, BF16>(t_s, k_desc, next_rows);
+          attn_mma_rows<D, BF16, G::kTok>(t_s, k_desc, next_rows);
           mma_commit(s_full);
         }
         __syncwarp();
       }
       if (!wait(ds_full, n & 1)) break;
       if (issuer) {
-        attn_mma_tokens<D, BF16>(t_dk, t_dp, by_tokens, n != 0);
+        attn_mma_tokens<D, BF16, G::kTok>(t_dk, t_dp, by_tokens, n != 0);
         mma_commit(&free_[stage]);
         if (more) {
-          attn_mma_rows<D, BF16>(t_dp, v_desc, next_rows + (L::kT >> 4));
+          attn_mma_rows<D, BF16, G::kTok>(t_dp, v_desc, next_rows + (G::kStr >> 4));
           mma_commit(dp_full);
         } else {
           mma_commit(done);
@@ -591,7 +606,7 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       s_abort = 1;
       if (issuer) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
     }
-  } else if (warp < 16) {
+  } else if (warp < G::kElem) {
     const int part = warp >> 2;                  // this warp's 32 queries of each tile
     const int key = k0 + (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -607,10 +622,10 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
     int stage = 0, in_head = 0;
     uint32_t stage_parity = 0;
     for (int n = 0; n < items; ++n) {
-      const int q0 = (first + in_head) * kAttnTile + part * 32;
+      const int q0 = (first + in_head) * G::kTok + part * 32;
       if (++in_head == per_head) in_head = 0;
-      const float4* lse2 = reinterpret_cast<const float4*>(smem + L::kStats + stage * 1024) + part * 8;
-      const float4* delta = reinterpret_cast<const float4*>(smem + L::kStats + stage * 1024 + 512) + part * 8;
+      const float4* lse2 = reinterpret_cast<const float4*>(smem + L::kStats + stage * 2 * L::kStat) + part * 8;
+      const float4* delta = reinterpret_cast<const float4*>(smem + L::kStats + stage * 2 * L::kStat + L::kStat) + part * 8;
       // key j is seen by query i when j < kv_len and j - off <= i
       const int from = key >= kv_len ? 0x7fffffff : p.causal ? key - off - q0 : 0;       // first column of this row that is not masked
       const int warp_from = k0 + (warp & 3) * 32 + 31 >= kv_len ? 0x7fffffff : p.causal ? key - lane + 31 - off - q0 : 0;
@@ -668,12 +683,16 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       if (lane == 0) mbar_arrive_one(ds_full);
     }
     const bool live = key < p.Sk;
-    const AttnOut& mine = part < 2 ? p.dv : p.dk;
+    // half of the warps for each gradient, 64 columns a warp
+    constexpr int kShare = G::kParts / 2;
+    const bool is_dv = part < kShare;
+    const int columns = (part % kShare) * 64;
+    const AttnOut& mine = is_dv ? p.dv : p.dk;
     if (items > 0) {
       if (ok) wait(done, 0);
-      if (ok) attn_store_row<D / 64, BF16>(p, mine, (part < 2 ? t_dv : t_dk) + lanes, (part & 1) * (D / 2), batch, kv_head, key, live, part < 2 ? 1.f : p.scale);
+      if (ok) attn_store_row<2, BF16>(p, mine, (is_dv ? t_dv : t_dk) + lanes, columns, batch, kv_head, key, live, is_dv ? 1.f : p.scale);
       else s_abort = 1;
-    } else if (live && (part & 1) == 0) {
+    } else if (live && columns == 0) {
       attn_zero_row(p, mine, batch, kv_head, key);
     }
   }
@@ -681,9 +700,9 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
   tc_fence_before();
   __syncthreads();
   if (s_abort && threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
-  if (warp == kAttnMmaWarp) {
+  if (warp == G::kMmaWarp) {
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(tmem, G::kTmem);
   }
 }
 
@@ -695,15 +714,16 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
 // dQ += dS(j) K(j), with dS in the place of S(j), beside that of tile j+1.
 // ----------------------------------------------------------------------------------------------
 template <int D> struct AttnDqSmem {
-  static constexpr uint32_t kT = AttnTile<D>::kBytes;
+  using G = AttnBwd<D>;
   static constexpr int kKs = D == 128 ? 3 : 5, kVs = D == 128 ? 2 : 4;
-  static constexpr uint32_t kK = 2 * kT, kV = kK + kKs * kT, kBars = kV + kVs * kT, kBytes = kBars + 256 + 1024;
+  static constexpr uint32_t kK = 2 * G::kRes, kV = kK + kKs * G::kStr, kBars = kV + kVs * G::kStr, kBytes = kBars + 256 + 1024;
 };
 
 template <int D, bool BF16>
 __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo,
                                               const AttnParams& p, const int tile, const int head, const int batch) {
   using L = AttnDqSmem<D>;
+  using G = AttnBwd<D>;
   uint64_t* q_full = reinterpret_cast<uint64_t*>(smem + L::kBars);
   uint64_t* k_full = q_full + 1;                 // [kKs]
   uint64_t* k_free = k_full + L::kKs;            // [kKs]
@@ -729,44 +749,44 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
     mbar_init(&s_full[0], 1);
     mbar_init(&s_full[1], 1);
     mbar_init(dp_full, 1);
-    mbar_init(dp_read, 16);
-    mbar_init(&ds_full[0], 16);
-    mbar_init(&ds_full[1], 16);
+    mbar_init(dp_read, G::kElem);
+    mbar_init(&ds_full[0], G::kElem);
+    mbar_init(&ds_full[1], G::kElem);
     mbar_init(done, 1);
     mbar_init(drain, 1);
     s_abort = 0;
     mbar_init_fence();
     fence_proxy_async_smem();
   }
-  if (warp == kAttnMmaWarp) tmem_alloc(&s_tmem, 512);
+  if (warp == G::kMmaWarp) tmem_alloc(&s_tmem, G::kTmem);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
-  const uint32_t t_dp = tmem + 256, t_dq = tmem + 384;
+  const uint32_t t_dp = tmem + 2 * G::kTok, t_dq = t_dp + G::kTok;
   const int kv_len = attn_kv_len(p, batch);
   const int off = p.Sk - p.Sq;
   const int q_last = min(q0 + kAttnTile, p.Sq) - 1;
   const int seen = p.causal ? min(kv_len, max(0, q_last + off + 1)) : kv_len;
-  const int tiles = (seen + kAttnTile - 1) / kAttnTile;
+  const int tiles = (seen + G::kTok - 1) / G::kTok;
   pdl_wait();
 
-  if (tiles > 0 && warp == kAttnCopyWarp) {
+  if (tiles > 0 && warp == G::kCopyWarp) {
     if (lane == 0) {
-      mbar_expect_tx(q_full, 2 * L::kT);
-      attn_load_tile<D>(smem, &mq, q_full, q0, head, batch);
-      attn_load_tile<D>(smem + L::kT, &mdo, q_full, q0, head, batch);
+      mbar_expect_tx(q_full, 2 * G::kRes);
+      G::load_resident(smem, &mq, q_full, q0, head, batch);
+      G::load_resident(smem + G::kRes, &mdo, q_full, q0, head, batch);
       const int kv_head = head / (p.Hq / p.Hkv);
       int issued = 0;
       for (int j = 0; j < tiles; ++j) {
         const int ks = j % L::kKs, vs = j % L::kVs;
         if (s_abort || !mbar_wait_bounded(&k_free[ks], ((j / L::kKs) & 1) ^ 1)) { s_abort = 1; break; }
-        mbar_expect_tx(&k_full[ks], L::kT);
-        attn_load_tile<D>(smem + L::kK + ks * L::kT, &mk, &k_full[ks], j * kAttnTile, kv_head, batch);
+        mbar_expect_tx(&k_full[ks], G::kStr);
+        attn_load_tile<D>(smem + L::kK + ks * G::kStr, &mk, &k_full[ks], j * G::kTok, kv_head, batch);
         issued = 2 * j + 1;
         if (s_abort || !mbar_wait_bounded(&v_free[vs], ((j / L::kVs) & 1) ^ 1)) { s_abort = 1; break; }
-        mbar_expect_tx(&v_full[vs], L::kT);
-        attn_load_tile<D>(smem + L::kV + vs * L::kT, &mv, &v_full[vs], j * kAttnTile, kv_head, batch);
+        mbar_expect_tx(&v_full[vs], G::kStr);
+        attn_load_tile<D>(smem + L::kV + vs * G::kStr, &mv, &v_full[vs], j * G::kTok, kv_head, batch);
         issued = 2 * j + 2;
       }
       if (s_abort) {
@@ -776,7 +796,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
         for (int s = 0; s < L::kVs && s < nv; ++s) mbar_wait_bounded(&v_full[s], ((nv - 1 - s) / L::kVs) & 1);
       }
     }
-  } else if (tiles > 0 && warp == kAttnMmaWarp) {
+  } else if (tiles > 0 && warp == G::kMmaWarp) {
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       ok = ok && !s_abort && mbar_wait_bounded(bar, parity);
@@ -785,15 +805,15 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       return ok;
     };
     const bool issuer = elect_one();
-    const uint64_t q_desc = AttnDesc<D>::rows(smem_addr(smem)), do_desc = q_desc + (L::kT >> 4);
+    const uint64_t q_desc = AttnDesc<D>::rows(smem_addr(smem)), do_desc = q_desc + (G::kRes >> 4);
     auto scores = [&](int j) {                   // S(j)
       const int ks = j % L::kKs;
       if (!wait(&k_full[ks], (j / L::kKs) & 1)) return;
-      unsigned char* at = smem + L::kK + ks * L::kT;
-      if ((j + 1) * kAttnTile > kv_len) attn_zero_rows<D>(at, kv_len - j * kAttnTile);
+      unsigned char* at = smem + L::kK + ks * G::kStr;
+      if ((j + 1) * G::kTok > kv_len) attn_zero_rows<D, G::kTok>(at, kv_len - j * G::kTok);
       const uint64_t k_desc = AttnDesc<D>::rows(smem_addr(at));
       if (issuer) {
-        attn_mma_rows<D, BF16>(tmem + (j & 1) * 128, q_desc, k_desc);
+        attn_mma_rows<D, BF16, G::kTok>(tmem + (j & 1) * G::kTok, q_desc, k_desc);
         mma_commit(&s_full[j & 1]);
       }
       __syncwarp();
@@ -801,11 +821,11 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
     auto dprobs = [&](int j) {                   // dP(j)
       const int vs = j % L::kVs;
       if (!wait(&v_full[vs], (j / L::kVs) & 1)) return;
-      unsigned char* at = smem + L::kV + vs * L::kT;
-      if ((j + 1) * kAttnTile > kv_len) attn_zero_rows<D>(at, kv_len - j * kAttnTile);
+      unsigned char* at = smem + L::kV + vs * G::kStr;
+      if ((j + 1) * G::kTok > kv_len) attn_zero_rows<D, G::kTok>(at, kv_len - j * G::kTok);
       const uint64_t v_desc = AttnDesc<D>::rows(smem_addr(at));
       if (issuer) {
-        attn_mma_rows<D, BF16>(t_dp, do_desc, v_desc);
+        attn_mma_rows<D, BF16, G::kTok>(t_dp, do_desc, v_desc);
         mma_commit(dp_full);
         mma_commit(&v_free[vs]);
       }
@@ -823,9 +843,9 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
         if (!ok) break;
       }
       if (!wait(&ds_full[j & 1], (j >> 1) & 1)) break;
-      const uint64_t k_desc = AttnDesc<D>::tokens(smem_addr(smem) + L::kK + (j % L::kKs) * L::kT);
+      const uint64_t k_desc = AttnDesc<D>::tokens(smem_addr(smem) + L::kK + (j % L::kKs) * G::kStr);
       if (issuer) {
-        attn_mma_tokens<D, BF16>(t_dq, tmem + (j & 1) * 128, k_desc, j != 0);
+        attn_mma_tokens<D, BF16, G::kTok>(t_dq, tmem + (j & 1) * G::kTok, k_desc, j != 0);
         mma_commit(&k_free[j % L::kKs]);
         if (j == tiles - 1) mma_commit(done);
       }
@@ -835,7 +855,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       s_abort = 1;
       if (issuer) { mma_commit(drain); mbar_wait_bounded(drain, 0); }
     }
-  } else if (warp < 16) {
+  } else if (warp < G::kElem) {
     const int part = warp >> 2;                  // this warp's 32 keys of each tile
     const int row = q0 + (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -852,8 +872,8 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       return ok;
     };
     for (int j = 0; j < tiles; ++j) {
-      const uint32_t s_at = tmem + (j & 1) * 128 + lanes + part * 32, dp_at = t_dp + lanes + part * 32;
-      const int k0 = j * kAttnTile + part * 32;
+      const uint32_t s_at = tmem + (j & 1) * G::kTok + lanes + part * 32, dp_at = t_dp + lanes + part * 32;
+      const int k0 = j * G::kTok + part * 32;
       if (!wait(&s_full[j & 1], (j >> 1) & 1)) break;
       float pr[32];
       {
@@ -895,7 +915,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
     const bool live = row < p.Sq;
     if (tiles > 0) {
       if (ok) wait(done, 0);
-      if (ok && part < 2) attn_store_row<D / 64, BF16>(p, p.out, t_dq + lanes, part * (D / 2), batch, head, row, live, p.scale);
+      if (ok && part < D / 64) attn_store_row<2, BF16>(p, p.out, t_dq + lanes, part * 64, batch, head, row, live, p.scale);
       if (!ok) s_abort = 1;
     } else if (live && part == 0) {
       attn_zero_row(p, p.out, batch, head, row);
@@ -905,9 +925,9 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
   tc_fence_before();
   __syncthreads();
   if (s_abort && threadIdx.x == 0) atomicOr(p.flags, kFlagTimeout);
-  if (warp == kAttnMmaWarp) {
+  if (warp == G::kMmaWarp) {
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(tmem, G::kTmem);
   }
 }
 
@@ -917,7 +937,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
 template <int D> constexpr uint32_t attn_backward_smem() { return AttnDkvSmem<D>::kBytes > AttnDqSmem<D>::kBytes ? AttnDkvSmem<D>::kBytes : AttnDqSmem<D>::kBytes; }
 
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kAttnThreads, 1)
+__global__ void __launch_bounds__(AttnBwd<D>::kThreads, AttnBwd<D>::kBlocks)
 attn_backward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                      const __grid_constant__ CUtensorMap mdo, const AttnParams p, const int key_blocks, const int q_tiles) {
   extern __shared__ unsigned char smem_dyn[];
