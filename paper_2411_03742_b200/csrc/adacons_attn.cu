@@ -124,18 +124,22 @@ bool run_forward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap
 template <int D, bool BF16>
 bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo, AttnParams p, const adacons_attn_tensor* dout,
                   const adacons_attn_tensor* out, const float* lse, AttnOut dq, AttnOut dk, AttnOut dv, float* lse2, float* delta, cudaStream_t st) {
-  const long long rows = static_cast<long long>(p.B) * p.Hq * p.sq_pad;
+  p.dout = {dout->data, dout->batch_stride, dout->seq_stride, dout->head_stride};
+  p.o = {out->data, out->batch_stride, out->seq_stride, out->head_stride};
+  p.lse_in = lse;
   p.lse2 = lse2;
   p.delta = delta;
-  const AttnRows a = {dout->data, dout->batch_stride, dout->seq_stride, dout->head_stride}, b = {out->data, out->batch_stride, out->seq_stride, out->head_stride};
-  if (rows > 0 && !launch(&attn_delta_kernel<BF16>, dim3(static_cast<unsigned>((rows + 7) / 8)), dim3(256), 0, st, kLaunchPlain, 1, a, b, lse, p.Hq, p.Sq, p.sq_pad, p.D, rows, lse2, delta))
-    return false;
+  const bool separate = delta != nullptr && p.sq_pad > 0;
+  if (separate) {
+    if (!launch(&attn_delta_kernel<D, BF16>, dim3(p.sq_pad / (256 / (D / 8)), p.Hq, p.B), dim3(256), 0, st, kLaunchPlain, 1, p, lse2, delta)) return false;
+  }
   p.out = dq;
   p.dk = dk;
   p.dv = dv;
   const int64_t q_tiles = p.sq_pad / kAttnTile, k_tiles = (static_cast<int64_t>(p.Sk) + kAttnTile - 1) / kAttnTile;
   const int64_t key_blocks = k_tiles * p.Hkv * p.B, blocks = key_blocks + q_tiles * p.Hq * p.B;
-  return blocks <= 0x7fffffff && launch(&attn_backward_kernel<D, BF16>, dim3(static_cast<unsigned>(blocks)), dim3(AttnBwd<D>::kThreads), attn_backward_smem<D>(), st, kLaunchOverlap, 1,
+  return blocks <= 0x7fffffff && launch(&attn_backward_kernel<D, BF16>, dim3(static_cast<unsigned>(blocks)), dim3(AttnBwd<D>::kThreads), attn_backward_smem<D>(), st,
+                                        separate ? kLaunchOverlap : kLaunchPlain, 1,
                                         mq, mk, mv, mdo, p, static_cast<int>(key_blocks), static_cast<int>(q_tiles));
 }
 
@@ -192,7 +196,11 @@ int adacons_attn_backward(const adacons_attn_shape* s, const adacons_attn_tensor
   for (const adacons_attn_tensor* t : by_k)
     if ((rc = check_tensor(t, s->batch, s->kv_len, s->kv_heads)) != ADACONS_OK) return rc;
   if (s->batch == 0 || (s->q_len == 0 && s->kv_len == 0)) return ADACONS_OK;
-  if (s->q_len > 0 && (lse == nullptr || reinterpret_cast<uintptr_t>(lse) % 4 != 0 || workspace == nullptr || bytes < workspace_bytes(s))) return ADACONS_EINVAL;
+  if (s->q_len > 0) {
+    const int64_t pad = (static_cast<int64_t>(s->q_len) + kAttnTile - 1) / kAttnTile * kAttnTile;
+    if (lse == nullptr || reinterpret_cast<uintptr_t>(lse) % 4 != 0) return ADACONS_EINVAL;
+    if (workspace == nullptr ? s->q_heads / s->kv_heads * pad > ADACONS_ATTN_SHORT_ROWS : bytes < workspace_bytes(s)) return ADACONS_EINVAL;
+  }
   if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return ADACONS_EALIGN;
   AttnDevice* d = nullptr;
   if ((rc = attn_device(&d)) != ADACONS_OK) return rc;
@@ -204,7 +212,7 @@ int adacons_attn_backward(const adacons_attn_shape* s, const adacons_attn_tensor
     return ADACONS_ECUDA;
   const AttnParams p = base_params(*d, s);
   float* lse2 = static_cast<float*>(workspace);
-  float* delta = lse2 + static_cast<int64_t>(p.B) * p.Hq * p.sq_pad;
+  float* delta = lse2 == nullptr ? nullptr : lse2 + static_cast<int64_t>(p.B) * p.Hq * p.sq_pad;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   auto go = [&](auto run) { return run(mq, mk, mv, mdo, p, dout, out, lse, as_out(dq), as_out(dk), as_out(dv), lse2, delta, st); };
   bool ok;

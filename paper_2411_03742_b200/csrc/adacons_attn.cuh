@@ -3,6 +3,7 @@
 
 #include <cuda_fp16.h>
 
+#include "adacons_ops.h"
 #include "adacons_tc.cuh"
 
 namespace adacons {
@@ -29,6 +30,7 @@ constexpr int kAttnTile = 128;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttnOut { void* p; long long batch, seq, head; };     // element strides
+struct AttnRows { const void* p; long long batch, seq, head; };
 
 struct AttnParams {
   int B, Hq, Hkv, Sq, Sk, D;
@@ -38,7 +40,9 @@ struct AttnParams {
   const int* kv_lens;            // [B] or null
   float* lse;                    // forward: [B][Hq][Sq]
   const float* lse2;             // backward: lse log2(e), +inf where a row has no key or does not exist: [B][Hq][sq_pad]
-  const float* delta;            // likewise, 0 there
+  const float* delta;            // likewise, 0 there; null: each block makes both for its own queries, from what follows
+  AttnRows dout, o;
+  const float* lse_in;           // [B][Hq][Sq]
   AttnOut out, dk, dv;           // forward: O; backward: dQ, dK, dV
   uint32_t* flags;
 };
@@ -397,39 +401,67 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
 }
 
 // ----------------------------------------------------------------------------------------------
-// Before the gradient: Delta_i = sum_d dO_id O_id and the log-sum-exp in base 2, padded to whole tiles
-// so that the gradient kernels copy them 128 at a time.  One warp per query and head.
+// Before the gradient: Delta_i = sum_d dO_id O_id and the log-sum-exp in base 2, +inf and 0 where a query sees no key.
+// D / 8 lanes take a query's row, eight elements each.
+//
+// With a workspace a kernel of its own writes them there, padded to whole tiles, so that the gradient's blocks copy them a
+// tile at a time.  Without one (short queries only) every block of the gradient makes its own, in shared memory: this
+// repeats the work in each block of a head and costs up to 2 us of it, but saves a launch.
 // ----------------------------------------------------------------------------------------------
-struct AttnRows { const void* p; long long batch, seq, head; };
-
-template <bool BF16>
-__global__ void __launch_bounds__(256) attn_delta_kernel(const AttnRows dout, const AttnRows out, const float* lse, int Hq, int Sq, int sq_pad, int D,
-                                                         long long rows, float* lse2, float* delta) {
-  const long long n = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  pdl_launch_dependents();
-  if (n >= rows) return;
-  const long long bh = n / sq_pad;
-  const int row = static_cast<int>(n - bh * sq_pad), head = static_cast<int>(bh % Hq);
-  const long long batch = bh / Hq;
-  float sum = 0.f, l = -INFINITY;
-  if (row < Sq) {
-    const unsigned short* a = static_cast<const unsigned short*>(dout.p) + batch * dout.batch + row * dout.seq + head * dout.head;
-    const unsigned short* b = static_cast<const unsigned short*>(out.p) + batch * out.batch + row * out.seq + head * out.head;
-    if (4 * lane < D) {                          // D <= 128, a multiple of eight
-      const uint2 x = *reinterpret_cast<const uint2*>(a + 4 * lane), y = *reinterpret_cast<const uint2*>(b + 4 * lane);
-      const float2 x0 = unpack16<BF16>(x.x), x1 = unpack16<BF16>(x.y), y0 = unpack16<BF16>(y.x), y1 = unpack16<BF16>(y.y);
-      sum = (x0.x * y0.x + x0.y * y0.y) + (x1.x * y1.x + x1.y * y1.y);
+// U rows of each group of lanes, `step` places apart from place n on: rows of `heads` heads from `head` on, `pitch` places
+// each; `total` places in all.  Whole warps.
+template <int D, bool BF16, int U>
+__device__ __forceinline__ void attn_row_stats(const AttnParams& p, int batch, int head, int first_row, int pitch, int n, int step, int total, float* lse2, float* delta) {
+  constexpr int kLanes = D / 8;
+  const int e = 8 * (threadIdx.x % kLanes);
+  uint4 x[U], y[U];
+  float l[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int at = n + u * step, h = head + at / pitch, row = first_row + at % pitch;
+    x[u] = y[u] = make_uint4(0u, 0u, 0u, 0u);
+    l[u] = -INFINITY;
+    if (at < total && row < p.Sq) {
+      if (e < p.D) {
+        x[u] = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(p.dout.p) + batch * p.dout.batch + row * p.dout.seq + h * p.dout.head + e);
+        y[u] = *reinterpret_cast<const uint4*>(static_cast<const unsigned short*>(p.o.p) + batch * p.o.batch + row * p.o.seq + h * p.o.head + e);
+      }
+      l[u] = p.lse_in[(static_cast<long long>(batch) * p.Hq + h) * p.Sq + row];
     }
-    l = lse[bh * Sq + row];
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (lane == 0) {
-    const bool none = l == -INFINITY;
-    lse2[n] = none ? INFINITY : l * kLog2e;
-    delta[n] = none ? 0.f : sum;
+  for (int u = 0; u < U; ++u) {
+    const uint32_t xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w}, ys[4] = {y[u].x, y[u].y, y[u].z, y[u].w};
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 a = unpack16<BF16>(xs[k]), b = unpack16<BF16>(ys[k]);
+      sum += a.x * b.x + a.y * b.y;
+    }
+#pragma unroll
+    for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const int at = n + u * step;
+    if (e == 0 && at < total) {
+      const bool none = l[u] == -INFINITY;
+      lse2[at] = none ? INFINITY : l[u] * kLog2e;
+      delta[at] = none ? 0.f : sum;
+    }
   }
+}
+// All of `total` places by the THREADS elementwise threads of a block, which meet at the end.
+template <int D, bool BF16, int THREADS>
+__device__ __forceinline__ void attn_block_stats(const AttnParams& p, int batch, int head, int first_row, int pitch, int total, float* lse2, float* delta) {
+  constexpr int kStep = THREADS / (D / 8), kU = 4;
+  const int n = threadIdx.x / (D / 8);
+  for (int base = 0; base < total; base += kU * kStep) attn_row_stats<D, BF16, kU>(p, batch, head, first_row, pitch, base + n, kStep, total, lse2, delta);
+  asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+}
+
+template <int D, bool BF16>
+__global__ void __launch_bounds__(256) attn_delta_kernel(const AttnParams p, float* lse2, float* delta) {      // grid: rows of a head, heads, batch
+  pdl_launch_dependents();
+  const long long at = (static_cast<long long>(blockIdx.z) * p.Hq + blockIdx.y) * p.sq_pad;
+  attn_row_stats<D, BF16, 1>(p, blockIdx.z, blockIdx.y, 0, p.sq_pad, blockIdx.x * (256 / (D / 8)) + threadIdx.x / (D / 8), 0, p.sq_pad, lse2 + at, delta + at);
 }
 
 // ----------------------------------------------------------------------------------------------
@@ -463,7 +495,8 @@ template <int D> struct AttnDkvSmem {
   static constexpr uint32_t kRing = 2 * G::kRes, kStage = 2 * G::kStr;          // K, V | (Q, dO) per stage
   static constexpr uint32_t kStat = G::kTok * 4;                                // lse2, delta: bytes per stage of each
   static constexpr uint32_t kStats = kRing + kStages * kStage;
-  static constexpr uint32_t kBars = kStats + kStages * 2 * kStat, kBytes = kBars + 256 + 1024;
+  static constexpr uint32_t kTable = kStats + kStages * 2 * kStat;              // short queries' lse2, delta
+  static constexpr uint32_t kBars = kTable + 2 * 4 * ADACONS_ATTN_SHORT_ROWS, kBytes = kBars + 256 + 1024;
 };
 
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
@@ -532,11 +565,13 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
         unsigned char* at = smem + L::kRing + stage * L::kStage;
         unsigned char* stats = smem + L::kStats + stage * 2 * L::kStat;
         const long long base = (static_cast<long long>(batch) * p.Hq + head) * p.sq_pad + q0;
-        mbar_expect_tx(&full[stage], L::kStage + 2 * L::kStat);
+        mbar_expect_tx(&full[stage], L::kStage + (p.delta != nullptr ? 2 * L::kStat : 0));
         attn_load_tile<D>(at, &mq, &full[stage], q0, head, batch);
         attn_load_tile<D>(at + G::kStr, &mdo, &full[stage], q0, head, batch);
-        bulk_load(stats, p.lse2 + base, L::kStat, &full[stage]);
-        bulk_load(stats + L::kStat, p.delta + base, L::kStat, &full[stage]);
+        if (p.delta != nullptr) {
+          bulk_load(stats, p.lse2 + base, L::kStat, &full[stage]);
+          bulk_load(stats + L::kStat, p.delta + base, L::kStat, &full[stage]);
+        }
         ++issued;
         if (++stage == L::kStages) { stage = 0; parity ^= 1u; }
       }
@@ -619,13 +654,19 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       tc_fence_after();
       return ok;
     };
-    int stage = 0, in_head = 0;
+    const bool table = p.delta == nullptr;
+    if (table && items > 0) {
+      float* at = reinterpret_cast<float*>(smem + L::kTable);
+      attn_block_stats<D, BF16, G::kElem * 32>(p, batch, kv_head * group, 0, q_tiles * G::kTok, group * q_tiles * G::kTok, at, at + ADACONS_ATTN_SHORT_ROWS);
+    }
+    int stage = 0, in_head = 0, head_at = 0;
     uint32_t stage_parity = 0;
     for (int n = 0; n < items; ++n) {
       const int q0 = (first + in_head) * G::kTok + part * 32;
-      if (++in_head == per_head) in_head = 0;
-      const float4* lse2 = reinterpret_cast<const float4*>(smem + L::kStats + stage * 2 * L::kStat) + part * 8;
-      const float4* delta = reinterpret_cast<const float4*>(smem + L::kStats + stage * 2 * L::kStat + L::kStat) + part * 8;
+      const uint32_t place = table ? L::kTable + (head_at + q0) * 4 : L::kStats + stage * 2 * L::kStat + part * 128;
+      if (++in_head == per_head) { in_head = 0; head_at += q_tiles * G::kTok; }
+      const float4* lse2 = reinterpret_cast<const float4*>(smem + place);
+      const float4* delta = reinterpret_cast<const float4*>(smem + place + (table ? 4 * ADACONS_ATTN_SHORT_ROWS : L::kStat));
       // key j is seen by query i when j < kv_len and j - off <= i
       const int from = key >= kv_len ? 0x7fffffff : p.causal ? key - off - q0 : 0;       // first column of this row that is not masked
       const int warp_from = k0 + (warp & 3) * 32 + 31 >= kv_len ? 0x7fffffff : p.causal ? key - lane + 31 - off - q0 : 0;
@@ -716,7 +757,7 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
 template <int D> struct AttnDqSmem {
   using G = AttnBwd<D>;
   static constexpr int kKs = D == 128 ? 3 : 5, kVs = D == 128 ? 2 : 4;
-  static constexpr uint32_t kK = 2 * G::kRes, kV = kK + kKs * G::kStr, kBars = kV + kVs * G::kStr, kBytes = kBars + 256 + 1024;
+  static constexpr uint32_t kK = 2 * G::kRes, kV = kK + kKs * G::kStr, kTable = kV + kVs * G::kStr, kBars = kTable + 2 * 4 * kAttnTile, kBytes = kBars + 256 + 1024;
 };
 
 template <int D, bool BF16>
@@ -859,8 +900,17 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
     const int part = warp >> 2;                  // this warp's 32 keys of each tile
     const int row = q0 + (warp & 3) * 32 + lane;
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const long long stat = (static_cast<long long>(batch) * p.Hq + head) * p.sq_pad + row;      // rows are padded: always there
-    const float lse2 = p.lse2[stat], delta = p.delta[stat];
+    float lse2 = INFINITY, delta = 0.f;
+    if (p.delta != nullptr) {
+      const long long stat = (static_cast<long long>(batch) * p.Hq + head) * p.sq_pad + row;    // rows are padded: always there
+      lse2 = p.lse2[stat];
+      delta = p.delta[stat];
+    } else if (tiles > 0) {
+      float* at = reinterpret_cast<float*>(smem + L::kTable);
+      attn_block_stats<D, BF16, G::kElem * 32>(p, batch, head, q0, kAttnTile, kAttnTile, at, at + kAttnTile);
+      lse2 = at[row - q0];
+      delta = at[kAttnTile + row - q0];
+    }
     const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), lse22 = make_float2(-lse2, -lse2), delta2 = make_float2(-delta, -delta);
     const int limit = p.causal ? min(kv_len, row + off + 1) : kv_len;
     const int warp_limit = p.causal ? min(kv_len, row - lane + off + 1) : kv_len;

@@ -198,6 +198,35 @@ def test_given_outputs_streams_and_repeats():
         assert (t[:, 0] == 7.0).all() and (t[:, S + 1:] == 7.0).all() and (t[..., D:] == 7.0).all()
 
 
+@pytest.mark.parametrize("B, Sq, Sk, Hq, Hk, D, causal", [(3, 77, 91, 4, 2, 40, False), (1, 1, 300, 2, 1, 128, True), (2, 128, 129, 4, 2, 128, False),
+                                                           (1, 256, 256, 3, 3, 64, True), (2, 65, 1, 2, 2, 72, False)])
+def test_short_queries_with_and_without_a_workspace(B, Sq, Sk, Hq, Hk, D, causal):
+    """The statistics made in each block and those of the kernel before it are the same sums: the gradients agree bit for bit."""
+    from paper_2411_03742_b200 import attention_backward, attention_forward
+    from paper_2411_03742_b200.attention import workspace_bytes
+    g = torch.Generator(device="cuda").manual_seed(Sq + D)
+    q, dout = (torch.randn((B, Sq, Hq, D), generator=g, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn((B, Sk, Hk, D), generator=g, device="cuda").bfloat16() for _ in range(2))
+    lens = torch.randint(0, Sk + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    out, lse = attention_forward(q, k, v, causal=causal, kv_lens=lens)
+    work = torch.full((workspace_bytes(q, k),), 255, dtype=torch.uint8, device="cuda")
+    one = attention_backward(dout, q, k, v, out, lse, causal=causal, kv_lens=lens)
+    two = attention_backward(dout, q, k, v, out, lse, causal=causal, kv_lens=lens, workspace=work)
+    assert all(torch.equal(x, y) for x, y in zip(one, two))
+
+
+def test_long_queries_need_a_workspace():
+    import ctypes
+    from paper_2411_03742_b200.attention import SHORT_ROWS, _Shape, _Tensor
+    from paper_2411_03742_b200.binding import EINVAL, load_library
+    for q_len, q_heads in ((SHORT_ROWS + 1, 1), (1, SHORT_ROWS // 128 + 1)):
+        t = torch.zeros((1, q_len, q_heads, 64), dtype=torch.bfloat16, device="cuda")
+        rows = torch.zeros((1, q_heads, q_len), device="cuda")
+        s, x = _Shape(1, 1, q_heads, 1, q_len, q_len, 64, 0, 0.125, None), _Tensor(t.data_ptr(), *t.stride()[:3])
+        r = ctypes.byref
+        assert load_library().adacons_attn_backward(r(s), r(x), r(x), r(x), r(x), r(x), rows.data_ptr(), r(x), r(x), r(x), None, 0, None) == EINVAL
+
+
 def test_strides_past_32_bits():
     from paper_2411_03742_b200 import attention_backward, attention_forward
     far = torch.zeros((1 << 31) + 64 * 140 * 2, dtype=torch.bfloat16, device="cuda")
