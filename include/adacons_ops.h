@@ -31,7 +31,7 @@ extern "C" {
  *            Elements outside the matrices (biases, gains) are neither read nor written.
  *   scaling  0: none; 1: each matrix's result times sqrt(max(1, rows / cols)).
  *   coeffs   host array of 3 * steps values a, b, c (one triple per step), 1 <= steps <= 64.  Iterates
- *            are held to |x| < 32; coefficients that let them grow beyond give Inf or NaN.
+ *            and a I + b S + c S S are held to |x| < 32; coefficients that let them grow beyond give Inf or NaN.
  *   eps      >= 0.  A matrix of zeros gives zeros when eps > 0.  Inf or NaN in a matrix give NaN in
  *            that matrix only.
  * adacons_orth_create allocates about 8 bytes per element of the matrices and 4 (bf16) or 8 (fp32) per

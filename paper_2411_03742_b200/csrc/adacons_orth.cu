@@ -300,7 +300,8 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   std::vector<OrthStep> step_coeffs(steps);
   for (int s = 0; s < steps; ++s) {
     const double* q = coeffs + 3 * s;
-    step_coeffs[s] = {static_cast<float>(q[0]), static_cast<float>(q[1]), static_cast<float>(q[2]), s >= 3 ? static_cast<float>(-0.75 * (q[1] + q[2])) : 0.f};
+    step_coeffs[s] = {static_cast<float>(q[0]), static_cast<float>(q[1]), static_cast<float>(q[2]),
+                      static_cast<float>(!split && !c->small ? q[0] : s >= 3 ? -0.75 * (q[1] + q[2]) : 0.0)};
   }
   c->num_chunks = static_cast<int>(chunks.size());
   c->num_load = static_cast<int>(load.size());

@@ -17,20 +17,22 @@ namespace adacons {
 //
 // Number format.  The products run on the tensor cores from fp16 operands.  An iterate is kept as a
 // pair hi + lo of fp16 values of 2^11 X (22 bits, range 2^-25 .. 2^16 after the power-of-two scale),
-// S and B as 2^13 S and 2^11 B.  In a bf16 context the products take the hi parts only, and the term
-// a X takes the pair; in an fp32 context S and B are pairs too and each product is the sum
-// (lo hi + hi lo) + hi hi.  The tensor cores round a running sum toward zero, low by up to 4e-8 of it
+// S and B as 2^13 S and 2^11 B.  In a bf16 context the products take the hi parts only, and B is stored as
+// B + a I, so that X <- (B + a I) X_hi + a X_lo: the epilogue reads the lo part alone, and in the last step, whose
+// errors no further step enlarges, nothing.  (With a X added from the pair the steps moved an eighth more bytes, and
+// bytes between L2 and the SMs are what bounds them: twelve encoder layers 3.76 -> 3.60 ms.)  In an fp32 context S and B are pairs too
+// and each product is the sum (lo hi + hi lo) + hi hi.  The tensor cores round a running sum toward zero, low by up to 4e-8 of it
 // per chained product: harmless beside an 11-bit operand, but 4e-5 of an fp32 result after five steps
 // on sides of 1024.  There the hi hi terms are chained over 64 K elements at most and the chunks'
 // sums added by the epilogue, round to nearest (the small terms, 2^-11 of the sum, in one accumulator).
 // Why not bf16 operands: rounding the iterates to 8 bits costs 1e-2 of the result's norm on a
 // Gaussian matrix and 1e-1 on one with a few strong directions (the small singular values grow
 // 3.4-fold per step and the rounding noise of the strong ones grows with them); 11 bits with the
-// a X term exact stay below 1.8e-3, the size of one bf16 rounding of the result.
-// The diagonal: near orthogonality B is close to (b + c) I, and rounding that diagonal is the largest
-// single error.  From the fourth step on B + t I is stored with t = -3/4 (b + c) and a - t takes the
-// place of a, an identity in exact arithmetic; it brings the error from 1.7e-3 to 1.1e-3 on Gaussian
-// matrices (on a matrix of rank 8 plus noise 5e-4 instead of 1.5e-4, still a third of the rounding).
+// a X term from the pair stay below 1.5e-3 before the result's own rounding, 1.7e-3 (Gaussian, rank 8 plus noise,
+// singular values over four decades).
+// The diagonal in an fp32 context, and where a matrix stays in one block: near orthogonality B is close to (b + c) I, and rounding that diagonal is the
+// largest single error.  From the fourth step on B + t I is stored with t = -3/4 (b + c) and a - t takes the
+// place of a, an identity in exact arithmetic.
 // ----------------------------------------------------------------------------------------------
 constexpr int kOrthTK = 64;              // K elements per stage: one 128-byte swizzled row
 constexpr int kOrthChunk = 1;            // fp32 contexts: stages (64 K elements) per hi hi accumulator
@@ -381,7 +383,7 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
   const bool turned = last && m.transposed;
   unsigned char* hrow = hi + lane * 128;
   unsigned char* lrow = lo + lane * 128;
-  const float by_x = KIND == kOrthPoly ? step.b * (kOrthBScale / kOrthSScale) : step.a - step.t;
+  const float by_x = KIND == kOrthPoly ? step.b * (kOrthBScale / kOrthSScale) : SPLIT ? step.a - step.t : step.a;
   const float by_v = KIND == kOrthGram ? kOrthSScale / (kOrthXScale * kOrthXScale) : KIND == kOrthPoly ? step.c * (kOrthBScale / (kOrthSScale * kOrthSScale)) : 1.f / kOrthBScale;
 #pragma unroll 1
   for (int turn = 0; turn < 2; ++turn) {
@@ -396,11 +398,12 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
 #pragma unroll
     for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(a[8 * sub + 2 * k]), __uint_as_float(a[8 * sub + 2 * k + 1]));
     orth_scale8(v, by_v);
-    if constexpr (KIND != kOrthGram) {
+    if constexpr (KIND == kOrthPoly || SPLIT && KIND == kOrthApply) {
       orth_add8(v, by_x, hrow + at);
-      if (kPair) orth_add8(v, by_x, lrow + at);
+      if (SPLIT) orth_add8(v, by_x, lrow + at);
       if (KIND == kOrthPoly && row0 == col0) orth_diagonal8(v, lane - 8 * g, step.t * kOrthBScale);
     }
+    if (!SPLIT && KIND == kOrthApply && !last) orth_add8(v, by_x, lrow + at);      // t = a: the hi part's share is in the product
     if (!last) {
       uint4 h, l;
       orth_round8<kPair>(v, h, l);
@@ -674,7 +677,8 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
         if (ask.w.more() && ahead < T::kRing) {
           const int to = loads % T::kRing;
           unsigned char* at = smem + T::kStrips + to * 2 * kOrthStripPart;
-          if (ask.w.kind() == kOrthGram) {
+          const bool apply = ask.w.kind() == kOrthApply;
+          if (ask.w.kind() == kOrthGram || (!SPLIT && apply && ask.w.step() == p.steps - 1)) {
             mbar_arrive_one(&strip_full[to]);
             ++loads;
             ask.next(rank);
@@ -683,11 +687,12 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
           // nothing of this block may stay unsent while it waits for what others compute from it
           const bool there = ahead > 0 ? orth_ready(ask.w) : orth_wait_ready(ask.w, &s_abort);
           if (there) {
-            const int parts = ask.w.kind() == kOrthApply || SPLIT ? 2 : 1;   // X is always a pair, S only in an fp32 context
-            const CUtensorMap* map = p.maps + static_cast<long long>(ask.w.t.mat) * kMapCount + (ask.w.kind() == kOrthPoly ? kMapS : kMapX0 + 2 * (ask.w.step() & 1));
+            // in a bf16 context S, and the lo part of X; in an fp32 context both parts of either
+            const int first = !SPLIT && apply ? 1 : 0, parts = SPLIT || apply ? 2 : 1;
+            const CUtensorMap* map = p.maps + static_cast<long long>(ask.w.t.mat) * kMapCount + (apply ? kMapX0 + 2 * (ask.w.step() & 1) : kMapS);
             const int row = ask.w.t.i * T::kTM + rank * 128, col = ask.w.t.j * T::kTN + ask.strip * 64;
-            mbar_expect_tx(&strip_full[to], parts * kOrthStripPart);
-            for (int part = 0; part < parts; ++part)
+            mbar_expect_tx(&strip_full[to], (parts - first) * kOrthStripPart);
+            for (int part = first; part < parts; ++part)
 #pragma unroll
               for (int h = 0; h < 2; ++h) tma_load_2d(at + part * kOrthStripPart + h * 8192, map + part, &strip_full[to], col, row + h * 64);
             ++loads;
@@ -699,7 +704,8 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
         if (!mbar_wait_bounded(&strip_done[b], parity)) { s_abort = 1; break; }
         const bool last = give.w.kind() == kOrthApply && give.w.step() == p.steps - 1;     // written to the result by the warps themselves
         if (!last) {
-          const int parts = give.w.kind() == kOrthApply || SPLIT ? 2 : 1;
+          // in a bf16 context the last step does without X's lo part
+          const int parts = SPLIT || (give.w.kind() == kOrthApply && give.w.step() < p.steps - 2) ? 2 : 1;
           const CUtensorMap* map = p.maps + static_cast<long long>(give.w.t.mat) * kMapCount +
                                    (give.w.kind() == kOrthGram ? kMapS : give.w.kind() == kOrthPoly ? kMapB : kMapX0 + 2 * ((give.w.step() & 1) ^ 1));
           const unsigned char* at = smem + T::kStrips + b * 2 * kOrthStripPart;
