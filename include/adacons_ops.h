@@ -35,7 +35,7 @@ extern "C" {
  *   eps      >= 0.  A matrix of zeros gives zeros when eps > 0.  Inf or NaN in a matrix give NaN in
  *            that matrix only.
  * adacons_orth_create allocates about 8 bytes per element of the matrices and 4 (bf16) or 8 (fp32) per
- * element of their short sides squared.
+ * element of their short sides squared; up to 19 MB more for a matrix whose long rows are split between blocks.
  * Errors: EINVAL, ELIMIT (a side beyond 2^18), ENOMEM, ECUDA, EARCH.
  */
 typedef struct adacons_orth adacons_orth;

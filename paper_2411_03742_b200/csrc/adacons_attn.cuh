@@ -499,11 +499,6 @@ template <int D> struct AttnDkvSmem {
   static constexpr uint32_t kBars = kTable + 2 * 4 * ADACONS_ATTN_SHORT_ROWS, kBytes = kBars + 256 + 1024;
 };
 
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(smem_addr(dst)), "l"(src), "r"(bytes), "r"(smem_addr(bar)) : "memory");
-}
-
 template <int D, bool BF16>
 __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo,
                                                const AttnParams& p, const int tile, const int kv_head, const int batch) {

@@ -52,6 +52,7 @@ struct OrthPlan {
   int cg = 1, workers = 1, mirrored = 1;
   std::vector<std::vector<OrthTile>> lists;
   double cycles = 0;                  // modelled time
+  int slots = 0;                      // partial sums of split products
 };
 
 // The simulation's costs, in cycles, measured on the kernel.  A stage (64 K elements): what a block's operands take to
@@ -59,9 +60,12 @@ struct OrthPlan {
 // others may read it: the strips' arithmetic (a pair's tile has four of them), the store, the fence, the counter, the look.
 // An fp32 context's mirror image is written from registers.
 struct OrthCosts {
-  double stage, strip, mirror, tail;
-  OrthCosts(bool split, int cg) : stage(split ? 1300 : cg == 2 ? 800 : 600), strip(split ? 1500 : 1300), mirror(split ? 6000 : 600), tail(6500) {}
+  double stage, strip, mirror, tail, add;
+  OrthCosts(bool split, int cg) : stage(split ? 1300 : cg == 2 ? 800 : 600), strip(split ? 1500 : 1300), mirror(split ? 6000 : 600), tail(6500), add(900) {}
 };
+constexpr int kPartStages = 4;        // the fewest stages of a part: below, adding it costs what it saves
+// Split products move more bytes, which the model does not see where every block loads: a plan with them has to be better by this.
+constexpr double kSplitGain = 0.96;
 
 // The matrices' turns.  Of what is ready, the product with the longest way to go comes first, so that all matrices advance
 // side by side; their iterates (8 bytes an element: a pair read, a pair written) then go through HBM in every product once
@@ -86,18 +90,36 @@ std::vector<int> turns(const std::vector<OrthMat>& mats, const std::vector<doubl
   return turn;
 }
 
-OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int cg, bool mirrored, int workers) {
+OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int cg, bool mirrored, int most_parts, int workers) {
   OrthPlan plan;
   plan.cg = cg;
   plan.mirrored = mirrored;
   const OrthCosts cost(split, cg);
   const int tm = 128 * cg, tn = 128 * cg, num = static_cast<int>(mats.size());
   struct Spot { int i, j; };
-  struct Product { std::vector<Spot> spots; unsigned stored = 0, before = 0; int depth = 0; double busy = 0, after = 0, way = 0; };   // after: last stage to readable; way: both
+  // after: from the last stage to readable; way: all of it.  A product split over K hands out, before its own tiles, those of
+  // the parts 1 .. parts - 1: `helpers` tiles stored, `handed` their way from last stage to readable, `adding` what adding them costs.
+  struct Product {
+    std::vector<Spot> spots;
+    unsigned stored = 0, helpers = 0, before = 0;
+    int depth = 0, parts = 1, part_depth = 0, slot = 0;
+    double busy = 0, after = 0, way = 0, handed = 0, adding = 0;
+    size_t tiles() const { return spots.size() * parts; }
+  };
   std::vector<Product> products(static_cast<size_t>(num) * 3);
   size_t most = 1;
-  for (int k = 0; k < num; ++k) {
-    unsigned before = 0;
+  // what depends on the number of parts: how long a part, and the way of all of it
+  auto cut = [&](Product& pr, int kind, int rows, int cols, int parts) {
+    const int live = std::min((cols + 63) / 64, tn / 64), stages = (pr.depth + kOrthTK - 1) / kOrthTK, part_stages = (stages + parts - 1) / parts;
+    pr.parts = (stages + part_stages - 1) / part_stages;
+    pr.part_depth = part_stages * kOrthTK;
+    pr.adding = (pr.parts - 1) * live * cost.add;
+    pr.busy = std::max(part_stages * cost.stage, tn / 64 * cost.strip + pr.adding);
+    pr.after = cost.tail + live * cost.strip + (kind != kOrthApply && mirrored && rows > tm ? cost.mirror : 0.0) + pr.adding;
+    pr.handed = cost.tail + live * cost.strip;
+    pr.way = pr.busy + pr.after + (pr.parts > 1 ? pr.handed : 0.0);
+  };
+  for (int k = 0; k < num; ++k)
     for (int kind = 0; kind < 3; ++kind) {
       Product& pr = products[3 * k + kind];
       const int rows = mats[k].r, cols = kind == kOrthApply ? mats[k].l : mats[k].r;
@@ -108,29 +130,50 @@ OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int c
           pr.spots.push_back({static_cast<int>(i), static_cast<int>(j)});
           for (int rank = 0; rank < cg; ++rank) pr.stored += i * tm + rank * 128 < rows;
         }
+      cut(pr, kind, rows, cols, 1);
+    }
+  // A Gram product is split no further than the longest matrix's step calls for, at its own best.
+  auto step = [&](int k) { return products[3 * k].way + products[3 * k + 1].way + products[3 * k + 2].way; };
+  auto most_of = [&](int k) {
+    const Product& pr = products[3 * k];
+    return std::min(most_parts, std::min(workers / static_cast<int>(pr.spots.size()), (pr.depth + kOrthTK - 1) / kOrthTK / kPartStages));
+  };
+  double longest = 0.0;
+  for (int k = 0; k < num; ++k) {
+    double best = step(k);
+    for (int parts = 2; parts <= most_of(k); ++parts) {
+      cut(products[3 * k], kOrthGram, mats[k].r, mats[k].r, parts);
+      best = std::min(best, step(k));
+    }
+    longest = std::max(longest, best);
+  }
+  std::vector<double> step_way(num, 0.0);
+  for (int k = 0; k < num; ++k) {
+    int parts = 1;
+    do cut(products[3 * k], kOrthGram, mats[k].r, mats[k].r, parts);
+    while (step(k) > longest && ++parts <= most_of(k));
+    step_way[k] = step(k);
+    unsigned before = 0;
+    for (int kind = 0; kind < 3; ++kind) {
+      Product& pr = products[3 * k + kind];
+      pr.helpers = pr.stored * (pr.parts - 1);
+      pr.slot = plan.slots;
+      plan.slots += static_cast<int>(pr.spots.size()) * (pr.parts - 1);
       pr.before = before;
-      before += pr.stored;
-      const int live = std::min((cols + 63) / 64, tn / 64);
-      pr.busy = std::max((pr.depth + kOrthTK - 1) / kOrthTK * cost.stage, tn / 64 * cost.strip);
-      pr.after = cost.tail + live * cost.strip + (kind != kOrthApply && mirrored && rows > tm ? cost.mirror : 0.0);
-      pr.way = pr.busy + pr.after;
-      most = std::max(most, pr.spots.size() * static_cast<size_t>(num));
+      before += pr.stored + pr.helpers;
+      most = std::max(most, pr.tiles() * static_cast<size_t>(num));
     }
   }
   plan.workers = static_cast<int>(std::min<size_t>(workers, most));
   plan.lists.resize(plan.workers);
-  std::vector<double> step_way(num, 0.0);
-  for (int k = 0; k < num; ++k)
-    for (int kind = 0; kind < 3; ++kind) step_way[k] += products[3 * k + kind].way;
-
-  struct Open { double at, way; int mat, step, kind; size_t next; double end; };       // a product that may start at `at`
+  struct Open { double at, way; int mat, step, kind; size_t next; double end, handed; };       // a product that may start at `at`; handed: when its parts are there
   auto sooner = [](const Open& x, const Open& y) { return x.at != y.at ? x.at > y.at : x.mat > y.mat; };
   const std::vector<int> turn = turns(mats, step_way);
   auto shorter = [&](const Open& x, const Open& y) {
     return turn[x.mat] != turn[y.mat] ? turn[x.mat] > turn[y.mat] : x.way != y.way ? x.way < y.way : x.mat > y.mat;
   };
   std::vector<Open> future, ready;     // heaps: the soonest, the one with the longest way to go
-  for (int k = 0; k < num; ++k) future.push_back({0.0, step_way[k] * steps, k, 0, 0, 0, 0.0});
+  for (int k = 0; k < num; ++k) future.push_back({0.0, step_way[k] * steps, k, 0, 0, 0, 0.0, 0.0});
   std::make_heap(future.begin(), future.end(), sooner);
   typedef std::pair<double, int> Free;                                                 // when, who
   std::vector<Free> idle;
@@ -148,15 +191,30 @@ OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int c
     }
     Open& open = ready.front();
     const Product& pr = products[3 * open.mat + open.kind];
-    const Spot spot = pr.spots[open.next++];
+    const int number = static_cast<int>(open.next % pr.spots.size()), part = (static_cast<int>(open.next / pr.spots.size()) + 1) % pr.parts;      // part 0, the tiles themselves, last
+    const Spot spot = pr.spots[number];
+    ++open.next;
     const OrthMat& m = mats[open.mat];
     const unsigned per_step = products[3 * open.mat + 2].before + products[3 * open.mat + 2].stored;
-    plan.lists[who.second].push_back({open.mat, spot.i, spot.j, pr.depth, m.r, open.kind == kOrthApply ? m.l : m.r, open.step * per_step + pr.before,
-                                      open.step * 4 + open.kind});
+    OrthTile tile = {};
+    tile.mat = open.mat;
+    tile.i = spot.i;
+    tile.j = spot.j;
+    tile.first = part * pr.part_depth;
+    tile.depth = std::min(pr.part_depth, pr.depth - tile.first);
+    tile.rows = m.r;
+    tile.cols = open.kind == kOrthApply ? m.l : m.r;
+    tile.needs = open.step * per_step + pr.before;
+    tile.ready = tile.needs + (part == 0 ? pr.helpers : 0);
+    tile.step_kind = open.step * 4 + (part == 0 ? open.kind : kOrthPart);
+    tile.adds = part == 0 ? pr.parts - 1 : 0;
+    tile.slot = pr.slot + number * (pr.parts - 1) + (part == 0 ? 0 : part - 1);
+    plan.lists[who.second].push_back(tile);
     who.first = std::max(who.first, open.at) + pr.busy;      // idle since before the product could start
-    open.end = std::max(open.end, who.first + pr.after);
+    if (part != 0) open.handed = std::max(open.handed, who.first + pr.handed);
+    else open.end = std::max(open.end, std::max(who.first, open.handed) + pr.after);
     std::push_heap(idle.begin(), idle.end(), std::greater<Free>());
-    if (open.next == pr.spots.size()) {
+    if (open.next == pr.tiles()) {
       Open then = open;
       std::pop_heap(ready.begin(), ready.end(), shorter);
       ready.pop_back();
@@ -164,6 +222,7 @@ OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int c
       then.at = then.end;
       then.way -= pr.way;
       then.next = 0;
+      then.handed = 0.0;
       if (++then.kind == 3) { then.kind = 0; ++then.step; }
       if (then.step < steps) {
         future.push_back(then);
@@ -174,19 +233,20 @@ OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int c
   return plan;
 }
 
-// The plan with the shortest simulated time: pairs or lone blocks, symmetric products mirrored or, where blocks
-// would idle, computed in full.  For vectors of many tiles only the first choice is tried.
+// The plan with the shortest simulated time: pairs or lone blocks, Gram products whole or split over K, symmetric products
+// mirrored or, where blocks would idle, computed in full.  For vectors of many tiles only the first choice is tried.
 OrthPlan choose_plan(const std::vector<OrthMat>& mats, bool split, int steps, int singles, int pairs) {
   double tiles = 0;
   for (const OrthMat& m : mats) tiles += 3.0 * ((m.r + 255) / 256) * ((m.l + 255) / 256);
   const bool many = tiles * steps > 40000;
-  OrthPlan best = simulate(mats, split, steps, split ? 1 : 2, true, split ? singles : pairs);
+  OrthPlan best = simulate(mats, split, steps, split ? 1 : 2, true, 1, split ? singles : pairs);
   for (int cg = split ? 1 : 2; !many && cg >= 1; --cg)
-    for (int mirrored = 1; mirrored >= 0; --mirrored) {
-      if (cg == best.cg && mirrored) continue;
-      OrthPlan plan = simulate(mats, split, steps, cg, mirrored != 0, cg == 2 ? pairs : singles);
-      if (plan.cycles < best.cycles) best = std::move(plan);
-    }
+    for (int parts = 1; parts <= 8; parts *= 2)
+      for (int mirrored = 1; mirrored >= 0; --mirrored) {
+        if (cg == best.cg && mirrored && parts == 1) continue;
+        OrthPlan plan = simulate(mats, split, steps, cg, mirrored != 0, parts, cg == 2 ? pairs : singles);
+        if (plan.cycles < (parts > 1 && best.slots == 0 ? kSplitGain : 1.0) * best.cycles) best = std::move(plan);
+      }
   return best;
 }
 
@@ -313,6 +373,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   const size_t at_load = a.take(load.size() * sizeof(OrthSpot)), at_chunks = a.take(chunks.size() * sizeof(OrthChunk));
   const size_t at_partial = a.take(chunks.size() * sizeof(double)), at_flags = a.take(sizeof(uint32_t));
   const size_t head = a.used;
+  const size_t at_sums = a.take(static_cast<size_t>(plan.slots) * plan.cg * 2 * plan.cg * 2 * kOrthStripPart);     // 2 cg strips of each of cg blocks
   std::vector<size_t> at(static_cast<size_t>(num) * kMapCount, 0);
   for (int k = 0; k < num && !c->small; ++k)
     for (int q = 0; q < kMapCount; ++q) {
@@ -364,6 +425,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   p.coeffs = reinterpret_cast<const OrthStep*>(c->memory + at_coeffs);
   p.done = reinterpret_cast<unsigned*>(c->memory + at_done);
   p.flags = reinterpret_cast<uint32_t*>(c->memory + at_flags);
+  p.sums = c->memory + at_sums;
   p.steps = steps;
   c->load_tiles = reinterpret_cast<const OrthSpot*>(c->memory + at_load);
   c->chunks = reinterpret_cast<const OrthChunk*>(c->memory + at_chunks);

@@ -41,7 +41,7 @@ constexpr int kOrthThreads = 352;        // warps 0-7 epilogue, 8 operand copies
 constexpr int kOrthNormChunk = 16384;    // elements per block of the norm kernel
 constexpr int kOrthLoadTile = 64, kOrthLoadCols = 256;
 
-enum OrthKind { kOrthGram = 0, kOrthPoly = 1, kOrthApply = 2 };
+enum OrthKind { kOrthGram = 0, kOrthPoly = 1, kOrthApply = 2, kOrthPart = 3 };     // part: of a Gram product split over K
 enum OrthMap { kMapX0 = 0, kMapX1 = 2, kMapS = 4, kMapB = 6, kMapCount = 8 };   // + 1: the lo part
 
 struct OrthMat {
@@ -60,10 +60,13 @@ struct OrthMat {
 struct OrthSpot { int mat, i, j; };           // load kernel: a tile of a matrix
 // One tile of one product, with all that the warps other than the epilogue's need to know of its matrix.
 struct __align__(16) OrthTile {
-  int mat, i, j, depth;    // depth: K elements
+  int mat, i, j, depth;    // depth: K elements, from `first` on
   int rows, cols;          // of the product: r x l or r x r
   unsigned needs;          // tiles of the matrix that the blocks must have stored before
   int step_kind;           // step * 4 + OrthKind
+  int first, adds;         // adds: partial sums that other tiles have of this one
+  int slot;                // where those are, one after the other, or where this part goes
+  unsigned ready;          // tiles that must have been stored before what the epilogue adds is there
 };
 struct OrthStep { float a, b, c, t; };         // t: what is added to B's diagonal
 struct OrthChunk { int mat; int first; };      // norm kernel: chunk number within the matrix
@@ -75,6 +78,7 @@ struct OrthParams {
   const int* begin;              // [workers + 1]
   const OrthStep* coeffs;        // [steps]
   unsigned* done;                // [matrix] blocks' tiles stored so far
+  unsigned char* sums;           // partial sums: [slot][block of a pair][strip], each strip as it lies in shared memory
   int mirrored;                  // symmetric products are computed on and below the diagonal only
   int steps;
   void* out;                     // the flat result
@@ -245,7 +249,9 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, int alig
 // device idle at every boundary, half of the time of one encoder layer.
 // The blocks wait for one another, so the launch is cooperative; each wait is bounded.
 //
-//   Gram   S = X X^T        both operands K-major, straight from X's rows
+//   Gram   S = X X^T        both operands K-major, straight from X's rows; on long rows of few tiles split over K: other
+//                           blocks bring the partial sums, in fp32, which the tile's epilogue adds in the parts' order
+//                           (64 x 4096 fp32 283 -> 135 us, eight of 16 x 4096 bf16 156 -> 115 us)
 //   Poly   B = b S + c S S + t I
 //   Apply  X' = (a - t) X + B X    the right operand is X again, MN-major: no transposed copy exists
 // S and S S are symmetric: where there is work for all, only tiles that reach the lower triangle are computed,
@@ -486,6 +492,50 @@ __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const Ort
   }
 }
 
+// Partial sums travel as strips of fp32 words, their upper and lower halves in the two parts of a place, so
+// that each thread reads what its own place in the product is.
+__device__ __forceinline__ void orth_part_out(uint32_t acc, unsigned char* hi, unsigned char* lo, int half) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll 1
+  for (int turn = 0; turn < 2; ++turn) {
+    uint32_t a[16];
+    tmem_ld16(acc + turn * 16, a);
+    tmem_wait_ld();
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      const int at = lane * 128 + ((4 * half + 2 * turn + sub) ^ (lane & 7)) * 16;
+      float2 v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = make_float2(__uint_as_float(a[8 * sub + 2 * k]), __uint_as_float(a[8 * sub + 2 * k + 1]));
+      uint4 u, d;
+      orth_halves8(v, u, d);
+      *reinterpret_cast<uint4*>(hi + at) = u;
+      *reinterpret_cast<uint4*>(lo + at) = d;
+    }
+  }
+}
+__device__ __forceinline__ void orth_part_in(uint32_t acc, const unsigned char* hi, const unsigned char* lo, int half) {
+  const int lane = threadIdx.x & 31;
+  uint32_t a[32];
+  tmem_ld32(acc, a);
+  tmem_wait_ld();
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int at = lane * 128 + ((4 * half + g) ^ (lane & 7)) * 16;
+    const uint4 u = *reinterpret_cast<const uint4*>(hi + at), d = *reinterpret_cast<const uint4*>(lo + at);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 s = add2(make_float2(__uint_as_float(a[8 * g + 2 * k]), __uint_as_float(a[8 * g + 2 * k + 1])),
+                            make_float2(__uint_as_float(__byte_perm(orth_word(d, k), orth_word(u, k), 0x5410)),
+                                        __uint_as_float(__byte_perm(orth_word(d, k), orth_word(u, k), 0x7632))));
+      a[8 * g + 2 * k] = __float_as_uint(s.x);
+      a[8 * g + 2 * k + 1] = __float_as_uint(s.y);
+    }
+  }
+  tmem_st32(acc, a);
+  tmem_wait_st();
+}
+
 // The tiles of one block in the order in which all of its warps go through them.  The next tile's record
 // is on its way while a tile is worked on.
 struct OrthWalk {
@@ -512,16 +562,16 @@ __device__ __forceinline__ unsigned orth_load_acquire(const unsigned* p) {
   return v;
 }
 // Whether what a product reads is there; the copies that follow are ordered behind the look.
-__device__ __forceinline__ bool orth_ready(const OrthWalk& w) {
-  if (orth_load_acquire(w.p.done + w.t.mat) < w.t.needs) return false;
+__device__ __forceinline__ bool orth_ready(const OrthWalk& w, unsigned tiles) {
+  if (orth_load_acquire(w.p.done + w.t.mat) < tiles) return false;
   asm volatile("fence.proxy.async.global;" ::: "memory");
   return true;
 }
-__device__ __forceinline__ bool orth_wait_ready(const OrthWalk& w, volatile int* s_abort) {
-  if (orth_ready(w)) return true;
+__device__ __forceinline__ bool orth_wait_ready(const OrthWalk& w, unsigned tiles, volatile int* s_abort) {
+  if (orth_ready(w, tiles)) return true;
   const unsigned long long t0 = global_timer_ns();
   while (!*s_abort) {
-    if (orth_ready(w)) return true;
+    if (orth_ready(w, tiles)) return true;
     __nanosleep(40);
     if (global_timer_ns() - t0 > kWaitLimitNs) return false;
   }
@@ -573,12 +623,12 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
       for (OrthWalk w(p, worker); ok && w.more(); w.next()) {
         const CUtensorMap* maps = p.maps + static_cast<long long>(w.t.mat) * kMapCount;
         const CUtensorMap* x_map = maps + kMapX0 + 2 * (w.step() & 1);
-        const CUtensorMap* ma = w.kind() == kOrthGram ? x_map : w.kind() == kOrthPoly ? maps + kMapS : maps + kMapB;
+        const CUtensorMap* ma = w.kind() == kOrthPoly ? maps + kMapS : w.kind() == kOrthApply ? maps + kMapB : x_map;
         const CUtensorMap* mb = w.kind() == kOrthPoly ? maps + kMapS : x_map;
         const bool across = w.kind() == kOrthApply;                           // the right operand's K runs along its rows
         const int arow = w.t.i * T::kTM + rank * 128, brow = w.t.j * T::kTN + rank * T::kBRows;
-        if (!orth_wait_ready(w, &s_abort)) { s_abort = 1; break; }
-        for (int k0 = 0; k0 < w.t.depth; k0 += kOrthTK) {
+        if (!orth_wait_ready(w, w.t.needs, &s_abort)) { s_abort = 1; break; }
+        for (int k0 = w.t.first; k0 < w.t.first + w.t.depth; k0 += kOrthTK) {
           if (s_abort || !mbar_wait_bounded(&empty[stage], parity)) { s_abort = 1; ok = false; break; }
           unsigned char* at = smem + stage * T::kStage;
           if (rank == 0) mbar_expect_tx(&full[stage], CG * T::kStage);      // the pair's bytes all count on the even block's barrier
@@ -655,10 +705,11 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
     }
   } else if (warp == 10) {
     if (lane == 0) {
-      // `ask` brings strips, at most kRing of them ahead of `give`, which sends them off
+      // `ask` brings strips, at most kRing of them ahead of `give`, which sends them off.  A strip with partial sums to
+      // add takes a turn for each of them before its own.
       struct Strips {
         OrthWalk w;
-        int strip, live;
+        int strip, live, turn = 0;
         __device__ __forceinline__ Strips(const OrthParams& p, int worker, int rank) : w(p, worker) { open(rank); }
         __device__ __forceinline__ void open(int rank) {                   // the next tile that has strips here
           for (; w.more(); w.next()) {
@@ -667,7 +718,15 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
             if (live > 0) return;
           }
         }
-        __device__ __forceinline__ void next(int rank) { if (++strip == live) { w.next(); open(rank); } }
+        __device__ __forceinline__ void next(int rank) {
+          if (turn++ < w.t.adds) return;
+          turn = 0;
+          if (++strip == live) { w.next(); open(rank); }
+        }
+        __device__ __forceinline__ bool adds() const { return turn < w.t.adds; }
+        __device__ __forceinline__ unsigned char* sum(int slot, int rank) const {
+          return w.p.sums + (static_cast<size_t>(slot * CG + rank) * T::kBlocks + strip) * (2 * kOrthStripPart);
+        }
       };
       Strips ask(p, worker, rank), give(p, worker, rank);
       int loads = 0, stored = 0, b = 0;
@@ -678,14 +737,21 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
           const int to = loads % T::kRing;
           unsigned char* at = smem + T::kStrips + to * 2 * kOrthStripPart;
           const bool apply = ask.w.kind() == kOrthApply;
-          if (ask.w.kind() == kOrthGram || (!SPLIT && apply && ask.w.step() == p.steps - 1)) {
+          if (((ask.w.kind() == kOrthGram || ask.w.kind() == kOrthPart) && !ask.adds()) || (!SPLIT && apply && ask.w.step() == p.steps - 1)) {
             mbar_arrive_one(&strip_full[to]);
             ++loads;
             ask.next(rank);
             continue;
           }
           // nothing of this block may stay unsent while it waits for what others compute from it
-          const bool there = ahead > 0 ? orth_ready(ask.w) : orth_wait_ready(ask.w, &s_abort);
+          const bool there = ahead > 0 ? orth_ready(ask.w, ask.w.t.ready) : orth_wait_ready(ask.w, ask.w.t.ready, &s_abort);
+          if (there && ask.adds()) {
+            mbar_expect_tx(&strip_full[to], 2 * kOrthStripPart);
+            bulk_load(at, ask.sum(ask.w.t.slot + ask.turn, rank), 2 * kOrthStripPart, &strip_full[to]);
+            ++loads;
+            ask.next(rank);
+            continue;
+          }
           if (there) {
             // in a bf16 context S, and the lo part of X; in an fp32 context both parts of either
             const int first = !SPLIT && apply ? 1 : 0, parts = SPLIT || apply ? 2 : 1;
@@ -703,18 +769,22 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
         }
         if (!mbar_wait_bounded(&strip_done[b], parity)) { s_abort = 1; break; }
         const bool last = give.w.kind() == kOrthApply && give.w.step() == p.steps - 1;     // written to the result by the warps themselves
-        if (!last) {
+        if (!last && !give.adds()) {
           // in a bf16 context the last step does without X's lo part
           const int parts = SPLIT || (give.w.kind() == kOrthApply && give.w.step() < p.steps - 2) ? 2 : 1;
           const CUtensorMap* map = p.maps + static_cast<long long>(give.w.t.mat) * kMapCount +
                                    (give.w.kind() == kOrthGram ? kMapS : give.w.kind() == kOrthPoly ? kMapB : kMapX0 + 2 * ((give.w.step() & 1) ^ 1));
           const unsigned char* at = smem + T::kStrips + b * 2 * kOrthStripPart;
           const int row = give.w.t.i * T::kTM + rank * 128, col = give.w.t.j * T::kTN + give.strip * 64;
-          for (int part = 0; part < parts; ++part)
+          if (give.w.kind() == kOrthPart) {
+            bulk_store(give.sum(give.w.t.slot, rank), at, 2 * kOrthStripPart);
+          } else {
+            for (int part = 0; part < parts; ++part)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-              if (row + h * 64 < give.w.t.rows) tma_store_2d(map + part, at + part * kOrthStripPart + h * 8192, col, row + h * 64);
-          if (!SPLIT && p.mirrored && give.w.kind() != kOrthApply && give.w.t.i > give.w.t.j) {      // the mirror image
+              for (int h = 0; h < 2; ++h)
+                if (row + h * 64 < give.w.t.rows) tma_store_2d(map + part, at + part * kOrthStripPart + h * 8192, col, row + h * 64);
+          }
+          if (!SPLIT && p.mirrored && (give.w.kind() == kOrthGram || give.w.kind() == kOrthPoly) && give.w.t.i > give.w.t.j) {      // the mirror image
 #pragma unroll
             for (int h = 0; h < 2; ++h)
               if (row + h * 64 < give.w.t.rows) tma_store_2d(map, at + kOrthStripPart + h * 8192, row + h * 64, col);
@@ -752,24 +822,36 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
       buf ^= 1;
       if (buf == 0) parity ^= 1u;
     };
+    auto used = [&]() {                                    // this warp is through with a place
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_one(&strip_done[place]);
+      if (++place == T::kRing) { place = 0; strip_parity ^= 1u; }
+    };
     auto finish = [&](const OrthWalk& w, const OrthStep& step, const OrthView& m, int strip, uint32_t acc) {
       if (!wait_for(&strip_full[place], strip_parity)) return false;
       unsigned char* at = smem + T::kStrips + place * 2 * kOrthStripPart + (warp & 3) * 32 * 128;
       const int row0 = w.t.i * T::kTM + rank * 128 + (warp & 3) * 32, col0 = w.t.j * T::kTN + strip * 64 + half * 32;
       const bool last = w.step() == p.steps - 1;
-      if (w.kind() == kOrthGram) orth_finish_block<kOrthGram, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
+      if (w.kind() == kOrthPart) orth_part_out(acc, at, at + kOrthStripPart, half);
+      else if (w.kind() == kOrthGram) orth_finish_block<kOrthGram, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
       else if (w.kind() == kOrthPoly) orth_finish_block<kOrthPoly, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
       else orth_finish_block<kOrthApply, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_one(&strip_done[place]);
-      if (++place == T::kRing) { place = 0; strip_parity ^= 1u; }
+      used();
       return true;
     };
     auto finish_tile = [&](const OrthWalk& w, const OrthStep& step, const OrthView& m, int live, uint32_t base) {
 #pragma unroll 1
-      for (int s = 0; s < live; ++s)
+      for (int s = 0; s < live; ++s) {
+#pragma unroll 1
+        for (int n = 0; n < w.t.adds; ++n) {               // in the parts' order, whoever is first
+          if (!wait_for(&strip_full[place], strip_parity)) return false;
+          const unsigned char* at = smem + T::kStrips + place * 2 * kOrthStripPart + (warp & 3) * 32 * 128;
+          orth_part_in(base + s * 64, at, at + kOrthStripPart, half);
+          used();
+        }
         if (!finish(w, step, m, s, base + s * 64)) return false;
+      }
       return true;
     };
     bool ok = true;

@@ -84,6 +84,17 @@ def test_enough_tiles_for_pairs_of_blocks():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shapes", [[(1, 100003)], [(29, 3381)], [(4096, 64)], [(130, 4001)], [(300, 5000), (40, 40)], [(16, 4096)] * 8 + [(2051, 17)]])
+def test_long_rows_split_over_their_length(dtype, shapes):
+    out = run(shapes, dtype, gap=3)
+    assert torch.equal(out, run(shapes, dtype, gap=3)), "partial sums are added in one order"
+
+
+def test_vectors_larger_than_the_cache_go_in_turns():
+    run([(1024, 4096)] * 8 + [(2000, 1000)] * 10, "bf16", gap=8)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_in_place_and_scaling(dtype):
     run([(200, 96), (96, 200)], dtype, gap=1, in_place=True)
     run([(200, 96), (96, 200)], dtype, scaling=True)
