@@ -90,7 +90,8 @@ std::vector<int> turns(const std::vector<OrthMat>& mats, const std::vector<doubl
   return turn;
 }
 
-OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int cg, bool mirrored, int most_parts, int workers) {
+// Plans that cannot be shorter than `limit` are given up before their lists are made.
+OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int cg, bool mirrored, int most_parts, int workers, double limit) {
   OrthPlan plan;
   plan.cg = cg;
   plan.mirrored = mirrored;
@@ -165,6 +166,11 @@ OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int c
     }
   }
   plan.workers = static_cast<int>(std::min<size_t>(workers, most));
+  double busy = 0.0;                                       // of all workers: no plan is shorter than their even share
+  for (const Product& pr : products) busy += pr.busy * pr.tiles();
+  plan.cycles = steps * busy / plan.workers;
+  if (plan.cycles >= limit) return plan;
+  plan.cycles = 0.0;
   plan.lists.resize(plan.workers);
   struct Open { double at, way; int mat, step, kind; size_t next; double end, handed; };       // a product that may start at `at`; handed: when its parts are there
   auto sooner = [](const Open& x, const Open& y) { return x.at != y.at ? x.at > y.at : x.mat > y.mat; };
@@ -239,13 +245,14 @@ OrthPlan choose_plan(const std::vector<OrthMat>& mats, bool split, int steps, in
   double tiles = 0;
   for (const OrthMat& m : mats) tiles += 3.0 * ((m.r + 255) / 256) * ((m.l + 255) / 256);
   const bool many = tiles * steps > 40000;
-  OrthPlan best = simulate(mats, split, steps, split ? 1 : 2, true, 1, split ? singles : pairs);
+  OrthPlan best = simulate(mats, split, steps, split ? 1 : 2, true, 1, split ? singles : pairs, 1e300);
   for (int cg = split ? 1 : 2; !many && cg >= 1; --cg)
     for (int parts = 1; parts <= 8; parts *= 2)
       for (int mirrored = 1; mirrored >= 0; --mirrored) {
         if (cg == best.cg && mirrored && parts == 1) continue;
-        OrthPlan plan = simulate(mats, split, steps, cg, mirrored != 0, parts, cg == 2 ? pairs : singles);
-        if (plan.cycles < (parts > 1 && best.slots == 0 ? kSplitGain : 1.0) * best.cycles) best = std::move(plan);
+        const double limit = (parts > 1 && best.slots == 0 ? kSplitGain : 1.0) * best.cycles;
+        OrthPlan plan = simulate(mats, split, steps, cg, mirrored != 0, parts, cg == 2 ? pairs : singles, limit);
+        if (plan.cycles < limit) best = std::move(plan);
       }
   return best;
 }
