@@ -734,7 +734,11 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
       while (give.w.more() && !s_abort) {
         const int ahead = loads - stored;
         if (ask.w.more() && ahead < T::kRing) {
-          const int to = loads % T::kRing;
+          // the strip that was here has been sent: every strip is a group, and `pending` of them left after it
+          const int to = loads % T::kRing, pending = T::kRing - 1 - ahead;
+          if (pending == 0) bulk_wait_read<0>();
+          else if (pending == 1) bulk_wait_read<1>();
+          else bulk_wait_read<2>();
           unsigned char* at = smem + T::kStrips + to * 2 * kOrthStripPart;
           const bool apply = ask.w.kind() == kOrthApply;
           if (((ask.w.kind() == kOrthGram || ask.w.kind() == kOrthPart) && !ask.adds()) || (!SPLIT && apply && ask.w.step() == p.steps - 1)) {
@@ -789,14 +793,12 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
             for (int h = 0; h < 2; ++h)
               if (row + h * 64 < give.w.t.rows) tma_store_2d(map, at + kOrthStripPart + h * 8192, row + h * 64, col);
           }
-          bulk_commit();
-          if (give.strip == give.live - 1) {               // the tile is complete: say so once its bytes are
-            bulk_wait<0>();
-            asm volatile("fence.proxy.async.global;" ::: "memory");
-            asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.done + give.w.t.mat) : "memory");
-          } else {
-            bulk_wait_read<0>();
-          }
+        }
+        bulk_commit();
+        if (!last && !give.adds() && give.strip == give.live - 1) {      // the tile is complete: say so once its bytes are
+          bulk_wait<0>();
+          asm volatile("fence.proxy.async.global;" ::: "memory");
+          asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.done + give.w.t.mat) : "memory");
         }
         ++stored;
         give.next(rank);
