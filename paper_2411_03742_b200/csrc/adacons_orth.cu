@@ -26,7 +26,7 @@ struct adacons_orth {
   const OrthChunk* chunks = nullptr;
   double* partial = nullptr;
   OrthParams params = {};             // all but the result's address
-  int cg = 1, blocks = 0;
+  int cg = 1, tn = 128, blocks = 0;
   bool small = false;                 // all matrices fit the one-block kernel
   int num_load = 0, num_chunks = 0, num_mats = 0;
   int64_t launches = 0;
@@ -49,7 +49,7 @@ struct Arena {                        // offsets first, pointers once the alloca
 
 // Who computes which tile when: one list of tiles per worker (a block, or a pair of them).
 struct OrthPlan {
-  int cg = 1, workers = 1, mirrored = 1;
+  int cg = 1, tn = 128, workers = 1, mirrored = 1;
   std::vector<std::vector<OrthTile>> lists;
   double cycles = 0;                  // modelled time
   int slots = 0;                      // partial sums of split products
@@ -60,8 +60,8 @@ struct OrthPlan {
 // others may read it: the strips' arithmetic (a pair's tile has four of them), the store, the fence, the counter, the look.
 // An fp32 context's mirror image is written from registers.
 struct OrthCosts {
-  double stage, strip, mirror, tail, add;
-  OrthCosts(bool split, int cg) : stage(split ? 1300 : cg == 2 ? 800 : 600), strip(split ? 1500 : 1300), mirror(split ? 6000 : 600), tail(6500), add(900) {}
+  double stage, strip, mirror, tail, add, crowd;      // crowd: of the workers' mean busy time, what they take from one another where all load
+  OrthCosts(bool split, int cg, int tn) : stage((split ? 1300 : cg == 2 ? 800 : 600) * (tn == 64 ? 0.75 : 1.0)), strip(split ? 1500 : 1300), mirror(split ? 6000 : 600), tail(6500), add(900), crowd(cg == 2 ? 0.1 : 0.3) {}
 };
 constexpr int kPartStages = 4;        // the fewest stages of a part: below, adding it costs what it saves
 // Split products move more bytes, which the model does not see where every block loads: a plan with them has to be better by this.
@@ -91,12 +91,13 @@ std::vector<int> turns(const std::vector<OrthMat>& mats, const std::vector<doubl
 }
 
 // Plans that cannot be shorter than `limit` are given up before their lists are made.
-OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int cg, bool mirrored, int most_parts, int workers, double limit) {
+OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int cg, int tn, bool mirrored, int most_parts, int workers, double limit) {
   OrthPlan plan;
   plan.cg = cg;
+  plan.tn = tn;
   plan.mirrored = mirrored;
-  const OrthCosts cost(split, cg);
-  const int tm = 128 * cg, tn = 128 * cg, num = static_cast<int>(mats.size());
+  const OrthCosts cost(split, cg, tn);
+  const int tm = 128 * cg, num = static_cast<int>(mats.size());
   struct Spot { int i, j; };
   // after: from the last stage to readable; way: all of it.  A product split over K hands out, before its own tiles, those of
   // the parts 1 .. parts - 1: `helpers` tiles stored, `handed` their way from last stage to readable, `adding` what adding them costs.
@@ -168,9 +169,10 @@ OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int c
   plan.workers = static_cast<int>(std::min<size_t>(workers, most));
   double busy = 0.0;                                       // of all workers: no plan is shorter than their even share
   for (const Product& pr : products) busy += pr.busy * pr.tiles();
-  plan.cycles = steps * busy / plan.workers;
+  const double share = steps * busy / plan.workers, crowd = cost.crowd * share;
+  plan.cycles = share + crowd;
   if (plan.cycles >= limit) return plan;
-  plan.cycles = 0.0;
+  plan.cycles = crowd;
   plan.lists.resize(plan.workers);
   struct Open { double at, way; int mat, step, kind; size_t next; double end, handed; };       // a product that may start at `at`; handed: when its parts are there
   auto sooner = [](const Open& x, const Open& y) { return x.at != y.at ? x.at > y.at : x.mat > y.mat; };
@@ -224,7 +226,7 @@ OrthPlan simulate(const std::vector<OrthMat>& mats, bool split, int steps, int c
       Open then = open;
       std::pop_heap(ready.begin(), ready.end(), shorter);
       ready.pop_back();
-      plan.cycles = std::max(plan.cycles, then.end);
+      plan.cycles = std::max(plan.cycles, then.end + crowd);
       then.at = then.end;
       then.way -= pr.way;
       then.next = 0;
@@ -245,23 +247,26 @@ OrthPlan choose_plan(const std::vector<OrthMat>& mats, bool split, int steps, in
   double tiles = 0;
   for (const OrthMat& m : mats) tiles += 3.0 * ((m.r + 255) / 256) * ((m.l + 255) / 256);
   const bool many = tiles * steps > 40000;
-  OrthPlan best = simulate(mats, split, steps, split ? 1 : 2, true, 1, split ? singles : pairs, 1e300);
-  for (int cg = split ? 1 : 2; !many && cg >= 1; --cg)
-    for (int parts = 1; parts <= 8; parts *= 2)
-      for (int mirrored = 1; mirrored >= 0; --mirrored) {
-        if (cg == best.cg && mirrored && parts == 1) continue;
-        const double limit = (parts > 1 && best.slots == 0 ? kSplitGain : 1.0) * best.cycles;
-        OrthPlan plan = simulate(mats, split, steps, cg, mirrored != 0, parts, cg == 2 ? pairs : singles, limit);
-        if (plan.cycles < limit) best = std::move(plan);
-      }
+  struct Tiling { int cg, tn; bool mirrored; };
+  std::vector<Tiling> tilings = {{1, 128, true}, {1, 128, false}, {1, 64, false}};
+  if (!split) tilings.insert(tilings.begin(), {{2, 256, true}, {2, 256, false}});
+  if (many) tilings.resize(1);
+  OrthPlan best;
+  best.cycles = 1e300;
+  for (int parts = 1; parts <= (many ? 1 : 8); parts *= 2)
+    for (const Tiling& t : tilings) {
+      const double limit = (parts > 1 && best.slots == 0 ? kSplitGain : 1.0) * best.cycles;
+      OrthPlan plan = simulate(mats, split, steps, t.cg, t.tn, t.mirrored, parts, t.cg == 2 ? pairs : singles, limit);
+      if (plan.cycles < limit) best = std::move(plan);
+    }
   return best;
 }
 
-template <bool SPLIT, int CG>
+template <bool SPLIT, int CG, int TN>
 int prepare_kernel(int sms, int* workers) {
-  using T = OrthTiling<SPLIT, CG>;
+  using T = OrthTiling<SPLIT, CG, TN>;
   static_assert(T::kBytes <= 227 * 1024, "shared memory of a block");
-  auto* kernel = &orth_steps_kernel<SPLIT, CG>;
+  auto* kernel = &orth_steps_kernel<SPLIT, CG, TN>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, T::kBytes) != cudaSuccess) { cudaGetLastError(); return ADACONS_ECUDA; }
   if (CG == 1) {
     *workers = sms;                   // one block an SM fits: its shared memory is checked above
@@ -291,9 +296,9 @@ int prepare_small() {
   return ADACONS_ECUDA;
 }
 
-template <bool SPLIT, int CG>
+template <bool SPLIT, int CG, int TN>
 bool launch_steps(const adacons_orth* c, const OrthParams& p, cudaStream_t st) {
-  return launch(&orth_steps_kernel<SPLIT, CG>, dim3(c->blocks), dim3(kOrthThreads), OrthTiling<SPLIT, CG>::kBytes, st, kLaunchCooperative, CG, p);
+  return launch(&orth_steps_kernel<SPLIT, CG, TN>, dim3(c->blocks), dim3(kOrthThreads), OrthTiling<SPLIT, CG, TN>::kBytes, st, kLaunchCooperative, CG, p);
 }
 
 int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* rows, const int64_t* cols, const int64_t* offsets, int scaling,
@@ -316,8 +321,9 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   if (rc != ADACONS_OK) return rc;
   const bool split = dtype == ADACONS_F32;
   int singles = 0, pairs = 0;
-  rc = split ? prepare_kernel<true, 1>(dev.sms, &singles) : prepare_kernel<false, 1>(dev.sms, &singles);
-  if (rc == ADACONS_OK && !split) rc = prepare_kernel<false, 2>(dev.sms, &pairs);
+  rc = split ? prepare_kernel<true, 1, 128>(dev.sms, &singles) : prepare_kernel<false, 1, 128>(dev.sms, &singles);
+  if (rc == ADACONS_OK) rc = split ? prepare_kernel<true, 1, 64>(dev.sms, &singles) : prepare_kernel<false, 1, 64>(dev.sms, &singles);
+  if (rc == ADACONS_OK && !split) rc = prepare_kernel<false, 2, 256>(dev.sms, &pairs);
   if (rc == ADACONS_OK) rc = split ? prepare_small<true>() : prepare_small<false>();
   if (rc != ADACONS_OK) return rc;
 
@@ -356,6 +362,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   for (const OrthMat& m : mats) c->small = c->small && m.r <= kOrthSmallR && m.l <= kOrthSmallL;
   const OrthPlan plan = c->small ? OrthPlan() : choose_plan(mats, split, steps, singles, pairs);
   c->cg = plan.cg;
+  c->tn = plan.tn;
   c->blocks = plan.workers * plan.cg;
   std::vector<OrthTile> tiles;
   std::vector<int> begin(1, 0);
@@ -380,7 +387,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   const size_t at_load = a.take(load.size() * sizeof(OrthSpot)), at_chunks = a.take(chunks.size() * sizeof(OrthChunk));
   const size_t at_partial = a.take(chunks.size() * sizeof(double)), at_flags = a.take(sizeof(uint32_t));
   const size_t head = a.used;
-  const size_t at_sums = a.take(static_cast<size_t>(plan.slots) * plan.cg * 2 * plan.cg * 2 * kOrthStripPart);     // 2 cg strips of each of cg blocks
+  const size_t at_sums = a.take(static_cast<size_t>(plan.slots) * plan.cg * (plan.tn / 64) * 2 * kOrthStripPart);     // the strips of each of cg blocks
   std::vector<size_t> at(static_cast<size_t>(num) * kMapCount, 0);
   for (int k = 0; k < num && !c->small; ++k)
     for (int q = 0; q < kMapCount; ++q) {
@@ -478,11 +485,11 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
   } else if (c->dtype == ADACONS_F32) {
     ok = launch(&orth_norm_kernel<0>, dim3(c->num_chunks), dim3(256), 0, st, kLaunchPlain, 1, update, aligned, p.mats, c->chunks, c->partial) &&
          launch(&orth_load_kernel<0>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, aligned, p.mats, c->load_tiles, partial, c->eps, p.done, c->num_mats) &&
-         launch_steps<true, 1>(c, p, st);
+         (c->tn == 128 ? launch_steps<true, 1, 128>(c, p, st) : launch_steps<true, 1, 64>(c, p, st));
   } else {
     ok = launch(&orth_norm_kernel<1>, dim3(c->num_chunks), dim3(256), 0, st, kLaunchPlain, 1, update, aligned, p.mats, c->chunks, c->partial) &&
          launch(&orth_load_kernel<1>, dim3(c->num_load), dim3(256), 0, st, kLaunchOverlap, 1, update, aligned, p.mats, c->load_tiles, partial, c->eps, p.done, c->num_mats) &&
-         (c->cg == 2 ? launch_steps<false, 2>(c, p, st) : launch_steps<false, 1>(c, p, st));
+         (c->cg == 2 ? launch_steps<false, 2, 256>(c, p, st) : c->tn == 128 ? launch_steps<false, 1, 128>(c, p, st) : launch_steps<false, 1, 64>(c, p, st));
   }
   return ok ? ADACONS_OK : ADACONS_ECUDA;
 }

@@ -260,7 +260,9 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, int alig
 // Tiles.  CG = 2: a pair of blocks (two SMs) shares a tile of 256 x TN; each holds 128 rows of the left
 // operand, half of the right one and 128 rows of the result, so that an operand byte from L2 feeds
 // twice the products of a single block's tile.  CG = 1: 128 x 128, for problems with too few tiles to occupy the device, and
-// for fp32 contexts, whose three products a stage need no more of the operands than arrives (pairs were no faster there).
+// for fp32 contexts, whose three products a stage need no more of the operands than arrives (pairs were no faster there);
+// or 128 x 64, where blocks would idle all the same: what bounds such a matrix is its chain of products, three quarters of
+// the operands to wait for and one strip instead of two (256 x 512 bf16 91 -> 78 us, fp32 136 -> 110 us).
 // In each block one warp copies operand stages by TMA, one thread (of the even block) issues the
 // tcgen05 products into one of two TMEM accumulators, and eight warps drain the other.
 //
@@ -273,9 +275,9 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, int alig
 // where the lanes of a warp are neighbours).  Written to global memory two bytes a lane, they cost a phase 13,000 cycles.
 // ----------------------------------------------------------------------------------------------
 constexpr uint32_t kOrthStripPart = 128 * 128;   // 128 rows x 64 fp16 values: two boxes of 64 swizzled rows
-template <bool SPLIT, int CG> struct OrthTiling {
+template <bool SPLIT, int CG, int TN> struct OrthTiling {
   static_assert(!SPLIT || CG == 1, "fp32 contexts use lone blocks");
-  static constexpr int kTM = 128 * CG, kTN = 128 * CG;
+  static constexpr int kTM = 128 * CG, kTN = TN;
   static constexpr int kParts = SPLIT ? 2 : 1;
   static constexpr int kBRows = kTN / CG;                            // of the right operand, in each block
   static constexpr uint32_t kA = 128 * kOrthTK * 2, kB = kBRows * kOrthTK * 2;
@@ -286,13 +288,13 @@ template <bool SPLIT, int CG> struct OrthTiling {
   static constexpr uint32_t kBars = kStrips + kRing * 2 * kOrthStripPart;
   static constexpr uint32_t kBytes = kBars + 256 + 1024;             // + alignment of the base
   static constexpr int kBlocks = kTN / 64;                           // strips of a tile
-  static constexpr uint32_t kTmemCols = SPLIT ? 512 : 2 * kTN;       // big[2] (small[2])
+  static constexpr uint32_t kTmemCols = (SPLIT ? 4 : 2) * kTN;       // big[2] (small[2])
 };
 
 // What of a tile exists: strips with columns inside the matrix, none for a block without rows.
-template <bool SPLIT, int CG>
+template <bool SPLIT, int CG, int TN>
 __device__ __forceinline__ int orth_live_strips(const OrthTile& t, int rank) {
-  using T = OrthTiling<SPLIT, CG>;
+  using T = OrthTiling<SPLIT, CG, TN>;
   if (t.i * T::kTM + rank * 128 >= t.rows) return 0;
   const int left = (t.cols - t.j * T::kTN + 63) / 64;
   return left < T::kBlocks ? left : T::kBlocks;
@@ -376,10 +378,10 @@ struct OrthView {
 // tensor memory at `acc`.  hi / lo: the block's place in the strip, `half` selecting its 64 bytes of each 128-byte row.
 // A loop of 16 columns and not unrolled code for 32: every product of a small matrix runs this once, and
 // fetching the longer code took 3000 to 6000 cycles of it.  (With 8 columns a turn large matrices lose a tenth to the waits.)
-template <int KIND, bool SPLIT, int CG>
+template <int KIND, bool SPLIT, int CG, int TN>
 __device__ __forceinline__ void orth_finish_block(const OrthParams& p, const OrthStep& step, bool last_step, const OrthView& m, int row0, int col0, uint32_t acc,
                                                   unsigned char* hi, unsigned char* lo, int half) {
-  using T = OrthTiling<SPLIT, CG>;
+  using T = OrthTiling<SPLIT, CG, TN>;
   const int lane = threadIdx.x & 31;
   const int r = m.r, ncols = m.cols, row = row0 + lane;
   const bool last = KIND == kOrthApply && last_step;
@@ -578,10 +580,10 @@ __device__ __forceinline__ bool orth_wait_ready(const OrthWalk& w, unsigned tile
   return false;
 }
 
-template <bool SPLIT, int CG>
+template <bool SPLIT, int CG, int TN>
 __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthParams p) {
   extern __shared__ unsigned char smem_dyn[];
-  using T = OrthTiling<SPLIT, CG>;
+  using T = OrthTiling<SPLIT, CG, TN>;
   unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + T::kBars);
   uint64_t* empty = full + T::kStages;
@@ -713,7 +715,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
         __device__ __forceinline__ Strips(const OrthParams& p, int worker, int rank) : w(p, worker) { open(rank); }
         __device__ __forceinline__ void open(int rank) {                   // the next tile that has strips here
           for (; w.more(); w.next()) {
-            live = orth_live_strips<SPLIT, CG>(w.t, rank);
+            live = orth_live_strips<SPLIT, CG, TN>(w.t, rank);
             strip = 0;
             if (live > 0) return;
           }
@@ -836,9 +838,9 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
       const int row0 = w.t.i * T::kTM + rank * 128 + (warp & 3) * 32, col0 = w.t.j * T::kTN + strip * 64 + half * 32;
       const bool last = w.step() == p.steps - 1;
       if (w.kind() == kOrthPart) orth_part_out(acc, at, at + kOrthStripPart, half);
-      else if (w.kind() == kOrthGram) orth_finish_block<kOrthGram, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
-      else if (w.kind() == kOrthPoly) orth_finish_block<kOrthPoly, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
-      else orth_finish_block<kOrthApply, SPLIT, CG>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
+      else if (w.kind() == kOrthGram) orth_finish_block<kOrthGram, SPLIT, CG, TN>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
+      else if (w.kind() == kOrthPoly) orth_finish_block<kOrthPoly, SPLIT, CG, TN>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
+      else orth_finish_block<kOrthApply, SPLIT, CG, TN>(p, step, last, m, row0, col0, acc, at, at + kOrthStripPart, half);
       used();
       return true;
     };
@@ -860,7 +862,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
     for (OrthWalk w(p, worker); ok && w.more(); w.next()) {
       const OrthView m(p, w.t);
       const OrthStep step = p.coeffs[w.step()];
-      const int live = orth_live_strips<SPLIT, CG>(w.t, rank);
+      const int live = orth_live_strips<SPLIT, CG, TN>(w.t, rank);
       if (!SPLIT) {
         if (!wait_for(&acc_full[buf], parity)) break;
         tc_fence_after();
