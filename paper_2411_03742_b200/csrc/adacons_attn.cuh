@@ -27,6 +27,7 @@ namespace adacons {
 // inputs' 16-bit type as operands of the second products, an error of the size of the results' own rounding.
 // ----------------------------------------------------------------------------------------------
 constexpr int kAttnTile = 128;
+constexpr int kFwdThreads = 320;                 // warps 0-7 softmax, 8 copies, 9 products
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct AttnOut { void* p; long long batch, seq, head; };     // element strides
@@ -36,6 +37,7 @@ struct AttnParams {
   int B, Hq, Hkv, Sq, Sk, D;
   int causal;
   int sq_pad;                    // rows of the padded statistics
+  int split;                     // forward: blocks of a cluster that share a query tile's keys
   float scale, scale_log2;       // scale, scale * log2(e)
   const int* kv_lens;            // [B] or null
   float* lse;                    // forward: [B][Hq][Sq]
@@ -91,10 +93,11 @@ __device__ __forceinline__ void attn_zero_rows(unsigned char* tile, int first) {
 }
 
 // The products are issued by one lane, but their descriptors are made by the whole warp, so that they are
-// uniform values (made inside the lane's branch they cost more time than the products themselves).
+// uniform values (made inside the lane's branch they cost more time than the products themselves).  In a cluster a shared
+// address has the block's rank in its upper bits, which must not reach the descriptor's other fields.
 template <int D> struct AttnDesc {
-  static __device__ __forceinline__ uint64_t rows(uint32_t addr) { return desc_kmajor(0) + (addr >> 4); }                                  // product over head elements
-  static __device__ __forceinline__ uint64_t tokens(uint32_t addr) { return desc_mnmajor(0, AttnTile<D>::kBlock) + (addr >> 4); }          // product over tokens
+  static __device__ __forceinline__ uint64_t rows(uint32_t addr) { return desc_kmajor(0) + ((addr & 0x3ffffu) >> 4); }                                  // product over head elements
+  static __device__ __forceinline__ uint64_t tokens(uint32_t addr) { return desc_mnmajor(0, AttnTile<D>::kBlock) + ((addr & 0x3ffffu) >> 4); }          // product over tokens
 };
 // 128 x N product over head elements: rows of `a` with rows of `b`
 template <int D, bool BF16, int N>
@@ -152,18 +155,68 @@ __device__ __forceinline__ int attn_kv_len(const AttnParams& p, int batch) {
   return n < 0 ? 0 : n > p.Sk ? p.Sk : n;
 }
 
+// A share of an accumulator, 128 rows of D fp32 values in shared memory, the 16-byte groups of a row
+// exchanged by its lowest three bits: written a row a thread, read a few rows a warp.
+template <int D>
+__device__ __forceinline__ void attn_keep_row(unsigned char* keep, uint32_t tmem, int first, int row) {
+#pragma unroll
+  for (int c = 0; c < D / 64; ++c) {
+    uint32_t v[32];
+    __syncwarp();
+    tmem_ld32(tmem + first + c * 32, v);
+    tmem_wait_ld();
+#pragma unroll
+    for (int g = 0; g < 8; ++g)
+      *reinterpret_cast<uint4*>(keep + row * (D * 4) + (((first + c * 32) / 4 + g) ^ (row & 7)) * 16) = make_uint4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+  }
+}
+// Shares of a query tile, one in each block of the cluster, become the result: every block joins its part of the rows,
+//     m = max_c m_c     O = sum_c 2^(m_c - m) O_c / sum_c 2^(m_c - m) sum_c
+// in the blocks' order.  `row` stands for the shares' maxima, then their sums.
+template <int D, bool BF16>
+__device__ __forceinline__ void attn_join(const AttnParams& p, const unsigned char* keep, const float* row_at, int rank, int q0, int head, int batch) {
+  const int rows = kAttnTile / p.split;
+  for (int n = threadIdx.x; n < rows * (D / 8); n += kFwdThreads) {
+    const int lrow = rank * rows + n / (D / 8), e = n % (D / 8) * 8, row = q0 + lrow;
+    if (row >= p.Sq) continue;
+    float m = -INFINITY;
+    for (int c = 0; c < p.split; ++c) m = fmaxf(m, ld_cluster_f32(row_at + lrow, c));
+    float sum = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < p.split; ++c) {
+      const float top = ld_cluster_f32(row_at + lrow, c);
+      if (top == -INFINITY) continue;            // no key there that the query sees: nothing was kept
+      const float w = exp2_fast(top - m);
+      sum = fmaf(w, ld_cluster_f32(row_at + kAttnTile + lrow, c), sum);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float4 o = ld_cluster_f32x4(keep + lrow * (D * 4) + ((e / 4 + h) ^ (lrow & 7)) * 16, c);
+        v[4 * h] = fmaf(w, o.x, v[4 * h]);
+        v[4 * h + 1] = fmaf(w, o.y, v[4 * h + 1]);
+        v[4 * h + 2] = fmaf(w, o.z, v[4 * h + 2]);
+        v[4 * h + 3] = fmaf(w, o.w, v[4 * h + 3]);
+      }
+    }
+    const float by = sum == 0.f ? 0.f : 1.f / sum;
+    if (e < p.D)
+      *reinterpret_cast<uint4*>(static_cast<unsigned short*>(p.out.p) + batch * p.out.batch + static_cast<long long>(row) * p.out.seq + head * p.out.head + e) =
+          make_uint4(pack16<BF16>(v[0] * by, v[1] * by), pack16<BF16>(v[2] * by, v[3] * by), pack16<BF16>(v[4] * by, v[5] * by), pack16<BF16>(v[6] * by, v[7] * by));
+    if (e == 0) p.lse[(static_cast<long long>(batch) * p.Hq + head) * p.Sq + row] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
+  }
+}
+
 // ----------------------------------------------------------------------------------------------
 // Forward.  A block owns 128 queries of one head and walks over the key tiles: S = Q K^T, softmax, O += P V,
 // one after the other; two blocks share an SM, and one's softmax runs while the tensor cores work for the other.
 // (One block with two query tiles in turn reads K and V half as often, but is no faster at 8192 tokens, 562 us
 // against 573, and slower where blocks are few or short: 2048 causal tokens of 8 heads 42 us against 35.)
 // Tensor memory: S (128 columns, later the rounded P in its place) and the accumulator.
+// Few query tiles and many keys: the blocks of a cluster share the keys of a query tile and join their shares through one
+// another's shared memory, no workspace and no second launch (one query over 4000 keys 57 -> 14 us).
 // Two threads share one query's row of scores and exchange their maxima (one thread a row needs none, but with two
 // warps per scheduler every instruction's latency shows).  The running maximum is only raised when a row's scores exceed
 // it by more than 2^8 in the exponential (the quotient O / sum does not depend on it, and fp32 and bf16 have the
 // range): the accumulator is then rescaled in place, which after the first few key tiles hardly happens.
 // ----------------------------------------------------------------------------------------------
-constexpr int kFwdThreads = 320;                 // warps 0-7 softmax, 8 copies, 9 products
 template <int D> struct AttnFwdSmem {
   static constexpr uint32_t kT = AttnTile<D>::kBytes;
   static constexpr int kSlots = D == 128 ? 2 : 5;              // ring of K and V tiles in turn
@@ -187,9 +240,11 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
   __shared__ float s_row[2][kAttnTile];          // [half][row]
+  __shared__ float s_share[2][kAttnTile];        // maxima and sums of this block's share
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int head = blockIdx.y, batch = blockIdx.z;
-  const int q0 = (gridDim.x - 1 - blockIdx.x) * kAttnTile;     // with a causal mask the last queries have the most keys: first
+  const int rank = static_cast<int>(blockIdx.x) % p.split;
+  const int q0 = static_cast<int>((gridDim.x - 1 - blockIdx.x) / p.split) * kAttnTile;     // with a causal mask the last queries have the most keys: first
 
   if (threadIdx.x == 0) {
     mbar_init(q_full, 1);
@@ -213,7 +268,8 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
   const int off = p.Sk - p.Sq;
   const int q_last = min(q0 + kAttnTile, p.Sq) - 1;
   const int seen = p.causal ? min(kv_len, max(0, q_last + off + 1)) : kv_len;     // keys that any query of the block sees
-  const int tiles = (seen + kAttnTile - 1) / kAttnTile;
+  const int all_tiles = (seen + kAttnTile - 1) / kAttnTile, share = (all_tiles + p.split - 1) / p.split;
+  const int first = min(rank * share, all_tiles), tiles = min(share, all_tiles - first);        // this block's key tiles
 
   if (tiles > 0 && warp == 8) {
     if (lane == 0) {
@@ -225,7 +281,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       for (int n = 0; n < 2 * tiles; ++n) {      // K_0 V_0 K_1 V_1 ..
         if (s_abort || !mbar_wait_bounded(&kv_free[slot], parity)) { s_abort = 1; break; }
         mbar_expect_tx(&kv_full[slot], L::kT);
-        attn_load_tile<D>(smem + L::kKV + slot * L::kT, n & 1 ? &mv : &mk, &kv_full[slot], (n >> 1) * kAttnTile, kv_head, batch);
+        attn_load_tile<D>(smem + L::kKV + slot * L::kT, n & 1 ? &mv : &mk, &kv_full[slot], (first + (n >> 1)) * kAttnTile, kv_head, batch);
         ++issued;
         if (++slot == L::kSlots) { slot = 0; parity ^= 1u; }
       }
@@ -259,7 +315,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       }
       __syncwarp();
       advance();
-      const uint64_t v_desc = AttnDesc<D>::tokens(take(min(kv_len - j * kAttnTile, kAttnTile)));
+      const uint64_t v_desc = AttnDesc<D>::tokens(take(min(kv_len - (first + j) * kAttnTile, kAttnTile)));
       // the product over the even 32 keys of either half runs beside the exponentials of the odd ones
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
@@ -312,7 +368,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tc_fence_after();
-      const int k0 = j * kAttnTile + half * 64;
+      const int k0 = (first + j) * kAttnTile + half * 64;
       const bool masked = k0 + 64 > warp_limit;              // warp-uniform: some score is masked
       // 32 scores at a time, read again for the exponentials: 64 registers more would spill at this block size
       uint32_t s[32];
@@ -383,11 +439,13 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       ok = __all_sync(0xffffffffu, ok);
       tc_fence_after();
       sum += exchange(sum);
-      if (ok) attn_store_row<D / 64, BF16>(p, p.out, o_at, half * (D / 2), batch, head, row, live, sum == 0.f ? 0.f : 1.f / sum);
-    } else if (tiles == 0 && live && half == 0) {
+      if (p.split > 1) attn_keep_row<D>(smem + L::kKV, o_at, half * (D / 2), lrow);
+      else if (ok) attn_store_row<D / 64, BF16>(p, p.out, o_at, half * (D / 2), batch, head, row, live, sum == 0.f ? 0.f : 1.f / sum);
+    } else if (p.split == 1 && tiles == 0 && live && half == 0) {
       attn_zero_row(p, p.out, batch, head, row);
     }
-    if (ok && live && half == 0) p.lse[(static_cast<long long>(batch) * p.Hq + head) * p.Sq + row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+    if (p.split > 1) s_share[half][lrow] = half == 0 ? top : sum;
+    else if (ok && live && half == 0) p.lse[(static_cast<long long>(batch) * p.Hq + head) * p.Sq + row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
     if (!ok) s_abort = 1;
   }
   __syncwarp();
@@ -397,6 +455,12 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
   if (warp == 9) {
     tc_fence_after();
     tmem_dealloc(t_s, 256);
+  }
+  if (p.split > 1) {
+    __syncwarp();
+    cluster_sync_all();
+    attn_join<D, BF16>(p, smem + L::kKV, s_share[0], rank, q0, head, batch);
+    cluster_sync_all();                          // the others may still read this block's share
   }
 }
 

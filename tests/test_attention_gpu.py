@@ -198,6 +198,39 @@ def test_given_outputs_streams_and_repeats():
         assert (t[:, 0] == 7.0).all() and (t[:, S + 1:] == 7.0).all() and (t[..., D:] == 7.0).all()
 
 
+@pytest.mark.parametrize("B, Sq, Sk, Hq, Hk, D, causal, lens", [
+    (1, 1, 4000, 4, 1, 128, False, None), (3, 1, 1111, 2, 2, 64, True, [1111, 0, 300]), (1, 200, 3000, 4, 2, 72, True, None), (2, 130, 2049, 2, 1, 40, False, [1, 2049]),
+    (1, 3000, 3000, 2, 1, 64, True, None), (1, 700, 500, 2, 1, 128, True, None), (2, 257, 1500, 1, 1, 96, False, [129, 700])])
+def test_few_rows_over_many_keys(B, Sq, Sk, Hq, Hk, D, causal, lens):
+    """Several blocks share a tile's walk over the other side, some of them without anything to see.  Rows of dk and dv are as
+    large as their keys' probabilities, which differ by orders here, so each element's bound is u times the sum of its terms' sizes:
+    one unit for P or dS (rounded to 16 bits, half a unit), for Delta (from the rounded out), and for the result itself."""
+    from paper_2411_03742_b200 import attention, attention_backward, attention_forward
+    g = torch.Generator(device="cuda").manual_seed(Sq + Sk)
+    q, dout = (torch.randn((B, Sq, Hq, D), generator=g, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn((B, Sk, Hk, D), generator=g, device="cuda").bfloat16() for _ in range(2))
+    L = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    out, lse = attention_forward(q, k, v, causal=causal, kv_lens=L)
+    grads = attention_backward(dout, q, k, v, out, lse, causal=causal, kv_lens=L)
+    again = attention_forward(q, k, v, causal=causal, kv_lens=L) + attention_backward(dout, q, k, v, out, lse, causal=causal, kv_lens=L)
+    torch.cuda.synchronize()
+    assert attention.status() == 0
+    assert all(torch.equal(x, y) for x, y in zip((out, lse) + grads, again)), "shares are joined in one order"
+    sc, r, u = 1 / math.sqrt(D), Hq // Hk, U[torch.bfloat16]
+    O, LSE, P = plain_forward(q, k, v, sc, causal, L)
+    none = LSE == -math.inf
+    assert torch.equal(lse == -math.inf, none) and float((lse.double() - LSE).masked_fill(none, 0.0).abs().max()) <= 1e-5
+    K, V, dO = heads(k, r), heads(v, r), heads(dout)
+    dq, dk, dv = plain_backward(q, k, v, sc, P, out, dout)
+    ds = P * (dO @ V.mT - (dO * heads(out)).sum(-1, keepdim=True)) * sc
+    slack = ds.abs() + P * (dO * heads(out)).abs().sum(-1, keepdim=True) * sc
+    share = lambda x: x.view(B, Hk, r, Sk, D).sum(2)  # noqa: E731
+    for name, got, want, terms in (("out", out, O, P @ V.abs()), ("dq", grads[0], dq, slack @ K.abs()), ("dk", grads[1], dk, share(slack.mT @ heads(q).abs())),
+                                   ("dv", grads[2], dv, share(P.mT @ dO.abs()))):
+        err = (got.double().transpose(1, 2) - want).abs()
+        assert bool((err <= u * (terms + want.abs()) + 1e-30).all()), (name, float((err - u * (terms + want.abs())).max()))
+
+
 @pytest.mark.parametrize("B, Sq, Sk, Hq, Hk, D, causal", [(3, 77, 91, 4, 2, 40, False), (1, 1, 300, 2, 1, 128, True), (2, 128, 129, 4, 2, 128, False),
                                                            (1, 256, 256, 3, 3, 64, True), (2, 65, 1, 2, 2, 72, False)])
 def test_short_queries_with_and_without_a_workspace(B, Sq, Sk, Hq, Hk, D, causal):
