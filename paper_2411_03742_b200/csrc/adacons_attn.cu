@@ -1,6 +1,7 @@
 // Host side of attention and its gradient (include/adacons_ops.h): checks, tensor maps and launches.
 #include "adacons_ops.h"
 
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 
@@ -124,6 +125,26 @@ int key_shares(int64_t blocks, int64_t tiles, int resident) {
   return shares;
 }
 
+// The gradient's two kinds of block, with walks of `queries` and `keys` tiles: the sharing with the shortest of what bounds it, the longest
+// block or the work of all.  In tiles: a block's start and end cost about three, a join two; the work is spread unevenly, hence the 1.3.
+// 4000 queries on 200 keys of 8 / 2 heads (64 elements): 281 us alone, 147, 80 and 47 us with a key tile's walk shared by 2, 4, 8; 200 on 3000 causal 44 -> 15 us;
+// 2000 x 2000 of 4 / 2 heads (128) 64 us, 41 with the key tiles' walks shared by 2, 56 by 4, 60 with both kinds' by 4; 300 x 300 13.7 us alone, 14.9 by 2.
+void share_walks(AttnParams* p, int64_t key_blocks, int64_t queries, int64_t query_blocks, int64_t keys, int resident) {
+  double best = 0.0;
+  for (int split = 1; split <= 8; split *= 2)
+    for (int which = split > 1 ? 1 : 3; which <= 3; ++which) {
+      const int k = which & 1 ? split : 1, q = which & 2 ? split : 1;
+      const double by_key = static_cast<double>((queries + k - 1) / k) + 3.0 + (k > 1 ? 2.0 : 0.0);
+      const double by_query = static_cast<double>((keys + q - 1) / q) + 3.0 + (q > 1 ? 2.0 : 0.0);
+      const double time = std::max(std::max(by_key, by_query), 1.3 * (key_blocks * k * by_key + query_blocks * q * by_query) / resident);
+      if (split > 1 && time >= best) continue;
+      best = time;
+      p->split = split;
+      p->key_split = k;
+      p->query_split = q;
+    }
+}
+
 template <int D, bool BF16>
 bool run_forward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, AttnParams p, int sms, cudaStream_t st) {
   const int q_tiles = (p.Sq + kAttnTile - 1) / kAttnTile;
@@ -134,7 +155,7 @@ bool run_forward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap
 
 template <int D, bool BF16>
 bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo, AttnParams p, const adacons_attn_tensor* dout,
-                  const adacons_attn_tensor* out, const float* lse, AttnOut dq, AttnOut dk, AttnOut dv, float* lse2, float* delta, cudaStream_t st) {
+                  const adacons_attn_tensor* out, const float* lse, AttnOut dq, AttnOut dk, AttnOut dv, float* lse2, float* delta, int sms, cudaStream_t st) {
   p.dout = {dout->data, dout->batch_stride, dout->seq_stride, dout->head_stride};
   p.o = {out->data, out->batch_stride, out->seq_stride, out->head_stride};
   p.lse_in = lse;
@@ -148,10 +169,13 @@ bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMa
   p.dk = dk;
   p.dv = dv;
   const int64_t q_tiles = p.sq_pad / kAttnTile, k_tiles = (static_cast<int64_t>(p.Sk) + kAttnTile - 1) / kAttnTile;
-  const int64_t key_blocks = k_tiles * p.Hkv * p.B, blocks = key_blocks + q_tiles * p.Hq * p.B;
-  return blocks <= 0x7fffffff && launch(&attn_backward_kernel<D, BF16>, dim3(static_cast<unsigned>(blocks)), dim3(AttnBwd<D>::kThreads), attn_backward_smem<D>(), st,
-                                        separate ? kLaunchOverlap : kLaunchPlain, 1,
-                                        mq, mk, mv, mdo, p, static_cast<int>(key_blocks), static_cast<int>(q_tiles));
+  int64_t key_blocks = k_tiles * p.Hkv * p.B, query_blocks = q_tiles * p.Hq * p.B;
+  share_walks(&p, key_blocks, p.Hq / p.Hkv * q_tiles, query_blocks, k_tiles, sms * AttnBwd<D>::kBlocks);
+  key_blocks = (key_blocks * p.key_split + p.split - 1) / p.split * p.split;
+  query_blocks = (query_blocks * p.query_split + p.split - 1) / p.split * p.split;
+  return key_blocks + query_blocks <= 0x7fffffff &&
+         launch(&attn_backward_kernel<D, BF16>, dim3(static_cast<unsigned>(key_blocks + query_blocks)), dim3(AttnBwd<D>::kThreads), attn_backward_smem<D>(), st,
+                separate ? kLaunchOverlap : kLaunchPlain, p.split, mq, mk, mv, mdo, p, static_cast<int>(key_blocks), static_cast<int>(q_tiles));
 }
 
 int64_t workspace_bytes(const adacons_attn_shape* s) {
@@ -225,7 +249,7 @@ int adacons_attn_backward(const adacons_attn_shape* s, const adacons_attn_tensor
   float* lse2 = static_cast<float*>(workspace);
   float* delta = lse2 == nullptr ? nullptr : lse2 + static_cast<int64_t>(p.B) * p.Hq * p.sq_pad;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  auto go = [&](auto run) { return run(mq, mk, mv, mdo, p, dout, out, lse, as_out(dq), as_out(dk), as_out(dv), lse2, delta, st); };
+  auto go = [&](auto run) { return run(mq, mk, mv, mdo, p, dout, out, lse, as_out(dq), as_out(dk), as_out(dv), lse2, delta, d->info.sms, st); };
   bool ok;
   if (s->head_dim <= 64) ok = s->dtype == ADACONS_BF16 ? go(run_backward<64, true>) : go(run_backward<64, false>);
   else ok = s->dtype == ADACONS_BF16 ? go(run_backward<128, true>) : go(run_backward<128, false>);
