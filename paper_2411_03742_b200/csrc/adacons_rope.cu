@@ -22,7 +22,6 @@ namespace {
 
 RopeDivisor divisor(int64_t d) {
   RopeDivisor r;
-  r.d = static_cast<int>(d);
   r.s = 0;
   while ((1ll << r.s) < d) ++r.s;
   r.m = static_cast<unsigned>(((1ull << (31 + r.s)) + static_cast<unsigned long long>(d) - 1) / static_cast<unsigned long long>(d));

@@ -23,7 +23,7 @@ constexpr int kRopeMaxTokens = 64;             // of a block
 // n / d for 0 <= n < 2^31 by a multiplication: m = ceil(2^(31 + s) / d) with s = ceil(log2 d)
 struct RopeDivisor {
   unsigned m;
-  int s, d;
+  int s;
   __device__ __forceinline__ int divide(int n) const { return static_cast<int>((static_cast<unsigned long long>(static_cast<unsigned>(n)) * m) >> (31 + s)); }
 };
 
