@@ -452,6 +452,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_one(&p_full[c]);
+        __syncwarp();                            // the reads of tensor memory that follow want the whole warp
       }
       part[0] = add2(part[0], part[1]);
       sum += part[0].x + part[0].y;
@@ -480,7 +481,6 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     tmem_dealloc(t_s, 256);
   }
   if (p.split > 1) {
-    __syncwarp();
     cluster_sync_all();
     attn_join<D, BF16>(p, smem + L::kKV, s_share[0], rank, q0, head, batch);
     cluster_sync_all();                          // the others may still read this block's share
@@ -831,7 +831,6 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
   }
   if (p.key_split > 1) {
     const int shares = all == 0 ? 0 : (all + share - 1) / share;
-    __syncwarp();
     cluster_sync_all();
     attn_join_sum<D, BF16, G::kThreads>(p, p.dv, smem, rank, shares, k0, p.Sk, kv_head, batch, 1.f);
     attn_join_sum<D, BF16, G::kThreads>(p, p.dk, smem + kAttnTile * D * 4, rank, shares, k0, p.Sk, kv_head, batch, p.scale);
@@ -1045,6 +1044,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_one(dp_read);
+        __syncwarp();
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const float2 a = mul2(add2(make_float2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1])), delta2), make_float2(pr[2 * e], pr[2 * e + 1]));
@@ -1077,7 +1077,6 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
     tmem_dealloc(tmem, G::kTmem);
   }
   if (p.query_split > 1) {
-    __syncwarp();
     cluster_sync_all();
     attn_join_sum<D, BF16, G::kThreads>(p, p.out, smem, rank, all == 0 ? 0 : (all + share - 1) / share, q0, p.Sq, head, batch, p.scale);
     cluster_sync_all();

@@ -823,6 +823,7 @@ __global__ void __launch_bounds__(kOrthThreads, 1) orth_steps_kernel(const OrthP
       tc_fence_before();
       __syncwarp();
       if (lane == 0) { if (CG == 2) mbar_arrive_leader(&acc_free[buf]); else mbar_arrive_one(&acc_free[buf]); }
+      __syncwarp();                                        // an fp32 context writes tensor memory next, as a whole warp
       buf ^= 1;
       if (buf == 0) parity ^= 1u;
     };

@@ -168,7 +168,9 @@ __device__ __forceinline__ float4 ld_cluster_f32x4(const void* p, int rank) {
   asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_address(p, rank)) : "memory");
   return v;
 }
+// `.aligned` wants whole warps: lanes that left a loop early or took a branch alone meet first.
 __device__ __forceinline__ void cluster_sync_all() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
 // Loads into this block's shared memory, reported on the barrier of the pair's even block.

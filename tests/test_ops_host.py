@@ -172,3 +172,14 @@ def test_rotary_frequencies():
     for bad in [dict(dim=3), dict(dim=0), dict(dim=8, base=0.0), dict(dim=8, scaling=("linear", 0.5)), dict(dim=8, scaling=("what", 2.0)), dict(dim=2, scaling=("ntk", 2.0))]:
         with pytest.raises(ValueError):
             frequencies(**bad)
+
+
+def test_aligned_cluster_barriers_meet_as_whole_warps():
+    """`barrier.cluster` with `.aligned` is undefined for lanes that arrive apart, and the joins before it let lanes of a ragged tile
+    go early: the helper itself brings the warp together, and nothing goes round the helper."""
+    csrc = os.path.join(ROOT, "paper_2411_03742_b200", "csrc")
+    text = {n: open(os.path.join(csrc, n)).read() for n in ("adacons_tc.cuh", "adacons_attn.cuh", "adacons_orth.cuh", "adacons_rope.cuh")}
+    places = [(n, m.start()) for n, t in text.items() for m in re.finditer(r'asm volatile\("barrier\.cluster', t)]
+    assert [n for n, _ in places] == ["adacons_tc.cuh"], places
+    before = text["adacons_tc.cuh"][:places[0][1]].rstrip().splitlines()
+    assert before[-1].strip() == "__syncwarp();"
