@@ -2,8 +2,9 @@
  * adacons_ops.h -- C ABI of the training operators beside the aggregation (NVIDIA B200, sm_100a).
  *
  * The conventions are those of adacons.h: every function returns an adacons_error code, none throws
- * or aborts; pointers are device pointers unless said otherwise; `cuda_stream` is a cudaStream_t
- * passed as void*; calls are asynchronous on that stream, allocate nothing (create calls do) and
+ * or aborts; pointers are device pointers unless said otherwise, of the device that was current when the context
+ * was created, whichever is current at the call (attention has no context: of the device that is current);
+ * `cuda_stream` is a cudaStream_t of that device passed as void*; calls are asynchronous on that stream, allocate nothing (create calls do) and
  * perform no host synchronisation; results are deterministic (no floating-point atomics, fixed
  * reduction order); no wait inside a kernel lasts longer than 2 s.
  */

@@ -13,7 +13,7 @@ import threading
 
 import torch
 
-from .binding import BF16, _check, _raw_stream, _stream_handle, load_library
+from .binding import BF16, _check, _raw_stream, _stream_handle, check_stream, load_library
 
 F16 = 2
 SHORT_ROWS = 256        # query rows around a key head up to which the backward pass can do without a workspace
@@ -102,6 +102,11 @@ def attention_forward(q, k, v, *, scale=None, causal: bool = False, kv_lens=None
     plan = _plans.known.get(sig)
     if plan is None:
         check_attention(q, k, v, kv_lens, like_q=[] if out is None else [("out", out)], rows=[] if lse is None else [("lse", lse)])
+    if sig[0][3] != torch.cuda.current_device():        # the kernels run on the current device
+        with torch.cuda.device(sig[0][3]):
+            return attention_forward(q, k, v, scale=scale, causal=causal, kv_lens=kv_lens, out=out, lse=lse, stream=stream)
+    if stream is not None:
+        check_stream(stream, sig[0][3])
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None:
@@ -144,6 +149,11 @@ def attention_backward(dout, q, k, v, out, lse, *, scale=None, causal: bool = Fa
     if plan is None:
         check_attention(q, k, v, kv_lens, like_q=[(n, t) for n, t in (("dout", dout), ("out", out), ("dq", dq)) if t is not None],
                         like_k=[(n, t) for n, t in (("dk", dk), ("dv", dv)) if t is not None], rows=[("lse", lse)])
+    if sig[0][3] != torch.cuda.current_device():        # the kernels run on the current device
+        with torch.cuda.device(sig[0][3]):
+            return attention_backward(dout, q, k, v, out, lse, scale=scale, causal=causal, kv_lens=kv_lens, dq=dq, dk=dk, dv=dv, workspace=workspace, stream=stream)
+    if stream is not None:
+        check_stream(stream, sig[0][3])
     dq = torch.empty_like(q, memory_format=torch.contiguous_format) if dq is None else dq
     dk = torch.empty_like(k, memory_format=torch.contiguous_format) if dk is None else dk
     dv = torch.empty_like(v, memory_format=torch.contiguous_format) if dv is None else dv
@@ -169,7 +179,11 @@ def attention_backward(dout, q, k, v, out, lse, *, scale=None, causal: bool = Fa
 
 
 def status(stream=None) -> int:
-    """The ADACONS_FLAG_TIMEOUT bit of the current device's attention calls since the last look (0: all waits ended)."""
+    """The ADACONS_FLAG_TIMEOUT bit of the attention calls on the current device (a given stream's) since the last look (0: all waits ended)."""
+    device = getattr(stream, "device", None)
+    if device is not None and device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return status(stream)
     v = ctypes.c_uint32()
     _check(load_library().adacons_attn_get_status(ctypes.byref(v), _stream_handle(stream)), "adacons_attn_get_status")
     return v.value

@@ -126,6 +126,13 @@ def _raw_stream(stream, device_index: int) -> int:
         return int(torch.cuda.current_stream(device_index).cuda_stream)
 
 
+def check_stream(stream, device_index: int) -> None:
+    """Raise ValueError if `stream` is known to belong to another device than the tensors."""
+    index = getattr(getattr(stream, "device", None), "index", None)
+    if index is not None and index != device_index:
+        raise ValueError(f"the stream belongs to device {index}, the tensors to device {device_index}")
+
+
 def stats_noalloc(grads, pq_out, stream=None) -> None:
     """p_i = <g_i, gbar> and q_i = ||g_i||^2 of an N x d CUDA tensor into `pq_out` (CUDA tensor of
     2N float64), through the entry point that allocates no device memory (N <= NOALLOC_MAX_N).

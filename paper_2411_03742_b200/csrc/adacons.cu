@@ -711,19 +711,6 @@ int encode_map(adacons_ctx* c, const void* grads) {
 
 bool launch_ok() { return cudaGetLastError() == cudaSuccess; }
 
-struct DeviceGuard {   // make the context's device current for the duration of a call
-  int prev = -1;
-  bool ok = true;
-  explicit DeviceGuard(int dev) {
-    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
-  }
-  ~DeviceGuard() {
-    int cur = -1;
-    if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
-  }
-};
-
 int alloc_sets(adacons_ctx* c) {   // (re)allocate everything whose size depends on sets()
   cudaFree(c->coef); cudaFree(c->gamma_f32); cudaFree(c->m); cudaFree(c->z);
   c->coef = nullptr; c->gamma_f32 = nullptr; c->m = nullptr; c->z = nullptr;

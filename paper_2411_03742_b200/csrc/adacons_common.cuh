@@ -21,6 +21,20 @@ template <int DT> struct Elem;                       // DT: 0 = fp32, 1 = bf16
 template <> struct Elem<0> { static constexpr int kVec = 4, kBytes = 4; };
 template <> struct Elem<1> { static constexpr int kVec = 8, kBytes = 2; };
 
+// Host: make a context's device current for the duration of a call.
+struct DeviceGuard {
+  int prev = -1;
+  bool ok = true;
+  explicit DeviceGuard(int dev) {
+    if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
+    if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
+  }
+  ~DeviceGuard() {
+    int cur = -1;
+    if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
+  }
+};
+
 // ----------------------------------------------------------------------------------------------
 // small PTX helpers
 // ----------------------------------------------------------------------------------------------

@@ -471,6 +471,8 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
   if (c == nullptr || update == nullptr || out == nullptr) return ADACONS_EINVAL;
   const size_t elem = c->dtype == ADACONS_F32 ? 4 : 2;
   if (reinterpret_cast<uintptr_t>(update) % elem != 0 || reinterpret_cast<uintptr_t>(out) % elem != 0) return ADACONS_EINVAL;
+  DeviceGuard guard(c->dev.device);
+  if (!guard.ok) return ADACONS_ECUDA;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   OrthParams p = c->params;
   p.out = out;
@@ -496,6 +498,8 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
 
 int adacons_orth_get_status(adacons_orth* c, uint32_t* flags, void* cuda_stream) {
   if (c == nullptr || flags == nullptr) return ADACONS_EINVAL;
+  DeviceGuard guard(c->dev.device);
+  if (!guard.ok) return ADACONS_ECUDA;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (cudaMemcpyAsync(flags, c->params.flags, sizeof(uint32_t), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
       cudaMemsetAsync(c->params.flags, 0, sizeof(uint32_t), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
@@ -515,10 +519,8 @@ int adacons_orth_get_info(adacons_orth* c, int key, int64_t* value) {
 
 int adacons_orth_destroy(adacons_orth* c) {
   if (c == nullptr) return ADACONS_OK;
-  int now = 0;
-  const bool moved = cudaGetDevice(&now) == cudaSuccess && now != c->dev.device && cudaSetDevice(c->dev.device) == cudaSuccess;
+  DeviceGuard guard(c->dev.device);
   cudaFree(c->memory);
-  if (moved) cudaSetDevice(now);
   cudaGetLastError();
   delete c;
   return ADACONS_OK;

@@ -115,6 +115,8 @@ int adacons_rope_apply(adacons_rope* c, const adacons_rope_shape* s, const void*
   p.per_token = divisor(per_head * p.heads);
   const int64_t blocks = (p.tokens + tpb - 1) / tpb;
   if (blocks > 0x7fffffff) return ADACONS_ELIMIT;
+  DeviceGuard guard(c->device);
+  if (!guard.ok) return ADACONS_ECUDA;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   bool ok;
   if (s->dtype == ADACONS_F32) ok = c->interleaved ? launch_rope<0, true>(p, vec, static_cast<unsigned>(blocks), st) : launch_rope<0, false>(p, vec, static_cast<unsigned>(blocks), st);
@@ -124,10 +126,8 @@ int adacons_rope_apply(adacons_rope* c, const adacons_rope_shape* s, const void*
 
 int adacons_rope_destroy(adacons_rope* c) {
   if (c == nullptr) return ADACONS_OK;
-  int now = 0;
-  const bool moved = cudaGetDevice(&now) == cudaSuccess && now != c->device && cudaSetDevice(c->device) == cudaSuccess;
+  DeviceGuard guard(c->device);
   cudaFree(c->turns);
-  if (moved) cudaSetDevice(now);
   cudaGetLastError();
   delete c;
   return ADACONS_OK;

@@ -11,7 +11,7 @@ import ctypes
 
 import torch
 
-from .binding import BF16, F32, _check, _raw_stream, _stream_handle, load_library
+from .binding import BF16, F32, _check, _raw_stream, check_stream, load_library
 
 # enum adacons_orth_info
 INFO_BYTES, INFO_LAUNCHES = 0, 1
@@ -55,6 +55,7 @@ class Orthogonalizer:
         _check(self._lib.adacons_orth_create(ctypes.byref(self._ctx), {"f32": F32, "bf16": BF16}[dtype], self.d, n, i64(*[m for m, _ in shapes]),
                                              i64(*[k for _, k in shapes]), i64(*offsets), int(bool(scaling)), int(steps), flat, float(eps)),
                "adacons_orth_create")
+        self.device = torch.cuda.current_device()        # where the plan's memory is
         self._checked = None
 
     def close(self) -> None:
@@ -80,14 +81,16 @@ class Orthogonalizer:
         device = update.get_device()
         sig = (update.dtype, update.shape, update.stride(), device, out.dtype, out.shape, out.stride(), out.get_device())
         if sig != self._checked:
-            check_vectors(self.d, self.dtype, update, out)
+            check_vectors(self.d, self.dtype, update, out, device=self.device)
             self._checked = sig
+        if stream is not None:
+            check_stream(stream, device)
         _check(self._lib.adacons_orth_apply(self._ctx, update.data_ptr(), out.data_ptr(), _raw_stream(stream, device)), "adacons_orth_apply")
 
     def status(self, stream=None) -> int:
         """The ADACONS_FLAG_TIMEOUT bit since the last call (0: all waits ended)."""
         v = ctypes.c_uint32()
-        _check(self._lib.adacons_orth_get_status(self._ctx, ctypes.byref(v), _stream_handle(stream)), "adacons_orth_get_status")
+        _check(self._lib.adacons_orth_get_status(self._ctx, ctypes.byref(v), _raw_stream(stream, self.device)), "adacons_orth_get_status")
         return v.value
 
     def info(self, key: int) -> int:
@@ -96,8 +99,9 @@ class Orthogonalizer:
         return v.value
 
 
-def check_vectors(d: int, dtype: str, update, out, want_cuda: bool = True) -> None:
-    """Raise ValueError unless both are contiguous vectors of d elements of `dtype` on one (CUDA) device."""
+def check_vectors(d: int, dtype: str, update, out, want_cuda: bool = True, device=None) -> None:
+    """Raise ValueError unless both are contiguous vectors of d elements of `dtype` on one (CUDA) device, the one of
+    index `device` if given."""
     tdt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
     for name, t in (("update", update), ("out", out)):
         if t.dtype != tdt:
@@ -110,3 +114,5 @@ def check_vectors(d: int, dtype: str, update, out, want_cuda: bool = True) -> No
             raise ValueError(f"{name} must be a CUDA tensor")
     if update.device != out.device:
         raise ValueError("update and out must be on the same device")
+    if device is not None and update.get_device() != device:
+        raise ValueError(f"update and out are on device {update.get_device()}, the plan was made on device {device}")

@@ -10,7 +10,7 @@ import math
 
 import torch
 
-from .binding import BF16, F32, _check, _raw_stream, load_library
+from .binding import BF16, F32, _check, _raw_stream, check_stream, load_library
 
 
 def frequencies(dim: int, base: float = 10000.0, scaling=None):
@@ -68,6 +68,7 @@ class Rope:
         self.dim, self.interleaved, self.angles, self.gain = int(dim), bool(interleaved), angles, float(gain)
         _check(self._lib.adacons_rope_create(ctypes.byref(self._ctx), self.dim, (ctypes.c_double * len(angles))(*angles), self.gain, int(self.interleaved)),
                "adacons_rope_create")
+        self.device = torch.cuda.current_device()        # where the angles are
         self._checked = {}
 
     def close(self) -> None:
@@ -98,12 +99,14 @@ class Rope:
         if out is None:
             out = torch.empty_like(x, memory_format=torch.contiguous_format)
         if args is None:
-            check_rope(self.dim, x, positions, out)
+            check_rope(self.dim, x, positions, out, device=self.device)
             B, S, H, D = x.shape
             i64 = ctypes.c_int64 * 3
             if len(self._checked) >= 1024:       # a program with ever new lengths
                 self._checked.clear()
             args = self._checked[sig] = (_Shape(F32 if x.dtype == torch.float32 else BF16, B, S, H, D), i64(*x.stride()[:3]), i64(*out.stride()[:3]))
+        if stream is not None:
+            check_stream(stream, device)
         _check(self._lib.adacons_rope_apply(self._ctx, ctypes.byref(args[0]), x.data_ptr(), args[1], out.data_ptr(), args[2],
                                             None if positions is None else positions.data_ptr(), int(first), int(bool(inverse)), _raw_stream(stream, device)),
                "adacons_rope_apply")
@@ -114,8 +117,9 @@ class Rope:
         return _Turn.apply(x, self, positions, first)
 
 
-def check_rope(dim: int, x, positions, out, want_cuda: bool = True) -> None:
-    """Raise ValueError unless x and out are alike, four-dimensional, of a type the kernel has, and positions fit."""
+def check_rope(dim: int, x, positions, out, want_cuda: bool = True, device=None) -> None:
+    """Raise ValueError unless x and out are alike, four-dimensional, of a type the kernel has, on the device of
+    index `device` if given, and positions fit."""
     if x.dim() != 4:
         raise ValueError("x must have four dimensions: batch, token, head, element")
     if x.dtype not in (torch.float32, torch.bfloat16):
@@ -129,6 +133,8 @@ def check_rope(dim: int, x, positions, out, want_cuda: bool = True) -> None:
             raise ValueError(f"{name} must have unit stride along the elements of a head")
         if want_cuda and not t.is_cuda:
             raise ValueError(f"{name} must be a CUDA tensor")
+    if device is not None and x.get_device() != device:
+        raise ValueError(f"x is on device {x.get_device()}, the angles are on device {device}")
     if any(n > 1 and s == 0 for n, s in zip(out.shape, out.stride())):
         raise ValueError("out must not be a broadcast view")
     if out.data_ptr() == x.data_ptr() and out.stride() != x.stride():

@@ -183,3 +183,114 @@ def test_aligned_cluster_barriers_meet_as_whole_warps():
     assert [n for n, _ in places] == ["adacons_tc.cuh"], places
     before = text["adacons_tc.cuh"][:places[0][1]].rstrip().splitlines()
     assert before[-1].strip() == "__syncwarp();"
+
+
+class _Fake:
+    """A tensor as far as the checks look, on a device of any number; its storage is never touched."""
+
+    def __init__(self, shape, dtype=torch.bfloat16, device=1, data=1 << 20):
+        self.shape, self.dtype, self.device, self.is_cuda, self.data = torch.Size(shape), dtype, torch.device("cuda", device), True, data
+
+    def stride(self, k=None):
+        steps = [math.prod(self.shape[i + 1:]) for i in range(len(self.shape))]
+        return tuple(steps) if k is None else steps[k]
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        return math.prod(self.shape)
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def get_device(self):
+        return self.device.index
+
+    def data_ptr(self):
+        return self.data
+
+    def is_contiguous(self):
+        return True
+
+
+class _FakeLibrary:
+    """Notes the device that is current at each call instead of launching anything."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append((name, torch.cuda.current_device(), args))
+            return 0
+        return call
+
+
+@pytest.fixture
+def fake(monkeypatch):
+    """Two devices, 0 current, and a library that launches nothing."""
+    from types import SimpleNamespace
+    from paper_2411_03742_b200 import attention, orth, rope
+    now, library = [0], _FakeLibrary()
+
+    class Device:
+        def __init__(self, device):
+            self.to = device if isinstance(device, int) else device.index
+
+        def __enter__(self):
+            self.was, now[0] = now[0], self.to
+
+        def __exit__(self, *exc):
+            now[0] = self.was
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(torch.cuda, "get_device_properties", lambda device: SimpleNamespace(multi_processor_count=148))
+    for module in (attention, orth, rope):
+        monkeypatch.setattr(module, "load_library", lambda: library)
+        monkeypatch.setattr(module, "_raw_stream", lambda stream, device: 0 if stream is None else stream.cuda_stream)
+    monkeypatch.setattr(attention, "_plans", attention._Plans())
+    return library
+
+
+def test_contexts_refuse_tensors_of_another_device(fake):
+    from paper_2411_03742_b200 import Orthogonalizer, Rope
+    with Orthogonalizer([(4, 8)], "bf16") as plan, Rope(16) as turn:
+        assert plan.device == turn.device == 0
+        del fake.calls[:]
+        for bad in (lambda: plan.apply(_Fake((32,)), _Fake((32,))), lambda: turn.apply(_Fake((1, 2, 3, 16)), out=_Fake((1, 2, 3, 16)))):
+            with pytest.raises(ValueError, match="device 1"):
+                bad()
+        assert not fake.calls
+        plan.apply(_Fake((32,), device=0), _Fake((32,), device=0))
+        turn.apply(_Fake((1, 2, 3, 16), device=0), out=_Fake((1, 2, 3, 16), device=0))
+        assert [c[0] for c in fake.calls] == ["adacons_orth_apply", "adacons_rope_apply"]
+        with torch.cuda.device(1):           # the library makes the context's device current by itself
+            plan.apply(_Fake((32,), device=0), _Fake((32,), device=0))
+
+
+def test_attention_runs_on_its_tensors_device(fake):
+    from paper_2411_03742_b200 import attention_backward, attention_forward
+    q, lse = _Fake((1, 200, 2, 64)), _Fake((1, 2, 200), torch.float32)
+    for device in (1, 0):
+        q.device = lse.device = torch.device("cuda", device)
+        attention_forward(q, q, q, out=q, lse=lse)
+        attention_backward(q, q, q, q, q, lse, dq=q, dk=q, dv=q, workspace=_Fake((1 << 20,), torch.uint8, device))
+        assert [c[1] for c in fake.calls if c[0] in ("adacons_attn_forward", "adacons_attn_backward")] == [device, device]
+        assert torch.cuda.current_device() == 0
+        del fake.calls[:]
+
+
+def test_streams_of_another_device_are_refused(fake):
+    from types import SimpleNamespace
+    from paper_2411_03742_b200 import Orthogonalizer, Rope, attention_forward
+    other = SimpleNamespace(cuda_stream=7, device=torch.device("cuda", 1))
+    q, lse = _Fake((1, 200, 2, 64), device=0), _Fake((1, 2, 200), torch.float32, 0)
+    with Orthogonalizer([(4, 8)], "bf16") as plan, Rope(16) as turn:
+        del fake.calls[:]
+        for bad in (lambda: attention_forward(q, q, q, out=q, lse=lse, stream=other), lambda: plan.apply(_Fake((32,), device=0), _Fake((32,), device=0), stream=other),
+                    lambda: turn.apply(q, out=q, stream=other)):
+            with pytest.raises(ValueError, match="stream"):
+                bad()
+        assert not fake.calls
