@@ -13,7 +13,7 @@ import threading
 
 import torch
 
-from .binding import BF16, _check, _raw_stream, _stream_handle, check_stream, load_library
+from .binding import BF16, _check, _raw_stream, _stream_handle, check_stream, load_library, on_stream
 
 F16 = 2
 SHORT_ROWS = 256        # query rows around a key head up to which the backward pass can do without a workspace
@@ -97,7 +97,9 @@ def _shape(q, k, scale, causal, kv_lens):
 
 def attention_forward(q, k, v, *, scale=None, causal: bool = False, kv_lens=None, out=None, lse=None, stream=None):
     """(out, lse): out = softmax(scale q k^T + mask) v, shaped like q, and the rows' log-sum-exp, (batch,
-    q_heads, q_len) fp32.  scale defaults to head_dim^-1/2; kv_lens (int32) hides each batch's keys from there on."""
+    q_heads, q_len) fp32.  scale defaults to head_dim^-1/2; kv_lens (int32) hides each batch's keys from there on.
+    stream: where the kernels go (the current one by default); the caller orders it behind whatever makes the inputs, and its own
+    use of the results behind it."""
     sig = (_layout(q), _layout(k), _layout(v), _layout(kv_lens), scale, causal, _layout(out), _layout(lse))
     plan = _plans.known.get(sig)
     if plan is None:
@@ -107,6 +109,8 @@ def attention_forward(q, k, v, *, scale=None, causal: bool = False, kv_lens=None
             return attention_forward(q, k, v, scale=scale, causal=causal, kv_lens=kv_lens, out=out, lse=lse, stream=stream)
     if stream is not None:
         check_stream(stream, sig[0][3])
+        if stream.cuda_stream != _raw_stream(None, sig[0][3]):
+            return on_stream(stream, sig[0][3], (out, lse), lambda: attention_forward(q, k, v, scale=scale, causal=causal, kv_lens=kv_lens, out=out, lse=lse))
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None:
@@ -142,8 +146,7 @@ def _one_launch(q, k) -> bool:
 def attention_backward(dout, q, k, v, out, lse, *, scale=None, causal: bool = False, kv_lens=None, dq=None, dk=None, dv=None, workspace=None,
                        stream=None):
     """(dq, dk, dv) of attention_forward with the same scale, causal and kv_lens, from its out and lse and the
-    gradient dout.  workspace: a uint8 tensor of workspace_bytes(q, k), made here if needed and not given (a call on
-    a stream other than the current one should bring its own)."""
+    gradient dout.  workspace: a uint8 tensor of workspace_bytes(q, k), made here if needed and not given."""
     sig = (_layout(q), _layout(k), _layout(v), _layout(kv_lens), scale, causal, _layout(out), _layout(lse), _layout(dout), _layout(dq), _layout(dk), _layout(dv))
     plan = _plans.known.get(sig)
     if plan is None:
@@ -154,6 +157,9 @@ def attention_backward(dout, q, k, v, out, lse, *, scale=None, causal: bool = Fa
             return attention_backward(dout, q, k, v, out, lse, scale=scale, causal=causal, kv_lens=kv_lens, dq=dq, dk=dk, dv=dv, workspace=workspace, stream=stream)
     if stream is not None:
         check_stream(stream, sig[0][3])
+        if stream.cuda_stream != _raw_stream(None, sig[0][3]):
+            return on_stream(stream, sig[0][3], (dq, dk, dv), lambda: attention_backward(
+                dout, q, k, v, out, lse, scale=scale, causal=causal, kv_lens=kv_lens, dq=dq, dk=dk, dv=dv, workspace=workspace))
     dq = torch.empty_like(q, memory_format=torch.contiguous_format) if dq is None else dq
     dk = torch.empty_like(k, memory_format=torch.contiguous_format) if dk is None else dk
     dv = torch.empty_like(v, memory_format=torch.contiguous_format) if dv is None else dv

@@ -133,6 +133,22 @@ def check_stream(stream, device_index: int) -> None:
         raise ValueError(f"the stream belongs to device {index}, the tensors to device {device_index}")
 
 
+def on_stream(stream, device_index: int, given, call):
+    """call() with `stream` current, where that is another than the current one: what it allocates then comes from that stream's
+    memory, so that neither work still queued on the caller's stream nor what the caller allocates next meets it there.  The
+    results that were not given are the caller's to use on its own stream, which is noted for when they are freed."""
+    import torch
+    caller = torch.cuda.current_stream(device_index)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device_index)
+    with torch.cuda.stream(stream):
+        results = call()
+    for before, made in zip(given, results):
+        if before is None:
+            made.record_stream(caller)
+    return results
+
+
 def stats_noalloc(grads, pq_out, stream=None) -> None:
     """p_i = <g_i, gbar> and q_i = ||g_i||^2 of an N x d CUDA tensor into `pq_out` (CUDA tensor of
     2N float64), through the entry point that allocates no device memory (N <= NOALLOC_MAX_N).

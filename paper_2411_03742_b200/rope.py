@@ -10,7 +10,7 @@ import math
 
 import torch
 
-from .binding import BF16, F32, _check, _raw_stream, check_stream, load_library
+from .binding import BF16, F32, _check, _raw_stream, check_stream, load_library, on_stream
 
 
 def frequencies(dim: int, base: float = 10000.0, scaling=None):
@@ -93,6 +93,10 @@ class Rope:
         positions: int32 (batch, token), or None: token s is at position first + s.  out: a new tensor
         unless given; x itself is allowed.  inverse: the gradient's turn, by the negative angles."""
         device = x.get_device()
+        if stream is not None and x.is_cuda:
+            check_stream(stream, device)
+            if stream.cuda_stream != _raw_stream(None, device):
+                return on_stream(stream, device, (out,), lambda: (self.apply(x, positions, out, inverse, first),))[0]
         sig = (x.dtype, x.shape, x.stride(), device, None if out is None else (out.dtype, out.shape, out.stride(), out.get_device(), out.data_ptr() == x.data_ptr()),
                None if positions is None else (positions.dtype, positions.shape, positions.stride(), positions.get_device()))
         args = self._checked.get(sig)
@@ -105,8 +109,6 @@ class Rope:
             if len(self._checked) >= 1024:       # a program with ever new lengths
                 self._checked.clear()
             args = self._checked[sig] = (_Shape(F32 if x.dtype == torch.float32 else BF16, B, S, H, D), i64(*x.stride()[:3]), i64(*out.stride()[:3]))
-        if stream is not None:
-            check_stream(stream, device)
         _check(self._lib.adacons_rope_apply(self._ctx, ctypes.byref(args[0]), x.data_ptr(), args[1], out.data_ptr(), args[2],
                                             None if positions is None else positions.data_ptr(), int(first), int(bool(inverse)), _raw_stream(stream, device)),
                "adacons_rope_apply")

@@ -294,3 +294,51 @@ def test_streams_of_another_device_are_refused(fake):
             with pytest.raises(ValueError, match="stream"):
                 bad()
         assert not fake.calls
+
+
+def test_what_a_call_on_another_stream_allocates_belongs_to_that_stream(fake, monkeypatch):
+    """Made from the current stream's memory, results could meet work still queued there, and a workspace dropped at the
+    return what the caller allocates next."""
+    from types import SimpleNamespace
+    from paper_2411_03742_b200 import Rope, attention, attention_backward, attention_forward, binding, rope
+    mine, side = SimpleNamespace(cuda_stream=5, device=torch.device("cuda", 0)), SimpleNamespace(cuda_stream=7, device=torch.device("cuda", 0))
+    now, made = [mine], []
+
+    class On:
+        def __init__(self, stream):
+            self.to = stream
+
+        def __enter__(self):
+            self.was, now[0] = now[0], self.to
+
+        def __exit__(self, *exc):
+            now[0] = self.was
+
+    class Made(_Fake):
+        def __init__(self, shape, dtype):
+            super().__init__(shape, dtype, 0)
+            self.stream, self.users = now[0], []
+            made.append(self)
+
+        def record_stream(self, stream):
+            self.users.append(stream)
+
+    monkeypatch.setattr(_Fake, "new_empty", lambda self, shape, dtype=None: Made((shape,) if isinstance(shape, int) else shape, dtype or self.dtype), raising=False)
+    monkeypatch.setattr(torch, "empty_like", lambda t, **how: Made(t.shape, t.dtype))
+    monkeypatch.setattr(torch.cuda, "stream", On)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: now[0])
+    monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle, device: {5: mine, 7: side}[handle])
+    for module in (attention, rope, binding):
+        monkeypatch.setattr(module, "_raw_stream", lambda stream, device: (now[0] if stream is None else stream).cuda_stream)
+    monkeypatch.setattr(attention, "workspace_bytes", lambda q, k: 4096)
+    q, lse = _Fake((1, 400, 2, 64), device=0), _Fake((1, 2, 400), torch.float32, 0)
+    with Rope(16) as turn:
+        for stream in (side, mine, None):
+            del made[:], fake.calls[:]
+            results = [*attention_forward(q, q, q, stream=stream), *attention_backward(q, q, q, q, q, lse, stream=stream), turn.apply(q, stream=stream)]
+            on = side if stream is side else mine
+            assert len(made) == 7 and all(t.stream is on for t in made), "outputs, workspace"
+            assert [c[2][-1] for c in fake.calls] == [on.cuda_stream] * 3
+            if stream is side:
+                assert all(t.users == [mine] for t in results), "freed only after what the caller does with them"
+            assert now[0] is mine
