@@ -89,10 +89,16 @@ def _layout(t):
     return None if t is None else (t.dtype, t.shape, t.stride(), t.get_device())
 
 
+def _how(scale, causal):
+    """scale and causal as the plain values that they have now: a tensor in the key of a layout would go by its identity, and
+    a scale that a program changes in place would stay what it was at the first call."""
+    return None if scale is None else float(scale), bool(causal)
+
+
 def _shape(q, k, scale, causal, kv_lens):
     B, Sq, Hq, D = q.shape
-    return _Shape(BF16 if q.dtype == torch.bfloat16 else F16, B, Hq, k.shape[2], Sq, k.shape[1], D, int(bool(causal)),
-                  1.0 / math.sqrt(D) if scale is None else float(scale), None if kv_lens is None else kv_lens.data_ptr())
+    return _Shape(BF16 if q.dtype == torch.bfloat16 else F16, B, Hq, k.shape[2], Sq, k.shape[1], D, int(causal),
+                  1.0 / math.sqrt(D) if scale is None else scale, None if kv_lens is None else kv_lens.data_ptr())
 
 
 def attention_forward(q, k, v, *, scale=None, causal: bool = False, kv_lens=None, out=None, lse=None, stream=None):
@@ -100,6 +106,7 @@ def attention_forward(q, k, v, *, scale=None, causal: bool = False, kv_lens=None
     q_heads, q_len) fp32.  scale defaults to head_dim^-1/2; kv_lens (int32) hides each batch's keys from there on.
     stream: where the kernels go (the current one by default); the caller orders it behind whatever makes the inputs, and its own
     use of the results behind it."""
+    scale, causal = _how(scale, causal)
     sig = (_layout(q), _layout(k), _layout(v), _layout(kv_lens), scale, causal, _layout(out), _layout(lse))
     plan = _plans.known.get(sig)
     if plan is None:
@@ -147,6 +154,7 @@ def attention_backward(dout, q, k, v, out, lse, *, scale=None, causal: bool = Fa
                        stream=None):
     """(dq, dk, dv) of attention_forward with the same scale, causal and kv_lens, from its out and lse and the
     gradient dout.  workspace: a uint8 tensor of workspace_bytes(q, k), made here if needed and not given."""
+    scale, causal = _how(scale, causal)
     sig = (_layout(q), _layout(k), _layout(v), _layout(kv_lens), scale, causal, _layout(out), _layout(lse), _layout(dout), _layout(dq), _layout(dk), _layout(dv))
     plan = _plans.known.get(sig)
     if plan is None:
@@ -196,8 +204,11 @@ def status(stream=None) -> int:
 
 
 def attention(q, k, v, *, scale=None, causal: bool = False, kv_lens=None):
-    """attention_forward's out as a differentiable function of q, k and v."""
-    return _Attention.apply(q, k, v, scale, causal, kv_lens)
+    """attention_forward's out as a differentiable function of q, k and v.  Not of the scale: a learned temperature
+    belongs into q."""
+    if getattr(scale, "requires_grad", False):
+        raise ValueError("attention has no gradient for its scale: multiply q by a learned temperature instead")
+    return _Attention.apply(q, k, v, *_how(scale, causal), kv_lens)
 
 
 class _Attention(torch.autograd.Function):

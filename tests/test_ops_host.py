@@ -342,3 +342,24 @@ def test_what_a_call_on_another_stream_allocates_belongs_to_that_stream(fake, mo
             if stream is side:
                 assert all(t.users == [mine] for t in results), "freed only after what the caller does with them"
             assert now[0] is mine
+
+
+def test_a_scale_held_in_a_tensor_is_read_at_every_call(fake):
+    from paper_2411_03742_b200 import attention_backward, attention_forward
+    q, lse, scale = _Fake((1, 400, 2, 64), device=0), _Fake((1, 2, 400), torch.float32, 0), torch.tensor(0.5)
+    work = _Fake((1 << 20,), torch.uint8, 0)
+    seen = []
+    for factor in (1.0, 4.0, 0.25):
+        scale.mul_(factor)
+        for call in (lambda: attention_forward(q, q, q, scale=scale, out=q, lse=lse), lambda: attention_backward(q, q, q, q, q, lse, scale=scale, dq=q, dk=q, dv=q, workspace=work)):
+            del fake.calls[:]
+            call()
+            seen.append([c[2][0]._obj.scale for c in fake.calls if c[0] in ("adacons_attn_forward", "adacons_attn_backward")])
+    assert seen == [[0.5], [0.5], [2.0], [2.0], [0.5], [0.5]]
+
+
+def test_a_scale_that_wants_a_gradient_is_refused():
+    from paper_2411_03742_b200.attention import attention
+    q = torch.zeros((1, 8, 2, 64), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="scale"):
+        attention(q, q, q, scale=torch.tensor(0.5, requires_grad=True))
