@@ -204,7 +204,7 @@ def status(stream=None) -> int:
 
 
 def attention(q, k, v, *, scale=None, causal: bool = False, kv_lens=None):
-    """attention_forward's out as a differentiable function of q, k and v.  Not of the scale: a learned temperature
+    """attention_forward's out as a function of q, k and v that can be differentiated once.  Not of the scale: a learned temperature
     belongs into q."""
     if getattr(scale, "requires_grad", False):
         raise ValueError("attention has no gradient for its scale: multiply q by a learned temperature instead")
@@ -224,5 +224,22 @@ class _Attention(torch.autograd.Function):
         q, k, v, out, lse, *lens = ctx.saved_tensors
         if dout.stride(3) != 1 or any(n > 1 and (s % 8 != 0 or s <= 0) for n, s in zip(dout.shape[:3], dout.stride())):
             dout = dout.contiguous()        # a broadcast gradient, of a sum for instance
-        dq, dk, dv = attention_backward(dout, q, k, v, out, lse, scale=ctx.how[0], causal=ctx.how[1], kv_lens=lens[0] if lens else None)
-        return dq, dk, dv, None, None, None
+        gradient = _Gradient.apply if torch.is_grad_enabled() else _Gradient.compute
+        return (*gradient(dout, q, k, v, out.detach(), lse, lens[0] if lens else None, *ctx.how), None, None, None)
+
+
+class _Gradient(torch.autograd.Function):
+    """The gradient where a graph of it is recorded: it depends on dout, q, k and v, and differentiating it again is an error
+    (taken for a constant, it would silently leave terms out of a second derivative)."""
+
+    @staticmethod
+    def compute(dout, q, k, v, out, lse, lens, scale, causal):
+        return attention_backward(dout, q, k, v, out, lse, scale=scale, causal=causal, kv_lens=lens)
+
+    @staticmethod
+    def forward(ctx, *args):
+        return _Gradient.compute(*args)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise NotImplementedError("attention can be differentiated once: its gradient has no gradient of its own")

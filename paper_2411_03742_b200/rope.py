@@ -116,7 +116,7 @@ class Rope:
 
     def __call__(self, x, positions=None, first: int = 0):
         """apply as a differentiable function of x."""
-        return _Turn.apply(x, self, positions, first)
+        return _Turn.apply(x, self, positions, first, False)
 
 
 def check_rope(dim: int, x, positions, out, want_cuda: bool = True, device=None) -> None:
@@ -146,14 +146,16 @@ def check_rope(dim: int, x, positions, out, want_cuda: bool = True, device=None)
 
 
 class _Turn(torch.autograd.Function):
+    """The turn, or the turn back.  It is linear: its gradient is the other of the two, as often as one differentiates."""
+
     @staticmethod
-    def forward(ctx, x, rope, positions, first):
-        ctx.rope, ctx.first = rope, first
+    def forward(ctx, x, rope, positions, first, inverse):
+        ctx.rope, ctx.first, ctx.inverse = rope, first, inverse
         ctx.save_for_backward(*([] if positions is None else [positions]))
-        return rope.apply(x, positions, first=first)
+        return rope.apply(x, positions, inverse=inverse, first=first)
 
     @staticmethod
     def backward(ctx, dy):
         pos = ctx.saved_tensors[0] if ctx.saved_tensors else None
         dy = dy if dy.stride(3) == 1 else dy.contiguous()
-        return ctx.rope.apply(dy, pos, inverse=True, first=ctx.first), None, None, None
+        return _Turn.apply(dy, ctx.rope, pos, ctx.first, not ctx.inverse), None, None, None, None

@@ -340,3 +340,15 @@ def test_refusals():
         attention_backward(q, q, q, q, out, lse, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ValueError):
         attention_backward(q, q, q, q, out, lse.bfloat16())
+
+
+def test_second_derivatives_are_refused():
+    from paper_2411_03742_b200.attention import attention
+    x = torch.randn((1, 64, 2, 64), device="cuda").bfloat16().requires_grad_()
+    y = torch.randn((1, 64, 2, 64), device="cuda").bfloat16().requires_grad_()
+    for f in (lambda: attention(x * x, x, y).float().square().sum(), lambda: attention(x * x, x, y).sum()):
+        g = torch.autograd.grad(f(), x, create_graph=True)[0]
+        with pytest.raises(NotImplementedError, match="once"):
+            torch.autograd.grad(g.float().square().sum(), x)
+    (z,) = torch.autograd.grad((attention(x, x, x) * y).sum() + (y * y * y).float().sum(), y, create_graph=True)       # what does not pass it is served
+    assert torch.autograd.grad(z.float().sum(), y, allow_unused=True)[0] is not None

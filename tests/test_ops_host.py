@@ -363,3 +363,31 @@ def test_a_scale_that_wants_a_gradient_is_refused():
     q = torch.zeros((1, 8, 2, 64), dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="scale"):
         attention(q, q, q, scale=torch.tensor(0.5, requires_grad=True))
+
+
+def test_second_derivatives(monkeypatch):
+    """Attention says that it has none; the turn, a linear map, has its own back again.  In place of the kernels stand products
+    on the CPU that have the formulas' linear structure."""
+    from paper_2411_03742_b200 import attention as module
+    from paper_2411_03742_b200.rope import _Turn
+    monkeypatch.setattr(module, "attention_forward", lambda q, k, v, **how: ((q * k).detach(), torch.zeros(1)))
+    monkeypatch.setattr(module, "attention_backward", lambda dout, q, k, v, out, lse, **how: ((dout * k).detach(), (dout * q).detach(), torch.zeros_like(v)))
+    x = torch.randn((1, 3, 2, 8), generator=torch.Generator().manual_seed(1), requires_grad=True)
+    for f in (lambda x: module.attention(x, x, x).sum(), lambda x: module.attention(x * x, x, x).square().sum()):
+        one = torch.autograd.grad(f(x), x, create_graph=True)[0]
+        with pytest.raises(NotImplementedError, match="once"):
+            torch.autograd.grad(one.square().sum(), x)
+
+    class Turn:                       # (a, b) -> (2 a - b, a + 2 b) and its transpose
+        def apply(self, x, positions=None, inverse=False, first=0):
+            a, b = x.detach().chunk(2, -1)
+            s = -1.0 if inverse else 1.0
+            return torch.cat([2 * a - s * b, s * a + 2 * b], -1)
+
+    f = lambda x: _Turn.apply(x * x * x, Turn(), None, 0, False).square().sum()  # noqa: E731
+    g = torch.autograd.grad(f(x), x, create_graph=True)[0]
+    h = torch.autograd.grad(g.square().sum(), x)[0]
+    y = x.detach().double().requires_grad_()              # |R y|^2 = 5 |y|^2
+    g2 = torch.autograd.grad(5 * (y ** 3).square().sum(), y, create_graph=True)[0]
+    want = torch.autograd.grad(g2.square().sum(), y)[0]
+    assert float((h.double() - want).abs().max()) <= 1e-5 * float(want.abs().max())

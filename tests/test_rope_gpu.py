@@ -135,3 +135,18 @@ def test_refusals():
             rope.apply(x, positions=torch.zeros((1, 3), dtype=torch.int32, device="cuda"))
     with pytest.raises(ValueError):
         Rope(16, angles=[1.0])
+
+
+def test_second_derivatives():
+    """|R y|^2 = gain^2 |y|^2 where all is turned, so the gradient of the gradient's norm through y = x^3 is known."""
+    from paper_2411_03742_b200 import Rope
+    x = torch.randn((2, 33, 3, 64), device="cuda", dtype=torch.float32, requires_grad=True)
+    pos = torch.randint(0, 4000, (2, 33), device="cuda", dtype=torch.int32)
+    with Rope(64, scaling=("yarn", 8.0, 512)) as rope:
+        g = torch.autograd.grad(rope(x * x * x, pos).square().sum(), x, create_graph=True)[0]
+        h = torch.autograd.grad(g.square().sum(), x)[0]
+        y = x.detach().double().requires_grad_()
+        g2 = torch.autograd.grad(rope.gain ** 2 * (y ** 3).square().sum(), y, create_graph=True)[0]
+        want = torch.autograd.grad(g2.square().sum(), y)[0]
+    # fp32 throughout: two turns each way at 1e-6 of their pairs
+    assert float((h.double() - want).norm() / want.norm()) <= 1e-5
