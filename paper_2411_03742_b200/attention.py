@@ -222,8 +222,8 @@ class _Attention(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dout):
         q, k, v, out, lse, *lens = ctx.saved_tensors
-        if dout.stride(3) != 1 or any(n > 1 and (s % 8 != 0 or s <= 0) for n, s in zip(dout.shape[:3], dout.stride())):
-            dout = dout.contiguous()        # a broadcast gradient, of a sum for instance
+        if dout.data_ptr() % 16 != 0 or dout.stride(3) != 1 or any(n > 1 and (s % 8 != 0 or s <= 0) for n, s in zip(dout.shape[:3], dout.stride())):
+            dout = dout.clone(memory_format=torch.contiguous_format)        # a broadcast gradient, of a sum for instance, or a slice off a 16-byte boundary
         gradient = _Gradient.apply if torch.is_grad_enabled() else _Gradient.compute
         return (*gradient(dout, q, k, v, out.detach(), lse, lens[0] if lens else None, *ctx.how), None, None, None)
 

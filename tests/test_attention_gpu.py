@@ -352,3 +352,12 @@ def test_second_derivatives_are_refused():
             torch.autograd.grad(g.float().square().sum(), x)
     (z,) = torch.autograd.grad((attention(x, x, x) * y).sum() + (y * y * y).float().sum(), y, create_graph=True)       # what does not pass it is served
     assert torch.autograd.grad(z.float().sum(), y, allow_unused=True)[0] is not None
+
+
+def test_gradients_off_a_16_byte_boundary():
+    from paper_2411_03742_b200.attention import attention
+    x = [torch.randn((2, 64, 2, 64), device="cuda").bfloat16().requires_grad_() for _ in range(3)]
+    w = torch.randn((2 * 64 * 2 * 64 + 3,), device="cuda").bfloat16()
+    a = torch.autograd.grad((torch.cat([w[:3], attention(*x).flatten()]) * w).sum(), x)
+    b = torch.autograd.grad((attention(*x) * w[3:].view(2, 64, 2, 64).clone()).sum(), x)
+    assert all(torch.equal(s, t) for s, t in zip(a, b))

@@ -391,3 +391,21 @@ def test_second_derivatives(monkeypatch):
     g2 = torch.autograd.grad(5 * (y ** 3).square().sum(), y, create_graph=True)[0]
     want = torch.autograd.grad(g2.square().sum(), y)[0]
     assert float((h.double() - want).abs().max()) <= 1e-5 * float(want.abs().max())
+
+
+def test_gradients_that_the_kernel_cannot_read_are_copied(monkeypatch):
+    """What autograd hands on may be broadcast, strided or start anywhere: it reaches the kernel aligned, with its values."""
+    from paper_2411_03742_b200 import attention as module
+    seen = []
+    monkeypatch.setattr(module, "attention_forward", lambda q, k, v, **how: (q.detach().clone(), torch.zeros(1)))
+    monkeypatch.setattr(module, "attention_backward", lambda dout, q, k, v, out, lse, **how: (seen.append(dout), (dout, k, v))[1])
+    x = torch.randn((2, 3, 2, 16), generator=torch.Generator().manual_seed(1)).bfloat16().requires_grad_()
+    weight = torch.randn(200, generator=torch.Generator().manual_seed(2)).bfloat16()
+    for use, want in ((lambda y: (torch.cat([torch.zeros(3, dtype=y.dtype), y.flatten()]) * weight[:195]).sum(), weight[3:195].view(x.shape)),
+                      (lambda y: y.sum(), torch.ones_like(x)), (lambda y: (torch.cat([y, y[..., :4]], -1).flatten(2) * weight[:40]).sum(), None)):
+        x.grad = None
+        use(module.attention(x, x.detach(), x.detach())).backward()
+        dout = seen.pop()
+        assert dout.data_ptr() % 16 == 0 and dout.stride(3) == 1 and all(s % 8 == 0 and s > 0 for s in dout.stride()[:3])
+        if want is not None:
+            assert torch.equal(dout, want)
