@@ -184,10 +184,10 @@ __device__ __forceinline__ void attn_join(const AttnParams& p, const unsigned ch
     for (int c = 0; c < p.split; ++c) m = fmaxf(m, ld_cluster_f32(row_at + lrow, c));
     float sum = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int c = 0; c < p.split; ++c) {
-      const float top = ld_cluster_f32(row_at + lrow, c);
-      if (top == -INFINITY) continue;            // no key there that the query sees: nothing was kept
-      const float w = exp2_fast(top - m);
-      sum = fmaf(w, ld_cluster_f32(row_at + kAttnTile + lrow, c), sum);
+      const float part = ld_cluster_f32(row_at + kAttnTile + lrow, c);
+      if (part == 0.f) continue;                 // no key there that the query sees: nothing was kept
+      const float w = exp2_fast(ld_cluster_f32(row_at + lrow, c) - m);      // scores that are all NaN have no maximum, but a sum of NaN
+      sum = fmaf(w, part, sum);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const float4 o = ld_cluster_f32x4(keep + lrow * (D * 4) + ((e / 4 + h) ^ (lrow & 7)) * 16, c);

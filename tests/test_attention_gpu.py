@@ -361,3 +361,29 @@ def test_gradients_off_a_16_byte_boundary():
     a = torch.autograd.grad((torch.cat([w[:3], attention(*x).flatten()]) * w).sum(), x)
     b = torch.autograd.grad((attention(*x) * w[3:].view(2, 64, 2, 64).clone()).sum(), x)
     assert all(torch.equal(s, t) for s, t in zip(a, b))
+
+
+@pytest.mark.parametrize("Sq, Sk", [(1, 4000), (130, 2049), (300, 300)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_query_with_a_nan_shows_it(Sq, Sk, D):
+    """One element of one query is NaN: its row of out and lse is NaN and no other, whether its keys are shared between blocks or not;
+    so are its dq and, through dS and P, the gradients of its head's keys."""
+    from paper_2411_03742_b200 import attention_backward, attention_forward
+    g = torch.Generator(device="cuda").manual_seed(Sq)
+    q, dout = (torch.randn((2, Sq, 2, D), generator=g, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn((2, Sk, 2, D), generator=g, device="cuda").bfloat16() for _ in range(2))
+    clean = attention_forward(q, k, v)
+    row = Sq // 2
+    q[1, row, 0, 3] = math.nan
+    out, lse = attention_forward(q, k, v)
+    hit = torch.zeros((2, Sq, 2), dtype=torch.bool, device="cuda")
+    hit[1, row, 0] = True
+    assert out[hit].isnan().all() and lse.transpose(1, 2)[hit].isnan().all()
+    assert torch.equal(out[~hit], clean[0][~hit]) and torch.equal(lse.transpose(1, 2)[~hit], clean[1].transpose(1, 2)[~hit])
+    dq, dk, dv = attention_backward(dout, q, k, v, out, lse)
+    assert dq[hit].isnan().all() and not dq[~hit].isnan().any()
+    for t in (dk, dv):
+        assert t[1, :, 0].isnan().all() and not t[0].isnan().any() and not t[1, :, 1].isnan().any()
+    k[0, Sk - 1, 1, 0] = math.nan                     # a key that every query sees
+    out, lse = attention_forward(q, k, v)
+    assert out[0, :, 1].isnan().all() and lse[0, 1].isnan().all() and not out[0, :, 0].isnan().any()
