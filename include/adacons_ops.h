@@ -70,7 +70,7 @@ int adacons_orth_destroy(adacons_orth *ctx);
  *     O = exp(S - lse) V
  * Key j is visible to query i when j < kv_lens[batch] and, with `causal`, j <= i + kv_len - q_len (the
  * last query sees the last key).  A query that sees no key has O = 0, lse = -inf, and takes no part in any
- * gradient.  Keys from kv_lens[batch] on may hold anything, Inf and NaN included; their gradients are 0.
+ * gradient, whatever its q and dO hold.  Keys from kv_lens[batch] on may hold anything, Inf and NaN included; their gradients are 0.
  * Query heads h kv_heads / q_heads share a key head; its gradients are the sums over them.
  */
 enum { ADACONS_F16 = 2 }; /* attention takes ADACONS_BF16 and ADACONS_F16 */

@@ -23,6 +23,7 @@ namespace adacons {
 // elements, read across them the MN-major operand of a product over tokens, from the same bytes.
 // Keys from kv_len on may hold anything, Inf and NaN included: their rows are zeroed in shared
 // memory before any product over keys (0 x NaN would spread to every query).
+// So are the rows of queries that see no key, of q and dO in the gradient.
 // S, the statistics, the accumulators and dS up to its rounding are fp32; P and dS are rounded to the
 // inputs' 16-bit type as operands of the second products, an error of the size of the results' own rounding.
 // ----------------------------------------------------------------------------------------------
@@ -82,13 +83,13 @@ __device__ __forceinline__ void attn_load_tile(unsigned char* dst, const CUtenso
 #pragma unroll
   for (int h = 0; h < D / 64; ++h) tma_load_4d(dst + h * AttnTile<D>::kBlock, map, bar, h * 64, row, head, batch);
 }
-// rows [first, ROWS) of a tile become zero; called by one warp, before the tile is an operand
-template <int D, int ROWS>
-__device__ __forceinline__ void attn_zero_rows(unsigned char* tile, int first) {
+// rows [from, to) of a tile become zero; called by one warp, before the tile is an operand
+template <int D>
+__device__ __forceinline__ void attn_zero_rows(unsigned char* tile, int from, int to) {
   const int lane = threadIdx.x & 31;
-  for (int k = lane; k < (ROWS - first) * 8; k += 32)
+  for (int k = lane; k < (to - from) * 8; k += 32)
 #pragma unroll
-    for (int h = 0; h < D / 64; ++h) *reinterpret_cast<uint4*>(tile + h * AttnTile<D>::kBlock + first * 128 + k * 16) = make_uint4(0u, 0u, 0u, 0u);
+    for (int h = 0; h < D / 64; ++h) *reinterpret_cast<uint4*>(tile + h * AttnTile<D>::kBlock + from * 128 + k * 16) = make_uint4(0u, 0u, 0u, 0u);
   fence_proxy_async_smem();
   __syncwarp();
 }
@@ -322,7 +323,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
     auto take = [&](int valid) -> uint32_t {
       ok = ok && !s_abort && mbar_wait_bounded(&kv_full[slot], parity);
       ok = __all_sync(0xffffffffu, ok);
-      if (ok && valid < kAttnTile) attn_zero_rows<D, kAttnTile>(smem + L::kKV + slot * L::kT, valid);
+      if (ok && valid < kAttnTile) attn_zero_rows<D>(smem + L::kKV + slot * L::kT, valid, kAttnTile);
       return smem_addr(smem) + L::kKV + slot * L::kT;
     };
     auto advance = [&]() { if (++slot == L::kSlots) { slot = 0; parity ^= 1u; } };
@@ -666,8 +667,8 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
   } else if (items > 0 && warp == G::kMmaWarp) {
     bool ok = __all_sync(0xffffffffu, mbar_wait_bounded(kv_full, 0));
     if (ok && k0 + kAttnTile > kv_len) {
-      attn_zero_rows<D, kAttnTile>(smem, kv_len - k0);
-      attn_zero_rows<D, kAttnTile>(smem + G::kRes, kv_len - k0);
+      attn_zero_rows<D>(smem, kv_len - k0, kAttnTile);
+      attn_zero_rows<D>(smem + G::kRes, kv_len - k0, kAttnTile);
     }
     const bool issuer = elect_one();
     const uint64_t k_desc = AttnDesc<D>::rows(smem_addr(smem)), v_desc = k_desc + (G::kRes >> 4);
@@ -678,7 +679,15 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       tc_fence_after();
       return ok;
     };
+    // Queries of a head's first tile that see no key at all: what their q and dO hold, Inf and NaN included, must not reach a product.
+    const int none = p.causal && k0 == 0 ? -off - first * G::kTok : 0;
+    auto blank = [&](int n, int at) {
+      if (none <= 0 || (skip + n) % per_head != 0) return;
+      attn_zero_rows<D>(smem + L::kRing + at * L::kStage, 0, none);
+      attn_zero_rows<D>(smem + L::kRing + at * L::kStage + G::kStr, 0, none);
+    };
     if (wait(&full[0], 0)) {
+      blank(0, 0);
       const uint64_t q_desc = AttnDesc<D>::rows(ring);
       if (issuer) {
         attn_mma_rows<D, BF16, G::kTok>(t_s, k_desc, q_desc);
@@ -700,6 +709,7 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       __syncwarp();
       if (more) {
         if (!wait(&full[next_stage], next_parity)) break;
+        blank(n + 1, next_stage);
         if (issuer) {
           attn_mma_rows<D, BF16, G::kTok>(t_s, k_desc, next_rows);
           mma_commit(s_full);
@@ -945,7 +955,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       const int ks = j % L::kKs;
       if (!wait(&k_full[ks], (j / L::kKs) & 1)) return;
       unsigned char* at = smem + L::kK + ks * G::kStr;
-      if ((skip + j + 1) * G::kTok > kv_len) attn_zero_rows<D, G::kTok>(at, kv_len - (skip + j) * G::kTok);
+      if ((skip + j + 1) * G::kTok > kv_len) attn_zero_rows<D>(at, kv_len - (skip + j) * G::kTok, G::kTok);
       const uint64_t k_desc = AttnDesc<D>::rows(smem_addr(at));
       if (issuer) {
         attn_mma_rows<D, BF16, G::kTok>(tmem + (j & 1) * G::kTok, q_desc, k_desc);
@@ -957,7 +967,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       const int vs = j % L::kVs;
       if (!wait(&v_full[vs], (j / L::kVs) & 1)) return;
       unsigned char* at = smem + L::kV + vs * G::kStr;
-      if ((skip + j + 1) * G::kTok > kv_len) attn_zero_rows<D, G::kTok>(at, kv_len - (skip + j) * G::kTok);
+      if ((skip + j + 1) * G::kTok > kv_len) attn_zero_rows<D>(at, kv_len - (skip + j) * G::kTok, G::kTok);
       const uint64_t v_desc = AttnDesc<D>::rows(smem_addr(at));
       if (issuer) {
         attn_mma_rows<D, BF16, G::kTok>(t_dp, do_desc, v_desc);
@@ -967,6 +977,10 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       __syncwarp();
     };
     if (wait(q_full, 0)) {
+      if (p.causal && q0 + off < 0) {            // queries that see no key, as on the key side
+        attn_zero_rows<D>(smem, 0, -off - q0);
+        attn_zero_rows<D>(smem + G::kRes, 0, -off - q0);
+      }
       scores(0);
       if (ok) dprobs(0);
     }

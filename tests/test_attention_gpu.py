@@ -387,3 +387,19 @@ def test_a_query_with_a_nan_shows_it(Sq, Sk, D):
     k[0, Sk - 1, 1, 0] = math.nan                     # a key that every query sees
     out, lse = attention_forward(q, k, v)
     assert out[0, :, 1].isnan().all() and lse[0, 1].isnan().all() and not out[0, :, 0].isnan().any()
+
+
+@pytest.mark.parametrize("Sq, Sk, D, H", [(200, 100, 64, 1), (200, 100, 128, 1), (700, 20, 72, 1), (391, 100, 128, 3), (3000, 500, 64, 2), (330, 300, 40, 1), (100, 37, 128, 2)])
+def test_rubbish_in_queries_without_keys(Sq, Sk, D, H):
+    """q and dout of the queries before the first key hold NaN and Inf: not one byte of any result changes."""
+    from paper_2411_03742_b200 import attention_backward, attention_forward
+    g = torch.Generator(device="cuda").manual_seed(Sq)
+    q, dout = (torch.randn((2, Sq, 2 * H, D), generator=g, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn((2, Sk, 2, D), generator=g, device="cuda").bfloat16() for _ in range(2))
+    results = []
+    for _ in range(2):
+        out, lse = attention_forward(q, k, v, causal=True)
+        results.append((out, lse, *attention_backward(dout, q, k, v, out, lse, causal=True)))
+        q[:, :Sq - Sk], dout[:, :Sq - Sk] = math.nan, math.inf
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert not results[1][2][:, :Sq - Sk].any()
