@@ -103,9 +103,13 @@ int adacons_attn_forward(const adacons_attn_shape *shape, const adacons_attn_ten
 /* dq, dk, dv from dout, with the probabilities recomputed from lse.  dq, dk and dv are written, not added to,
  * and must not overlap the inputs.  workspace: device memory of adacons_attn_workspace_bytes, 16-byte
  * aligned, free for other use after the call's work.  It may be NULL where q_heads / kv_heads times q_len, rounded
- * up to a multiple of 128, is at most ADACONS_ATTN_SHORT_ROWS: one launch instead of two, each block making for itself
- * what the first would leave there; quicker for a few short heads.  Errors: as the forward pass. */
+ * up to a multiple of 128, is at most ADACONS_ATTN_SHORT_ROWS (fp16: and kv_len at most ADACONS_ATTN_SHORT_KEYS): one
+ * launch instead of two, each block making for itself what the first would leave there; quicker for a few short heads.
+ * Probabilities and dS are operands of the products in the tensors' type.  fp16 holds them scaled by powers of two (dS from the
+ * largest norms of dout's and v's rows), so that neither long rows nor small or large dout leave its range.
+ * Errors: as the forward pass. */
 #define ADACONS_ATTN_SHORT_ROWS 256
+#define ADACONS_ATTN_SHORT_KEYS 4096
 int adacons_attn_workspace_bytes(const adacons_attn_shape *shape, int64_t *bytes);
 int adacons_attn_backward(const adacons_attn_shape *shape, const adacons_attn_tensor *dout, const adacons_attn_tensor *q,
                           const adacons_attn_tensor *k, const adacons_attn_tensor *v, const adacons_attn_tensor *out,

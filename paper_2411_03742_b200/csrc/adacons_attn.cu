@@ -153,17 +153,23 @@ bool run_forward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap
                 mq, mk, mv, p);
 }
 
+template <int D> int stat_blocks(int rows) { return static_cast<int>((static_cast<int64_t>(rows) + kAttnStatRows<D> - 1) / kAttnStatRows<D>); }
+
 template <int D, bool BF16>
 bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo, AttnParams p, const adacons_attn_tensor* dout,
-                  const adacons_attn_tensor* out, const float* lse, AttnOut dq, AttnOut dk, AttnOut dv, float* lse2, float* delta, int sms, cudaStream_t st) {
+                  const adacons_attn_tensor* v, const adacons_attn_tensor* out, const float* lse, AttnOut dq, AttnOut dk, AttnOut dv, float* lse2, float* delta, float* peaks,
+                  int sms, cudaStream_t st) {
   p.dout = {dout->data, dout->batch_stride, dout->seq_stride, dout->head_stride};
   p.o = {out->data, out->batch_stride, out->seq_stride, out->head_stride};
+  p.v = {v->data, v->batch_stride, v->seq_stride, v->head_stride};
   p.lse_in = lse;
   p.lse2 = lse2;
   p.delta = delta;
   const bool separate = delta != nullptr && p.sq_pad > 0;
   if (separate) {
-    if (!launch(&attn_delta_kernel<D, BF16>, dim3(p.sq_pad / (256 / (D / 8)), p.Hq, p.B), dim3(256), 0, st, kLaunchPlain, 1, p, lse2, delta)) return false;
+    const int q_blocks = p.sq_pad / kAttnStatRows<D>, k_blocks = BF16 ? 0 : stat_blocks<D>(p.Sk);
+    if (!launch(&attn_delta_kernel<D, BF16>, dim3(q_blocks + k_blocks, p.Hq, p.B), dim3(256), 0, st, kLaunchPlain, 1, p, lse2, delta, peaks)) return false;
+    if (!BF16) p.peaks = peaks;
   }
   p.out = dq;
   p.dk = dk;
@@ -178,9 +184,15 @@ bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMa
                 separate ? kLaunchOverlap : kLaunchPlain, p.split, mq, mk, mv, mdo, p, static_cast<int>(key_blocks), static_cast<int>(q_tiles));
 }
 
+// lse2 and delta of every padded row; fp16: a maximum for each block of the kernel that makes them, of q's rows and of v's
 int64_t workspace_bytes(const adacons_attn_shape* s) {
   const int64_t pad = (static_cast<int64_t>(s->q_len) + kAttnTile - 1) / kAttnTile * kAttnTile;
-  return 2 * sizeof(float) * pad * s->q_heads * s->batch;
+  int64_t words = 2 * pad * s->q_heads;
+  if (s->dtype == ADACONS_F16) {
+    const int64_t rows = s->head_dim <= 64 ? kAttnStatRows<64> : kAttnStatRows<128>;
+    words += pad / rows * s->q_heads + (s->kv_len + rows - 1) / rows * s->kv_heads;
+  }
+  return static_cast<int64_t>(sizeof(float)) * words * s->batch;
 }
 
 }  // namespace
@@ -234,7 +246,8 @@ int adacons_attn_backward(const adacons_attn_shape* s, const adacons_attn_tensor
   if (s->q_len > 0) {
     const int64_t pad = (static_cast<int64_t>(s->q_len) + kAttnTile - 1) / kAttnTile * kAttnTile;
     if (lse == nullptr || reinterpret_cast<uintptr_t>(lse) % 4 != 0) return ADACONS_EINVAL;
-    if (workspace == nullptr ? s->q_heads / s->kv_heads * pad > ADACONS_ATTN_SHORT_ROWS : bytes < workspace_bytes(s)) return ADACONS_EINVAL;
+    const bool is_short = s->q_heads / s->kv_heads * pad <= ADACONS_ATTN_SHORT_ROWS && (s->dtype == ADACONS_BF16 || s->kv_len <= ADACONS_ATTN_SHORT_KEYS);
+    if (workspace == nullptr ? !is_short : bytes < workspace_bytes(s)) return ADACONS_EINVAL;
   }
   if (reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return ADACONS_EALIGN;
   AttnDevice* d = nullptr;
@@ -248,8 +261,9 @@ int adacons_attn_backward(const adacons_attn_shape* s, const adacons_attn_tensor
   const AttnParams p = base_params(*d, s);
   float* lse2 = static_cast<float*>(workspace);
   float* delta = lse2 == nullptr ? nullptr : lse2 + static_cast<int64_t>(p.B) * p.Hq * p.sq_pad;
+  float* peaks = delta == nullptr ? nullptr : delta + static_cast<int64_t>(p.B) * p.Hq * p.sq_pad;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  auto go = [&](auto run) { return run(mq, mk, mv, mdo, p, dout, out, lse, as_out(dq), as_out(dk), as_out(dv), lse2, delta, d->info.sms, st); };
+  auto go = [&](auto run) { return run(mq, mk, mv, mdo, p, dout, v, out, lse, as_out(dq), as_out(dk), as_out(dv), lse2, delta, peaks, d->info.sms, st); };
   bool ok;
   if (s->head_dim <= 64) ok = s->dtype == ADACONS_BF16 ? go(run_backward<64, true>) : go(run_backward<64, false>);
   else ok = s->dtype == ADACONS_BF16 ? go(run_backward<128, true>) : go(run_backward<128, false>);

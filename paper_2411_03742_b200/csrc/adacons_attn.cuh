@@ -26,6 +26,12 @@ namespace adacons {
 // So are the rows of queries that see no key, of q and dO in the gradient.
 // S, the statistics, the accumulators and dS up to its rounding are fp32; P and dS are rounded to the
 // inputs' 16-bit type as operands of the second products, an error of the size of the results' own rounding.
+// fp16 has that error only between 2^-14 and 2^16, and the gradient's P and dS lie far below on long rows or under small dO (P near
+// 2^-16 on 65,536 keys, whose dV was off by 7e-4 instead of 3e-4, and dQ by 8e-3 under dO of 0.01).  There they are rounded
+// as 2^12 P and 2^k dS, with 2^k from the bound |dS| <= 2 max |dO_i| max |V_j| over the queries and keys of a key head, so that
+// nothing overflows either, and the results are multiplied by 2^-12 and 2^-k.  The norms' maxima come with Delta, one for each block
+// of that kernel, and every block of the gradient looks through its head's: 3.54 ms against bf16's 3.39 (8192 x 8192, 32 / 8 heads of
+// 128), 28.9 against 24.8 us (8 x 256 tokens, 16 heads of 64).
 // ----------------------------------------------------------------------------------------------
 constexpr int kAttnTile = 128;
 constexpr int kFwdThreads = 320;                 // warps 0-7 softmax, 8 copies, 9 products
@@ -43,13 +49,19 @@ struct AttnParams {
   float scale, scale_log2;       // scale, scale * log2(e)
   const int* kv_lens;            // [B] or null
   float* lse;                    // forward: [B][Hq][Sq]
-  const float* lse2;             // backward: lse log2(e), +inf where a row has no key or does not exist: [B][Hq][sq_pad]
+  const float* lse2;             // backward: lse log2(e) - kAttnShift, +inf where a row has no key or does not exist: [B][Hq][sq_pad]
   const float* delta;            // likewise, 0 there; null: each block makes both for its own queries, from what follows
-  AttnRows dout, o;
+  const float* peaks;            // fp16, with a workspace: |dO_i|^2 at most, of the queries of each block of the kernel before: [B][Hq][blocks], then |V_j|^2: [B][Hkv][blocks]
+  AttnRows dout, o, v;
   const float* lse_in;           // [B][Hq][Sq]
   AttnOut out, dk, dv;           // forward: O; backward: dQ, dK, dV
   uint32_t* flags;
 };
+
+// P in an fp16 gradient is 2^kAttnShift P: whole rows of a million keys keep their 11 bits, and a P a little above one still fits.
+template <bool BF16> constexpr float kAttnShift = BF16 ? 0.f : 12.f;
+template <bool BF16> constexpr float kAttnUnshift = BF16 ? 1.f : 1.f / 4096.f;
+template <int D> constexpr int kAttnStatRows = 256 / (D / 8);     // rows of a block of the statistics kernel
 
 template <int D> struct AttnTile {
   static constexpr uint32_t kBlock = kAttnTile * 128;         // 128 rows x 64 elements
@@ -498,6 +510,17 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
 // ----------------------------------------------------------------------------------------------
 // U rows of each group of lanes, `step` places apart from place n on: rows of `heads` heads from `head` on, `pitch` places
 // each; `total` places in all.  Whole warps.
+template <bool BF16>
+__device__ __forceinline__ float attn_dot8(const uint4& x, const uint4& y) {
+  const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 a = unpack16<BF16>(xs[k]), b = unpack16<BF16>(ys[k]);
+    sum += a.x * b.x + a.y * b.y;
+  }
+  return sum;
+}
 template <int D, bool BF16, int U>
 __device__ __forceinline__ void attn_row_stats(const AttnParams& p, int batch, int head, int first_row, int pitch, int n, int step, int total, float* lse2, float* delta) {
   constexpr int kLanes = D / 8;
@@ -519,19 +542,13 @@ __device__ __forceinline__ void attn_row_stats(const AttnParams& p, int batch, i
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const uint32_t xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w}, ys[4] = {y[u].x, y[u].y, y[u].z, y[u].w};
-    float sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float2 a = unpack16<BF16>(xs[k]), b = unpack16<BF16>(ys[k]);
-      sum += a.x * b.x + a.y * b.y;
-    }
+    float sum = attn_dot8<BF16>(x[u], y[u]);
 #pragma unroll
     for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const int at = n + u * step;
     if (e == 0 && at < total) {
       const bool none = l[u] == -INFINITY;
-      lse2[at] = none ? INFINITY : l[u] * kLog2e;
+      lse2[at] = none ? INFINITY : fmaf(l[u], kLog2e, -kAttnShift<BF16>);
       delta[at] = none ? 0.f : sum;
     }
   }
@@ -545,9 +562,103 @@ __device__ __forceinline__ void attn_block_stats(const AttnParams& p, int batch,
   asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
 }
 
+// The largest |x|^2 of rows n, n + step, .. below `total`, D / 8 lanes a row.  `row_at`: where place n is, null where it does not count.
+template <int D, int STEP, typename RowAt>
+__device__ __forceinline__ float attn_peak(const AttnParams& p, int64_t total, RowAt row_at) {
+  constexpr int kLanes = D / 8, kU = 4;
+  const int e = 8 * (threadIdx.x % kLanes);
+  float peak = 0.f;
+  for (int64_t base = 0; base < total; base += kU * STEP) {
+    uint4 x[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int64_t n = base + u * STEP + threadIdx.x / kLanes;
+      const unsigned short* at = n < total && e < p.D ? row_at(n) : nullptr;
+      x[u] = at != nullptr ? *reinterpret_cast<const uint4*>(at + e) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      float sum = attn_dot8<false>(x[u], x[u]);
+#pragma unroll
+      for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      peak = fmaxf(peak, sum);
+    }
+  }
+  return peak;
+}
+__device__ __forceinline__ const unsigned short* attn_row(const AttnRows& t, int batch, int64_t row, int head) {
+  return static_cast<const unsigned short*>(t.p) + batch * t.batch + row * t.seq + head * t.head;
+}
+__device__ __forceinline__ bool attn_has_key(const AttnParams& p, int batch, int head, int64_t row) {
+  return p.lse_in[(static_cast<long long>(batch) * p.Hq + head) * p.Sq + row] != -INFINITY;
+}
+
+// fp16: 2^k for the dS of a key head, by the THREADS elementwise threads of a block, all blocks of the head alike.  The bound's
+// slack is a few binades of the forty that fp16 has.
+template <int D, int THREADS>
+__device__ __forceinline__ float attn_ds_scale(const AttnParams& p, int batch, int kv_head, int kv_len) {
+  __shared__ float s_peak[2][THREADS / 32];
+  const int group = p.Hq / p.Hkv;
+  float peak[2] = {0.f, 0.f};                      // |dO|^2, |V|^2
+  if (p.peaks != nullptr) {
+    const long long qb = p.sq_pad / kAttnStatRows<D>, kb = (p.Sk + kAttnStatRows<D> - 1ll) / kAttnStatRows<D>;
+    const float* at[2] = {p.peaks + (static_cast<long long>(batch) * p.Hq + kv_head * group) * qb,
+                          p.peaks + static_cast<long long>(p.B) * p.Hq * qb + (static_cast<long long>(batch) * p.Hkv + kv_head) * kb};
+    const long long count[2] = {group * qb, kb};
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll 4
+      for (long long k = threadIdx.x; k < count[t]; k += THREADS) peak[t] = fmaxf(peak[t], at[t][k]);
+  } else {
+    peak[0] = attn_peak<D, THREADS / (D / 8)>(p, static_cast<int64_t>(group) * p.Sq, [&](int64_t n) {
+      const int head = kv_head * group + static_cast<int>(n / p.Sq), row = static_cast<int>(n % p.Sq);
+      return attn_has_key(p, batch, head, row) ? attn_row(p.dout, batch, row, head) : nullptr;
+    });
+    peak[1] = attn_peak<D, THREADS / (D / 8)>(p, kv_len, [&](int64_t n) { return attn_row(p.v, batch, n, kv_head); });
+  }
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) peak[t] = fmaxf(peak[t], __shfl_xor_sync(0xffffffffu, peak[t], o));
+    if ((threadIdx.x & 31) == 0) s_peak[t][threadIdx.x >> 5] = peak[t];
+  }
+  asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+    for (int w = 0; w < THREADS / 32; ++w) peak[t] = fmaxf(peak[t], s_peak[t][w]);
+  const float square = peak[0] * peak[1];          // 2^-96 .. 2^78
+  if (!(square > 0.f && square < INFINITY)) return 1.f;
+  const int half = ((__float_as_int(square) >> 23) - 127 >> 1) + 1;      // |dO| |V| < 2^half, so |dS| < 2^(half + 1): 2^k dS < 2^14
+  return __int_as_float((13 - half + 127) << 23);
+}
+
 template <int D, bool BF16>
-__global__ void __launch_bounds__(256) attn_delta_kernel(const AttnParams p, float* lse2, float* delta) {      // grid: rows of a head, heads, batch
+__global__ void __launch_bounds__(256) attn_delta_kernel(const AttnParams p, float* lse2, float* delta, float* peaks) {      // grid: rows of a head (fp16: of q, then of v), heads, batch
   pdl_launch_dependents();
+  if constexpr (!BF16) {
+    __shared__ float s_peak[8];
+    constexpr int kRows = kAttnStatRows<D>;
+    const int qb = p.sq_pad / kRows, x = static_cast<int>(blockIdx.x);
+    const bool keys = x >= qb;
+    const int head = blockIdx.y, batch = blockIdx.z;
+    if (keys && head >= p.Hkv) return;
+    const int64_t first = static_cast<int64_t>(keys ? x - qb : x) * kRows;
+    const int kv_len = attn_kv_len(p, batch);
+    float peak = attn_peak<D, kRows>(p, kRows, [&](int64_t n) -> const unsigned short* {
+      if (keys) return first + n < kv_len ? attn_row(p.v, batch, first + n, head) : nullptr;
+      return first + n < p.Sq && attn_has_key(p, batch, head, first + n) ? attn_row(p.dout, batch, first + n, head) : nullptr;
+    });
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) peak = fmaxf(peak, __shfl_xor_sync(0xffffffffu, peak, o));
+    if ((threadIdx.x & 31) == 0) s_peak[threadIdx.x >> 5] = peak;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 1; w < 8; ++w) peak = fmaxf(peak, s_peak[w]);
+      const long long kb = static_cast<int>(gridDim.x) - qb;
+      peaks[keys ? static_cast<long long>(p.B) * p.Hq * qb + (static_cast<long long>(batch) * p.Hkv + head) * kb + (x - qb) : (static_cast<long long>(batch) * p.Hq + head) * qb + x] = peak;
+    }
+    if (keys) return;
+  }
   const long long at = (static_cast<long long>(blockIdx.z) * p.Hq + blockIdx.y) * p.sq_pad;
   attn_row_stats<D, BF16, 1>(p, blockIdx.z, blockIdx.y, 0, p.sq_pad, blockIdx.x * (256 / (D / 8)) + threadIdx.x / (D / 8), 0, p.sq_pad, lse2 + at, delta + at);
 }
@@ -603,6 +714,7 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
   uint64_t* drain = done + 1;
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
+  __shared__ float s_by_dk;                      // fp16 only
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int k0 = tile * kAttnTile;
   const int group = p.Hq / p.Hkv;
@@ -752,6 +864,15 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       float* at = reinterpret_cast<float*>(smem + L::kTable);
       attn_block_stats<D, BF16, G::kElem * 32>(p, batch, kv_head * group, 0, q_tiles * G::kTok, group * q_tiles * G::kTok, at, at + ADACONS_ATTN_SHORT_ROWS);
     }
+    float by_ds = 1.f, by_dk = p.scale;            // from 2^shift P (dP - Delta) to what is rounded; from the sum to dK
+    if constexpr (!BF16) {
+      if (all > 0) {
+        const float up = attn_ds_scale<D, G::kElem * 32>(p, batch, kv_head, kv_len);
+        by_ds = up * kAttnUnshift<BF16>;
+        by_dk = p.scale / up;
+        if (threadIdx.x == 0) s_by_dk = by_dk;
+      }
+    }
     int stage = 0, in_head = items > 0 ? skip % per_head : 0, head_at = items > 0 ? skip / per_head * q_tiles * G::kTok : 0;
     uint32_t stage_parity = 0;
     for (int n = 0; n < items; ++n) {
@@ -804,6 +925,10 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
           const float4 l = delta[g];
           float2 a = add2(make_float2(__uint_as_float(d[4 * g]), __uint_as_float(d[4 * g + 1])), make_float2(-l.x, -l.y));
           float2 b = add2(make_float2(__uint_as_float(d[4 * g + 2]), __uint_as_float(d[4 * g + 3])), make_float2(-l.z, -l.w));
+          if constexpr (!BF16) {
+            a = mul2(a, make_float2(by_ds, by_ds));
+            b = mul2(b, make_float2(by_ds, by_ds));
+          }
           a = mul2(a, make_float2(pr[4 * g], pr[4 * g + 1]));
           b = mul2(b, make_float2(pr[4 * g + 2], pr[4 * g + 3]));
           w[2 * g] = pack16<BF16>(a.x, a.y);
@@ -825,7 +950,7 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
     if (items > 0) {
       if (ok) wait(done, 0);
       if (ok && p.key_split > 1) attn_keep_row<D, 2>(smem + (is_dv ? 0 : kAttnTile * D * 4), (is_dv ? t_dv : t_dk) + lanes, columns, (warp & 3) * 32 + lane);
-      else if (ok) attn_store_row<2, BF16>(p, mine, (is_dv ? t_dv : t_dk) + lanes, columns, batch, kv_head, key, live, is_dv ? 1.f : p.scale);
+      else if (ok) attn_store_row<2, BF16>(p, mine, (is_dv ? t_dv : t_dk) + lanes, columns, batch, kv_head, key, live, is_dv ? kAttnUnshift<BF16> : by_dk);
       else s_abort = 1;
     } else if (p.key_split == 1 && live && columns == 0) {
       attn_zero_row(p, mine, batch, kv_head, key);
@@ -842,8 +967,8 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
   if (p.key_split > 1) {
     const int shares = all == 0 ? 0 : (all + share - 1) / share;
     cluster_sync_all();
-    attn_join_sum<D, BF16, G::kThreads>(p, p.dv, smem, rank, shares, k0, p.Sk, kv_head, batch, 1.f);
-    attn_join_sum<D, BF16, G::kThreads>(p, p.dk, smem + kAttnTile * D * 4, rank, shares, k0, p.Sk, kv_head, batch, p.scale);
+    attn_join_sum<D, BF16, G::kThreads>(p, p.dv, smem, rank, shares, k0, p.Sk, kv_head, batch, kAttnUnshift<BF16>);
+    attn_join_sum<D, BF16, G::kThreads>(p, p.dk, smem + kAttnTile * D * 4, rank, shares, k0, p.Sk, kv_head, batch, BF16 || all == 0 ? p.scale : s_by_dk);
     cluster_sync_all();                          // the others may still read this block's share
   }
 }
@@ -883,6 +1008,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
   uint64_t* drain = done + 1;
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_abort;
+  __shared__ float s_by_dq;                      // fp16 only
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int q0 = tile * kAttnTile;
 
@@ -1019,6 +1145,15 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       lse2 = at[row - q0];
       delta = at[kAttnTile + row - q0];
     }
+    float by_ds = 1.f, by_dq = p.scale;
+    if constexpr (!BF16) {
+      if (all > 0) {
+        const float up = attn_ds_scale<D, G::kElem * 32>(p, batch, head / (p.Hq / p.Hkv), kv_len);
+        by_ds = up * kAttnUnshift<BF16>;
+        by_dq = p.scale / up;
+        if (threadIdx.x == 0) s_by_dq = by_dq;
+      }
+    }
     const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), lse22 = make_float2(-lse2, -lse2), delta2 = make_float2(-delta, -delta);
     const int limit = p.causal ? min(kv_len, row + off + 1) : kv_len;
     const int warp_limit = p.causal ? min(kv_len, row - lane + off + 1) : kv_len;
@@ -1061,7 +1196,9 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
         __syncwarp();
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const float2 a = mul2(add2(make_float2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1])), delta2), make_float2(pr[2 * e], pr[2 * e + 1]));
+          float2 a = add2(make_float2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1])), delta2);
+          if constexpr (!BF16) a = mul2(a, make_float2(by_ds, by_ds));
+          a = mul2(a, make_float2(pr[2 * e], pr[2 * e + 1]));
           w[e] = pack16<BF16>(a.x, a.y);
         }
       }
@@ -1076,7 +1213,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       if (ok) wait(done, 0);
       if (p.query_split > 1) {
         if (ok && part < D / 64) attn_keep_row<D, 2>(smem, t_dq + lanes, part * 64, row - q0);
-      } else if (ok && part < D / 64) attn_store_row<2, BF16>(p, p.out, t_dq + lanes, part * 64, batch, head, row, live, p.scale);
+      } else if (ok && part < D / 64) attn_store_row<2, BF16>(p, p.out, t_dq + lanes, part * 64, batch, head, row, live, by_dq);
       if (!ok) s_abort = 1;
     } else if (p.query_split == 1 && live && part == 0) {
       attn_zero_row(p, p.out, batch, head, row);
@@ -1092,7 +1229,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
   }
   if (p.query_split > 1) {
     cluster_sync_all();
-    attn_join_sum<D, BF16, G::kThreads>(p, p.out, smem, rank, all == 0 ? 0 : (all + share - 1) / share, q0, p.Sq, head, batch, p.scale);
+    attn_join_sum<D, BF16, G::kThreads>(p, p.out, smem, rank, all == 0 ? 0 : (all + share - 1) / share, q0, p.Sq, head, batch, BF16 || all == 0 ? p.scale : s_by_dq);
     cluster_sync_all();
   }
 }

@@ -403,3 +403,76 @@ def test_rubbish_in_queries_without_keys(Sq, Sk, D, H):
         q[:, :Sq - Sk], dout[:, :Sq - Sk] = math.nan, math.inf
     assert all(torch.equal(a, b) for a, b in zip(*results))
     assert not results[1][2][:, :Sq - Sk].any()
+
+
+@pytest.mark.parametrize("Sq, Sk, Hq, Hk, D, by_dout, by_v, by_qk, lens", [
+    (130, 40000, 2, 1, 64, 1.0, 1.0, 1.0, None), (300, 70001, 1, 1, 128, 0.02, 1.0, 1.0, None), (1, 66000, 4, 2, 72, 1.0, 1.0, 1.0, None),
+    (700, 9000, 2, 2, 40, 0.01, 0.5, 1.0, [8000, 9000]), (2000, 2000, 4, 2, 64, 1e-3, 4.0, 1.0, None), (77, 3, 2, 1, 64, 1000.0, 30.0, 0.05, None),
+    (1000, 2, 1, 1, 128, 2000.0, 20.0, 0.02, [2, 1])])
+def test_half_precision_far_from_one(Sq, Sk, Hq, Hk, D, by_dout, by_v, by_qk, lens):
+    """fp16 gradients where P or dS would leave the type's range if they were rounded as they are: below 2^-14 on long rows and under
+    small dout, above 65504 under a large one.  The bounds are those of `close`, and half a unit of the smallest fp16 numbers, 2^-25, for
+    each result below 2^-14, and for dP - Delta, which a query with one key cancels to nothing, 2^-20 of the sums that are
+    subtracted (fp32, which the tensor cores round toward zero).  In the last case some of dv are beyond 65504.  Values hidden behind kv_lens are Inf and must not count."""
+    from paper_2411_03742_b200 import attention, attention_backward, attention_forward
+    g = torch.Generator(device="cuda").manual_seed(Sk)
+    rnd = lambda n, s, h, by: (torch.randn((n, s, h, D), generator=g, device="cuda") * by).half()  # noqa: E731
+    B = 1 if lens is None else len(lens)
+    q, k, v, dout = rnd(B, Sq, Hq, by_qk), rnd(B, Sk, Hk, by_qk), rnd(B, Sk, Hk, by_v), rnd(B, Sq, Hq, by_dout)
+    L = None if lens is None else torch.tensor(lens, dtype=torch.int32, device="cuda")
+    vs = v.clone()
+    for b, n in enumerate(lens or []):
+        v[b, n:] = math.inf
+    out, lse = attention_forward(q, k, v, kv_lens=L)
+    grads = attention_backward(dout, q, k, v, out, lse, kv_lens=L)
+    again = attention_backward(dout, q, k, v, out, lse, kv_lens=L)
+    torch.cuda.synchronize()
+    assert attention.status() == 0 and all(torch.equal(a, b) for a, b in zip(grads, again))
+    sc, u, tiny = 1 / math.sqrt(D), U[torch.float16], 2.0 ** -25
+    for b in range(B):                                  # one batch at a time: the 64-bit form is large
+        one = slice(b, b + 1)
+        _, _, P = plain_forward(q[one], k[one], vs[one], sc, False, None if L is None else L[one])
+        wants = plain_backward(q[one], k[one], vs[one], sc, P, out[one], dout[one])
+        r = Hq // Hk
+        share = lambda x: x.view(1, Hk, r, Sk, D).sum(2)  # noqa: E731
+        dO, O = heads(dout[one]).abs(), heads(out[one]).abs()
+        noise = 2.0 ** -20 * sc * P * (dO @ heads(vs[one], r).abs().mT + (dO * O).sum(-1, keepdim=True))
+        noises = (noise @ heads(k[one], r).abs(), share(noise.mT @ heads(q[one]).abs()), 2.0 ** -20 * share(P.mT @ dO))
+        for name, got, want, extra in zip(("dq", "dk", "dv"), grads, wants, noises):
+            err, n = (got[one].double().transpose(1, 2) - want).abs(), want.numel()
+            beyond = want.abs() > 65504 * (1 - 4 * u)           # the type has no number for it: Inf is the answer
+            assert not (err.isinf() & ~beyond).any()
+            err = err.masked_fill(err.isinf() & beyond, 0.0)
+            rms = float(want.norm()) / math.sqrt(n)
+            assert float(err.norm()) <= u * float(want.norm()) + tiny * math.sqrt(n) + float(extra.norm()), (name, float(err.norm() / want.norm()))
+            assert bool((err <= 4 * u * want.abs() + 8 * u * rms + tiny + extra).all()), (name, float(err.max()), rms)
+
+
+@pytest.mark.parametrize("B, Sq, Sk, Hq, Hk, D, causal", [(3, 77, 91, 4, 2, 40, False), (1, 1, 300, 2, 1, 128, True), (2, 128, 1025, 2, 2, 128, False), (1, 256, 256, 3, 3, 64, True),
+                                                           (1, 2, 4096, 2, 2, 64, False)])
+def test_short_half_precision_with_and_without_a_workspace(B, Sq, Sk, Hq, Hk, D, causal, monkeypatch):
+    """The powers of two found in each block and those of the kernel before it are the same: the gradients agree bit for bit."""
+    from paper_2411_03742_b200 import attention, attention_backward, attention_forward
+    g = torch.Generator(device="cuda").manual_seed(Sq + D)
+    q, dout = (torch.randn((B, Sq, Hq, D), generator=g, device="cuda").half() for _ in range(2))
+    k, v = (torch.randn((B, Sk, Hk, D), generator=g, device="cuda").half() for _ in range(2))
+    dout *= 1e-3
+    lens = torch.randint(0, Sk + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    out, lse = attention_forward(q, k, v, causal=causal, kv_lens=lens)
+    work = torch.full((attention.workspace_bytes(q, k),), 255, dtype=torch.uint8, device="cuda")
+    two = attention_backward(dout, q, k, v, out, lse, causal=causal, kv_lens=lens, workspace=work)
+    monkeypatch.setattr(attention, "_one_launch", lambda q, k: True)
+    monkeypatch.setattr(attention, "_plans", attention._Plans())
+    one = attention_backward(dout, q, k, v, out, lse, causal=causal, kv_lens=lens)
+    assert all(torch.equal(x, y) for x, y in zip(one, two))
+
+
+def test_many_keys_need_a_workspace_in_half_precision():
+    import ctypes
+    from paper_2411_03742_b200.attention import _Shape, _Tensor
+    from paper_2411_03742_b200.binding import EINVAL, load_library
+    t = torch.zeros((1, 4097, 1, 64), dtype=torch.float16, device="cuda")
+    rows = torch.zeros((1, 1, 8), device="cuda")
+    s, x = _Shape(2, 1, 1, 1, 8, 4097, 64, 0, 0.125, None), _Tensor(t.data_ptr(), *t.stride()[:3])
+    r = ctypes.byref
+    assert load_library().adacons_attn_backward(r(s), r(x), r(x), r(x), r(x), r(x), rows.data_ptr(), r(x), r(x), r(x), None, 0, None) == EINVAL
