@@ -139,7 +139,7 @@ def check_rope(dim: int, x, positions, out, want_cuda: bool = True, device=None)
         raise ValueError(f"x is on device {x.get_device()}, the angles are on device {device}")
     if any(n > 1 and s == 0 for n, s in zip(out.shape, out.stride())):
         raise ValueError("out must not be a broadcast view")
-    if out.data_ptr() == x.data_ptr() and out.stride() != x.stride():
+    if x.numel() > 0 and out.data_ptr() == x.data_ptr() and out.stride() != x.stride():      # tensors without elements may all be at address 0
         raise ValueError("in place, out must be x itself")
     if positions is not None and (positions.dtype != torch.int32 or tuple(positions.shape) != tuple(x.shape[:2]) or not positions.is_contiguous() or positions.device != x.device):
         raise ValueError(f"positions must be a contiguous int32 tensor of shape {tuple(x.shape[:2])} on x's device")
@@ -157,5 +157,5 @@ class _Turn(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         pos = ctx.saved_tensors[0] if ctx.saved_tensors else None
-        dy = dy if dy.stride(3) == 1 else dy.contiguous()
+        dy = dy if dy.stride(3) == 1 else dy.clone(memory_format=torch.contiguous_format)
         return _Turn.apply(dy, ctx.rope, pos, ctx.first, not ctx.inverse), None, None, None, None

@@ -409,3 +409,16 @@ def test_gradients_that_the_kernel_cannot_read_are_copied(monkeypatch):
         assert dout.data_ptr() % 16 == 0 and dout.stride(3) == 1 and all(s % 8 == 0 and s > 0 for s in dout.stride()[:3])
         if want is not None:
             assert torch.equal(dout, want)
+
+
+def test_turns_of_nothing_in_any_layout():
+    """Tensors without elements share the address 0 whatever their strides: that does not make them an in-place call."""
+    from paper_2411_03742_b200 import rope
+    for shape in ((2, 0, 6, 16), (0, 3, 6, 16)):
+        x = torch.zeros(shape)[:, :, :4]
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        assert x.data_ptr() == out.data_ptr() == 0
+        rope.check_rope(16, x, None, out, want_cuda=False)
+    x = torch.zeros((2, 3, 6, 16))
+    with pytest.raises(ValueError, match="in place"):
+        rope.check_rope(16, x[:, :, :4], None, torch.as_strided(x, (2, 3, 4, 16), (192, 64, 16, 1)), want_cuda=False)

@@ -150,3 +150,15 @@ def test_second_derivatives():
         want = torch.autograd.grad(g2.square().sum(), y)[0]
     # fp32 throughout: two turns each way at 1e-6 of their pairs
     assert float((h.double() - want).norm() / want.norm()) <= 1e-5
+
+
+def test_empty_slices():
+    """No tokens, no sequences, no heads, in slices of a packed projection; and back through autograd."""
+    from paper_2411_03742_b200 import Rope
+    with Rope(16) as rope:
+        for shape, heads in (((2, 0, 6, 16), 4), ((0, 3, 6, 16), 4), ((2, 3, 6, 16), 0)):
+            packed = torch.zeros(shape, device="cuda", requires_grad=True)
+            y = rope(packed[:, :, :heads])
+            assert y.shape == (*shape[:2], heads, 16)
+            y.sum().backward()
+            assert packed.grad.shape == shape and not packed.grad.any()
