@@ -422,3 +422,14 @@ def test_turns_of_nothing_in_any_layout():
     x = torch.zeros((2, 3, 6, 16))
     with pytest.raises(ValueError, match="in place"):
         rope.check_rope(16, x[:, :, :4], None, torch.as_strided(x, (2, 3, 4, 16), (192, 64, 16, 1)), want_cuda=False)
+
+
+def test_what_the_readme_imports_can_be_called():
+    """Every name that the README's snippets import from the package is a class or a function, not a module of that name."""
+    import importlib
+    text = open(os.path.join(ROOT, "README.md")).read()
+    found = re.findall(r"^from (paper_2411_03742_b200[\w.]*) import ([\w, ]+)$", text, flags=re.M)
+    names = [(module, name.strip()) for module, several in found for name in several.split(",")]
+    assert {"AdaCons", "Orthogonalizer", "Rope", "attention", "attention_forward", "attention_backward"} <= {n for _, n in names}
+    for module, name in names:
+        assert callable(getattr(importlib.import_module(module), name)), (module, name)
