@@ -88,7 +88,8 @@ struct OrthParams {
 
 // ----------------------------------------------------------------------------------------------
 // |G|_F^2 by chunks: fp64 throughout, so that no magnitude of the input over- or underflows; the
-// blocks' sums are added in a fixed order by whoever needs the norm.
+// blocks' sums are added in a fixed order by whoever needs the norm.  What it multiplies by, 2^11 / (|G|_F + eps), can lie
+// outside fp32 where G does not (norms below 6e-36): then it goes in two steps, the first an exact power of two.
 // ----------------------------------------------------------------------------------------------
 template <int DT>
 __device__ __forceinline__ float orth_in(const void* p, long long i) {
@@ -112,6 +113,18 @@ __device__ __forceinline__ void orth_in8(const void* p, long long i, float (&v)[
     }
   }
 }
+
+struct OrthFactor {
+  float first, then;                               // first: 1 unless the factor is outside 2^-100 .. 2^100
+  __device__ __forceinline__ OrthFactor(double square, double eps) {
+    const double norm = sqrt(square) + eps;
+    double by = static_cast<double>(kOrthXScale) / (norm > 0.0 ? fmax(norm, 0x1p-189) : norm);     // the smallest fp32 number is 2^-149: below it is eps, of a matrix of zeros
+    first = 1.f;
+    if (by > 0x1p100 && by < INFINITY) { first = 0x1p100f; by *= 0x1p-100; }
+    else if (by < 0x1p-100 && by > 0.0) { first = 0x1p-100f; by *= 0x1p100; }
+    then = static_cast<float>(by);
+  }
+};
 
 template <int DT>
 __global__ void __launch_bounds__(256) orth_norm_kernel(const void* in, int aligned, const OrthMat* mats, const OrthChunk* chunks, double* partial) {
@@ -175,7 +188,7 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, int alig
   __syncthreads();
   sum = 0.0;
   for (int w = 0; w < 8; ++w) sum += s_sum[w];
-  const float mul = static_cast<float>(static_cast<double>(kOrthXScale) / (sqrt(sum) + eps));
+  const OrthFactor by(sum, eps);
   const int rows = m.transposed ? m.l : m.r, cols = m.transposed ? m.r : m.l;      // as it lies in the vector, row-major
   const bool vec = aligned && m.vec_in && cols % 8 == 0;
   const int r = m.r, ldx = m.ldx, transposed = m.transposed;
@@ -191,7 +204,7 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, int alig
       orth_in8<DT>(in, offset + static_cast<long long>(row) * cols + col, v);
       __half h[8], l[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) orth_split(v[e] * mul, h[e], l[e]);
+      for (int e = 0; e < 8; ++e) orth_split(v[e] * by.first * by.then, h[e], l[e]);
       const long long at = static_cast<long long>(row) * ldx + col;
       *reinterpret_cast<uint4*>(hi + at) = *reinterpret_cast<const uint4*>(h);
       *reinterpret_cast<uint4*>(lo + at) = *reinterpret_cast<const uint4*>(l);
@@ -209,14 +222,14 @@ __global__ void __launch_bounds__(256) orth_load_kernel(const void* in, int alig
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (r0 + y < rows && c0 + x < cols) orth_in8<DT>(in, offset + static_cast<long long>(r0 + y) * cols + c0 + x, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s_tile[y][x + e] = v[e] * mul;
+        for (int e = 0; e < 8; ++e) s_tile[y][x + e] = v[e] * by.first * by.then;
       }
     } else {
       const int tx = tid & 63, ty = tid >> 6;
 #pragma unroll 8
       for (int y = ty; y < kOrthLoadTile; y += 4) {
         const int row = r0 + y, col = c0 + tx;
-        s_tile[y][tx] = row < rows && col < cols ? orth_in<DT>(in, offset + static_cast<long long>(row) * cols + col) * mul : 0.f;
+        s_tile[y][tx] = row < rows && col < cols ? orth_in<DT>(in, offset + static_cast<long long>(row) * cols + col) * by.first * by.then : 0.f;
       }
     }
     __syncthreads();
@@ -1026,7 +1039,7 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
   const uint32_t tmem = s_tmem;
   sum = s_last;
   for (int w = 0; w < 16; ++w) sum += s_sum[w];
-  const float mul = static_cast<float>(static_cast<double>(kOrthXScale) / (sqrt(sum) + eps));
+  const OrthFactor by(sum, eps);
   if (vec) {
 #pragma unroll
     for (int q = 0; q < kHeld; ++q) {
@@ -1036,7 +1049,8 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
       float2 v[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = make_float2(held[q][2 * e], held[q][2 * e + 1]);
-      orth_scale8(v, mul);
+      orth_scale8(v, by.first);
+      orth_scale8(v, by.then);
       uint4 h, l;
       orth_round8<true>(v, h, l);
       if (!m.transposed) {
@@ -1063,7 +1077,8 @@ __global__ void __launch_bounds__(kOrthSmallThreads, 1) orth_small_kernel(const 
         const uint32_t a = orth_word(u, q), b = SPLIT ? orth_word(d, q) : 0u;
         v[q] = make_float2(__uint_as_float(__byte_perm(b, a, 0x5410)), __uint_as_float(__byte_perm(b, a, 0x7632)));
       }
-      orth_scale8(v, mul);
+      orth_scale8(v, by.first);
+      orth_scale8(v, by.then);
       uint4 h, l;
       orth_round8<true>(v, h, l);
       *reinterpret_cast<uint4*>(at) = h;

@@ -197,3 +197,27 @@ def test_refuses_wrong_tensors():
         Orthogonalizer([(2, 2)], "bf16", offsets=[0, 4])
     with pytest.raises(ValueError):
         Orthogonalizer([(2, 2)], "bf16", steps=2, coeffs=[(1, 0, 0)])
+
+
+@pytest.mark.parametrize("shape", [(64, 80), (150, 300), (300, 150), (131, 257)])
+def test_norms_whose_inverse_leaves_fp32(shape):
+    """fp32 matrices down to the smallest numbers of the type and up to near its largest, in one block and in the general kernel; with eps
+    of no weight.  A matrix of such small numbers carries few bits itself: the formula is taken from what it holds."""
+    from paper_2411_03742_b200 import Orthogonalizer
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for dtype in ("f32", "bf16"):
+        for scale in (1e-44, 1e-40, 1e-37, 1e-35, 1e20, 3e37):
+            u = (torch.randn(shape[0] * shape[1], generator=g, device="cuda", dtype=torch.float64) * scale).clamp(-3.3e38, 3.3e38).to(TYPES[dtype])
+            if not u.any():                             # bf16 has nothing as small as 1e-44
+                assert dtype == "bf16" and scale == 1e-44
+                continue
+            out = torch.empty_like(u)
+            with Orthogonalizer([shape], dtype, eps=0.0) as plan:
+                plan.apply(u, out)
+            want = plain(u.view(shape), [COEFFS] * 5, 0.0)
+            assert float((out.view(shape).double() - want).norm() / want.norm()) <= tol(dtype, *shape), (dtype, scale)
+    u = torch.zeros(shape[0] * shape[1], device="cuda")
+    out = torch.full_like(u, 7.0)
+    with Orthogonalizer([shape], "f32", eps=1e-310) as plan:       # zeros give zeros for any eps > 0
+        plan.apply(u, out)
+    assert not out.any()
