@@ -31,8 +31,10 @@ extern "C" {
  *   rows, cols, offsets  host arrays; matrices must not overlap and must lie inside [0, d); sides up to 2^18.
  *            Elements outside the matrices (biases, gains) are neither read nor written.
  *   scaling  0: none; 1: each matrix's result times sqrt(max(1, rows / cols)).
- *   coeffs   host array of 3 * steps values a, b, c (one triple per step), 1 <= steps <= 64.  Iterates
- *            and a I + b S + c S S are held to |x| < 32; coefficients that let them grow beyond give Inf or NaN.
+ *   coeffs   host array of 3 * steps values a, b, c (one triple per step), 1 <= steps <= 64.  What the steps hold in 16-bit
+ *            parts must stay in their range: elements of X below 32, of S = X X^T below 8 (no row of X longer than
+ *            2.8, as no singular value beyond that), of a I + b S + c S S below 32.  Coefficients that let
+ *            them grow beyond give Inf or NaN; the usual ones stay below 1.3, 1.5 and 3.5.
  *   eps      >= 0.  A matrix of zeros gives zeros when eps > 0.  Inf or NaN in a matrix give NaN in
  *            that matrix only.
  * adacons_orth_create allocates about 8 bytes per element of the matrices and 4 (bf16) or 8 (fp32) per

@@ -221,3 +221,26 @@ def test_norms_whose_inverse_leaves_fp32(shape):
     with Orthogonalizer([shape], "f32", eps=1e-310) as plan:       # zeros give zeros for any eps > 0
         plan.apply(u, out)
     assert not out.any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(64, 80), (150, 300), (300, 150)])
+def test_coefficients_up_to_the_limit_of_the_products(dtype, shape):
+    """One row (or column) of the matrix is not zero, so the first step makes its length a, and S = a^2 in the second: right below
+    8, not finite from there on."""
+    from paper_2411_03742_b200 import Orthogonalizer
+    u = torch.zeros(shape, dtype=TYPES[dtype], device="cuda")
+    if shape[0] < shape[1]:
+        u[3] = torch.randn(shape[1], generator=torch.Generator().manual_seed(1)).cuda()
+    else:
+        u[:, 3] = torch.randn(shape[0], generator=torch.Generator().manual_seed(1)).cuda()
+    u = u.flatten()
+    for a, inside in ((2.82, True), (2.84, False)):
+        triples, out = [(a, 0.0, 0.0), (1.0, 0.0, 0.0)], torch.empty_like(u)
+        with Orthogonalizer([shape], dtype, steps=2, coeffs=triples) as plan:
+            plan.apply(u, out)
+        if inside:
+            want = plain(u.view(shape), triples, 1e-7)
+            assert float((out.view(shape).double() - want).norm() / want.norm()) <= tol(dtype, *shape)
+        else:
+            assert not out.isfinite().all()
