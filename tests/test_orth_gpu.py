@@ -244,3 +244,64 @@ def test_coefficients_up_to_the_limit_of_the_products(dtype, shape):
             assert float((out.view(shape).double() - want).norm() / want.norm()) <= tol(dtype, *shape)
         else:
             assert not out.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(150, 300), (300, 150), (40, 1000)])
+def test_magnitudes_and_degenerate_matrices_of_the_general_kernel(dtype, shape):
+    from paper_2411_03742_b200 import Orthogonalizer
+    n = shape[0] * shape[1]
+    g = torch.Generator(device="cuda").manual_seed(n)
+    for scale in (1e-30, 1e-6, 1e6, 1e30):
+        u = (torch.randn(n, generator=g, device="cuda") * scale).to(TYPES[dtype])
+        out = torch.empty_like(u)
+        with Orthogonalizer([shape], dtype, eps=0.0) as plan:
+            plan.apply(u, out)
+        want = plain(u.view(shape), [COEFFS] * 5, 0.0)
+        assert float((out.view(shape).double() - want).norm() / want.norm()) <= tol(dtype, *shape), scale
+    u = torch.randn(4 * n, generator=g, device="cuda").to(TYPES[dtype])
+    u[:n] = 0
+    u[n + 500] = math.inf
+    u[2 * n + 100] = math.nan
+    out = torch.full_like(u, 7.0)
+    with Orthogonalizer([shape] * 4, dtype) as plan:
+        plan.apply(u, out)
+        torch.cuda.synchronize()
+        assert plan.status() == 0
+    assert not out[:n].any()
+    assert out[n:3 * n].isnan().all()
+    want = plain(u[3 * n:].view(shape), [COEFFS] * 5, 1e-7)
+    assert float((out[3 * n:].view(shape).double() - want).norm() / want.norm()) <= tol(dtype, *shape)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_unaligned_buffers_and_far_offsets_in_the_general_kernel(dtype):
+    """The same bytes wherever buffers and matrices start, 2^31 elements in among them, in place and not."""
+    from paper_2411_03742_b200 import Orthogonalizer
+    shapes = [(160, 296), (296, 160), (150, 301)]
+    sizes = [m * n for m, n in shapes]
+    near = [0, sizes[0], sizes[0] + sizes[1]]
+    u = torch.randn(sum(sizes), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(TYPES[dtype])
+    want = torch.empty_like(u)
+    with Orthogonalizer(shapes, dtype) as plan:
+        plan.apply(u, want)
+        wide, far = (torch.full((plan.d + 9,), 7.0, dtype=TYPES[dtype], device="cuda") for _ in range(2))
+        for k in (1, 3, 8):
+            wide[k:k + plan.d] = u
+            plan.apply(wide[k:k + plan.d], far[k:k + plan.d])
+            assert torch.equal(far[k:k + plan.d], want), k
+            assert (far[k + plan.d:] == 7.0).all()
+            far.fill_(7.0)
+    at = [5, (1 << 31) + 12345, (1 << 31) + 12345 + sizes[1] + 1]
+    d = at[2] + sizes[2] + 3
+    big = torch.zeros(d, dtype=TYPES[dtype], device="cuda")
+    for o, p, s in zip(at, near, sizes):
+        big[o:o + s] = u[p:p + s]
+    with Orthogonalizer(shapes, dtype, offsets=at, d=d) as plan:
+        plan.apply(big, big)
+        torch.cuda.synchronize()
+        assert plan.status() == 0
+    for o, p, s in zip(at, near, sizes):
+        assert torch.equal(big[o:o + s], want[p:p + s])
+        big[o:o + s] = 0
+    assert not any(part.any() for part in big.split(1 << 28))
