@@ -19,10 +19,6 @@ using namespace adacons;
 
 namespace {
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 // TMA coordinates are 32-bit: longer vectors are walked in column chunks of this many elements,
 // each with its own tensor map and its own slice of the partial records.
 constexpr long long kChunkCols = 1ll << 30;
@@ -161,7 +157,7 @@ struct adacons_ctx {
   int* d_pass2_blk_seg = nullptr;       // [pass-2 blocks][2]: segment code, last segment
   size_t seg_bytes = 0;
 
-  EncodeTiledFn encode = nullptr;
+  TensorMapEncoder encode;
   int num_chunks = 1;                   // ceil(d / kChunkCols)
   std::vector<CUtensorMap> tmaps;       // one per column chunk; tmaps[0] covers everything when d <= 2^30
   const void* tmap_for = nullptr;
@@ -878,7 +874,7 @@ int adacons_create(adacons_ctx** out, int N, int64_t d, int dtype, const int64_t
   cudaDriverEntryPointQueryResult qres;
   if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) == cudaSuccess &&
       qres == cudaDriverEntryPointSuccess)
-    c->encode = reinterpret_cast<EncodeTiledFn>(fn);
+    c->encode.fn = reinterpret_cast<TensorMapEncodeFn>(fn);
   else
     cudaGetLastError();
 
@@ -1648,7 +1644,7 @@ constexpr size_t kNoAllocPartialBytes =
 struct NoAllocDevice {
   bool ready = false;
   unsigned char* scratch = nullptr;   // device address of g_noalloc_scratch on this device
-  EncodeTiledFn encode = nullptr;
+  TensorMapEncoder encode;
   int sms = 0;
   // launch plan of the most recent shape (a hook calls with the same shape every step)
   bool plan_valid = false;
@@ -1691,7 +1687,7 @@ int noalloc_setup(int dev, NoAllocDevice** out) {
       cudaDriverEntryPointQueryResult qres;
       if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) == cudaSuccess &&
           qres == cudaDriverEntryPointSuccess)
-        nd.encode = reinterpret_cast<EncodeTiledFn>(fn);
+        nd.encode.fn = reinterpret_cast<TensorMapEncodeFn>(fn);
       else
         cudaGetLastError();
       nd.ready = true;

@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <cstddef>
+
 namespace adacons {
 
 constexpr int kThreads = 256;          // threads per block in both streaming passes
@@ -20,6 +22,24 @@ constexpr uint32_t kFlagZeroRow = 1u, kFlagDegenerateZ = 2u, kFlagNonfinite = 4u
 template <int DT> struct Elem;                       // DT: 0 = fp32, 1 = bf16
 template <> struct Elem<0> { static constexpr int kVec = 4, kBytes = 4; };
 template <> struct Elem<1> { static constexpr int kVec = 8, kBytes = 2; };
+
+// Host: the driver's function that encodes a tensor map.  It needs a driver context, which a thread that has made no CUDA call
+// yet does not have (autograd's in a first backward pass): where it fails, the current device is made so and it is asked again.
+typedef CUresult (*TensorMapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                      const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+struct TensorMapEncoder {
+  TensorMapEncodeFn fn = nullptr;
+  bool operator==(std::nullptr_t) const { return fn == nullptr; }
+  bool operator!=(std::nullptr_t) const { return fn != nullptr; }
+  template <typename... Args>
+  CUresult operator()(Args... args) const {
+    const CUresult r = fn(args...);
+    int dev = 0;
+    if (r == CUDA_SUCCESS || cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return r;
+    return fn(args...);
+  }
+};
 
 // Host: make a context's device current for the duration of a call.
 struct DeviceGuard {

@@ -6,15 +6,12 @@
 #include <stdint.h>
 
 #include "adacons.h"
+#include "adacons_common.cuh"
 
 namespace adacons {
 
-typedef CUresult (*TensorMapEncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                      const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                      CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 // What the operators need to know of the current device; looked up once per device.
-struct DeviceInfo { int device = -1, sms = 0; TensorMapEncodeFn encode = nullptr; };
+struct DeviceInfo { int device = -1, sms = 0; TensorMapEncoder encode; };
 
 inline int query_device(DeviceInfo* info) {
   int dev = 0, major = 0, sms = 0;
@@ -33,7 +30,7 @@ inline int query_device(DeviceInfo* info) {
   }
   info->device = dev;
   info->sms = sms;
-  info->encode = reinterpret_cast<TensorMapEncodeFn>(fn);
+  info->encode.fn = reinterpret_cast<TensorMapEncodeFn>(fn);
   return ADACONS_OK;
 }
 

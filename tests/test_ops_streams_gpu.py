@@ -68,3 +68,42 @@ def test_results_freed_early_outlive_the_callers_reading():
             rope.apply(other, stream=side)
         torch.cuda.synchronize()
         assert torch.equal(copy, want)
+
+
+def test_calls_that_are_the_first_of_their_thread():
+    """A thread that has made no CUDA call yet, autograd's among them, has no context current until the call makes it so."""
+    import threading
+    from paper_2411_03742_b200 import AdaCons, Orthogonalizer, Rope, attention_backward, attention_forward
+    from paper_2411_03742_b200.attention import attention
+    q, dout = (torch.randn((1, 200, 2, 64), device="cuda").bfloat16() for _ in range(2))
+    u = torch.randn(300 * 200, device="cuda").bfloat16()
+    few, many = torch.randn((8, 4096), device="cuda"), torch.randn((8, 2_000_000), device="cuda")
+    out, lse = attention_forward(q, q, q)
+    want = attention_backward(dout, q, q, q, out, lse)
+    with Rope(64) as rope, Orthogonalizer([(300, 200)], "bf16") as plan, AdaCons(8, 4096) as small, AdaCons(8, 2_000_000) as large:
+        made = torch.empty_like(u)
+        spare = [torch.empty_like(t) for t in (out, lse, q, q, q, q)]
+        rope.apply(q, out=spare[5])
+        torch.cuda.synchronize()
+        errors = []
+
+        def run(call):
+            try:
+                call()
+            except Exception as e:
+                errors.append(repr(e))
+
+        # (a context of another thread must not be rebuilt in between: each call gets a thread of its own)
+        for call in (lambda: attention_forward(q, q, q, out=spare[0], lse=spare[1]),
+                     lambda: attention_backward(dout, q, q, q, out, lse, dq=spare[2], dk=spare[3], dv=spare[4]),
+                     lambda: rope.apply(q, out=spare[5]), lambda: plan.apply(u, made), lambda: small.aggregate(few, few.clone()[0]),
+                     lambda: large.aggregate(many, torch.empty_like(many[0]))):
+            t = threading.Thread(target=run, args=(call,))
+            t.start()
+            t.join()
+        torch.cuda.synchronize()
+        assert not errors, errors
+        assert torch.equal(spare[0], out) and torch.equal(spare[1], lse) and all(torch.equal(a, b) for a, b in zip(spare[2:5], want))
+        leaves = [q.clone().requires_grad_() for _ in range(3)]
+        attention(*leaves).backward(dout)               # the first thing that autograd's thread does on this device, where this test runs alone
+        assert all(torch.equal(t.grad, w) for t, w in zip(leaves, want))
