@@ -13,7 +13,7 @@ import threading
 
 import torch
 
-from .binding import BF16, _check, _raw_stream, _stream_handle, check_stream, load_library, on_stream
+from .binding import BF16, _check, _current_device, _raw_stream, _stream_handle, check_stream, load_library, on_stream
 
 F16 = 2
 SHORT_ROWS = 256        # query rows around a key head up to which the backward pass can do without a workspace
@@ -30,7 +30,8 @@ class _Shape(ctypes.Structure):
 
 class _Plans(threading.local):
     """Per thread: the argument blocks of layouts that have passed the checks.  Only the data pointers change between
-    calls, and nothing of a call is kept but its layout."""
+    calls, and nothing of a call is kept but its layout, the scale's value and the kind of mask (a tensor in the key would
+    go by its identity: a scale that a program changes in place would stay what it was at the first call)."""
 
     def __init__(self):
         self.known = {}
@@ -89,12 +90,6 @@ def _layout(t):
     return None if t is None else (t.dtype, t.shape, t.stride(), t.get_device())
 
 
-def _how(scale, causal):
-    """scale and causal as the plain values that they have now: a tensor in the key of a layout would go by its identity, and
-    a scale that a program changes in place would stay what it was at the first call."""
-    return None if scale is None else float(scale), bool(causal)
-
-
 def _shape(q, k, scale, causal, kv_lens):
     B, Sq, Hq, D = q.shape
     return _Shape(BF16 if q.dtype == torch.bfloat16 else F16, B, Hq, k.shape[2], Sq, k.shape[1], D, int(causal),
@@ -106,12 +101,12 @@ def attention_forward(q, k, v, *, scale=None, causal: bool = False, kv_lens=None
     q_heads, q_len) fp32.  scale defaults to head_dim^-1/2; kv_lens (int32) hides each batch's keys from there on.
     stream: where the kernels go (the current one by default); the caller orders it behind whatever makes the inputs, and its own
     use of the results behind it."""
-    scale, causal = _how(scale, causal)
+    scale, causal = None if scale is None else float(scale), bool(causal)        # as they are now: see _Plans
     sig = (_layout(q), _layout(k), _layout(v), _layout(kv_lens), scale, causal, _layout(out), _layout(lse))
     plan = _plans.known.get(sig)
     if plan is None:
         check_attention(q, k, v, kv_lens, like_q=[] if out is None else [("out", out)], rows=[] if lse is None else [("lse", lse)])
-    if sig[0][3] != torch.cuda.current_device():        # the kernels run on the current device
+    if sig[0][3] != _current_device():        # the kernels run on the current device
         with torch.cuda.device(sig[0][3]):
             return attention_forward(q, k, v, scale=scale, causal=causal, kv_lens=kv_lens, out=out, lse=lse, stream=stream)
     if stream is not None:
@@ -158,13 +153,13 @@ def attention_backward(dout, q, k, v, out, lse, *, scale=None, causal: bool = Fa
                        stream=None):
     """(dq, dk, dv) of attention_forward with the same scale, causal and kv_lens, from its out and lse and the
     gradient dout.  workspace: a uint8 tensor of workspace_bytes(q, k), made here if needed and not given."""
-    scale, causal = _how(scale, causal)
+    scale, causal = None if scale is None else float(scale), bool(causal)        # as they are now: see _Plans
     sig = (_layout(q), _layout(k), _layout(v), _layout(kv_lens), scale, causal, _layout(out), _layout(lse), _layout(dout), _layout(dq), _layout(dk), _layout(dv))
     plan = _plans.known.get(sig)
     if plan is None:
         check_attention(q, k, v, kv_lens, like_q=[(n, t) for n, t in (("dout", dout), ("out", out), ("dq", dq)) if t is not None],
                         like_k=[(n, t) for n, t in (("dk", dk), ("dv", dv)) if t is not None], rows=[("lse", lse)])
-    if sig[0][3] != torch.cuda.current_device():        # the kernels run on the current device
+    if sig[0][3] != _current_device():        # the kernels run on the current device
         with torch.cuda.device(sig[0][3]):
             return attention_backward(dout, q, k, v, out, lse, scale=scale, causal=causal, kv_lens=kv_lens, dq=dq, dk=dk, dv=dv, workspace=workspace, stream=stream)
     if stream is not None:
@@ -212,7 +207,7 @@ def attention(q, k, v, *, scale=None, causal: bool = False, kv_lens=None):
     belongs into q."""
     if getattr(scale, "requires_grad", False):
         raise ValueError("attention has no gradient for its scale: multiply q by a learned temperature instead")
-    return _Attention.apply(q, k, v, *_how(scale, causal), kv_lens)
+    return _Attention.apply(q, k, v, None if scale is None else float(scale), bool(causal), kv_lens)
 
 
 class _Attention(torch.autograd.Function):

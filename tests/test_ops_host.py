@@ -250,6 +250,7 @@ def fake(monkeypatch):
     for module in (attention, orth, rope):
         monkeypatch.setattr(module, "load_library", lambda: library)
         monkeypatch.setattr(module, "_raw_stream", lambda stream, device: 0 if stream is None else stream.cuda_stream)
+    monkeypatch.setattr(attention, "_current_device", lambda: now[0])
     monkeypatch.setattr(attention, "_plans", attention._Plans())
     return library
 
