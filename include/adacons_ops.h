@@ -155,6 +155,20 @@ int adacons_rope_apply(adacons_rope *ctx, const adacons_rope_shape *shape, const
 /* NULL is accepted. */
 int adacons_rope_destroy(adacons_rope *ctx);
 
+/* ------------------------------------------------------------------------------------------------
+ * Self-tests of the hang protection, as adacons_selftest_bounded_wait: the kernels of a call with one tile left
+ * out, so that the waits behind it run out after 2 s each, the blocks let go of what they hold and return, and the
+ * status word says ADACONS_FLAG_TIMEOUT.  The results are invalid, the next call's are not touched by it.
+ *   adacons_selftest_orth       adacons_orth_apply whose first tile nobody computes; EINVAL for a context all of whose
+ *                               matrices fit one block (128 x 256), whose kernel has no such wait
+ *   adacons_selftest_attention  the forward pass (dq NULL) or the gradient, with out in the place of dout; every block
+ *                               lacks its last tile.  ADACONS_BF16 and head_dim up to 64, otherwise EINVAL
+ */
+int adacons_selftest_orth(adacons_orth *ctx, const void *update, void *out, void *cuda_stream);
+int adacons_selftest_attention(const adacons_attn_shape *shape, const adacons_attn_tensor *q, const adacons_attn_tensor *k,
+                               const adacons_attn_tensor *v, const adacons_attn_tensor *out, float *lse, const adacons_attn_tensor *dq,
+                               const adacons_attn_tensor *dk, const adacons_attn_tensor *dv, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -202,6 +202,18 @@ def status(stream=None) -> int:
     return v.value
 
 
+def selftest_bounded_wait(q, k, v, out, lse, gradients=None) -> None:
+    """The forward pass, or with gradients = (dq, dk, dv) the backward pass, on the current device and stream, with tiles that never come:
+    the waits run out (2 s each) and status() says so.  What is written is invalid.  bf16, head sizes up to 64."""
+    check_attention(q, k, v, like_q=[("out", out)], rows=[("lse", lse)])
+    plan = _Plan(_shape(q, k, None, False, None), (q, k, v, out) + tuple(gradients or ()))
+    for block, t in zip(plan.blocks, (q, k, v, out) + tuple(gradients or ())):
+        block.data = t.data_ptr()
+    workspace = lse.new_empty(workspace_bytes(q, k) // 4)
+    _check(load_library().adacons_selftest_attention(plan.shape_ref, *plan.refs[:4], lse.data_ptr(), *(plan.refs[4:] or (None,) * 3), workspace.data_ptr(),
+                                                     workspace.numel() * 4, _raw_stream(None, q.get_device())), "adacons_selftest_attention")
+
+
 def attention(q, k, v, *, scale=None, causal: bool = False, kv_lens=None):
     """attention_forward's out as a function of q, k and v that can be differentiated once.  Not of the scale: a learned temperature
     belongs into q."""

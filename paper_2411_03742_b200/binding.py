@@ -88,6 +88,8 @@ def load_library() -> ctypes.CDLL:
         "adacons_rope_create": [P(vp), i32, P(dbl), dbl, i32],
         "adacons_rope_apply": [vp, vp, vp, P(i64), vp, P(i64), vp, i64, i32, vp],
         "adacons_rope_destroy": [vp],
+        "adacons_selftest_orth": [vp, vp, vp, vp],
+        "adacons_selftest_attention": [vp] * 10 + [i64, vp],
     }
     for name, args in protos.items():
         fn = getattr(lib, name)

@@ -28,10 +28,10 @@ bool raise(K kernel, uint32_t bytes) {
   cudaGetLastError();
   return false;
 }
-template <int D, bool BF16>
+template <int D, bool BF16, bool STARVE = false>
 bool raise_all() {
   static_assert(AttnFwdSmem<D>::kBytes <= 112 * 1024 && attn_backward_smem<D>() <= (AttnBwd<D>::kBlocks == 2 ? 112 : 227) * 1024, "shared memory of a block");
-  return raise(attn_forward_kernel<D, BF16>, AttnFwdSmem<D>::kBytes) && raise(attn_backward_kernel<D, BF16>, attn_backward_smem<D>());
+  return raise(attn_forward_kernel<D, BF16, STARVE>, AttnFwdSmem<D>::kBytes) && raise(attn_backward_kernel<D, BF16, STARVE>, attn_backward_smem<D>());
 }
 
 // The first call on a device sets the kernels' shared-memory limits; later ones only look the entry up.
@@ -145,17 +145,17 @@ void share_walks(AttnParams* p, int64_t key_blocks, int64_t queries, int64_t que
     }
 }
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool STARVE = false>
 bool run_forward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, AttnParams p, int sms, cudaStream_t st) {
   const int q_tiles = (p.Sq + kAttnTile - 1) / kAttnTile;
   p.split = key_shares(static_cast<int64_t>(q_tiles) * p.Hq * p.B, (p.Sk + kAttnTile - 1) / kAttnTile, 2 * sms);
-  return launch(&attn_forward_kernel<D, BF16>, dim3(q_tiles * p.split, p.Hq, p.B), dim3(kFwdThreads), AttnFwdSmem<D>::kBytes, st, kLaunchPlain, p.split,
+  return launch(&attn_forward_kernel<D, BF16, STARVE>, dim3(q_tiles * p.split, p.Hq, p.B), dim3(kFwdThreads), AttnFwdSmem<D>::kBytes, st, kLaunchPlain, p.split,
                 mq, mk, mv, p);
 }
 
 template <int D> int stat_blocks(int rows) { return static_cast<int>((static_cast<int64_t>(rows) + kAttnStatRows<D> - 1) / kAttnStatRows<D>); }
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool STARVE = false>
 bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo, AttnParams p, const adacons_attn_tensor* dout,
                   const adacons_attn_tensor* v, const adacons_attn_tensor* out, const float* lse, AttnOut dq, AttnOut dk, AttnOut dv, float* lse2, float* delta, float* peaks,
                   int sms, cudaStream_t st) {
@@ -180,7 +180,7 @@ bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMa
   key_blocks = (key_blocks * p.key_split + p.split - 1) / p.split * p.split;
   query_blocks = (query_blocks * p.query_split + p.split - 1) / p.split * p.split;
   return key_blocks + query_blocks <= 0x7fffffff &&
-         launch(&attn_backward_kernel<D, BF16>, dim3(static_cast<unsigned>(key_blocks + query_blocks)), dim3(AttnBwd<D>::kThreads), attn_backward_smem<D>(), st,
+         launch(&attn_backward_kernel<D, BF16, STARVE>, dim3(static_cast<unsigned>(key_blocks + query_blocks)), dim3(AttnBwd<D>::kThreads), attn_backward_smem<D>(), st,
                 separate ? kLaunchOverlap : kLaunchPlain, p.split, mq, mk, mv, mdo, p, static_cast<int>(key_blocks), static_cast<int>(q_tiles));
 }
 
@@ -197,10 +197,10 @@ int64_t workspace_bytes(const adacons_attn_shape* s) {
 
 }  // namespace
 
-extern "C" {
+namespace {
 
-int adacons_attn_forward(const adacons_attn_shape* s, const adacons_attn_tensor* q, const adacons_attn_tensor* k, const adacons_attn_tensor* v,
-                         const adacons_attn_tensor* out, float* lse, void* cuda_stream) {
+int forward(const adacons_attn_shape* s, const adacons_attn_tensor* q, const adacons_attn_tensor* k, const adacons_attn_tensor* v,
+            const adacons_attn_tensor* out, float* lse, void* cuda_stream, bool starve) {
   int rc = check_shape(s);
   if (rc != ADACONS_OK) return rc;
   if ((rc = check_tensor(q, s->batch, s->q_len, s->q_heads)) != ADACONS_OK || (rc = check_tensor(out, s->batch, s->q_len, s->q_heads)) != ADACONS_OK ||
@@ -219,21 +219,15 @@ int adacons_attn_forward(const adacons_attn_shape* s, const adacons_attn_tensor*
   p.lse = lse;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   bool ok;
-  if (s->head_dim <= 64) ok = s->dtype == ADACONS_BF16 ? run_forward<64, true>(mq, mk, mv, p, d->info.sms, st) : run_forward<64, false>(mq, mk, mv, p, d->info.sms, st);
+  if (starve) ok = run_forward<64, true, true>(mq, mk, mv, p, d->info.sms, st);
+  else if (s->head_dim <= 64) ok = s->dtype == ADACONS_BF16 ? run_forward<64, true>(mq, mk, mv, p, d->info.sms, st) : run_forward<64, false>(mq, mk, mv, p, d->info.sms, st);
   else ok = s->dtype == ADACONS_BF16 ? run_forward<128, true>(mq, mk, mv, p, d->info.sms, st) : run_forward<128, false>(mq, mk, mv, p, d->info.sms, st);
   return ok ? ADACONS_OK : ADACONS_ECUDA;
 }
 
-int adacons_attn_workspace_bytes(const adacons_attn_shape* s, int64_t* bytes) {
-  if (bytes == nullptr) return ADACONS_EINVAL;
-  const int rc = check_shape(s);
-  if (rc == ADACONS_OK) *bytes = workspace_bytes(s);
-  return rc;
-}
-
-int adacons_attn_backward(const adacons_attn_shape* s, const adacons_attn_tensor* dout, const adacons_attn_tensor* q, const adacons_attn_tensor* k,
-                          const adacons_attn_tensor* v, const adacons_attn_tensor* out, const float* lse, const adacons_attn_tensor* dq,
-                          const adacons_attn_tensor* dk, const adacons_attn_tensor* dv, void* workspace, int64_t bytes, void* cuda_stream) {
+int backward(const adacons_attn_shape* s, const adacons_attn_tensor* dout, const adacons_attn_tensor* q, const adacons_attn_tensor* k,
+             const adacons_attn_tensor* v, const adacons_attn_tensor* out, const float* lse, const adacons_attn_tensor* dq,
+             const adacons_attn_tensor* dk, const adacons_attn_tensor* dv, void* workspace, int64_t bytes, void* cuda_stream, bool starve) {
   int rc = check_shape(s);
   if (rc != ADACONS_OK) return rc;
   const adacons_attn_tensor* by_q[] = {dout, q, out, dq};
@@ -265,9 +259,44 @@ int adacons_attn_backward(const adacons_attn_shape* s, const adacons_attn_tensor
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   auto go = [&](auto run) { return run(mq, mk, mv, mdo, p, dout, v, out, lse, as_out(dq), as_out(dk), as_out(dv), lse2, delta, peaks, d->info.sms, st); };
   bool ok;
-  if (s->head_dim <= 64) ok = s->dtype == ADACONS_BF16 ? go(run_backward<64, true>) : go(run_backward<64, false>);
+  if (starve) ok = go(run_backward<64, true, true>);
+  else if (s->head_dim <= 64) ok = s->dtype == ADACONS_BF16 ? go(run_backward<64, true>) : go(run_backward<64, false>);
   else ok = s->dtype == ADACONS_BF16 ? go(run_backward<128, true>) : go(run_backward<128, false>);
   return ok ? ADACONS_OK : ADACONS_ECUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+int adacons_attn_forward(const adacons_attn_shape* s, const adacons_attn_tensor* q, const adacons_attn_tensor* k, const adacons_attn_tensor* v,
+                         const adacons_attn_tensor* out, float* lse, void* cuda_stream) {
+  return forward(s, q, k, v, out, lse, cuda_stream, false);
+}
+
+int adacons_attn_workspace_bytes(const adacons_attn_shape* s, int64_t* bytes) {
+  if (bytes == nullptr) return ADACONS_EINVAL;
+  const int rc = check_shape(s);
+  if (rc == ADACONS_OK) *bytes = workspace_bytes(s);
+  return rc;
+}
+
+int adacons_attn_backward(const adacons_attn_shape* s, const adacons_attn_tensor* dout, const adacons_attn_tensor* q, const adacons_attn_tensor* k,
+                          const adacons_attn_tensor* v, const adacons_attn_tensor* out, const float* lse, const adacons_attn_tensor* dq,
+                          const adacons_attn_tensor* dk, const adacons_attn_tensor* dv, void* workspace, int64_t bytes, void* cuda_stream) {
+  return backward(s, dout, q, k, v, out, lse, dq, dk, dv, workspace, bytes, cuda_stream, false);
+}
+
+int adacons_selftest_attention(const adacons_attn_shape* s, const adacons_attn_tensor* q, const adacons_attn_tensor* k, const adacons_attn_tensor* v,
+                               const adacons_attn_tensor* out, float* lse, const adacons_attn_tensor* dq, const adacons_attn_tensor* dk,
+                               const adacons_attn_tensor* dv, void* workspace, int64_t bytes, void* cuda_stream) {
+  if (s == nullptr || s->dtype != ADACONS_BF16 || s->head_dim > 64) return ADACONS_EINVAL;
+  AttnDevice* d = nullptr;
+  int rc = attn_device(&d);
+  if (rc != ADACONS_OK) return rc;
+  if (!raise_all<64, true, true>()) return ADACONS_ECUDA;
+  if (dq == nullptr) return forward(s, q, k, v, out, lse, cuda_stream, true);
+  return backward(s, out, q, k, v, out, lse, dq, dk, dv, workspace, bytes, cuda_stream, true);
 }
 
 int adacons_attn_get_status(uint32_t* flags, void* cuda_stream) {

@@ -259,7 +259,9 @@ template <int D> struct AttnFwdSmem {
   static constexpr uint32_t kKV = kT, kBars = kKV + kSlots * kT, kBytes = kBars + 256 + 1024;
 };
 
-template <int D, bool BF16>
+// STARVE, here and in the gradient: the self-test's form, whose copies leave the last tile out, so that every wait behind it
+// runs out.
+template <int D, bool BF16, bool STARVE = false>
 __global__ void __launch_bounds__(kFwdThreads, 2)
 attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv, const AttnParams p) {
   extern __shared__ unsigned char smem_dyn[];
@@ -315,6 +317,7 @@ attn_forward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constan
       int slot = 0, issued = 0;
       uint32_t parity = 1;
       for (int n = 0; n < 2 * tiles; ++n) {      // K_0 V_0 K_1 V_1 ..
+        if (STARVE && n == 2 * tiles - 1) break;
         if (s_abort || !mbar_wait_bounded(&kv_free[slot], parity)) { s_abort = 1; break; }
         mbar_expect_tx(&kv_full[slot], L::kT);
         attn_load_tile<D>(smem + L::kKV + slot * L::kT, n & 1 ? &mv : &mk, &kv_full[slot], (first + (n >> 1)) * kAttnTile, kv_head, batch);
@@ -698,7 +701,7 @@ template <int D> struct AttnDkvSmem {
   static constexpr uint32_t kBars = kTable + 2 * 4 * ADACONS_ATTN_SHORT_ROWS, kBytes = kBars + 256 + 1024;
 };
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool STARVE>
 __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo,
                                                const AttnParams& p, const int tile, const int kv_head, const int batch, const int rank) {
   using L = AttnDkvSmem<D>;
@@ -756,6 +759,7 @@ __device__ __forceinline__ void attn_dkv_block(unsigned char* smem, const CUtens
       int stage = 0, issued = 0;
       uint32_t parity = 1;
       for (int n = 0; n < items; ++n) {
+        if (STARVE && n == items - 1) break;
         const int head = kv_head * group + (skip + n) / per_head, q0 = (first + (skip + n) % per_head) * G::kTok;
         if (s_abort || !mbar_wait_bounded(&free_[stage], parity)) { s_abort = 1; break; }
         unsigned char* at = smem + L::kRing + stage * L::kStage;
@@ -988,7 +992,7 @@ template <int D> struct AttnDqSmem {
   static constexpr uint32_t kK = 2 * G::kRes, kV = kK + kKs * G::kStr, kTable = kV + kVs * G::kStr, kBars = kTable + 2 * 4 * kAttnTile, kBytes = kBars + 256 + 1024;
 };
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool STARVE>
 __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo,
                                               const AttnParams& p, const int tile, const int head, const int batch, const int rank) {
   using L = AttnDqSmem<D>;
@@ -1050,6 +1054,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
       const int kv_head = head / (p.Hq / p.Hkv);
       int issued = 0;
       for (int j = 0; j < tiles; ++j) {
+        if (STARVE && j == tiles - 1) break;
         const int ks = j % L::kKs, vs = j % L::kVs;
         if (s_abort || !mbar_wait_bounded(&k_free[ks], ((j / L::kKs) & 1) ^ 1)) { s_abort = 1; break; }
         mbar_expect_tx(&k_full[ks], G::kStr);
@@ -1239,7 +1244,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
 // most queries and the last queries the most keys: long blocks first in either part, all heads of one tile together.
 template <int D> constexpr uint32_t attn_backward_smem() { return AttnDkvSmem<D>::kBytes > AttnDqSmem<D>::kBytes ? AttnDkvSmem<D>::kBytes : AttnDqSmem<D>::kBytes; }
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool STARVE = false>
 __global__ void __launch_bounds__(AttnBwd<D>::kThreads, AttnBwd<D>::kBlocks)
 attn_backward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                      const __grid_constant__ CUtensorMap mdo, const AttnParams p, const int key_blocks, const int q_tiles) {
@@ -1250,13 +1255,13 @@ attn_backward_kernel(const __grid_constant__ CUtensorMap mq, const __grid_consta
     const int heads = p.Hkv * p.B, unit = n / p.key_split, tile = unit / heads, rank = n % p.key_split;
     if (tile * kAttnTile >= p.Sk) return;        // rounds the key blocks up to whole clusters
     n = unit - tile * heads;
-    attn_dkv_block<D, BF16>(smem, mq, mk, mv, mdo, p, tile, n % p.Hkv, n / p.Hkv, rank);
+    attn_dkv_block<D, BF16, STARVE>(smem, mq, mk, mv, mdo, p, tile, n % p.Hkv, n / p.Hkv, rank);
   } else {
     n -= key_blocks;
     const int heads = p.Hq * p.B, unit = n / p.query_split, tile = unit / heads, rank = n % p.query_split;
     if (tile >= q_tiles) return;
     n = unit - tile * heads;
-    attn_dq_block<D, BF16>(smem, mq, mk, mv, mdo, p, q_tiles - 1 - tile, n % p.Hq, n / p.Hq, rank);
+    attn_dq_block<D, BF16, STARVE>(smem, mq, mk, mv, mdo, p, q_tiles - 1 - tile, n % p.Hq, n / p.Hq, rank);
   }
 }
 

@@ -26,6 +26,7 @@ struct adacons_orth {
   const OrthChunk* chunks = nullptr;
   double* partial = nullptr;
   OrthParams params = {};             // all but the result's address
+  const int* starved = nullptr;       // the self-test's params.begin
   int cg = 1, tn = 128, blocks = 0;
   bool small = false;                 // all matrices fit the one-block kernel
   int num_load = 0, num_chunks = 0, num_mats = 0;
@@ -382,7 +383,7 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
 
   Arena a;
   const size_t at_mats = a.take(num * sizeof(OrthMat)), at_maps = a.take(static_cast<size_t>(num) * kMapCount * sizeof(CUtensorMap));
-  const size_t at_tiles = a.take(tiles.size() * sizeof(OrthTile)), at_begin = a.take(begin.size() * sizeof(int));
+  const size_t at_tiles = a.take(tiles.size() * sizeof(OrthTile)), at_begin = a.take(begin.size() * sizeof(int)), at_starved = a.take(begin.size() * sizeof(int));
   const size_t at_coeffs = a.take(step_coeffs.size() * sizeof(OrthStep)), at_done = a.take(num * sizeof(unsigned));
   const size_t at_load = a.take(load.size() * sizeof(OrthSpot)), at_chunks = a.take(chunks.size() * sizeof(OrthChunk));
   const size_t at_partial = a.take(chunks.size() * sizeof(double)), at_flags = a.take(sizeof(uint32_t));
@@ -421,6 +422,9 @@ int create(adacons_orth** out, int dtype, int64_t d, int num, const int64_t* row
   OrthParams& p = c->params;
   std::memcpy(host.data() + at_tiles, tiles.data(), tiles.size() * sizeof(OrthTile));
   std::memcpy(host.data() + at_begin, begin.data(), begin.size() * sizeof(int));
+  begin[0] = 1;                                              // the first worker's first tile is nobody's, which its matrix waits for
+  std::memcpy(host.data() + at_starved, begin.data(), begin.size() * sizeof(int));
+  c->starved = reinterpret_cast<const int*>(c->memory + at_starved);
   p.tiles = reinterpret_cast<const OrthTile*>(c->memory + at_tiles);
   p.begin = reinterpret_cast<const int*>(c->memory + at_begin);
   p.mirrored = plan.mirrored;
@@ -467,7 +471,11 @@ int adacons_orth_create(adacons_orth** out, int dtype, int64_t d, int num_matric
   }
 }
 
-int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cuda_stream) {
+}  // extern "C"
+
+namespace {
+
+int apply(adacons_orth* c, const void* update, void* out, void* cuda_stream, bool starve) {
   if (c == nullptr || update == nullptr || out == nullptr) return ADACONS_EINVAL;
   const size_t elem = c->dtype == ADACONS_F32 ? 4 : 2;
   if (reinterpret_cast<uintptr_t>(update) % elem != 0 || reinterpret_cast<uintptr_t>(out) % elem != 0) return ADACONS_EINVAL;
@@ -477,6 +485,7 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
   OrthParams p = c->params;
   p.out = out;
   p.out_aligned = reinterpret_cast<uintptr_t>(out) % 16 == 0;
+  if (starve) p.begin = c->starved;
   const double* partial = c->partial;
   const int aligned = reinterpret_cast<uintptr_t>(update) % 16 == 0;
   c->launches = c->small ? 1 : 3;
@@ -494,6 +503,17 @@ int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cud
          (c->cg == 2 ? launch_steps<false, 2, 256>(c, p, st) : c->tn == 128 ? launch_steps<false, 1, 128>(c, p, st) : launch_steps<false, 1, 64>(c, p, st));
   }
   return ok ? ADACONS_OK : ADACONS_ECUDA;
+}
+
+}  // namespace
+
+extern "C" {
+
+int adacons_orth_apply(adacons_orth* c, const void* update, void* out, void* cuda_stream) { return apply(c, update, out, cuda_stream, false); }
+
+int adacons_selftest_orth(adacons_orth* c, const void* update, void* out, void* cuda_stream) {
+  if (c == nullptr || c->small) return ADACONS_EINVAL;
+  return apply(c, update, out, cuda_stream, true);
 }
 
 int adacons_orth_get_status(adacons_orth* c, uint32_t* flags, void* cuda_stream) {

@@ -87,6 +87,11 @@ class Orthogonalizer:
             check_stream(stream, device)
         _check(self._lib.adacons_orth_apply(self._ctx, update.data_ptr(), out.data_ptr(), _raw_stream(stream, device)), "adacons_orth_apply")
 
+    def selftest_bounded_wait(self, update, out, stream=None) -> None:
+        """apply with a tile that nobody computes: its waits run out (2 s each) and status() says so.  `out` is invalid."""
+        check_vectors(self.d, self.dtype, update, out, device=self.device)
+        _check(self._lib.adacons_selftest_orth(self._ctx, update.data_ptr(), out.data_ptr(), _raw_stream(stream, self.device)), "adacons_selftest_orth")
+
     def status(self, stream=None) -> int:
         """The ADACONS_FLAG_TIMEOUT bit since the last call (0: all waits ended)."""
         v = ctypes.c_uint32()
