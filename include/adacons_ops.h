@@ -47,7 +47,7 @@ int adacons_orth_create(adacons_orth **out, int dtype, int64_t d, int num_matric
                         const int64_t *cols, const int64_t *offsets, int scaling, int steps,
                         const double *coeffs, double eps);
 
-/* One pass over the vector.  update and out may be the same buffer; any element alignment is served
+/* One pass over the vector.  update and out may be the same buffer, otherwise they must not overlap; any element alignment is served
  * (16-byte aligned buffers, offsets and rows that are multiples of 8 elements let the result be written in vectors).  A context holds the iterates:
  * calls on one context must be ordered (one stream, or events).  Errors: EINVAL, ECUDA. */
 int adacons_orth_apply(adacons_orth *ctx, const void *update, void *out, void *cuda_stream);
@@ -97,13 +97,13 @@ typedef struct adacons_attn_shape {
   const int32_t *kv_lens; /* device pointer, `batch` values (clamped to 0 .. kv_len), or NULL: all keys */
 } adacons_attn_shape;
 
-/* out: as q; lse: (batch, q_heads, q_len) fp32, contiguous.  out must not overlap the inputs.
+/* out: as q; lse: (batch, q_heads, q_len) fp32, contiguous.  out must not overlap the inputs (EINVAL where it starts with k or v).
  * Errors: EINVAL, EALIGN, ELIMIT (head_dim > 128, sizes beyond the above), ECUDA, EARCH. */
 int adacons_attn_forward(const adacons_attn_shape *shape, const adacons_attn_tensor *q, const adacons_attn_tensor *k,
                          const adacons_attn_tensor *v, const adacons_attn_tensor *out, float *lse, void *cuda_stream);
 
 /* dq, dk, dv from dout, with the probabilities recomputed from lse.  dq, dk and dv are written, not added to,
- * and must not overlap the inputs.  workspace: device memory of adacons_attn_workspace_bytes, 16-byte
+ * and must not overlap the inputs or one another (EINVAL where two start together).  workspace: device memory of adacons_attn_workspace_bytes, 16-byte
  * aligned, free for other use after the call's work.  It may be NULL where q_heads / kv_heads times q_len, rounded
  * up to a multiple of 128, is at most ADACONS_ATTN_SHORT_ROWS (fp16: and kv_len at most ADACONS_ATTN_SHORT_KEYS): one
  * launch instead of two, each block making for itself what the first would leave there; quicker for a few short heads.

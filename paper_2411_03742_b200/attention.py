@@ -99,6 +99,7 @@ def _shape(q, k, scale, causal, kv_lens):
 def attention_forward(q, k, v, *, scale=None, causal: bool = False, kv_lens=None, out=None, lse=None, stream=None):
     """(out, lse): out = softmax(scale q k^T + mask) v, shaped like q, and the rows' log-sum-exp, (batch,
     q_heads, q_len) fp32.  scale defaults to head_dim^-1/2; kv_lens (int32) hides each batch's keys from there on.
+    out and lse are made here unless given; a given out must not share memory with the inputs.
     stream: where the kernels go (the current one by default); the caller orders it behind whatever makes the inputs, and its own
     use of the results behind it."""
     scale, causal = None if scale is None else float(scale), bool(causal)        # as they are now: see _Plans
@@ -152,7 +153,8 @@ def _one_launch(q, k) -> bool:
 def attention_backward(dout, q, k, v, out, lse, *, scale=None, causal: bool = False, kv_lens=None, dq=None, dk=None, dv=None, workspace=None,
                        stream=None):
     """(dq, dk, dv) of attention_forward with the same scale, causal and kv_lens, from its out and lse and the
-    gradient dout.  workspace: a uint8 tensor of workspace_bytes(q, k), made here if needed and not given."""
+    gradient dout.  workspace: a uint8 tensor of workspace_bytes(q, k), made here if needed and not given.
+    dq, dk and dv, where given, must not share memory with the inputs or one another."""
     scale, causal = None if scale is None else float(scale), bool(causal)        # as they are now: see _Plans
     sig = (_layout(q), _layout(k), _layout(v), _layout(kv_lens), scale, causal, _layout(out), _layout(lse), _layout(dout), _layout(dq), _layout(dk), _layout(dv))
     plan = _plans.known.get(sig)

@@ -85,6 +85,9 @@ int check_tensor(const adacons_attn_tensor* t, int batch, int len, int heads) {
   return ADACONS_OK;
 }
 
+// Whether two tensors with elements start at the same place: a result there would be written while other blocks still read.
+bool same_place(const adacons_attn_tensor* a, int a_len, const adacons_attn_tensor* b, int b_len) { return a_len > 0 && b_len > 0 && a->data == b->data; }
+
 bool make_map(const AttnDevice& d, CUtensorMap* map, const adacons_attn_shape* s, const adacons_attn_tensor* t, int len, int heads, const void* spare, int rows) {
   // a tensor without tokens is never read, but its map has to exist
   const void* base = len > 0 ? t->data : spare;
@@ -207,6 +210,7 @@ int forward(const adacons_attn_shape* s, const adacons_attn_tensor* q, const ada
       (rc = check_tensor(k, s->batch, s->kv_len, s->kv_heads)) != ADACONS_OK || (rc = check_tensor(v, s->batch, s->kv_len, s->kv_heads)) != ADACONS_OK)
     return rc;
   if (s->batch == 0 || s->q_len == 0) return ADACONS_OK;
+  if (same_place(out, s->q_len, k, s->kv_len) || same_place(out, s->q_len, v, s->kv_len)) return ADACONS_EINVAL;
   if (lse == nullptr || reinterpret_cast<uintptr_t>(lse) % 4 != 0) return ADACONS_EINVAL;
   AttnDevice* d = nullptr;
   if ((rc = attn_device(&d)) != ADACONS_OK) return rc;
@@ -237,6 +241,11 @@ int backward(const adacons_attn_shape* s, const adacons_attn_tensor* dout, const
   for (const adacons_attn_tensor* t : by_k)
     if ((rc = check_tensor(t, s->batch, s->kv_len, s->kv_heads)) != ADACONS_OK) return rc;
   if (s->batch == 0 || (s->q_len == 0 && s->kv_len == 0)) return ADACONS_OK;
+  const adacons_attn_tensor* all[] = {dout, q, out, k, v, dq, dk, dv};
+  auto len_of = [&](int t) { return t < 3 || t == 5 ? s->q_len : s->kv_len; };
+  for (int r = 5; r < 8; ++r)
+    for (int t = 0; t < r; ++t)
+      if (same_place(all[r], len_of(r), all[t], len_of(t))) return ADACONS_EINVAL;
   if (s->q_len > 0) {
     const int64_t pad = (static_cast<int64_t>(s->q_len) + kAttnTile - 1) / kAttnTile * kAttnTile;
     if (lse == nullptr || reinterpret_cast<uintptr_t>(lse) % 4 != 0) return ADACONS_EINVAL;

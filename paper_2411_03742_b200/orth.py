@@ -77,7 +77,7 @@ class Orthogonalizer:
 
     def apply(self, update, out, stream=None) -> None:
         """out[matrix] = orthogonalised update[matrix] for every matrix; the rest of `out` stays as it is.
-        Flat CUDA tensors of d elements; `out` may be `update`."""
+        Flat CUDA tensors of d elements; `out` may be `update`, otherwise they must not share memory."""
         device = update.get_device()
         sig = (update.dtype, update.shape, update.stride(), device, out.dtype, out.shape, out.stride(), out.get_device())
         if sig != self._checked:

@@ -91,7 +91,7 @@ class Rope:
     def apply(self, x, positions=None, out=None, inverse: bool = False, first: int = 0, stream=None):
         """x turned, (batch, token, head, element) in float32 or bfloat16 with unit stride along the elements;
         positions: int32 (batch, token), or None: token s is at position first + s.  out: a new tensor
-        unless given; x itself is allowed.  inverse: the gradient's turn, by the negative angles."""
+        unless given; x itself is allowed, no other overlap.  inverse: the gradient's turn, by the negative angles."""
         device = x.get_device()
         if stream is not None and x.is_cuda:
             check_stream(stream, device)

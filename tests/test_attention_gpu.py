@@ -476,3 +476,23 @@ def test_many_keys_need_a_workspace_in_half_precision():
     s, x = _Shape(2, 1, 1, 1, 8, 4097, 64, 0, 0.125, None), _Tensor(t.data_ptr(), *t.stride()[:3])
     r = ctypes.byref
     assert load_library().adacons_attn_backward(r(s), r(x), r(x), r(x), r(x), r(x), rows.data_ptr(), r(x), r(x), r(x), None, 0, None) == EINVAL
+
+
+def test_given_results_that_share_an_input_are_refused():
+    from paper_2411_03742_b200 import AdaConsError, attention_backward, attention_forward
+    q, k, v, dout = (torch.randn((1, 64, 2, 64), device="cuda").bfloat16() for _ in range(4))
+    out, lse = attention_forward(q, k, v)
+    for t in (k, v):
+        with pytest.raises(AdaConsError):
+            attention_forward(q, k, v, out=t)
+    for t in (dout, q, k, v, out):
+        for name in ("dq", "dk", "dv"):
+            with pytest.raises(AdaConsError):
+                attention_backward(dout, q, k, v, out, lse, **{name: t})
+    one = torch.empty_like(k)
+    with pytest.raises(AdaConsError):
+        attention_backward(dout, q, k, v, out, lse, dk=one, dv=one)
+    want = attention_backward(dout, q, k, v, out, lse)
+    packed = torch.empty((1, 64, 6, 64), dtype=torch.bfloat16, device="cuda")      # slices of one buffer are not the same memory
+    got = attention_backward(dout, q, k, v, out, lse, dq=packed[:, :, :2], dk=packed[:, :, 2:4], dv=packed[:, :, 4:])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))

@@ -434,3 +434,18 @@ def test_what_the_readme_imports_can_be_called():
     assert {"AdaCons", "Orthogonalizer", "Rope", "attention", "attention_forward", "attention_backward"} <= {n for _, n in names}
     for module, name in names:
         assert callable(getattr(importlib.import_module(module), name)), (module, name)
+
+
+def test_results_in_the_place_of_what_is_read_are_refused(lib):
+    """Written where other blocks still read, they would be right or wrong by chance.  Checked before any device is touched."""
+    from paper_2411_03742_b200.attention import _Shape, _Tensor
+    s = _Shape(1, 2, 4, 2, 3, 5, 64, 0, 0.125, None)
+    at = lambda n: _Tensor((1 << 20) + (n << 16), 1024, 256, 64)  # noqa: E731
+    r, rows = ctypes.byref, 1 << 30
+    q, k, v, out, dout, dq, dk, dv = (at(n) for n in range(8))
+    assert lib.adacons_attn_forward(r(s), r(q), r(k), r(v), r(k), rows, None) == EINVAL
+    assert lib.adacons_attn_forward(r(s), r(q), r(k), r(v), r(v), rows, None) == EINVAL
+    back = lambda *g: lib.adacons_attn_backward(r(s), r(dout), r(q), r(k), r(v), r(out), rows, *(r(t) for t in g), 1 << 29, 1 << 20, None)  # noqa: E731
+    for t in (dout, q, k, v, out):
+        assert back(t, dk, dv) == back(dq, t, dv) == back(dq, dk, t) == EINVAL
+    assert back(dq, dk, dk) == back(dq, dq, dv) == EINVAL
