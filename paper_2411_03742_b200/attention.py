@@ -137,10 +137,10 @@ def workspace_bytes(q, k) -> int:
 
 def _one_launch(q, k) -> bool:
     """Whether the backward pass goes without a workspace: where its blocks all run at once (two an SM up to head size 64)
-    the call is bound by the host, and one launch without an allocation is 3.7 us less (15.5 against 19.2 for 3 x 77
-    tokens of 4 heads); where they do not, the repeated statistics show (8 x 256 tokens of 16 heads: 24.0 against 22.1 us).
-    In fp16 every block looks through all values of its head as well: 18.3 against 20.2 us at 1024 keys of 64 elements,
-    18.7 and 20.3 at 512 of 128, but 23.5 and 20.2 at 1024 of 128."""
+    the call is bound by the host, and one launch without an allocation is 4 us less (16.0 against 20.2 for 3 x 77
+    tokens of 4 heads); where they do not, the repeated statistics show (8 x 256 tokens of 16 heads: 26.0 against 24.7 us).
+    In fp16 every block looks through all values of its head as well: 17.8 against 20.3 us at 1024 keys of 64 elements,
+    18.9 and 20.5 at 512 of 128, but 23.7 and 20.5 at 1024 of 128."""
     q_tiles, k_tiles = -(-q.shape[1] // 128), -(-k.shape[1] // 128)
     if q.shape[2] // k.shape[2] * q_tiles * 128 > SHORT_ROWS:
         return False

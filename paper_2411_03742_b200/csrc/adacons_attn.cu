@@ -85,6 +85,8 @@ int check_tensor(const adacons_attn_tensor* t, int batch, int len, int heads) {
   return ADACONS_OK;
 }
 
+int64_t peak_blocks(int kv_len) { return (static_cast<int64_t>(kv_len) + kAttnPeakRows - 1) / kAttnPeakRows; }
+
 // Whether two tensors with elements start at the same place: a result there would be written while other blocks still read.
 bool same_place(const adacons_attn_tensor* a, int a_len, const adacons_attn_tensor* b, int b_len) { return a_len > 0 && b_len > 0 && a->data == b->data; }
 
@@ -156,8 +158,6 @@ bool run_forward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap
                 mq, mk, mv, p);
 }
 
-template <int D> int stat_blocks(int rows) { return static_cast<int>((static_cast<int64_t>(rows) + kAttnStatRows<D> - 1) / kAttnStatRows<D>); }
-
 template <int D, bool BF16, bool STARVE = false>
 bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mdo, AttnParams p, const adacons_attn_tensor* dout,
                   const adacons_attn_tensor* v, const adacons_attn_tensor* out, const float* lse, AttnOut dq, AttnOut dk, AttnOut dv, float* lse2, float* delta, float* peaks,
@@ -170,7 +170,7 @@ bool run_backward(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMa
   p.delta = delta;
   const bool separate = delta != nullptr && p.sq_pad > 0;
   if (separate) {
-    const int q_blocks = p.sq_pad / kAttnStatRows<D>, k_blocks = BF16 ? 0 : stat_blocks<D>(p.Sk);
+    const int q_blocks = p.sq_pad / kAttnStatRows<D>, k_blocks = BF16 ? 0 : static_cast<int>((peak_blocks(p.Sk) * p.Hkv + p.Hq - 1) / p.Hq);
     if (!launch(&attn_delta_kernel<D, BF16>, dim3(q_blocks + k_blocks, p.Hq, p.B), dim3(256), 0, st, kLaunchPlain, 1, p, lse2, delta, peaks)) return false;
     if (!BF16) p.peaks = peaks;
   }
@@ -193,7 +193,7 @@ int64_t workspace_bytes(const adacons_attn_shape* s) {
   int64_t words = 2 * pad * s->q_heads;
   if (s->dtype == ADACONS_F16) {
     const int64_t rows = s->head_dim <= 64 ? kAttnStatRows<64> : kAttnStatRows<128>;
-    words += pad / rows * s->q_heads + (s->kv_len + rows - 1) / rows * s->kv_heads;
+    words += pad / rows * s->q_heads + peak_blocks(s->kv_len) * s->kv_heads;
   }
   return static_cast<int64_t>(sizeof(float)) * words * s->batch;
 }

@@ -30,8 +30,8 @@ namespace adacons {
 // 2^-16 on 65,536 keys, whose dV was off by 7e-4 instead of 3e-4, and dQ by 8e-3 under dO of 0.01).  There they are rounded
 // as 2^12 P and 2^k dS, with 2^k from the bound |dS| <= 2 max |dO_i| max |V_j| over the queries and keys of a key head, so that
 // nothing overflows either, and the results are multiplied by 2^-12 and 2^-k.  The norms' maxima come with Delta, one for each block
-// of that kernel, and every block of the gradient looks through its head's: 3.54 ms against bf16's 3.39 (8192 x 8192, 32 / 8 heads of
-// 128), 28.9 against 24.8 us (8 x 256 tokens, 16 heads of 64).
+// of that kernel, and every block of the gradient looks through its head's: 3.61 ms against bf16's 3.43 (8192 x 8192, 32 / 8 heads of
+// 128), 28.9 against 24.7 us (8 x 256 tokens, 16 heads of 64).
 // ----------------------------------------------------------------------------------------------
 constexpr int kAttnTile = 128;
 constexpr int kFwdThreads = 320;                 // warps 0-7 softmax, 8 copies, 9 products
@@ -62,6 +62,7 @@ struct AttnParams {
 template <bool BF16> constexpr float kAttnShift = BF16 ? 0.f : 12.f;
 template <bool BF16> constexpr float kAttnUnshift = BF16 ? 1.f : 1.f / 4096.f;
 template <int D> constexpr int kAttnStatRows = 256 / (D / 8);     // rows of a block of the statistics kernel
+constexpr int kAttnPeakRows = 128;                                // of v, of a block that looks for its largest (fp16)
 
 template <int D> struct AttnTile {
   static constexpr uint32_t kBlock = kAttnTile * 128;         // 128 rows x 64 elements
@@ -604,7 +605,7 @@ __device__ __forceinline__ float attn_ds_scale(const AttnParams& p, int batch, i
   const int group = p.Hq / p.Hkv;
   float peak[2] = {0.f, 0.f};                      // |dO|^2, |V|^2
   if (p.peaks != nullptr) {
-    const long long qb = p.sq_pad / kAttnStatRows<D>, kb = (p.Sk + kAttnStatRows<D> - 1ll) / kAttnStatRows<D>;
+    const long long qb = p.sq_pad / kAttnStatRows<D>, kb = (p.Sk + kAttnPeakRows - 1ll) / kAttnPeakRows;
     const float* at[2] = {p.peaks + (static_cast<long long>(batch) * p.Hq + kv_head * group) * qb,
                           p.peaks + static_cast<long long>(p.B) * p.Hq * qb + (static_cast<long long>(batch) * p.Hkv + kv_head) * kb};
     const long long count[2] = {group * qb, kb};
@@ -641,13 +642,16 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnParams p, flo
   if constexpr (!BF16) {
     __shared__ float s_peak[8];
     constexpr int kRows = kAttnStatRows<D>;
-    const int qb = p.sq_pad / kRows, x = static_cast<int>(blockIdx.x);
+    const int qb = p.sq_pad / kRows, x = static_cast<int>(blockIdx.x), batch = blockIdx.z;
     const bool keys = x >= qb;
-    const int head = blockIdx.y, batch = blockIdx.z;
-    if (keys && head >= p.Hkv) return;
-    const int64_t first = static_cast<int64_t>(keys ? x - qb : x) * kRows;
+    const long long kb = (p.Sk + kAttnPeakRows - 1ll) / kAttnPeakRows;
+    // the blocks beyond q's share all key heads' rows of v
+    const long long unit = static_cast<long long>(x - qb) * p.Hq + blockIdx.y;
+    if (keys && unit >= kb * p.Hkv) return;
+    const int head = keys ? static_cast<int>(unit / kb) : static_cast<int>(blockIdx.y);
+    const long long block = keys ? unit % kb : x, first = block * (keys ? kAttnPeakRows : kRows);
     const int kv_len = attn_kv_len(p, batch);
-    float peak = attn_peak<D, kRows>(p, kRows, [&](int64_t n) -> const unsigned short* {
+    float peak = attn_peak<D, kRows>(p, keys ? kAttnPeakRows : kRows, [&](int64_t n) -> const unsigned short* {
       if (keys) return first + n < kv_len ? attn_row(p.v, batch, first + n, head) : nullptr;
       return first + n < p.Sq && attn_has_key(p, batch, head, first + n) ? attn_row(p.dout, batch, first + n, head) : nullptr;
     });
@@ -657,8 +661,7 @@ __global__ void __launch_bounds__(256) attn_delta_kernel(const AttnParams p, flo
     __syncthreads();
     if (threadIdx.x == 0) {
       for (int w = 1; w < 8; ++w) peak = fmaxf(peak, s_peak[w]);
-      const long long kb = static_cast<int>(gridDim.x) - qb;
-      peaks[keys ? static_cast<long long>(p.B) * p.Hq * qb + (static_cast<long long>(batch) * p.Hkv + head) * kb + (x - qb) : (static_cast<long long>(batch) * p.Hq + head) * qb + x] = peak;
+      peaks[keys ? static_cast<long long>(p.B) * p.Hq * qb + (static_cast<long long>(batch) * p.Hkv + head) * kb + block : (static_cast<long long>(batch) * p.Hq + head) * qb + block] = peak;
     }
     if (keys) return;
   }
@@ -1159,7 +1162,7 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
         if (threadIdx.x == 0) s_by_dq = by_dq;
       }
     }
-    const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), lse22 = make_float2(-lse2, -lse2), delta2 = make_float2(-delta, -delta);
+    const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), lse22 = make_float2(-lse2, -lse2), delta2 = make_float2(-delta * by_ds, -delta * by_ds);
     const int limit = p.causal ? min(kv_len, row + off + 1) : kv_len;
     const int warp_limit = p.causal ? min(kv_len, row - lane + off + 1) : kv_len;
     bool ok = true;
@@ -1201,9 +1204,8 @@ __device__ __forceinline__ void attn_dq_block(unsigned char* smem, const CUtenso
         __syncwarp();
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          float2 a = add2(make_float2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1])), delta2);
-          if constexpr (!BF16) a = mul2(a, make_float2(by_ds, by_ds));
-          a = mul2(a, make_float2(pr[2 * e], pr[2 * e + 1]));
+          const float2 dp = make_float2(__uint_as_float(d[2 * e]), __uint_as_float(d[2 * e + 1]));
+          const float2 a = mul2(BF16 ? add2(dp, delta2) : fma2(dp, make_float2(by_ds, by_ds), delta2), make_float2(pr[2 * e], pr[2 * e + 1]));
           w[e] = pack16<BF16>(a.x, a.y);
         }
       }
