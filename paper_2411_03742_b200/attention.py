@@ -13,9 +13,11 @@ import threading
 
 import torch
 
-from .binding import BF16, _check, _current_device, _raw_stream, _stream_handle, check_stream, load_library, on_stream
+from .binding import BF16, _check, _raw_stream, _stream_handle, check_stream, load_library, on_stream
 
 F16 = 2
+# torch.cuda.current_device() without its look whether the runtime is up: whoever asks here holds a CUDA tensor
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 SHORT_ROWS = 256        # query rows around a key head up to which the backward pass can do without a workspace
 
 

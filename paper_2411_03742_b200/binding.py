@@ -128,15 +128,6 @@ def _raw_stream(stream, device_index: int) -> int:
         return int(torch.cuda.current_stream(device_index).cuda_stream)
 
 
-def _current_device() -> int:
-    """torch.cuda.current_device() for callers that hold a CUDA tensor: the runtime is up."""
-    import torch
-    try:
-        return torch._C._cuda_getDevice()
-    except AttributeError:
-        return torch.cuda.current_device()
-
-
 def check_stream(stream, device_index: int) -> None:
     """Raise ValueError if `stream` is known to belong to another device than the tensors."""
     index = getattr(getattr(stream, "device", None), "index", None)

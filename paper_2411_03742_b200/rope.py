@@ -158,4 +158,8 @@ class _Turn(torch.autograd.Function):
     def backward(ctx, dy):
         pos = ctx.saved_tensors[0] if ctx.saved_tensors else None
         dy = dy if dy.stride(3) == 1 else dy.clone(memory_format=torch.contiguous_format)
-        return _Turn.apply(dy, ctx.rope, pos, ctx.first, not ctx.inverse), None, None, None, None
+        if torch.is_grad_enabled():         # a graph of the gradient is recorded
+            dx = _Turn.apply(dy, ctx.rope, pos, ctx.first, not ctx.inverse)
+        else:
+            dx = ctx.rope.apply(dy, pos, inverse=not ctx.inverse, first=ctx.first)
+        return dx, None, None, None, None
