@@ -2,11 +2,11 @@
  * adacons_ops.h -- C ABI of the training operators beside the aggregation (NVIDIA B200, sm_100a).
  *
  * The conventions are those of adacons.h: every function returns an adacons_error code, none throws
- * or aborts; pointers are device pointers unless said otherwise, of the device that was current when the context
- * was created, whichever is current at the call (attention has no context: of the device that is current);
- * `cuda_stream` is a cudaStream_t of that device passed as void*; calls are asynchronous on that stream, allocate nothing (create calls do) and
- * perform no host synchronisation; results are deterministic (no floating-point atomics, fixed
- * reduction order); no wait inside a kernel lasts longer than 2 s.
+ * or aborts; pointers are device pointers unless said otherwise, of the device that was current when the
+ * context was created, whichever is current at the call (attention has no context: of the device that is
+ * current); `cuda_stream` is a cudaStream_t of that device passed as void*; calls are asynchronous on that
+ * stream, allocate nothing (create calls do) and perform no host synchronisation; results are deterministic
+ * (no floating-point atomics, fixed reduction order); no wait inside a kernel lasts longer than 2 s.
  */
 #ifndef ADACONS_OPS_H_
 #define ADACONS_OPS_H_
@@ -26,8 +26,9 @@ extern "C" {
  * taken on its short side.  With the usual coefficients (3.4445, -4.7750, 2.0315) five steps bring
  * all singular values that are not tiny near one.
  *   dtype    ADACONS_F32 or ADACONS_BF16: storage of the update and of the result.  bf16: products of
- *            fp16 operands with the iterate held in 22 bits; the result is within about one bf16
- *            rounding.  fp32: operands as pairs of fp16 values, about 1e-6 of the result's norm.
+ *            fp16 operands with the iterate held in 22 bits; the result is within 2.4e-3 of its norm (one bf16
+ *            rounding is 1.7e-3), 4e-3 where all singular values are alike, 1.6e-2 on sides below 16.
+ *            fp32: operands as pairs of fp16 values, about 1e-6 of the result's norm.
  *   rows, cols, offsets  host arrays; matrices must not overlap and must lie inside [0, d); sides up to 2^18.
  *            Elements outside the matrices (biases, gains) are neither read nor written.
  *   scaling  0: none; 1: each matrix's result times sqrt(max(1, rows / cols)).
