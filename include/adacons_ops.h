@@ -157,6 +157,93 @@ int adacons_rope_apply(adacons_rope *ctx, const adacons_rope_shape *shape, const
 int adacons_rope_destroy(adacons_rope *ctx);
 
 /* ------------------------------------------------------------------------------------------------
+ * Norms before and after a block, with the block's gate and the residual addition.
+ *
+ * For every token's row of `dim` elements, with c = scale act(gate), one where there is no gate:
+ *     n = f r_f,  r_f = (mean f^2 + eps)^-1/2       (post NULL: n = f)
+ *     out = x + c n post                            (f NULL: out is x, and is not written)
+ *     normed = out r_x pre,  r_x = (mean out^2 + eps)^-1/2        (pre NULL: not made)
+ * r_x is that of the sum before it is rounded to the stream's type.  Sums, means and factors are fp32: rows whose squares
+ * leave its range (elements beyond 1e19) give what fp32 gives.
+ */
+enum { ADACONS_NORM_GATE_NONE = 0, ADACONS_NORM_GATE_CHANNEL = 1, ADACONS_NORM_GATE_SEQUENCE = 2, ADACONS_NORM_GATE_TOKEN = 3 };
+enum { ADACONS_NORM_BY_ITSELF = 0, ADACONS_NORM_BY_SIGMOID = 1, ADACONS_NORM_BY_TANH = 2 };
+
+/* Rows (batch, token): strides in elements, any values; those of dimensions of size 1 are not looked at.  Rows of 16-byte
+ * aligned data whose strides and `dim` are multiples of 16 bytes (dim of 8 elements) are moved in vectors, anything else element by element. */
+typedef struct adacons_norm_rows {
+  void *data;
+  int64_t batch_stride, row_stride;
+} adacons_norm_rows;
+
+typedef struct adacons_norm_shape {
+  int stream_dtype;       /* of x, out and their gradients: `dtype` or ADACONS_F32 */
+  int dtype;              /* of f, normed and their gradients: ADACONS_F32, ADACONS_BF16 or ADACONS_F16 */
+  int batch, len;         /* batch * len up to 2^31 - 1 */
+  int dim;                /* 1 .. 16384 */
+  int gate;               /* ADACONS_NORM_GATE_: its rows are one for all (strides not looked at), one for each sequence
+                             (batch_stride), or one for each token */
+  int gate_by;            /* ADACONS_NORM_BY_: act */
+  int gate_dtype, post_dtype, pre_dtype;  /* each `dtype` or ADACONS_F32; a gradient has its tensor's type */
+  float scale;            /* finite */
+  float eps;              /* > 0 */
+} adacons_norm_shape;
+
+/* rows: 2 * batch * len fp32 values, r_f of every token and then r_x (0 where there is no such norm), for the gradient.  post, pre: `dim` values.
+ * out may be x itself; no other result may share memory with what is read or with another (EINVAL where two start together).
+ * Errors: EINVAL, EALIGN, ELIMIT, ECUDA, EARCH. */
+int adacons_norm_forward(const adacons_norm_shape *shape, const adacons_norm_rows *x, const adacons_norm_rows *f, const adacons_norm_rows *gate,
+                         const void *post, const void *pre, const adacons_norm_rows *out, const adacons_norm_rows *normed, float *rows, void *cuda_stream);
+
+/* The gradients from those of out (dout; NULL data: zeros) and normed (dnormed; NULL: zeros).  out, rows: the forward pass's.  Everything that has a
+ * gradient gets one, written and not added to: x, f, the gate (in its own rows), post, pre.  dx may be dout itself.  The sums over tokens are
+ * added in a fixed order, from records in the workspace (adacons_norm_workspace_bytes for this shape on the current device, 16-byte
+ * aligned, free for other use after the call's work; not needed without post, pre and a gate that tokens share).  Errors: as the forward pass. */
+int adacons_norm_workspace_bytes(const adacons_norm_shape *shape, int64_t *bytes);
+int adacons_norm_backward(const adacons_norm_shape *shape, const adacons_norm_rows *dout, const adacons_norm_rows *dnormed, const adacons_norm_rows *out,
+                          const adacons_norm_rows *f, const adacons_norm_rows *gate, const void *post, const void *pre, const float *rows,
+                          const adacons_norm_rows *dx, const adacons_norm_rows *df, const adacons_norm_rows *dgate, void *dpost, void *dpre, void *workspace,
+                          int64_t workspace_bytes, void *cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Distillation from a teacher's top logits.
+ *
+ * For every token, with the student's logits z, the teacher's logits t_j of `top` entries with indices i_j, and a label y:
+ *     p = softmax(t / tau) over the entries that are there,   L = ln sum exp(z / tau),   L1 = ln sum exp(z)
+ *     loss = mix tau^2 sum_j p_j (ln p_j - z_{i_j} / tau + L) + (1 - mix) (L1 - z_y)
+ * An entry is there when its index lies in 0 .. vocab-1 (any other says that it is not) and its logit is not -inf.  A token without
+ * entries has no first term, one without a label in 0 .. vocab-1 no second; one without either has loss 0 and a gradient of zeros, and its
+ * logits are not read.  The same index may come several times: each time counts.  Logits of -inf have probability 0.
+ */
+typedef struct adacons_distill_matrix {   /* (token, column): stride in elements, any value; not looked at for one token.  Columns are 1 apart. */
+  void *data;
+  int64_t row_stride;
+} adacons_distill_matrix;
+
+typedef struct adacons_distill_shape {
+  int dtype;              /* of the student's logits and their gradient: ADACONS_F32, ADACONS_BF16 or ADACONS_F16 */
+  int teacher_dtype;      /* of the teacher's: any of them */
+  int ids_bits;           /* 32 or 64 */
+  int labels_bits;        /* 32 or 64; 0: no labels */
+  int tokens;             /* 0 .. 2^27 */
+  int vocab;              /* 1 .. 2^30 */
+  int top;                /* 1 .. 1024 */
+  float temperature;      /* tau > 0 */
+  float mix;              /* 0 .. 1 */
+} adacons_distill_shape;
+
+/* loss: `tokens` fp32 values; rows: 2 * tokens fp32 values, L of every token and then L1 (0 without labels), for the gradient.  Results must not share memory with
+ * what is read or with one another (EINVAL where two start together).  Errors: EINVAL, EALIGN, ELIMIT, ECUDA, EARCH. */
+int adacons_distill_forward(const adacons_distill_shape *shape, const adacons_distill_matrix *logits, const adacons_distill_matrix *ids,
+                            const adacons_distill_matrix *teacher, const void *labels, float *loss, float *rows, void *cuda_stream);
+
+/* dlogits from dloss (fp32 values dloss_stride apart: 0 for one value for all) and the forward pass's rows.  dlogits may be logits itself, otherwise it must not
+ * overlap what is read.  Moved in vectors where logits and dlogits lie alike relative to 16 bytes, otherwise written one by one.  Errors: as the forward pass. */
+int adacons_distill_backward(const adacons_distill_shape *shape, const float *dloss, int64_t dloss_stride, const adacons_distill_matrix *logits,
+                             const adacons_distill_matrix *ids, const adacons_distill_matrix *teacher, const void *labels, const float *rows,
+                             const adacons_distill_matrix *dlogits, void *cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------
  * Self-tests of the hang protection, as adacons_selftest_bounded_wait: the kernels of a call with one tile left
  * out, so that the waits behind it run out after 2 s each, the blocks let go of what they hold and return, and the
  * status word says ADACONS_FLAG_TIMEOUT.  The results are invalid, the next call's are not touched by it.

@@ -88,6 +88,11 @@ def load_library() -> ctypes.CDLL:
         "adacons_rope_create": [P(vp), i32, P(dbl), dbl, i32],
         "adacons_rope_apply": [vp, vp, vp, P(i64), vp, P(i64), vp, i64, i32, vp],
         "adacons_rope_destroy": [vp],
+        "adacons_norm_forward": [vp] * 10,
+        "adacons_norm_workspace_bytes": [vp, P(i64)],
+        "adacons_norm_backward": [vp] * 15 + [i64, vp],
+        "adacons_distill_forward": [vp] * 8,
+        "adacons_distill_backward": [vp, vp, i64] + [vp] * 7,
         "adacons_selftest_orth": [vp, vp, vp, vp],
         "adacons_selftest_attention": [vp] * 10 + [i64, vp],
     }
@@ -146,7 +151,7 @@ def on_stream(stream, device_index: int, given, call):
     with torch.cuda.stream(stream):
         results = call()
     for before, made in zip(given, results):
-        if before is None:
+        if before is None and made is not None:
             made.record_stream(caller)
     return results
 

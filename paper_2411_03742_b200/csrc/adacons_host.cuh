@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <mutex>
+
 #include "adacons.h"
 #include "adacons_common.cuh"
 
@@ -31,6 +33,24 @@ inline int query_device(DeviceInfo* info) {
   info->device = dev;
   info->sms = sms;
   info->encode.fn = reinterpret_cast<TensorMapEncodeFn>(fn);
+  return ADACONS_OK;
+}
+
+// The multiprocessors of the current device, for operators that need no more of it.
+inline int device_sms(int* sms) {
+  static std::mutex mutex;
+  static int known[64] = {};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return ADACONS_ECUDA; }
+  if (dev < 0 || dev >= 64) return ADACONS_ELIMIT;
+  std::lock_guard<std::mutex> lock(mutex);
+  if (known[dev] == 0) {
+    DeviceInfo info;
+    const int rc = query_device(&info);
+    if (rc != ADACONS_OK) return rc;
+    known[dev] = info.sms;
+  }
+  *sms = known[dev];
   return ADACONS_OK;
 }
 
