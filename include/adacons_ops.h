@@ -244,6 +244,47 @@ int adacons_distill_backward(const adacons_distill_shape *shape, const float *dl
                              const adacons_distill_matrix *dlogits, void *cuda_stream);
 
 /* ------------------------------------------------------------------------------------------------
+ * Gated feed-forward block and its gradient.
+ *
+ *     gate = x Wg^T,  up = x Wu^T,  y = (act(gate) up) Wd^T
+ * x, y: tokens x dim;  Wg, Wu: hidden x dim;  Wd: dim x hidden;  gate, up: tokens x hidden.  Sums are fp32; gate, up, their gradients and act(gate) up
+ * are rounded to the tensors' type once, as operands of the next product (what leaves its range there becomes Inf).
+ */
+enum { ADACONS_FFN_SILU = 0, ADACONS_FFN_GELU = 1, ADACONS_FFN_GELU_TANH = 2, ADACONS_FFN_RELU = 3 };
+
+typedef struct adacons_ffn_matrix {       /* (row, column), 16-byte aligned; the row stride in elements a multiple of 8 and at least a row (not looked at for one row) */
+  void *data;
+  int64_t row_stride;
+} adacons_ffn_matrix;
+
+typedef struct adacons_ffn_shape {
+  int dtype;              /* ADACONS_BF16 or ADACONS_F16 */
+  int tokens;             /* 0 .. 2^24 */
+  int dim, hidden;        /* multiples of 8, 8 .. 2^18 */
+  int act;                /* ADACONS_FFN_ */
+} adacons_ffn_shape;
+
+/* out: y.  gate, up: written for the gradient; without data, both of them, they are not.  workspace: device memory of adacons_ffn_workspace_bytes, 16-byte
+ * aligned, free for other use after the call's work.  Results must not share memory with what is read or with one another (EINVAL where two start together).
+ * Errors: EINVAL, EALIGN, ELIMIT, ECUDA, EARCH. */
+int adacons_ffn_workspace_bytes(const adacons_ffn_shape *shape, int backward, int64_t *bytes);
+int adacons_ffn_forward(const adacons_ffn_shape *shape, const adacons_ffn_matrix *x, const adacons_ffn_matrix *w_gate, const adacons_ffn_matrix *w_up,
+                        const adacons_ffn_matrix *w_down, const adacons_ffn_matrix *out, const adacons_ffn_matrix *gate, const adacons_ffn_matrix *up, void *workspace,
+                        int64_t workspace_bytes, void *cuda_stream);
+
+/* The gradients of x and the weights from that of y (dout) and the forward pass's gate and up; written, not added to.  One without data is not made.
+ * ADACONS_F16 holds the gradients of gate and up times a power of two, taken from dout's largest finite element, so that small or large ones stay in
+ * the type's range between the products.  No tokens: the weights' gradients are zeros.  Errors: as the forward pass. */
+int adacons_ffn_backward(const adacons_ffn_shape *shape, const adacons_ffn_matrix *dout, const adacons_ffn_matrix *x, const adacons_ffn_matrix *w_gate,
+                         const adacons_ffn_matrix *w_up, const adacons_ffn_matrix *w_down, const adacons_ffn_matrix *gate, const adacons_ffn_matrix *up,
+                         const adacons_ffn_matrix *dx, const adacons_ffn_matrix *dw_gate, const adacons_ffn_matrix *dw_up, const adacons_ffn_matrix *dw_down,
+                         void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/* ADACONS_FLAG_TIMEOUT if a bounded wait expired in a feed-forward kernel of the current device since the last call (results since are invalid);
+ * clears it.  Synchronises `cuda_stream`. */
+int adacons_ffn_get_status(uint32_t *flags, void *cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------
  * Self-tests of the hang protection, as adacons_selftest_bounded_wait: the kernels of a call with one tile left
  * out, so that the waits behind it run out after 2 s each, the blocks let go of what they hold and return, and the
  * status word says ADACONS_FLAG_TIMEOUT.  The results are invalid, the next call's are not touched by it.
@@ -251,7 +292,11 @@ int adacons_distill_backward(const adacons_distill_shape *shape, const float *dl
  *                               matrices fit one block (128 x 256), whose kernel has no such wait
  *   adacons_selftest_attention  the forward pass (dq NULL) or the gradient, with out in the place of dout; every block
  *                               lacks its last tile.  ADACONS_BF16 and head_dim up to 64, otherwise EINVAL
+ *   adacons_selftest_ffn        the first product of the feed-forward block whose one tile lacks its last operands; ADACONS_BF16, a single tile: up to
+ *                               256 tokens and 128 hidden elements for a pair of blocks (paired 1), half of either for a lone one
  */
+int adacons_selftest_ffn(const adacons_ffn_shape *shape, int paired, const adacons_ffn_matrix *x, const adacons_ffn_matrix *w_gate, const adacons_ffn_matrix *w_up, void *workspace,
+                         int64_t workspace_bytes, void *cuda_stream);
 int adacons_selftest_orth(adacons_orth *ctx, const void *update, void *out, void *cuda_stream);
 int adacons_selftest_attention(const adacons_attn_shape *shape, const adacons_attn_tensor *q, const adacons_attn_tensor *k,
                                const adacons_attn_tensor *v, const adacons_attn_tensor *out, float *lse, const adacons_attn_tensor *dq,

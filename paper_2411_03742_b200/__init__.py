@@ -10,6 +10,7 @@ from . import workloads  # noqa: F401
 _LAZY = {"AdaCons": "binding", "AdaConsError": "binding", "load_library": "binding", "Orthogonalizer": "orth",
          "attention_forward": "attention", "attention_backward": "attention", "Rope": "rope",
          "residual_norm_forward": "norms", "residual_norm_backward": "norms", "residual_norm": "norms",
+         "feedforward_forward": "feedforward", "feedforward_backward": "feedforward", "gated_feedforward": "feedforward",
          "distill_forward": "distillation", "distill_backward": "distillation", "distill": "distillation"}
 
 

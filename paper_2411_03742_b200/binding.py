@@ -91,6 +91,11 @@ def load_library() -> ctypes.CDLL:
         "adacons_norm_forward": [vp] * 10,
         "adacons_norm_workspace_bytes": [vp, P(i64)],
         "adacons_norm_backward": [vp] * 15 + [i64, vp],
+        "adacons_ffn_workspace_bytes": [vp, i32, P(i64)],
+        "adacons_ffn_forward": [vp] * 9 + [i64, vp],
+        "adacons_ffn_backward": [vp] * 13 + [i64, vp],
+        "adacons_ffn_get_status": [P(ctypes.c_uint32), vp],
+        "adacons_selftest_ffn": [vp, i32, vp, vp, vp, vp, i64, vp],
         "adacons_distill_forward": [vp] * 8,
         "adacons_distill_backward": [vp, vp, i64] + [vp] * 7,
         "adacons_selftest_orth": [vp, vp, vp, vp],

@@ -25,6 +25,7 @@ SOURCES = {
     "adacons_orth.cu": _OPS + ["csrc/adacons_orth.cuh"],
     "adacons_attn.cu": _OPS + ["csrc/adacons_attn.cuh"],
     "adacons_rope.cu": _OPS + ["csrc/adacons_rope.cuh"],
+    "adacons_ffn.cu": _OPS + ["csrc/adacons_ffn.cuh"],
     "adacons_distill.cu": _OPS + ["csrc/adacons_distill.cuh"],
     **{f"adacons_norm{t}.cu": _OPS + ["csrc/adacons_norm.cuh", "csrc/adacons_norm_run.cuh"] for t in ("", "_f32", "_bf16", "_f16")},
 }
