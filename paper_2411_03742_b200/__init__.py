@@ -18,5 +18,8 @@ def __getattr__(name):
     if name in _LAZY or name in _LAZY.values():
         import importlib
         mod = importlib.import_module("." + _LAZY.get(name, name), __name__)
-        return getattr(mod, name) if name in _LAZY else mod
+        if name not in _LAZY:
+            return mod
+        globals()[name] = value = getattr(mod, name)        # looked up once
+        return value
     raise AttributeError(name)

@@ -29,6 +29,11 @@ def layout(t):
     return None if t is None else (t.dtype, t.shape, t.stride(), t.get_device())
 
 
+def here(device: int, stream) -> bool:
+    """Whether a call on tensors of `device` can go ahead as it is; elsewhere() makes it otherwise."""
+    return stream is None and device == _current_device()
+
+
 def elsewhere(device: int, stream, given, call):
     """None where a call on tensors of `device` can go ahead as it is; otherwise the results of call() with their device current, or
     with the stream that was asked for current, for whose results that were not `given` the caller's stream is noted as a user."""

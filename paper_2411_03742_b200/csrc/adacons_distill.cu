@@ -56,11 +56,10 @@ DistillParams base_params(const adacons_distill_shape* s, const adacons_distill_
   p.tau = s->temperature;
   p.mix = s->mix;
   p.tokens = s->tokens;
-  p.power = s->temperature == 2.f || s->temperature == 3.f || s->temperature == 4.f ? static_cast<int>(s->temperature) : 0;
   return p;
 }
 // which exponentials a call takes: see DistillState
-int mode_of(const DistillParams& p) { return p.labels == nullptr || p.tau == 1.f ? 0 : p.power != 0 ? 1 : 2; }
+int mode_of(const DistillParams& p) { return p.labels == nullptr || p.tau == 1.f ? 0 : p.tau == 2.f || p.tau == 3.f || p.tau == 4.f ? static_cast<int>(p.tau) : 1; }
 
 // A warp for a short vocabulary, sixteen for a long one: a block's start and joins cost about 2 us, and that many more blocks run at once.
 int threads_of(int elements) { return elements <= 1024 ? 32 : elements <= 8192 ? 128 : 512; }
@@ -72,23 +71,25 @@ int shares_of(int64_t tokens, int vocab, int resident, int most) {
   return shares;
 }
 
-template <typename T>
-bool forward(const DistillParams& p, int threads, cudaStream_t st) {
+template <typename T, int MODE>
+bool run(const DistillParams& p, bool back, int threads, cudaStream_t st) {
   const dim3 grid(static_cast<unsigned>(p.tokens * p.shares)), block(threads);
-  switch (mode_of(p)) {
-    case 0: return launch(&distill_forward_kernel<T, 0>, grid, block, 0, st, kLaunchPlain, p.shares, p);
-    case 1: return launch(&distill_forward_kernel<T, 1>, grid, block, 0, st, kLaunchPlain, p.shares, p);
-    default: return launch(&distill_forward_kernel<T, 2>, grid, block, 0, st, kLaunchPlain, p.shares, p);
-  }
+  return back ? launch(&distill_backward_kernel<T, MODE>, grid, block, 0, st, kLaunchPlain, 1, p) : launch(&distill_forward_kernel<T, MODE>, grid, block, 0, st, kLaunchPlain, p.shares, p);
 }
 template <typename T>
-bool backward(const DistillParams& p, int threads, cudaStream_t st) {
-  const dim3 grid(static_cast<unsigned>(p.tokens * p.shares)), block(threads);
+bool run(const DistillParams& p, bool back, int threads, cudaStream_t st) {
   switch (mode_of(p)) {
-    case 0: return launch(&distill_backward_kernel<T, 0>, grid, block, 0, st, kLaunchPlain, 1, p);
-    case 1: return launch(&distill_backward_kernel<T, 1>, grid, block, 0, st, kLaunchPlain, 1, p);
-    default: return launch(&distill_backward_kernel<T, 2>, grid, block, 0, st, kLaunchPlain, 1, p);
+    case 0: return run<T, 0>(p, back, threads, st);
+    case 1: return run<T, 1>(p, back, threads, st);
+    case 2: return run<T, 2>(p, back, threads, st);
+    case 3: return run<T, 3>(p, back, threads, st);
+    default: return run<T, 4>(p, back, threads, st);
   }
+}
+bool run(const adacons_distill_shape* s, const DistillParams& p, bool back, cudaStream_t st) {
+  const int threads = threads_of(p.vocab / p.shares);
+  if (s->dtype == ADACONS_F32) return run<float>(p, back, threads, st);
+  return s->dtype == ADACONS_BF16 ? run<__nv_bfloat16>(p, back, threads, st) : run<__half>(p, back, threads, st);
 }
 
 }  // namespace
@@ -109,10 +110,7 @@ int adacons_distill_forward(const adacons_distill_shape* s, const adacons_distil
   p.loss = loss;
   p.rows = rows;
   p.shares = shares_of(p.tokens, p.vocab, 2 * sms, 8);
-  const int threads = threads_of(p.vocab / p.shares);
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const bool ok = s->dtype == ADACONS_F32 ? forward<float>(p, threads, st) : s->dtype == ADACONS_BF16 ? forward<__nv_bfloat16>(p, threads, st) : forward<__half>(p, threads, st);
-  return ok ? ADACONS_OK : ADACONS_ECUDA;
+  return run(s, p, false, static_cast<cudaStream_t>(cuda_stream)) ? ADACONS_OK : ADACONS_ECUDA;
 }
 
 int adacons_distill_backward(const adacons_distill_shape* s, const float* dloss, int64_t dloss_stride, const adacons_distill_matrix* logits, const adacons_distill_matrix* ids,
@@ -136,10 +134,7 @@ int adacons_distill_backward(const adacons_distill_shape* s, const float* dloss,
   p.dz_row = dlogits->row_stride;
   p.vectors = (reinterpret_cast<uintptr_t>(p.dz) - reinterpret_cast<uintptr_t>(p.z)) % 16 == 0 && (p.tokens == 1 || (p.dz_row - p.z_row) * size % 16 == 0);
   p.shares = shares_of(p.tokens, p.vocab, 2 * sms, 64);
-  const int threads = threads_of(p.vocab / p.shares);
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const bool ok = s->dtype == ADACONS_F32 ? backward<float>(p, threads, st) : s->dtype == ADACONS_BF16 ? backward<__nv_bfloat16>(p, threads, st) : backward<__half>(p, threads, st);
-  return ok ? ADACONS_OK : ADACONS_ECUDA;
+  return run(s, p, true, static_cast<cudaStream_t>(cuda_stream)) ? ADACONS_OK : ADACONS_ECUDA;
 }
 
 }  // extern "C"

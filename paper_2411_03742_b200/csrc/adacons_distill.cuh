@@ -80,7 +80,6 @@ struct DistillParams {
   long long dz_row;
   int shares;                                    // blocks of a token
   int vectors;                                   // z and dz lie alike relative to 16 bytes
-  int power;                                     // of the first exponential that the second is; 0: none
 };
 
 __device__ __forceinline__ float distill_ex2(float x) {
@@ -88,9 +87,19 @@ __device__ __forceinline__ float distill_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float distill_power(float e, int power) {       // 1 .. 4
+template <int POWER>
+__device__ __forceinline__ float distill_power(float e) {
   const float e2 = e * e;
-  return power == 1 ? e : power == 2 ? e2 : power == 3 ? e2 * e : e2 * e2;
+  return POWER == 2 ? e2 : POWER == 3 ? e2 * e : e2 * e2;
+}
+// the larger of two in each half of a vector's words, and of all of them; NaN where nothing else is left
+__device__ __forceinline__ uint32_t distill_max2(uint32_t a, uint32_t b, __nv_bfloat16) {
+  const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
+__device__ __forceinline__ uint32_t distill_max2(uint32_t a, uint32_t b, __half) {
+  const __half2 m = __hmax2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&m);
 }
 __device__ __forceinline__ long long distill_index(const void* p, int wide, long long at) {
   return wide ? static_cast<const long long*>(p)[at] : static_cast<const int*>(p)[at];
@@ -155,32 +164,27 @@ __device__ __forceinline__ void distill_share(int vocab, int shares, int share, 
   end = static_cast<int>(min(static_cast<long long>(vocab), static_cast<long long>(begin) + size));
 }
 
-// MODE 0: L alone; 1: L1 by powers; 2: L1 by exponentials of its own.
+// MODE 0: L alone; 1: L1 by exponentials of its own; 2, 3, 4: L1 from powers of L's.
 template <int MODE>
 struct DistillState {
   float m, s, s1;
   float k;                                       // log2(e) / tau
-  int power;
-  __device__ __forceinline__ DistillState(const DistillParams& p) : m(kDistillLow), s(0.f), s1(0.f), k(kDistillLog2e / p.tau), power(p.power) {}
+  __device__ __forceinline__ DistillState(const DistillParams& p) : m(kDistillLow), s(0.f), s1(0.f), k(kDistillLog2e / p.tau) {}
+  // the factor on s1 that goes with the factor e = 2^(d k) on s
+  __device__ __forceinline__ float second(float d, float e) const { return MODE == 1 ? distill_ex2(d * kDistillLog2e) : distill_power<MODE>(e); }
   __device__ __forceinline__ void rescale(float top) {         // to a larger maximum
     const float e = distill_ex2((m - top) * k);
     s *= e;
-    if (MODE == 1) s1 *= distill_power(e, power);
-    if (MODE == 2) s1 *= distill_ex2((m - top) * kDistillLog2e);
+    if (MODE != 0) s1 *= second(m - top, e);
     m = top;
   }
-  __device__ __forceinline__ void add(float z) {               // z <= m
+  __device__ __forceinline__ void add(float z) {
+    if (z > m) rescale(z);
     const float d = z - m, e = distill_ex2(d * k);
     s += e;
-    if (MODE == 1) s1 += distill_power(e, power);
-    if (MODE == 2) s1 += distill_ex2(d * kDistillLog2e);
+    if (MODE != 0) s1 += second(d, e);
   }
-  template <int N> __device__ __forceinline__ void add_all(const float (&z)[N]) {
-    float top = m;
-#pragma unroll
-    for (int i = 0; i < N; ++i) top = fmaxf(top, z[i]);
-    if (top > m) rescale(top);
-    float2 a = make_float2(0.f, 0.f), b = make_float2(0.f, 0.f);
+  template <int N> __device__ __forceinline__ void add_all(const float (&z)[N], float2& a, float2& b) const {      // none above m
     const float2 minus = make_float2(-m, -m), by = make_float2(k, k), by1 = make_float2(kDistillLog2e, kDistillLog2e);
 #pragma unroll
     for (int i = 0; i < N; i += 2) {
@@ -188,26 +192,39 @@ struct DistillState {
       const float2 e = make_float2(distill_ex2(x.x), distill_ex2(x.y));
       a = add2(a, e);
       if (MODE == 1) {
-        const float2 e2 = mul2(e, e);
-        b = add2(b, power == 2 ? e2 : power == 3 ? mul2(e2, e) : mul2(e2, e2));
-      }
-      if (MODE == 2) {
         const float2 y = mul2(d, by1);
         b = add2(b, make_float2(distill_ex2(y.x), distill_ex2(y.y)));
+      } else if (MODE != 0) {
+        const float2 e2 = mul2(e, e);
+        b = MODE == 2 ? fma2(e, e, b) : fma2(e2, MODE == 3 ? e : e2, b);
       }
     }
-    s += a.x + a.y;
-    if (MODE != 0) s1 += b.x + b.y;
   }
   __device__ __forceinline__ void join(float m2, float s2, float t2) {
     const float top = fmaxf(m, m2);
     if (top > m) rescale(top);
     const float e = distill_ex2((m2 - top) * k);
     s = fmaf(s2, e, s);
-    if (MODE == 1) s1 = fmaf(t2, distill_power(e, power), s1);
-    if (MODE == 2) s1 = fmaf(t2, distill_ex2((m2 - top) * kDistillLog2e), s1);
+    if (MODE != 0) s1 = fmaf(t2, second(m2 - top, e), s1);
   }
 };
+template <typename T, int N>
+__device__ __forceinline__ float distill_top(const uint4 (&raw)[N]) {
+  if constexpr (sizeof(T) == 4) {
+    float m = kDistillLow;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(raw[i].x), __uint_as_float(raw[i].y)), fmaxf(__uint_as_float(raw[i].z), __uint_as_float(raw[i].w))));
+    return m;
+  } else {
+    uint32_t m = raw[0].x;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m = distill_max2(distill_max2(m, raw[i].x, T()), distill_max2(distill_max2(raw[i].y, raw[i].z, T()), raw[i].w, T()), T());
+    const uint4 all = make_uint4(m, m, m, m);
+    float f[DistillVec<T>::kN];
+    DistillVec<T>::unpack(all, f);
+    return fmaxf(f[0], f[1]);
+  }
+}
 
 template <typename T, int MODE>
 __global__ void __launch_bounds__(512, 2) distill_forward_kernel(const DistillParams p) {
@@ -252,30 +269,46 @@ __global__ void __launch_bounds__(512, 2) distill_forward_kernel(const DistillPa
     int begin, end;
     distill_share(p.vocab, shares, share, begin, end);
     const DistillSpan<T> span(z, begin, end);
-    if (tid < span.head) { const float v = V::one(span.from + tid); if (v > st.m) st.rescale(v); st.add(v); }
+    if (tid < span.head) st.add(V::one(span.from + tid));
     const uint4* body = reinterpret_cast<const uint4*>(span.from + span.head);
-    constexpr int kDeep = 32 / V::kN;            // vectors between two looks
+    constexpr int kDeep = 4;                     // vectors between two looks; the next ones are on their way meanwhile
+    auto take = [&](const auto& raw) {
+      const float top = distill_top<T>(raw);
+      if (top > st.m) st.rescale(top);
+      float2 a = make_float2(0.f, 0.f), b = make_float2(0.f, 0.f);
+#pragma unroll
+      for (const uint4& v : raw) {
+        float g[V::kN];
+        V::unpack(v, g);
+        st.add_all(g, a, b);
+      }
+      st.s += a.x + a.y;
+      if (MODE != 0) st.s1 += b.x + b.y;
+    };
     int at_vector = tid;
-    for (; at_vector + (kDeep - 1) * threads < span.vectors; at_vector += kDeep * threads) {
-      uint4 raw[kDeep];
+    const int last = span.vectors - (kDeep - 1) * threads;       // where a thread's kDeep vectors may start at most
+    uint4 raw[kDeep];
+    if (at_vector < last) {
 #pragma unroll
       for (int i = 0; i < kDeep; ++i) raw[i] = ld_stream_v4(body + at_vector + i * threads);
-      float f[32];
+    }
+    while (at_vector < last) {
+      uint4 next[kDeep];
+      const int ahead = at_vector + kDeep * threads;
+      if (ahead < last) {
 #pragma unroll
-      for (int i = 0; i < kDeep; ++i) {
-        float g[V::kN];
-        V::unpack(raw[i], g);
-#pragma unroll
-        for (int e = 0; e < V::kN; ++e) f[i * V::kN + e] = g[e];
+        for (int i = 0; i < kDeep; ++i) next[i] = ld_stream_v4(body + ahead + i * threads);
       }
-      st.add_all(f);
+      take(raw);
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) raw[i] = next[i];
+      at_vector = ahead;
     }
     for (; at_vector < span.vectors; at_vector += threads) {
-      float g[V::kN];
-      V::unpack(ld_stream_v4(body + at_vector), g);
-      st.add_all(g);
+      const uint4 one[1] = {ld_stream_v4(body + at_vector)};
+      take(one);
     }
-    if (tid < span.tail) { const float v = V::one(span.from + span.head + span.vectors * V::kN + tid); if (v > st.m) st.rescale(v); st.add(v); }
+    if (tid < span.tail) st.add(V::one(span.from + span.head + span.vectors * V::kN + tid));
   }
   // lanes, warps, blocks
 #pragma unroll
@@ -385,12 +418,12 @@ __global__ void __launch_bounds__(512, 2) distill_backward_kernel(const DistillP
   // exp(z - L1) = exp(z / tau - L)^tau exp(tau L - L1)
   const float L = p.rows[row], L1 = p.rows[p.tokens + row];
   const float with = MODE == 0 ? soft + hard : soft;
-  const float by_power = MODE == 1 ? hard * expf(p.tau * L - L1) : 0.f;
+  const float by_power = MODE > 1 ? hard * expf(p.tau * L - L1) : 0.f;
   auto gradient = [&](float v) {
     const float e = distill_ex2(fmaf(v, inv_tau, -L) * kDistillLog2e);
     if (MODE == 0) return with * e;
-    if (MODE == 1) return fmaf(by_power, distill_power(e, p.power), with * e);
-    return fmaf(hard, distill_ex2((v - L1) * kDistillLog2e), with * e);
+    if (MODE == 1) return fmaf(hard, distill_ex2((v - L1) * kDistillLog2e), with * e);
+    return fmaf(by_power, distill_power<MODE>(e), with * e);
   };
   if (p.vectors) {
     const DistillSpan<T> span(z, begin, end);

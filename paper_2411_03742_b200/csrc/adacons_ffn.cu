@@ -2,6 +2,7 @@
 #include "adacons_ops.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <mutex>
 
@@ -25,7 +26,7 @@ struct FfnDevice {
 
 template <int KIND, bool BF16, int CG, bool STARVE = false>
 bool raise() {
-  if (cudaFuncSetAttribute(ffn_kernel<KIND, BF16, CG, STARVE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kFfnBytes)) == cudaSuccess) return true;
+  if (cudaFuncSetAttribute(ffn_kernel<KIND, BF16, CG, STARVE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(FfnTiling<CG>::bytes(CG == 2 ? kFfnPairStages : kFfnLoneStages))) == cudaSuccess) return true;
   cudaGetLastError();
   return false;
 }
@@ -55,7 +56,7 @@ int ffn_device(FfnDevice** out) {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3(2 * d.info.sms);
     cfg.blockDim = dim3(kFfnThreads);
-    cfg.dynamicSmemBytes = kFfnBytes;
+    cfg.dynamicSmemBytes = FfnTiling<2>::bytes(kFfnPairStages);
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     int pairs = 0;
@@ -95,6 +96,15 @@ bool make_map(const FfnDevice& d, CUtensorMap* map, const adacons_ffn_shape* s, 
   return encode_map(d.info, map, s->dtype == ADACONS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, data, dims, strides, box);
 }
 
+// results, for stores of 32 x 32
+bool make_out(const FfnDevice& d, CUtensorMap* map, const adacons_ffn_shape* s, const FfnRows& r, int rows, int cols) {
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(r.row) * 2};
+  const cuuint32_t box[2] = {32, 32}, ones[2] = {1, 1};
+  return d.info.encode(map, s->dtype == ADACONS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, static_cast<cuuint32_t>(2), r.data, dims, strides, box, ones,
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 FfnRows as_rows(const void* data, int64_t row_stride, int cols, int rows) {
   FfnRows r;
   r.data = const_cast<void*>(data);
@@ -113,22 +123,26 @@ int64_t workspace_bytes(const adacons_ffn_shape* s, bool back) {
 
 struct FfnPlan { int cg, shares; double time; };
 
-// Tiles by pairs of blocks or by lone ones, and how many share one's K: the quickest by a count of cycles.  A stage of a pair takes the tensor pipe's 512
-// cycles, a lone block's 256 but its operands 600 from L2; a launch costs 6000 cycles from the first operand to the last store, a join 2500.
+// Tiles by pairs of blocks or by lone ones, and how many share one's K: the quickest by a count of cycles.  A stage of half a pair's tile takes the tensor pipe
+// 512 cycles, one of a lone block's 256 but its operands some 500 from L2 beside the SM's other block; a launch costs 6000 cycles from the first operand to the
+// last store, a join 2500.
 FfnPlan plan_of(const FfnDevice& d, const FfnProblem* q, int n, int columns_by) {
-  auto tiles = [&](int tm, int tn) {
-    int64_t sum = 0;
-    for (int k = 0; k < n; ++k) sum += static_cast<int64_t>((q[k].m + tm - 1) / tm) * ((q[k].n + tn - 1) / tn);
-    return sum;
-  };
+  double work = 0.0;                             // stages of halves
+  int64_t lone_tiles = 0;
   int steps = 1;
-  for (int k = 0; k < n; ++k) steps = std::max(steps, q[k].steps * q[k].segments);
-  const int64_t pair_tiles = tiles(256, 256 / columns_by), lone_tiles = tiles(128, 128 / columns_by);
-  FfnPlan best = {2, 1, static_cast<double>((pair_tiles + d.pairs - 1) / d.pairs) * steps * 520.0 + 7000.0};
+  for (int k = 0; k < n; ++k) {
+    const int all = q[k].steps * q[k].segments, half = 256 / columns_by, lone = 128 / columns_by;
+    work += static_cast<double>((q[k].m + 255) / 256) * ((q[k].n + half - 1) / half) * all;
+    lone_tiles += static_cast<int64_t>((q[k].m + 127) / 128) * ((q[k].n + lone - 1) / lone);
+    steps = std::max(steps, all);
+  }
+  // whole halves: the pairs with the most of them
+  FfnPlan best = {2, 1, std::max(std::ceil(work / steps / d.pairs) * steps, work / d.pairs) * 530.0 + 7000.0};
   for (int shares = 1; shares <= 8; shares *= 2) {
     if (shares > 1 && (steps < 2 * shares || n > 1)) break;
-    const double waves = static_cast<double>((lone_tiles * shares + d.info.sms - 1) / d.info.sms);
-    const double time = waves * ((steps + shares - 1) / shares * 600.0 + 6000.0 + (shares > 1 ? 2500.0 : 0.0));
+    const int64_t blocks = lone_tiles * shares, per_sm = (blocks + d.info.sms - 1) / d.info.sms;
+    const double each = (steps + shares - 1) / shares * 500.0;
+    const double time = per_sm * each + ((per_sm + 1) / 2) * (6000.0 + (shares > 1 ? 2500.0 : 0.0));
     if (time < best.time) best = {1, shares, time};
   }
   return best;
@@ -136,15 +150,17 @@ FfnPlan plan_of(const FfnDevice& d, const FfnProblem* q, int n, int columns_by) 
 
 template <int KIND, bool BF16, int CG>
 bool run(const FfnParams& p, int blocks, int cluster, bool overlap, cudaStream_t st) {
-  return launch(&ffn_kernel<KIND, BF16, CG>, dim3(blocks), dim3(kFfnThreads), kFfnBytes, st, overlap ? kLaunchOverlap : kLaunchPlain, cluster, p);
+  return launch(&ffn_kernel<KIND, BF16, CG>, dim3(blocks), dim3(kFfnThreads), FfnTiling<CG>::bytes(CG == 2 ? kFfnPairStages : p.stages), st, overlap ? kLaunchOverlap : kLaunchPlain, cluster, p);
 }
 
 // Numbers the problems' tiles and launches.
 template <int KIND>
 bool run(const FfnDevice& d, const adacons_ffn_shape* s, FfnParams* p, int n, const FfnPlan& plan, bool overlap, cudaStream_t st) {
-  const int tm = 128 * plan.cg, tn = KIND == kFfnUp ? tm / 2 : tm;
+  const int tm = 128 * plan.cg, tn = KIND == kFfnUp ? tm / 2 : tm;       // of half a tile
+  for (int k = 0; KIND == kFfnPlain && k < n; ++k)
+    if (!make_out(d, &p->outs[k], s, p->problem[k].out, p->problem[k].m, p->problem[k].n)) return false;
   p->problems = n;
-  p->tiles = 0;
+  p->wholes = 0;
   p->shares = plan.shares;
   p->act = s->act;
   p->flags = d.flags;
@@ -152,15 +168,23 @@ bool run(const FfnDevice& d, const adacons_ffn_shape* s, FfnParams* p, int n, co
     FfnProblem& q = p->problem[k];
     q.tiles_m = (q.m + tm - 1) / tm;
     q.tiles_n = (q.n + tn - 1) / tn;
-    q.first = p->tiles;
-    p->tiles += q.tiles_m * q.tiles_n;
+    q.first = p->wholes;
+    p->wholes += q.tiles_m * ((q.tiles_n + plan.cg - 1) / plan.cg);
   }
+  p->tiles = p->wholes;
   const bool bf16 = s->dtype == ADACONS_BF16;
   if (plan.cg == 2) {
+    // a last round in which at most half of the pairs would have a tile: halves, for all
+    const int rest = p->wholes % d.pairs;
+    if (2 * rest <= d.pairs) {
+      p->wholes -= rest;
+      p->tiles += rest;
+    }
     const int blocks = 2 * std::min(p->tiles, d.pairs);
     return bf16 ? run<KIND, true, 2>(*p, blocks, 2, overlap, st) : run<KIND, false, 2>(*p, blocks, 2, overlap, st);
   }
   const int blocks = p->tiles * plan.shares;
+  p->stages = blocks <= d.info.sms ? kFfnLoneStages : kFfnCrowdStages;
   return bf16 ? run<KIND, true, 1>(*p, blocks, plan.shares, overlap, st) : run<KIND, false, 1>(*p, blocks, plan.shares, overlap, st);
 }
 
@@ -189,6 +213,7 @@ FfnProblem up_problem(const adacons_ffn_shape* s, void* h) {
   q.n = s->hidden;
   q.steps = steps_of(s->dim);
   q.segments = 1;
+  q.early = 1;
   q.out = as_rows(h, s->hidden, s->hidden, s->tokens);
   return q;
 }
@@ -230,7 +255,9 @@ int adacons_ffn_forward(const adacons_ffn_shape* s, const adacons_ffn_matrix* x,
   p.problem[0] = up_problem(s, workspace);
   p.gate = as_rows(gate, s->hidden, s->tokens);
   p.up = as_rows(up, s->hidden, s->tokens);
-  if (!run<kFfnUp>(*d, s, &p, 1, plan_of(*d, p.problem, 1, 2), false, st)) return ADACONS_ECUDA;
+  if ((p.gate.data != nullptr && (!make_out(*d, &p.outs[0], s, p.gate, s->tokens, s->hidden) || !make_out(*d, &p.outs[1], s, p.up, s->tokens, s->hidden))) ||
+      !make_out(*d, &p.outs[2], s, p.problem[0].out, s->tokens, s->hidden) || !run<kFfnUp>(*d, s, &p, 1, plan_of(*d, p.problem, 1, 2), false, st))
+    return ADACONS_ECUDA;
   if (!make_map(*d, &p.maps[0], s, workspace, s->hidden, s->tokens, s->hidden) || !make_map(*d, &p.maps[1], s, wd->data, wd->row_stride, s->dim, s->hidden)) return ADACONS_ECUDA;
   FfnProblem q = {};
   q.b[0] = 1;
@@ -238,6 +265,7 @@ int adacons_ffn_forward(const adacons_ffn_shape* s, const adacons_ffn_matrix* x,
   q.n = s->dim;
   q.steps = steps_of(s->hidden);
   q.segments = 1;
+  q.early = 1;
   q.out = as_rows(out, s->dim, s->tokens);
   p.problem[0] = q;
   return run<kFfnPlain>(*d, s, &p, 1, plan_of(*d, p.problem, 1, 1), true, st) ? ADACONS_OK : ADACONS_ECUDA;
@@ -299,9 +327,12 @@ int adacons_ffn_backward(const adacons_ffn_shape* s, const adacons_ffn_matrix* d
   q.n = s->hidden;
   q.steps = steps_of(s->dim);
   q.segments = 1;
+  q.early = 1;
   q.out = as_rows(h, s->hidden, s->hidden, s->tokens);
   p.problem[0] = q;
-  if (!run<kFfnBack>(*d, s, &p, 1, plan_of(*d, p.problem, 1, 1), peaks != nullptr, st)) return ADACONS_ECUDA;
+  if (!make_out(*d, &p.outs[0], s, p.dgate, s->tokens, s->hidden) || !make_out(*d, &p.outs[1], s, p.dup, s->tokens, s->hidden) ||
+      !make_out(*d, &p.outs[2], s, q.out, s->tokens, s->hidden) || !run<kFfnBack>(*d, s, &p, 1, plan_of(*d, p.problem, 1, 1), peaks != nullptr, st))
+    return ADACONS_ECUDA;
   // dx, and the weights' gradients
   FfnProblem by_x = {}, by_w[3];
   int weights = 0;
@@ -313,6 +344,7 @@ int adacons_ffn_backward(const adacons_ffn_shape* s, const adacons_ffn_matrix* d
   by_x.n = s->dim;
   by_x.steps = steps_of(s->hidden);
   by_x.segments = 2;
+  by_x.early = 1;
   by_x.scaled = peaks != nullptr;
   by_x.out = as_rows(dx, s->dim, s->tokens);
   auto weight = [&](const adacons_ffn_matrix* to, int a, int b, int m, int n, bool scaled) {
@@ -385,12 +417,13 @@ int adacons_selftest_ffn(const adacons_ffn_shape* s, int paired, const adacons_f
     return ADACONS_ECUDA;
   p.problem[0] = up_problem(s, workspace);
   p.problem[0].tiles_m = p.problem[0].tiles_n = 1;
-  p.problems = p.tiles = p.shares = 1;
+  p.problems = p.tiles = p.wholes = p.shares = 1;
+  p.stages = kFfnCrowdStages;
   p.act = s->act;
   p.flags = d->flags;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const bool ok = paired ? launch(&ffn_kernel<kFfnUp, true, 2, true>, dim3(2), dim3(kFfnThreads), kFfnBytes, st, kLaunchPlain, 2, p)
-                         : launch(&ffn_kernel<kFfnUp, true, 1, true>, dim3(1), dim3(kFfnThreads), kFfnBytes, st, kLaunchPlain, 1, p);
+  const bool ok = paired ? launch(&ffn_kernel<kFfnUp, true, 2, true>, dim3(2), dim3(kFfnThreads), FfnTiling<2>::bytes(kFfnPairStages), st, kLaunchPlain, 2, p)
+                         : launch(&ffn_kernel<kFfnUp, true, 1, true>, dim3(1), dim3(kFfnThreads), FfnTiling<1>::bytes(kFfnCrowdStages), st, kLaunchPlain, 1, p);
   return ok ? ADACONS_OK : ADACONS_ECUDA;
 }
 

@@ -21,25 +21,36 @@ namespace adacons {
 // The operands lie as the caller has them: every tensor is a matrix of 64 x 64 boxes, taken K-major where its rows run along K and MN-major
 // where they run across it, and no transposed copy is made.
 //
-// Tiles.  CG = 2: a pair of blocks (two SMs) shares a tile of 256 x 256; each holds 128 rows of the left operand, half of the right one
-// and 128 rows of the result, 64 bytes from L2 a cycle and SM at the tensor pipe's full rate where a block alone would need 96.
-// One pair per two SMs walks through the tiles; one warp of each block copies operand stages by TMA, one thread of the even block issues the products
-// into one of two accumulators, eight warps work off the other.  CG = 1: tiles of 128 x 128, one block each, for problems whose
-// larger tiles would leave SMs idle; the blocks of a cluster may share one tile's K and add up their sums, in order, through one another's
+// Tiles.  CG = 2: a pair of blocks (two SMs) shares a tile of 256 x 512, in two halves of 256 columns; each block holds 128 rows of the left operand, half of
+// the right one's and 128 rows of the result, all 512 columns of its tensor memory.  That takes 48 bytes from L2 a cycle and SM at the tensor
+// pipe's full rate; L2 gives 40 to 50, and tiles of 256 x 256 in two buffers, which take 64, kept the pipe 69 to 74 % busy.
+// One pair per two SMs walks through the tiles; one warp of each block copies operand stages by TMA, one thread of the even block issues the products,
+// eight warps work off what is complete, 32 rows x 32 columns at a time, which leave through shared memory by TMA (stored by the lanes, each at
+// its own row, they took three times as long as what is computed for them).  The products of a tile's first and last stages run half by half, so that one half is worked off, or
+// freed, beside the other's products.  The last tiles are halves where that evens out the pairs' work.  CG = 1: tiles of 128 x 128, one block each and two blocks an SM,
+// for problems whose larger tiles would leave SMs idle; the blocks of a cluster may share one tile's K and add up their sums, in order, through one another's
 // shared memory.  Sums are fp32 throughout; g, u, h, dg and du are rounded to the tensors' type once, as operands.
 // fp16 holds dg and du times 2^k, with 2^k from dy's largest element, so that small or large gradients do not leave its range; the products
 // that they go into are divided by it again.
 // ----------------------------------------------------------------------------------------------
 constexpr int kFfnTK = 64;                       // K elements per stage: one 128-byte swizzled row
-constexpr int kFfnStages = 6;
-constexpr uint32_t kFfnOperand = 128 * kFfnTK * 2, kFfnStage = 2 * kFfnOperand;      // of a block: 128 rows of either operand
-constexpr uint32_t kFfnBars = kFfnStages * kFfnStage;
-constexpr uint32_t kFfnBytes = kFfnBars + 256 + 1024;          // + alignment of the base
-constexpr int kFfnThreads = 320;                 // warps 0-7 endings, 8 operand copies, 9 products
-constexpr int kFfnGroup = 8;                     // rows of tiles that are walked through together: their operands stay in L2
+constexpr uint32_t kFfnOperand = 128 * kFfnTK * 2;             // of a block: 128 rows of an operand
 constexpr int kFfnSumRow = 132;                  // floats of a row of partial sums
+constexpr int kFfnEndWarps = 8, kFfnThreads = 32 * (kFfnEndWarps + 2);      // endings, operand copies, products
+constexpr uint32_t kFfnPatch = 32 * 64;          // bytes of 32 rows x 32 columns on their way out: two of them a warp
+template <int CG> struct FfnTiling {
+  static constexpr int kHalves = CG;             // of a tile's columns
+  static constexpr uint32_t kStage = (1 + kHalves) * kFfnOperand;
+  static constexpr uint32_t bytes(int stages) { return stages * kStage + 512 + (CG == 2 ? 2 * kFfnEndWarps * kFfnPatch : 0u) + 1024; }       // + alignment of the base
+  static constexpr uint32_t kTmemCols = kHalves * 128 * CG;
+};
+// Stages: of a pair; of a lone block where one runs on an SM, and where two do
+constexpr int kFfnPairStages = 4, kFfnLoneStages = 6, kFfnCrowdStages = 3;
+static_assert(128 * kFfnSumRow * 4 <= kFfnCrowdStages * FfnTiling<1>::kStage, "partial sums take the stages' place");
+static_assert(FfnTiling<2>::bytes(kFfnPairStages) <= 227 * 1024 && FfnTiling<1>::bytes(kFfnLoneStages) <= 227 * 1024 && FfnTiling<1>::bytes(kFfnCrowdStages) <= 112 * 1024,
+              "shared memory of a block");
+constexpr int kFfnGroup = 8;                     // rows of tiles that are walked through together: their operands stay in L2
 constexpr int kFfnPeaks = 128;                   // blocks that look for dy's largest element
-static_assert(128 * kFfnSumRow * 4 <= kFfnBars, "partial sums take the stages' place");
 
 enum FfnKind { kFfnUp = 0, kFfnBack = 1, kFfnPlain = 2 };
 enum FfnAct { kActSilu = 0, kActGelu = 1, kActGeluTanh = 2, kActRelu = 3 };
@@ -54,14 +65,18 @@ struct FfnProblem {
   int a[2], b[2];                                // tensor maps: of each segment (Plain, Back), b: of Wg and Wu (Up)
   int m, n, steps, segments;                     // steps of kFfnTK of a segment
   int a_across, b_across;                        // the operand's rows are the K index
-  int tiles_m, tiles_n, first;                   // first: number of its first tile
+  int tiles_m, tiles_n, first;                   // tiles_n: counted in halves; first: number of its first whole tile
   int scaled;                                    // the operands hold 2^k times
+  int early;                                     // the right operand is not the work of the kernel before
   FfnRows out;
 };
 struct FfnParams {
-  CUtensorMap maps[8];
+  CUtensorMap maps[8];                           // operands: boxes of 64 x 64
+  CUtensorMap outs[4];                           // results: boxes of 32 x 32.  Up, Back: the two beside `out`, then out; Plain: each problem's
   FfnProblem problem[4];
   int problems, tiles, act, shares;
+  int wholes;                                    // tiles from this number on are halves
+  int stages;                                    // of a lone block
   FfnRows gate, up;                              // Up: written; Back: read
   FfnRows dgate, dup;                            // Back
   const unsigned* peaks;                         // of dy, kFfnPeaks of them (fp16), or null
@@ -80,30 +95,70 @@ __device__ __forceinline__ uint32_t ffn_pack(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// act(g) and its derivative.  gelu: g Phi(g) with Phi from the error function's approximation by Abramowitz and Stegun, 7.1.26 (absolute error
+__device__ __forceinline__ float2 ffn_ex2(float2 x) {
+  float2 y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(x.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(x.y));
+  return y;
+}
+__device__ __forceinline__ float2 ffn_rcp(float2 x) {
+  float2 y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(x.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(x.y));
+  return y;
+}
+__device__ __forceinline__ float2 ffn_both(float v) { return make_float2(v, v); }
+// act(g) and its derivative, of two values.  gelu: g Phi(g) with Phi from the error function's approximation by Abramowitz and Stegun, 7.1.26 (absolute error
 // 1.5e-7 of a value that is rounded to 11 bits at most), whose exponential is the derivative's as well.
-template <bool SLOPE>
-__device__ __forceinline__ void ffn_act(int act, float g, float& a, float& slope) {
-  if (act == kActSilu) {
-    const float s = __fdividef(1.f, 1.f + __expf(-g));
-    a = g * s;
-    if (SLOPE) slope = fmaf(a, 1.f - s, s);
-  } else if (act == kActGelu) {
-    const float e = __expf(-0.5f * g * g);
-    const float t = __fdividef(1.f, fmaf(0.3275911f * 0.70710678118654752f, fabsf(g), 1.f));
-    const float q = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    const float phi = g < 0.f ? q : 1.f - q;
-    a = g * phi;
-    if (SLOPE) slope = fmaf(g * 0.39894228040143268f, e, phi);
-  } else if (act == kActGeluTanh) {
-    const float k = 0.79788456080286536f, in = k * fmaf(0.044715f * g * g, g, g);
-    const float s = __fdividef(1.f, 1.f + __expf(-2.f * in));        // (1 + tanh in) / 2
-    a = g * s;
-    if (SLOPE) slope = fmaf(2.f * a * (1.f - s), k * fmaf(3.f * 0.044715f * g, g, 1.f), s);
+template <int ACT, bool SLOPE>
+__device__ __forceinline__ void ffn_act(float2 g, float2& a, float2& slope) {
+  constexpr float kLog2 = 1.4426950408889634f;
+  const float2 one = ffn_both(1.f);
+  if (ACT == kActSilu) {
+    const float2 s = ffn_rcp(add2(ffn_ex2(mul2(g, ffn_both(-kLog2))), one));
+    a = mul2(g, s);
+    if (SLOPE) slope = fma2(a, fma2(s, ffn_both(-1.f), one), s);
+  } else if (ACT == kActGelu) {
+    const float2 e = ffn_ex2(mul2(mul2(g, ffn_both(-0.5f * kLog2)), g));
+    const float2 t = ffn_rcp(fma2(make_float2(fabsf(g.x), fabsf(g.y)), ffn_both(0.3275911f * 0.70710678118654752f), one));
+    float2 q = fma2(t, ffn_both(0.5f * 1.061405429f), ffn_both(0.5f * -1.453152027f));
+    q = fma2(t, q, ffn_both(0.5f * 1.421413741f));
+    q = fma2(t, q, ffn_both(0.5f * -0.284496736f));
+    q = fma2(t, q, ffn_both(0.5f * 0.254829592f));
+    q = mul2(mul2(e, t), q);
+    const float2 rest = fma2(q, ffn_both(-1.f), one), phi = make_float2(g.x < 0.f ? q.x : rest.x, g.y < 0.f ? q.y : rest.y);
+    a = mul2(g, phi);
+    if (SLOPE) slope = fma2(mul2(g, ffn_both(0.39894228040143268f)), e, phi);
+  } else if (ACT == kActGeluTanh) {
+    constexpr float k = 0.79788456080286536f;
+    const float2 g2 = mul2(g, g), in = mul2(g, fma2(g2, ffn_both(0.044715f * k), ffn_both(k)));
+    const float2 s = ffn_rcp(add2(ffn_ex2(mul2(in, ffn_both(-2.f * kLog2))), one));        // (1 + tanh in) / 2
+    a = mul2(g, s);
+    if (SLOPE) slope = fma2(mul2(mul2(a, ffn_both(2.f)), fma2(s, ffn_both(-1.f), one)), fma2(g2, ffn_both(3.f * 0.044715f * k), ffn_both(k)), s);
   } else {
-    a = fmaxf(g, 0.f);
-    if (g != g) a = g;
-    if (SLOPE) slope = g > 0.f ? 1.f : 0.f;
+    a = make_float2(g.x < 0.f ? 0.f : g.x, g.y < 0.f ? 0.f : g.y);
+    if (SLOPE) slope = make_float2(g.x > 0.f ? 1.f : 0.f, g.y > 0.f ? 1.f : 0.f);
+  }
+}
+// of N pairs, the choice made once: the values' chains run beside one another (with a choice for each of them 512 columns took 35,000 cycles)
+template <bool SLOPE, int N>
+__device__ __forceinline__ void ffn_act_all(int act, const float2 (&g)[N], float2 (&a)[N], float2 (&slope)[N]) {
+  switch (act) {
+    case kActSilu:
+#pragma unroll
+      for (int e = 0; e < N; ++e) ffn_act<kActSilu, SLOPE>(g[e], a[e], slope[e]);
+      break;
+    case kActGelu:
+#pragma unroll
+      for (int e = 0; e < N; ++e) ffn_act<kActGelu, SLOPE>(g[e], a[e], slope[e]);
+      break;
+    case kActGeluTanh:
+#pragma unroll
+      for (int e = 0; e < N; ++e) ffn_act<kActGeluTanh, SLOPE>(g[e], a[e], slope[e]);
+      break;
+    default:
+#pragma unroll
+      for (int e = 0; e < N; ++e) ffn_act<kActRelu, SLOPE>(g[e], a[e], slope[e]);
   }
 }
 
@@ -119,104 +174,130 @@ __device__ __forceinline__ int ffn_exponent(const unsigned* peaks) {
 }
 __device__ __forceinline__ float ffn_power(int e) { return __int_as_float((127 + e) << 23); }
 
-// Eight values of a row, 16 bytes; `full`: sixteen, 32 bytes.
-template <bool BF16>
-__device__ __forceinline__ uint4 ffn_round8(const float* v) {
-  return make_uint4(ffn_pack<BF16>(v[0], v[1]), ffn_pack<BF16>(v[2], v[3]), ffn_pack<BF16>(v[4], v[5]), ffn_pack<BF16>(v[6], v[7]));
-}
 template <bool BF16, int N>
-__device__ __forceinline__ void ffn_put(const FfnRows& to, int row, int col, int cols, const float (&v)[N]) {
-  unsigned char* at = static_cast<unsigned char*>(to.data) + (row * to.row + col) * 2;
-  const uint4 a = ffn_round8<BF16>(v);
-  if constexpr (N == 16) {
-    const uint4 b = ffn_round8<BF16>(v + 8);
-    if (to.wide && col + 16 <= cols) {
-      st_global_v8(at, a, b, 0ull);
-      return;
+__device__ __forceinline__ void ffn_round(const float2 (&v)[N / 2], uint4* w) {
+#pragma unroll
+  for (int k = 0; k < N / 8; ++k)
+    w[k] = make_uint4(ffn_pack<BF16>(v[4 * k].x, v[4 * k].y), ffn_pack<BF16>(v[4 * k + 1].x, v[4 * k + 1].y), ffn_pack<BF16>(v[4 * k + 2].x, v[4 * k + 2].y),
+                      ffn_pack<BF16>(v[4 * k + 3].x, v[4 * k + 3].y));
+}
+// A warp's way out: 32 rows x 32 columns, a row a lane, into one of two places of shared memory, 16-byte units permuted as the tensor map's 64-byte swizzle
+// has them, and from there by TMA, which clips the matrix's edges.  The place is free again once the copy before last has read it.
+struct FfnWay {
+  unsigned char* places;
+  int next;
+  __device__ __forceinline__ void put(const uint4 (&v)[4], const CUtensorMap* map, int row0, int col) {
+    const int lane = threadIdx.x & 31;
+    if (lane == 0) bulk_wait_read<1>();
+    __syncwarp();
+    unsigned char* at = places + next * kFfnPatch;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(at + lane * 64 + ((k ^ ((lane >> 1) & 3)) * 16)) = v[k];
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store_2d(map, at, col, row0);
+      bulk_commit();
     }
-    if (col + 16 <= cols) *reinterpret_cast<uint4*>(at + 16) = b;
+    next ^= 1;
   }
-  *reinterpret_cast<uint4*>(at) = a;
+};
+__device__ __forceinline__ uint4* ffn_at(const FfnRows& t, int row, int col) {
+  return reinterpret_cast<uint4*>(static_cast<unsigned char*>(t.data) + (row * t.row + col) * 2);
 }
 template <int N>
 __device__ __forceinline__ void ffn_get(uint4 (&v)[N / 8], const FfnRows& from, int row, int col, int cols, bool there) {
+  const uint4* at = ffn_at(from, row, col);
+  if (from.wide && there && col + N <= cols) {
+#pragma unroll
+    for (int k = 0; k + 1 < N / 8; k += 2) ld_stream_v8(at + k, v[k], v[k + 1]);
+    if (N / 8 % 2 != 0) v[N / 8 - 1] = at[N / 8 - 1];
+    return;
+  }
 #pragma unroll
   for (int k = 0; k < N / 8; ++k) {
     v[k] = make_uint4(0u, 0u, 0u, 0u);
-    if (there && col + 8 * k < cols) v[k] = *reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(from.data) + (row * from.row + col + 8 * k) * 2);
+    if (there && col + 8 * k + 8 <= cols) v[k] = at[k];
   }
 }
 
-// What becomes of N neighbouring results of a row inside the matrix.  v: the sums (Up: of g), w: Up: of u; gate, up: Back: g and u there.
+// What becomes of N neighbouring results of a row.  v: the sums (Up: of g), w: Up: of u; gate, up: Back: g and u there.  one, two: g and u (Up), dg and du (Back);
+// result: h, or what Plain writes.
 template <int KIND, bool BF16, int N>
-__device__ __forceinline__ void ffn_end(const FfnParams& p, const FfnProblem& q, float factor, int row, int col, float (&v)[N], float (&w)[N], const uint4 (&gate)[N / 8],
-                                        const uint4 (&up)[N / 8]) {
+__device__ __forceinline__ void ffn_end(int act, float factor, float2 (&v)[N / 2], float2 (&w)[N / 2], const uint4* gate, const uint4* up, uint4* one, uint4* two, uint4* result) {
+  float2 a[N / 2];
   if constexpr (KIND == kFfnPlain) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] *= factor;
-    ffn_put<BF16>(q.out, row, col, q.n, v);
+    for (int e = 0; e < N / 2; ++e) a[e] = mul2(v[e], ffn_both(factor));
   } else if constexpr (KIND == kFfnUp) {
-    if (p.gate.data != nullptr) {
-      ffn_put<BF16>(p.gate, row, col, q.n, v);
-      ffn_put<BF16>(p.up, row, col, q.n, w);
-    }
+    ffn_act_all<false>(act, v, a, a);
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      float a, unused;
-      ffn_act<false>(p.act, v[e], a, unused);
-      w[e] *= a;
-    }
-    ffn_put<BF16>(q.out, row, col, q.n, w);
+    for (int e = 0; e < N / 2; ++e) a[e] = mul2(a[e], w[e]);
   } else {
-    float h[N];
+    float2 g[N / 2], slope[N / 2];
 #pragma unroll
     for (int k = 0; k < N / 8; ++k) {
-      const uint32_t gs[4] = {gate[k].x, gate[k].y, gate[k].z, gate[k].w}, us[4] = {up[k].x, up[k].y, up[k].z, up[k].w};
+      g[4 * k] = ffn_unpack<BF16>(gate[k].x);
+      g[4 * k + 1] = ffn_unpack<BF16>(gate[k].y);
+      g[4 * k + 2] = ffn_unpack<BF16>(gate[k].z);
+      g[4 * k + 3] = ffn_unpack<BF16>(gate[k].w);
+    }
+    ffn_act_all<true>(act, g, a, slope);
+#pragma unroll
+    for (int k = 0; k < N / 8; ++k) {
+      const uint32_t us[4] = {up[k].x, up[k].y, up[k].z, up[k].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float2 g2 = ffn_unpack<BF16>(gs[i]), u2 = ffn_unpack<BF16>(us[i]);
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const int e = 8 * k + 2 * i + s;
-          const float u = s ? u2.y : u2.x, dh = v[e] * factor;
-          float a, slope;
-          ffn_act<true>(p.act, s ? g2.y : g2.x, a, slope);
-          h[e] = a * u;
-          v[e] = dh * u * slope;
-          w[e] = dh * a;
-        }
+        const int e = 4 * k + i;
+        const float2 u = ffn_unpack<BF16>(us[i]), dh = mul2(v[e], ffn_both(factor));
+        v[e] = mul2(mul2(dh, u), slope[e]);
+        w[e] = mul2(dh, a[e]);
+        a[e] = mul2(a[e], u);
       }
     }
-    ffn_put<BF16>(p.dgate, row, col, q.n, v);
-    ffn_put<BF16>(p.dup, row, col, q.n, w);
-    ffn_put<BF16>(q.out, row, col, q.n, h);
   }
+  if (KIND != kFfnPlain) {
+    ffn_round<BF16, N>(v, one);
+    ffn_round<BF16, N>(w, two);
+  }
+  ffn_round<BF16, N>(a, result);
 }
 
-// Tile t: its problem, and which one of it; kFfnGroup rows of tiles at a time, along the columns.
-struct FfnSpot { int problem, i, j; };
+// Tile t: its problem, the row of tiles, its first half and how many of them.  kFfnGroup rows of tiles at a time, along the columns.
+struct FfnSpot { int problem, i, j, halves; };
+template <int CG>
 __device__ __forceinline__ FfnSpot ffn_spot(const FfnParams& p, int t) {
+  constexpr int kHalves = FfnTiling<CG>::kHalves;
   FfnSpot s;
+  const int whole = t < p.wholes ? t : p.wholes + (t - p.wholes) / kHalves;
   s.problem = 0;
-  while (s.problem + 1 < p.problems && t >= p.problem[s.problem + 1].first) ++s.problem;
+  while (s.problem + 1 < p.problems && whole >= p.problem[s.problem + 1].first) ++s.problem;
   const FfnProblem& q = p.problem[s.problem];
-  const int at = t - q.first, group = at / (kFfnGroup * q.tiles_n), in = at - group * kFfnGroup * q.tiles_n;
+  const int columns = (q.tiles_n + kHalves - 1) / kHalves;
+  const int at = whole - q.first, group = at / (kFfnGroup * columns), in = at - group * kFfnGroup * columns;
   const int rows = min(kFfnGroup, q.tiles_m - group * kFfnGroup);
-  s.j = in / rows;
-  s.i = group * kFfnGroup + in - s.j * rows;
+  const int j = in / rows;
+  s.i = group * kFfnGroup + in - j * rows;
+  s.j = j * kHalves;
+  s.halves = min(kHalves, q.tiles_n - s.j);
+  if (t >= p.wholes) {
+    const int half = (t - p.wholes) % kHalves;
+    s.j += half;
+    s.halves = half < s.halves ? 1 : 0;          // the second half of a tile that has one: nothing
+  }
   return s;
 }
 
 template <int KIND, bool BF16, int CG, bool STARVE = false>
-__global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_constant__ FfnParams p) {
+__global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const __grid_constant__ FfnParams p) {
   extern __shared__ unsigned char smem_dyn[];
-  constexpr int kTM = 128 * CG, kTN = 128 * CG, kCols = KIND == kFfnUp ? kTN / 2 : kTN;      // kCols: columns of the result in a tile
-  constexpr int kBuffers = CG;                   // a lone block has one tile
-  constexpr uint32_t kTmemCols = kBuffers * kTN;
+  using T = FfnTiling<CG>;
+  constexpr int kTM = 128 * CG, kTN = 128 * CG, kCols = KIND == kFfnUp ? kTN / 2 : kTN;      // of half a tile; kCols: columns of the result
   unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + kFfnBars);
-  uint64_t* empty = full + kFfnStages;
-  uint64_t* acc_full = empty + kFfnStages;       // [2]
+  const int stages = CG == 2 ? kFfnPairStages : p.stages;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + stages * T::kStage);
+  uint64_t* empty = full + stages;
+  uint64_t* acc_full = empty + stages;       // [2] half by half
   uint64_t* acc_free = acc_full + 2;             // [2]
   uint64_t* drain = acc_free + 2;
   __shared__ uint32_t s_tmem;
@@ -225,26 +306,25 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int shares = CG == 2 ? 1 : p.shares;
   const int rank = CG == 2 || shares > 1 ? static_cast<int>(cluster_rank()) : 0;
-  const int half = CG == 2 ? rank : 0;           // of a pair
+  const int side_of_pair = CG == 2 ? rank : 0;
   const int worker = CG == 2 ? blockIdx.x / 2 : blockIdx.x / shares, workers = CG == 2 ? gridDim.x / 2 : p.tiles;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kFfnStages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_free[s], 8 * CG); }
+    for (int s = 0; s < stages; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(&acc_full[s], 1); mbar_init(&acc_free[s], kFfnEndWarps * CG); }
     mbar_init(drain, 1);
     s_abort = 0;
     s_issued = 0;
     mbar_init_fence();
     fence_proxy_async_smem();
   }
-  if (warp == 9) tmem_alloc<CG>(&s_tmem, kTmemCols);
+  if (warp == kFfnEndWarps + 1) tmem_alloc<CG>(&s_tmem, T::kTmemCols);
   tc_fence_before();
   __syncthreads();
   if (CG == 2) cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
   pdl_launch_dependents();
-  pdl_wait();
 
   // K steps of a tile that are this block's
   auto steps_of = [&](const FfnProblem& q, int& begin, int& end) {
@@ -253,164 +333,226 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
     end = CG == 2 ? all : static_cast<int>(static_cast<long long>(all) * (rank + 1) / shares);
   };
 
-  if (warp == 8) {
+  if (warp == kFfnEndWarps) {
     if (lane == 0) {
       int stage = 0, issued = 0;
       uint32_t parity = 1;                       // the stages start out empty
       bool ok = true;
-      for (int t = worker; ok && t < p.tiles; t += workers) {
-        const FfnSpot s = ffn_spot(p, t);
-        const FfnProblem& q = p.problem[s.problem];
-        int begin, end;
-        steps_of(q, begin, end);
-        const int arow = s.i * kTM + half * 128;
-        for (int k = begin; k < end; ++k) {
-          if (STARVE && k == end - 1) break;
-          if (s_abort || !mbar_wait_bounded(&empty[stage], parity)) { s_abort = 1; ok = false; break; }
-          const int segment = k >= q.steps ? 1 : 0, k0 = (k - segment * q.steps) * kFfnTK;
-          unsigned char* at = smem + stage * kFfnStage;
-          if (half == 0) mbar_expect_tx(&full[stage], CG * kFfnStage);      // a pair's bytes all count on the even block's barrier
-          auto load = [&](unsigned char* dst, int map, int x, int y) {
-            if (CG == 2) tma_load_2d_pair(dst, &p.maps[map], &full[stage], x, y);
-            else tma_load_2d(dst, &p.maps[map], &full[stage], x, y);
-          };
+      auto load = [&](unsigned char* dst, int map, int x, int y, int s) {
+        if (CG == 2) tma_load_2d_pair(dst, &p.maps[map], &full[s], x, y);
+        else tma_load_2d(dst, &p.maps[map], &full[s], x, y);
+      };
+      auto load_left = [&](const FfnSpot& s, const FfnProblem& q, int k, int at) {
+        const int segment = k >= q.steps ? 1 : 0, k0 = (k - segment * q.steps) * kFfnTK;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int r = arow + h * 64;
-            load(at + h * 8192, q.a[segment], q.a_across ? r : k0, q.a_across ? k0 : r);
-          }
+        for (int h = 0; h < 2; ++h) {
+          const int r = s.i * kTM + side_of_pair * 128 + h * 64;
+          load(smem + at * T::kStage + h * 8192, q.a[segment], q.a_across ? r : k0, q.a_across ? k0 : r, at);
+        }
+      };
+      auto load_right = [&](const FfnSpot& s, const FfnProblem& q, int k, int at) {
+        const int segment = k >= q.steps ? 1 : 0, k0 = (k - segment * q.steps) * kFfnTK;
+        if (side_of_pair == 0) mbar_expect_tx(&full[at], CG * (1 + s.halves) * kFfnOperand);      // a pair's bytes all count on the even block's barrier
+        for (int n = 0; n < s.halves; ++n)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             int map, r;
             if (KIND == kFfnUp) {
-              map = q.b[CG == 2 ? half : h];
-              r = s.j * kCols + (CG == 2 ? h * 64 : 0);
+              map = q.b[CG == 2 ? side_of_pair : h];
+              r = (s.j + n) * kCols + (CG == 2 ? h * 64 : 0);
             } else {
               map = q.b[segment];
-              r = s.j * kCols + half * 128 + h * 64;
+              r = (s.j + n) * kCols + side_of_pair * 128 + h * 64;
             }
-            load(at + kFfnOperand + h * 8192, map, q.b_across ? r : k0, q.b_across ? k0 : r);
+            load(smem + at * T::kStage + (1 + n) * kFfnOperand + h * 8192, map, q.b_across ? r : k0, q.b_across ? k0 : r, at);
           }
-          ++issued;
-          if (++stage == kFfnStages) { stage = 0; parity ^= 1u; }
-        }
-      }
-      s_issued = issued;
-    }
-  } else if (warp == 9) {
-    if (half == 0) {
-      // The whole warp goes through the loop, so that addresses and descriptors are uniform values; one lane issues.
-      const bool issuer = elect_one();
-      const uint32_t base = (smem_addr(smem) & 0x3ffffu) >> 4;             // descriptors count 16-byte units; above are a cluster block's number and their other fields
-      int stage = 0, buf = 0;
-      uint32_t parity = 0, acc_parity = 1;
-      bool ok = true;
-      for (int t = worker; ok && t < p.tiles; t += workers) {
-        const FfnSpot s = ffn_spot(p, t);
+      };
+      // What does not come from the kernel before is on its way while that one ends.
+      int ahead = 0;
+      if (worker < p.tiles) {
+        const FfnSpot s = ffn_spot<CG>(p, worker);
         const FfnProblem& q = p.problem[s.problem];
         int begin, end;
         steps_of(q, begin, end);
+        if (q.early && s.halves > 0 && !STARVE)
+          for (; ahead < stages && begin + ahead < end; ++ahead) load_right(s, q, begin + ahead, ahead);
+      }
+      pdl_wait();
+      for (int t = worker; ok && t < p.tiles; t += workers) {
+        const FfnSpot s = ffn_spot<CG>(p, t);
+        if (s.halves == 0) continue;
+        const FfnProblem& q = p.problem[s.problem];
+        int begin, end;
+        steps_of(q, begin, end);
+        for (int k = begin; k < end; ++k) {
+          if (STARVE && k == end - 1) break;
+          if (s_abort || !mbar_wait_bounded(&empty[stage], parity)) { s_abort = 1; ok = false; break; }
+          if (issued >= ahead) load_right(s, q, k, stage);
+          load_left(s, q, k, stage);
+          ++issued;
+          if (++stage == stages) { stage = 0; parity ^= 1u; }
+        }
+      }
+      s_issued = max(issued, ahead);
+    }
+  } else if (warp == kFfnEndWarps + 1) {
+    if (side_of_pair == 0) {
+      // The whole warp goes through the loop, so that addresses and descriptors are uniform values; one lane issues.
+      const bool issuer = elect_one();
+      const uint32_t base = (smem_addr(smem) & 0x3ffffu) >> 4;             // descriptors count 16-byte units; above are a cluster block's number and their other fields
+      int stage = 0;
+      uint32_t parity = 0, free_parity[2] = {1u, 1u};
+      bool ok = true;
+      for (int t = worker; ok && t < p.tiles; t += workers) {
+        const FfnSpot s = ffn_spot<CG>(p, t);
+        if (s.halves == 0) continue;
+        const FfnProblem& q = p.problem[s.problem];
+        int begin, end;
+        steps_of(q, begin, end);
+        const int steps = end - begin;
         const uint32_t idesc = mma_idesc(kTM, kTN, BF16, false, false) | (q.a_across ? 1u << 15 : 0u) | (q.b_across ? 1u << 16 : 0u);
         const uint64_t a_base = q.a_across ? desc_mnmajor(0, 8192) : desc_kmajor(0), b_base = q.b_across ? desc_mnmajor(0, 8192) : desc_kmajor(0);
         const uint32_t a_step = q.a_across ? 2048 / 16 : 32 / 16, b_step = q.b_across ? 2048 / 16 : 32 / 16;
-        if (s_abort || !mbar_wait_bounded(&acc_free[buf], acc_parity)) ok = false;
-        for (int k = begin; k < end; ++k) {
-          ok = ok && !s_abort && mbar_wait_bounded(&full[stage], parity);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) { s_abort = 1; break; }
-          tc_fence_after();
-          const uint64_t a = a_base + (base + stage * (kFfnStage >> 4)), b = b_base + (base + stage * (kFfnStage >> 4) + (kFfnOperand >> 4));
+        auto get = [&](uint64_t* bar, uint32_t phase) {
+          const bool got = !s_abort && mbar_wait_bounded(bar, phase);
+          if (!__all_sync(0xffffffffu, got)) { s_abort = 1; ok = false; }
+          return ok;
+        };
+        auto products = [&](int at, int half, bool first) {
+          const uint64_t a = a_base + (base + at * (T::kStage >> 4)), b = b_base + (base + at * (T::kStage >> 4) + (1 + half) * (kFfnOperand >> 4));
           if (issuer) {
 #pragma unroll
-            for (int kk = 0; kk < kFfnTK / 16; ++kk) mma_ss<CG>(tmem + buf * kTN, a + kk * a_step, b + kk * b_step, idesc, kk != 0 ? 1u : k != begin);
-            mma_commit<CG>(&empty[stage]);
+            for (int kk = 0; kk < kFfnTK / 16; ++kk) mma_ss<CG>(tmem + half * kTN, a + kk * a_step, b + kk * b_step, idesc, kk != 0 || !first ? 1u : 0u);
           }
           __syncwarp();
-          if (++stage == kFfnStages) { stage = 0; parity ^= 1u; }
+        };
+        auto commit = [&](uint64_t* bar) {
+          if (issuer) mma_commit<CG>(bar);
+          __syncwarp();
+        };
+        // `count` stages from the present one on, half after half; `opens`: the tile's first, `closes`: its last
+        auto by_halves = [&](int count, bool opens, bool closes) {
+          for (int half = 0; half < s.halves; ++half) {
+            if (opens) {
+              if (!get(&acc_free[half], free_parity[half])) return;
+              free_parity[half] ^= 1u;
+            }
+            int at = stage;
+            uint32_t phase = parity;
+            for (int k = 0; k < count; ++k) {
+              if (half == 0 && !get(&full[at], phase)) return;
+              tc_fence_after();
+              products(at, half, opens && k == 0);
+              if (half == s.halves - 1) commit(&empty[at]);
+              if (++at == stages) { at = 0; phase ^= 1u; }
+            }
+            if (closes) commit(&acc_full[half]);
+            if (half == s.halves - 1) { stage = at; parity = phase; }
+          }
+        };
+        const int first = min(steps, stages), last = min(steps - first, stages);
+        by_halves(first, true, last == 0);
+        for (int k = first; ok && k < steps - last; ++k) {
+          if (!get(&full[stage], parity)) break;
+          tc_fence_after();
+          for (int half = 0; half < s.halves; ++half) products(stage, half, false);
+          commit(&empty[stage]);
+          if (++stage == stages) { stage = 0; parity ^= 1u; }
         }
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) { s_abort = 1; break; }
-        if (issuer) mma_commit<CG>(&acc_full[buf]);
-        __syncwarp();
-        if (++buf == kBuffers) { buf = 0; acc_parity ^= 1u; }
+        if (ok && last > 0) by_halves(last, false, true);
       }
       if (s_abort && issuer) { mma_commit<CG>(drain); mbar_wait_bounded(drain, 0); }
       __syncwarp();
     }
   } else {
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
-    const int side = warp >> 2;                  // this warp's half of the columns
-    int buf = 0;
-    uint32_t parity = 0;
+    constexpr int kShare = kCols / (kFfnEndWarps / 4);       // columns of a warp
+    const int side = warp >> 2;                  // which of them
+    uint32_t parity[2] = {0u, 0u};
+    // a lone block's products have all read their stages by the time anything is put there
+    FfnWay way = {smem + (CG == 2 ? stages * T::kStage + 512 : 0u) + warp * 2 * kFfnPatch, 0};
+    pdl_wait();
     int exponent = 0;
     if (p.peaks != nullptr) exponent = ffn_exponent(p.peaks);
-    for (int t = worker; t < p.tiles; t += workers) {
-      const FfnSpot s = ffn_spot(p, t);
+    bool ok = true;
+    for (int t = worker; ok && t < p.tiles; t += workers) {
+      const FfnSpot s = ffn_spot<CG>(p, t);
       const FfnProblem& q = p.problem[s.problem];
-      const int row = s.i * kTM + half * 128 + (warp & 3) * 32 + lane, col0 = s.j * kCols + side * (kCols / 2);
+      const int row0 = s.i * kTM + side_of_pair * 128 + (warp & 3) * 32, row = row0 + lane;
       const float factor = KIND == kFfnBack ? ffn_power(exponent) : q.scaled ? ffn_power(-exponent) : 1.f;
       const bool there = row < q.m;
-      uint4 gate[2], up[2];
-      if (KIND == kFfnBack && shares == 1) {     // under way while the products are
-        ffn_get<16>(gate, p.gate, row, col0, q.n, there);
-        ffn_get<16>(up, p.up, row, col0, q.n, there);
-      }
-      const bool got = !s_abort && mbar_wait_bounded(&acc_full[buf], parity);
-      if (!__all_sync(0xffffffffu, got)) { s_abort = 1; break; }
-      tc_fence_after();
-      const uint32_t acc = tmem + buf * kTN + side * (kCols / 2) + lanes;
-      if (shares == 1) {
 #pragma unroll 1
-        for (int c = 0; c < kCols / 2; c += 16) {
-          const int col = col0 + c;
-          uint32_t raw[16], raw_up[16];
-          tmem_ld16(acc + c, raw);
-          if (KIND == kFfnUp) tmem_ld16(acc + kCols + c, raw_up);
-          uint4 next_gate[2], next_up[2];
-          if (KIND == kFfnBack && c + 16 < kCols / 2) {
-            ffn_get<16>(next_gate, p.gate, row, col + 16, q.n, there);
-            ffn_get<16>(next_up, p.up, row, col + 16, q.n, there);
-          }
-          tmem_wait_ld();
-          if (there && col < q.n) {
-            float v[16], w[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              v[e] = __uint_as_float(raw[e]);
-              w[e] = KIND == kFfnUp ? __uint_as_float(raw_up[e]) : 0.f;
+      for (int half = 0; half < s.halves; ++half) {
+        const int col0 = (s.j + half) * kCols + side * kShare;
+        uint4 gate[4], up[4];
+        if (KIND == kFfnBack && shares == 1) {   // under way while the products are
+          ffn_get<32>(gate, p.gate, row, col0, q.n, there);
+          ffn_get<32>(up, p.up, row, col0, q.n, there);
+        }
+        const bool got = !s_abort && mbar_wait_bounded(&acc_full[half], parity[half]);
+        if (!__all_sync(0xffffffffu, got)) { s_abort = 1; ok = false; break; }
+        parity[half] ^= 1u;
+        tc_fence_after();
+        const uint32_t acc = tmem + half * kTN + side * kShare + lanes;
+        if (shares == 1) {
+#pragma unroll 1
+          for (int c = 0; c < kShare && row0 < q.m; c += 32) {
+            const int col = col0 + c;
+            if (col >= q.n) break;
+            uint32_t raw[32], raw_up[32];
+            tmem_ld32(acc + c, raw);
+            if (KIND == kFfnUp) tmem_ld32(acc + kCols + c, raw_up);
+            uint4 one[4], two[4], result[4], next_gate[4], next_up[4];
+            if (KIND == kFfnBack && c + 32 < kShare) {
+              ffn_get<32>(next_gate, p.gate, row, col + 32, q.n, there);
+              ffn_get<32>(next_up, p.up, row, col + 32, q.n, there);
             }
-            ffn_end<KIND, BF16, 16>(p, q, factor, row, col, v, w, gate, up);
+            tmem_wait_ld();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float2 v[8], w[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                v[e] = make_float2(__uint_as_float(raw[16 * h + 2 * e]), __uint_as_float(raw[16 * h + 2 * e + 1]));
+                if (KIND == kFfnUp) w[e] = make_float2(__uint_as_float(raw_up[16 * h + 2 * e]), __uint_as_float(raw_up[16 * h + 2 * e + 1]));
+              }
+              ffn_end<KIND, BF16, 16>(p.act, factor, v, w, gate + 2 * h, up + 2 * h, one + 2 * h, two + 2 * h, result + 2 * h);
+            }
+            if (KIND == kFfnBack || (KIND == kFfnUp && p.gate.data != nullptr)) {
+              way.put(one, &p.outs[0], row0, col);
+              way.put(two, &p.outs[1], row0, col);
+            }
+            way.put(result, &p.outs[KIND == kFfnPlain ? s.problem : 2], row0, col);
+            if (KIND == kFfnBack) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) { gate[k] = next_gate[k]; up[k] = next_up[k]; }
+            }
           }
+          tc_fence_before();
           __syncwarp();
-          if (KIND == kFfnBack) {
-#pragma unroll
-            for (int k = 0; k < 2; ++k) { gate[k] = next_gate[k]; up[k] = next_up[k]; }
-          }
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) { if (CG == 2) mbar_arrive_leader(&acc_free[buf]); else mbar_arrive_one(&acc_free[buf]); }
-        __syncwarp();
-      } else {                                   // this block's sums, where the stages were: all products that read those are complete
-        float* sums = reinterpret_cast<float*>(smem) + ((warp & 3) * 32 + lane) * kFfnSumRow + side * 64;
+          if (lane == 0) { if (CG == 2) mbar_arrive_leader(&acc_free[half]); else mbar_arrive_one(&acc_free[half]); }
+          __syncwarp();
+        } else {                                 // this block's sums, where the stages were: all products that read those are complete
+          float* sums = reinterpret_cast<float*>(smem) + ((warp & 3) * 32 + lane) * kFfnSumRow + side * 64;
 #pragma unroll 1
-        for (int c = 0; c < 64; c += 16) {
-          uint32_t raw[16];
-          tmem_ld16(tmem + side * 64 + c + lanes, raw);
-          tmem_wait_ld();
+          for (int c = 0; c < 64; c += 16) {
+            uint32_t raw[16];
+            tmem_ld16(tmem + side * 64 + c + lanes, raw);
+            tmem_wait_ld();
 #pragma unroll
-          for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(sums + c + 4 * k) = make_uint4(raw[4 * k], raw[4 * k + 1], raw[4 * k + 2], raw[4 * k + 3]);
+            for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(sums + c + 4 * k) = make_uint4(raw[4 * k], raw[4 * k + 1], raw[4 * k + 2], raw[4 * k + 3]);
+          }
         }
       }
-      if (++buf == kBuffers) { buf = 0; parity ^= 1u; }
     }
+    if (lane == 0) bulk_wait<0>();
   }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
   if (CG == 1 && shares > 1) {
     cluster_sync_all();                          // every block's sums are in place
-    const FfnSpot s = ffn_spot(p, worker);
+    const FfnSpot s = ffn_spot<CG>(p, worker);
     const FfnProblem& q = p.problem[s.problem];
     if (warp < 8 && !s_abort) {
       const float factor = KIND == kFfnBack ? ffn_power(p.peaks == nullptr ? 0 : ffn_exponent(p.peaks)) : q.scaled ? ffn_power(p.peaks == nullptr ? 0 : -ffn_exponent(p.peaks)) : 1.f;
@@ -419,44 +561,51 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_kernel(const __grid_consta
         const int r = unit / kEights * shares + rank, c = unit % kEights * 8;        // the blocks take the rows in turn
         const int row = s.i * kTM + r, col = s.j * kCols + c;
         if (row >= q.m || col >= q.n) continue;
-        uint4 gate[1], up[1];
+        uint4 gate, up, one, two, result;
         if (KIND == kFfnBack) {
-          ffn_get<8>(gate, p.gate, row, col, q.n, true);
-          ffn_get<8>(up, p.up, row, col, q.n, true);
+          gate = *ffn_at(p.gate, row, col);
+          up = *ffn_at(p.up, row, col);
         }
-        float v[8], w[8];
+        float2 v[4], w[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = w[e] = 0.f;
+        for (int e = 0; e < 4; ++e) v[e] = w[e] = make_float2(0.f, 0.f);
         const float* at = reinterpret_cast<const float*>(smem) + r * kFfnSumRow + c;
         for (int b = 0; b < shares; ++b) {
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const float4 f = ld_cluster_f32x4(at + 4 * k, b);
-            v[4 * k] += f.x; v[4 * k + 1] += f.y; v[4 * k + 2] += f.z; v[4 * k + 3] += f.w;
+            v[2 * k] = add2(v[2 * k], make_float2(f.x, f.y));
+            v[2 * k + 1] = add2(v[2 * k + 1], make_float2(f.z, f.w));
             if (KIND == kFfnUp) {
               const float4 d = ld_cluster_f32x4(at + kCols + 4 * k, b);
-              w[4 * k] += d.x; w[4 * k + 1] += d.y; w[4 * k + 2] += d.z; w[4 * k + 3] += d.w;
+              w[2 * k] = add2(w[2 * k], make_float2(d.x, d.y));
+              w[2 * k + 1] = add2(w[2 * k + 1], make_float2(d.z, d.w));
             }
           }
         }
-        ffn_end<KIND, BF16, 8>(p, q, factor, row, col, v, w, gate, up);
+        ffn_end<KIND, BF16, 8>(p.act, factor, v, w, &gate, &up, &one, &two, &result);
+        if (KIND == kFfnBack || (KIND == kFfnUp && p.gate.data != nullptr)) {
+          *ffn_at(KIND == kFfnUp ? p.gate : p.dgate, row, col) = one;
+          *ffn_at(KIND == kFfnUp ? p.up : p.dup, row, col) = two;
+        }
+        *ffn_at(q.out, row, col) = result;
       }
     }
     cluster_sync_all();                          // nobody leaves while its sums are read
   }
   if (CG == 2) cluster_sync_all();               // the pair's copies and arrivals are all in, unless a wait expired
   if (s_abort && threadIdx.x == 0) {             // no copy may land after the block has gone
-    for (int s = 0; half == 0 && s < kFfnStages && s < s_issued; ++s) {
-      const int uses = (s_issued - 1 - s) / kFfnStages;          // the stage's last copy is its use number `uses`
+    for (int s = 0; side_of_pair == 0 && s < stages && s < s_issued; ++s) {
+      const int uses = (s_issued - 1 - s) / stages;          // the stage's last copy is its use number `uses`
       mbar_wait_bounded(&full[s], uses & 1);
     }
     atomicOr(p.flags, kFlagTimeout);
   }
   __syncthreads();
   if (CG == 2) cluster_sync_all();
-  if (warp == 9) {
+  if (warp == kFfnEndWarps + 1) {
     tc_fence_after();
-    tmem_dealloc<CG>(tmem, kTmemCols);
+    tmem_dealloc<CG>(tmem, T::kTmemCols);
   }
 }
 

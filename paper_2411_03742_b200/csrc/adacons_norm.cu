@@ -36,21 +36,18 @@ int check_shape(const adacons_norm_shape* s) {
 
 NormPlan plan_of(const adacons_norm_shape* s, int sms) {
   NormPlan n = {};
-  n.c = s->dim <= 4096 ? 1 : s->dim <= 8192 ? 2 : 4;
+  n.c = s->dim <= 256 ? 1 : s->dim <= 8192 ? 2 : 4;
   const int wanted = (s->dim + kNormN * n.c - 1) / (kNormN * n.c);
   n.tpr = 32;
   while (n.tpr < wanted) n.tpr *= 2;
-  n.threads = n.tpr <= 256 ? 256 : 512;
   const int64_t tokens = static_cast<int64_t>(s->batch) * s->len;
-  const int per_block = n.threads / n.tpr;
-  const int64_t blocks = (tokens + per_block - 1) / per_block;
-  n.forward_blocks = static_cast<int>(std::min<int64_t>(blocks, static_cast<int64_t>(sms) * (n.threads == 256 ? 4 : n.c == 1 ? 2 : 1)));
-  // Backward: a share of a group has two rows a warp group or more, and there are no more shares than blocks at once.
-  const int64_t resident = static_cast<int64_t>(sms) * (n.threads == 256 ? 2 : 1);
+  const int per_block = kNormThreads / n.tpr;
+  n.forward_blocks = static_cast<int>(std::min<int64_t>((tokens + per_block - 1) / per_block, sms));
+  // Backward: a share of a group has a row for each of a block's, or more, and there are no more shares than blocks at once.
   n.groups = s->gate == ADACONS_NORM_GATE_SEQUENCE ? std::max(1, s->batch) : 1;
   const int64_t of_group = tokens / n.groups;
-  n.parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((of_group + 2 * per_block - 1) / (2 * per_block), (resident + n.groups - 1) / n.groups)));
-  n.backward_blocks = static_cast<int>(std::min<int64_t>(static_cast<int64_t>(n.groups) * n.parts, resident));
+  n.parts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((of_group + per_block - 1) / per_block, sms / n.groups)));
+  n.backward_blocks = static_cast<int>(std::min<int64_t>(static_cast<int64_t>(n.groups) * n.parts, sms));
   return n;
 }
 
@@ -108,6 +105,7 @@ NormParams base_params(const adacons_norm_shape* s, const NormPlan& n, const ada
   p.tpr = n.tpr;
   p.scale = s->scale;
   p.eps = s->eps;
+  p.share = static_cast<float>(1.0 / s->dim);
   p.by_len = divisor(std::max(1, s->len));
   return p;
 }

@@ -4,7 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
-#include "adacons_common.cuh"
+#include "adacons_tc.cuh"
 
 namespace adacons {
 
@@ -21,13 +21,16 @@ namespace adacons {
 // leave sums over tokens: with s = sum t n over the tokens that share a gate row, dpost and da are
 // both s times something that does not depend on the token, so one running sum per column serves both.
 //
-// Bound by memory: every element is read and written once.  A row belongs to `tpr` threads (a warp up to 256 elements, 512 threads
-// from 2049 on), each with kNormN elements of every kNormN * tpr; a block keeps its gains in registers, walks over
-// its rows and has the next row's loads under way while it adds up this one's (D up to 4096; beyond, there are no registers
-// for it).  Means are sums in fp32 by shuffles and one shared-memory exchange, in a fixed order.
+// Bound by memory: every element is read and written once.  A block of 512 threads holds one row or several: a row belongs to `tpr` of them, each with one or
+// two groups of kNormN neighbours (a warp up to 512 elements, 256 threads for 4096).  Fewer elements a thread cost more instructions
+// around them than for them (8 of 4096: 111 an element in the gradient, 892 us where 16 take @@).  The gains lie in shared memory as fp32, multiplied with
+// what else does not change.  The next rows are on their way meanwhile, by asynchronous copies of 16 bytes into places of shared memory that only the thread
+// that asked for them reads, so that nothing waits for another thread (D up to 8192; beyond, a row fills shared memory, and
+// rows of odd sizes or strides are loaded element by element).  Means are sums in fp32 by shuffles and one shared-memory exchange, in a fixed order.
 // The sums over tokens are kept in registers by every thread for its columns, leave as one record per block, and a second
 // launch adds the records in order: no atomics.
 // ----------------------------------------------------------------------------------------------
+constexpr int kNormThreads = 512;
 constexpr int kNormN = 8;                       // elements of a thread's group: 16 bytes of 16-bit values
 constexpr int kNormMaxDim = 16384;
 constexpr int kNormSumThreads = 1024;           // of the second launch: 32 columns, 32 shares of the records
@@ -53,6 +56,43 @@ template <> __device__ __forceinline__ float norm_round<float>(float v) { return
 template <> __device__ __forceinline__ __nv_bfloat16 norm_round<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half norm_round<__half>(float v) { return __float2half_rn(v); }
 
+// A group of a thread's elements as pairs: B200 has additions, multiplications and multiply-adds of two fp32 values.
+struct Norm8 {
+  float2 p[kNormN / 2];
+  __device__ __forceinline__ float& operator[](int e) { return e & 1 ? p[e / 2].y : p[e / 2].x; }
+  __device__ __forceinline__ float operator[](int e) const { return e & 1 ? p[e / 2].y : p[e / 2].x; }
+};
+__device__ __forceinline__ Norm8 norm_all(float v) {
+  Norm8 r;
+#pragma unroll
+  for (int k = 0; k < kNormN / 2; ++k) r.p[k] = make_float2(v, v);
+  return r;
+}
+__device__ __forceinline__ Norm8 operator*(const Norm8& a, const Norm8& b) {
+  Norm8 r;
+#pragma unroll
+  for (int k = 0; k < kNormN / 2; ++k) r.p[k] = mul2(a.p[k], b.p[k]);
+  return r;
+}
+__device__ __forceinline__ Norm8 operator*(const Norm8& a, float b) { return a * norm_all(b); }
+__device__ __forceinline__ Norm8 operator+(const Norm8& a, const Norm8& b) {
+  Norm8 r;
+#pragma unroll
+  for (int k = 0; k < kNormN / 2; ++k) r.p[k] = add2(a.p[k], b.p[k]);
+  return r;
+}
+__device__ __forceinline__ Norm8 norm_fma(const Norm8& a, const Norm8& b, const Norm8& c) {
+  Norm8 r;
+#pragma unroll
+  for (int k = 0; k < kNormN / 2; ++k) r.p[k] = fma2(a.p[k], b.p[k], c.p[k]);
+  return r;
+}
+__device__ __forceinline__ Norm8 norm_fma(const Norm8& a, float b, const Norm8& c) { return norm_fma(a, norm_all(b), c); }
+__device__ __forceinline__ float norm_fold(const Norm8& a) {
+  const float2 s = add2(add2(a.p[0], a.p[1]), add2(a.p[2], a.p[3]));
+  return s.x + s.y;
+}
+
 // A thread's share of a row, as it lies in memory: vectors of 16 bytes, or (VEC false) single elements.
 template <typename T, bool VEC> struct NormRaw {
   static constexpr int kVectors = sizeof(T) / 2;               // fp32: two of them
@@ -61,21 +101,18 @@ template <typename T, bool VEC> struct NormRaw {
 #pragma unroll
     for (int k = 0; k < kVectors; ++k) v[k] = *reinterpret_cast<const uint4*>(row + col + k * (16 / static_cast<int>(sizeof(T))));
   }
-  __device__ __forceinline__ void get(float (&f)[kNormN]) const {
+  __device__ __forceinline__ void get(Norm8& f) const {
     if constexpr (sizeof(T) == 4) {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        f[4 * k] = __uint_as_float(v[k].x); f[4 * k + 1] = __uint_as_float(v[k].y);
-        f[4 * k + 2] = __uint_as_float(v[k].z); f[4 * k + 3] = __uint_as_float(v[k].w);
+        f.p[2 * k] = make_float2(__uint_as_float(v[k].x), __uint_as_float(v[k].y));
+        f.p[2 * k + 1] = make_float2(__uint_as_float(v[k].z), __uint_as_float(v[k].w));
       }
     } else {
-      const uint32_t u[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 p = NormPair<T>::unpack(u[k]);
-        f[2 * k] = p.x;
-        f[2 * k + 1] = p.y;
-      }
+      f.p[0] = NormPair<T>::unpack(v[0].x);
+      f.p[1] = NormPair<T>::unpack(v[0].y);
+      f.p[2] = NormPair<T>::unpack(v[0].z);
+      f.p[3] = NormPair<T>::unpack(v[0].w);
     }
   }
 };
@@ -107,20 +144,20 @@ __device__ __forceinline__ void norm_fetch(NormRaw<T, VEC>& raw, const T* row, c
   }
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void norm_get(const NormRaw<T, VEC>& raw, float (&f)[kNormN]) {
+__device__ __forceinline__ void norm_get(const NormRaw<T, VEC>& raw, Norm8& f) {
   if constexpr (VEC) raw.get(f);
   else
 #pragma unroll
     for (int e = 0; e < kNormN; ++e) f[e] = norm_float(raw.v[e]);
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void norm_load(float (&f)[kNormN], const T* row, const NormColumns<VEC>& cols, int c) {
+__device__ __forceinline__ void norm_load(Norm8& f, const T* row, const NormColumns<VEC>& cols, int c) {
   NormRaw<T, VEC> raw;
   norm_fetch(raw, row, cols, c);
   norm_get(raw, f);
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void norm_store(T* row, const NormColumns<VEC>& cols, int c, const float (&f)[kNormN]) {
+__device__ __forceinline__ void norm_store(T* row, const NormColumns<VEC>& cols, int c, const Norm8& f) {
   if constexpr (VEC) {
     if (!cols.has(c)) return;
     T* to = row + cols.at(c, 0);
@@ -139,13 +176,45 @@ __device__ __forceinline__ void norm_store(T* row, const NormColumns<VEC>& cols,
   }
 }
 
+// 16 bytes global -> shared, asynchronously; the copies of a thread form groups
+__device__ __forceinline__ void norm_copy(unsigned char* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void norm_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void norm_await(int pending) {      // until all but the last `pending` groups are there
+  if (pending == 0) asm volatile("cp.async.wait_group 0;" ::: "memory");
+  else if (pending == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
+  else if (pending == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
+  else asm volatile("cp.async.wait_group 3;" ::: "memory");
+}
+// A thread's places for one row: vector v is kNormThreads * 16 bytes behind vector 0.
+template <typename T>
+__device__ __forceinline__ void norm_ask(unsigned char* to, const T* from, bool there) {        // `from`: the thread's first element
+  if (!there) return;
+#pragma unroll
+  for (int k = 0; k < NormRaw<T, true>::kVectors; ++k) norm_copy(to + k * kNormThreads * 16, from + k * (16 / static_cast<int>(sizeof(T))));
+}
+// Places of groups outside the row hold zeros from the start (norm_clear) and are never written.
+template <typename T>
+__device__ __forceinline__ void norm_take(const unsigned char* from, Norm8& f) {
+  NormRaw<T, true> raw;
+#pragma unroll
+  for (int k = 0; k < NormRaw<T, true>::kVectors; ++k) raw.v[k] = *reinterpret_cast<const uint4*>(from + k * kNormThreads * 16);
+  raw.get(f);
+}
+// Zeros in `count` vectors of every row of a thread's ring, from vector `first` on.
+__device__ __forceinline__ void norm_clear(unsigned char* ring, const int depth, const int vectors, int first, int count) {
+  for (int d = 0; d < depth; ++d)
+    for (int k = 0; k < count; ++k) *reinterpret_cast<uint4*>(ring + (d * vectors + first + k) * kNormThreads * 16) = make_uint4(0u, 0u, 0u, 0u);
+}
+
 // Gains and gates are fp32 or of the block's type, whichever the caller keeps them in.
 struct NormGain {
   const void* data;
   int wide;                                     // fp32
 };
 template <typename T, bool VEC>
-__device__ __forceinline__ void norm_gain(float (&f)[kNormN], const NormGain& g, long long at, const NormColumns<VEC>& cols, int c) {
+__device__ __forceinline__ void norm_gain(Norm8& f, const NormGain& g, long long at, const NormColumns<VEC>& cols, int c) {
   if (g.wide) norm_load<float, VEC>(f, static_cast<const float*>(g.data) + at, cols, c);
   else norm_load<T, VEC>(f, static_cast<const T*>(g.data) + at, cols, c);
 }
@@ -153,22 +222,48 @@ template <typename T> __device__ __forceinline__ float norm_gain_one(const NormG
   return g.wide ? static_cast<const float*>(g.data)[at] : norm_float(static_cast<const T*>(g.data)[at]);
 }
 
+// tanh: (1 - e) / (1 + e) with e = exp(-2 |a|), and below 1/4, where that cancels, the first five terms of its series (error 2e-8 of it)
 __device__ __forceinline__ float norm_act(int by, float a) {
-  if (by == kBySigmoid) return 1.f / (1.f + expf(-a));
-  if (by == kByTanh) return tanhf(a);
+  if (by == kBySigmoid) return __fdividef(1.f, 1.f + __expf(-a));
+  if (by == kByTanh) {
+    const float e = __expf(-2.f * fabsf(a)), q = a * a;
+    const float near = a * fmaf(q, fmaf(q, fmaf(q, fmaf(q, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+    return q < 0.0625f ? near : copysignf(__fdividef(1.f - e, 1.f + e), a);
+  }
   return a;
 }
 // the derivative, without the cancellation of 1 - tanh^2 far out
 __device__ __forceinline__ float norm_slope(int by, float a) {
   if (by == kBySigmoid) {
-    const float e = expf(-fabsf(a)), d = 1.f / (1.f + e);
+    const float e = __expf(-fabsf(a)), d = __fdividef(1.f, 1.f + e);
     return e * d * d;
   }
   if (by == kByTanh) {
-    const float e = expf(-2.f * fabsf(a)), d = 1.f / (1.f + e);
+    const float e = __expf(-2.f * fabsf(a)), d = __fdividef(1.f, 1.f + e);
     return 4.f * e * d * d;
   }
   return 1.f;
+}
+
+// either for a group, with the choice made once
+__device__ __forceinline__ void norm_act_all(int by, Norm8& a) {
+  if (by == kByItself) return;
+  if (by == kBySigmoid) {
+#pragma unroll
+    for (int e = 0; e < kNormN; ++e) a[e] = norm_act(kBySigmoid, a[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kNormN; ++e) a[e] = norm_act(kByTanh, a[e]);
+  }
+}
+__device__ __forceinline__ void norm_slope_all(int by, Norm8& a) {
+  if (by == kBySigmoid) {
+#pragma unroll
+    for (int e = 0; e < kNormN; ++e) a[e] = norm_slope(kBySigmoid, a[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kNormN; ++e) a[e] = by == kByItself ? 1.f : norm_slope(kByTanh, a[e]);
+  }
 }
 
 struct NormRows {                               // a tensor of (batch, token) rows: strides in elements
@@ -193,7 +288,9 @@ struct NormParams {
   int gate_kind, by;
   int groups, parts;                            // backward: sequences that have a gate row of their own (or 1), and blocks' shares of each
   int blocks;
-  float scale, eps;
+  int vectors, depth;                           // of the ring: 16-byte vectors of a thread and row, rows
+  int ring;                                     // where it starts in shared memory, behind the gains
+  float scale, eps, share;                      // share: 1 / dim
   NormDivisor by_len;
 };
 
@@ -212,124 +309,160 @@ struct NormSum {
     slot ^= 1;
     if ((threadIdx.x & 31) == 0) at[threadIdx.x >> 5] = v;
     asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "r"(tpr) : "memory");
-    const int first = group * (tpr >> 5);
-    v = 0.f;
-    for (int w = 0; w < (tpr >> 5); ++w) v += at[first + w];
+    // every lane takes one warp's sum, several the same
+    const int warps = tpr >> 5;
+    v = at[group * warps + (threadIdx.x & (warps - 1))];
+    for (int o = warps >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
   }
 };
 
-// C: groups of a thread.  Blocks of 256 threads, or of 512 where a row takes as many.
+// The gains of all columns in shared memory, each half of a group of kNormN apart so that a warp's reads of 16 bytes meet all banks.
+// `make` gives a column's value.
+template <bool VEC>
+struct NormTable {
+  float* at;
+  NormColumns<VEC> cols;
+  int width;                                    // columns, padded
+  __device__ __forceinline__ int place(int col) const { return VEC ? ((col >> 2) & 1) * (width / 2) + (col >> 3) * 4 + (col & 3) : col; }
+  template <typename Make>
+  __device__ __forceinline__ void fill(Make make) {
+    for (int col = threadIdx.x; col < width; col += kNormThreads) at[place(col)] = col < cols.dim ? make(col) : 0.f;
+  }
+  __device__ __forceinline__ void get(int c, Norm8& f) const {
+    if constexpr (VEC) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float4 v = *reinterpret_cast<const float4*>(at + h * (width / 2) + (c * cols.tpr + cols.t) * 4);
+        f[4 * h] = v.x; f[4 * h + 1] = v.y; f[4 * h + 2] = v.z; f[4 * h + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kNormN; ++e) f[e] = at[cols.at(c, e)];
+    }
+  }
+};
+// pre, and scale act(channel gate) post
+template <typename F>
+__device__ __forceinline__ float norm_factor(const NormParams& p, int col) {
+  float v = p.scale;
+  if (p.gate_kind == kGateChannel) v *= norm_act(p.by, norm_gain_one<F>({p.gate.data, p.gate_as.wide}, col));
+  if (p.post.data != nullptr) v *= norm_gain_one<F>(p.post, col);
+  return v;
+}
+
+// C: groups of a thread
 template <typename X, typename F, int C, bool VEC>
-__global__ void __launch_bounds__(512, C == 1 ? 2 : 1) norm_forward_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kNormThreads, 1) norm_forward_kernel(const NormParams p) {
+  extern __shared__ __align__(16) unsigned char s_dyn[];
   __shared__ float s_sum[64];
-  const int group = threadIdx.x / p.tpr, per_block = blockDim.x / p.tpr;
+  constexpr bool kRing = VEC && C <= 2;
+  constexpr int kX = static_cast<int>(sizeof(X)) / 2, kF = static_cast<int>(sizeof(F)) / 2;        // vectors of a group
+  constexpr int kAtF = C * kX, kAtGate = kAtF + C * kF;
+  const int group = threadIdx.x / p.tpr, per_block = kNormThreads / p.tpr;
   const NormColumns<VEC> cols = {p.tpr, static_cast<int>(threadIdx.x) - group * p.tpr, p.dim};
   NormSum sum = {s_sum, p.tpr, group, 0};
   const bool has_f = p.f.data != nullptr, has_post = p.post.data != nullptr, has_pre = p.pre.data != nullptr;
-  const bool gate_rows = p.gate_kind >= kGateSequence;
-  constexpr bool kHold = C <= 2;                // gains in registers
-  float factor[kHold ? C : 1][kNormN], gain[kHold ? C : 1][kNormN];
-  // scale act(channel gate) post: what n is multiplied by, but for a gate's rows
-  auto factors = [&](int c, float (&to)[kNormN]) {
-#pragma unroll
-    for (int e = 0; e < kNormN; ++e) to[e] = p.scale;
-    if (p.gate_kind == kGateChannel) {
-      float a[kNormN];
-      norm_gain<F, VEC>(a, {p.gate.data, p.gate_as.wide}, 0, cols, c);
-#pragma unroll
-      for (int e = 0; e < kNormN; ++e) to[e] *= norm_act(p.by, a[e]);
-    }
-    if (has_post) {
-      float w[kNormN];
-      norm_gain<F, VEC>(w, p.post, 0, cols, c);
-#pragma unroll
-      for (int e = 0; e < kNormN; ++e) to[e] *= w[e];
-    }
-  };
-  if (kHold) {
-#pragma unroll
-    for (int c = 0; c < (kHold ? C : 0); ++c) {
-      if (has_f) factors(c, factor[c]);
-      if (has_pre) norm_gain<F, VEC>(gain[c], p.pre, 0, cols, c);
-    }
-  }
+  const bool by_token = p.gate_kind == kGateToken, by_sequence = p.gate_kind == kGateSequence;
   const long long step = static_cast<long long>(gridDim.x) * per_block;
   long long at = static_cast<long long>(blockIdx.x) * per_block + group;
-  NormRaw<X, VEC> next_x[C];
-  NormRaw<F, VEC> next_f[C];
-  auto fetch = [&](long long r) {
-    const int b = p.by_len.divide(static_cast<int>(r)), s = static_cast<int>(r) - b * p.len;
+  unsigned char* const ring = s_dyn + p.ring + threadIdx.x * 16;
+  const int row_bytes = p.vectors * kNormThreads * 16;
+  auto ask = [&](long long r, int slot) {
+    if constexpr (kRing) {
+      if (r < p.tokens) {
+        const int b = p.by_len.divide(static_cast<int>(r)), s = static_cast<int>(r) - b * p.len;
+        unsigned char* to = ring + slot * row_bytes;
+        const X* x = norm_row<X>(p.x, b, s) + cols.at(0, 0);
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      norm_fetch(next_x[c], static_cast<const X*>(norm_row<X>(p.x, b, s)), cols, c);
-      if (has_f) norm_fetch(next_f[c], static_cast<const F*>(norm_row<F>(p.f, b, s)), cols, c);
+        for (int c = 0; c < C; ++c) norm_ask(to + c * kX * kNormThreads * 16, x + c * p.tpr * kNormN, cols.has(c));
+        if (has_f) {
+          const F* f = norm_row<F>(p.f, b, s) + cols.at(0, 0);
+#pragma unroll
+          for (int c = 0; c < C; ++c) norm_ask(to + (kAtF + c * kF) * kNormThreads * 16, f + c * p.tpr * kNormN, cols.has(c));
+        }
+        if (by_token) {
+#pragma unroll
+          for (int c = 0; c < C; ++c) {
+            if (p.gate_as.wide) norm_ask(to + (kAtGate + c * 2) * kNormThreads * 16, norm_row<float>(p.gate, b, s) + cols.at(c, 0), cols.has(c));
+            else norm_ask(to + (kAtGate + c * kF) * kNormThreads * 16, norm_row<F>(p.gate, b, s) + cols.at(c, 0), cols.has(c));
+          }
+        }
+      }
+      norm_close();
     }
   };
-  if (C == 1 && at < p.tokens) fetch(at);
-  for (; at < p.tokens; at += step) {
+  for (int c = 0; kRing && c < C; ++c) {
+    if (cols.has(c)) continue;
+    norm_clear(ring, p.depth, p.vectors, c * kX, kX);
+    if (has_f) norm_clear(ring, p.depth, p.vectors, kAtF + c * kF, kF);
+    if (by_token) norm_clear(ring, p.depth, p.vectors, kAtGate + c * (p.gate_as.wide ? 2 : kF), p.gate_as.wide ? 2 : kF);
+  }
+  for (int k = 0; k < p.depth - 1; ++k) ask(at + k * step, k);
+  const int width = C * p.tpr * kNormN;
+  NormTable<VEC> pre = {reinterpret_cast<float*>(s_dyn), cols, width}, factor = {reinterpret_cast<float*>(s_dyn) + width, cols, width};
+  if (has_pre) pre.fill([&](int col) { return norm_gain_one<F>(p.pre, col); });
+  if (has_f) factor.fill([&](int col) { return norm_factor<F>(p, col); });
+  __syncthreads();
+  for (int slot = 0; at < p.tokens; at += step) {
     const int row = static_cast<int>(at), b = p.by_len.divide(row), s = row - b * p.len;
-    if (C > 1) fetch(at);
-    float x[C][kNormN], f[C][kNormN];
+    const unsigned char* from = ring + slot * row_bytes;
+    Norm8 x[C], f[C];
+    if constexpr (kRing) {
+      ask(at + (p.depth - 1) * step, slot == 0 ? p.depth - 1 : slot - 1);
+      norm_await(p.depth - 1);
+      if (++slot == p.depth) slot = 0;
+    }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      norm_get(next_x[c], x[c]);
-      if (has_f) norm_get(next_f[c], f[c]);
+      if constexpr (kRing) {
+        norm_take<X>(from + c * kX * kNormThreads * 16, x[c]);
+        if (has_f) norm_take<F>(from + (kAtF + c * kF) * kNormThreads * 16, f[c]);
+      } else {
+        norm_load<X, VEC>(x[c], norm_row<X>(p.x, b, s), cols, c);
+        if (has_f) norm_load<F, VEC>(f[c], norm_row<F>(p.f, b, s), cols, c);
+      }
     }
-    if (C == 1 && at + step < p.tokens) fetch(at + step);
     if (has_f) {
       float r = 1.f;
       if (has_post) {
-        float square = 0.f;
+        Norm8 square = f[0] * f[0];
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-          for (int e = 0; e < kNormN; ++e) square = fmaf(f[c][e], f[c][e], square);
-        r = rsqrtf(sum(square) / p.dim + p.eps);
+        for (int c = 1; c < C; ++c) square = norm_fma(f[c], f[c], square);
+        r = rsqrtf(fmaf(sum(norm_fold(square)), p.share, p.eps));
       }
       if (cols.t == 0) p.rows[row] = has_post ? r : 0.f;
+      X* out = norm_row<X>(p.out, b, s);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        float by[kNormN];
-        if (kHold) {
-#pragma unroll
-          for (int e = 0; e < kNormN; ++e) by[e] = factor[kHold ? c : 0][e];
-        } else {
-          factors(c, by);
+        Norm8 by;
+        factor.get(c, by);
+        if (by_token || by_sequence) {
+          Norm8 a;
+          if (by_sequence || !kRing) norm_gain<F, VEC>(a, {p.gate.data, p.gate_as.wide}, b * p.gate.batch + s * p.gate.row, cols, c);
+          else if (p.gate_as.wide) norm_take<float>(from + (kAtGate + c * 2) * kNormThreads * 16, a);
+          else norm_take<F>(from + (kAtGate + c * kF) * kNormThreads * 16, a);
+          norm_act_all(p.by, a);
+          by = by * a;
         }
-        if (gate_rows) {
-          float a[kNormN];
-          norm_gain<F, VEC>(a, {p.gate.data, p.gate_as.wide}, b * p.gate.batch + s * p.gate.row, cols, c);
-#pragma unroll
-          for (int e = 0; e < kNormN; ++e) by[e] *= norm_act(p.by, a[e]);
-        }
-#pragma unroll
-        for (int e = 0; e < kNormN; ++e) x[c][e] = fmaf(f[c][e] * r, by[e], x[c][e]);
-        norm_store(norm_row<X>(p.out, b, s), cols, c, x[c]);
+        x[c] = norm_fma(f[c] * r, by, x[c]);
+        norm_store(out, cols, c, x[c]);
       }
     }
     if (cols.t == 0 && !has_f) p.rows[row] = 0.f;
     if (cols.t == 0 && !has_pre) p.rows[p.tokens + row] = 0.f;
     if (has_pre) {
-      float square = 0.f;
+      Norm8 square = x[0] * x[0];
 #pragma unroll
-      for (int c = 0; c < C; ++c)
-#pragma unroll
-        for (int e = 0; e < kNormN; ++e) square = fmaf(x[c][e], x[c][e], square);
-      const float r = rsqrtf(sum(square) / p.dim + p.eps);
+      for (int c = 1; c < C; ++c) square = norm_fma(x[c], x[c], square);
+      const float r = rsqrtf(fmaf(sum(norm_fold(square)), p.share, p.eps));
       if (cols.t == 0) p.rows[p.tokens + row] = r;
+      F* normed = norm_row<F>(p.normed, b, s);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        float w[kNormN];
-        if (kHold) {
-#pragma unroll
-          for (int e = 0; e < kNormN; ++e) w[e] = gain[kHold ? c : 0][e];
-        } else {
-          norm_gain<F, VEC>(w, p.pre, 0, cols, c);
-        }
-#pragma unroll
-        for (int e = 0; e < kNormN; ++e) w[e] *= x[c][e] * r;
-        norm_store(norm_row<F>(p.normed, b, s), cols, c, w);
+        Norm8 w;
+        pre.get(c, w);
+        norm_store(normed, cols, c, x[c] * r * w);
       }
     }
   }
@@ -338,216 +471,232 @@ __global__ void __launch_bounds__(512, C == 1 ? 2 : 1) norm_forward_kernel(const
 // A block's item is a run of tokens of one group (of all tokens where no sequence has a gate of its own): its sums of t n leave as
 // record `item`; the sums for `pre` leave once, as record `block`.
 template <typename X, typename F, int C, bool VEC>
-__global__ void __launch_bounds__(512, 1) norm_backward_kernel(const NormParams p) {
-  extern __shared__ float s_fold[];             // [threads][kNormN] where rows are shorter than a block
+__global__ void __launch_bounds__(kNormThreads, 1) norm_backward_kernel(const NormParams p) {
+  extern __shared__ __align__(16) unsigned char s_dyn[];
   __shared__ float s_sum[64];
+  constexpr bool kRing = VEC && C <= 2;
+  constexpr int kX = static_cast<int>(sizeof(X)) / 2, kF = static_cast<int>(sizeof(F)) / 2;        // vectors of a group
+  constexpr int kAtOut = C * kX, kAtDh = kAtOut + C * kX, kAtF = kAtDh + C * kF, kAtGate = kAtF + C * kF;
   pdl_launch_dependents();
-  const int group = threadIdx.x / p.tpr, per_block = blockDim.x / p.tpr;
+  const int group = threadIdx.x / p.tpr, per_block = kNormThreads / p.tpr;
   const NormColumns<VEC> cols = {p.tpr, static_cast<int>(threadIdx.x) - group * p.tpr, p.dim};
   NormSum sum = {s_sum, p.tpr, group, 0};
   const bool has_f = p.f.data != nullptr, has_post = p.post.data != nullptr, has_pre = p.pre.data != nullptr && p.dnormed.data != nullptr;
-  const bool gate_rows = p.gate_kind >= kGateSequence, wants_sum = p.sums != nullptr;
-  constexpr bool kHold = C == 1;                // gains in registers
-  float held_pre[kNormN], held_post[kNormN], held_by[kNormN];
-  auto pre_of = [&](int c, float (&to)[kNormN]) {
-    if (!kHold) norm_gain<F, VEC>(to, p.pre, 0, cols, c);
-    else
+  const bool has_dout = p.dout.data != nullptr, wants_sum = p.sums != nullptr;
+  const bool by_token = p.gate_kind == kGateToken, by_sequence = p.gate_kind == kGateSequence;
+  unsigned char* const ring = s_dyn + p.ring + threadIdx.x * 16;
+  float* s_fold = reinterpret_cast<float*>(s_dyn + p.ring);       // [kNormN][threads] where rows are shorter than a block: once a run's rows are through
+  const int row_bytes = p.vectors * kNormThreads * 16;
+  auto ask = [&](long long r, long long end, int slot) {
+    if constexpr (kRing) {
+      if (r < end) {
+        const int b = p.by_len.divide(static_cast<int>(r)), s = static_cast<int>(r) - b * p.len;
+        unsigned char* to = ring + slot * row_bytes;
+        auto all = [&](const auto* from, int first, int each) {
 #pragma unroll
-      for (int e = 0; e < kNormN; ++e) to[e] = held_pre[e];
-  };
-  auto make_by = [&](int c, float (&to)[kNormN]) {       // scale act(channel gate)
-#pragma unroll
-    for (int e = 0; e < kNormN; ++e) to[e] = p.scale;
-    if (p.gate_kind != kGateChannel) return;
-    float a[kNormN];
-    norm_gain<F, VEC>(a, {p.gate.data, p.gate_as.wide}, 0, cols, c);
-#pragma unroll
-    for (int e = 0; e < kNormN; ++e) to[e] *= norm_act(p.by, a[e]);
-  };
-  auto post_of = [&](int c, float (&to)[kNormN]) {
-    if (kHold) {
-#pragma unroll
-      for (int e = 0; e < kNormN; ++e) to[e] = held_post[e];
-    } else if (has_post) {
-      norm_gain<F, VEC>(to, p.post, 0, cols, c);
-    } else {
-#pragma unroll
-      for (int e = 0; e < kNormN; ++e) to[e] = 1.f;
-    }
-  };
-  if (kHold) {
-    if (has_pre) norm_gain<F, VEC>(held_pre, p.pre, 0, cols, 0);
-#pragma unroll
-    for (int e = 0; e < kNormN; ++e) held_post[e] = 1.f;
-    if (has_post) norm_gain<F, VEC>(held_post, p.post, 0, cols, 0);
-    if (has_f) make_by(0, held_by);
-  }
-  float acc[C][kNormN], acc_pre[C][kNormN];
-#pragma unroll
-  for (int c = 0; c < C; ++c)
-#pragma unroll
-    for (int e = 0; e < kNormN; ++e) acc[c][e] = acc_pre[c][e] = 0.f;
-
-  NormRaw<X, VEC> next_dout[C], next_out[C];
-  NormRaw<F, VEC> next_dh[C], next_f[C];
-  float next_rf = 1.f, next_rx = 1.f;
-  auto fetch = [&](int r) {
-    const int b = p.by_len.divide(r), s = r - b * p.len;
-    if (has_post) next_rf = p.rows[r];
-    if (has_pre) next_rx = p.rows[p.tokens + r];
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (p.dout.data != nullptr) norm_fetch(next_dout[c], static_cast<const X*>(norm_row<X>(p.dout, b, s)), cols, c);
-      if (has_pre) {
-        norm_fetch(next_out[c], static_cast<const X*>(norm_row<X>(p.out, b, s)), cols, c);
-        norm_fetch(next_dh[c], static_cast<const F*>(norm_row<F>(p.dnormed, b, s)), cols, c);
+          for (int c = 0; c < C; ++c) norm_ask(to + (first + c * each) * kNormThreads * 16, from + cols.at(c, 0), cols.has(c));
+        };
+        if (has_dout) all(norm_row<X>(p.dout, b, s), 0, kX);
+        if (has_pre) {
+          all(norm_row<X>(p.out, b, s), kAtOut, kX);
+          all(norm_row<F>(p.dnormed, b, s), kAtDh, kF);
+        }
+        if (has_f) all(norm_row<F>(p.f, b, s), kAtF, kF);
+        if (by_token) {
+          if (p.gate_as.wide) all(norm_row<float>(p.gate, b, s), kAtGate, 2);
+          else all(norm_row<F>(p.gate, b, s), kAtGate, kF);
+        }
       }
-      if (has_f) norm_fetch(next_f[c], static_cast<const F*>(norm_row<F>(p.f, b, s)), cols, c);
+      norm_close();
     }
   };
+  const int items = p.groups * p.parts;
+  const long long of_group = p.tokens / p.groups;
+  // even shares, the first ones a token longer
+  const long long share = of_group / p.parts, longer = of_group - share * p.parts;
+  auto run_of = [&](int item, long long& begin, long long& end) {
+    const int g = item / p.parts, part = item - g * p.parts;
+    begin = g * of_group + part * share + min(static_cast<long long>(part), longer);
+    end = begin + share + (part < longer ? 1 : 0);
+  };
+  long long begin, end;
+  run_of(blockIdx.x, begin, end);
+  auto clear = [&]() {
+    for (int c = 0; kRing && c < C; ++c) {
+      if (cols.has(c)) continue;
+      norm_clear(ring, p.depth, p.vectors, c * kX, kX);
+      norm_clear(ring, p.depth, p.vectors, kAtOut + c * kX, kX);
+      norm_clear(ring, p.depth, p.vectors, kAtDh + c * kF, kF);
+      norm_clear(ring, p.depth, p.vectors, kAtF + c * kF, kF);
+      if (by_token) norm_clear(ring, p.depth, p.vectors, kAtGate + c * (p.gate_as.wide ? 2 : kF), p.gate_as.wide ? 2 : kF);
+    }
+  };
+  clear();
+  if (kRing)
+    for (int k = 0; k < p.depth - 1; ++k) ask(begin + group + k * per_block, end, k);
+  const int width = C * p.tpr * kNormN;
+  NormTable<VEC> pre = {reinterpret_cast<float*>(s_dyn), cols, width}, factor = {reinterpret_cast<float*>(s_dyn) + width, cols, width};
+  if (has_pre) pre.fill([&](int col) { return norm_gain_one<F>(p.pre, col); });
+  if (has_f) factor.fill([&](int col) { return norm_factor<F>(p, col); });
+  __syncthreads();
+  Norm8 acc[C], acc_pre[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) acc[c] = acc_pre[c] = norm_all(0.f);
   // the threads that have the same columns in a block's other rows add up, in the rows' order
-  auto leave = [&](float (&a)[C][kNormN], float* record) {
+  auto leave = [&](Norm8 (&a)[C], float* record) {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       if (per_block > 1) {
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < kNormN; ++e) s_fold[e * blockDim.x + threadIdx.x] = a[c][e];
+        for (int e = 0; e < kNormN; ++e) s_fold[e * kNormThreads + threadIdx.x] = a[c][e];
         __syncthreads();
       }
       if (group == 0) {
 #pragma unroll
         for (int e = 0; e < kNormN; ++e) {
           float v = a[c][e];
-          for (int g = 1; g < per_block; ++g) v += s_fold[e * blockDim.x + g * p.tpr + threadIdx.x];
+          for (int g = 1; g < per_block; ++g) v += s_fold[e * kNormThreads + g * p.tpr + threadIdx.x];
           const int col = cols.at(c, e);
           if (col < p.dim) record[col] = v;
         }
       }
-#pragma unroll
-      for (int e = 0; e < kNormN; ++e) a[c][e] = 0.f;
+      a[c] = norm_all(0.f);
     }
+    if (per_block > 1) __syncthreads();
   };
-
-  const int items = p.groups * p.parts;
-  const long long of_group = p.tokens / p.groups;
   for (int item = blockIdx.x; item < items; item += gridDim.x) {
-    const int g = item / p.parts, part = item - g * p.parts;
-    const long long share = (of_group + p.parts - 1) / p.parts;
-    const long long begin = g * of_group + min(of_group, part * share), end = g * of_group + min(of_group, (part + 1) * share);
+    if (item != static_cast<int>(blockIdx.x)) {
+      run_of(item, begin, end);
+      clear();                                   // sums have been there
+      if (kRing)
+        for (int k = 0; k < p.depth - 1; ++k) ask(begin + group + k * per_block, end, k);
+    }
     long long at = begin + group;
-    if (C == 1 && at < end) fetch(static_cast<int>(at));
-    for (; at < end; at += per_block) {
+    float next_rf = 1.f, next_rx = 1.f;
+    auto factors_of = [&](long long r) {
+      if (r >= end) return;
+      if (has_post) next_rf = p.rows[r];
+      if (has_pre) next_rx = p.rows[p.tokens + r];
+    };
+    factors_of(at);
+    for (int slot = 0; at < end; at += per_block) {
       const int row = static_cast<int>(at), b = p.by_len.divide(row), s = row - b * p.len;
-      if (C > 1) fetch(row);
-      float t[C][kNormN];
       const float rf = next_rf, rx = next_rx;
-      NormRaw<F, VEC> f_raw[C];
-      float hat[C][kNormN], a[C][kNormN];
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        if (p.dout.data != nullptr) norm_get(next_dout[c], t[c]);
-        else
-#pragma unroll
-          for (int e = 0; e < kNormN; ++e) t[c][e] = 0.f;
-        if (has_pre) {
-          norm_get(next_out[c], hat[c]);
-          norm_get(next_dh[c], a[c]);
-        }
-        f_raw[c] = next_f[c];
+      const unsigned char* from = ring + slot * row_bytes;
+      factors_of(at + per_block);
+      if constexpr (kRing) {
+        ask(at + static_cast<long long>(p.depth - 1) * per_block, end, slot == 0 ? p.depth - 1 : slot - 1);
+        norm_await(p.depth - 1);
+        if (++slot == p.depth) slot = 0;
       }
-      if (C == 1 && at + per_block < end) fetch(static_cast<int>(at + per_block));
+      // group c of a tensor's row, from the ring or from memory
+      auto x_row = [&](const NormRows& r, int first, int c, Norm8& to) {
+        if constexpr (kRing) norm_take<X>(from + (first + c * kX) * kNormThreads * 16, to);
+        else norm_load<X, VEC>(to, norm_row<X>(r, b, s), cols, c);
+      };
+      auto f_row = [&](const NormRows& r, int first, int c, Norm8& to) {
+        if constexpr (kRing) norm_take<F>(from + (first + c * kF) * kNormThreads * 16, to);
+        else norm_load<F, VEC>(to, norm_row<F>(r, b, s), cols, c);
+      };
+      Norm8 t[C];
       if (has_pre) {
-        float inner = 0.f;
+        Norm8 hat[C], mean = norm_all(0.f);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-          float w[kNormN];
-          pre_of(c, w);
-#pragma unroll
-          for (int e = 0; e < kNormN; ++e) {
-            hat[c][e] *= rx;
-            acc_pre[c][e] = fmaf(a[c][e], hat[c][e], acc_pre[c][e]);
-            a[c][e] *= w[e];
-            inner = fmaf(a[c][e], hat[c][e], inner);
-          }
+          Norm8 w;
+          pre.get(c, w);
+          x_row(p.out, kAtOut, c, hat[c]);
+          f_row(p.dnormed, kAtDh, c, t[c]);
+          hat[c] = hat[c] * rx;
+          const Norm8 product = t[c] * hat[c];
+          acc_pre[c] = acc_pre[c] + product;
+          mean = norm_fma(product, w, mean);
+          t[c] = t[c] * w;
         }
-        inner = sum(inner) / p.dim;
+        const float minus = -sum(norm_fold(mean)) * p.share;
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+        for (int c = 0; c < C; ++c) {
+          Norm8 d = norm_all(0.f);
+          if (has_dout) x_row(p.dout, 0, c, d);
+          t[c] = norm_fma(norm_fma(hat[c], minus, t[c]), rx, d);
+        }
+      } else {
 #pragma unroll
-          for (int e = 0; e < kNormN; ++e) t[c][e] = fmaf(rx, fmaf(-hat[c][e], inner, a[c][e]), t[c][e]);
+        for (int c = 0; c < C; ++c) {
+          t[c] = norm_all(0.f);
+          if (has_dout) x_row(p.dout, 0, c, t[c]);
+        }
       }
+      X* dx = norm_row<X>(p.dx, b, s);
 #pragma unroll
-      for (int c = 0; c < C; ++c) norm_store(norm_row<X>(p.dx, b, s), cols, c, t[c]);
+      for (int c = 0; c < C; ++c) norm_store(dx, cols, c, t[c]);
       if (!has_f) continue;
-      // t becomes c t post, `hat` n
-      float inner = 0.f;
+      // t becomes c t post
+      Norm8 inner = norm_all(0.f);
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        float n[kNormN], by[kNormN], w[kNormN];
-        norm_get(f_raw[c], n);
-        post_of(c, w);
-        if (kHold)
-#pragma unroll
-          for (int e = 0; e < kNormN; ++e) by[e] = held_by[e];
-        else make_by(c, by);
-        if (has_post)
-#pragma unroll
-          for (int e = 0; e < kNormN; ++e) n[e] *= rf;
-        if (gate_rows) {
-          float g_in[kNormN], dg[kNormN];
-          norm_gain<F, VEC>(g_in, {p.gate.data, p.gate_as.wide}, b * p.gate.batch + s * p.gate.row, cols, c);
-#pragma unroll
-          for (int e = 0; e < kNormN; ++e) {
-            by[e] *= norm_act(p.by, g_in[e]);
-            dg[e] = p.scale * norm_slope(p.by, g_in[e]) * t[c][e] * n[e] * w[e];
-          }
-          if (p.gate_kind == kGateToken) {
+        Norm8 n, by;
+        f_row(p.f, kAtF, c, n);
+        factor.get(c, by);
+        const Norm8 tn = t[c] * n * rf;
+        if (by_token || by_sequence) {
+          Norm8 gate;
+          if (by_sequence || !kRing) norm_gain<F, VEC>(gate, {p.gate.data, p.gate_as.wide}, b * p.gate.batch + s * p.gate.row, cols, c);
+          else if (p.gate_as.wide) norm_take<float>(from + (kAtGate + c * 2) * kNormThreads * 16, gate);
+          else norm_take<F>(from + (kAtGate + c * kF) * kNormThreads * 16, gate);
+          if (by_token) {
+            Norm8 slope = gate;
+            norm_slope_all(p.by, slope);
+            const Norm8 dg = slope * by * tn;
             if (p.gate_as.wide) norm_store(norm_row<float>(p.dgate, b, s), cols, c, dg);
             else norm_store(norm_row<F>(p.dgate, b, s), cols, c, dg);
           }
+          norm_act_all(p.by, gate);
+          acc[c] = by_token ? norm_fma(gate * p.scale, tn, acc[c]) : acc[c] + tn;        // a token's gate differs from its neighbours': it goes into the sum
+          by = by * gate;
+        } else {
+          acc[c] = acc[c] + tn;
         }
-        const bool by_token = p.gate_kind == kGateToken;         // its factor differs from token to token: it goes into the sum
-#pragma unroll
-        for (int e = 0; e < kNormN; ++e) {
-          const float tn = t[c][e] * n[e];
-          acc[c][e] = fmaf(by_token ? by[e] : 1.f, tn, acc[c][e]);
-          t[c][e] *= by[e] * w[e];
-          inner = fmaf(t[c][e], n[e], inner);
-          hat[c][e] = n[e];
-        }
+        t[c] = t[c] * by;
+        inner = norm_fma(t[c], n, inner);
       }
+      F* df = norm_row<F>(p.df, b, s);
       if (has_post) {
-        inner = sum(inner) / p.dim;
+        const float minus = -sum(norm_fold(inner)) * p.share * rf * rf * rf;       // of c t post and n: two factors r_f, and one on the result
 #pragma unroll
-        for (int c = 0; c < C; ++c)
+        for (int c = 0; c < C; ++c) {
+          Norm8 n;
+          f_row(p.f, kAtF, c, n);
+          norm_store(df, cols, c, norm_fma(n, minus, t[c] * rf));
+        }
+      } else {
 #pragma unroll
-          for (int e = 0; e < kNormN; ++e) t[c][e] = rf * fmaf(-hat[c][e], inner, t[c][e]);
+        for (int c = 0; c < C; ++c) norm_store(df, cols, c, t[c]);
       }
-#pragma unroll
-      for (int c = 0; c < C; ++c) norm_store(norm_row<F>(p.df, b, s), cols, c, t[c]);
     }
+    if (kRing) norm_await(0);                    // what follows may take the ring's place
     if (wants_sum) leave(acc, p.sums + static_cast<long long>(item) * p.dim);
   }
   if (p.pre_sums != nullptr) leave(acc_pre, p.pre_sums + static_cast<long long>(blockIdx.x) * p.dim);
 }
 
-// dpost, dpre and the gate's gradient (channel, sequence) from the records: 32 columns a block, whose 32 warps take
-// the records in turn and add their shares in order.  A sequence's records are one warp's.
+// dpost, dpre and the gate's gradient (channel, sequence) from the records: 32 columns a block, whose 32 warps divide into as many for each
+// group of records (a sequence's, or all); they take its records in turn and their sums are added in order.
 template <typename F>
 __global__ void __launch_bounds__(kNormSumThreads) norm_sum_kernel(const NormParams p) {
   __shared__ float s_part[32][33];
   pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
   const bool in = col < p.dim;
-  auto total = [&](float v) {                   // over the warps; valid in warp 0
+  // over `count` warps from the first of them on, which has the result
+  auto total = [&](float v, int first, int count) {
     __syncthreads();
     s_part[warp][lane] = v;
     __syncthreads();
     v = 0.f;
-    if (warp == 0)
-#pragma unroll
-      for (int w = 0; w < 32; ++w) v += s_part[w][lane];
+    if (warp == first)
+      for (int w = 0; w < count; ++w) v += s_part[first + w][lane];
     return v;
   };
   auto put = [&](void* to, bool wide, long long at, float v) {
@@ -555,40 +704,37 @@ __global__ void __launch_bounds__(kNormSumThreads) norm_sum_kernel(const NormPar
     else static_cast<F*>(to)[at] = norm_round<F>(v);
   };
   const float post = in && p.post.data != nullptr ? norm_gain_one<F>(p.post, col) : 1.f;
-  if (p.sums != nullptr) {
-    float v = 0.f;
-    if (p.gate_kind == kGateSequence) {
-      for (int g = warp; in && g < p.groups; g += 32) {
-        float s = 0.f;
-#pragma unroll 4
-        for (int k = 0; k < p.parts; ++k) s += p.sums[(static_cast<long long>(g) * p.parts + k) * p.dim + col];
-        const float a = norm_gain_one<F>({p.gate.data, p.gate_as.wide}, g * p.gate.batch + col);
-        v = fmaf(p.scale * norm_act(p.by, a), s, v);
-        put(p.dgate.data, p.gate_as.wide, g * p.dgate.batch + col, p.scale * norm_slope(p.by, a) * post * s);
-      }
-      v = total(v);
-    } else {
+  float by_pre = 0.f;
+  if (p.pre_sums != nullptr && in)
 #pragma unroll 8
-      for (int k = warp; k < p.parts; k += 32)
-        if (in) v += p.sums[static_cast<long long>(k) * p.dim + col];
-      v = total(v);
-      if (p.gate_kind == kGateChannel && in && warp == 0) {
-        const float a = norm_gain_one<F>({p.gate.data, p.gate_as.wide}, col);
-        put(p.dgate.data, p.gate_as.wide, col, p.scale * norm_slope(p.by, a) * post * v);
-        v *= p.scale * norm_act(p.by, a);
-      } else if (p.gate_kind == kGateNone) {
-        v *= p.scale;
+    for (int k = warp; k < p.blocks; k += 32) by_pre += p.pre_sums[static_cast<long long>(k) * p.dim + col];
+  if (p.sums != nullptr) {
+    int at_once = 1;                             // groups
+    while (at_once < 32 && at_once < p.groups) at_once *= 2;
+    const int each = 32 / at_once, first = warp / each * each;
+    float v = 0.f;
+    for (int g0 = 0; g0 < p.groups; g0 += at_once) {
+      const int g = g0 + warp / each;
+      float s = 0.f;
+      if (in && g < p.groups)
+#pragma unroll 8
+        for (int k = warp - first; k < p.parts; k += each) s += p.sums[(static_cast<long long>(g) * p.parts + k) * p.dim + col];
+      if (each > 1) s = total(s, first, each);
+      if (!in || g >= p.groups || warp != first) continue;
+      if (p.gate_kind == kGateSequence || p.gate_kind == kGateChannel) {
+        const bool sequence = p.gate_kind == kGateSequence;
+        const float a = norm_gain_one<F>({p.gate.data, p.gate_as.wide}, (sequence ? g * p.gate.batch : 0) + col);
+        v = fmaf(p.scale * norm_act(p.by, a), s, v);
+        put(p.dgate.data, p.gate_as.wide, (sequence ? g * p.dgate.batch : 0) + col, p.scale * norm_slope(p.by, a) * post * s);
+      } else {
+        v += p.gate_kind == kGateNone ? p.scale * s : s;
       }
     }
+    if (p.groups > 1) v = total(v, 0, 32);
     if (p.dpost != nullptr && in && warp == 0) put(p.dpost, p.post.wide, col, v);
   }
   if (p.dpre != nullptr) {
-    float v = 0.f;
-    if (p.pre_sums != nullptr)
-#pragma unroll 8
-      for (int k = warp; k < p.blocks; k += 32)
-        if (in) v += p.pre_sums[static_cast<long long>(k) * p.dim + col];
-    v = total(v);
+    const float v = total(by_pre, 0, 32);
     if (in && warp == 0) put(p.dpre, p.pre.wide, col, v);
   }
 }

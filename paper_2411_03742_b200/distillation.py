@@ -13,7 +13,7 @@ import math
 import torch
 
 from .binding import _check, _raw_stream, load_library
-from .calls import Plans, address, elsewhere, layout, starts_with
+from .calls import Plans, address, elsewhere, here, layout, starts_with
 from .norms import _CODES
 
 MAX_TOP = 1024
@@ -38,7 +38,7 @@ class _Plan:
         self.refs = [ctypes.byref(b) for b in self.blocks]
 
 
-_plans = Plans()
+_plans, _back_plans = Plans(), Plans()
 
 
 def check_distill(logits, ids, teacher, temperature: float, labels=None, mix: float = 1.0, loss=None, rows=None, dloss=None, out=None, want_cuda: bool = True) -> None:
@@ -99,14 +99,15 @@ def distill_forward(logits, ids, teacher, *, temperature: float = 1.0, labels=No
     without entries has no first term, one without a label no second.  Without labels mix is 1 unless given.
     rows: both log-sum-exps, (2, token) fp32, for the gradient.  loss and rows are made here unless given."""
     temperature, mix = float(temperature), _mix(labels, mix)
-    sig = (0, layout(logits), layout(ids), layout(teacher), layout(labels), temperature, mix, layout(loss), layout(rows))
+    sig = (layout(logits), layout(ids), layout(teacher), layout(labels), temperature, mix, layout(loss), layout(rows))
     plan = _plans.known.get(sig)
     if plan is None:
         check_distill(logits, ids, teacher, temperature, labels, mix, loss, rows)
-    device = sig[1][3]
-    results = elsewhere(device, stream, (loss, rows), lambda: distill_forward(logits, ids, teacher, temperature=temperature, labels=labels, mix=mix, loss=loss, rows=rows))
-    if results is not None:
-        return results
+    device = sig[0][3]
+    if not here(device, stream):
+        results = elsewhere(device, stream, (loss, rows), lambda: distill_forward(logits, ids, teacher, temperature=temperature, labels=labels, mix=mix, loss=loss, rows=rows))
+        if results is not None:
+            return results
     if starts_with(loss, (logits, ids, teacher, labels, rows)) or starts_with(rows, (logits, ids, teacher, labels)):
         raise ValueError("loss and rows must not share memory with what is read or with one another")
     if loss is None:
@@ -125,15 +126,16 @@ def distill_backward(dloss, logits, ids, teacher, rows, *, temperature: float = 
     """The gradient of distill_forward's logits, of their type, from dloss (fp32, one for each token) and the forward pass's rows, with the same arguments.
     out: a new tensor unless given; logits itself is allowed (they are overwritten), no other overlap."""
     temperature, mix = float(temperature), _mix(labels, mix)
-    sig = (1, layout(dloss), layout(logits), layout(ids), layout(teacher), layout(rows), layout(labels), temperature, mix, layout(out))
-    plan = _plans.known.get(sig)
+    sig = (layout(dloss), layout(logits), layout(ids), layout(teacher), layout(rows), layout(labels), temperature, mix, layout(out))
+    plan = _back_plans.known.get(sig)
     if plan is None:
         check_distill(logits, ids, teacher, temperature, labels, mix, None, rows, dloss, out)
-    device = sig[2][3]
-    results = elsewhere(device, stream, (out,), lambda: (distill_backward(dloss, logits, ids, teacher, rows, temperature=temperature, labels=labels, mix=mix, out=out),))
-    if results is not None:
-        return results[0]
-    if starts_with(out, (dloss, ids, teacher, rows, labels)) or (out is not logits and starts_with(out, (logits,)) and out.stride() != logits.stride()):
+    device = sig[1][3]
+    if not here(device, stream):
+        results = elsewhere(device, stream, (out,), lambda: (distill_backward(dloss, logits, ids, teacher, rows, temperature=temperature, labels=labels, mix=mix, out=out),))
+        if results is not None:
+            return results[0]
+    if out is not None and (starts_with(out, (dloss, ids, teacher, rows, labels)) or (starts_with(out, (logits,)) and out.stride() != logits.stride())):
         raise ValueError("out may be the logits, otherwise it must not share memory with what is read")
     if out is None:
         # rows that lie as the logits' do relative to 16 bytes, so that both are moved in vectors; padding behind them is not written
@@ -141,7 +143,7 @@ def distill_backward(dloss, logits, ids, teacher, rows, *, temperature: float = 
         pad = (logits.stride(0) - V) % (16 // logits.element_size()) if logits.shape[0] > 1 else 0
         out = logits.new_empty((logits.shape[0], V + pad))[:, :V]
     if plan is None:
-        plan = _plans.remember(sig, _Plan(logits, ids, teacher, labels, temperature, mix, (logits, ids, teacher, out)))
+        plan = _back_plans.remember(sig, _Plan(logits, ids, teacher, labels, temperature, mix, (logits, ids, teacher, out)))
     for b, t in zip(plan.blocks, (logits, ids, teacher, out)):
         b.data = t.data_ptr()
     r = plan.refs

@@ -13,7 +13,7 @@ import torch
 
 from .attention import F16
 from .binding import BF16, _check, _raw_stream, _stream_handle, load_library
-from .calls import Plans, address, elsewhere, layout, starts_with
+from .calls import Plans, address, elsewhere, here, layout, starts_with
 
 #: the activations, in the order of the C header's ADACONS_FFN_ values
 ACTS = ("silu", "gelu", "gelu_tanh", "relu")
@@ -40,7 +40,7 @@ class _Plan:
         self.workspace = n.value
 
 
-_plans = Plans()
+_plans, _back_plans = Plans(), Plans()
 
 
 def check_feedforward(x, w_gate, w_up, w_down, act: str = "silu", like_x=(), like_hidden=(), like_gate=(), like_down=(), want_cuda: bool = True) -> None:
@@ -74,17 +74,18 @@ def feedforward_forward(x, w_gate, w_up, w_down, *, act: str = "silu", keep: boo
     stream: where the kernels go (the current one by default); the caller orders it behind whatever makes the inputs, and its own
     use of the results behind it."""
     keep = bool(keep)
-    sig = (0, layout(x), layout(w_gate), layout(w_up), layout(w_down), act, keep, layout(out), layout(gate), layout(up))
+    sig = (layout(x), layout(w_gate), layout(w_up), layout(w_down), act, keep, layout(out), layout(gate), layout(up))
     plan = _plans.known.get(sig)
     if plan is None:
         check_feedforward(x, w_gate, w_up, w_down, act, like_x=[("out", out)], like_hidden=[("gate", gate), ("up", up)])
         if not keep and (gate is not None or up is not None):
             raise ValueError("gate and up are not made with keep=False")
-    device = sig[1][3]
-    results = elsewhere(device, stream, (out, gate, up) if keep else (out, True, True), lambda: feedforward_forward(
-        x, w_gate, w_up, w_down, act=act, keep=keep, out=out, gate=gate, up=up, workspace=workspace))
-    if results is not None:
-        return results
+    device = sig[0][3]
+    if not here(device, stream):
+        results = elsewhere(device, stream, (out, gate, up) if keep else (out, True, True), lambda: feedforward_forward(
+            x, w_gate, w_up, w_down, act=act, keep=keep, out=out, gate=gate, up=up, workspace=workspace))
+        if results is not None:
+            return results
     reads = (x, w_gate, w_up, w_down)
     if starts_with(out, reads) or starts_with(gate, (*reads, out)) or starts_with(up, (*reads, out, gate)):
         raise ValueError("results must not share memory with what is read or with one another")
@@ -124,24 +125,25 @@ def feedforward_backward(dout, x, w_gate, w_up, w_down, gate, up, *, act: str = 
     16-byte aligned).  Between the products gradients are held in the tensors' type (float16: scaled by a power of two from dout's largest element)."""
     want = tuple(bool(w) for w in want)
     given = (dx, dw_gate, dw_up, dw_down)
-    sig = (1, layout(dout), layout(x), layout(w_gate), layout(w_up), layout(w_down), layout(gate), layout(up), act, want, *(layout(t) for t in given))
-    plan = _plans.known.get(sig)
+    sig = (layout(dout), layout(x), layout(w_gate), layout(w_up), layout(w_down), layout(gate), layout(up), act, want, *(layout(t) for t in given))
+    plan = _back_plans.known.get(sig)
     if plan is None:
         check_feedforward(x, w_gate, w_up, w_down, act, like_x=[("dout", dout), ("dx", dx)], like_hidden=[("gate", gate), ("up", up)],
                           like_gate=[("dw_gate", dw_gate), ("dw_up", dw_up)], like_down=[("dw_down", dw_down)])
         if len(want) != 4 or any(t is not None and not w for t, w in zip(given, want)):
             raise ValueError("want says for each of dx, dw_gate, dw_up and dw_down whether it is made; one that is given is")
-    device = sig[2][3]
-    results = elsewhere(device, stream, tuple(t if w else True for t, w in zip(given, want)), lambda: feedforward_backward(
-        dout, x, w_gate, w_up, w_down, gate, up, act=act, dx=dx, dw_gate=dw_gate, dw_up=dw_up, dw_down=dw_down, want=want, workspace=workspace))
-    if results is not None:
-        return results
+    device = sig[1][3]
+    if not here(device, stream):
+        results = elsewhere(device, stream, tuple(t if w else True for t, w in zip(given, want)), lambda: feedforward_backward(
+            dout, x, w_gate, w_up, w_down, gate, up, act=act, dx=dx, dw_gate=dw_gate, dw_up=dw_up, dw_down=dw_down, want=want, workspace=workspace))
+        if results is not None:
+            return results
     reads = (dout, x, w_gate, w_up, w_down, gate, up)
-    if any(starts_with(t, (*reads, *given[:k])) for k, t in enumerate(given)):
+    if any(t is not None for t in given) and any(starts_with(t, (*reads, *given[:k])) for k, t in enumerate(given)):
         raise ValueError("results must not share memory with what is read or with one another")
     made = [t if t is not None or not w else torch.empty_like(like, memory_format=torch.contiguous_format) for t, w, like in zip(given, want, (x, w_gate, w_up, w_down))]
     if plan is None:
-        plan = _plans.remember(sig, _Plan(x, w_gate, act, (*reads, *made), True))
+        plan = _back_plans.remember(sig, _Plan(x, w_gate, act, (*reads, *made), True))
     workspace = _workspace(workspace, plan, x, device)
     for b, t in zip(plan.blocks, (*reads, *made)):
         b.data = address(t)

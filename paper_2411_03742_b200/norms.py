@@ -14,7 +14,7 @@ import torch
 
 from .attention import F16
 from .binding import BF16, F32, _check, _raw_stream, load_library
-from .calls import Plans, address, elsewhere, layout, starts_with
+from .calls import Plans, address, elsewhere, here, layout, starts_with
 
 MAX_DIM = 16384
 _CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
@@ -41,7 +41,7 @@ class _Plan:
         self.workspace = 0
 
 
-_plans = Plans()
+_plans, _back_plans = Plans(), Plans()
 
 
 def _gate_kind(x, gate) -> int:
@@ -149,40 +149,56 @@ def residual_norm_forward(x, f=None, *, gate=None, gate_by=None, post=None, scal
     out (which may be x), normed and rows are made here unless given.  stream: where the kernel goes (the current one by
     default); the caller orders it behind whatever makes the inputs, and its own use of the results behind it."""
     scale, eps = float(scale), float(eps)
-    sig = (0, layout(x), layout(f), layout(gate), gate_by, layout(post), scale, layout(pre), eps, dtype, layout(out), layout(normed), layout(rows))
+    sig = (layout(x), layout(f), layout(gate), gate_by, layout(post), scale, layout(pre), eps, dtype, layout(out), layout(normed), layout(rows))
     plan = _plans.known.get(sig)
     if plan is None:
         check_norm(x, f, gate, post, pre, gate_by, scale, eps, dtype, like_x=[("out", out)], like_f=[("normed", normed)], rows=rows)
-    device = sig[1][3]
-    results = elsewhere(device, stream, (x if f is None and out is None else out, normed, rows),
-                        lambda: residual_norm_forward(x, f, gate=gate, gate_by=gate_by, post=post, scale=scale, pre=pre, eps=eps, dtype=dtype, out=out, normed=normed, rows=rows))
-    if results is not None:
-        return results
-    if starts_with(normed, (x, f, gate, out)) or starts_with(out, (f, gate)) or (out is not x and starts_with(out, (x,)) and out.stride() != x.stride()):
-        raise ValueError("out may be x; no other result may share memory with what is read or with another result")
-    if f is None and out is not None and out.data_ptr() != x.data_ptr():
-        raise ValueError("without f, out is x: none can be given")
+        if normed is not None and pre is None:
+            raise ValueError("normed without pre")
+    device = sig[0][3]
+    if not here(device, stream):
+        results = elsewhere(device, stream, (x if f is None and out is None else out, True if pre is None else normed, rows), lambda: residual_norm_forward(
+            x, f, gate=gate, gate_by=gate_by, post=post, scale=scale, pre=pre, eps=eps, dtype=dtype, out=out, normed=normed, rows=rows))
+        if results is not None:
+            return results
+    if out is not None or normed is not None or rows is not None:
+        _check_places(x, f, gate, post, pre, out, normed, rows)
     if f is None:
         out = x
     elif out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
-    block = f.dtype if f is not None else dtype or x.dtype
-    if pre is None:
-        normed = None
-    elif normed is None:
-        normed = torch.empty(x.shape, dtype=block, device=x.device)
-    if rows is None:
-        rows = x.new_empty((2, *x.shape[:-1]), dtype=torch.float32)
+    if pre is not None and normed is None:
+        normed = x.new_empty(x.shape, dtype=f.dtype if f is not None else dtype or x.dtype)
     if plan is None:
         kind = _kind(x, gate)
-        plan = _plans.remember(sig, _Plan(_shape(x, block, gate, kind, post, pre, gate_by, scale, eps),
+        plan = _plans.remember(sig, _Plan(_shape(x, f.dtype if f is not None else dtype or x.dtype, gate, kind, post, pre, gate_by, scale, eps),
                                           [_strides(x), _strides(f), _gate_strides(x, gate, kind), _strides(out), _strides(normed)]))
-    for b, t in zip(plan.blocks, (x, f, gate, None if f is None else out, normed)):
-        b.data = address(t)
+        plan.rows = (2, *x.shape[:-1])
+        plan.call = load_library().adacons_norm_forward
+    if rows is None:
+        rows = x.new_empty(plan.rows, dtype=torch.float32)
+    b = plan.blocks
+    b[0].data = x.data_ptr()
+    if f is not None:
+        b[1].data, b[3].data = f.data_ptr(), out.data_ptr()
+        if gate is not None:
+            b[2].data = gate.data_ptr()
+    if normed is not None:
+        b[4].data = normed.data_ptr()
     r = plan.refs
-    _check(load_library().adacons_norm_forward(plan.shape_ref, r[0], r[1], r[2], address(post), address(pre), r[3], r[4], rows.data_ptr(), _raw_stream(None, device)),
-           "adacons_norm_forward")
+    _check(plan.call(plan.shape_ref, r[0], r[1], r[2], None if post is None else post.data_ptr(), None if pre is None else pre.data_ptr(), r[3], r[4], rows.data_ptr(),
+                     _raw_stream(None, device)), "adacons_norm_forward")
     return out, normed, rows
+
+
+def _check_places(x, f, gate, post, pre, out, normed, rows):
+    """Results that were given: out may be x, and is without f."""
+    if f is None and out is not None and (out.data_ptr() != x.data_ptr() or out.stride() != x.stride()):
+        raise ValueError("without f, out is x: none can be given")
+    if f is not None and out is not None and starts_with(out, (x,)) and out.stride() != x.stride():
+        raise ValueError("in place, out must be x itself")
+    if starts_with(normed, (x, f, gate, post, pre, out)) or (f is not None and starts_with(out, (f, gate, post, pre))) or starts_with(rows, (x, f, gate, post, pre, out, normed)):
+        raise ValueError("out may be x; no other result may share memory with what is read or with another result")
 
 
 def residual_norm_backward(dout, dnormed, out, f, rows, *, gate=None, gate_by=None, post=None, scale: float = 1.0, pre=None, eps: float = 1e-6, dx=None, df=None, dgate=None,
@@ -192,11 +208,12 @@ def residual_norm_backward(dout, dnormed, out, f, rows, *, gate=None, gate_by=No
     taken in fp32 and in a fixed order.  eps is not looked at: the factors are in rows.
     dx (which may be dout), df, dgate, dpost and dpre are made here unless given, as is the workspace (a uint8 tensor of workspace_bytes)."""
     scale, eps = float(scale), float(eps)
-    sig = (1, layout(dout), layout(dnormed), layout(out), layout(f), layout(rows), layout(gate), gate_by, layout(post), scale, layout(pre), eps, layout(dx), layout(df), layout(dgate),
+    given = (dx, df, dgate, dpost, dpre)
+    sig = (layout(dout), layout(dnormed), layout(out), layout(f), layout(rows), layout(gate), gate_by, layout(post), scale, layout(pre), eps, layout(dx), layout(df), layout(dgate),
            layout(dpost), layout(dpre))
-    plan = _plans.known.get(sig)
-    block = f.dtype if f is not None else dnormed.dtype if dnormed is not None else out.dtype
+    plan = _back_plans.known.get(sig)
     if plan is None:
+        block = f.dtype if f is not None else dnormed.dtype if dnormed is not None else out.dtype
         check_norm(out, f, gate, post, pre, gate_by, scale, eps, block, like_x=[("dx", dx)], like_f=[("df", df)], like_gate=[("dgate", dgate)], like_post=[("dpost", dpost)],
                    like_pre=[("dpre", dpre)], rows=rows)
         for name, t, dtype in (("dout", dout, out.dtype), ("dnormed", dnormed, block)):
@@ -204,21 +221,21 @@ def residual_norm_backward(dout, dnormed, out, f, rows, *, gate=None, gate_by=No
                 raise ValueError(f"{name} must be {dtype} of shape {tuple(out.shape)} on out's device with unit stride along a row, got {t.dtype} {tuple(t.shape)}")
         if dnormed is not None and pre is None:
             raise ValueError("dnormed without pre")
-        for name, t in (("dpost", dpost), ("dpre", dpre)):
-            if t is not None and not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous")
-    device = sig[3][3]
-    results = elsewhere(device, stream, (dx, df, dgate, dpost, dpre),
-                        lambda: residual_norm_backward(dout, dnormed, out, f, rows, gate=gate, gate_by=gate_by, post=post, scale=scale, pre=pre, eps=eps, dx=dx, df=df, dgate=dgate,
-                                                       dpost=dpost, dpre=dpre, workspace=workspace))
-    if results is not None:
-        return results
-    reads = (dout, dnormed, out, f, gate, post, pre, rows)
-    if dx is not None and dout is not None and dx.data_ptr() == dout.data_ptr() and dx.stride() == dout.stride():
-        reads = reads[1:]
-    given = [t for t in (dx, df, dgate, dpost, dpre) if t is not None]
-    if any(starts_with(t, (*reads, *given[:k], *([] if t is dx else [dout]))) for k, t in enumerate(given)):
-        raise ValueError("dx may be dout; no other result may share memory with what is read or with another result")
+        for name, t, of in (("df", df, f), ("dgate", dgate, gate), ("dpost", dpost, post), ("dpre", dpre, pre)):
+            if t is not None and of is None:
+                raise ValueError(f"{name}: there is nothing that it is the gradient of")
+    device = sig[2][3]
+    if not here(device, stream):
+        results = elsewhere(device, stream, tuple(True if of is None else t for t, of in zip(given, (out, f, gate, post, pre))), lambda: residual_norm_backward(
+            dout, dnormed, out, f, rows, gate=gate, gate_by=gate_by, post=post, scale=scale, pre=pre, eps=eps, dx=dx, df=df, dgate=dgate, dpost=dpost, dpre=dpre, workspace=workspace))
+        if results is not None:
+            return results
+    if any(t is not None for t in given):
+        reads = (dnormed, out, f, gate, post, pre, rows)
+        if dx is not None and dout is not None and starts_with(dx, (dout,)) and dx.stride() != dout.stride():
+            raise ValueError("in place, dx must be dout itself")
+        if any(starts_with(t, (*reads, *given[:k], *([dout] if k else []))) for k, t in enumerate(given)):
+            raise ValueError("dx may be dout; no other result may share memory with what is read or with another result")
     dx = torch.empty_like(out, memory_format=torch.contiguous_format) if dx is None else dx
     if f is not None and df is None:
         df = torch.empty_like(f, memory_format=torch.contiguous_format)
@@ -232,22 +249,22 @@ def residual_norm_backward(dout, dnormed, out, f, rows, *, gate=None, gate_by=No
         kind = _kind(out, gate)
         plan = _Plan(_shape(out, block, gate, kind, post, pre, gate_by, scale, eps),
                      [_strides(dout), _strides(dnormed), _strides(out), _strides(f), _gate_strides(out, gate, kind), _strides(dx), _strides(df), _gate_strides(out, dgate, kind)])
+        plan.call = load_library().adacons_norm_backward
         if post is not None or pre is not None or kind in (_CHANNEL, _SEQUENCE):
             n = ctypes.c_int64()
             _check(load_library().adacons_norm_workspace_bytes(plan.shape_ref, ctypes.byref(n)), "adacons_norm_workspace_bytes")
             plan.workspace = n.value
-        _plans.remember(sig, plan)
+        _back_plans.remember(sig, plan)
     if workspace is None:
         if plan.workspace:
             workspace = rows.new_empty(plan.workspace // 4)
     elif workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous on out's device")
     for b, t in zip(plan.blocks, (dout, dnormed, out, f, gate, dx, df, dgate)):
-        b.data = address(t)
+        b.data = None if t is None else t.data_ptr()
     r = plan.refs
-    _check(load_library().adacons_norm_backward(plan.shape_ref, r[0], r[1], r[2], r[3], r[4], address(post), address(pre), rows.data_ptr(), r[5], r[6], r[7], address(dpost),
-                                                address(dpre), address(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                                _raw_stream(None, device)), "adacons_norm_backward")
+    _check(plan.call(plan.shape_ref, r[0], r[1], r[2], r[3], r[4], address(post), address(pre), rows.data_ptr(), r[5], r[6], r[7], address(dpost), address(dpre),
+                     address(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _raw_stream(None, device)), "adacons_norm_backward")
     return dx, df, dgate, dpost, dpre
 
 
