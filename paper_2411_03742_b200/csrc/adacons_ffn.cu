@@ -123,26 +123,26 @@ int64_t workspace_bytes(const adacons_ffn_shape* s, bool back) {
 
 struct FfnPlan { int cg, shares; double time; };
 
-// Tiles by pairs of blocks or by lone ones, and how many share one's K: the quickest by a count of cycles.  A stage of half a pair's tile takes the tensor pipe
-// 512 cycles, one of a lone block's 256 but its operands some 500 from L2 beside the SM's other block; a launch costs 6000 cycles from the first operand to the
-// last store, a join 2500.
+// Tiles by pairs of blocks or by lone ones, and how many share one's K: the quickest by a count of cycles.  A stage of half a pair's tile takes 540 cycles where both halves
+// of a tile share the left operand, 720 where pairs have one each; one of a lone block's 1000 (its operands, from L2; 128 tiles of 86 stages: 97,000), two beside one another
+// twice that.  A launch costs 8000 cycles from the first operand to the last store, a join 2500.
 FfnPlan plan_of(const FfnDevice& d, const FfnProblem* q, int n, int columns_by) {
   double work = 0.0;                             // stages of halves
-  int64_t lone_tiles = 0;
+  int64_t lone_tiles = 0, halves = 0;
   int steps = 1;
   for (int k = 0; k < n; ++k) {
     const int all = q[k].steps * q[k].segments, half = 256 / columns_by, lone = 128 / columns_by;
-    work += static_cast<double>((q[k].m + 255) / 256) * ((q[k].n + half - 1) / half) * all;
+    const int64_t of_this = static_cast<int64_t>((q[k].m + 255) / 256) * ((q[k].n + half - 1) / half);
+    halves += of_this;
+    work += static_cast<double>(of_this) * all;
     lone_tiles += static_cast<int64_t>((q[k].m + 127) / 128) * ((q[k].n + lone - 1) / lone);
     steps = std::max(steps, all);
   }
-  // whole halves: the pairs with the most of them
-  FfnPlan best = {2, 1, std::max(std::ceil(work / steps / d.pairs) * steps, work / d.pairs) * 530.0 + 7000.0};
+  FfnPlan best = {2, 1, 8000.0 + (halves <= d.pairs ? steps * 720.0 : std::max(std::ceil(work / steps / d.pairs) * steps, work / d.pairs) * 540.0)};
   for (int shares = 1; shares <= 8; shares *= 2) {
     if (shares > 1 && (steps < 2 * shares || n > 1)) break;
-    const int64_t blocks = lone_tiles * shares, per_sm = (blocks + d.info.sms - 1) / d.info.sms;
-    const double each = (steps + shares - 1) / shares * 500.0;
-    const double time = per_sm * each + ((per_sm + 1) / 2) * (6000.0 + (shares > 1 ? 2500.0 : 0.0));
+    const int64_t per_sm = (lone_tiles * shares + d.info.sms - 1) / d.info.sms;
+    const double time = per_sm * ((steps + shares - 1) / shares) * 1000.0 + ((per_sm + 1) / 2) * (8000.0 + (shares > 1 ? 2500.0 : 0.0));
     if (time < best.time) best = {1, shares, time};
   }
   return best;
@@ -348,7 +348,6 @@ int adacons_ffn_backward(const adacons_ffn_shape* s, const adacons_ffn_matrix* d
   by_x.scaled = peaks != nullptr;
   by_x.out = as_rows(dx, s->dim, s->tokens);
   auto weight = [&](const adacons_ffn_matrix* to, int a, int b, int m, int n, bool scaled) {
-    if (to->data == nullptr) return;
     FfnProblem w = {};
     w.a[0] = a;
     w.b[0] = b;
@@ -364,7 +363,11 @@ int adacons_ffn_backward(const adacons_ffn_shape* s, const adacons_ffn_matrix* d
   weight(dwg, kDg, kX, s->hidden, s->dim, peaks != nullptr);
   weight(dwu, kDu, kX, s->hidden, s->dim, peaks != nullptr);
   weight(dwd, kDy, kH, s->dim, s->hidden, false);
-  const FfnPlan x_plan = plan_of(*d, &by_x, 1, 1), w_plan = weights > 0 ? plan_of(*d, by_w, weights, 1) : x_plan;
+  // whichever are wanted, each comes from the plan for all: the same bits
+  const FfnPlan x_plan = plan_of(*d, &by_x, 1, 1), w_plan = plan_of(*d, by_w, weights, 1);
+  weights = 0;
+  for (int k = 0; k < 3; ++k)
+    if (results[k + 1]->data != nullptr) by_w[weights++] = by_w[k];
   if (has_x && weights > 0 && x_plan.cg == 2 && w_plan.cg == 2) {      // one launch, the longer tiles first
     const bool x_first = by_x.steps * 2 >= by_w[0].steps;
     for (int k = 0; k < weights; ++k) p.problem[k + x_first] = by_w[k];

@@ -195,19 +195,31 @@ int adacons_norm_backward(const adacons_norm_shape* s, const adacons_norm_rows* 
   const bool has_post = has_f && post != nullptr, has_gate = has_f && s->gate != ADACONS_NORM_GATE_NONE;
   if (has_gate && ((rc = check_gate(s, gate)) != ADACONS_OK || (rc = check_gate(s, dgate)) != ADACONS_OK)) return rc;
   if ((has_post && dpost == nullptr) || (pre != nullptr && dpre == nullptr)) return ADACONS_EINVAL;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const bool empty = s->batch == 0 || s->len == 0;
-  if (!empty && (has_post || has_pre) && (rows == nullptr || reinterpret_cast<uintptr_t>(rows) % 4 != 0)) return ADACONS_EINVAL;
+  if (empty) {                                   // sums over no tokens; tensors without elements may all be at address 0
+    bool ok = true;
+    if (dpost != nullptr) ok = ok && cudaMemsetAsync(dpost, 0, static_cast<size_t>(s->dim) * size_of(s->post_dtype), st) == cudaSuccess;
+    if (dpre != nullptr) ok = ok && cudaMemsetAsync(dpre, 0, static_cast<size_t>(s->dim) * size_of(s->pre_dtype), st) == cudaSuccess;
+    const bool summed = dgate != nullptr && dgate->data != nullptr;
+    const int rows = !summed ? 0 : s->gate == ADACONS_NORM_GATE_CHANNEL ? 1 : s->gate == ADACONS_NORM_GATE_SEQUENCE ? s->batch : 0;
+    const size_t size = size_of(s->gate_dtype), width = s->dim * size, pitch = rows > 1 ? static_cast<size_t>(dgate->batch_stride) * size : width;
+    if (rows > 0) ok = ok && cudaMemset2DAsync(dgate->data, pitch, 0, width, rows, st) == cudaSuccess;
+    if (!ok) cudaGetLastError();
+    return ok ? ADACONS_OK : ADACONS_ECUDA;
+  }
+  if ((has_post || has_pre) && (rows == nullptr || reinterpret_cast<uintptr_t>(rows) % 4 != 0)) return ADACONS_EINVAL;
   const adacons_norm_rows *gate_rows = has_gate ? gate : nullptr, *to_gate = has_gate ? dgate : nullptr, *to_f = has_f ? df : nullptr;
   const adacons_norm_rows* reads[] = {has_pre ? out : nullptr, has_pre ? dnormed : nullptr, has_f ? f : nullptr, gate_rows};
   const adacons_norm_rows* writes[] = {dx, to_f, to_gate};
   for (const adacons_norm_rows* w : writes) {
     for (const adacons_norm_rows* r : reads)
-      if (!empty && same_place(w, r)) return ADACONS_EINVAL;
+      if (same_place(w, r)) return ADACONS_EINVAL;
     for (const adacons_norm_rows* other : writes)
-      if (!empty && w != other && same_place(w, other)) return ADACONS_EINVAL;
+      if (w != other && same_place(w, other)) return ADACONS_EINVAL;
   }
-  if (!empty && same_place(dx, dout) && !same_rows(dx, dout, s)) return ADACONS_EINVAL;      // dx may take dout's place
-  if (!empty && (same_place(to_f, dout) || same_place(to_gate, dout))) return ADACONS_EINVAL;
+  if (same_place(dx, dout) && !same_rows(dx, dout, s)) return ADACONS_EINVAL;      // dx may take dout's place
+  if (same_place(to_f, dout) || same_place(to_gate, dout)) return ADACONS_EINVAL;
   int sms = 0;
   if ((rc = device_sms(&sms)) != ADACONS_OK) return rc;
   const NormPlan n = plan_of(s, sms);
@@ -246,17 +258,10 @@ int adacons_norm_backward(const adacons_norm_shape* s, const adacons_norm_rows* 
   v.rows(to_gate, s->gate_dtype, gate_batch(s), gate_len(s));
   v.gain(p.post.data);
   v.gain(p.pre.data);
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (!empty && !go(s, p, n, v.ok, true, st)) return ADACONS_ECUDA;
-  if (empty) {                                   // sums over no tokens
-    p.parts = 0;
-    p.pre_sums = nullptr;
-    if (wants_sum) p.sums = static_cast<float*>(workspace);
-  }
+  if (!go(s, p, n, v.ok, true, st)) return ADACONS_ECUDA;
   if (!wants_sum && pre == nullptr) return ADACONS_OK;
-  if (empty && p.gate_kind == kGateSequence && s->batch == 0) p.groups = 0;
   const dim3 grid(static_cast<unsigned>((s->dim + 31) / 32));
-  const LaunchKind kind = empty ? kLaunchPlain : kLaunchOverlap;
+  const LaunchKind kind = kLaunchOverlap;
   bool ok;
   if (s->dtype == ADACONS_F32) ok = norm_run_sum_f32(p, grid, kind, st);
   else if (s->dtype == ADACONS_BF16) ok = norm_run_sum_bf16(p, grid, kind, st);

@@ -25,7 +25,8 @@ bool norm_launch(NormParams p, const NormPlan& n, bool back, cudaStream_t st) {
     const int x = static_cast<int>(sizeof(X)) / 2, f = static_cast<int>(sizeof(F)) / 2, gate = p.gate_kind != kGateToken ? 0 : p.gate_as.wide ? 2 : f;
     p.vectors = C * (back ? 2 * x + 2 * f + gate : x + (p.f.data != nullptr ? f : 0) + gate);
     const int row = p.vectors * 16 * kNormThreads;
-    p.depth = std::max(1, std::min(4, (kNormShared - p.ring) / row));
+    const long long turns = back ? (p.tokens / p.groups + p.parts - 1) / p.parts : (p.tokens + n.forward_blocks - 1) / n.forward_blocks;       // tokens of a block
+    p.depth = static_cast<int>(std::max(1ll, std::min<long long>({4, (kNormShared - p.ring) / row, (turns * n.tpr + kNormThreads - 1) / kNormThreads})));
     shared += p.depth * row;
   }
   if (back && kNormThreads > n.tpr) shared = std::max(shared, p.ring + kNormThreads * kNormN * static_cast<int>(sizeof(float)));

@@ -153,11 +153,13 @@ def distill_backward(dloss, logits, ids, teacher, rows, *, temperature: float = 
 
 
 def distill(logits, ids, teacher, *, temperature: float = 1.0, labels=None, mix=None):
-    """distill_forward's loss, one for each token, as a function of the logits that can be differentiated once.  The teacher is a constant."""
+    """distill_forward's loss, one for each token, as a function of the logits that can be differentiated once.  The teacher is a constant.
+    What does not lie as the passes want it, along rows, is copied."""
     for name, t in (("the teacher's logits", teacher), ("the temperature", temperature), ("mix", mix)):
         if getattr(t, "requires_grad", False):
             raise ValueError(f"distillation has no gradient for {name}")
-    return _Distill.apply(logits, ids, teacher, float(temperature), labels, _mix(labels, mix))
+    logits, ids, teacher = (t if t.dim() != 2 or t.shape[1] <= 1 or t.stride(1) == 1 else t.contiguous() for t in (logits, ids, teacher))
+    return _Distill.apply(logits, ids, teacher, float(temperature), None if labels is None else labels.contiguous(), _mix(labels, mix))
 
 
 class _Distill(torch.autograd.Function):

@@ -7,6 +7,10 @@ it is applied.  The task is synthetic: sequences of an affine recurrence modulo 
 follows from the one before it and the sequence's own hidden multiplier.
 
     python -m paper_2411_03742_b200.examples.transformer_workers --workers 8 --steps 100
+
+With --gated the layers are those of `GatedModel`: every block's norms, gate and residual addition in one operation (`residual_norm`) and the
+gated feed-forward block in another (`gated_feedforward`).  With --teacher K the workers learn from the K largest logits that a teacher, trained
+the same way first, has for each token (`distill`), mixed with the tokens themselves.
 """
 from __future__ import annotations
 
@@ -18,6 +22,9 @@ import torch.nn.functional as F
 
 from .. import binding
 from ..attention import attention
+from ..distillation import distill
+from ..feedforward import gated_feedforward
+from ..norms import residual_norm
 from ..orth import Orthogonalizer
 from ..rope import Rope
 
@@ -28,11 +35,9 @@ class Model:
 
     def __init__(self, vocab: int, dim: int = 128, heads: int = 4, kv_heads: int = 2, layers: int = 2, device="cuda:0", seed: int = 0):
         self.dim, self.heads, self.kv_heads, self.layers, self.head_dim = dim, heads, kv_heads, layers, dim // heads
-        qkv = (heads + 2 * kv_heads) * self.head_dim
         shapes = [("embed", (vocab, dim))]
         for i in range(layers):
-            shapes += [(f"{i}.gain1", (dim,)), (f"{i}.qkv", (qkv, dim)), (f"{i}.out", (dim, dim)), (f"{i}.gain2", (dim,)),
-                       (f"{i}.up", (4 * dim, dim)), (f"{i}.down", (dim, 4 * dim))]
+            shapes += self.layer(i)
         shapes += [("gain", (dim,))]
         g = torch.Generator().manual_seed(seed)
         pieces, self.views, self.matrices, at = [], {}, [], 0
@@ -47,12 +52,17 @@ class Model:
         self.flat = torch.cat(pieces).to(device).requires_grad_()
         self.rope = Rope(self.head_dim)
 
+    def layer(self, i: int):
+        """Names and shapes of a layer's parameters."""
+        dim, qkv = self.dim, (self.heads + 2 * self.kv_heads) * self.head_dim
+        return [(f"{i}.gain1", (dim,)), (f"{i}.qkv", (qkv, dim)), (f"{i}.out", (dim, dim)), (f"{i}.gain2", (dim,)), (f"{i}.up", (4 * dim, dim)), (f"{i}.down", (dim, 4 * dim))]
+
     def _w(self, name):
         at, shape = self.views[name]
         return self.flat[at:at + math.prod(shape)].view(shape)
 
-    def loss(self, tokens):
-        """Mean next-token cross entropy of (batch, length) tokens."""
+    def logits(self, tokens):
+        """Next-token logits (batch, length, vocabulary) of (batch, length) tokens."""
         x = self._w("embed")[tokens]
         B, S = tokens.shape
         H, K, D = self.heads, self.kv_heads, self.head_dim
@@ -65,8 +75,47 @@ class Model:
             h = F.rms_norm(x, (self.dim,)) * self._w(f"{i}.gain2")
             x = x + (F.gelu(h.bfloat16() @ self._w(f"{i}.up").bfloat16().T) @ self._w(f"{i}.down").bfloat16().T).float()
         x = F.rms_norm(x, (self.dim,)) * self._w("gain")
-        logits = x @ self._w("embed").T
-        return F.cross_entropy(logits[:, :-1].reshape(-1, logits.shape[-1]), tokens[:, 1:].reshape(-1))
+        return x @ self._w("embed").T
+
+    def loss(self, tokens, teacher=None, temperature: float = 2.0, mix: float = 0.5):
+        """Mean next-token cross entropy of (batch, length) tokens; with teacher = (ids, logits), both (batch, length, K), `mix` of it is the divergence from the
+        teacher's distribution over its K entries."""
+        logits = self.logits(tokens)
+        rows, labels = logits[:, :-1].reshape(-1, logits.shape[-1]), tokens[:, 1:].reshape(-1)
+        if teacher is None:
+            return F.cross_entropy(rows, labels)
+        ids, top = (t[:, :-1].reshape(-1, t.shape[-1]) for t in teacher)
+        return distill(rows, ids, top, temperature=temperature, labels=labels, mix=mix).mean()
+
+    @torch.no_grad()
+    def top_logits(self, tokens, k: int):
+        """(ids, logits) of the k largest logits of every token: what a teacher leaves for its students."""
+        top, ids = self.logits(tokens).topk(k, dim=-1)
+        return ids, top
+
+
+class GatedModel(Model):
+    """The same with a norm before and behind every block, a gate a channel on what it adds, and gated feed-forward blocks of the same size."""
+
+    def layer(self, i: int):
+        dim, qkv, hidden = self.dim, (self.heads + 2 * self.kv_heads) * self.head_dim, self.dim * 8 // 3 // 8 * 8
+        gains = [(f"{i}.{name}{k}", (dim,)) for k in (1, 2) for name in ("gain", "post", "gate")]
+        return gains + [(f"{i}.qkv", (qkv, dim)), (f"{i}.out", (dim, dim)), (f"{i}.gating", (hidden, dim)), (f"{i}.up", (hidden, dim)), (f"{i}.down", (dim, hidden))]
+
+    def logits(self, tokens):
+        B, S = tokens.shape
+        H, K, D = self.heads, self.kv_heads, self.head_dim
+        w = lambda name: self._w(name).bfloat16()  # noqa: E731
+        x, h = residual_norm(self._w("embed")[tokens], pre=self._w("0.gain1"), dtype=torch.bfloat16)
+        for i in range(self.layers):
+            qkv = (h @ w(f"{i}.qkv").T).view(B, S, H + 2 * K, D)
+            turned = self.rope(qkv[:, :, :H + K])                  # queries and keys in one call
+            a = attention(turned[:, :, :H], turned[:, :, H:], qkv[:, :, H + K:], causal=True).reshape(B, S, self.dim) @ w(f"{i}.out").T
+            x, h = residual_norm(x, a, post=self._w(f"{i}.post1"), gate=self._w(f"{i}.gate1"), gate_by="sigmoid", pre=self._w(f"{i}.gain2"))
+            f = gated_feedforward(h, w(f"{i}.gating"), w(f"{i}.up"), w(f"{i}.down"), act="silu")
+            after = f"{i + 1}.gain1" if i + 1 < self.layers else "gain"
+            x, h = residual_norm(x, f, post=self._w(f"{i}.post2"), gate=self._w(f"{i}.gate2"), gate_by="sigmoid", pre=self._w(after))
+        return h.float() @ self._w("embed").T
 
 
 def batch(workers: int, size: int, length: int, prime: int, gen: torch.Generator, device):
@@ -81,10 +130,11 @@ def batch(workers: int, size: int, length: int, prime: int, gen: torch.Generator
 
 
 def run(workers: int = 8, size: int = 16, length: int = 96, steps: int = 60, prime: int = 61, lr: float = 0.02, beta: float = 0.9, seed: int = 0,
-        device: str = "cuda:0", orthogonalise: bool = True):
-    """Mean loss over the workers, one value per step."""
+        device: str = "cuda:0", orthogonalise: bool = True, gated: bool = False, teacher=None, top: int = 8, model=None):
+    """Mean loss over the workers, one value per step.  teacher: a model whose `top` largest logits the workers learn from; model: one to train instead of a new one."""
     dev = torch.device(device)
-    model = Model(prime, device=dev, seed=seed)
+    if model is None:
+        model = (GatedModel if gated else Model)(prime, device=dev, seed=seed)
     d = model.flat.numel()
     grads = torch.empty((workers, d), device=dev)
     psi, momentum = torch.empty(d, device=dev), torch.zeros(d, device=dev)
@@ -99,7 +149,7 @@ def run(workers: int = 8, size: int = 16, length: int = 96, steps: int = 60, pri
             tokens = batch(workers, size, length, prime, gen, dev)
             total = 0.0
             for w in range(workers):
-                loss = model.loss(tokens[w])
+                loss = model.loss(tokens[w], None if teacher is None else teacher.top_logits(tokens[w], top))
                 grads[w], = torch.autograd.grad(loss, model.flat)
                 total += float(loss.detach())
             agg.aggregate(grads, psi)
@@ -127,8 +177,15 @@ def main(argv=None):
     ap.add_argument("--steps", type=int, default=60)
     ap.add_argument("--lr", type=float, default=0.02)
     ap.add_argument("--plain", action="store_true", help="scaled instead of orthogonalised updates")
+    ap.add_argument("--gated", action="store_true", help="norms on both sides of every block, gated residuals and feed-forward blocks")
+    ap.add_argument("--teacher", type=int, default=0, metavar="K", help="learn from the K largest logits of a teacher that is trained first")
     a = ap.parse_args(argv)
-    losses = run(a.workers, a.batch, a.length, a.steps, lr=a.lr, orthogonalise=not a.plain)
+    how = {"lr": a.lr, "orthogonalise": not a.plain, "gated": a.gated}
+    if a.teacher:
+        teacher = (GatedModel if a.gated else Model)(61, seed=1)
+        print(f"teacher after {a.steps} steps: loss {run(a.workers, a.batch, a.length, a.steps, model=teacher, **how)[-1]:.4f}")
+        how |= {"teacher": teacher, "top": a.teacher}
+    losses = run(a.workers, a.batch, a.length, a.steps, **how)
     for k in range(0, a.steps, max(1, a.steps // 10)):
         print(f"step {k:4d}  loss {losses[k]:.4f}")
     print(f"step {a.steps - 1:4d}  loss {losses[-1]:.4f}")

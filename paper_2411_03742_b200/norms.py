@@ -168,7 +168,7 @@ def residual_norm_forward(x, f=None, *, gate=None, gate_by=None, post=None, scal
     elif out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
     if pre is not None and normed is None:
-        normed = x.new_empty(x.shape, dtype=f.dtype if f is not None else dtype or x.dtype)
+        normed = x.new_empty(x.shape, dtype=dtype or x.dtype) if f is None else torch.empty_like(f, memory_format=torch.contiguous_format)
     if plan is None:
         kind = _kind(x, gate)
         plan = _plans.remember(sig, _Plan(_shape(x, f.dtype if f is not None else dtype or x.dtype, gate, kind, post, pre, gate_by, scale, eps),

@@ -1,0 +1,316 @@
+"""The gated feed-forward block and its gradient against the formulas in 64 bits.
+
+Tolerances.  u = eps / 2 of the type (bf16 2^-8, fp16 2^-11) is the largest relative error of a rounding.  A result is a sum of products of which one
+operand is rounded (h, dg or du), and is rounded itself: u of the products by magnitude plus u of the value, element by element, with 2^-13 of the products for sums in
+fp32 (tensor cores drop 4e-8 of the running sum a product) and, where an activation is nearly zero, 2e-7 of |g u| for its approximation.  fp16 holds operands below
+2^-14 with a step of 2^-24.  In the 2-norm independent roundings of 0.43 u each make 0.6 u; u is allowed.
+"""
+import math
+
+import pytest
+import torch
+import torch.nn.functional as fn
+
+pytestmark = pytest.mark.gpu
+ACTS = {"silu": fn.silu, "gelu": fn.gelu, "gelu_tanh": lambda v: fn.gelu(v, approximate="tanh"), "relu": fn.relu}
+
+
+def make(T, D, F, dtype=torch.bfloat16, seed=0, wide=0, dy=0.1):
+    g = torch.Generator(device="cuda").manual_seed(seed + T)
+    r = lambda m, n, s: (s * torch.randn((m, n + wide), generator=g, device="cuda")).to(dtype)[:, :n]  # noqa: E731
+    return [r(T, D, 1.0), r(F, D, D ** -0.5), r(F, D, D ** -0.5), r(D, F, F ** -0.5)], r(T, D, dy)
+
+
+def slope(act, g):
+    leaf = g.detach().clone().requires_grad_()
+    return torch.autograd.grad(ACTS[act](leaf).sum(), leaf)[0]
+
+
+def close(got, want, size, what):
+    assert got.shape == want.shape, what
+    if want.numel() == 0:
+        return
+    u, largest = torch.finfo(got.dtype).eps / 2, torch.finfo(got.dtype).max
+    allowed = u * want.abs() + size
+    # from half a step above the type's largest value on, a result rounds to infinity
+    beyond = got.isinf() & (got.double() * want > 0) & (want.abs() + allowed >= largest * (1 + u / 2))
+    diff = (got.double() - want).abs().masked_fill(beyond, 0.0)
+    bad = diff > allowed
+    assert not bool(bad.any()), (what, int(bad.sum()), float(diff.max()))
+    if want.numel() >= 4096:
+        # fp16 rounds results below 2^-14 by up to 2^-25 each, whatever their size
+        step = 2.0 ** -25 if got.dtype == torch.float16 else 0.0
+        assert float(diff.norm()) <= u * float(want.norm()) + step * math.sqrt(want.numel()), (what, float(diff.norm() / want.norm()) / u)
+
+
+def check(T, D, F, act="silu", dtype=torch.bfloat16, wide=0, seed=0, dy=0.1, given=None):
+    from paper_2411_03742_b200 import feedforward, feedforward_backward, feedforward_forward
+    (x, wg, wu, wd), dout = given or make(T, D, F, dtype, seed, wide, dy)
+    u = torch.finfo(dtype).eps / 2
+    step = 2.0 ** -25 if dtype == torch.float16 else 0.0
+    near = u + 2.0 ** -13
+    out, gate, up = feedforward_forward(x, wg, wu, wd, act=act)
+    X, G, U, Dn = (t.double() for t in (x, wg, wu, wd))
+    g, p = X @ G.T, X @ U.T
+    close(gate, g, 2.0 ** -13 * (X.abs() @ G.abs().T) + step, "gate")
+    close(up, p, 2.0 ** -13 * (X.abs() @ U.abs().T) + step, "up")
+    h = ACTS[act](g) * p
+    # g and u behind the activation are sums in fp32
+    h_size = near * h.abs() + 2e-7 * (g * p).abs() + 2.0 ** -13 * ((slope(act, g) * p).abs() * (X.abs() @ G.abs().T) + ACTS[act](g).abs() * (X.abs() @ U.abs().T)) + step
+    close(out, h @ Dn.T, h_size @ Dn.abs().T + 2.0 ** -13 * (h.abs() @ Dn.abs().T) + step, "out")
+    alone = feedforward_forward(x, wg, wu, wd, act=act, keep=False)
+    assert alone[1] is None and alone[2] is None and torch.equal(alone[0], out)
+    grads = feedforward_backward(dout, x, wg, wu, wd, gate, up, act=act)
+    dy, g, p = dout.double(), gate.double(), up.double()
+    a, s = ACTS[act](g), slope(act, g)
+    dh, dh_size = dy @ Dn, dy.abs() @ Dn.abs()
+    dg, du, h = dh * p * s, dh * a, a * p
+    top = float(dy.abs().max()) if dy.numel() else 0.0
+    held = step * 2 * top                          # fp16 holds dg and du times a power of two that brings dy's largest element to 1/2 .. 1
+    dg_size = near * dg.abs() + 2.0 ** -13 * (dh_size * (p * s).abs()) + 4e-7 * dh_size * p.abs() * (1 + g.abs()) + held
+    du_size = near * du.abs() + 2.0 ** -13 * dh_size * a.abs() + 4e-7 * dh_size * g.abs() + held
+    h_size = near * h.abs() + 2e-7 * (g * p).abs() + step
+    wants = (dg @ G + du @ U, dg.T @ X, du.T @ X, dy.T @ h)
+    sizes = (dg_size @ G.abs() + du_size @ U.abs(), dg_size.T @ X.abs(), du_size.T @ X.abs(), dy.abs().T @ h_size)
+    for name, got, want, size, mag in zip(("dx", "dw_gate", "dw_up", "dw_down"), grads, wants, sizes,
+                                          (dg.abs() @ G.abs() + du.abs() @ U.abs(), dg.abs().T @ X.abs(), du.abs().T @ X.abs(), dy.abs().T @ h.abs())):
+        close(got, want, size + 2.0 ** -13 * mag + step, name)
+    assert feedforward.status() == 0
+    return (out, gate, up), grads
+
+
+@pytest.mark.parametrize("act", sorted(ACTS))
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T, D, F", [(5, 64, 72), (77, 128, 512), (300, 264, 1368)])
+def test_activations_and_types(T, D, F, act, dtype):
+    check(T, D, F, act, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T, D, F", [(1, 8, 8), (1, 1024, 4096), (2, 8, 4096), (16, 1024, 4096), (17, 520, 1368), (33, 4096, 64), (63, 64, 64), (64, 64, 64), (65, 72, 200), (128, 128, 128),
+                                     (129, 136, 264), (255, 512, 1024), (257, 1000, 72), (520, 8, 3000), (1000, 768, 2056), (2049, 1032, 1544), (4096, 256, 1024), (3000, 2048, 520)])
+def test_sizes(T, D, F, dtype):
+    """One token to many, sides that end inside tiles; lone blocks, shared K, pairs, whole and half tiles."""
+    check(T, D, F, "silu" if D > 600 else "gelu", dtype)
+
+
+def test_long():
+    check(4100, 2048, 5464, "gelu")
+
+
+@pytest.mark.parametrize("wide", [8, 40])
+@pytest.mark.parametrize("T, D, F", [(50, 128, 384), (700, 256, 1024)])
+def test_wider_rows_and_given_results(T, D, F, wide):
+    """Slices of wider matrices; results into slices too, whose surroundings stay as they were."""
+    from paper_2411_03742_b200 import feedforward_backward, feedforward_forward
+    inputs, dout = make(T, D, F, wide=wide)
+    made, grads = check(T, D, F, given=(inputs, dout))
+    room = lambda m, n: torch.full((m + 2, n + 16), 7.0, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    rooms = [room(T, D), room(T, F), room(T, F)]
+    spots = [r[1:-1, 8:-8] for r in rooms]
+    feedforward_forward(*inputs, out=spots[0], gate=spots[1], up=spots[2])
+    back = [room(T, D), room(F, D), room(F, D), room(D, F)]
+    spots += [r[1:-1, 8:-8] for r in back]
+    feedforward_backward(dout, *inputs, made[1], made[2], dx=spots[3], dw_gate=spots[4], dw_up=spots[5], dw_down=spots[6])
+    for spot, want in zip(spots, (*made, *grads)):
+        assert torch.equal(spot, want)
+    for r in rooms + back:
+        assert bool((r[0] == 7).all() and (r[-1] == 7).all() and (r[:, :8] == 7).all() and (r[:, -8:] == 7).all())
+
+
+def test_parts_of_the_gradient():
+    from paper_2411_03742_b200 import feedforward_backward, feedforward_forward
+    for T in (40, 900):
+        inputs, dout = make(T, 256, 1024)
+        _, gate, up = feedforward_forward(*inputs)
+        want = feedforward_backward(dout, *inputs, gate, up)
+        for k in range(16):
+            pick = tuple(bool(k >> i & 1) for i in range(4))
+            got = feedforward_backward(dout, *inputs, gate, up, want=pick)
+            assert all((a is None) if not p else torch.equal(a, b) for a, b, p in zip(got, want, pick))
+
+
+@pytest.mark.parametrize("dy", [1e-5, 1e-3, 30.0, 2000.0])
+def test_fp16_gradients_of_any_size(dy):
+    """Between the products gradients are held scaled: neither small ones lose their bits nor large ones leave the range."""
+    check(200, 128, 512, "silu", torch.float16, dy=dy)
+
+
+def test_no_tokens():
+    from paper_2411_03742_b200 import feedforward_backward, feedforward_forward
+    inputs, dout = make(0, 64, 128)
+    out, gate, up = feedforward_forward(*inputs)
+    assert out.shape == (0, 64) and gate.shape == up.shape == (0, 128)
+    grads = feedforward_backward(dout, *inputs, gate, up)
+    assert [tuple(g.shape) for g in grads] == [(0, 64), (128, 64), (128, 64), (64, 128)] and not any(bool(g.any()) for g in grads)
+
+
+def test_nan_stays_in_its_token():
+    from paper_2411_03742_b200 import feedforward_forward
+    for T, D, F in ((30, 128, 256), (600, 512, 1024)):
+        (x, *w), _ = make(T, D, F)
+        want = feedforward_forward(x, *w)
+        bad = x.clone()
+        bad[7, 3], bad[20, 9] = math.nan, math.inf
+        got = feedforward_forward(bad, *w)
+        keep = [i for i in range(T) if i not in (7, 20)]
+        assert all(torch.equal(a[keep], b[keep]) for a, b in zip(got, want)) and got[0][7].isnan().all()
+
+
+def test_large_activations():
+    """Far out the activations are 0 or g, without Inf or NaN on the way."""
+    from paper_2411_03742_b200 import feedforward_backward, feedforward_forward
+    eye = torch.eye(64, dtype=torch.bfloat16, device="cuda")
+    x = torch.linspace(-300, 300, 64 * 40, device="cuda").bfloat16().view(40, 64)
+    x[0, :4] = torch.tensor([-3e4, 3e4, -1e-30, 0.0])
+    ones = torch.zeros((64, 64), dtype=torch.bfloat16, device="cuda")
+    ones[:, 0] = 1.0
+    x1 = torch.cat([torch.ones_like(x[:, :64]), x], 1)          # up = 1
+    wg = torch.cat([torch.zeros_like(eye), eye], 1)
+    wu = torch.cat([ones, torch.zeros_like(eye)], 1)
+    for act in ACTS:
+        out, gate, up = feedforward_forward(x1, wg, wu, torch.cat([eye, eye], 0), act=act)
+        assert torch.equal(gate, x) and bool((up == 1).all())
+        want = ACTS[act](x.double())
+        assert bool(((out[:, :64].double() - want).abs() <= 2.0 ** -8 * want.abs() + 2e-7 * x.double().abs()).all()), act
+        grads = feedforward_backward(torch.ones_like(out), x1, wg, wu, torch.cat([eye, eye], 0), gate, up, act=act)
+        assert all(bool(g.isfinite().all()) for g in grads)
+
+
+def test_autograd():
+    """gated_feedforward against autograd through the formula in 64 bits; leading dimensions, transposed weights, broadcast gradients, frozen ones."""
+    from paper_2411_03742_b200 import gated_feedforward
+    (x, wg, wu, wd), dout = make(60, 64, 160)
+    leaves = [x.view(3, 20, 64).clone().requires_grad_(), wg.clone().requires_grad_(), wu.clone().requires_grad_(), wd.clone().requires_grad_()]
+    y = gated_feedforward(*leaves, act="gelu")
+    assert y.shape == (3, 20, 64)
+    got = torch.autograd.grad(y, leaves, dout.view(3, 20, 64))
+    wide = [t.detach().double().requires_grad_() for t in leaves]
+    Y = (fn.gelu(wide[0] @ wide[1].T) * (wide[0] @ wide[2].T)) @ wide[3].T
+    want = torch.autograd.grad(Y, wide, dout.view(3, 20, 64).double())
+    # gate and up are rounded as well here: three roundings, 0.43 sqrt(3) u
+    for a, b in zip((y, *got), (Y.detach(), *want)):
+        assert float((a.detach().double() - b).norm() / b.norm()) <= 1.2 * 2.0 ** -8
+    turned = wg.T.contiguous().T.detach().requires_grad_()
+    again = gated_feedforward(leaves[0], turned, leaves[2], leaves[3], act="gelu")
+    assert torch.equal(again, y)
+    g1, = torch.autograd.grad(again.sum(), turned)
+    g2, = torch.autograd.grad(y.sum(), leaves[1]) if False else torch.autograd.grad(gated_feedforward(*leaves, act="gelu").sum(), leaves[1])
+    assert torch.equal(g1, g2)
+    frozen = gated_feedforward(leaves[0], *(t.detach() for t in leaves[1:]), act="gelu")
+    gx, = torch.autograd.grad(frozen, leaves[0], dout.view(3, 20, 64))
+    assert torch.equal(gx, got[0])
+    with torch.no_grad():
+        assert torch.equal(gated_feedforward(*leaves, act="gelu"), y)
+    with pytest.raises(NotImplementedError, match="once"):
+        one, = torch.autograd.grad(gated_feedforward(*leaves).sum(), leaves[0], create_graph=True)
+        torch.autograd.grad(one.sum(), leaves[1])
+
+
+def test_gradient_against_differences():
+    """The loss along a random direction of each input, by central differences of the formula in 64 bits."""
+    from paper_2411_03742_b200 import gated_feedforward
+    inputs, dout = make(40, 48, 104)
+    leaves = [t.clone().requires_grad_() for t in inputs]
+    grads = torch.autograd.grad(gated_feedforward(*leaves), leaves, dout)
+    loss = lambda v: float((((fn.silu(v[0] @ v[1].T) * (v[0] @ v[2].T)) @ v[3].T) * dout.double()).sum())  # noqa: E731
+    for k, g in enumerate(grads):
+        d = torch.randn_like(g).double()
+        up, down = ([t.detach().double() + (s * 1e-5 * d if i == k else 0) for i, t in enumerate(leaves)] for s in (1, -1))
+        want = (loss(up) - loss(down)) / 2e-5
+        # independent errors of 1.2 u of the elements
+        assert abs(float((g.double() * d).sum()) - want) <= 4 * 1.2 * 2.0 ** -8 * float((g.double() * d).norm())
+
+
+@pytest.mark.parametrize("T, D, F", [(16, 512, 1024), (900, 512, 1024)])
+def test_repeats_graphs_and_streams(T, D, F):
+    from paper_2411_03742_b200 import feedforward_backward, feedforward_forward
+    for dtype in (torch.bfloat16, torch.float16):
+        inputs, dout = make(T, D, F, dtype)
+
+        def step(stream=None):
+            out, gate, up = feedforward_forward(*inputs, stream=stream)
+            return (out, gate, up, *feedforward_backward(dout, *inputs, gate, up, stream=stream))
+
+        want = step()
+        for _ in range(5):
+            assert all(torch.equal(a, b) for a, b in zip(step(), want))
+        graphs = []
+        for _ in range(2):                              # two captured graphs have workspaces of their own
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                graphs.append((g, step()))
+        keep = inputs[0].clone()
+        inputs[0].zero_()
+        graphs[0][0].replay()
+        inputs[0].copy_(keep)
+        for g, _ in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for _, got in graphs:
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(50_000_000)
+        got = step(side)
+        rubbish = [torch.full((n,), math.nan, dtype=dtype, device="cuda") for n in (T * D, T * F, F * D, 3 * T * F) for _ in range(4)]
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        del rubbish
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, each larger than the device: their kernels share it and their results are their own."""
+    from paper_2411_03742_b200 import feedforward, feedforward_backward, feedforward_forward
+    sets = [make(1500, 512, 2048, seed=k) for k in range(2)]
+    want = []
+    for inputs, dout in sets:
+        made = feedforward_forward(*inputs)
+        want.append((*made, *feedforward_backward(dout, *inputs, made[1], made[2])))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        got = []
+        for s, (inputs, dout) in zip(streams, sets):
+            with torch.cuda.stream(s):
+                made = feedforward_forward(*inputs)
+                got.append((*made, *feedforward_backward(dout, *inputs, made[1], made[2])))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
+    assert feedforward.status() == 0
+
+
+@pytest.mark.parametrize("paired", [False, True])
+def test_waits_that_run_out(paired):
+    """Operands that never come: the kernel ends by itself, says so, and the next call is right."""
+    from paper_2411_03742_b200 import feedforward
+    (x, wg, wu, _), _ = make(100, 128, 64)
+    assert feedforward.status() == 0
+    feedforward.selftest_bounded_wait(x, wg, wu, paired)
+    assert feedforward.status() == 0x100 and feedforward.status() == 0
+    check(100, 128, 64)
+
+
+def test_first_of_a_thread():
+    """A call in a thread that has made no CUDA call yet."""
+    import threading
+    from paper_2411_03742_b200 import feedforward_forward
+    inputs, _ = make(300, 128, 512)
+    want = feedforward_forward(*inputs)
+    spots = [torch.empty_like(t) for t in want]
+    work = torch.empty(300 * 512 * 2 + 256, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    errors = []
+
+    def run():
+        try:
+            feedforward_forward(*inputs, out=spots[0], gate=spots[1], up=spots[2], workspace=work)
+        except Exception as e:
+            errors.append(repr(e))
+
+    t = threading.Thread(target=run)
+    t.start()
+    t.join()
+    torch.cuda.synchronize()
+    assert not errors and all(torch.equal(a, b) for a, b in zip(spots, want))
