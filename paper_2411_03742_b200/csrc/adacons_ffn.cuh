@@ -334,67 +334,77 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
   };
 
   if (warp == kFfnEndWarps) {
-    if (lane == 0) {
-      int stage = 0, issued = 0;
-      uint32_t parity = 1;                       // the stages start out empty
-      bool ok = true;
-      auto load = [&](unsigned char* dst, int map, int x, int y, int s) {
-        if (CG == 2) tma_load_2d_pair(dst, &p.maps[map], &full[s], x, y);
-        else tma_load_2d(dst, &p.maps[map], &full[s], x, y);
-      };
-      auto load_left = [&](const FfnSpot& s, const FfnProblem& q, int k, int at) {
-        const int segment = k >= q.steps ? 1 : 0, k0 = (k - segment * q.steps) * kFfnTK;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = s.i * kTM + side_of_pair * 128 + h * 64;
-          load(smem + at * T::kStage + h * 8192, q.a[segment], q.a_across ? r : k0, q.a_across ? k0 : r, at);
-        }
-      };
-      auto load_right = [&](const FfnSpot& s, const FfnProblem& q, int k, int at) {
-        const int segment = k >= q.steps ? 1 : 0, k0 = (k - segment * q.steps) * kFfnTK;
-        if (side_of_pair == 0) mbar_expect_tx(&full[at], CG * (1 + s.halves) * kFfnOperand);      // a pair's bytes all count on the even block's barrier
-        for (int n = 0; n < s.halves; ++n)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            int map, r;
-            if (KIND == kFfnUp) {
-              map = q.b[CG == 2 ? side_of_pair : h];
-              r = (s.j + n) * kCols + (CG == 2 ? h * 64 : 0);
-            } else {
-              map = q.b[segment];
-              r = (s.j + n) * kCols + side_of_pair * 128 + h * 64;
-            }
-            load(smem + at * T::kStage + (1 + n) * kFfnOperand + h * 8192, map, q.b_across ? r : k0, q.b_across ? k0 : r, at);
+    // The whole warp goes through the loop, so that maps and coordinates are uniform values; one lane issues.  With the loop inside one lane's branch a
+    // copy took 220 cycles to issue, 890 a stage of four.
+    const bool issuer = elect_one();
+    int stage = 0, issued = 0, ahead = 0;
+    uint32_t parity = 1;                         // the stages start out empty
+    bool ok = true;
+    auto copy = [&](unsigned char* dst, const CUtensorMap* map, int x, int y, int at) {
+      if (CG == 2) tma_load_2d_pair(dst, map, &full[at], x, y);
+      else tma_load_2d(dst, map, &full[at], x, y);
+    };
+    // Stages `from` to `to` of a tile, both operands, or as much as `left` and `right` say; `wait`: for each to be empty.
+    auto stages_of = [&](const FfnSpot& s, const FfnProblem& q, int from, int to, bool left, int right_from, bool wait) {
+      for (int segment = 0; segment < q.segments && ok; ++segment) {
+        const CUtensorMap* a_map = &p.maps[q.a[segment]];
+        const CUtensorMap* b_map[2] = {&p.maps[KIND == kFfnUp ? q.b[CG == 2 ? side_of_pair : 0] : q.b[segment]], &p.maps[KIND == kFfnUp ? q.b[CG == 2 ? side_of_pair : 1] : q.b[segment]]};
+        const int first = max(from, segment * q.steps), last = min(to, (segment + 1) * q.steps);
+        const int a_row = s.i * kTM + side_of_pair * 128;
+        const int b_row = s.j * kCols + (KIND == kFfnUp ? 0 : side_of_pair * 128), b_box = KIND == kFfnUp && CG == 1 ? 0 : 64;       // to the operand's second box
+        const int halves = s.halves, a_across = q.a_across, b_across = q.b_across;
+        for (int k = first; k < last; ++k) {
+          if (wait) {
+            const bool got = !s_abort && mbar_wait_bounded(&empty[stage], parity);
+            if (!__all_sync(0xffffffffu, got)) { s_abort = 1; ok = false; break; }
           }
-      };
-      // What does not come from the kernel before is on its way while that one ends.
-      int ahead = 0;
-      if (worker < p.tiles) {
-        const FfnSpot s = ffn_spot<CG>(p, worker);
-        const FfnProblem& q = p.problem[s.problem];
-        int begin, end;
-        steps_of(q, begin, end);
-        if (q.early && s.halves > 0 && !STARVE)
-          for (; ahead < stages && begin + ahead < end; ++ahead) load_right(s, q, begin + ahead, ahead);
-      }
-      pdl_wait();
-      for (int t = worker; ok && t < p.tiles; t += workers) {
-        const FfnSpot s = ffn_spot<CG>(p, t);
-        if (s.halves == 0) continue;
-        const FfnProblem& q = p.problem[s.problem];
-        int begin, end;
-        steps_of(q, begin, end);
-        for (int k = begin; k < end; ++k) {
-          if (STARVE && k == end - 1) break;
-          if (s_abort || !mbar_wait_bounded(&empty[stage], parity)) { s_abort = 1; ok = false; break; }
-          if (issued >= ahead) load_right(s, q, k, stage);
-          load_left(s, q, k, stage);
-          ++issued;
+          if (issuer) {
+            const int k0 = (k - segment * q.steps) * kFfnTK;
+            unsigned char* at = smem + stage * T::kStage;
+            if (k >= right_from) {
+              if (side_of_pair == 0) mbar_expect_tx(&full[stage], CG * (1 + halves) * kFfnOperand);      // a pair's bytes all count on the even block's barrier
+#pragma unroll
+              for (int n = 0; n < T::kHalves; ++n) {
+                if (n >= halves) break;
+                const int r = b_row + n * kCols;
+                copy(at + (1 + n) * kFfnOperand, b_map[0], b_across ? r : k0, b_across ? k0 : r, stage);
+                copy(at + (1 + n) * kFfnOperand + 8192, b_map[1], b_across ? r + b_box : k0, b_across ? k0 : r + b_box, stage);
+              }
+            }
+            if (left) {
+              copy(at, a_map, a_across ? a_row : k0, a_across ? k0 : a_row, stage);
+              copy(at + 8192, a_map, a_across ? a_row + 64 : k0, a_across ? k0 : a_row + 64, stage);
+            }
+          }
+          __syncwarp();
+          if (left) ++issued;
           if (++stage == stages) { stage = 0; parity ^= 1u; }
         }
       }
-      s_issued = max(issued, ahead);
+    };
+    // What does not come from the kernel before is on its way while that one ends.
+    if (worker < p.tiles && !STARVE) {
+      const FfnSpot s = ffn_spot<CG>(p, worker);
+      const FfnProblem& q = p.problem[s.problem];
+      int begin, end;
+      steps_of(q, begin, end);
+      if (q.early && s.halves > 0) {
+        ahead = min(stages, end - begin);
+        stages_of(s, q, begin, begin + ahead, false, 0, false);
+        stage = 0;
+        parity = 1;
+      }
     }
+    pdl_wait();
+    for (int t = worker; ok && t < p.tiles; t += workers) {
+      const FfnSpot s = ffn_spot<CG>(p, t);
+      if (s.halves == 0) continue;
+      const FfnProblem& q = p.problem[s.problem];
+      int begin, end;
+      steps_of(q, begin, end);
+      stages_of(s, q, begin, STARVE ? end - 1 : end, true, t == worker ? begin + ahead : begin, true);
+    }
+    if (lane == 0) s_issued = max(issued, ahead);
   } else if (warp == kFfnEndWarps + 1) {
     if (side_of_pair == 0) {
       // The whole warp goes through the loop, so that addresses and descriptors are uniform values; one lane issues.
@@ -570,18 +580,29 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = w[e] = make_float2(0.f, 0.f);
         const float* at = reinterpret_cast<const float*>(smem) + r * kFfnSumRow + c;
-        for (int b = 0; b < shares; ++b) {
+        for (int b0 = 0; b0 < shares; b0 += 4) {       // four blocks' sums under way at once, added in order
+          float4 f[4][2], d[4][2];
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float4 f = ld_cluster_f32x4(at + 4 * k, b);
-            v[2 * k] = add2(v[2 * k], make_float2(f.x, f.y));
-            v[2 * k + 1] = add2(v[2 * k + 1], make_float2(f.z, f.w));
-            if (KIND == kFfnUp) {
-              const float4 d = ld_cluster_f32x4(at + kCols + 4 * k, b);
-              w[2 * k] = add2(w[2 * k], make_float2(d.x, d.y));
-              w[2 * k + 1] = add2(w[2 * k + 1], make_float2(d.z, d.w));
+          for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              f[b][k] = d[b][k] = make_float4(0.f, 0.f, 0.f, 0.f);
+              if (b0 + b < shares) {
+                f[b][k] = ld_cluster_f32x4(at + 4 * k, b0 + b);
+                if (KIND == kFfnUp) d[b][k] = ld_cluster_f32x4(at + kCols + 4 * k, b0 + b);
+              }
             }
-          }
+#pragma unroll
+          for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              v[2 * k] = add2(v[2 * k], make_float2(f[b][k].x, f[b][k].y));
+              v[2 * k + 1] = add2(v[2 * k + 1], make_float2(f[b][k].z, f[b][k].w));
+              if (KIND == kFfnUp) {
+                w[2 * k] = add2(w[2 * k], make_float2(d[b][k].x, d[b][k].y));
+                w[2 * k + 1] = add2(w[2 * k + 1], make_float2(d[b][k].z, d[b][k].w));
+              }
+            }
         }
         ffn_end<KIND, BF16, 8>(p.act, factor, v, w, &gate, &up, &one, &two, &result);
         if (KIND == kFfnBack || (KIND == kFfnUp && p.gate.data != nullptr)) {
