@@ -190,6 +190,20 @@ bool run(const FfnDevice& d, const adacons_ffn_shape* s, FfnParams* p, int n, co
 
 int steps_of(int k) { return (k + kFfnTK - 1) / kFfnTK; }
 
+// The forward pass of a few tokens.  Eight warps a block, or sixteen where that leaves each of them eight stages of 32 K or more.
+template <int KIND, bool BF16>
+bool run_few(const FfnFewParams& p, bool overlap, cudaStream_t st) {
+  const int warps = p.k >= 8 * 16 * 32 ? 16 : 8, sixteens = p.tokens <= 16 ? 1 : p.tokens <= 32 ? 2 : 4;
+  const size_t bytes = static_cast<size_t>(warps) * (KIND == kFfnUp ? 2 : 1) * sixteens * 16 * 8 * sizeof(float);
+  const dim3 grid((p.n + 7) / 8), block(32 * warps);
+  const LaunchKind kind = overlap ? kLaunchOverlap : kLaunchPlain;
+  if (bytes > 40 * 1024) {                       // the same limit at every launch
+    if (cudaFuncSetAttribute(ffn_few_kernel<KIND, BF16, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024) != cudaSuccess) { cudaGetLastError(); return false; }
+  }
+  if (sixteens == 1) return launch(&ffn_few_kernel<KIND, BF16, 1>, grid, block, bytes, st, kind, 1, p);
+  return sixteens == 2 ? launch(&ffn_few_kernel<KIND, BF16, 2>, grid, block, bytes, st, kind, 1, p) : launch(&ffn_few_kernel<KIND, BF16, 4>, grid, block, bytes, st, kind, 1, p);
+}
+
 // Whether two matrices start at the same place: a result there would be written while other blocks still read.
 bool same_place(const adacons_ffn_matrix* a, const adacons_ffn_matrix* b) { return a != b && a->data != nullptr && a->data == b->data; }
 
@@ -247,6 +261,28 @@ int adacons_ffn_forward(const adacons_ffn_shape* s, const adacons_ffn_matrix* x,
   FfnDevice* d = nullptr;
   if ((rc = ffn_device(&d)) != ADACONS_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (s->tokens <= kFfnFew) {
+    FfnFewParams few = {};
+    few.x = as_rows(x, s->dim, s->tokens);
+    few.w[0] = as_rows(wg, s->dim, s->hidden);
+    few.w[1] = as_rows(wu, s->dim, s->hidden);
+    few.gate = as_rows(gate, s->hidden, s->tokens);
+    few.up = as_rows(up, s->hidden, s->tokens);
+    few.out = as_rows(workspace, s->hidden, s->hidden, s->tokens);
+    few.tokens = s->tokens;
+    few.n = s->hidden;
+    few.k = s->dim;
+    few.act = s->act;
+    FfnFewParams down = few;
+    down.x = few.out;
+    down.w[0] = as_rows(wd, s->hidden, s->dim);
+    down.out = as_rows(out, s->dim, s->tokens);
+    down.n = s->dim;
+    down.k = s->hidden;
+    const bool ok = s->dtype == ADACONS_BF16 ? run_few<kFfnUp, true>(few, false, st) && run_few<kFfnPlain, true>(down, true, st)
+                                             : run_few<kFfnUp, false>(few, false, st) && run_few<kFfnPlain, false>(down, true, st);
+    return ok ? ADACONS_OK : ADACONS_ECUDA;
+  }
   FfnParams p;
   std::memset(&p, 0, sizeof(p));
   if (!make_map(*d, &p.maps[0], s, x->data, x->row_stride, s->tokens, s->dim) || !make_map(*d, &p.maps[1], s, wg->data, wg->row_stride, s->hidden, s->dim) ||

@@ -630,6 +630,117 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
   }
 }
 
+// ----------------------------------------------------------------------------------------------
+// A few tokens (up to 64): the weights are what has to be read, 2 bytes for one or two products each, and what counts is how soon all of them are asked
+// for.  A block takes eight rows of the weights (Up: of both projections), its warps divide K among them, 32 at a time in turn, and add up
+// their sums through shared memory in order.  A lane's 16 bytes of a weight row and of a token's row are the same eight K; which of a product's sixteen
+// places a K takes is the same on both sides, so they go into the warp's products as they were loaded, without a
+// turn through shared memory.  What the kernel before does not make, the first weights, is asked for while that one ends.
+// 16 tokens through 1024 x 4096: @@ us where tiles of 128 tokens take 19.5.
+// ----------------------------------------------------------------------------------------------
+constexpr int kFfnFew = 64, kFfnFewWarps = 16;
+struct FfnFewParams {
+  FfnRows x, w[2], out, gate, up;                // w: rows of weights; Plain: one
+  int tokens, n, k, act;
+};
+
+template <bool BF16>
+__device__ __forceinline__ void ffn_mma(float (&c)[4], const uint32_t a0, const uint32_t a1, const uint32_t a2, const uint32_t a3, const uint32_t b0, const uint32_t b1) {
+  if (BF16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// MT: sixteens of tokens
+template <int KIND, bool BF16, int MT>
+__global__ void __launch_bounds__(32 * kFfnFewWarps) ffn_few_kernel(const FfnFewParams p) {
+  constexpr int kW = KIND == kFfnUp ? 2 : 1;
+  constexpr int kDeep = MT == 1 ? 4 : 2;         // of a warp's K under way at once, and as many again of the weights
+  extern __shared__ float s_sums[];              // [warp][kW][16 MT][8]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  const int row = lane >> 2, at = (lane & 3) * 8, col = blockIdx.x * 8 + row;
+  const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+  pdl_launch_dependents();
+  float acc[kW][MT][4];
+#pragma unroll
+  for (int w = 0; w < kW; ++w)
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[w][m][e] = 0.f;
+  uint4 weights[kDeep][kW];
+  auto ask = [&](int k0) {
+#pragma unroll
+    for (int d = 0; d < kDeep; ++d) {
+      const int k = k0 + d * warps * 32 + at;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) weights[d][w] = k < p.k && col < p.n ? ld_stream_v4(ffn_at(p.w[w], col, k)) : none;
+    }
+  };
+  int k0 = warp * 32;
+  ask(k0);
+  pdl_wait();
+  for (; k0 < p.k; k0 += kDeep * warps * 32) {
+    uint4 x[kDeep][MT][2], now[kDeep][kW];
+#pragma unroll
+    for (int d = 0; d < kDeep; ++d) {
+      const int k = k0 + d * warps * 32 + at;
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int token = m * 16 + h * 8 + row;
+          x[d][m][h] = k < p.k && token < p.tokens ? *ffn_at(p.x, token, k) : none;
+        }
+#pragma unroll
+      for (int w = 0; w < kW; ++w) now[d][w] = weights[d][w];
+    }
+    ask(k0 + kDeep * warps * 32);
+#pragma unroll
+    for (int d = 0; d < kDeep; ++d)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int w = 0; w < kW; ++w) {
+          ffn_mma<BF16>(acc[w][m], x[d][m][0].x, x[d][m][1].x, x[d][m][0].y, x[d][m][1].y, now[d][w].x, now[d][w].y);
+          ffn_mma<BF16>(acc[w][m], x[d][m][0].z, x[d][m][1].z, x[d][m][0].w, x[d][m][1].w, now[d][w].z, now[d][w].w);
+        }
+  }
+  auto place = [&](int of_warp, int w, int token, int c) { return s_sums + ((of_warp * kW + w) * MT * 16 + token) * 8 + c; };
+#pragma unroll
+  for (int w = 0; w < kW; ++w)
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) *reinterpret_cast<float2*>(place(warp, w, m * 16 + h * 8 + row, (lane & 3) * 2)) = make_float2(acc[w][m][2 * h], acc[w][m][2 * h + 1]);
+  __syncthreads();
+  for (int o = threadIdx.x; o < MT * 16 * 4; o += blockDim.x) {
+    const int token = o >> 2, c = (o & 3) * 2, to = blockIdx.x * 8 + c;
+    if (token >= p.tokens || to >= p.n) continue;
+    float2 sum[kW][1];
+#pragma unroll
+    for (int w = 0; w < kW; ++w) {
+      sum[w][0] = make_float2(0.f, 0.f);
+      for (int v = 0; v < warps; ++v) sum[w][0] = add2(sum[w][0], *reinterpret_cast<const float2*>(place(v, w, token, c)));
+    }
+    auto put = [&](const FfnRows& r, float2 v) { *reinterpret_cast<uint32_t*>(static_cast<unsigned char*>(r.data) + (token * r.row + to) * 2) = ffn_pack<BF16>(v.x, v.y); };
+    if constexpr (KIND == kFfnUp) {
+      if (p.gate.data != nullptr) {
+        put(p.gate, sum[0][0]);
+        put(p.up, sum[kW - 1][0]);
+      }
+      float2 a[1];
+      ffn_act_all<false>(p.act, sum[0], a, a);
+      put(p.out, mul2(a[0], sum[kW - 1][0]));
+    } else {
+      put(p.out, sum[0][0]);
+    }
+  }
+}
+
 // fp16: the largest finite |element| of dy, as the bits of its fp32 value, one for each block.
 __global__ void __launch_bounds__(256) ffn_peak_kernel(const void* dy, long long pitch, int rows, int cols, unsigned* peaks) {
   __shared__ unsigned s_top[8];
