@@ -34,9 +34,10 @@ int check_shape(const adacons_norm_shape* s) {
   return ADACONS_OK;
 }
 
-NormPlan plan_of(const adacons_norm_shape* s, int sms) {
+// Two groups a thread for rows that are moved in vectors; one where single elements are, whose loads otherwise wait for one another.
+NormPlan plan_of(const adacons_norm_shape* s, int sms, bool vec) {
   NormPlan n = {};
-  n.c = s->dim <= 256 ? 1 : s->dim <= 8192 ? 2 : 4;
+  n.c = s->dim <= (vec ? 256 : 4096) ? 1 : s->dim <= 8192 ? 2 : 4;
   const int wanted = (s->dim + kNormN * n.c - 1) / (kNormN * n.c);
   n.tpr = 32;
   while (n.tpr < wanted) n.tpr *= 2;
@@ -54,8 +55,12 @@ NormPlan plan_of(const adacons_norm_shape* s, int sms) {
 // Records of the sums over tokens: one row of `dim` for each item, and one for each block where `pre` has a gradient.
 int64_t item_records(const NormPlan& n) { return static_cast<int64_t>(n.groups) * n.parts; }
 int64_t workspace_bytes(const adacons_norm_shape* s, int sms) {
-  const NormPlan n = plan_of(s, sms);
-  return (item_records(n) + n.backward_blocks) * s->dim * static_cast<int64_t>(sizeof(float));
+  int64_t records = 0;
+  for (bool vec : {false, true}) {
+    const NormPlan n = plan_of(s, sms, vec);
+    records = std::max(records, item_records(n) + n.backward_blocks);
+  }
+  return records * s->dim * static_cast<int64_t>(sizeof(float));
 }
 
 // Strides of dimensions of size one are never used, whatever the caller has there.
@@ -156,20 +161,20 @@ int adacons_norm_forward(const adacons_norm_shape* s, const adacons_norm_rows* x
     return ADACONS_EINVAL;
   int sms = 0;
   if ((rc = device_sms(&sms)) != ADACONS_OK) return rc;
-  const NormPlan n = plan_of(s, sms);
-  NormParams p = base_params(s, n, f, gate, post, pre);
-  p.x = as_rows(x);
-  p.out = as_rows(to_out);
-  p.normed = as_rows(to_normed);
-  p.rows = rows;
   Vectors v(s);
   v.rows(x, s->stream_dtype, s->batch, s->len);
   v.rows(f, s->dtype, s->batch, s->len);
   v.rows(to_out, s->stream_dtype, s->batch, s->len);
   v.rows(to_normed, s->dtype, s->batch, s->len);
   v.rows(gate_rows, s->gate_dtype, gate_batch(s), gate_len(s));
-  v.gain(p.post.data);
-  v.gain(p.pre.data);
+  if (has_f) v.gain(post);
+  v.gain(pre);
+  const NormPlan n = plan_of(s, sms, v.ok);
+  NormParams p = base_params(s, n, f, gate, post, pre);
+  p.x = as_rows(x);
+  p.out = as_rows(to_out);
+  p.normed = as_rows(to_normed);
+  p.rows = rows;
   return go(s, p, n, v.ok, false, static_cast<cudaStream_t>(cuda_stream)) ? ADACONS_OK : ADACONS_ECUDA;
 }
 
@@ -222,7 +227,20 @@ int adacons_norm_backward(const adacons_norm_shape* s, const adacons_norm_rows* 
   if (same_place(to_f, dout) || same_place(to_gate, dout)) return ADACONS_EINVAL;
   int sms = 0;
   if ((rc = device_sms(&sms)) != ADACONS_OK) return rc;
-  const NormPlan n = plan_of(s, sms);
+  Vectors v(s);
+  v.rows(dout, s->stream_dtype, s->batch, s->len);
+  v.rows(dx, s->stream_dtype, s->batch, s->len);
+  if (has_pre) {
+    v.rows(out, s->stream_dtype, s->batch, s->len);
+    v.rows(dnormed, s->dtype, s->batch, s->len);
+  }
+  v.rows(has_f ? f : nullptr, s->dtype, s->batch, s->len);
+  v.rows(to_f, s->dtype, s->batch, s->len);
+  v.rows(gate_rows, s->gate_dtype, gate_batch(s), gate_len(s));
+  v.rows(to_gate, s->gate_dtype, gate_batch(s), gate_len(s));
+  if (has_f) v.gain(post);
+  v.gain(pre);
+  const NormPlan n = plan_of(s, sms, v.ok);
   const bool wants_sum = has_post || (has_gate && s->gate != ADACONS_NORM_GATE_TOKEN);
   if (wants_sum || pre != nullptr) {
     if (workspace == nullptr || bytes < workspace_bytes(s, sms)) return ADACONS_EINVAL;
@@ -245,19 +263,6 @@ int adacons_norm_backward(const adacons_norm_shape* s, const adacons_norm_rows* 
   p.blocks = n.backward_blocks;
   if (wants_sum) p.sums = static_cast<float*>(workspace);
   if (has_pre) p.pre_sums = static_cast<float*>(workspace) + item_records(n) * s->dim;
-  Vectors v(s);
-  v.rows(dout, s->stream_dtype, s->batch, s->len);
-  v.rows(dx, s->stream_dtype, s->batch, s->len);
-  if (has_pre) {
-    v.rows(out, s->stream_dtype, s->batch, s->len);
-    v.rows(dnormed, s->dtype, s->batch, s->len);
-  }
-  v.rows(has_f ? f : nullptr, s->dtype, s->batch, s->len);
-  v.rows(to_f, s->dtype, s->batch, s->len);
-  v.rows(gate_rows, s->gate_dtype, gate_batch(s), gate_len(s));
-  v.rows(to_gate, s->gate_dtype, gate_batch(s), gate_len(s));
-  v.gain(p.post.data);
-  v.gain(p.pre.data);
   if (!go(s, p, n, v.ok, true, st)) return ADACONS_ECUDA;
   if (!wants_sum && pre == nullptr) return ADACONS_OK;
   const dim3 grid(static_cast<unsigned>((s->dim + 31) / 32));

@@ -485,7 +485,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_backward_kernel(const No
   const bool has_dout = p.dout.data != nullptr, wants_sum = p.sums != nullptr;
   const bool by_token = p.gate_kind == kGateToken, by_sequence = p.gate_kind == kGateSequence;
   unsigned char* const ring = s_dyn + p.ring + threadIdx.x * 16;
-  float* s_fold = reinterpret_cast<float*>(s_dyn + p.ring);       // [kNormN][threads] where rows are shorter than a block: once a run's rows are through
+  float* s_fold = reinterpret_cast<float*>(s_dyn + p.ring);       // [C kNormN][threads] where rows are shorter than a block: once a run's rows are through
   const int row_bytes = p.vectors * kNormThreads * 16;
   auto ask = [&](long long r, long long end, int slot) {
     if constexpr (kRing) {
@@ -542,28 +542,35 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_backward_kernel(const No
   Norm8 acc[C], acc_pre[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) acc[c] = acc_pre[c] = norm_all(0.f);
-  // the threads that have the same columns in a block's other rows add up, in the rows' order
+  // what the threads of a block's rows have for the same columns, added in the rows' order
   auto leave = [&](Norm8 (&a)[C], float* record) {
+    if (per_block > 1) {
+      __syncthreads();
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      if (per_block > 1) {
-        __syncthreads();
+      for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int e = 0; e < kNormN; ++e) s_fold[e * kNormThreads + threadIdx.x] = a[c][e];
-        __syncthreads();
+        for (int e = 0; e < kNormN; ++e) s_fold[(c * kNormN + e) * kNormThreads + threadIdx.x] = a[c][e];
+      __syncthreads();
+      const int shift = 31 - __clz(p.tpr);
+      for (int k = threadIdx.x; k < C * kNormN * p.tpr; k += kNormThreads) {
+        const int t = k & (p.tpr - 1), ce = k >> shift, c = ce / kNormN, e = ce % kNormN;
+        float v = 0.f;
+        for (int g = 0; g < per_block; ++g) v += s_fold[ce * kNormThreads + g * p.tpr + t];
+        const int col = VEC ? (c * p.tpr + t) * kNormN + e : (c * kNormN + e) * p.tpr + t;
+        if (col < p.dim) record[col] = v;
       }
-      if (group == 0) {
+      __syncthreads();
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int e = 0; e < kNormN; ++e) {
-          float v = a[c][e];
-          for (int g = 1; g < per_block; ++g) v += s_fold[e * kNormThreads + g * p.tpr + threadIdx.x];
           const int col = cols.at(c, e);
-          if (col < p.dim) record[col] = v;
+          if (col < p.dim) record[col] = a[c][e];
         }
-      }
-      a[c] = norm_all(0.f);
     }
-    if (per_block > 1) __syncthreads();
+#pragma unroll
+    for (int c = 0; c < C; ++c) a[c] = norm_all(0.f);
   };
   for (int item = blockIdx.x; item < items; item += gridDim.x) {
     if (item != static_cast<int>(blockIdx.x)) {
@@ -590,13 +597,26 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_backward_kernel(const No
         norm_await(p.depth - 1);
         if (++slot == p.depth) slot = 0;
       }
-      // group c of a tensor's row, from the ring or from memory
+      // group c of a tensor's row, from the ring or from memory; with one group a thread (rows up to 4096 elements) all that comes from memory is asked for at once
+      constexpr bool kAtOnce = !kRing && C == 1;
+      NormRaw<X, VEC> raw_out, raw_dout;
+      NormRaw<F, VEC> raw_dh, raw_f;
+      if constexpr (kAtOnce) {
+        if (has_pre) {
+          norm_fetch(raw_out, static_cast<const X*>(norm_row<X>(p.out, b, s)), cols, 0);
+          norm_fetch(raw_dh, static_cast<const F*>(norm_row<F>(p.dnormed, b, s)), cols, 0);
+        }
+        if (has_dout) norm_fetch(raw_dout, static_cast<const X*>(norm_row<X>(p.dout, b, s)), cols, 0);
+        if (has_f) norm_fetch(raw_f, static_cast<const F*>(norm_row<F>(p.f, b, s)), cols, 0);
+      }
       auto x_row = [&](const NormRows& r, int first, int c, Norm8& to) {
-        if constexpr (kRing) norm_take<X>(from + (first + c * kX) * kNormThreads * 16, to);
+        if constexpr (kAtOnce) norm_get(first == kAtOut ? raw_out : raw_dout, to);
+        else if constexpr (kRing) norm_take<X>(from + (first + c * kX) * kNormThreads * 16, to);
         else norm_load<X, VEC>(to, norm_row<X>(r, b, s), cols, c);
       };
       auto f_row = [&](const NormRows& r, int first, int c, Norm8& to) {
-        if constexpr (kRing) norm_take<F>(from + (first + c * kF) * kNormThreads * 16, to);
+        if constexpr (kAtOnce) norm_get(first == kAtDh ? raw_dh : raw_f, to);
+        else if constexpr (kRing) norm_take<F>(from + (first + c * kF) * kNormThreads * 16, to);
         else norm_load<F, VEC>(to, norm_row<F>(r, b, s), cols, c);
       };
       Norm8 t[C];

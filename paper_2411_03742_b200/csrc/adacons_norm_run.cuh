@@ -29,7 +29,7 @@ bool norm_launch(NormParams p, const NormPlan& n, bool back, cudaStream_t st) {
     p.depth = static_cast<int>(std::max(1ll, std::min<long long>({4, (kNormShared - p.ring) / row, (turns * n.tpr + kNormThreads - 1) / kNormThreads})));
     shared += p.depth * row;
   }
-  if (back && kNormThreads > n.tpr) shared = std::max(shared, p.ring + kNormThreads * kNormN * static_cast<int>(sizeof(float)));
+  if (back && kNormThreads > n.tpr) shared = std::max(shared, p.ring + C * kNormThreads * kNormN * static_cast<int>(sizeof(float)));
   // Beyond what a kernel has without asking, its static part aside.  The same limit at every launch, whichever thread or device: it costs little beside one.
   if (shared > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNormShared) != cudaSuccess) {
     cudaGetLastError();
