@@ -23,7 +23,7 @@ namespace adacons {
 //
 // Tiles.  CG = 2: a pair of blocks (two SMs) shares a tile of 256 x 512, in two halves of 256 columns; each block holds 128 rows of the left operand, half of
 // the right one's and 128 rows of the result, all 512 columns of its tensor memory.  That takes 48 bytes from L2 a cycle and SM at the tensor
-// pipe's full rate; L2 gives 40 to 50, and tiles of 256 x 256 in two buffers, which take 64, kept the pipe 69 to 74 % busy.
+// pipe's full rate; L2 gives 40 to 50, and tiles of 256 x 256 in two buffers, which take 64, kept the pipe 69 to 74 % busy where these keep it 82 to 90 %.
 // One pair per two SMs walks through the tiles; one warp of each block copies operand stages by TMA, one thread of the even block issues the products,
 // eight warps work off what is complete, 32 rows x 32 columns at a time, which leave through shared memory by TMA (stored by the lanes, each at
 // its own row, they took three times as long as what is computed for them).  The products of a tile's first and last stages run half by half, so that one half is worked off, or
@@ -636,7 +636,7 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
 // their sums through shared memory in order.  A lane's 16 bytes of a weight row and of a token's row are the same eight K; which of a product's sixteen
 // places a K takes is the same on both sides, so they go into the warp's products as they were loaded, without a
 // turn through shared memory.  What the kernel before does not make, the first weights, is asked for while that one ends.
-// 16 tokens through 1024 x 4096: @@ us where tiles of 128 tokens take 19.5.
+// 16 tokens through 1024 x 4096: 11.9 us where tiles of 128 tokens take 19.5, one 10.7; 4096 x 10944, whose weights do not stay in L2, 84 and 74 us (3.2 and 3.6 TB/s).
 // ----------------------------------------------------------------------------------------------
 constexpr int kFfnFew = 64, kFfnFewWarps = 16;
 struct FfnFewParams {
