@@ -190,18 +190,20 @@ bool run(const FfnDevice& d, const adacons_ffn_shape* s, FfnParams* p, int n, co
 
 int steps_of(int k) { return (k + kFfnTK - 1) / kFfnTK; }
 
-// The forward pass of a few tokens.  Eight warps a block, or sixteen where that leaves each of them eight stages of 32 K or more.
+// Whether the forward pass goes by the kernel for a few tokens: where the weights stay in L2 it is the quicker one up to 32 tokens, elsewhere up to 4; the figures stand there.
+bool few_tokens(const adacons_ffn_shape* s) {
+  return s->tokens <= (6 * static_cast<int64_t>(s->dim) * s->hidden <= kFfnL2 ? kFfnFew : kFfnFewLong);
+}
+
+// Sixteen warps a block where there are few blocks and K leaves each of the warps eight stages of 32 or more, eight elsewhere, whose blocks end and begin beside one another
+// (1 x 1024 x 4096, 512 blocks and 128: 10.1 us, by eight alone 11.8, by sixteen 13.5; 1 x 4096 x 10944, 1368 blocks and 512: by eight 61.6 to 63.4, by sixteen 70.0).
 template <int KIND, bool BF16>
-bool run_few(const FfnFewParams& p, bool overlap, cudaStream_t st) {
-  const int warps = p.k >= 8 * 16 * 32 ? 16 : 8, sixteens = p.tokens <= 16 ? 1 : p.tokens <= 32 ? 2 : 4;
+bool run_few(const FfnDevice& d, const FfnFewParams& p, bool overlap, cudaStream_t st) {
+  const int warps = p.k >= 8 * 16 * 32 && (p.n + 7) / 8 <= 4 * d.info.sms ? 16 : 8, sixteens = p.tokens <= 16 ? 1 : 2;
   const size_t bytes = static_cast<size_t>(warps) * (KIND == kFfnUp ? 2 : 1) * sixteens * 16 * 8 * sizeof(float);
   const dim3 grid((p.n + 7) / 8), block(32 * warps);
   const LaunchKind kind = overlap ? kLaunchOverlap : kLaunchPlain;
-  if (bytes > 40 * 1024) {                       // the same limit at every launch
-    if (cudaFuncSetAttribute(ffn_few_kernel<KIND, BF16, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024) != cudaSuccess) { cudaGetLastError(); return false; }
-  }
-  if (sixteens == 1) return launch(&ffn_few_kernel<KIND, BF16, 1>, grid, block, bytes, st, kind, 1, p);
-  return sixteens == 2 ? launch(&ffn_few_kernel<KIND, BF16, 2>, grid, block, bytes, st, kind, 1, p) : launch(&ffn_few_kernel<KIND, BF16, 4>, grid, block, bytes, st, kind, 1, p);
+  return sixteens == 1 ? launch(&ffn_few_kernel<KIND, BF16, 1>, grid, block, bytes, st, kind, 1, p) : launch(&ffn_few_kernel<KIND, BF16, 2>, grid, block, bytes, st, kind, 1, p);
 }
 
 // Whether two matrices start at the same place: a result there would be written while other blocks still read.
@@ -261,7 +263,7 @@ int adacons_ffn_forward(const adacons_ffn_shape* s, const adacons_ffn_matrix* x,
   FfnDevice* d = nullptr;
   if ((rc = ffn_device(&d)) != ADACONS_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (s->tokens <= kFfnFew) {
+  if (few_tokens(s)) {
     FfnFewParams few = {};
     few.x = as_rows(x, s->dim, s->tokens);
     few.w[0] = as_rows(wg, s->dim, s->hidden);
@@ -279,8 +281,8 @@ int adacons_ffn_forward(const adacons_ffn_shape* s, const adacons_ffn_matrix* x,
     down.out = as_rows(out, s->dim, s->tokens);
     down.n = s->dim;
     down.k = s->hidden;
-    const bool ok = s->dtype == ADACONS_BF16 ? run_few<kFfnUp, true>(few, false, st) && run_few<kFfnPlain, true>(down, true, st)
-                                             : run_few<kFfnUp, false>(few, false, st) && run_few<kFfnPlain, false>(down, true, st);
+    const bool ok = s->dtype == ADACONS_BF16 ? run_few<kFfnUp, true>(*d, few, false, st) && run_few<kFfnPlain, true>(*d, down, true, st)
+                                             : run_few<kFfnUp, false>(*d, few, false, st) && run_few<kFfnPlain, false>(*d, down, true, st);
     return ok ? ADACONS_OK : ADACONS_ECUDA;
   }
   FfnParams p;

@@ -629,14 +629,17 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
 }
 
 // ----------------------------------------------------------------------------------------------
-// A few tokens (up to 64): the weights are what has to be read, 2 bytes for one or two products each, and what counts is how soon all of them are asked
-// for.  A block takes eight rows of the weights (Up: of both projections), its warps divide K among them, 32 at a time in turn, and add up
+// A few tokens (up to 32): the weights are what has to be read, 2 bytes for one or two products each, and what counts is how soon all of them are asked
+// for.  A block takes eight rows of the weights (Up: of both projections), its warps divide K among them, up to 128 at a time in turn, and add up
 // their sums through shared memory in order.  A lane's 16 bytes of a weight row and of a token's row are the same eight K; which of a product's sixteen
 // places a K takes is the same on both sides, so they go into the warp's products as they were loaded, without a
 // turn through shared memory.  What the kernel before does not make, the first weights, is asked for while that one ends.
-// 16 tokens through 1024 x 4096: 11.9 us where tiles of 128 tokens take 19.5, one 10.7; 4096 x 10944, whose weights do not stay in L2, 84 and 74 us (3.2 and 3.6 TB/s).
+// 1024 x 4096: one token 10.1 us, 16 11.8, 32 16.1 where tiles of 128 tokens take 19.5; 2048 x 8192, 101 MB of weights: 16 31.2, 32 42.1, tiles 42.6.  Weights that do not
+// stay in L2 (4096 x 10944, 269 MB): one 63.4 (4.2 TB/s), eight 73.1, tiles 68.5.  Blocks that go on from tile to tile with the next tile's weights under way were slower
+// (12.4 us, 15.1 and 77.0): a block's join then holds up its own next products, where now another block's go on.
 // ----------------------------------------------------------------------------------------------
-constexpr int kFfnFew = 64, kFfnFewWarps = 16;
+constexpr int kFfnFew = 32, kFfnFewLong = 4, kFfnFewWarps = 16;
+constexpr long long kFfnL2 = 126ll << 20;
 struct FfnFewParams {
   FfnRows x, w[2], out, gate, up;                // w: rows of weights; Plain: one
   int tokens, n, k, act;
@@ -673,19 +676,19 @@ __global__ void __launch_bounds__(32 * kFfnFewWarps) ffn_few_kernel(const FfnFew
   auto ask = [&](int k0) {
 #pragma unroll
     for (int d = 0; d < kDeep; ++d) {
-      const int k = k0 + d * warps * 32 + at;
+      const int k = k0 + d * 32 + at;
 #pragma unroll
       for (int w = 0; w < kW; ++w) weights[d][w] = k < p.k && col < p.n ? ld_stream_v4(ffn_at(p.w[w], col, k)) : none;
     }
   };
-  int k0 = warp * 32;
+  int k0 = warp * kDeep * 32;
   ask(k0);
   pdl_wait();
   for (; k0 < p.k; k0 += kDeep * warps * 32) {
     uint4 x[kDeep][MT][2], now[kDeep][kW];
 #pragma unroll
     for (int d = 0; d < kDeep; ++d) {
-      const int k = k0 + d * warps * 32 + at;
+      const int k = k0 + d * 32 + at;
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
