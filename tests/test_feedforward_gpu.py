@@ -94,6 +94,13 @@ def test_sizes(T, D, F, dtype):
     check(T, D, F, "silu" if D > 600 else "gelu", dtype)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T, D, F", [(7, 2048, 5464), (24, 1024, 4096), (31, 4104, 520), (32, 2056, 6152), (33, 1024, 4096), (4, 4096, 10944), (5, 4096, 10944)])
+def test_few_tokens(T, D, F, dtype):
+    """The kernel for single tokens: several blocks on an SM, eight and sixteen warps, one and two sixteens of tokens, and beside it the tiles that take over."""
+    check(T, D, F, "gelu_tanh", dtype)
+
+
 def test_long():
     check(4100, 2048, 5464, "gelu")
 

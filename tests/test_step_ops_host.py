@@ -26,6 +26,15 @@ def test_every_declared_function_is_exported_and_has_a_prototype(lib):
         assert len(getattr(lib, name).argtypes) == args.count(",") + 1, name
 
 
+def test_loads_stay_behind_their_guards():
+    """A load in an asm statement without `volatile` may be moved in front of the branch that guards it, to an address that does not exist."""
+    folder = os.path.join(ROOT, "paper_2411_03742_b200", "csrc")
+    for name in sorted(os.listdir(folder)):
+        if name.endswith((".cu", ".cuh")):
+            for asm in re.findall(r"\basm\s*\(([^;]*);", open(os.path.join(folder, name)).read()):
+                assert not re.search(r"\b(ld|ldmatrix|multimem)\b", asm), (name, asm[:80])
+
+
 # ---- norms ----------------------------------------------------------------------------------------------
 def _norm(lib, data=AT, apart=1 << 16, pre=AT + (1 << 19), post=AT + (1 << 18), rows=1 << 30, **change):
     from paper_2411_03742_b200.norms import _Rows, _Shape
