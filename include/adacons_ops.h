@@ -214,6 +214,7 @@ int adacons_norm_backward(const adacons_norm_shape *shape, const adacons_norm_ro
  * An entry is there when its index lies in 0 .. vocab-1 (any other says that it is not) and its logit is not -inf.  A token without
  * entries has no first term, one without a label in 0 .. vocab-1 no second; one without either has loss 0 and a gradient of zeros, and its
  * logits are not read.  The same index may come several times: each time counts.  Logits of -inf have probability 0.
+ * Exponentials are fp32 and those below 2^-126 count as 0; gradients of bf16 and fp32 logits that small are 0 then.
  */
 typedef struct adacons_distill_matrix {   /* (token, column): stride in elements, any value; not looked at for one token.  Columns are 1 apart. */
   void *data;

@@ -22,11 +22,12 @@ namespace adacons {
 // both s times something that does not depend on the token, so one running sum per column serves both.
 //
 // Bound by memory: every element is read and written once.  A block of 512 threads, one an SM, holds one row or several: a row belongs to `tpr` of them, each with one or
-// two groups of kNormN neighbours (a warp up to 512 elements, 256 threads for 4096).  The gradient at 4096 elements, fp32 stream, 32,768 tokens: 0.56 ms, 4.3 TB/s; with one group
-// and 1024 threads 0.91 (the instructions around 8 elements are more than for them), with four groups and 256 threads 0.57; forward 0.27 ms, 0.31 and 0.34.  What holds it below
-// the copy rate, 6.6 TB/s, is a row's chain through two sums with 16 warps to cover it.  The gains lie in shared memory as fp32, multiplied with
-// what else does not change.  The next rows are on their way meanwhile, by asynchronous copies of 16 bytes into places of shared memory that only the thread
-// that asked for them reads, so that nothing waits for another thread (D up to 8192; beyond, a row fills shared memory, and
+// two groups of kNormN neighbours (a warp up to 512 elements, 256 threads for 4096).  The gradient at 4096 elements, fp32 stream, 32,768 tokens: 0.51 ms, 4.7 TB/s; when every fp32 sector was asked for
+// twice (see norm_ask) 0.56, and then with one group and 1024 threads 0.91 (the instructions around 8 elements are more than for them), with four groups and 256 threads 0.57;
+// forward, bf16, 0.27 ms, 0.31 and 0.34.  What holds it below the copy rate, 6.6 TB/s, is that a row's loads go out in one burst, which takes as long as the row's two sums: asked for
+// piece by piece between them they come too late (0.62), and rows brought into L2 before do not help (0.60).  The gains lie in shared memory as fp32, multiplied with
+// what else does not change.  The next rows are on their way meanwhile, by asynchronous copies of 16 bytes into places of shared memory that only threads
+// of the same warp read, so that nothing waits for another warp (D up to 8192; beyond, a row fills shared memory, and
 // rows of odd sizes or strides are loaded element by element).  Means are sums in fp32 by shuffles and one shared-memory exchange, in a fixed order.
 // The sums over tokens are kept in registers by every thread for its columns, leave as one record per block, and a second
 // launch adds the records in order: no atomics.
@@ -163,8 +164,15 @@ __device__ __forceinline__ void norm_store(T* row, const NormColumns<VEC>& cols,
     if (!cols.has(c)) return;
     T* to = row + cols.at(c, 0);
     if constexpr (sizeof(T) == 4) {
+      uint4 v[2];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) *reinterpret_cast<float4*>(to + 4 * k) = make_float4(f[4 * k], f[4 * k + 1], f[4 * k + 2], f[4 * k + 3]);
+      for (int k = 0; k < 2; ++k) v[k] = make_uint4(__float_as_uint(f[4 * k]), __float_as_uint(f[4 * k + 1]), __float_as_uint(f[4 * k + 2]), __float_as_uint(f[4 * k + 3]));
+      if ((reinterpret_cast<uintptr_t>(to) & 31) == 0) {       // whole sectors
+        st_global_v8(to, v[0], v[1], 0ull);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) *reinterpret_cast<uint4*>(to + 4 * k) = v[k];
+      }
     } else {
       *reinterpret_cast<uint4*>(to) = make_uint4(NormPair<T>::pack(f[0], f[1]), NormPair<T>::pack(f[2], f[3]), NormPair<T>::pack(f[4], f[5]), NormPair<T>::pack(f[6], f[7]));
     }
@@ -188,12 +196,21 @@ __device__ __forceinline__ void norm_await(int pending) {      // until all but 
   else if (pending == 2) asm volatile("cp.async.wait_group 2;" ::: "memory");
   else asm volatile("cp.async.wait_group 3;" ::: "memory");
 }
-// A thread's places for one row: vector v is kNormThreads * 16 bytes behind vector 0.
+// A thread's places for one row: vector v is kNormThreads * 16 bytes behind vector 0.  Of fp32 rows a warp's copies follow one another, 512 bytes an instruction, each into the
+// place of the thread that wants it: two halves of a thread's own 32 bytes would ask for every sector twice (the gradient of a 4096-element fp32 stream 560 us, 511 like this).  So a row is
+// complete for a thread when its warp has waited and met.
 template <typename T>
-__device__ __forceinline__ void norm_ask(unsigned char* to, const T* from, bool there) {        // `from`: the thread's first element
-  if (!there) return;
+__device__ __forceinline__ void norm_ask(unsigned char* to, const T* row, const NormColumns<true>& cols, int c) {
+  if constexpr (sizeof(T) == 2) {
+    if (cols.has(c)) norm_copy(to, row + cols.at(c, 0));
+  } else {
+    const int lane = threadIdx.x & 31, first = cols.at(c, 0) - lane * kNormN;
 #pragma unroll
-  for (int k = 0; k < NormRaw<T, true>::kVectors; ++k) norm_copy(to + k * kNormThreads * 16, from + k * (16 / static_cast<int>(sizeof(T))));
+    for (int k = 0; k < 2; ++k) {
+      const int vector = k * 32 + lane, owner = vector >> 1;
+      if (first + owner * kNormN < cols.dim) norm_copy(to + (owner - lane) * 16 + (vector & 1) * kNormThreads * 16, row + first + vector * 4);
+    }
+  }
 }
 // Places of groups outside the row hold zeros from the start (norm_clear) and are never written.
 template <typename T>
@@ -371,23 +388,19 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_forward_kernel(const Nor
   const int row_bytes = p.vectors * kNormThreads * 16;
   auto ask = [&](long long r, int slot) {
     if constexpr (kRing) {
+      __syncwarp();                              // the slot's last row is read
       if (r < p.tokens) {
         const int b = p.by_len.divide(static_cast<int>(r)), s = static_cast<int>(r) - b * p.len;
         unsigned char* to = ring + slot * row_bytes;
-        const X* x = norm_row<X>(p.x, b, s) + cols.at(0, 0);
+        auto all = [&](const auto* from, int first, int each) {
 #pragma unroll
-        for (int c = 0; c < C; ++c) norm_ask(to + c * kX * kNormThreads * 16, x + c * p.tpr * kNormN, cols.has(c));
-        if (has_f) {
-          const F* f = norm_row<F>(p.f, b, s) + cols.at(0, 0);
-#pragma unroll
-          for (int c = 0; c < C; ++c) norm_ask(to + (kAtF + c * kF) * kNormThreads * 16, f + c * p.tpr * kNormN, cols.has(c));
-        }
+          for (int c = 0; c < C; ++c) norm_ask(to + (first + c * each) * kNormThreads * 16, from, cols, c);
+        };
+        all(norm_row<X>(p.x, b, s), 0, kX);
+        if (has_f) all(norm_row<F>(p.f, b, s), kAtF, kF);
         if (by_token) {
-#pragma unroll
-          for (int c = 0; c < C; ++c) {
-            if (p.gate_as.wide) norm_ask(to + (kAtGate + c * 2) * kNormThreads * 16, norm_row<float>(p.gate, b, s) + cols.at(c, 0), cols.has(c));
-            else norm_ask(to + (kAtGate + c * kF) * kNormThreads * 16, norm_row<F>(p.gate, b, s) + cols.at(c, 0), cols.has(c));
-          }
+          if (p.gate_as.wide) all(norm_row<float>(p.gate, b, s), kAtGate, 2);
+          else all(norm_row<F>(p.gate, b, s), kAtGate, kF);
         }
       }
       norm_close();
@@ -412,6 +425,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_forward_kernel(const Nor
     if constexpr (kRing) {
       ask(at + (p.depth - 1) * step, slot == 0 ? p.depth - 1 : slot - 1);
       norm_await(p.depth - 1);
+      __syncwarp();
       if (++slot == p.depth) slot = 0;
     }
 #pragma unroll
@@ -490,12 +504,13 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_backward_kernel(const No
   const int row_bytes = p.vectors * kNormThreads * 16;
   auto ask = [&](long long r, long long end, int slot) {
     if constexpr (kRing) {
+      __syncwarp();                              // the slot's last row is read
       if (r < end) {
         const int b = p.by_len.divide(static_cast<int>(r)), s = static_cast<int>(r) - b * p.len;
         unsigned char* to = ring + slot * row_bytes;
         auto all = [&](const auto* from, int first, int each) {
 #pragma unroll
-          for (int c = 0; c < C; ++c) norm_ask(to + (first + c * each) * kNormThreads * 16, from + cols.at(c, 0), cols.has(c));
+          for (int c = 0; c < C; ++c) norm_ask(to + (first + c * each) * kNormThreads * 16, from, cols, c);
         };
         if (has_dout) all(norm_row<X>(p.dout, b, s), 0, kX);
         if (has_pre) {
@@ -596,6 +611,7 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_backward_kernel(const No
       if constexpr (kRing) {
         ask(at + static_cast<long long>(p.depth - 1) * per_block, end, slot == 0 ? p.depth - 1 : slot - 1);
         norm_await(p.depth - 1);
+        __syncwarp();
         if (++slot == p.depth) slot = 0;
       }
       // group c of a tensor's row, from the ring or from memory; with one group a thread (rows up to 4096 elements) all that comes from memory is asked for at once
