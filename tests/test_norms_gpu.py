@@ -172,6 +172,33 @@ def test_slices_of_wider_rows_and_two_dimensions(wide):
     both(odd)
 
 
+@pytest.mark.parametrize("dtype, gate", [("bf16", "token"), ("f32", "token"), ("f16", "sequence")])
+@pytest.mark.parametrize("D", [8, 264, 520, 1000, 4096, 8184])
+def test_fp32_rows_on_16_bytes(D, dtype, gate):
+    """Rows of an fp32 stream that start on 16 bytes but not on 32 and end inside what a warp moves at once; results there too, the same bits, nothing around them touched."""
+    from paper_2411_03742_b200 import residual_norm_backward, residual_norm_forward
+    m = make((3, 167, D), dtype, "f32", gate)
+
+    def moved(t, fill=None):
+        if t is None or t.dim() != 3 or t.dtype != torch.float32:
+            return t
+        room = torch.full((*t.shape[:-1], D + 12), 7.0, device="cuda")
+        room[..., 4:-8] = t if fill is None else fill
+        return room[..., 4:-8]
+
+    a, b = both(m, "tanh"), both({k: moved(v) for k, v in m.items()}, "tanh")
+    for one, two in zip((*a[0], *a[1]), (*b[0], *b[1])):
+        assert torch.equal(one, two)
+    how = {"gate": m["gate"], "gate_by": "tanh", "post": m["post"], "scale": 0.7, "pre": m["pre"], "eps": 1e-5}
+    to = [moved(t, 0.0) for t in (a[0][0], a[1][0])]
+    residual_norm_forward(m["x"], m["f"], out=to[0], **how)
+    residual_norm_backward(m["dout"], m["dnormed"], a[0][0], m["f"], a[0][2], dx=to[1], **how)
+    for t, want in zip(to, (a[0][0], a[1][0])):
+        assert torch.equal(t, want)
+        room = t._base
+        assert bool((room[..., :4] == 7).all()) and bool((room[..., -8:] == 7).all())
+
+
 def test_time_first_memory():
     m = make((4, 50, 136), gate="sequence")
     turned = {k: v.transpose(0, 1).contiguous().transpose(0, 1) if v is not None and v.dim() == 3 else v for k, v in m.items()}
