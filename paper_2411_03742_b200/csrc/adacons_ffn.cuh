@@ -27,7 +27,8 @@ namespace adacons {
 // One pair per two SMs walks through the tiles; one warp of each block copies operand stages by TMA, one thread of the even block issues the products,
 // eight warps work off what is complete, 32 rows x 32 columns at a time, which leave through shared memory by TMA (stored by the lanes, each at
 // its own row, they took three times as long as what is computed for them).  The products of a tile's first and last stages run half by half, so that one half is worked off, or
-// freed, beside the other's products.  The last tiles are halves where that evens out the pairs' work.  CG = 1: tiles of 128 x 128, one block each and two blocks an SM,
+// freed, beside the other's products.  The last tiles are halves where that evens out the pairs' work, and all are where K is short against the
+// ending: then the two accumulators take turns.  CG = 1: tiles of 128 x 128, one block each and two blocks an SM,
 // for problems whose larger tiles would leave SMs idle; the blocks of a cluster may share one tile's K and add up their sums, in order, through one another's
 // shared memory.  Sums are fp32 throughout; g, u, h, dg and du are rounded to the tensors' type once, as operands.
 // fp16 holds dg and du times 2^k, with 2^k from dy's largest element, so that small or large gradients do not leave its range; the products
@@ -411,7 +412,8 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
       const bool issuer = elect_one();
       const uint32_t base = (smem_addr(smem) & 0x3ffffu) >> 4;             // descriptors count 16-byte units; above are a cluster block's number and their other fields
       int stage = 0;
-      uint32_t parity = 0, free_parity[2] = {1u, 1u};
+      uint32_t parity = 0, free_parity = 3u;     // of accumulator a: bit a
+      int turn = 0;                              // the accumulator of the next half by itself: they take turns
       bool ok = true;
       for (int t = worker; ok && t < p.tiles; t += workers) {
         const FfnSpot s = ffn_spot<CG>(p, t);
@@ -419,7 +421,8 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
         const FfnProblem& q = p.problem[s.problem];
         int begin, end;
         steps_of(q, begin, end);
-        const int steps = end - begin;
+        const int steps = end - begin, acc0 = s.halves == 1 ? turn : 0;
+        if (CG == 2 && s.halves == 1) turn ^= 1;
         const uint32_t idesc = mma_idesc(kTM, kTN, BF16, false, false) | (q.a_across ? 1u << 15 : 0u) | (q.b_across ? 1u << 16 : 0u);
         const uint64_t a_base = q.a_across ? desc_mnmajor(0, 8192) : desc_kmajor(0), b_base = q.b_across ? desc_mnmajor(0, 8192) : desc_kmajor(0);
         const uint32_t a_step = q.a_across ? 2048 / 16 : 32 / 16, b_step = q.b_across ? 2048 / 16 : 32 / 16;
@@ -432,7 +435,7 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
           const uint64_t a = a_base + (base + at * (T::kStage >> 4)), b = b_base + (base + at * (T::kStage >> 4) + (1 + half) * (kFfnOperand >> 4));
           if (issuer) {
 #pragma unroll
-            for (int kk = 0; kk < kFfnTK / 16; ++kk) mma_ss<CG>(tmem + half * kTN, a + kk * a_step, b + kk * b_step, idesc, kk != 0 || !first ? 1u : 0u);
+            for (int kk = 0; kk < kFfnTK / 16; ++kk) mma_ss<CG>(tmem + (acc0 + half) * kTN, a + kk * a_step, b + kk * b_step, idesc, kk != 0 || !first ? 1u : 0u);
           }
           __syncwarp();
         };
@@ -444,8 +447,8 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
         auto by_halves = [&](int count, bool opens, bool closes) {
           for (int half = 0; half < s.halves; ++half) {
             if (opens) {
-              if (!get(&acc_free[half], free_parity[half])) return;
-              free_parity[half] ^= 1u;
+              if (!get(&acc_free[acc0 + half], (free_parity >> (acc0 + half)) & 1u)) return;
+              free_parity ^= 1u << (acc0 + half);
             }
             int at = stage;
             uint32_t phase = parity;
@@ -456,7 +459,7 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
               if (half == s.halves - 1) commit(&empty[at]);
               if (++at == stages) { at = 0; phase ^= 1u; }
             }
-            if (closes) commit(&acc_full[half]);
+            if (closes) commit(&acc_full[acc0 + half]);
             if (half == s.halves - 1) { stage = at; parity = phase; }
           }
         };
@@ -478,7 +481,8 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     constexpr int kShare = kCols / (kFfnEndWarps / 4);       // columns of a warp
     const int side = warp >> 2;                  // which of them
-    uint32_t parity[2] = {0u, 0u};
+    uint32_t parity = 0u;                        // of accumulator a: bit a
+    int turn = 0;
     // a lone block's products have all read their stages by the time anything is put there
     FfnWay way = {smem + (CG == 2 ? stages * T::kStage + 512 : 0u) + warp * 2 * kFfnPatch, 0};
     pdl_wait();
@@ -491,6 +495,8 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
       const int row0 = s.i * kTM + side_of_pair * 128 + (warp & 3) * 32, row = row0 + lane;
       const float factor = KIND == kFfnBack ? ffn_power(exponent) : q.scaled ? ffn_power(-exponent) : 1.f;
       const bool there = row < q.m;
+      const int acc0 = s.halves == 1 ? turn : 0;
+      if (CG == 2 && s.halves == 1) turn ^= 1;
 #pragma unroll 1
       for (int half = 0; half < s.halves; ++half) {
         const int col0 = (s.j + half) * kCols + side * kShare;
@@ -499,11 +505,11 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
           ffn_get<32>(gate, p.gate, row, col0, q.n, there);
           ffn_get<32>(up, p.up, row, col0, q.n, there);
         }
-        const bool got = !s_abort && mbar_wait_bounded(&acc_full[half], parity[half]);
+        const bool got = !s_abort && mbar_wait_bounded(&acc_full[acc0 + half], (parity >> (acc0 + half)) & 1u);
         if (!__all_sync(0xffffffffu, got)) { s_abort = 1; ok = false; break; }
-        parity[half] ^= 1u;
+        parity ^= 1u << (acc0 + half);
         tc_fence_after();
-        const uint32_t acc = tmem + half * kTN + side * kShare + lanes;
+        const uint32_t acc = tmem + (acc0 + half) * kTN + side * kShare + lanes;
         if (shares == 1) {
 #pragma unroll 1
           for (int c = 0; c < kShare && row0 < q.m; c += 32) {
@@ -540,7 +546,7 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
           }
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) { if (CG == 2) mbar_arrive_leader(&acc_free[half]); else mbar_arrive_one(&acc_free[half]); }
+          if (lane == 0) { if (CG == 2) mbar_arrive_leader(&acc_free[acc0 + half]); else mbar_arrive_one(&acc_free[acc0 + half]); }
           __syncwarp();
         } else {                                 // this block's sums, where the stages were: all products that read those are complete
           float* sums = reinterpret_cast<float*>(smem) + ((warp & 3) * 32 + lane) * kFfnSumRow + side * 64;
