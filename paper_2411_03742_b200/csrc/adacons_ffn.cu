@@ -154,10 +154,11 @@ bool run(const FfnParams& p, int blocks, int cluster, bool overlap, cudaStream_t
 }
 
 // Whether all tiles of pairs go as halves by themselves, whose two accumulators take turns, so that one half's ending runs beside the next one's products; a whole tile's two
-// endings have little beside them.  A half's ending takes about 14,500 cycles (Back: two matrices read, three written), 8000 (Up) or 5000.
-// 4096 x 1024 x 4096 (16 stages) gradient 208 -> 201.5 us with silu, 212 -> 206 with gelu; 8192 x 4096 x 10944 (64) 3474 -> 3386; whole tiles share a stage's left operand, 540 cycles for 720.
+// endings have little beside them, but it shares a stage's left operand (540 cycles for 720).  A half's ending takes about 12,500 cycles (Back: two matrices read, three written;
+// 14,500 with gelu), 8000 (Up) or 5000.  Gradient of 8192 x 512 x 2048 (8 stages) 145 -> 139 us, 4096 x 1024 x 4096 (16) 200 -> 190.5, 2048 x 2048 x 8192 (32) 375 -> 364; with 64
+// stages, 4096 x 4096 x 10944, 1527 -> 1543.
 bool by_halves(int kind, int problems, const FfnProblem& q) {
-  const double ending = kind == kFfnBack ? 14500.0 : kind == kFfnUp ? 8000.0 : 5000.0, steps = static_cast<double>(q.steps) * q.segments;
+  const double ending = kind == kFfnBack ? 12500.0 : kind == kFfnUp ? 8000.0 : 5000.0, steps = static_cast<double>(q.steps) * q.segments;
   return problems == 1 && 2 * std::max(720.0 * steps, ending) < 1080.0 * steps + 2 * ending - 4000.0;
 }
 
@@ -183,8 +184,9 @@ bool run(const FfnDevice& d, const adacons_ffn_shape* s, FfnParams* p, int n, co
   const bool bf16 = s->dtype == ADACONS_BF16;
   if (plan.cg == 2) {
     // a last round in which at most half of the pairs would have a tile: halves, for all
-    const int rest = by_halves(KIND, n, p->problem[0]) ? p->wholes : p->wholes % d.pairs;
-    if (rest == p->wholes || 2 * rest <= d.pairs) {
+    const bool all = by_halves(KIND, n, p->problem[0]);
+    const int rest = all ? p->wholes : p->wholes % d.pairs;
+    if (all || 2 * rest <= d.pairs) {
       p->wholes -= rest;
       p->tiles += rest;
     }
