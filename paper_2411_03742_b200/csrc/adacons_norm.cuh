@@ -24,8 +24,8 @@ namespace adacons {
 // Bound by memory: every element is read and written once.  A block of 512 threads, one an SM, holds one row or several: a row belongs to `tpr` of them, each with one or
 // two groups of kNormN neighbours (a warp up to 512 elements, 256 threads for 4096).  The gradient at 4096 elements, fp32 stream, 32,768 tokens: 0.51 ms, 4.7 TB/s; when every fp32 sector was asked for
 // twice (see norm_ask) 0.56, and then with one group and 1024 threads 0.91 (the instructions around 8 elements are more than for them), with four groups and 256 threads 0.57;
-// forward, bf16, 0.27 ms, 0.31 and 0.34.  What holds it below the copy rate, 6.6 TB/s, is that a row's loads go out in one burst, which takes as long as the row's two sums: asked for
-// piece by piece between them they come too late (0.62), and rows brought into L2 before do not help (0.60).  The gains lie in shared memory as fp32, multiplied with
+// forward, bf16, 0.27 ms, 0.31 and 0.34.  What holds it below the copy rate, 6.6 TB/s, is that a row's loads go out in one burst, 4300 to 5000 of its 10,000 cycles: asked for
+// piece by piece between the sums they come too late (0.62), rows brought into L2 before do not help (0.60), nor does one exchange for both sums (0.51).  The gains lie in shared memory as fp32, multiplied with
 // what else does not change.  The next rows are on their way meanwhile, by asynchronous copies of 16 bytes into places of shared memory that only threads
 // of the same warp read, so that nothing waits for another warp (D up to 8192; beyond, a row fills shared memory, and
 // rows of odd sizes or strides are loaded element by element).  Means are sums in fp32 by shuffles and one shared-memory exchange, in a fixed order.
