@@ -274,8 +274,9 @@ int adacons_ffn_forward(const adacons_ffn_shape *shape, const adacons_ffn_matrix
                         int64_t workspace_bytes, void *cuda_stream);
 
 /* The gradients of x and the weights from that of y (dout) and the forward pass's gate and up; written, not added to.  One without data is not made.
- * ADACONS_F16 holds the gradients of gate and up times a power of two, taken from dout's largest finite element, so that small or large ones stay in
- * the type's range between the products.  No tokens: the weights' gradients are zeros.  Errors: as the forward pass. */
+ * ADACONS_F16 holds the gradients of gate and up (of all tokens) times one power of two between the products: 1, or the one that brings dout's largest finite
+ * element to [1/2, 1) where that is smaller; a smaller one, possibly below 1, only where a finite gradient of gate or up would round to infinity, and then the largest
+ * that keeps all of them finite.  Held values below 2^-14 have steps of 2^-24.  No tokens: the weights' gradients are zeros.  Errors: as the forward pass. */
 int adacons_ffn_backward(const adacons_ffn_shape *shape, const adacons_ffn_matrix *dout, const adacons_ffn_matrix *x, const adacons_ffn_matrix *w_gate,
                          const adacons_ffn_matrix *w_up, const adacons_ffn_matrix *w_down, const adacons_ffn_matrix *gate, const adacons_ffn_matrix *up,
                          const adacons_ffn_matrix *dx, const adacons_ffn_matrix *dw_gate, const adacons_ffn_matrix *dw_up, const adacons_ffn_matrix *dw_down,

@@ -118,7 +118,7 @@ int64_t up_to(int64_t n, int64_t unit) { return (n + unit - 1) / unit * unit; }
 // A matrix (tokens x hidden) of the workspace
 int64_t hidden_bytes(const adacons_ffn_shape* s) { return up_to(static_cast<int64_t>(s->tokens) * s->hidden * 2, 256); }
 int64_t workspace_bytes(const adacons_ffn_shape* s, bool back) {
-  return back ? 3 * hidden_bytes(s) + (s->dtype == ADACONS_F16 ? static_cast<int64_t>(kFfnPeaks) * 4 : 0) : hidden_bytes(s);
+  return back ? 3 * hidden_bytes(s) + (s->dtype == ADACONS_F16 ? static_cast<int64_t>(kFfnWords) * 4 : 0) : hidden_bytes(s);
 }
 
 struct FfnPlan { int cg, shares; double time; };
@@ -363,6 +363,7 @@ int adacons_ffn_backward(const adacons_ffn_shape* s, const adacons_ffn_matrix* d
       !make_map(*d, &p.maps[kX], s, x->data, x->row_stride, s->tokens, s->dim) || !make_map(*d, &p.maps[kH], s, h, s->hidden, s->tokens, s->hidden))
     return ADACONS_ECUDA;
   p.peaks = peaks;
+  p.beyond = peaks == nullptr ? nullptr : peaks + kFfnPeaks;
   p.gate = as_rows(gate, s->hidden, s->tokens);
   p.up = as_rows(up, s->hidden, s->tokens);
   p.dgate = as_rows(dg, s->hidden, s->hidden, s->tokens);
@@ -381,6 +382,11 @@ int adacons_ffn_backward(const adacons_ffn_shape* s, const adacons_ffn_matrix* d
   if (!make_out(*d, &p.outs[0], s, p.dgate, s->tokens, s->hidden) || !make_out(*d, &p.outs[1], s, p.dup, s->tokens, s->hidden) ||
       !make_out(*d, &p.outs[2], s, q.out, s->tokens, s->hidden) || !run<kFfnBack>(*d, s, &p, 1, plan_of(*d, p.problem, 1, 1), peaks != nullptr, st))
     return ADACONS_ECUDA;
+  if (peaks != nullptr) {                        // once more where dg or du do not fit, with a factor that makes them
+    p.beyond = nullptr;
+    p.again = 1;
+    if (!run<kFfnBack>(*d, s, &p, 1, plan_of(*d, p.problem, 1, 1), true, st)) return ADACONS_ECUDA;
+  }
   // dx, and the weights' gradients
   FfnProblem by_x = {}, by_w[3];
   int weights = 0;

@@ -31,8 +31,11 @@ namespace adacons {
 // ending: then the two accumulators take turns.  CG = 1: tiles of 128 x 128, one block each and two blocks an SM,
 // for problems whose larger tiles would leave SMs idle; the blocks of a cluster may share one tile's K and add up their sums, in order, through one another's
 // shared memory.  Sums are fp32 throughout; g, u, h, dg and du are rounded to the tensors' type once, as operands.
-// fp16 holds dg and du times 2^k, with 2^k from dy's largest element, so that small or large gradients do not leave its range; the products
-// that they go into are divided by it again.
+// fp16 holds dg and du times 2^k; the products that they go into are divided by it again.  k is 0, or brings dy's largest element to [1/2, 1) where that is smaller, so that small
+// gradients keep their bits.  How much larger than dy the products are is known once they are there: if dg or du round to infinity, the first product notes the largest of them and is
+// made again with the k, possibly below 0, that just holds it; otherwise its second launch returns at once (231 x 520 x 1368
+// 31.4 -> 32.8 us, 4096 x 1024 x 4096 195 -> 197.5; made again, 43 and 298).  So no token has fewer bits than without a factor, unless
+// dg or du were infinite then (bringing the largest element down to 1 in any case left tokens with 1e-3 beside one with 3000 half of their dx).
 // ----------------------------------------------------------------------------------------------
 constexpr int kFfnTK = 64;                       // K elements per stage: one 128-byte swizzled row
 constexpr uint32_t kFfnOperand = 128 * kFfnTK * 2;             // of a block: 128 rows of an operand
@@ -51,7 +54,9 @@ static_assert(128 * kFfnSumRow * 4 <= kFfnCrowdStages * FfnTiling<1>::kStage, "p
 static_assert(FfnTiling<2>::bytes(kFfnPairStages) <= 227 * 1024 && FfnTiling<1>::bytes(kFfnLoneStages) <= 227 * 1024 && FfnTiling<1>::bytes(kFfnCrowdStages) <= 112 * 1024,
               "shared memory of a block");
 constexpr int kFfnGroup = 8;                     // rows of tiles that are walked through together: their operands stay in L2
-constexpr int kFfnPeaks = 128;                   // blocks that look for dy's largest element
+constexpr int kFfnPeaks = 127;                   // blocks that look for dy's largest element
+constexpr int kFfnWords = kFfnPeaks + 1;         // what they find, then the largest of dg and du that rounds to infinity as it is held (0: none)
+constexpr float kFfnBeyond = 65520.f;            // rounds to infinity in fp16, as all above it
 
 enum FfnKind { kFfnUp = 0, kFfnBack = 1, kFfnPlain = 2 };
 enum FfnAct { kActSilu = 0, kActGelu = 1, kActGeluTanh = 2, kActRelu = 3 };
@@ -80,7 +85,9 @@ struct FfnParams {
   int stages;                                    // of a lone block
   FfnRows gate, up;                              // Up: written; Back: read
   FfnRows dgate, dup;                            // Back
-  const unsigned* peaks;                         // of dy, kFfnPeaks of them (fp16), or null
+  const unsigned* peaks;                         // kFfnWords of them (fp16), or null
+  unsigned* beyond;                              // the last of them, where it is still to be found (Back)
+  int again;                                     // Back: only if there is one
   uint32_t* flags;
 };
 
@@ -163,15 +170,36 @@ __device__ __forceinline__ void ffn_act_all(int act, const float2 (&g)[N], float
   }
 }
 
-// The power of two that dg and du are held with (fp16): dy's largest element comes to lie in [1/2, 1).
-__device__ __forceinline__ int ffn_exponent(const unsigned* peaks) {
+// The power of two that dg and du are held with (fp16).  `settled`: whether they are known to fit, or by how much they do not.
+__device__ __forceinline__ int ffn_exponent(const unsigned* peaks, bool settled) {
   const int lane = threadIdx.x & 31;
   unsigned top = 0;
   for (int k = lane; k < kFfnPeaks; k += 32) top = max(top, peaks[k]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-  const int e = static_cast<int>(top >> 23);      // of a finite positive fp32 value; fp16 has none below 2^-24
-  return e == 0 ? 0 : 126 - e;
+  int e = static_cast<int>(top >> 23);           // of a finite fp32 value that fp16 can have
+  e = e == 0 ? 0 : max(0, 126 - e);
+  if (settled && peaks[kFfnPeaks] != 0u) {       // down to the largest power that keeps it below kFfnBeyond, 2^15 (2 - 2^-11)
+    const unsigned beyond = peaks[kFfnPeaks];
+    e -= static_cast<int>(beyond >> 23) - (127 + 15) + ((beyond & 0x7fffffu) >= 0x7ff000u ? 1 : 0);
+  }
+  return e;
+}
+// The largest finite one of dg and du that does not fit.
+template <int N>
+__device__ __forceinline__ void ffn_note(const float2 (&v)[N], const float2 (&w)[N], unsigned* beyond) {
+  float top = 0.f;
+#pragma unroll
+  for (int e = 0; e < N; ++e) top = fmaxf(fmaxf(fmaxf(top, fabsf(v[e].x)), fmaxf(fabsf(v[e].y), fabsf(w[e].x))), fabsf(w[e].y));
+  if (top < kFfnBeyond) return;
+  top = 0.f;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    const float all[4] = {fabsf(v[e].x), fabsf(v[e].y), fabsf(w[e].x), fabsf(w[e].y)};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top = all[k] < INFINITY ? fmaxf(top, all[k]) : top;
+  }
+  if (top >= kFfnBeyond) atomicMax(beyond, __float_as_uint(top));
 }
 __device__ __forceinline__ float ffn_power(int e) { return __int_as_float((127 + e) << 23); }
 
@@ -292,6 +320,11 @@ __device__ __forceinline__ FfnSpot ffn_spot(const FfnParams& p, int t) {
 template <int KIND, bool BF16, int CG, bool STARVE = false>
 __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const __grid_constant__ FfnParams p) {
   extern __shared__ unsigned char smem_dyn[];
+  if (KIND == kFfnBack && !BF16 && p.again) {    // the same in all blocks
+    pdl_launch_dependents();
+    pdl_wait();
+    if (p.peaks[kFfnPeaks] == 0u) return;
+  }
   using T = FfnTiling<CG>;
   constexpr int kTM = 128 * CG, kTN = 128 * CG, kCols = KIND == kFfnUp ? kTN / 2 : kTN;      // of half a tile; kCols: columns of the result
   unsigned char* smem = smem_dyn + ((1024u - (smem_addr(smem_dyn) & 1023u)) & 1023u);
@@ -487,7 +520,7 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
     FfnWay way = {smem + (CG == 2 ? stages * T::kStage + 512 : 0u) + warp * 2 * kFfnPatch, 0};
     pdl_wait();
     int exponent = 0;
-    if (p.peaks != nullptr) exponent = ffn_exponent(p.peaks);
+    if (p.peaks != nullptr) exponent = ffn_exponent(p.peaks, KIND == kFfnPlain || p.again);
     bool ok = true;
     for (int t = worker; ok && t < p.tiles; t += workers) {
       const FfnSpot s = ffn_spot<CG>(p, t);
@@ -533,6 +566,7 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
                 if (KIND == kFfnUp) w[e] = make_float2(__uint_as_float(raw_up[16 * h + 2 * e]), __uint_as_float(raw_up[16 * h + 2 * e + 1]));
               }
               ffn_end<KIND, BF16, 16>(p.act, factor, v, w, gate + 2 * h, up + 2 * h, one + 2 * h, two + 2 * h, result + 2 * h);
+              if (KIND == kFfnBack && !BF16 && p.beyond != nullptr) ffn_note(v, w, p.beyond);
             }
             if (KIND == kFfnBack || (KIND == kFfnUp && p.gate.data != nullptr)) {
               way.put(one, &p.outs[0], row0, col);
@@ -571,7 +605,8 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
     const FfnSpot s = ffn_spot<CG>(p, worker);
     const FfnProblem& q = p.problem[s.problem];
     if (warp < 8 && !s_abort) {
-      const float factor = KIND == kFfnBack ? ffn_power(p.peaks == nullptr ? 0 : ffn_exponent(p.peaks)) : q.scaled ? ffn_power(p.peaks == nullptr ? 0 : -ffn_exponent(p.peaks)) : 1.f;
+      const int exponent = p.peaks == nullptr ? 0 : ffn_exponent(p.peaks, KIND == kFfnPlain || p.again);
+      const float factor = KIND == kFfnBack ? ffn_power(exponent) : q.scaled ? ffn_power(-exponent) : 1.f;
       // The blocks take the rows in turn.  First the sums, neighbouring lanes at neighbouring 16 bytes of the other blocks' memory and all blocks' under way at once, into this
       // block's own place for them, which nobody else reads (8 columns a lane straight into the ending took 9,000 to 12,000 cycles for 16 rows).
       float* mine = reinterpret_cast<float*>(smem);
@@ -609,6 +644,7 @@ __global__ void __launch_bounds__(kFfnThreads, CG == 2 ? 1 : 2) ffn_kernel(const
           w[e] = KIND == kFfnUp ? *reinterpret_cast<const float2*>(at + kCols + 2 * e) : make_float2(0.f, 0.f);
         }
         ffn_end<KIND, BF16, 8>(p.act, factor, v, w, &gate, &up, &one, &two, &result);
+        if (KIND == kFfnBack && !BF16 && p.beyond != nullptr) ffn_note(v, w, p.beyond);
         if (KIND == kFfnBack || (KIND == kFfnUp && p.gate.data != nullptr)) {
           *ffn_at(KIND == kFfnUp ? p.gate : p.dgate, row, col) = one;
           *ffn_at(KIND == kFfnUp ? p.up : p.dup, row, col) = two;
@@ -748,7 +784,7 @@ __global__ void __launch_bounds__(32 * kFfnFewWarps) ffn_few_kernel(const FfnFew
   }
 }
 
-// fp16: the largest finite |element| of dy, as the bits of its fp32 value, one for each block.
+// fp16: the largest finite |element| of dy, as the bits of its fp32 value, one for each block; the word behind them is cleared.
 __global__ void __launch_bounds__(256) ffn_peak_kernel(const void* dy, long long pitch, int rows, int cols, unsigned* peaks) {
   __shared__ unsigned s_top[8];
   pdl_launch_dependents();
@@ -772,6 +808,7 @@ __global__ void __launch_bounds__(256) ffn_peak_kernel(const void* dy, long long
   if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;
   __syncthreads();
   if (threadIdx.x == 0) {
+    if (blockIdx.x == 0) peaks[kFfnPeaks] = 0u;
     for (int w = 1; w < 8; ++w) top = max(top, s_top[w]);
     peaks[blockIdx.x] = __float_as_uint(__half2float(__ushort_as_half(static_cast<unsigned short>(top))));
   }

@@ -122,7 +122,8 @@ def feedforward_backward(dout, x, w_gate, w_up, w_down, gate, up, *, act: str = 
                          workspace=None, stream=None):
     """(dx, dw_gate, dw_up, dw_down) of feedforward_forward with the same act, from its gate and up and the gradient dout.
     want: which of the four are made; the others are None.  They are made here unless given, as is the workspace (a uint8 tensor of workspace_bytes,
-    16-byte aligned).  Between the products gradients are held in the tensors' type (float16: scaled by a power of two from dout's largest element)."""
+    16-byte aligned).  Between the products gradients are held in the tensors' type (float16: times a power of two where dout is small or they would be
+    infinite)."""
     want = tuple(bool(w) for w in want)
     given = (dx, dw_gate, dw_up, dw_down)
     sig = (layout(dout), layout(x), layout(w_gate), layout(w_up), layout(w_down), layout(gate), layout(up), act, want, *(layout(t) for t in given))
