@@ -21,7 +21,8 @@ namespace adacons {
 // them, when there are few tokens: the blocks of a cluster join their maxima and sums in a fixed order through one another's shared memory)
 // with one running maximum and sum a thread, 32 elements between two looks at the maximum.  Both sums need an exponential
 // of every logit where tau is not one, and the exponential unit would then be the limit (16 a cycle and SM against 12 bf16 logits
-// that memory brings): for tau = 2, 3 and 4 the second is a power of the first, exp(z) = exp(z / tau)^tau.
+// that memory brings): for tau = 2, 3 and 4 the second is a power of the first, exp(z) = exp(z / tau)^tau (backward: of exp((z - L1) / tau), so that small probabilities are not lost
+// on the way).
 // ----------------------------------------------------------------------------------------------
 constexpr int kDistillMaxK = 1024;
 constexpr float kDistillLow = -3.402823466e38f;
@@ -415,15 +416,17 @@ __global__ void __launch_bounds__(512, 2) distill_backward_kernel(const DistillP
     if (label >= begin && label < end) s_z[p.top] = V::one(z + label);
   }
   __syncthreads();
-  // exp(z - L1) = exp(z / tau - L)^tau exp(tau L - L1)
+  // Powers: exp(z - L1) = exp(z / tau - L1 / tau)^tau, which leaves fp32 no sooner than it does itself, and exp(z / tau - L) = exp(z / tau - L1 / tau) exp(L1 / tau - L), whose last
+  // factor lies between V^(1 / tau - 1) and 1.
   const float L = p.rows[row], L1 = p.rows[p.tokens + row];
-  const float with = MODE == 0 ? soft + hard : soft;
-  const float by_power = MODE > 1 ? hard * expf(p.tau * L - L1) : 0.f;
+  const bool powers = MODE > 1 && label >= 0;
+  const float from = powers ? L1 * inv_tau : L;
+  const float with = MODE == 0 ? soft + hard : powers ? soft * expf(from - L) : soft;
   auto gradient = [&](float v) {
-    const float e = distill_ex2(fmaf(v, inv_tau, -L) * kDistillLog2e);
+    const float e = distill_ex2(fmaf(v, inv_tau, -from) * kDistillLog2e);
     if (MODE == 0) return with * e;
     if (MODE == 1) return fmaf(hard, distill_ex2((v - L1) * kDistillLog2e), with * e);
-    return fmaf(by_power, distill_power<MODE>(e), with * e);
+    return fmaf(hard, distill_power<MODE>(e), with * e);
   };
   if (p.vectors) {
     const DistillSpan<T> span(z, begin, end);
