@@ -124,7 +124,7 @@ def distill_forward(logits, ids, teacher, *, temperature: float = 1.0, labels=No
 
 def distill_backward(dloss, logits, ids, teacher, rows, *, temperature: float = 1.0, labels=None, mix=None, out=None, stream=None):
     """The gradient of distill_forward's logits, of their type, from dloss (fp32, one for each token) and the forward pass's rows, with the same arguments.
-    out: a new tensor unless given; logits itself is allowed (they are overwritten), no other overlap."""
+    out: a new tensor unless given, whose rows lie as the logits' do relative to 16 bytes; logits itself is allowed (they are overwritten), no other overlap."""
     temperature, mix = float(temperature), _mix(labels, mix)
     sig = (layout(dloss), layout(logits), layout(ids), layout(teacher), layout(rows), layout(labels), temperature, mix, layout(out))
     plan = _back_plans.known.get(sig)
@@ -138,10 +138,16 @@ def distill_backward(dloss, logits, ids, teacher, rows, *, temperature: float = 
     if out is not None and (starts_with(out, (dloss, ids, teacher, rows, labels)) or (starts_with(out, (logits,)) and out.stride() != logits.stride())):
         raise ValueError("out may be the logits, otherwise it must not share memory with what is read")
     if out is None:
-        # rows that lie as the logits' do relative to 16 bytes, so that both are moved in vectors; padding behind them is not written
-        V = logits.shape[1]
-        pad = (logits.stride(0) - V) % (16 // logits.element_size()) if logits.shape[0] > 1 else 0
-        out = logits.new_empty((logits.shape[0], V + pad))[:, :V]
+        # it lies as the logits do relative to 16 bytes, so that both are moved in vectors (one by one they take five times as long): as far behind the first boundary, rows
+        # as far apart.  What lies between the rows is not written.
+        T, V = logits.shape
+        unit = 16 // logits.element_size()
+        pad = (logits.stride(0) - V) % unit if T > 1 else 0
+        lead = logits.data_ptr() % 16 // logits.element_size()
+        if lead:
+            out = torch.as_strided(logits.new_empty(lead + T * (V + pad)), (T, V), (V + pad, 1), lead)
+        else:
+            out = logits.new_empty((T, V + pad))[:, :V]
     if plan is None:
         plan = _back_plans.remember(sig, _Plan(logits, ids, teacher, labels, temperature, mix, (logits, ids, teacher, out)))
     for b, t in zip(plan.blocks, (logits, ids, teacher, out)):
