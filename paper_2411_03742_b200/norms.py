@@ -270,18 +270,21 @@ def residual_norm_backward(dout, dnormed, out, f, rows, *, gate=None, gate_by=No
 
 def residual_norm(x, f=None, *, gate=None, gate_by=None, post=None, scale: float = 1.0, pre=None, eps: float = 1e-6, dtype=None):
     """(out, normed) of residual_norm_forward as functions of x, f, the gate and the gains that can be differentiated once.  Not of the
-    scale: a learned one belongs into the gate.  normed is None without `pre`."""
+    scale: a learned one belongs into the gate.  normed is None without `pre`.  What does not lie as the passes want it, along rows (transposed, broadcast), is copied."""
     if getattr(scale, "requires_grad", False):
         raise ValueError("the residual addition has no gradient for its scale: make it a gate")
-    out, normed = _Residual.apply(x, f, gate, post, pre, gate_by, float(scale), float(eps), dtype)
+    out, normed = _Residual.apply(*(_along(t) for t in (x, f, gate, post, pre)), gate_by, float(scale), float(eps), dtype)
     return (x if f is None else out), normed
+
+
+def _along(t):
+    """t, or a copy of it where its last dimension has not unit stride."""
+    return t if t is None or t.dim() == 0 or t.shape[-1] <= 1 or t.stride(-1) == 1 else t.contiguous()
 
 
 class _Residual(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, f, gate, post, pre, gate_by, scale, eps, dtype):
-        gains = [None if t is None or t.is_contiguous() else t.contiguous() for t in (post, pre)]
-        post, pre = (t if g is None else g for t, g in zip((post, pre), gains))
         out, normed, rows = residual_norm_forward(x, f, gate=gate, gate_by=gate_by, post=post, scale=scale, pre=pre, eps=eps, dtype=dtype)
         ctx.set_materialize_grads(False)
         ctx.save_for_backward(out, f, rows, gate, post, pre)
@@ -291,11 +294,10 @@ class _Residual(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dout, dnormed):
         out, f, rows, gate, post, pre = ctx.saved_tensors
-        args = [t if t is None or t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous() for t in (dout, dnormed)]
         compute = _Gradient.apply if torch.is_grad_enabled() else _Gradient.compute
         if dout is None and dnormed is None:
             return (None,) * 9
-        dx, df, dgate, dpost, dpre = compute(*args, out.detach(), f, rows, gate, post, pre, ctx.how)
+        dx, df, dgate, dpost, dpre = compute(_along(dout), _along(dnormed), out.detach(), f, rows, gate, post, pre, ctx.how)
         return dx, df, dgate, dpost, dpre, None, None, None, None
 
 
