@@ -176,9 +176,12 @@ def selftest_bounded_wait(x, w_gate, w_up, paired: bool) -> None:
 
 
 def gated_feedforward(x, w_gate, w_up, w_down, act: str = "silu"):
-    """feedforward_forward's out as a function of x, of any leading dimensions, and the weights that can be differentiated once."""
+    """feedforward_forward's out as a function of x, of any leading dimensions, and the weights that can be differentiated once.  Where no gradient is
+    recorded, gate and up are not made."""
     rows = _aligned(x.reshape(-1, x.shape[-1]))
-    return _FeedForward.apply(rows, *(_aligned(w) for w in (w_gate, w_up, w_down)), act).view(*x.shape[:-1], w_down.shape[0])
+    # asked here: inside a Function's forward gradients are off, and what its inputs need is told whether or not they were on
+    keep = torch.is_grad_enabled() and any(t.requires_grad for t in (x, w_gate, w_up, w_down))
+    return _FeedForward.apply(rows, *(_aligned(w) for w in (w_gate, w_up, w_down)), act, keep).view(*x.shape[:-1], w_down.shape[0])
 
 
 def _aligned(t):
@@ -190,8 +193,7 @@ def _aligned(t):
 
 class _FeedForward(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w_gate, w_up, w_down, act):
-        keep = any(ctx.needs_input_grad)
+    def forward(ctx, x, w_gate, w_up, w_down, act, keep):
         out, gate, up = feedforward_forward(x, w_gate, w_up, w_down, act=act, keep=keep)
         if keep:
             ctx.save_for_backward(x, w_gate, w_up, w_down, gate, up)
@@ -202,7 +204,7 @@ class _FeedForward(torch.autograd.Function):
     def backward(ctx, dout):
         x, w_gate, w_up, w_down, gate, up = ctx.saved_tensors
         compute = _Gradient.apply if torch.is_grad_enabled() else _Gradient.compute
-        return (*compute(_aligned(dout), x, w_gate, w_up, w_down, gate, up, ctx.act, tuple(ctx.needs_input_grad[:4])), None)
+        return (*compute(_aligned(dout), x, w_gate, w_up, w_down, gate, up, ctx.act, tuple(ctx.needs_input_grad[:4])), None, None)
 
 
 class _Gradient(torch.autograd.Function):

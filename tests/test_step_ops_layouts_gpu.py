@@ -59,3 +59,26 @@ def test_norms_take_one_gate_value_a_token():
         dout = randn(3, 20, 72, seed=5, dtype=torch.float32)
         (a,), (b,) = (torch.autograd.grad(o, g, dout) for o, g in zip(outs, (gate, wide)))
         assert a.shape == shape and torch.equal(a, b.sum(-1, keepdim=True))
+
+
+def test_inference_keeps_nothing():
+    """Without gradients neither gate nor up is made, whether or not the weights are parameters."""
+    from paper_2411_03742_b200 import gated_feedforward
+    T, D, F = 4096, 64, 2048
+    x, wg, wu, wd = randn(T, D), randn(F, D, seed=1), randn(F, D, seed=2), randn(D, F, seed=3)
+    want = gated_feedforward(x, wg, wu, wd)
+    weights = [torch.nn.Parameter(w) for w in (wg, wu, wd)]
+    for mode in (torch.no_grad, torch.inference_mode):
+        with mode():
+            torch.cuda.synchronize()
+            torch.cuda.reset_peak_memory_stats()
+            before = torch.cuda.memory_allocated()
+            got = gated_feedforward(x, *weights)
+            used = torch.cuda.max_memory_allocated() - before
+        assert torch.equal(got, want) and not got.requires_grad
+        # the result and one matrix (token, hidden) of working memory, and the allocator's rounding
+        assert used <= 2 * T * D + 2 * T * F + (1 << 21), used
+    y = gated_feedforward(x, *weights)
+    assert y.requires_grad and torch.equal(y, want)
+    y.sum().backward()
+    assert all(w.grad is not None for w in weights)
