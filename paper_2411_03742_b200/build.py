@@ -17,7 +17,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG_DIR, "libadacons_b200.so")
 OBJ_DIR = os.path.join(PKG_DIR, "_build")
 _COMMON = ["csrc/adacons_common.cuh", "include/adacons.h"]
-_OPS = _COMMON + ["csrc/adacons_tc.cuh", "csrc/adacons_host.cuh", "include/adacons_ops.h"]
+_OPS = _COMMON + ["csrc/adacons_tc.cuh", "csrc/adacons_host.cuh", "csrc/adacons_status.cuh", "include/adacons_ops.h"]
 # translation units and what each includes
 SOURCES = {
     "adacons.cu": _COMMON + ["csrc/" + f for f in ("adacons_kernels.cuh", "adacons_pass1.cuh", "adacons_coeff.cuh", "adacons_pass2.cuh",

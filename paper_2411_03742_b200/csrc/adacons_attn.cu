@@ -313,13 +313,7 @@ int adacons_attn_get_status(uint32_t* flags, void* cuda_stream) {
   AttnDevice* d = nullptr;
   const int rc = attn_device(&d);
   if (rc != ADACONS_OK) return rc;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (cudaMemcpyAsync(flags, d->flags, sizeof(uint32_t), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
-      cudaMemsetAsync(d->flags, 0, sizeof(uint32_t), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
-    cudaGetLastError();
-    return ADACONS_ECUDA;
-  }
-  return ADACONS_OK;
+  return take_status(d->flags, flags, static_cast<cudaStream_t>(cuda_stream));
 }
 
 }  // extern "C"

@@ -444,13 +444,7 @@ int adacons_ffn_get_status(uint32_t* flags, void* cuda_stream) {
   FfnDevice* d = nullptr;
   const int rc = ffn_device(&d);
   if (rc != ADACONS_OK) return rc;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (cudaMemcpyAsync(flags, d->flags, sizeof(uint32_t), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
-      cudaMemsetAsync(d->flags, 0, sizeof(uint32_t), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
-    cudaGetLastError();
-    return ADACONS_ECUDA;
-  }
-  return ADACONS_OK;
+  return take_status(d->flags, flags, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int adacons_selftest_ffn(const adacons_ffn_shape* s, int paired, const adacons_ffn_matrix* x, const adacons_ffn_matrix* wg, const adacons_ffn_matrix* wu, void* workspace,

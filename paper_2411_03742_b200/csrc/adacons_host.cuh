@@ -9,6 +9,7 @@
 
 #include "adacons.h"
 #include "adacons_common.cuh"
+#include "adacons_status.cuh"
 
 namespace adacons {
 

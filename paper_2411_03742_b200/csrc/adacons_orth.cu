@@ -520,13 +520,7 @@ int adacons_orth_get_status(adacons_orth* c, uint32_t* flags, void* cuda_stream)
   if (c == nullptr || flags == nullptr) return ADACONS_EINVAL;
   DeviceGuard guard(c->dev.device);
   if (!guard.ok) return ADACONS_ECUDA;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (cudaMemcpyAsync(flags, c->params.flags, sizeof(uint32_t), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
-      cudaMemsetAsync(c->params.flags, 0, sizeof(uint32_t), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
-    cudaGetLastError();
-    return ADACONS_ECUDA;
-  }
-  return ADACONS_OK;
+  return take_status(c->params.flags, flags, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int adacons_orth_get_info(adacons_orth* c, int key, int64_t* value) {

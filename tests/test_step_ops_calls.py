@@ -23,3 +23,38 @@ def test_gate_and_up_are_kept_where_a_gradient_is_recorded(monkeypatch, mode, pa
         y = feedforward.gated_feedforward(x, *w)
     recorded = parameters and mode is torch.enable_grad
     assert asked == [recorded] and y.requires_grad == recorded and y.shape == x.shape
+
+
+STATUS = r"""
+#include <cstdio>
+#include "adacons_status.cuh"
+static uint32_t word, late;      // `late`: what a kernel of another stream sets between the call's first step and its next
+static void between() { word |= late; late = 0; }
+cudaError_t cudaMemcpyAsync(void* to, const void* from, size_t, cudaMemcpyKind, cudaStream_t) { *static_cast<uint32_t*>(to) = *static_cast<const uint32_t*>(from); between(); return cudaSuccess; }
+cudaError_t cudaMemsetAsync(void* to, int, size_t, cudaStream_t) { *static_cast<uint32_t*>(to) = 0; return cudaSuccess; }
+cudaError_t cudaStreamSynchronize(cudaStream_t) { return cudaSuccess; }
+cudaError_t cudaGetLastError() { return cudaSuccess; }
+static void look() { uint32_t v = 9; const int rc = adacons::take_status(&word, &v, nullptr); std::printf("%d %x\n", rc, v); }
+int main() {
+  look();
+  word = 0x100; look(); look();
+  late = 0x100; look(); look(); look();
+  word = late = 0x100; look(); look();
+}
+"""
+
+
+def test_a_status_set_behind_the_look_is_told_by_the_next(tmp_path):
+    """The reading of a status word against a runtime of its own, in which another stream's kernel comes between two steps."""
+    import os
+    import shutil
+    import subprocess
+    if shutil.which("g++") is None:
+        pytest.skip("no C++ compiler")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    (tmp_path / "status.cpp").write_text(STATUS)
+    home = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    subprocess.run(["g++", "-std=c++17", "-I", os.path.join(root, "paper_2411_03742_b200", "csrc"), "-I", os.path.join(root, "include"), "-I", os.path.join(home, "include"),
+                    "-o", str(tmp_path / "status"), str(tmp_path / "status.cpp")], check=True)
+    told = subprocess.run([str(tmp_path / "status")], check=True, capture_output=True, text=True).stdout.split("\n")[:-1]
+    assert told == ["0 0", "0 100", "0 0", "0 0", "0 100", "0 0", "0 100", "0 0"]

@@ -82,3 +82,20 @@ def test_inference_keeps_nothing():
     assert y.requires_grad and torch.equal(y, want)
     y.sum().backward()
     assert all(w.grad is not None for w in weights)
+
+
+def test_status_words_are_read_by_one_caller():
+    """A wait that expires while another stream looks at the status again and again is told once, to whoever looks next."""
+    from paper_2411_03742_b200 import feedforward
+    x, w = randn(100, 128), randn(64, 128, seed=1)
+    assert feedforward.status() == 0
+    work, side = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(work):
+        feedforward.selftest_bounded_wait(x, w, w, False)
+    seen = []
+    while not work.query():
+        seen.append(feedforward.status(side))
+    work.synchronize()
+    seen.append(feedforward.status(side))
+    assert [v for v in seen if v] == [0x100] and feedforward.status() == 0
