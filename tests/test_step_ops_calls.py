@@ -58,3 +58,40 @@ def test_a_status_set_behind_the_look_is_told_by_the_next(tmp_path):
                     "-o", str(tmp_path / "status"), str(tmp_path / "status.cpp")], check=True)
     told = subprocess.run([str(tmp_path / "status")], check=True, capture_output=True, text=True).stdout.split("\n")[:-1]
     assert told == ["0 0", "0 100", "0 0", "0 0", "0 100", "0 0", "0 100", "0 0"]
+
+
+def movable_loads(text):
+    """The asm statements without `volatile` that load, whichever of their instructions it is."""
+    import re
+    found = []
+    for start in re.finditer(r"\b(?:asm|__asm__|__asm)\b\s*(\w*)\s*\(", text):
+        at, depth = start.end(), 1
+        while depth:
+            if text[at] == '"':                        # to the end of the literal
+                at = re.compile(r'"(?:[^"\\]|\\.)*"').match(text, at).end()
+                continue
+            depth += {"(": 1, ")": -1}.get(text[at], 0)
+            at += 1
+        if not start[1].strip("_").startswith("volatile") and re.search(r"\b(ld|ldu|ldmatrix|multimem|atom|red)\b", text[start.start():at]):
+            found.append(text[start.start():at])
+    return found
+
+
+def test_loads_stay_behind_their_guards_whatever_comes_before_them():
+    """A load in an asm statement without `volatile` may be moved in front of the branch that guards it; it need not be the statement's first instruction."""
+    import os
+    positive = ['asm("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p));', 'asm ("{ .reg .pred q; setp.ne.u32 q, %2, 0;" "@q ld.global.u32 %0, [%1]; }" : "=r"(v) : "l"(p), "r"(f(x)));',
+                '__asm__("mov.u32 %0, 1; \\"; ld.global.u32 %0, [%1];" : "=r"(v) : "l"(p));']
+    for text in positive:
+        assert movable_loads(f"int a(int);\n{text}\nreturn;") == [text[:-1]], text
+        for word in ("volatile", "__volatile__"):
+            assert movable_loads(text.replace("(", f" {word}(", 1)) == []
+    assert movable_loads('asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));') == []
+    folder = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2411_03742_b200", "csrc")
+    seen = 0
+    for name in sorted(os.listdir(folder)):
+        if name.endswith((".cu", ".cuh")):
+            text = open(os.path.join(folder, name)).read()
+            assert movable_loads(text) == [], name
+            seen += text.count("asm")
+    assert seen > 50
