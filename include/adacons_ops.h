@@ -214,7 +214,7 @@ int adacons_norm_backward(const adacons_norm_shape *shape, const adacons_norm_ro
  * An entry is there when its index lies in 0 .. vocab-1 (any other says that it is not) and its logit is not -inf.  A token without
  * entries has no first term, one without a label in 0 .. vocab-1 no second; one without either has loss 0 and a gradient of zeros, and its
  * logits are not read.  The same index may come several times: each time counts.  Logits of -inf have probability 0.
- * Exponentials are fp32 and those below 2^-126 count as 0; gradients of bf16 and fp32 logits that small are 0 then.
+ * Exponentials are fp32, good to 2^-21 (8 + |z / tau| + |L|) of themselves, and those below 2^-126 count as 0; gradients of bf16 and fp32 logits that small are 0 then.
  */
 typedef struct adacons_distill_matrix {   /* (token, column): stride in elements, any value; not looked at for one token.  Columns are 1 apart. */
   void *data;
@@ -229,7 +229,7 @@ typedef struct adacons_distill_shape {
   int tokens;             /* 0 .. 2^27 */
   int vocab;              /* 1 .. 2^30 */
   int top;                /* 1 .. 1024 */
-  float temperature;      /* tau > 0 */
+  float temperature;      /* tau: 2^-60 .. 2^60 */
   float mix;              /* 0 .. 1 */
 } adacons_distill_shape;
 

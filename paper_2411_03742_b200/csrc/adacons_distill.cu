@@ -18,7 +18,8 @@ int check_shape(const adacons_distill_shape* s) {
   if (s == nullptr || !known(s->dtype) || !known(s->teacher_dtype)) return ADACONS_EINVAL;
   if ((s->ids_bits != 32 && s->ids_bits != 64) || (s->labels_bits != 0 && s->labels_bits != 32 && s->labels_bits != 64)) return ADACONS_EINVAL;
   if (s->tokens < 0 || s->vocab < 1 || s->top < 1) return ADACONS_EINVAL;
-  if (!(s->temperature > 0.f) || !std::isfinite(s->temperature) || !(s->mix >= 0.f && s->mix <= 1.f)) return ADACONS_EINVAL;
+  // 1 / tau and tau^2 stay in fp32's range
+  if (!(s->temperature >= 0x1p-60f && s->temperature <= 0x1p60f) || !(s->mix >= 0.f && s->mix <= 1.f)) return ADACONS_EINVAL;
   if (s->top > kDistillMaxK || s->vocab > (1 << 30) || s->tokens > (1 << 27)) return ADACONS_ELIMIT;
   return ADACONS_OK;
 }

@@ -8,7 +8,6 @@ differentiable torch operation.  Argument marshalling only: the arithmetic runs 
 from __future__ import annotations
 
 import ctypes
-import math
 
 import torch
 
@@ -58,8 +57,8 @@ def check_distill(logits, ids, teacher, temperature: float, labels=None, mix: fl
         raise ValueError("ids and labels are int32 or int64")
     if tuple(ids.shape) != (T, K) or tuple(teacher.shape) != (T, K):
         raise ValueError(f"ids {tuple(ids.shape)} and teacher {tuple(teacher.shape)} do not fit logits {tuple(logits.shape)}")
-    if not (temperature > 0 and math.isfinite(temperature)):
-        raise ValueError("temperature must be positive")
+    if not 2.0 ** -60 <= temperature <= 2.0 ** 60:
+        raise ValueError(f"temperature must lie between 2^-60 and 2^60, got {temperature}")
     if not 0 <= mix <= 1:
         raise ValueError("mix lies between 0 and 1")
     if out is not None and (out.dtype != logits.dtype or out.shape != logits.shape):

@@ -95,3 +95,22 @@ def test_loads_stay_behind_their_guards_whatever_comes_before_them():
             assert movable_loads(text) == [], name
             seen += text.count("asm")
     assert seen > 50
+
+
+@pytest.mark.parametrize("temperature", [1e-45, 1e-39, 1e-25, 2.0 ** -61, 2.0 ** 61, 1e30, 3e38])
+def test_temperatures_whose_square_or_reciprocal_leave_the_range_are_refused(temperature):
+    """tau^2 or 1 / tau would be 0 or infinite in fp32, and the loss 0, infinite or not a number."""
+    import ctypes
+    from paper_2411_03742_b200 import binding
+    from paper_2411_03742_b200.distillation import _Matrix, _Shape, check_distill
+    z, ids, top = torch.zeros(4, 50), torch.zeros(4, 5, dtype=torch.int64), torch.zeros(4, 5)
+    with pytest.raises(ValueError, match="temperature"):
+        check_distill(z, ids, top, temperature, want_cuda=False)
+    lib, r = binding.load_library(), ctypes.byref
+    # no tokens: nothing is launched
+    for tau, code in ((temperature, 1), (2.0 ** -60, 0), (2.0 ** 60, 0)):
+        s, m = _Shape(1, 0, 64, 0, 0, 100, 5, tau, 1.0), [_Matrix(None, 128) for _ in range(4)]
+        assert lib.adacons_distill_forward(r(s), r(m[0]), r(m[1]), r(m[2]), None, None, None, None) == code
+        assert lib.adacons_distill_backward(r(s), None, 1, r(m[0]), r(m[1]), r(m[2]), None, None, r(m[3]), None) == code
+        if code == 0:
+            check_distill(z, ids, top, tau, want_cuda=False)
